@@ -376,6 +376,92 @@ int cngp_mlp_bwd(const cngp_mlp_config *cfg, const void *y, int64_t N, const voi
 int cngp_adam_step(const cngp_adam *opt, int64_t n, float *master, void *half_copy, float *m, float *v,
                    float *grad, int clear_grad, void *stream);
 
+/* Gated linear recurrence over the rows of ragged or equal sequences, forward and backward.  With it the decoded samples of a
+ * ray become the pixel of the ray (the paper's radiance fields are trained on pixels): colour c and optical depth t of a sample
+ * composite as h <- exp(-t) h + (1 - exp(-t)) c from the farthest sample to the nearest, h starting as the background.
+ *     a_t = gate_t, or exp(gate_t) with CNGP_RECUR_LOG_GATE          v_t = x_t, or (1 - a_t) x_t with CNGP_RECUR_MIX
+ *     h_t = a_t h_{t-1} + v_t     within a sequence, from its first row to its last, or from the last to the first with
+ *                                 CNGP_RECUR_REVERSE; the state before the first row taken is h0 of the sequence, or 0
+ * gate_channels == channels: every channel has a gate of its own; gate_channels == 1: one gate per row for all channels.
+ * Arithmetic and states in fp32, one rounding to the storage type at the end.  Long sequences are cut and their pieces joined:
+ * meant for |a| <= 1; larger gates work while the product of a piece's gates stays within fp32 (a state that grows past it is
+ * not finite, then or later).  A state that is not finite stays in its sequence and channel.
+ * Sequences: rows [offsets[s], offsets[s + 1]) of the N rows, offsets dev int32 [sequences + 1], non-decreasing within 0 .. N
+ * (entries outside are taken as the nearest of the two; with entries that decrease the results are unspecified, but no array is
+ * left).  Rows before the first sequence and behind the last one are neither used nor written.
+ * offsets NULL: N / sequences rows each, which must divide.  A sequence without rows passes its state on (last = h0, dh0 = dlast).
+ *   channels  1 .. 65536       N, sequences  below 2^31       gate dev gate_dtype [N, gate_channels]      x dev io_dtype [N, channels]
+ *   h0    dev float32 [sequences, channels], or NULL (zeros)
+ *   y     dev io_dtype [N, channels], every row's state, written; or NULL
+ *   last  dev float32 [sequences, channels], the state after the last row taken, written; or NULL; may be h0 itself.
+ * One token each for many running sequences is N == sequences with offsets NULL.
+ * Backward, for L = sum(y * dy) + sum(last * dlast) (dy io_dtype [N, channels], dlast float32; either may be NULL, not both):
+ *   dgate dev gate_dtype [N, gate_channels], dx dev io_dtype [N, channels], written; dh0 dev float32 [sequences, channels], written,
+ *   or NULL; may be dlast itself.  y: the forward's states if they were kept; with NULL they are computed again, in fp32, into
+ *   the workspace.  Sums over channels are formed in a fixed order: the same call gives the same bits.
+ * `longest` (host): no sequence has more rows than this; 0: unknown.  It only decides how the work is cut.
+ * Workspace: cngp_recur_workspace_bytes(cfg, N, sequences, call) bytes, 256-byte aligned (may be 0), for call = the sum of
+ * CNGP_RECUR_CALL_*; undefined before and after.  Other arrays must not overlap. */
+enum { CNGP_RECUR_REVERSE = 1u, CNGP_RECUR_LOG_GATE = 2u, CNGP_RECUR_MIX = 4u };
+enum { CNGP_RECUR_CALL_BWD = 1u,      /* cngp_recur_bwd, else cngp_recur_fwd */
+       CNGP_RECUR_CALL_RAGGED = 2u,   /* offsets are given                  */
+       CNGP_RECUR_CALL_NO_Y = 4u };   /* backward without y                 */
+typedef struct cngp_recur_config {
+    int32_t  channels, gate_channels;
+    int32_t  io_dtype;        /* cngp_dtype of x, y and their gradients */
+    int32_t  gate_dtype;      /* cngp_dtype of gate and its gradient    */
+    int32_t  longest;
+    uint32_t flags;           /* CNGP_RECUR_*                           */
+} cngp_recur_config;
+size_t cngp_recur_workspace_bytes(const cngp_recur_config *cfg, int64_t N, int64_t sequences, uint32_t call);
+int cngp_recur_fwd(const cngp_recur_config *cfg, const void *gate, const void *x, int64_t N, const int32_t *offsets, int64_t sequences,
+                   const float *h0, void *y, float *last, void *workspace, size_t workspace_bytes, void *stream);
+int cngp_recur_bwd(const cngp_recur_config *cfg, const void *gate, const void *x, int64_t N, const int32_t *offsets, int64_t sequences,
+                   const float *h0, const void *y, const void *dy, const float *dlast, void *dgate, void *dx, float *dh0,
+                   void *workspace, size_t workspace_bytes, void *stream);
+
+/* Lookup of codes with scaling, and its gradient: a row per image, object or token, chosen by an id per point, alone or added to
+ * the point's encoding (a field conditioned on the image it is seen in, several shapes in one field).
+ *     y[n] = base[n] + scale * table[ids[n]]           grad_table[r] += scale * sum over n with ids[n] == r of dy[n]
+ * in fp32, one rounding to io_dtype.  An id below 0 or not below `rows` is padding: y[n] = base[n] (0 without base), no gradient.
+ * The gradient sorts the ids (the library's own stable radix sort) and adds up the rows of an id in an order that depends on the
+ * ids alone: no floating-point atomics, the same call gives the same bits.  The gradient of base is dy.
+ *   rows 1 .. 2^31 - 2    dim 1 .. 65536    N below 2^31    scale finite
+ *   ids  dev id_dtype [N]       table dev table_dtype [rows, dim]       base dev io_dtype [N, dim], may be y itself; or NULL
+ *   y    dev io_dtype [N, dim], written            dy dev io_dtype [N, dim]
+ *   grad_table dev float32 [rows, dim], accumulated (+=), or cleared first with CNGP_ZERO_GRADS (also when N == 0)
+ *   workspace  dev, 256-byte aligned, cngp_embed_workspace_bytes(cfg, N) bytes (0 for N == 0); undefined before and after */
+typedef enum { CNGP_I32 = 0, CNGP_I64 = 1 } cngp_id_dtype;
+typedef struct cngp_embed_config {
+    int64_t  rows;
+    int32_t  dim;
+    int32_t  table_dtype, io_dtype;   /* cngp_dtype    */
+    int32_t  id_dtype;                /* cngp_id_dtype */
+    float    scale;
+    uint32_t flags;                   /* CNGP_ZERO_GRADS: cngp_embed_bwd clears grad_table before accumulating */
+} cngp_embed_config;
+size_t cngp_embed_workspace_bytes(const cngp_embed_config *cfg, int64_t N);
+int cngp_embed_fwd(const cngp_embed_config *cfg, const void *ids, int64_t N, const void *table, const void *base, void *y, void *stream);
+int cngp_embed_bwd(const cngp_embed_config *cfg, const void *ids, int64_t N, const void *dy, float *grad_table,
+                   void *workspace, size_t workspace_bytes, void *stream);
+
+/* Balance of the probing candidates: how often the bake picks each of the N_p candidates of a level, and a loss that is lowest
+ * (1) where the picks and the softmax weights of the rows spread evenly, with its gradient.  Not part of the paper's method: a probing
+ * range whose rows all pick the same candidate leaves the others' features unused.  Over the counted rows r of level l (W_l of them),
+ * sigma = the weights of the backward pass (softmax of the row; with cfg->top_k over the largest only):
+ *     counts[l][k] = rows whose winner (rule of cngp_bake_probes) is k       f_k = counts[l][k] / W_l       P_k = sum_r sigma_rk / W_l
+ *     loss[l] = N_p sum_k f_k P_k
+ *     grad_Dhat_c[l][r][k] += weight * d loss[l] / d Dhat_c[l][r][k] = weight * N_p / W_l * sigma_rk (f_k - sum_j f_j sigma_rj)
+ * (counts and the kept set are constants of the differentiation).  A level without counted rows: counts, loss and gradient 0.
+ *   Dhat_c dev float32 [L, N_c, N_p]       rows dev uint8 [L, N_c], 0 = not counted, whatever the row holds; or NULL: all are
+ *   loss   dev float32 [L], written        counts dev int32 [L, N_p], written
+ *   grad_Dhat_c dev float32 [L, N_c, N_p], accumulated, or written with CNGP_ZERO_GRADS (0 in rows that are not counted); or NULL
+ *   weight finite, host.  Sums are formed in a fixed order.
+ *   workspace dev, 256-byte aligned, cngp_probe_balance_workspace_bytes(cfg) bytes; undefined before and after */
+size_t cngp_probe_balance_workspace_bytes(const cngp_config *cfg);
+int cngp_probe_balance(const cngp_config *cfg, const float *Dhat_c, const uint8_t *rows, float weight, float *loss, int32_t *counts,
+                       float *grad_Dhat_c, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Index dump for parity checks: for every (point, level, corner) the integers of Eq. 6.
  * All outputs dev, shape [N, L, 2^d]; any of them may be NULL.
  *   base      (N_p * hash(v)) mod N_f        h2        hash2(v) mod N_c

@@ -630,3 +630,7 @@ def pack4(D_c_u8):
     """Repack a [L, N_c] uint8 index codebook into the two-entries-per-byte layout (entry 2i in
     the low nibble of byte i).  Pure data movement on whatever device the tensor lives on."""
     return (D_c_u8[..., 0::2] | (D_c_u8[..., 1::2] << 4)).contiguous()
+
+
+from .operators import (I32, I64, RECUR_LOG_GATE, RECUR_MIX, RECUR_REVERSE, EmbedConfig, RecurConfig, embed_bwd, embed_fwd,  # noqa: E402
+                        embed_workspace_bytes, probe_balance, probe_balance_workspace_bytes, recur_bwd, recur_fwd, recur_workspace_bytes)

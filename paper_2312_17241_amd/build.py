@@ -11,8 +11,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcngp.so")
-SOURCES = ["cngp_api.hip", "cngp_sort.hip"]
-HEADERS = ["cngp_device.h", "cngp_kernels.h", "cngp_fwd_level.h", "cngp_bwd_sliced.h", "cngp_bwd_binned.h", "cngp_bwd_merge.h", "cngp_bwd_runs.h", "cngp_optim.h", "cngp_mlp.h", "cngp_rates.h", os.path.join("..", "..", "include", "cngp.h")]
+SOURCES = ["cngp_api.hip", "cngp_sort.hip", "cngp_recur.hip", "cngp_embed.hip", "cngp_balance.hip"]
+HEADERS = ["cngp_launch.h", "cngp_radix.h", "cngp_device.h", "cngp_kernels.h", "cngp_fwd_level.h", "cngp_bwd_sliced.h", "cngp_bwd_binned.h", "cngp_bwd_merge.h", "cngp_bwd_runs.h", "cngp_optim.h", "cngp_mlp.h", "cngp_rates.h", os.path.join("..", "..", "include", "cngp.h")]
 
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-munsafe-fp-atomics",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wall", "-Wno-unused-function"]
@@ -29,11 +29,19 @@ def build(force: bool = True, extra=()) -> str:
     if not force and not stale():
         return LIB
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc] + FLAGS + list(extra) + ["-o", LIB] + [os.path.join(CSRC, s) for s in SOURCES]
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    msgs = [ln for ln in (res.stdout + res.stderr).splitlines()
-            if "packed-fp32-ops" not in ln]          # the host pass does not know the feature: harmless
-    if res.returncode != 0:
+    out_dir = os.path.join(os.path.dirname(HERE), "_build")
+    os.makedirs(out_dir, exist_ok=True)
+    objects = [os.path.join(out_dir, f + ".o") for f in SOURCES]
+    compile_flags = [f for f in FLAGS if f != "-shared"] + list(extra)
+    jobs = [subprocess.Popen([hipcc] + compile_flags + ["-c", "-o", o, os.path.join(CSRC, f)], stdout=subprocess.PIPE,
+                             stderr=subprocess.STDOUT, text=True) for f, o in zip(SOURCES, objects)]       # side by side
+    out = "".join(job.communicate()[0] for job in jobs)
+    failed = any(job.returncode for job in jobs)
+    if not failed:
+        res = subprocess.run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB] + objects, capture_output=True, text=True)
+        out, failed = out + res.stdout + res.stderr, res.returncode != 0
+    msgs = [ln for ln in out.splitlines() if "packed-fp32-ops" not in ln]          # the host pass does not know the feature: harmless
+    if failed:
         raise RuntimeError("hipcc failed:\n" + "\n".join(msgs))
     if msgs:
         print("\n".join(msgs), file=sys.stderr)

@@ -1,6 +1,7 @@
 // C ABI of the Compact NGP encoding library: argument checks, level table, kernel
 // selection and launches.  See include/cngp.h for the contract of every entry point.
 #include "../../include/cngp.h"
+#include "cngp_launch.h"
 #include "cngp_kernels.h"
 #include "cngp_fwd_level.h"
 #include "cngp_bwd_sliced.h"
@@ -35,7 +36,7 @@ int hip_fail(hipError_t e, const char *what) {
 }
 }  // namespace
 
-// for the other translation unit of the library (cngp_sort.hip): same record as cngp_last_hip_error() reads
+// for the library's other translation units: same record as cngp_last_hip_error() reads
 namespace cngp { int record_hip_failure(hipError_t e, const char *what) { return hip_fail(e, what); } }
 
 namespace {
@@ -64,8 +65,10 @@ int static_scratch(void **out) {
     return CNGP_OK;
 }
 
+}  // namespace
+
 // ---------------------------------------------------------------- validation (host only)
-int validate(const cngp_config *c) {
+int cngp::validate(const cngp_config *c) {
     if (!c) return CNGP_ERR_NULL;
     if (c->d < 2 || c->d > 4) return CNGP_ERR_INVALID;
     if (c->L < 1 || c->L > kMaxLevels) return CNGP_ERR_INVALID;
@@ -87,6 +90,8 @@ int validate(const cngp_config *c) {
     if (c->F != 1 && c->F != 2 && c->F != 4 && c->F != 8) return CNGP_ERR_UNSUPPORTED;
     return CNGP_OK;
 }
+
+namespace {
 
 // Table 1 (N_min, N_max, L): geometric growth, floor with a 1e-6 guard so that exact powers
 // (in particular N_{L-1} = N_max) survive the rounding of exp / pow.
@@ -133,9 +138,6 @@ bool index_codebook_is_empty(const cngp_config *c) { return c->index_format == C
 int check_blocks(int64_t blocks) { return (blocks > 0x7fffffffLL) ? CNGP_ERR_INVALID : CNGP_OK; }
 
 // ---------------------------------------------------------------- per-kernel timing
-enum KernelId { K_FWD = 0, K_BWD_DIRECT, K_BWD_PREP, K_BWD_SLICED, K_BWD_SLICED_V, K_BWD_GRID_DRAIN,
-                K_BAKE, K_ZERO, K_DEBUG, K_ADAM, K_MLP_FWD, K_MLP_BWD,
-                K_BWD_BIN_OFFSETS, K_BWD_BIN_SCATTER, K_BWD_BIN_DRAIN, K_BWD_INPUT, K_FUSED_FWD, K_PLANES, K_FWD_ROWS, K_BWD_SMALL, K_BWD_CELLS, K_BWD_MERGE, K_BWD_PARTIAL, K_COUNT };
 const char *const kKernelNames[K_COUNT] = {"encode_fwd", "encode_bwd_direct", "encode_bwd_prepare",
                                            "encode_bwd_sliced_points_and_grid", "encode_bwd_sliced_vertices",
                                            "encode_bwd_bin_grid_sums", "bake_probes", "zero", "debug_indices",
@@ -143,27 +145,29 @@ const char *const kKernelNames[K_COUNT] = {"encode_fwd", "encode_bwd_direct", "e
                                            "encode_bwd_bin_offsets", "encode_bwd_bin_scatter",
                                            "encode_bwd_bin_drain", "encode_bwd_input", "encode_mlp_fwd", "feature_planes",
                                            "encode_fwd_rows", "encode_bwd_small", "encode_bwd_cells", "encode_bwd_merge",
-                                           "encode_bwd_partial_sums"};
+                                           "encode_bwd_partial_sums",
+                                           "recur_fwd", "recur_bwd", "recur_carry", "embed_fwd", "embed_sort", "embed_sums", "probe_balance"};
 
 struct TimedLaunch { int id; hipEvent_t t0, t1; };
 bool g_profile = false;
 std::vector<TimedLaunch> g_timed;
 
-struct LaunchTimer {
-    hipStream_t s; int id; hipEvent_t t0 = nullptr, t1 = nullptr; bool on;
-    LaunchTimer(hipStream_t s_, int id_) : s(s_), id(id_), on(g_profile) {
-        if (on && (hipEventCreate(&t0) != hipSuccess || hipEventCreate(&t1) != hipSuccess)) on = false;
-        if (on) (void)hipEventRecord(t0, s);
-    }
-    ~LaunchTimer() {
-        if (on) { (void)hipEventRecord(t1, s); g_timed.push_back({id, t0, t1}); }
-    }
-};
+}  // namespace
 
-int launch_status(const char *what) {
+cngp::LaunchTimer::LaunchTimer(hipStream_t s_, int id_) : s(s_), id(id_), on(g_profile) {
+    if (on && (hipEventCreate(&t0) != hipSuccess || hipEventCreate(&t1) != hipSuccess)) on = false;
+    if (on) (void)hipEventRecord(t0, s);
+}
+cngp::LaunchTimer::~LaunchTimer() {
+    if (on) { (void)hipEventRecord(t1, s); g_timed.push_back({id, t0, t1}); }
+}
+
+int cngp::launch_status(const char *what) {
     hipError_t e = hipGetLastError();
     return e == hipSuccess ? CNGP_OK : hip_fail(e, what);
 }
+
+namespace {
 
 // ---------------------------------------------------------------- launches
 // Collects the arrays one call has to clear and clears them with a single launch.

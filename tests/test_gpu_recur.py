@@ -1,0 +1,222 @@
+"""The gated linear recurrence and its gradient on the GPU against the row-by-row evaluation in 64 bits (recur_ref.py)."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2312_17241_amd as cngp
+import recur_ref as R
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+REV, LOG, MIX = cngp.RECUR_REVERSE, cngp.RECUR_LOG_GATE, cngp.RECUR_MIX
+F16, F32 = cngp.F16, cngp.F32
+NP = {F16: np.float16, F32: np.float32}
+
+
+def offsets_of(lengths, lead=0):
+    return np.concatenate([[lead], lead + np.cumsum(lengths)]).astype(np.int32)
+
+
+def make(C, G, N, S, io, gt, flags, seed, near_one=False):
+    g = np.random.default_rng(seed)
+    if flags & LOG:
+        gate = -np.maximum(g.normal(size=(N, G)) * (0.01 if near_one else 0.5), 0)
+    else:
+        gate = 1 / (1 + np.exp(-g.normal(size=(N, G)) * 1.5 - (6 if near_one else 2)))
+        gate[g.random((N, G)) < 0.02] = 0.0
+        gate[g.random((N, G)) < 0.05] *= -1.0
+    return dict(gate=gate.astype(NP[gt]), x=g.normal(size=(N, C)).astype(NP[io]), h0=g.normal(size=(S, C)).astype(np.float32),
+                dy=g.normal(size=(N, C)).astype(NP[io]), dlast=g.normal(size=(S, C)).astype(np.float32))
+
+
+def dev(a):
+    return None if a is None else torch.from_numpy(np.ascontiguousarray(a)).to(DEV)
+
+
+def host(t):
+    return t.cpu().numpy().astype(np.float64)
+
+
+def check(C, shared, lengths, io=F32, gt=F32, flags=0, h0=True, dy=True, dlast=True, keep=True, lead=0, trail=0, uniform=False, longest=0,
+          seed=1, near_one=False):
+    G = 1 if shared else C
+    off = None if uniform else offsets_of(lengths, lead)
+    S, N = len(lengths), lead + int(np.sum(lengths)) + trail
+    d = make(C, G, N, S, io, gt, flags, seed, near_one)
+    if lead or trail:                      # rows of no sequence: not used, whatever they hold
+        for k in ("gate", "x", "dy"):
+            d[k][:lead] = np.nan
+            d[k][N - trail:] = np.nan
+    cfg = cngp.RecurConfig(C, G, io, gt, longest, flags)
+    sp = R.spans(N, S, off)
+    f64 = {k: v.astype(np.float64) for k, v in d.items()}
+    inside = np.zeros(N, bool)
+    for lo, hi in sp:
+        inside[lo:hi] = True
+    ref = R.backward(np.where(inside[:, None], f64["gate"], 0), np.where(inside[:, None], f64["x"], 0), sp, f64["h0"] if h0 else None,
+                     f64["dy"] if dy else None, f64["dlast"] if dlast else None, bool(flags & REV), bool(flags & LOG), bool(flags & MIX),
+                     R.half_step(NP[io]) if keep else 0.0)
+    t = {k: dev(v) for k, v in d.items()}
+    where = dict(h0=t["h0"] if h0 else None, offsets=dev(off), sequences=S)
+    sentinel = torch.full((N, C), 7.0, dtype=t["x"].dtype, device=DEV)
+    y, last = cngp.recur_fwd(cfg, t["gate"], t["x"], y=sentinel.clone(), **where)
+    R.within("y", host(y)[inside], ref["y"][inside], ref["Ey"][inside], NP[io])
+    R.within("last", host(last), ref["last"], ref["El"])
+    none, only = cngp.recur_fwd(cfg, t["gate"], t["x"], y=False, **where)
+    assert none is None and torch.equal(only, last)
+    ws = torch.full((max(cngp.recur_workspace_bytes(cfg, N, S, True, off is not None, keep), 256),), 255, dtype=torch.uint8, device=DEV)
+    out = [torch.full((N, G), 7.0, dtype=t["gate"].dtype, device=DEV), sentinel.clone(), torch.full((S, C), 7.0, device=DEV)]
+    dgate, dx, dh0 = cngp.recur_bwd(cfg, t["gate"], t["x"], dy=t["dy"] if dy else None, dlast=t["dlast"] if dlast else None,
+                                    y=y if keep else None, dgate=out[0], dx=out[1], dh0=out[2], workspace=ws, **where)
+    R.within("dx", host(dx)[inside], ref["dx"][inside], ref["Ex"][inside], NP[io])
+    R.within("dgate", host(dgate)[inside], ref["dgate"][inside], ref["Eg"][inside], NP[gt])
+    R.within("dh0", host(dh0), ref["dh0"], ref["E0"])
+    for name, a in (("y", y), ("dx", dx), ("dgate", dgate)):
+        assert bool((a[torch.from_numpy(~inside).to(DEV)] == 7.0).all()), f"{name}: a row of no sequence was written"
+
+
+RAGGED = [5, 0, 1, 64, 0, 63, 65, 130, 2, 0, 0, 17]
+
+
+@pytest.mark.parametrize("C,shared", [(1, False), (1, True), (2, True), (3, True), (4, True), (4, False), (5, False), (7, True), (16, True),
+                                      (16, False), (17, False), (31, True), (32, False), (33, False), (33, True), (64, False), (65, True),
+                                      (100, False), (130, True), (257, False)])
+@pytest.mark.parametrize("io,gt", [(F32, F32), (F16, F16), (F16, F32), (F32, F16)])
+def test_channels_and_types(C, shared, io, gt):
+    check(C, shared, RAGGED, io, gt, seed=C)
+
+
+@pytest.mark.parametrize("flags", range(8))
+@pytest.mark.parametrize("C,shared", [(3, True), (40, False)])
+@pytest.mark.parametrize("keep", [True, False])
+def test_directions_gates_and_inputs(flags, C, shared, keep):
+    check(C, shared, RAGGED, flags=flags, keep=keep, seed=flags)
+
+
+@pytest.mark.parametrize("kw", [dict(h0=False), dict(dy=False), dict(dlast=False), dict(lead=3, trail=5), dict(lead=100, trail=300),
+                                dict(longest=130), dict(longest=1), dict(longest=2**31 - 1)])
+@pytest.mark.parametrize("flags", [0, REV | LOG | MIX])
+@pytest.mark.parametrize("C,shared", [(3, True), (48, False)])
+def test_what_may_be_left_out(kw, flags, C, shared):
+    check(C, shared, RAGGED, flags=flags, **kw)
+
+
+@pytest.mark.parametrize("lengths,uniform", [
+    ([1], True), ([1] * 300, True), ([1] * 300, False), ([0, 0, 0], False), ([0], True), ([2047], True), ([2048], False), ([2049], False),
+    ([1023, 1025, 1], False), ([64] * 40, True), ([65] * 40, True), ([20011], True), ([3, 20011, 0, 2], False), ([700] * 9, True)])
+@pytest.mark.parametrize("C,shared,io,flags", [(1, True, F32, 0), (3, True, F32, REV | LOG | MIX), (8, False, F16, REV), (70, False, F32, 0), (66, True, F16, LOG)])
+def test_lengths(lengths, uniform, C, shared, io, flags):
+    check(C, shared, lengths, io, F32, flags, uniform=uniform, near_one=len(lengths) < 5)
+
+
+def test_a_long_sequence_of_few_channels_and_the_state_far_back():
+    """Gates close to one: the first rows still count at the end, through every cut."""
+    check(5, False, [100003], near_one=True, uniform=True)
+    check(33, False, [7, 60000, 9], near_one=True, flags=REV)
+
+
+def test_state_updated_in_place():
+    """One token each: last may be h0 itself, and dh0 dlast, in long sequences too."""
+    for S, T, C in ((64, 1, 130), (1, 30000, 3), (2, 9000, 40)):
+        cfg = cngp.RecurConfig(C, C)
+        d = {k: dev(v) for k, v in make(C, C, S * T, S, F32, F32, 0, 5).items()}
+        y, last = cngp.recur_fwd(cfg, d["gate"], d["x"], h0=d["h0"], sequences=S)
+        state = d["h0"].clone()
+        y2, same = cngp.recur_fwd(cfg, d["gate"], d["x"], h0=state, sequences=S, last=state)
+        assert same is state and torch.equal(state, last) and torch.equal(y, y2)
+        _, _, dh0 = cngp.recur_bwd(cfg, d["gate"], d["x"], dy=d["dy"], dlast=d["dlast"], h0=d["h0"], y=y, sequences=S)
+        grad = d["dlast"].clone()
+        cngp.recur_bwd(cfg, d["gate"], d["x"], dy=d["dy"], dlast=grad, h0=d["h0"], y=y, sequences=S, dh0=grad)
+        assert torch.equal(grad, dh0)
+
+
+@pytest.mark.parametrize("C,shared", [(3, True), (40, False)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_values_that_are_not_finite_stay_in_their_sequence_and_channel(C, shared, bad):
+    lengths = [30, 100, 1, 700, 50]
+    off, N, G = offsets_of(lengths), sum(lengths), 1 if shared else C
+    d = {k: dev(v) for k, v in make(C, G, N, 5, F32, F32, 0, 9).items()}
+    cfg = cngp.RecurConfig(C, G)
+    where = dict(h0=d["h0"], offsets=dev(off))
+    y, last = cngp.recur_fwd(cfg, d["gate"], d["x"], **where)
+    x = d["x"].clone()
+    x[35, 1] = bad                                  # the second sequence, its sixth row
+    yb, lastb = cngp.recur_fwd(cfg, d["gate"], x, **where)
+    hit = torch.zeros_like(y, dtype=torch.bool)
+    hit[35:130, 1] = True
+    assert torch.equal(yb[~hit], y[~hit]) and not bool(torch.isfinite(yb[35, 1]))
+    keep = torch.ones_like(last, dtype=torch.bool)
+    keep[1, 1] = False
+    assert torch.equal(lastb[keep], last[keep])
+    dlast = d["dlast"].clone()
+    dlast[1, 1] = bad
+    good = cngp.recur_bwd(cfg, d["gate"], d["x"], dy=d["dy"], dlast=d["dlast"], y=y, **where)
+    with_bad = cngp.recur_bwd(cfg, d["gate"], d["x"], dy=d["dy"], dlast=dlast, y=y, **where)
+    rows = torch.zeros(N, dtype=torch.bool, device=DEV)
+    rows[30:130] = True
+    assert torch.equal(with_bad[0][~rows], good[0][~rows]) and torch.equal(with_bad[1][~rows], good[1][~rows])
+    assert torch.equal(with_bad[1][:, [0, 2]], good[1][:, [0, 2]])
+
+
+def test_gates_that_shut():
+    """Log gates of minus infinity: nothing of the state passes, the input comes in whole, gradients are finite."""
+    cfg = cngp.RecurConfig(3, 1, flags=LOG | MIX)
+    d = make(3, 1, 500, 1, F32, F32, LOG, 4)
+    d["gate"][[0, 77, 78, 499]] = -np.inf
+    t = {k: dev(v) for k, v in d.items()}
+    y, last = cngp.recur_fwd(cfg, t["gate"], t["x"], h0=t["h0"])
+    assert torch.equal(y[77], t["x"][77]) and torch.equal(last[0], t["x"][499])
+    dgate, dx, dh0 = cngp.recur_bwd(cfg, t["gate"], t["x"], dy=t["dy"], dlast=t["dlast"], h0=t["h0"], y=y)
+    assert bool(torch.isfinite(dgate).all()) and bool((dgate[[0, 77, 78, 499]] == 0).all()) and bool((dh0 == 0).all())
+
+
+@pytest.mark.parametrize("lengths,C,shared,flags", [([4000, 0, 37], 3, True, REV | LOG | MIX), ([30000], 40, False, 0), ([1] * 100, 600, False, 0)])
+def test_graph_replays_another_stream_and_the_same_bits(lengths, C, shared, flags):
+    """Captured and replayed with eager work between, on another stream, twice: the same bits every time."""
+    off, N, G, S = offsets_of(lengths), sum(lengths), 1 if shared else C, len(lengths)
+    cfg = cngp.RecurConfig(C, G, flags=flags)
+    d = {k: dev(v) for k, v in make(C, G, N, S, F32, F32, flags, 3).items()}
+    off = dev(off)
+    outs = [torch.empty(N, C, device=DEV), torch.empty(S, C, device=DEV), torch.empty(N, G, device=DEV), torch.empty(N, C, device=DEV),
+            torch.empty(S, C, device=DEV)]
+    size = max(cngp.recur_workspace_bytes(cfg, N, S, b, True, False) for b in (False, True))
+    ws = torch.empty(max(size, 256), dtype=torch.uint8, device=DEV)
+
+    def step():
+        cngp.recur_fwd(cfg, d["gate"], d["x"], h0=d["h0"], offsets=off, y=outs[0], last=outs[1], workspace=ws)
+        cngp.recur_bwd(cfg, d["gate"], d["x"], dy=d["dy"], dlast=d["dlast"], h0=d["h0"], offsets=off, dgate=outs[2], dx=outs[3], dh0=outs[4],
+                       workspace=ws)
+
+    step()
+    want = [o.clone() for o in outs]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for o in outs:
+            o.fill_(7.0)
+        ws.fill_(255)
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(o, w) for o, w in zip(outs, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(3):
+        for o in outs:
+            o.fill_(float("nan"))
+        ws.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, w) for o, w in zip(outs, want))
+        step()
+
+
+def test_offsets_beyond_the_rows_are_taken_as_the_nearest():
+    cfg = cngp.RecurConfig(4, 4)
+    d = make(4, 4, 100, 4, F32, F32, 0, 8)
+    t = {k: dev(v) for k, v in d.items()}
+    spans, offsets = [(0, 40), (40, 100), (100, 100), (100, 100)], [-7, 40, 101, 2**31 - 1, 2**31 - 1]
+    y, last = cngp.recur_fwd(cfg, t["gate"], t["x"], h0=t["h0"], offsets=dev(np.array(offsets, np.int32)))
+    ref = R.forward(d["gate"].astype(np.float64), d["x"].astype(np.float64), spans, d["h0"].astype(np.float64), False, False, False)
+    R.within("y", host(y), ref["y"], ref["Ey"])
+    R.within("last", host(last), ref["last"], ref["El"])

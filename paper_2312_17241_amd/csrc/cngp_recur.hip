@@ -4,6 +4,7 @@
 //     da_t = dh_t (h_{t-1} [- x_t])     log gates: times a_t        dh0 = a_0 dh_0
 #include <algorithm>
 #include <cstdint>
+#include <initializer_list>
 
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
@@ -25,7 +26,7 @@ struct RecurArgs {
     const void    *y, *dy;               // backward; y_f32: y is the workspace's fp32 copy
     void          *out_y, *dgate, *dx;
     float         *last, *dh0;
-    float         *slope;                // backward of a gate shared by the channels: dL/dgate per channel, fp32 [N, C]
+    float         *slope;                // backward of a gate that several channel tiles share: their sums, fp32 [tiles][N]
     int64_t        N, S, rows_each;
     int32_t        C, G;
     uint32_t       flags;
@@ -37,83 +38,393 @@ __device__ __forceinline__ float load(const __half *p, const int64_t i) { return
 __device__ __forceinline__ void store(float *p, const int64_t i, const float v) { p[i] = v; }
 __device__ __forceinline__ void store(__half *p, const int64_t i, const float v) { p[i] = __float2half_rn(v); }
 
-// Rows [lo, hi) of sequence s, inside [0, N) whatever the offsets hold.
-__device__ __forceinline__ void bounds(const RecurArgs &a, const int64_t s, int64_t &lo, int64_t &hi) {
-    if (!a.offsets) { lo = s * a.rows_each; hi = lo + a.rows_each; return; }
-    const int64_t p = a.offsets[s], q = a.offsets[s + 1];
-    lo = p < 0 ? 0 : p > a.N ? a.N : p;
-    hi = q < lo ? lo : q > a.N ? a.N : q;
-}
-
 // The gate of a row and how much of the input it lets in.
 __device__ __forceinline__ void gate_of(const uint32_t flags, const float g, float &a, float &in) {
     a = flags & CNGP_RECUR_LOG_GATE ? expf(g) : g;
     in = !(flags & CNGP_RECUR_MIX) ? 1.0f : flags & CNGP_RECUR_LOG_GATE ? -expm1f(g) : 1.0f - g;
 }
 
-// One lane per sequence and channel.
-template <typename Io, typename Gate, typename Y>
-__global__ __launch_bounds__(kRecurBlock) void recur_fwd_kernel(const RecurArgs a)
-{
-    const int64_t i = (int64_t)blockIdx.x * kRecurBlock + threadIdx.x;
-    if (i >= a.S * a.C) return;
-    const int64_t s = i / a.C;
-    const int     c = (int)(i - s * a.C);
-    int64_t lo, hi;
-    bounds(a, s, lo, hi);
-    float h = a.h0 ? a.h0[i] : 0.0f;
-    for (int64_t k = lo; k < hi; ++k) {
-        const int64_t r = a.flags & CNGP_RECUR_REVERSE ? lo + hi - 1 - k : k;
-        float gate, in;
-        gate_of(a.flags, load((const Gate *)a.gate, a.G == 1 ? r : r * a.C + c), gate, in);
-        h = gate * h + in * load((const Io *)a.x, r * a.C + c);
-        if (a.out_y) store((Y *)a.out_y, r * a.C + c, h);
-    }
-    if (a.last) a.last[i] = h;
-}
+// ---------------------------------------------------------------- the scan
+// A row is the map h -> a h + v, and maps compose: rows (A, B) then (a, v) give (a A, a B + v).  So a sequence need not be walked
+// row after row: a workgroup takes a tile of RL * RB rows by CL * V channels, every lane composes the maps of its RB consecutive
+// rows, the lanes of the same channels join theirs (shuffles inside a wavefront, LDS between the four), and with the state that
+// then reaches its first row each lane walks its rows once more and writes.  The loads of a tile are all in flight at once, every
+// input is read once, every output written once.
+// The backward runs the same scan the other way: with u = a_{t+1} dh_{t+1} what arrives from later rows, dh = dy + u and what goes
+// on is a dh = a u + a dy.
+// Sequences are not handled one by one: the rows of all of them lie one behind the other, and the first row of a sequence takes
+// its map from h0 (or dlast) and forgets what came before -- a flag that travels with the map, not a factor of zero, so that
+// nothing that is not finite crosses over.
+// Positions: p counts rows in the order they are taken, p = row or N - 1 - row; ps(q) is where the q-th sequence in that order starts.
 
-template <typename Io, typename Gate>
-__global__ __launch_bounds__(kRecurBlock) void recur_bwd_kernel(const RecurArgs a)
-{
-    const int64_t i = (int64_t)blockIdx.x * kRecurBlock + threadIdx.x;
-    if (i >= a.S * a.C) return;
-    const int64_t s = i / a.C;
-    const int     c = (int)(i - s * a.C);
-    int64_t lo, hi;
-    bounds(a, s, lo, hi);
-    const bool    rev = a.flags & CNGP_RECUR_REVERSE;
-    float         u = a.dlast ? a.dlast[i] : 0.0f;           // what reaches the state after the row
-    for (int64_t k = lo; k < hi; ++k) {
-        const int64_t r = rev ? k : lo + hi - 1 - k, e = r * a.C + c, prev = rev ? r + 1 : r - 1;
-        float gate, in;
-        gate_of(a.flags, load((const Gate *)a.gate, a.G == 1 ? r : e), gate, in);
-        const bool  inner = k + 1 < hi;
-        const float before = !inner ? (a.h0 ? a.h0[i] : 0.0f)
-                             : a.y_f32 ? ((const float *)a.y)[prev * a.C + c] : load((const Io *)a.y, prev * a.C + c);
-        const float dh = u + (a.dy ? load((const Io *)a.dy, e) : 0.0f);
-        float       da = dh * (a.flags & CNGP_RECUR_MIX ? before - load((const Io *)a.x, e) : before);
-        if (a.flags & CNGP_RECUR_LOG_GATE) da *= gate;
-        if (a.slope) a.slope[e] = da;
-        else store((Gate *)a.dgate, e, da);
-        store((Io *)a.dx, e, in * dh);
-        u = gate * dh;
-    }
-    if (a.dh0) a.dh0[i] = u;
-}
+constexpr int kFlagRows = 2048;          // rows whose first / last marks are in LDS at a time; a multiple of every tile
 
-// dgate of a gate that all channels share: the sum over a row's channels.  A wavefront per row.
-template <typename Gate>
-__global__ __launch_bounds__(kRecurBlock) void recur_slope_kernel(const RecurArgs a)
-{
-    const int64_t r = ((int64_t)blockIdx.x * kRecurBlock + threadIdx.x) >> 6;
-    int64_t lo = 0, hi = a.N, unused;
-    if (a.offsets) { bounds(a, 0, lo, unused); bounds(a, a.S - 1, unused, hi); }
-    if (r < lo || r >= hi) return;
-    float sum = 0.0f;
-    for (int c = threadIdx.x & 63; c < a.C; c += 64) sum += a.slope[r * a.C + c];
+struct Order {
+    const int32_t *offsets;
+    int64_t        N, S, rows_each;
+    bool           back;                 // taken from the last row to the first
+    __device__ __forceinline__ int64_t at(const int64_t q) const {       // ps(q), 0 <= q <= S
+        if (!offsets) return q * rows_each;
+        int64_t o = offsets[back ? S - q : q];
+        o = o < 0 ? 0 : o > N ? N : o;
+        return back ? N - o : o;
+    }
+    __device__ __forceinline__ int64_t sequence(const int64_t q) const { return back ? S - 1 - q : q; }
+    __device__ __forceinline__ int64_t row(const int64_t p) const { return back ? N - 1 - p : p; }
+    // First q with ps(q) >= p (S + 1 if there is none); a wavefront calls this together, 64 probes at a time.
+    __device__ int64_t first_from(const int64_t p) const {
+        if (!offsets) { const int64_t q = rows_each ? (p + rows_each - 1) / rows_each : 0; return q < S + 1 ? q : S + 1; }
+        const int64_t lane = threadIdx.x & 63;
+        int64_t lo = 0, hi = S + 1;                      // the answer lies in [lo, hi]
+        while (lo < hi) {
+            const int64_t step = (hi - lo + 63) / 64, probe = lo + lane * step;
+            const uint64_t less = __ballot(probe < hi && at(probe) < p);
+            if (!less) { hi = lo; break; }
+            const int64_t last = lo + (63 - __clzll(less)) * step;      // the last probe that lies before p
+            lo = last + 1;
+            hi = last + step < hi ? last + step : hi;
+        }
+        return lo;
+    }
+};
+
+// Windows of rows: workgroup (k, channel tile) of a launch takes the sequences that start in [k R, (k + 1) R) -- or exactly those
+// rows, where a long sequence is cut: then the state at k R comes from `carry`.
+struct Cut {
+    int64_t  R;
+    uint32_t K;
+    float   *piece_a, *piece_b, *carry;  // [K][C]
+    int32_t *piece_cut;                  // [K]
+    int      exact;
+};
+
+template <typename T, int V>
+struct alignas(sizeof(T) * V) Vec { T e[V]; };
+
+template <typename T, int V>
+__device__ __forceinline__ void load_vec(float (&out)[V], const void *base, const int64_t i) {
+    const Vec<T, V> t = *reinterpret_cast<const Vec<T, V> *>((const T *)base + i);
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o, 64);
-    if ((threadIdx.x & 63) == 0) store((Gate *)a.dgate, r, sum);
+    for (int v = 0; v < V; ++v) out[v] = load(&t.e[v], 0);
+}
+template <typename T, int V>
+__device__ __forceinline__ void store_vec(void *base, const int64_t i, const float (&in)[V]) {
+    Vec<T, V> t;
+#pragma unroll
+    for (int v = 0; v < V; ++v) store(&t.e[v], 0, in[v]);
+    *reinterpret_cast<Vec<T, V> *>((T *)base + i) = t;
+}
+
+// PIECE: only the composed map of the rows that the next window continues, for `carry`; else the outputs.
+template <typename Io, typename Gate, int CL, int V, bool SHARED, bool BWD, bool PIECE>
+__global__ __launch_bounds__(kRecurBlock) void recur_scan_kernel(const RecurArgs a, const Cut cut)
+{
+    constexpr int RL = kRecurBlock / CL, RB = 8, TR = RL * RB, W = kRecurBlock / 64, GV = SHARED ? 1 : V;
+    static_assert(kFlagRows % TR == 0, "a tile's marks lie in one block of them");
+    __shared__ int32_t mark_first[PIECE ? 1 : kFlagRows], mark_last[PIECE ? 1 : kFlagRows];     // sequence (in order taken) or -1
+    __shared__ float   tot_a[2][W][CL * V], tot_b[2][W][CL * V];
+    __shared__ int     tot_cut[2][W];
+    __shared__ int     q_next;
+    const int      t = threadIdx.x, lane = t & 63, w = t >> 6, cl = t % CL, rl = t / CL;
+    const uint32_t k = blockIdx.x % cut.K, tile_c = blockIdx.x / cut.K;
+    const int      c = (int)tile_c * (CL * V) + cl * V;
+    const bool     c_ok = c < a.C;                             // V divides C
+    const bool     log_gate = a.flags & CNGP_RECUR_LOG_GATE, mix = a.flags & CNGP_RECUR_MIX;
+    const Order    o{a.offsets, a.N, a.S, a.rows_each, ((a.flags & CNGP_RECUR_REVERSE) != 0) != BWD};
+    const float   *before = BWD ? a.dlast : a.h0;              // what a sequence starts from, in the order taken
+
+    // the window's sequences [qa, qb) and rows [p0, p1)
+    const int64_t edge0 = (int64_t)k * cut.R, edge1 = edge0 + cut.R;
+    const bool    final_window = k + 1 == cut.K;
+    const int64_t qa = k == 0 ? 0 : o.first_from(edge0), qb = final_window ? a.S : o.first_from(edge1);
+    int64_t p0, p1;
+    if (cut.exact) {
+        const int64_t lo = o.at(0), hi = o.at(a.S);
+        p0 = edge0 < lo ? lo : edge0;
+        p1 = edge1 < hi && !final_window ? edge1 : hi;
+    } else {
+        p0 = qa <= a.S ? o.at(qa) : 0;
+        p1 = qa <= a.S ? o.at(qb < a.S ? qb : a.S) : 0;
+    }
+
+    float carry_a[V], carry_b[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) { carry_a[v] = 1.0f; carry_b[v] = 0.0f; }
+    if (PIECE) {
+        // only a sequence that goes on in the next window counts: the one that starts last in here, or none does and it is all rows
+        const int64_t q = (qb < a.S ? qb : a.S) - 1;
+        const bool    goes_on = !final_window && p1 > p0 && q >= 0 && o.at(q + 1) > p1;
+        const int64_t begin = goes_on ? o.at(q) : p1;
+        const bool    starts = !goes_on || begin >= p0;
+        if (t == 0 && tile_c == 0) cut.piece_cut[k] = starts;
+        if (!goes_on) return;                                  // the next window's first row starts a sequence
+        if (starts) {
+            p0 = begin;
+            if (c_ok && before) load_vec<float, V>(carry_b, before, o.sequence(q) * a.C + c);
+        }
+    } else if (cut.exact && k > 0 && c_ok) {
+        load_vec<float, V>(carry_b, cut.carry, (int64_t)k * a.C + c);
+    }
+
+    int64_t q_at = PIECE ? 0 : qa > 0 ? qa - 1 : 0;            // no sequence before this one reaches p0
+    const int64_t q_end = qb < a.S ? qb : a.S;
+    int buf = 0;
+    int64_t flags_from = p0;
+    for (int64_t pt = p0; pt < p1 || (!PIECE && pt == p0); pt += TR) {
+        if (!PIECE && (pt - p0) % kFlagRows == 0) {
+            // marks of the rows [flags_from, flags_to): first and last rows of sequences; sequences without rows pass their state on here
+            flags_from = pt;
+            const int64_t flags_to = p1 - pt < kFlagRows ? p1 : pt + kFlagRows;
+            const bool    at_end = flags_to == p1;
+            const int     rows = (int)(flags_to - flags_from);
+            for (int i = t; i < rows; i += kRecurBlock) { mark_first[i] = -1; mark_last[i] = -1; }
+            if (t == 0) q_next = (int)q_at;
+            __syncthreads();
+            int furthest = (int)q_at;
+            for (int64_t q = q_at + t; q < q_end; q += kRecurBlock) {
+                const int64_t f = o.at(q), l = o.at(q + 1);
+                if (f > flags_to || (f == flags_to && !at_end)) break;
+                if (f < l) {
+                    if (f < flags_to) furthest = (int)q;
+                    if (f >= flags_from && f < flags_to) mark_first[f - flags_from] = (int32_t)q;
+                    if (l > flags_from && l <= flags_to) mark_last[l - 1 - flags_from] = (int32_t)q;
+                } else if (f >= flags_from && q >= qa) {
+                    float        *to = BWD ? a.dh0 : a.last;
+                    const int64_t i = o.sequence(q) * a.C;
+                    for (int j = (int)tile_c * (CL * V); to && j < ((int)tile_c + 1) * (CL * V) && j < a.C; ++j) to[i + j] = before ? before[i + j] : 0.0f;
+                }
+            }
+            if (furthest > (int)q_at) atomicMax(&q_next, furthest);
+            __syncthreads();
+            q_at = q_next;
+        }
+        if (pt >= p1) break;
+
+        // the tile's rows of this lane: gates, what comes in
+        const int64_t pr = pt + rl * RB;
+        float    g[RB][GV], in[RB][V], share[RB][GV], left[BWD && !PIECE ? RB : 1][V];
+        uint32_t first = 0;
+#pragma unroll
+        for (int j = 0; j < RB; ++j) {
+            const int64_t p = pr + j, r = o.row(p);
+            const bool    ok = p < p1 && c_ok;
+#pragma unroll
+            for (int v = 0; v < GV; ++v) { g[j][v] = log_gate ? 0.0f : 1.0f; }
+#pragma unroll
+            for (int v = 0; v < V; ++v) in[j][v] = 0.0f;
+            if (ok) {
+                if (SHARED) g[j][0] = load((const Gate *)a.gate, r);
+                else load_vec<Gate, GV>(g[j], a.gate, r * a.C + c);
+                if (!BWD) load_vec<Io, V>(in[j], a.x, r * a.C + c);
+                else if (a.dy) load_vec<Io, V>(in[j], a.dy, r * a.C + c);
+            }
+        }
+        if constexpr (BWD && !PIECE) {
+#pragma unroll
+            for (int j = 0; j < RB; ++j) {                     // the state before the row: the next one's in the order taken
+                const int64_t p = pr + j, r = o.row(p);
+#pragma unroll
+                for (int v = 0; v < V; ++v) left[j][v] = 0.0f;
+                if (p < p1 && c_ok) {
+                    const int32_t q = mark_last[p - flags_from];
+                    if (q >= 0) {
+                        if (a.h0) load_vec<float, V>(left[j], a.h0, o.sequence(q) * a.C + c);
+                    } else if (p + 1 >= a.N) {                 // only where the offsets are not in order
+                    } else if (a.y_f32) {
+                        load_vec<float, V>(left[j], a.y, o.row(p + 1) * a.C + c);
+                    } else {
+                        load_vec<Io, V>(left[j], a.y, o.row(p + 1) * a.C + c);
+                    }
+                    if (mix) {
+                        float x[V];
+                        load_vec<Io, V>(x, a.x, r * a.C + c);
+#pragma unroll
+                        for (int v = 0; v < V; ++v) left[j][v] -= x[v];
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < RB; ++j) {
+            const int64_t p = pr + j;
+#pragma unroll
+            for (int v = 0; v < GV; ++v) gate_of(a.flags, g[j][v], g[j][v], share[j][v]);
+            if (!BWD) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) in[j][v] *= share[j][SHARED ? 0 : v];
+            }
+            if (!PIECE && p < p1) {
+                const int32_t q = mark_first[p - flags_from];
+                if (q >= 0) {
+                    first |= 1u << j;
+                    if (before && c_ok) {
+                        float h[V];
+                        load_vec<float, V>(h, before, o.sequence(q) * a.C + c);
+#pragma unroll
+                        for (int v = 0; v < V; ++v) in[j][v] = BWD ? in[j][v] + h[v] : fmaf(g[j][SHARED ? 0 : v], h[v], in[j][v]);
+                    }
+                }
+            }
+        }
+
+        // this lane's rows as one map, then those of the lanes before it
+        float A[V], B[V];
+        int   gone = first != 0;                               // whether what came before is forgotten
+#pragma unroll
+        for (int v = 0; v < V; ++v) { A[v] = 1.0f; B[v] = 0.0f; }
+#pragma unroll
+        for (int j = 0; j < RB; ++j)
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float gj = g[j][SHARED ? 0 : v];
+                const bool  f = (first >> j) & 1u;
+                B[v] = BWD ? gj * ((f ? 0.0f : B[v]) + in[j][v]) : (f ? in[j][v] : fmaf(gj, B[v], in[j][v]));
+                A[v] *= gj;
+            }
+#pragma unroll
+        for (int d = CL; d < 64; d <<= 1) {
+            const int gl = __shfl_up(gone, d, 64);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float Al = __shfl_up(A[v], d, 64), Bl = __shfl_up(B[v], d, 64);
+                if (lane >= d) {
+                    if (!gone) B[v] = fmaf(A[v], Bl, B[v]);
+                    A[v] *= Al;
+                }
+            }
+            if (lane >= d) gone |= gl;
+        }
+        if (lane >= 64 - CL) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) { tot_a[buf][w][cl * V + v] = A[v]; tot_b[buf][w][cl * V + v] = B[v]; }
+            if (lane == 63) tot_cut[buf][w] = gone;
+        }
+        __syncthreads();
+        float h[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) h[v] = carry_b[v];
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            const int forget = tot_cut[buf][i];
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                if (i == w) h[v] = carry_b[v];
+                const float Ai = tot_a[buf][i][cl * V + v], Bi = tot_b[buf][i][cl * V + v];
+                carry_b[v] = forget ? Bi : fmaf(Ai, carry_b[v], Bi);
+                if (PIECE) carry_a[v] *= Ai;
+            }
+        }
+        buf ^= 1;
+        if (PIECE) continue;
+        {
+            const int ge = __shfl_up(gone, CL, 64);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float Ae = __shfl_up(A[v], CL, 64), Be = __shfl_up(B[v], CL, 64);
+                if (lane >= CL) h[v] = ge ? Be : fmaf(Ae, h[v], Be);
+            }
+        }
+
+        // the rows once more, now with the state that reaches them
+#pragma unroll
+        for (int j = 0; j < RB; ++j) {
+            const int64_t p = pr + j, r = o.row(p);
+            const bool    f = (first >> j) & 1u, ok = p < p1 && c_ok;
+            const int32_t ends = p < p1 ? mark_last[p - flags_from] : -1;
+            if constexpr (!BWD) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) h[v] = f ? in[j][v] : fmaf(g[j][SHARED ? 0 : v], h[v], in[j][v]);
+                if (ok && a.out_y) {
+                    if (a.y_f32) store_vec<float, V>(a.out_y, r * a.C + c, h);
+                    else store_vec<Io, V>(a.out_y, r * a.C + c, h);
+                }
+                if (ok && ends >= 0 && a.last) store_vec<float, V>(a.last, o.sequence(ends) * a.C + c, h);
+            } else {
+                float dx[V], slope[V];
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const float gj = g[j][SHARED ? 0 : v];
+                    const float dh = (f ? 0.0f : h[v]) + in[j][v];
+                    dx[v] = share[j][SHARED ? 0 : v] * dh;
+                    slope[v] = log_gate ? dh * left[j][v] * gj : dh * left[j][v];
+                    h[v] = gj * dh;
+                }
+                if (ok) store_vec<Io, V>(a.dx, r * a.C + c, dx);
+                if constexpr (SHARED) {
+                    float sum = c_ok ? slope[0] : 0.0f;
+#pragma unroll
+                    for (int v = 1; v < V; ++v) sum += c_ok ? slope[v] : 0.0f;
+#pragma unroll
+                    for (int d = 1; d < CL; d <<= 1) sum += __shfl_xor(sum, d, 64);
+                    if (cl == 0 && p < p1) {
+                        if (a.slope) a.slope[(int64_t)tile_c * a.N + r] = sum;
+                        else store((Gate *)a.dgate, r, sum);
+                    }
+                } else if (ok) {
+                    store_vec<Gate, V>(a.dgate, r * a.C + c, slope);
+                }
+                if (ok && ends >= 0 && a.dh0) store_vec<float, V>(a.dh0, o.sequence(ends) * a.C + c, h);
+            }
+        }
+        if ((pt + TR - p0) % kFlagRows == 0) __syncthreads();  // the marks are written anew
+    }
+    if (PIECE && rl == 0 && c_ok) {
+        store_vec<float, V>(cut.piece_a, (int64_t)k * a.C + c, carry_a);
+        store_vec<float, V>(cut.piece_b, (int64_t)k * a.C + c, carry_b);
+    }
+}
+
+// The state that reaches each window, from the windows' maps: 32 channels to a workgroup, 32 lanes that take K / 32 windows each.
+constexpr int kCarryLanes = 32;
+__global__ __launch_bounds__(32 * kCarryLanes) void recur_carry_kernel(const Cut cut, const int C)
+{
+    __shared__ float sum_a[kCarryLanes][32], sum_b[kCarryLanes][32];
+    __shared__ int   sum_cut[kCarryLanes];
+    const int      cl = threadIdx.x & 31, rl = threadIdx.x >> 5, c = (int)blockIdx.x * 32 + cl;
+    const uint32_t per = (cut.K + kCarryLanes - 1) / kCarryLanes;
+    const uint32_t k0 = rl * per < cut.K ? rl * per : cut.K, k1 = k0 + per < cut.K ? k0 + per : cut.K;
+    const bool     ok = c < C;
+    float A = 1.0f, B = 0.0f;
+    int   gone = 0;
+#pragma unroll 8
+    for (uint32_t k = k0; k < k1; ++k) {
+        const int   f = cut.piece_cut[k];
+        const float a = ok && !f ? cut.piece_a[(size_t)k * C + c] : 0.0f, b = ok ? cut.piece_b[(size_t)k * C + c] : 0.0f;
+        B = f ? b : fmaf(a, B, b);
+        A *= a;
+        gone |= f;
+    }
+    sum_a[rl][cl] = A;
+    sum_b[rl][cl] = B;
+    if (cl == 0) sum_cut[rl] = gone;
+    __syncthreads();
+    float h = 0.0f;
+    for (int i = 0; i < rl; ++i) h = sum_cut[i] ? sum_b[i][cl] : fmaf(sum_a[i][cl], h, sum_b[i][cl]);
+#pragma unroll 8
+    for (uint32_t k = k0; k < k1; ++k) {
+        const int   f = cut.piece_cut[k];
+        const float a = ok && !f ? cut.piece_a[(size_t)k * C + c] : 0.0f, b = ok ? cut.piece_b[(size_t)k * C + c] : 0.0f;
+        if (ok) cut.carry[(size_t)k * C + c] = h;
+        h = f ? b : fmaf(a, h, b);
+    }
+}
+
+__global__ __launch_bounds__(kRecurBlock) void recur_copy_kernel(const float *__restrict__ from, float *__restrict__ to, const int64_t n)
+{
+    const int64_t i = (int64_t)blockIdx.x * kRecurBlock + threadIdx.x;
+    if (i < n) to[i] = from ? from[i] : 0.0f;
+}
+
+// dgate of a gate that all channels share, from the sums of the channel tiles.
+template <typename Gate>
+__global__ __launch_bounds__(kRecurBlock) void recur_slope_kernel(const RecurArgs a, const int tiles)
+{
+    const int64_t r = (int64_t)blockIdx.x * kRecurBlock + threadIdx.x;
+    const Order   o{a.offsets, a.N, a.S, a.rows_each, false};
+    if (r >= a.N || r < o.at(0) || r >= o.at(a.S)) return;
+    float sum = 0.0f;
+    for (int i = 0; i < tiles; ++i) sum += a.slope[(int64_t)i * a.N + r];
+    store((Gate *)a.dgate, r, sum);
 }
 
 int check(const cngp_recur_config *c, int64_t N, int64_t S, bool ragged) {
@@ -137,30 +448,123 @@ RecurArgs args_of(const cngp_recur_config *c, const void *gate, const void *x, i
     return a;
 }
 
+// How a call is cut.  CL lanes side by side hold V channels each: as many as there are channels, at most 32 (a row of a tile is then a
+// 128-byte line of fp32).
+struct RecurPlan {
+    int      CL, V, tiles;               // channel tiles
+    int64_t  R;                          // rows per window
+    uint32_t K;                          // windows
+    bool     exact;                      // long sequences are cut at the windows' edges
+};
+
+constexpr int64_t kEnoughGroups = 2048;  // workgroups that fill the chip's 256 CUs with eight each
+
+RecurPlan plan_of(const cngp_recur_config *c, int64_t N, int64_t S, bool ragged) {
+    RecurPlan p{};
+    p.CL = c->channels == 1 ? 1 : c->channels <= 4 ? 4 : c->channels <= 16 ? 16 : 32;
+    p.V = c->channels > 32 && c->channels % 2 == 0 ? 2 : 1;
+    p.tiles = (c->channels + p.CL * p.V - 1) / (p.CL * p.V);
+    const int64_t tile_rows = kRecurBlock / p.CL * 8;
+    const int64_t mean = S ? (N + S - 1) / S : 0;
+    // windows that give every CU eight workgroups, of whole tiles
+    int64_t R = (N * p.tiles + kEnoughGroups - 1) / kEnoughGroups;
+    R = std::max<int64_t>((R + tile_rows - 1) / tile_rows * tile_rows, tile_rows);
+    // sequences that are no longer than a few windows stay whole: one launch, every input read once.  Longer ones are cut
+    const int64_t longest = !ragged ? mean : c->longest ? std::min<int64_t>(c->longest, N) : 4 * mean;
+    p.exact = longest > 4 * R;
+    if (!p.exact && !ragged) R = std::max<int64_t>((R + mean / 2) / std::max<int64_t>(mean, 1), 1) * mean;
+    p.R = std::max<int64_t>(R, 1);
+    p.K = (uint32_t)std::max<int64_t>((N + p.R - 1) / p.R, 1);
+    return p;
+}
+
 // Where the parts of a workspace lie.
-struct RecurSpace { size_t y, slope, bytes; };
-RecurSpace space_of(const cngp_recur_config *c, int64_t N, uint32_t call) {
+struct RecurSpace { size_t y, slope, piece_a, piece_b, carry, piece_cut, state, bytes; };
+RecurSpace space_of(const cngp_recur_config *c, const RecurPlan &p, int64_t N, int64_t S, uint32_t call) {
     RecurSpace s{};
-    const size_t rows = align256((size_t)N * (size_t)c->channels * 4);
-    if (!(call & CNGP_RECUR_CALL_BWD)) return s;
-    s.y = 0;
-    s.slope = call & CNGP_RECUR_CALL_NO_Y ? rows : 0;
-    s.bytes = s.slope + (c->gate_channels != c->channels ? rows : 0);
+    size_t at = 0;
+    auto take = [&](bool wanted, size_t bytes) { const size_t o = at; if (wanted) at += align256(bytes); return o; };
+    const size_t C = (size_t)c->channels;
+    const bool   bwd = call & CNGP_RECUR_CALL_BWD;
+    s.y = take(bwd && (call & CNGP_RECUR_CALL_NO_Y), (size_t)N * C * 4);
+    const int singles = (c->channels + p.CL - 1) / p.CL;       // tiles of one channel to a lane, for arrays that are not aligned
+    s.slope = take(bwd && c->gate_channels == 1 && singles > 1, (size_t)N * (size_t)singles * 4);
+    s.piece_a = take(p.exact, p.K * C * 4);
+    s.piece_b = take(p.exact, p.K * C * 4);
+    s.carry = take(p.exact, p.K * C * 4);
+    s.piece_cut = take(p.exact, p.K * 4);
+    s.state = take(p.exact, (size_t)S * C * 4);
+    s.bytes = at;
     return s;
 }
 
-int launch_fwd(const cngp_recur_config *c, const RecurArgs &a, bool y_f32, hipStream_t s) {
-    const int64_t blocks = (a.S * a.C + kRecurBlock - 1) / kRecurBlock;
-    if (blocks > 0x7fffffffLL) return CNGP_ERR_INVALID;
-    LaunchTimer t(s, K_RECUR_FWD);
+template <typename Io, typename Gate, int CL, int V, bool SHARED, bool BWD>
+int launch_scan(const RecurArgs &a, const RecurPlan &p, const Cut &cut, hipStream_t s) {
+    const unsigned groups = cut.K * (unsigned)p.tiles;
+    if (cut.exact) {
+        {
+            LaunchTimer t(s, BWD ? K_RECUR_BWD : K_RECUR_FWD);
+            recur_scan_kernel<Io, Gate, CL, V, SHARED, BWD, true><<<groups, kRecurBlock, 0, s>>>(a, cut);
+            if (int rc = launch_status("recur_scan_kernel (pieces)")) return rc;
+        }
+        LaunchTimer t(s, K_RECUR_CARRY);
+        recur_carry_kernel<<<(unsigned)((a.C + 31) / 32), 32 * kCarryLanes, 0, s>>>(cut, a.C);
+        if (int rc = launch_status("recur_carry_kernel")) return rc;
+    }
+    LaunchTimer t(s, BWD ? K_RECUR_BWD : K_RECUR_FWD);
+    recur_scan_kernel<Io, Gate, CL, V, SHARED, BWD, false><<<groups, kRecurBlock, 0, s>>>(a, cut);
+    return launch_status("recur_scan_kernel");
+}
+
+template <typename Io, typename Gate, bool BWD>
+int launch_lanes(const RecurArgs &a, const RecurPlan &p, const Cut &cut, hipStream_t s) {
+    const bool shared = a.G == 1;
+    if (p.CL == 1) return launch_scan<Io, Gate, 1, 1, true, BWD>(a, p, cut, s);
+    if (p.CL == 4) return shared ? launch_scan<Io, Gate, 4, 1, true, BWD>(a, p, cut, s) : launch_scan<Io, Gate, 4, 1, false, BWD>(a, p, cut, s);
+    if (p.CL == 16) return shared ? launch_scan<Io, Gate, 16, 1, true, BWD>(a, p, cut, s) : launch_scan<Io, Gate, 16, 1, false, BWD>(a, p, cut, s);
+    if (p.V == 1) return shared ? launch_scan<Io, Gate, 32, 1, true, BWD>(a, p, cut, s) : launch_scan<Io, Gate, 32, 1, false, BWD>(a, p, cut, s);
+    return shared ? launch_scan<Io, Gate, 32, 2, true, BWD>(a, p, cut, s) : launch_scan<Io, Gate, 32, 2, false, BWD>(a, p, cut, s);
+}
+
+// One direction's launches.  state_in / state_out: what a sequence starts from and where it ends up; where they are one array and
+// sequences are cut, the workgroup that ends a sequence is not the one that starts it, so the start is taken from a copy.
+template <bool BWD>
+int launch(const cngp_recur_config *c, RecurArgs a, const RecurPlan &p, const RecurSpace &sp, char *ws, hipStream_t s) {
+    if ((int64_t)p.K * p.tiles > 0x7fffffffLL) return CNGP_ERR_UNSUPPORTED;
+    Cut cut{p.R, p.K, (float *)(ws + sp.piece_a), (float *)(ws + sp.piece_b), (float *)(ws + sp.carry), (int32_t *)(ws + sp.piece_cut), p.exact};
+    const float *&in = BWD ? a.dlast : a.h0;
+    float        *out = BWD ? a.dh0 : a.last;
+    if (p.exact && in && in == out) {
+        float        *copy = (float *)(ws + sp.state);
+        const int64_t n = a.S * a.C;
+        LaunchTimer t(s, K_RECUR_CARRY);
+        recur_copy_kernel<<<(unsigned)((n + kRecurBlock - 1) / kRecurBlock), kRecurBlock, 0, s>>>(in, copy, n);
+        if (int rc = launch_status("recur_copy_kernel")) return rc;
+        in = copy;
+    }
     const bool io16 = c->io_dtype == CNGP_F16, g16 = c->gate_dtype == CNGP_F16;
-#define CNGP_RECUR(Io, Gate) \
-    if (y_f32) recur_fwd_kernel<Io, Gate, float><<<(unsigned)blocks, kRecurBlock, 0, s>>>(a); \
-    else       recur_fwd_kernel<Io, Gate, Io><<<(unsigned)blocks, kRecurBlock, 0, s>>>(a)
-    if (io16 && g16) { CNGP_RECUR(__half, __half); } else if (io16) { CNGP_RECUR(__half, float); }
-    else if (g16) { CNGP_RECUR(float, __half); } else { CNGP_RECUR(float, float); }
-#undef CNGP_RECUR
-    return launch_status("recur_fwd_kernel");
+    return io16 ? (g16 ? launch_lanes<__half, __half, BWD>(a, p, cut, s) : launch_lanes<__half, float, BWD>(a, p, cut, s))
+                : (g16 ? launch_lanes<float, __half, BWD>(a, p, cut, s) : launch_lanes<float, float, BWD>(a, p, cut, s));
+}
+
+// One channel to a lane, the windows as they are: more channel tiles.
+void single_channels(const cngp_recur_config *c, RecurPlan &p) {
+    p.V = 1;
+    p.tiles = (c->channels + p.CL - 1) / p.CL;
+}
+
+// Two channels to a lane need arrays that start on a multiple of two values.
+bool pairs_fit(std::initializer_list<const void *> arrays) {
+    for (const void *p : arrays)
+        if ((uintptr_t)p & 7u) return false;
+    return true;
+}
+
+int pass_states(const float *in, float *out, int64_t n, hipStream_t s) {      // no rows at all
+    if (!out || in == out || n == 0) return CNGP_OK;
+    LaunchTimer t(s, K_RECUR_CARRY);
+    recur_copy_kernel<<<(unsigned)((n + kRecurBlock - 1) / kRecurBlock), kRecurBlock, 0, s>>>(in, out, n);
+    return launch_status("recur_copy_kernel");
 }
 
 }  // namespace
@@ -169,19 +573,23 @@ extern "C" {
 
 size_t cngp_recur_workspace_bytes(const cngp_recur_config *cfg, int64_t N, int64_t sequences, uint32_t call) {
     if (check(cfg, N, sequences, call & CNGP_RECUR_CALL_RAGGED)) return 0;
-    return space_of(cfg, N, call).bytes;
+    return space_of(cfg, plan_of(cfg, N, sequences, call & CNGP_RECUR_CALL_RAGGED), N, sequences, call).bytes;
 }
 
 int cngp_recur_fwd(const cngp_recur_config *cfg, const void *gate, const void *x, int64_t N, const int32_t *offsets, int64_t sequences,
                    const float *h0, void *y, float *last, void *workspace, size_t workspace_bytes, void *stream) {
     if (int rc = check(cfg, N, sequences, offsets != nullptr)) return rc;
     if (sequences == 0) return CNGP_OK;
-    if (N && (!gate || !x)) return CNGP_ERR_NULL;
-    if (!last && !y) return N ? CNGP_ERR_NULL : CNGP_OK;
-    (void)workspace; (void)workspace_bytes;
+    if (N && (!gate || !x || (!last && !y))) return CNGP_ERR_NULL;
+    hipStream_t s = (hipStream_t)stream;
+    if (N == 0) return pass_states(h0, last, sequences * cfg->channels, s);
+    RecurPlan        p = plan_of(cfg, N, sequences, offsets != nullptr);
+    const RecurSpace sp = space_of(cfg, p, N, sequences, offsets ? CNGP_RECUR_CALL_RAGGED : 0);
+    if (sp.bytes && (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < sp.bytes)) return CNGP_ERR_WORKSPACE;
     RecurArgs a = args_of(cfg, gate, x, N, offsets, sequences, h0);
     a.out_y = y; a.last = last;
-    return launch_fwd(cfg, a, false, (hipStream_t)stream);
+    if (p.V == 2 && !pairs_fit({gate, x, h0, y, last})) single_channels(cfg, p);
+    return launch<false>(cfg, a, p, sp, (char *)workspace, s);
 }
 
 int cngp_recur_bwd(const cngp_recur_config *cfg, const void *gate, const void *x, int64_t N, const int32_t *offsets, int64_t sequences,
@@ -190,38 +598,31 @@ int cngp_recur_bwd(const cngp_recur_config *cfg, const void *gate, const void *x
     if (int rc = check(cfg, N, sequences, offsets != nullptr)) return rc;
     if (sequences == 0) return CNGP_OK;
     if (N && (!gate || !x || !dgate || !dx || (!dy && !dlast))) return CNGP_ERR_NULL;
-    const uint32_t   call = CNGP_RECUR_CALL_BWD | (offsets ? CNGP_RECUR_CALL_RAGGED : 0) | (y ? 0 : CNGP_RECUR_CALL_NO_Y);
-    const RecurSpace sp = space_of(cfg, N, call);
-    if (sp.bytes && (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < sp.bytes)) return CNGP_ERR_WORKSPACE;
     hipStream_t s = (hipStream_t)stream;
+    if (N == 0) return pass_states(dlast, dh0, sequences * cfg->channels, s);
+    RecurPlan        p = plan_of(cfg, N, sequences, offsets != nullptr);
+    const uint32_t   call = CNGP_RECUR_CALL_BWD | (offsets ? CNGP_RECUR_CALL_RAGGED : 0) | (y ? 0 : CNGP_RECUR_CALL_NO_Y);
+    const RecurSpace sp = space_of(cfg, p, N, sequences, call);
+    char            *ws = (char *)workspace;
+    if (sp.bytes && (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < sp.bytes)) return CNGP_ERR_WORKSPACE;
+    if (p.V == 2 && !pairs_fit({gate, x, h0, y, dy, dlast, dgate, dx, dh0})) single_channels(cfg, p);
     RecurArgs a = args_of(cfg, gate, x, N, offsets, sequences, h0);
-    if (!y && N) {
-        a.out_y = (char *)workspace + sp.y;
-        if (int rc = launch_fwd(cfg, a, true, s)) return rc;
-        a.y = a.out_y;
+    a.y = y;
+    if (!y) {
+        a.out_y = ws + sp.y;
         a.y_f32 = 1;
-    } else {
-        a.y = y;
+        if (int rc = launch<false>(cfg, a, p, sp, ws, s)) return rc;
+        a.y = a.out_y;
     }
     a.dy = dy; a.dlast = dlast; a.dgate = dgate; a.dx = dx; a.dh0 = dh0;
-    const bool shared = cfg->gate_channels != cfg->channels;
-    a.slope = shared ? (float *)((char *)workspace + sp.slope) : nullptr;
-    const int64_t blocks = (a.S * a.C + kRecurBlock - 1) / kRecurBlock;
-    if (blocks > 0x7fffffffLL) return CNGP_ERR_INVALID;
-    const bool io16 = cfg->io_dtype == CNGP_F16, g16 = cfg->gate_dtype == CNGP_F16;
-    {
-        LaunchTimer t(s, K_RECUR_BWD);
-        if (io16 && g16) recur_bwd_kernel<__half, __half><<<(unsigned)blocks, kRecurBlock, 0, s>>>(a);
-        else if (io16) recur_bwd_kernel<__half, float><<<(unsigned)blocks, kRecurBlock, 0, s>>>(a);
-        else if (g16) recur_bwd_kernel<float, __half><<<(unsigned)blocks, kRecurBlock, 0, s>>>(a);
-        else recur_bwd_kernel<float, float><<<(unsigned)blocks, kRecurBlock, 0, s>>>(a);
-        if (int rc = launch_status("recur_bwd_kernel")) return rc;
-    }
-    if (!shared || !N) return CNGP_OK;
+    const bool sums = cfg->gate_channels == 1 && p.tiles > 1;
+    a.slope = sums ? (float *)(ws + sp.slope) : nullptr;
+    if (int rc = launch<true>(cfg, a, p, sp, ws, s)) return rc;
+    if (!sums) return CNGP_OK;
     LaunchTimer t(s, K_RECUR_BWD);
-    const int64_t sums = (N + kRecurBlock / 64 - 1) / (kRecurBlock / 64);
-    if (g16) recur_slope_kernel<__half><<<(unsigned)sums, kRecurBlock, 0, s>>>(a);
-    else recur_slope_kernel<float><<<(unsigned)sums, kRecurBlock, 0, s>>>(a);
+    const unsigned blocks = (unsigned)((N + kRecurBlock - 1) / kRecurBlock);
+    if (cfg->gate_dtype == CNGP_F16) recur_slope_kernel<__half><<<blocks, kRecurBlock, 0, s>>>(a, p.tiles);
+    else recur_slope_kernel<float><<<blocks, kRecurBlock, 0, s>>>(a, p.tiles);
     return launch_status("recur_slope_kernel");
 }
 

@@ -39,9 +39,10 @@ __device__ __forceinline__ void store(float *p, const int64_t i, const float v) 
 __device__ __forceinline__ void store(__half *p, const int64_t i, const float v) { p[i] = __float2half_rn(v); }
 
 // The gate of a row and how much of the input it lets in.
-__device__ __forceinline__ void gate_of(const uint32_t flags, const float g, float &a, float &in) {
-    a = flags & CNGP_RECUR_LOG_GATE ? expf(g) : g;
-    in = !(flags & CNGP_RECUR_MIX) ? 1.0f : flags & CNGP_RECUR_LOG_GATE ? -expm1f(g) : 1.0f - g;
+template <bool MIX>
+__device__ __forceinline__ void gate_of(const bool log_gate, const float g, float &a, float &in) {
+    in = !MIX ? 1.0f : log_gate ? -expm1f(g) : 1.0f - g;
+    a = log_gate ? expf(g) : g;
 }
 
 // ---------------------------------------------------------------- the scan
@@ -70,21 +71,38 @@ struct Order {
         return back ? N - o : o;
     }
     __device__ __forceinline__ int64_t sequence(const int64_t q) const { return back ? S - 1 - q : q; }
-    __device__ __forceinline__ int64_t row(const int64_t p) const { return back ? N - 1 - p : p; }
-    // First q with ps(q) >= p (S + 1 if there is none); a wavefront calls this together, 64 probes at a time.
-    __device__ int64_t first_from(const int64_t p) const {
-        if (!offsets) { const int64_t q = rows_each ? (p + rows_each - 1) / rows_each : 0; return q < S + 1 ? q : S + 1; }
-        const int64_t lane = threadIdx.x & 63;
-        int64_t lo = 0, hi = S + 1;                      // the answer lies in [lo, hi]
-        while (lo < hi) {
-            const int64_t step = (hi - lo + 63) / 64, probe = lo + lane * step;
-            const uint64_t less = __ballot(probe < hi && at(probe) < p);
-            if (!less) { hi = lo; break; }
-            const int64_t last = lo + (63 - __clzll(less)) * step;      // the last probe that lies before p
-            lo = last + 1;
-            hi = last + step < hi ? last + step : hi;
+    // First q with ps(q) >= p, for two p at once (S + 1 if there is none); a wavefront calls this together, 64 probes at a time.
+    __device__ void first_from(const int64_t pa, const int64_t pb, int64_t &qa, int64_t &qb) const {
+        if (!offsets) {
+            qa = (pa + rows_each - 1) / rows_each;
+            qb = (pb + rows_each - 1) / rows_each;
+            qa = qa < S + 1 ? qa : S + 1;
+            qb = qb < S + 1 ? qb : S + 1;
+            return;
         }
-        return lo;
+        const int64_t lane = threadIdx.x & 63;
+        int64_t lo[2] = {0, 0}, hi[2] = {S + 1, S + 1};         // the answers lie in [lo, hi]
+        const int64_t want[2] = {pa, pb};
+        while (lo[0] < hi[0] || lo[1] < hi[1]) {
+            bool    less[2];
+            int64_t step[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                step[i] = (hi[i] - lo[i] + 63) / 64;
+                const int64_t probe = lo[i] + lane * step[i];
+                less[i] = probe < hi[i] && at(probe < S ? probe : S) < want[i];
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint64_t before = __ballot(less[i]);
+                if (!before) { hi[i] = lo[i]; continue; }
+                const int64_t last = lo[i] + (63 - __clzll(before)) * step[i];      // the last probe that lies before p
+                lo[i] = last + 1;
+                hi[i] = last + step[i] < hi[i] ? last + step[i] : hi[i];
+            }
+        }
+        qa = lo[0];
+        qb = lo[1];
     }
 };
 
@@ -96,63 +114,101 @@ struct Cut {
     float   *piece_a, *piece_b, *carry;  // [K][C]
     int32_t *piece_cut;                  // [K]
     int      exact;
+    int      vec;                        // narrow rows: arrays start on 16-byte boundaries
 };
 
 template <typename T, int V>
-struct alignas(sizeof(T) * V) Vec { T e[V]; };
+struct alignas(V == 3 ? sizeof(T) : sizeof(T) * V) Vec { T e[V]; };
 
 template <typename T, int V>
-__device__ __forceinline__ void load_vec(float (&out)[V], const void *base, const int64_t i) {
-    const Vec<T, V> t = *reinterpret_cast<const Vec<T, V> *>((const T *)base + i);
+__device__ __forceinline__ void load_vec(float (&out)[V], const T *p) {
+    const Vec<T, V> t = *reinterpret_cast<const Vec<T, V> *>(p);
 #pragma unroll
     for (int v = 0; v < V; ++v) out[v] = load(&t.e[v], 0);
 }
 template <typename T, int V>
-__device__ __forceinline__ void store_vec(void *base, const int64_t i, const float (&in)[V]) {
+__device__ __forceinline__ void store_vec(T *p, const float (&in)[V]) {
     Vec<T, V> t;
 #pragma unroll
     for (int v = 0; v < V; ++v) store(&t.e[v], 0, in[v]);
-    *reinterpret_cast<Vec<T, V> *>((T *)base + i) = t;
+    *reinterpret_cast<Vec<T, V> *>(p) = t;
+}
+
+// Where a tile's rows lie.  Row j of a lane is memory row low + mine + j, or low + mine - j taken backwards; `low` is the same for
+// the whole workgroup, so a load is a scalar base and a 32-bit lane offset.
+struct Place {
+    int64_t  low;
+    uint32_t mine;                       // rows
+    int      dir;                        // 1 or -1
+};
+
+// RB rows of V values each, `width` values to a row of the array.  `shift`: the rows one further in the order taken.
+// Not a whole tile: rows outside [p0, p1) are read as the nearest row inside.
+template <typename T, int RB, int V>
+__device__ __forceinline__ void load_rows(float (&out)[RB][V], const void *array, const Place &at, const int width, const int c, const bool whole,
+                                          const int64_t pr, const int64_t p0, const int64_t p1)
+{
+    const uint32_t mine = at.mine * (uint32_t)width + (uint32_t)c;
+    const T       *base = (const T *)array + at.low * width;
+    if (whole) {
+#pragma unroll
+        for (int j = 0; j < RB; ++j) load_vec<T, V>(out[j], base + (int64_t)(at.dir * j) * width + mine);
+    } else {
+#pragma unroll
+        for (int j = 0; j < RB; ++j) {
+            const int64_t p = pr + j < p0 ? p0 : pr + j < p1 ? pr + j : p1 - 1;
+            load_vec<T, V>(out[j], base + (int64_t)mine + at.dir * (p - pr) * width);
+        }
+    }
 }
 
 // PIECE: only the composed map of the rows that the next window continues, for `carry`; else the outputs.
-template <typename Io, typename Gate, int CL, int V, bool SHARED, bool BWD, bool PIECE>
-__global__ __launch_bounds__(kRecurBlock) void recur_scan_kernel(const RecurArgs a, const Cut cut)
+// CL lanes side by side hold V channels each of a row, RB rows each.
+template <typename Io, typename Gate, int BLOCK, int CL, int V, int RB, bool SHARED, bool MIX, bool BWD, bool PIECE>
+__global__ __launch_bounds__(BLOCK) void recur_scan_kernel(const RecurArgs a, const Cut cut)
 {
-    constexpr int RL = kRecurBlock / CL, RB = 8, TR = RL * RB, W = kRecurBlock / 64, GV = SHARED ? 1 : V;
-    static_assert(kFlagRows % TR == 0, "a tile's marks lie in one block of them");
-    __shared__ int32_t mark_first[PIECE ? 1 : kFlagRows], mark_last[PIECE ? 1 : kFlagRows];     // sequence (in order taken) or -1
-    __shared__ float   tot_a[2][W][CL * V], tot_b[2][W][CL * V];
-    __shared__ int     tot_cut[2][W];
-    __shared__ int     q_next;
+    constexpr int RL = BLOCK / CL, TR = RL * RB, W = BLOCK / 64, GV = SHARED ? 1 : V;
+    static_assert(kFlagRows % TR == 0 && 32 % RB == 0, "a tile's marks lie in one block of them, a lane's in one word");
+    __shared__ uint32_t bits_first[PIECE ? 1 : kFlagRows / 32], bits_last[PIECE ? 1 : kFlagRows / 32];
+    __shared__ int32_t  mark_first[PIECE ? 1 : kFlagRows], mark_last[PIECE ? 1 : kFlagRows];     // sequence (in order taken), where the bit is set
+    __shared__ float    tot_a[2][W][CL * GV], tot_b[2][W][CL * V];
+    __shared__ int      tot_cut[2][W];
+    __shared__ int      q_next;
     const int      t = threadIdx.x, lane = t & 63, w = t >> 6, cl = t % CL, rl = t / CL;
     const uint32_t k = blockIdx.x % cut.K, tile_c = blockIdx.x / cut.K;
-    const int      c = (int)tile_c * (CL * V) + cl * V;
-    const bool     c_ok = c < a.C;                             // V divides C
-    const bool     log_gate = a.flags & CNGP_RECUR_LOG_GATE, mix = a.flags & CNGP_RECUR_MIX;
+    const int      c_here = (int)tile_c * (CL * V) + cl * V;
+    const bool     c_ok = c_here < a.C;                        // V divides C
+    const int      c = c_ok ? c_here : a.C - V;                // lanes without a channel read the last ones and write nothing
+    const int      gc = SHARED ? 0 : c, gw = SHARED ? 1 : a.C;
+    const bool     log_gate = a.flags & CNGP_RECUR_LOG_GATE;
     const Order    o{a.offsets, a.N, a.S, a.rows_each, ((a.flags & CNGP_RECUR_REVERSE) != 0) != BWD};
     const float   *before = BWD ? a.dlast : a.h0;              // what a sequence starts from, in the order taken
+    const int      dir = o.back ? -1 : 1;
 
     // the window's sequences [qa, qb) and rows [p0, p1)
     const int64_t edge0 = (int64_t)k * cut.R, edge1 = edge0 + cut.R;
     const bool    final_window = k + 1 == cut.K;
-    const int64_t qa = k == 0 ? 0 : o.first_from(edge0), qb = final_window ? a.S : o.first_from(edge1);
-    int64_t p0, p1;
+    int64_t qa, qb, p0, p1;
+    o.first_from(edge0, edge1, qa, qb);
+    if (k == 0) qa = 0;
+    if (final_window || qb > a.S) qb = a.S;
     if (cut.exact) {
         const int64_t lo = o.at(0), hi = o.at(a.S);
         p0 = edge0 < lo ? lo : edge0;
         p1 = edge1 < hi && !final_window ? edge1 : hi;
     } else {
         p0 = qa <= a.S ? o.at(qa) : 0;
-        p1 = qa <= a.S ? o.at(qb < a.S ? qb : a.S) : 0;
+        p1 = qa <= a.S ? o.at(qb) : 0;
     }
 
-    float carry_a[V], carry_b[V];
+    float carry_a[GV], carry_b[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) { carry_a[v] = 1.0f; carry_b[v] = 0.0f; }
+    for (int v = 0; v < GV; ++v) carry_a[v] = 1.0f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) carry_b[v] = 0.0f;
     if (PIECE) {
         // only a sequence that goes on in the next window counts: the one that starts last in here, or none does and it is all rows
-        const int64_t q = (qb < a.S ? qb : a.S) - 1;
+        const int64_t q = qb - 1;
         const bool    goes_on = !final_window && p1 > p0 && q >= 0 && o.at(q + 1) > p1;
         const int64_t begin = goes_on ? o.at(q) : p1;
         const bool    starts = !goes_on || begin >= p0;
@@ -160,34 +216,40 @@ __global__ __launch_bounds__(kRecurBlock) void recur_scan_kernel(const RecurArgs
         if (!goes_on) return;                                  // the next window's first row starts a sequence
         if (starts) {
             p0 = begin;
-            if (c_ok && before) load_vec<float, V>(carry_b, before, o.sequence(q) * a.C + c);
+            if (before) load_vec<float, V>(carry_b, before + o.sequence(q) * a.C + c);
         }
-    } else if (cut.exact && k > 0 && c_ok) {
-        load_vec<float, V>(carry_b, cut.carry, (int64_t)k * a.C + c);
+    } else if (cut.exact && k > 0) {
+        load_vec<float, V>(carry_b, cut.carry + (int64_t)k * a.C + c);
     }
 
     int64_t q_at = PIECE ? 0 : qa > 0 ? qa - 1 : 0;            // no sequence before this one reaches p0
-    const int64_t q_end = qb < a.S ? qb : a.S;
-    int buf = 0;
     int64_t flags_from = p0;
+    int     buf = 0;
     for (int64_t pt = p0; pt < p1 || (!PIECE && pt == p0); pt += TR) {
         if (!PIECE && (pt - p0) % kFlagRows == 0) {
             // marks of the rows [flags_from, flags_to): first and last rows of sequences; sequences without rows pass their state on here
             flags_from = pt;
             const int64_t flags_to = p1 - pt < kFlagRows ? p1 : pt + kFlagRows;
             const bool    at_end = flags_to == p1;
-            const int     rows = (int)(flags_to - flags_from);
-            for (int i = t; i < rows; i += kRecurBlock) { mark_first[i] = -1; mark_last[i] = -1; }
+            for (int i = t; i < kFlagRows / 32; i += BLOCK) { bits_first[i] = 0; bits_last[i] = 0; }
             if (t == 0) q_next = (int)q_at;
             __syncthreads();
             int furthest = (int)q_at;
-            for (int64_t q = q_at + t; q < q_end; q += kRecurBlock) {
+            for (int64_t q = q_at + t; q < qb; q += BLOCK) {
                 const int64_t f = o.at(q), l = o.at(q + 1);
                 if (f > flags_to || (f == flags_to && !at_end)) break;
                 if (f < l) {
                     if (f < flags_to) furthest = (int)q;
-                    if (f >= flags_from && f < flags_to) mark_first[f - flags_from] = (int32_t)q;
-                    if (l > flags_from && l <= flags_to) mark_last[l - 1 - flags_from] = (int32_t)q;
+                    if (f >= flags_from && f < flags_to) {
+                        const int i = (int)(f - flags_from);
+                        mark_first[i] = (int32_t)q;
+                        atomicOr(&bits_first[i >> 5], 1u << (i & 31));
+                    }
+                    if (l > flags_from && l <= flags_to) {
+                        const int i = (int)(l - 1 - flags_from);
+                        mark_last[i] = (int32_t)q;
+                        atomicOr(&bits_last[i >> 5], 1u << (i & 31));
+                    }
                 } else if (f >= flags_from && q >= qa) {
                     float        *to = BWD ? a.dh0 : a.last;
                     const int64_t i = o.sequence(q) * a.C;
@@ -200,212 +262,277 @@ __global__ __launch_bounds__(kRecurBlock) void recur_scan_kernel(const RecurArgs
         }
         if (pt >= p1) break;
 
-        // the tile's rows of this lane: gates, what comes in
-        const int64_t pr = pt + rl * RB;
-        float    g[RB][GV], in[RB][V], share[RB][GV], left[BWD && !PIECE ? RB : 1][V];
-        uint32_t first = 0;
+        const int64_t pr = pt + rl * RB;                       // this lane's first row, in the order taken
+        const bool    whole = pt + TR <= p1;
+        const Place   at{o.back ? a.N - TR - pt : pt, (uint32_t)(o.back ? TR - 1 - rl * RB : rl * RB), dir};
+        uint32_t first = 0, last = 0, live = (1u << RB) - 1u;
+        if (!whole) live = pr >= p1 ? 0u : pr + RB <= p1 ? live : (1u << (uint32_t)(p1 - pr)) - 1u;
+        if (!PIECE) {
+            const uint32_t i = (uint32_t)(pr - flags_from);
+            first = (bits_first[i >> 5] >> (i & 31)) & live;
+            last = (bits_last[i >> 5] >> (i & 31)) & live;
+        }
+
+        // gates and what comes in: x, or dy
+        float g[RB][GV], in[RB][V], share[MIX ? RB : 1][GV], left[BWD && !PIECE ? RB : 1][V];
+        load_rows<Gate, RB, GV>(g, a.gate, at, gw, gc, whole, pr, p0, p1);
+        if (!BWD || a.dy) {
+            load_rows<Io, RB, V>(in, BWD ? a.dy : a.x, at, a.C, c, whole, pr, p0, p1);
+        } else {
 #pragma unroll
-        for (int j = 0; j < RB; ++j) {
-            const int64_t p = pr + j, r = o.row(p);
-            const bool    ok = p < p1 && c_ok;
+            for (int j = 0; j < RB; ++j)
 #pragma unroll
-            for (int v = 0; v < GV; ++v) { g[j][v] = log_gate ? 0.0f : 1.0f; }
-#pragma unroll
-            for (int v = 0; v < V; ++v) in[j][v] = 0.0f;
-            if (ok) {
-                if (SHARED) g[j][0] = load((const Gate *)a.gate, r);
-                else load_vec<Gate, GV>(g[j], a.gate, r * a.C + c);
-                if (!BWD) load_vec<Io, V>(in[j], a.x, r * a.C + c);
-                else if (a.dy) load_vec<Io, V>(in[j], a.dy, r * a.C + c);
-            }
+                for (int v = 0; v < V; ++v) in[j][v] = 0.0f;
         }
         if constexpr (BWD && !PIECE) {
+            // the state before the row is that of the next row in the order taken (of the next window's first, at the end of this one)
+            const int64_t end = p1 + 1 <= a.N ? p1 + 1 : p1;
+            const Place   next{at.low + dir, at.mine, dir};
+            const bool    all = pt + TR + 1 <= end;
+            if (a.y_f32) load_rows<float, RB, V>(left, a.y, next, a.C, c, all, pr + 1, p0, end);
+            else load_rows<Io, RB, V>(left, a.y, next, a.C, c, all, pr + 1, p0, end);
+            if (__any(last != 0)) {
+                float h[RB][V];
 #pragma unroll
-            for (int j = 0; j < RB; ++j) {                     // the state before the row: the next one's in the order taken
-                const int64_t p = pr + j, r = o.row(p);
+                for (int j = 0; j < RB; ++j) {
 #pragma unroll
-                for (int v = 0; v < V; ++v) left[j][v] = 0.0f;
-                if (p < p1 && c_ok) {
-                    const int32_t q = mark_last[p - flags_from];
-                    if (q >= 0) {
-                        if (a.h0) load_vec<float, V>(left[j], a.h0, o.sequence(q) * a.C + c);
-                    } else if (p + 1 >= a.N) {                 // only where the offsets are not in order
-                    } else if (a.y_f32) {
-                        load_vec<float, V>(left[j], a.y, o.row(p + 1) * a.C + c);
-                    } else {
-                        load_vec<Io, V>(left[j], a.y, o.row(p + 1) * a.C + c);
-                    }
-                    if (mix) {
-                        float x[V];
-                        load_vec<Io, V>(x, a.x, r * a.C + c);
-#pragma unroll
-                        for (int v = 0; v < V; ++v) left[j][v] -= x[v];
+                    for (int v = 0; v < V; ++v) h[j][v] = 0.0f;
+                    if (a.h0) {
+                        const int64_t q = (last >> j) & 1u ? mark_last[(uint32_t)(pr - flags_from) + j] : 0;
+                        load_vec<float, V>(h[j], a.h0 + o.sequence(q) * a.C + c);
                     }
                 }
+#pragma unroll
+                for (int j = 0; j < RB; ++j)
+#pragma unroll
+                    for (int v = 0; v < V; ++v) left[j][v] = (last >> j) & 1u ? h[j][v] : left[j][v];
+            }
+            if (MIX) {
+                float x[RB][V];
+                load_rows<Io, RB, V>(x, a.x, at, a.C, c, whole, pr, p0, p1);
+#pragma unroll
+                for (int j = 0; j < RB; ++j)
+#pragma unroll
+                    for (int v = 0; v < V; ++v) left[j][v] -= x[j][v];
             }
         }
 #pragma unroll
         for (int j = 0; j < RB; ++j) {
-            const int64_t p = pr + j;
 #pragma unroll
-            for (int v = 0; v < GV; ++v) gate_of(a.flags, g[j][v], g[j][v], share[j][v]);
-            if (!BWD) {
-#pragma unroll
-                for (int v = 0; v < V; ++v) in[j][v] *= share[j][SHARED ? 0 : v];
+            for (int v = 0; v < GV; ++v) {
+                float in_share;
+                gate_of<MIX>(log_gate, g[j][v], g[j][v], in_share);
+                if (MIX) share[MIX ? j : 0][v] = in_share;
             }
-            if (!PIECE && p < p1) {
-                const int32_t q = mark_first[p - flags_from];
-                if (q >= 0) {
-                    first |= 1u << j;
-                    if (before && c_ok) {
-                        float h[V];
-                        load_vec<float, V>(h, before, o.sequence(q) * a.C + c);
+            if (MIX && !BWD) {
 #pragma unroll
-                        for (int v = 0; v < V; ++v) in[j][v] = BWD ? in[j][v] + h[v] : fmaf(g[j][SHARED ? 0 : v], h[v], in[j][v]);
-                    }
+                for (int v = 0; v < V; ++v) in[j][v] *= share[MIX ? j : 0][SHARED ? 0 : v];
+            }
+        }
+        if (!whole) {                                          // rows that are not there change nothing
+#pragma unroll
+            for (int j = 0; j < RB; ++j) {
+                const bool there = (live >> j) & 1u;
+#pragma unroll
+                for (int v = 0; v < GV; ++v) g[j][v] = there ? g[j][v] : 1.0f;
+#pragma unroll
+                for (int v = 0; v < V; ++v) in[j][v] = there ? in[j][v] : 0.0f;
+            }
+        }
+        if (!PIECE && before && __any(first != 0)) {
+            float h[RB][V];
+#pragma unroll
+            for (int j = 0; j < RB; ++j) {
+                const int64_t q = (first >> j) & 1u ? mark_first[(uint32_t)(pr - flags_from) + j] : 0;
+                load_vec<float, V>(h[j], before + o.sequence(q) * a.C + c);
+            }
+#pragma unroll
+            for (int j = 0; j < RB; ++j)
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const float with = BWD ? in[j][v] + h[j][v] : fmaf(g[j][SHARED ? 0 : v], h[j][v], in[j][v]);
+                    in[j][v] = (first >> j) & 1u ? with : in[j][v];
                 }
-            }
         }
 
         // this lane's rows as one map, then those of the lanes before it
-        float A[V], B[V];
+        float A[GV], B[V];
         int   gone = first != 0;                               // whether what came before is forgotten
 #pragma unroll
-        for (int v = 0; v < V; ++v) { A[v] = 1.0f; B[v] = 0.0f; }
+        for (int v = 0; v < GV; ++v) A[v] = 1.0f;
 #pragma unroll
-        for (int j = 0; j < RB; ++j)
+        for (int v = 0; v < V; ++v) B[v] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < RB; ++j) {
+            const bool f = (first >> j) & 1u;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const float gj = g[j][SHARED ? 0 : v];
-                const bool  f = (first >> j) & 1u;
                 B[v] = BWD ? gj * ((f ? 0.0f : B[v]) + in[j][v]) : (f ? in[j][v] : fmaf(gj, B[v], in[j][v]));
-                A[v] *= gj;
             }
+#pragma unroll
+            for (int v = 0; v < GV; ++v) A[v] *= g[j][v];
+        }
 #pragma unroll
         for (int d = CL; d < 64; d <<= 1) {
             const int gl = __shfl_up(gone, d, 64);
+            float     Al[GV], Bl[V];
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const float Al = __shfl_up(A[v], d, 64), Bl = __shfl_up(B[v], d, 64);
-                if (lane >= d) {
-                    if (!gone) B[v] = fmaf(A[v], Bl, B[v]);
-                    A[v] *= Al;
-                }
+            for (int v = 0; v < GV; ++v) Al[v] = __shfl_up(A[v], d, 64);
+#pragma unroll
+            for (int v = 0; v < V; ++v) Bl[v] = __shfl_up(B[v], d, 64);
+            if (lane >= d) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) B[v] = gone ? B[v] : fmaf(A[SHARED ? 0 : v], Bl[v], B[v]);
+#pragma unroll
+                for (int v = 0; v < GV; ++v) A[v] *= Al[v];
+                gone |= gl;
             }
-            if (lane >= d) gone |= gl;
         }
         if (lane >= 64 - CL) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) { tot_a[buf][w][cl * V + v] = A[v]; tot_b[buf][w][cl * V + v] = B[v]; }
+            for (int v = 0; v < GV; ++v) tot_a[buf][w][cl * GV + v] = A[v];
+#pragma unroll
+            for (int v = 0; v < V; ++v) tot_b[buf][w][cl * V + v] = B[v];
             if (lane == 63) tot_cut[buf][w] = gone;
         }
         __syncthreads();
         float h[V];
 #pragma unroll
-        for (int v = 0; v < V; ++v) h[v] = carry_b[v];
-#pragma unroll
         for (int i = 0; i < W; ++i) {
             const int forget = tot_cut[buf][i];
+            float     Ai[GV];
+#pragma unroll
+            for (int v = 0; v < GV; ++v) Ai[v] = tot_a[buf][i][cl * GV + v];
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 if (i == w) h[v] = carry_b[v];
-                const float Ai = tot_a[buf][i][cl * V + v], Bi = tot_b[buf][i][cl * V + v];
-                carry_b[v] = forget ? Bi : fmaf(Ai, carry_b[v], Bi);
-                if (PIECE) carry_a[v] *= Ai;
+                const float Bi = tot_b[buf][i][cl * V + v];
+                carry_b[v] = forget ? Bi : fmaf(Ai[SHARED ? 0 : v], carry_b[v], Bi);
+            }
+            if (PIECE) {
+#pragma unroll
+                for (int v = 0; v < GV; ++v) carry_a[v] *= Ai[v];
             }
         }
         buf ^= 1;
         if (PIECE) continue;
         {
             const int ge = __shfl_up(gone, CL, 64);
+            float     Ae[GV];
+#pragma unroll
+            for (int v = 0; v < GV; ++v) Ae[v] = __shfl_up(A[v], CL, 64);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const float Ae = __shfl_up(A[v], CL, 64), Be = __shfl_up(B[v], CL, 64);
-                if (lane >= CL) h[v] = ge ? Be : fmaf(Ae, h[v], Be);
+                const float Be = __shfl_up(B[v], CL, 64);
+                if (lane >= CL) h[v] = ge ? Be : fmaf(Ae[SHARED ? 0 : v], h[v], Be);
             }
         }
 
         // the rows once more, now with the state that reaches them
+        const uint32_t put = c_ok ? live : 0u;
+        const int64_t  row0 = at.low + at.mine;
 #pragma unroll
         for (int j = 0; j < RB; ++j) {
-            const int64_t p = pr + j, r = o.row(p);
-            const bool    f = (first >> j) & 1u, ok = p < p1 && c_ok;
-            const int32_t ends = p < p1 ? mark_last[p - flags_from] : -1;
+            const bool    f = (first >> j) & 1u, ok = (put >> j) & 1u;
+            const int64_t r = row0 + dir * j;
             if constexpr (!BWD) {
 #pragma unroll
                 for (int v = 0; v < V; ++v) h[v] = f ? in[j][v] : fmaf(g[j][SHARED ? 0 : v], h[v], in[j][v]);
-                if (ok && a.out_y) {
-                    if (a.y_f32) store_vec<float, V>(a.out_y, r * a.C + c, h);
-                    else store_vec<Io, V>(a.out_y, r * a.C + c, h);
+                if (a.out_y && ok) {
+                    if (a.y_f32) store_vec<float, V>((float *)a.out_y + r * a.C + c, h);
+                    else store_vec<Io, V>((Io *)a.out_y + r * a.C + c, h);
                 }
-                if (ok && ends >= 0 && a.last) store_vec<float, V>(a.last, o.sequence(ends) * a.C + c, h);
+                if ((last >> j) & 1u) {
+                    const int64_t q = mark_last[(uint32_t)(pr - flags_from) + j];
+                    if (ok && a.last) store_vec<float, V>(a.last + o.sequence(q) * a.C + c, h);
+                }
             } else {
                 float dx[V], slope[V];
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
                     const float gj = g[j][SHARED ? 0 : v];
                     const float dh = (f ? 0.0f : h[v]) + in[j][v];
-                    dx[v] = share[j][SHARED ? 0 : v] * dh;
-                    slope[v] = log_gate ? dh * left[j][v] * gj : dh * left[j][v];
+                    dx[v] = MIX ? share[MIX ? j : 0][SHARED ? 0 : v] * dh : dh;
+                    slope[v] = dh * left[j][v];
+                    if (log_gate) slope[v] *= gj;
                     h[v] = gj * dh;
                 }
-                if (ok) store_vec<Io, V>(a.dx, r * a.C + c, dx);
+                if (ok) store_vec<Io, V>((Io *)a.dx + r * a.C + c, dx);
                 if constexpr (SHARED) {
                     float sum = c_ok ? slope[0] : 0.0f;
 #pragma unroll
                     for (int v = 1; v < V; ++v) sum += c_ok ? slope[v] : 0.0f;
 #pragma unroll
                     for (int d = 1; d < CL; d <<= 1) sum += __shfl_xor(sum, d, 64);
-                    if (cl == 0 && p < p1) {
+                    if (cl == 0 && ((live >> j) & 1u)) {
                         if (a.slope) a.slope[(int64_t)tile_c * a.N + r] = sum;
                         else store((Gate *)a.dgate, r, sum);
                     }
                 } else if (ok) {
-                    store_vec<Gate, V>(a.dgate, r * a.C + c, slope);
+                    store_vec<Gate, V>((Gate *)a.dgate + r * a.C + c, slope);
                 }
-                if (ok && ends >= 0 && a.dh0) store_vec<float, V>(a.dh0, o.sequence(ends) * a.C + c, h);
+                if ((last >> j) & 1u) {
+                    const int64_t q = mark_last[(uint32_t)(pr - flags_from) + j];
+                    if (ok && a.dh0) store_vec<float, V>(a.dh0 + o.sequence(q) * a.C + c, h);
+                }
             }
         }
         if ((pt + TR - p0) % kFlagRows == 0) __syncthreads();  // the marks are written anew
     }
     if (PIECE && rl == 0 && c_ok) {
-        store_vec<float, V>(cut.piece_a, (int64_t)k * a.C + c, carry_a);
-        store_vec<float, V>(cut.piece_b, (int64_t)k * a.C + c, carry_b);
+        float A[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) A[v] = carry_a[SHARED ? 0 : v];
+        store_vec<float, V>(cut.piece_a + (int64_t)k * a.C + c, A);
+        store_vec<float, V>(cut.piece_b + (int64_t)k * a.C + c, carry_b);
     }
 }
 
-// The state that reaches each window, from the windows' maps: 32 channels to a workgroup, 32 lanes that take K / 32 windows each.
-constexpr int kCarryLanes = 32;
-__global__ __launch_bounds__(32 * kCarryLanes) void recur_carry_kernel(const Cut cut, const int C)
+// The state that reaches each window, from the windows' maps: 16 channels to a workgroup, 64 lanes with up to 16 windows each, held in
+// registers between composing them and walking them with the state.
+constexpr int kCarryChannels = 16, kCarryLanes = 64, kCarryEach = 16, kMostWindows = kCarryLanes * kCarryEach;
+__global__ __launch_bounds__(kCarryChannels * kCarryLanes) void recur_carry_kernel(const Cut cut, const int C)
 {
-    __shared__ float sum_a[kCarryLanes][32], sum_b[kCarryLanes][32];
+    __shared__ float sum_a[kCarryLanes][kCarryChannels], sum_b[kCarryLanes][kCarryChannels];
     __shared__ int   sum_cut[kCarryLanes];
-    const int      cl = threadIdx.x & 31, rl = threadIdx.x >> 5, c = (int)blockIdx.x * 32 + cl;
-    const uint32_t per = (cut.K + kCarryLanes - 1) / kCarryLanes;
-    const uint32_t k0 = rl * per < cut.K ? rl * per : cut.K, k1 = k0 + per < cut.K ? k0 + per : cut.K;
-    const bool     ok = c < C;
+    const int      cl = threadIdx.x % kCarryChannels, rl = threadIdx.x / kCarryChannels;
+    const int      c_here = (int)blockIdx.x * kCarryChannels + cl, c = c_here < C ? c_here : C - 1;
+    const uint32_t per = (cut.K + kCarryLanes - 1) / kCarryLanes, k0 = rl * per;
+    float a[kCarryEach], b[kCarryEach];
+    int   f[kCarryEach];
+#pragma unroll
+    for (int i = 0; i < kCarryEach; ++i) {
+        const uint32_t k = k0 + i;
+        const bool     there = (uint32_t)i < per && k < cut.K;
+        const size_t   at = (size_t)(there ? k : 0) * C + c;
+        f[i] = there ? cut.piece_cut[there ? k : 0] : 0;
+        a[i] = there ? cut.piece_a[at] : 1.0f;
+        b[i] = there ? cut.piece_b[at] : 0.0f;
+    }
     float A = 1.0f, B = 0.0f;
     int   gone = 0;
-#pragma unroll 8
-    for (uint32_t k = k0; k < k1; ++k) {
-        const int   f = cut.piece_cut[k];
-        const float a = ok && !f ? cut.piece_a[(size_t)k * C + c] : 0.0f, b = ok ? cut.piece_b[(size_t)k * C + c] : 0.0f;
-        B = f ? b : fmaf(a, B, b);
-        A *= a;
-        gone |= f;
+#pragma unroll
+    for (int i = 0; i < kCarryEach; ++i) {
+        B = f[i] ? b[i] : fmaf(a[i], B, b[i]);
+        A *= a[i];
+        gone |= f[i];
     }
     sum_a[rl][cl] = A;
     sum_b[rl][cl] = B;
     if (cl == 0) sum_cut[rl] = gone;
     __syncthreads();
     float h = 0.0f;
-    for (int i = 0; i < rl; ++i) h = sum_cut[i] ? sum_b[i][cl] : fmaf(sum_a[i][cl], h, sum_b[i][cl]);
 #pragma unroll 8
-    for (uint32_t k = k0; k < k1; ++k) {
-        const int   f = cut.piece_cut[k];
-        const float a = ok && !f ? cut.piece_a[(size_t)k * C + c] : 0.0f, b = ok ? cut.piece_b[(size_t)k * C + c] : 0.0f;
-        if (ok) cut.carry[(size_t)k * C + c] = h;
-        h = f ? b : fmaf(a, h, b);
+    for (int i = 0; i < kCarryLanes; ++i) {
+        const float next = sum_cut[i] ? sum_b[i][cl] : fmaf(sum_a[i][cl], h, sum_b[i][cl]);
+        h = i < rl ? next : h;
+    }
+#pragma unroll
+    for (int i = 0; i < kCarryEach; ++i) {
+        const uint32_t k = k0 + i;
+        if ((uint32_t)i < per && k < cut.K && c_here < C) cut.carry[(size_t)k * C + c] = h;
+        h = f[i] ? b[i] : fmaf(a[i], h, b[i]);
     }
 }
 
@@ -457,6 +584,7 @@ struct RecurPlan {
     bool     exact;                      // long sequences are cut at the windows' edges
 };
 
+constexpr int     kRowsEach = 8;          // rows of a tile per lane
 constexpr int64_t kEnoughGroups = 2048;  // workgroups that fill the chip's 256 CUs with eight each
 
 RecurPlan plan_of(const cngp_recur_config *c, int64_t N, int64_t S, bool ragged) {
@@ -464,7 +592,7 @@ RecurPlan plan_of(const cngp_recur_config *c, int64_t N, int64_t S, bool ragged)
     p.CL = c->channels == 1 ? 1 : c->channels <= 4 ? 4 : c->channels <= 16 ? 16 : 32;
     p.V = c->channels > 32 && c->channels % 2 == 0 ? 2 : 1;
     p.tiles = (c->channels + p.CL * p.V - 1) / (p.CL * p.V);
-    const int64_t tile_rows = kRecurBlock / p.CL * 8;
+    const int64_t tile_rows = kRecurBlock / p.CL * kRowsEach;
     const int64_t mean = S ? (N + S - 1) / S : 0;
     // windows that give every CU eight workgroups, of whole tiles
     int64_t R = (N * p.tiles + kEnoughGroups - 1) / kEnoughGroups;
@@ -472,6 +600,7 @@ RecurPlan plan_of(const cngp_recur_config *c, int64_t N, int64_t S, bool ragged)
     // sequences that are no longer than a few windows stay whole: one launch, every input read once.  Longer ones are cut
     const int64_t longest = !ragged ? mean : c->longest ? std::min<int64_t>(c->longest, N) : 4 * mean;
     p.exact = longest > 4 * R;
+    if (p.exact) R = std::max(R, ((N + kMostWindows - 1) / kMostWindows + tile_rows - 1) / tile_rows * tile_rows);
     if (!p.exact && !ragged) R = std::max<int64_t>((R + mean / 2) / std::max<int64_t>(mean, 1), 1) * mean;
     p.R = std::max<int64_t>(R, 1);
     p.K = (uint32_t)std::max<int64_t>((N + p.R - 1) / p.R, 1);
@@ -498,32 +627,37 @@ RecurSpace space_of(const cngp_recur_config *c, const RecurPlan &p, int64_t N, i
     return s;
 }
 
-template <typename Io, typename Gate, int CL, int V, bool SHARED, bool BWD>
+template <typename Io, typename Gate, int CL, int V, bool SHARED, bool MIX, bool BWD>
 int launch_scan(const RecurArgs &a, const RecurPlan &p, const Cut &cut, hipStream_t s) {
     const unsigned groups = cut.K * (unsigned)p.tiles;
     if (cut.exact) {
         {
             LaunchTimer t(s, BWD ? K_RECUR_BWD : K_RECUR_FWD);
-            recur_scan_kernel<Io, Gate, CL, V, SHARED, BWD, true><<<groups, kRecurBlock, 0, s>>>(a, cut);
+            recur_scan_kernel<Io, Gate, kRecurBlock, CL, V, kRowsEach, SHARED, MIX, BWD, true><<<groups, kRecurBlock, 0, s>>>(a, cut);
             if (int rc = launch_status("recur_scan_kernel (pieces)")) return rc;
         }
         LaunchTimer t(s, K_RECUR_CARRY);
-        recur_carry_kernel<<<(unsigned)((a.C + 31) / 32), 32 * kCarryLanes, 0, s>>>(cut, a.C);
+        recur_carry_kernel<<<(unsigned)((a.C + kCarryChannels - 1) / kCarryChannels), kCarryChannels * kCarryLanes, 0, s>>>(cut, a.C);
         if (int rc = launch_status("recur_carry_kernel")) return rc;
     }
     LaunchTimer t(s, BWD ? K_RECUR_BWD : K_RECUR_FWD);
-    recur_scan_kernel<Io, Gate, CL, V, SHARED, BWD, false><<<groups, kRecurBlock, 0, s>>>(a, cut);
+    recur_scan_kernel<Io, Gate, kRecurBlock, CL, V, kRowsEach, SHARED, MIX, BWD, false><<<groups, kRecurBlock, 0, s>>>(a, cut);
     return launch_status("recur_scan_kernel");
 }
 
-template <typename Io, typename Gate, bool BWD>
+template <typename Io, typename Gate, bool MIX, bool BWD>
 int launch_lanes(const RecurArgs &a, const RecurPlan &p, const Cut &cut, hipStream_t s) {
     const bool shared = a.G == 1;
-    if (p.CL == 1) return launch_scan<Io, Gate, 1, 1, true, BWD>(a, p, cut, s);
-    if (p.CL == 4) return shared ? launch_scan<Io, Gate, 4, 1, true, BWD>(a, p, cut, s) : launch_scan<Io, Gate, 4, 1, false, BWD>(a, p, cut, s);
-    if (p.CL == 16) return shared ? launch_scan<Io, Gate, 16, 1, true, BWD>(a, p, cut, s) : launch_scan<Io, Gate, 16, 1, false, BWD>(a, p, cut, s);
-    if (p.V == 1) return shared ? launch_scan<Io, Gate, 32, 1, true, BWD>(a, p, cut, s) : launch_scan<Io, Gate, 32, 1, false, BWD>(a, p, cut, s);
-    return shared ? launch_scan<Io, Gate, 32, 2, true, BWD>(a, p, cut, s) : launch_scan<Io, Gate, 32, 2, false, BWD>(a, p, cut, s);
+    if (p.CL == 1) return launch_scan<Io, Gate, 1, 1, true, MIX, BWD>(a, p, cut, s);
+    if (p.CL == 4) return shared ? launch_scan<Io, Gate, 4, 1, true, MIX, BWD>(a, p, cut, s) : launch_scan<Io, Gate, 4, 1, false, MIX, BWD>(a, p, cut, s);
+    if (p.CL == 16) return shared ? launch_scan<Io, Gate, 16, 1, true, MIX, BWD>(a, p, cut, s) : launch_scan<Io, Gate, 16, 1, false, MIX, BWD>(a, p, cut, s);
+    if (p.V == 1) return shared ? launch_scan<Io, Gate, 32, 1, true, MIX, BWD>(a, p, cut, s) : launch_scan<Io, Gate, 32, 1, false, MIX, BWD>(a, p, cut, s);
+    return shared ? launch_scan<Io, Gate, 32, 2, true, MIX, BWD>(a, p, cut, s) : launch_scan<Io, Gate, 32, 2, false, MIX, BWD>(a, p, cut, s);
+}
+
+template <typename Io, typename Gate, bool BWD>
+int launch_inputs(const RecurArgs &a, const RecurPlan &p, const Cut &cut, hipStream_t s) {
+    return a.flags & CNGP_RECUR_MIX ? launch_lanes<Io, Gate, true, BWD>(a, p, cut, s) : launch_lanes<Io, Gate, false, BWD>(a, p, cut, s);
 }
 
 // One direction's launches.  state_in / state_out: what a sequence starts from and where it ends up; where they are one array and
@@ -531,7 +665,7 @@ int launch_lanes(const RecurArgs &a, const RecurPlan &p, const Cut &cut, hipStre
 template <bool BWD>
 int launch(const cngp_recur_config *c, RecurArgs a, const RecurPlan &p, const RecurSpace &sp, char *ws, hipStream_t s) {
     if ((int64_t)p.K * p.tiles > 0x7fffffffLL) return CNGP_ERR_UNSUPPORTED;
-    Cut cut{p.R, p.K, (float *)(ws + sp.piece_a), (float *)(ws + sp.piece_b), (float *)(ws + sp.carry), (int32_t *)(ws + sp.piece_cut), p.exact};
+    Cut cut{p.R, p.K, (float *)(ws + sp.piece_a), (float *)(ws + sp.piece_b), (float *)(ws + sp.carry), (int32_t *)(ws + sp.piece_cut), p.exact, 0};
     const float *&in = BWD ? a.dlast : a.h0;
     float        *out = BWD ? a.dh0 : a.last;
     if (p.exact && in && in == out) {
@@ -543,8 +677,8 @@ int launch(const cngp_recur_config *c, RecurArgs a, const RecurPlan &p, const Re
         in = copy;
     }
     const bool io16 = c->io_dtype == CNGP_F16, g16 = c->gate_dtype == CNGP_F16;
-    return io16 ? (g16 ? launch_lanes<__half, __half, BWD>(a, p, cut, s) : launch_lanes<__half, float, BWD>(a, p, cut, s))
-                : (g16 ? launch_lanes<float, __half, BWD>(a, p, cut, s) : launch_lanes<float, float, BWD>(a, p, cut, s));
+    return io16 ? (g16 ? launch_inputs<__half, __half, BWD>(a, p, cut, s) : launch_inputs<__half, float, BWD>(a, p, cut, s))
+                : (g16 ? launch_inputs<float, __half, BWD>(a, p, cut, s) : launch_inputs<float, float, BWD>(a, p, cut, s));
 }
 
 // One channel to a lane, the windows as they are: more channel tiles.

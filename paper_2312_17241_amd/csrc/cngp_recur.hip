@@ -4,7 +4,6 @@
 //     da_t = dh_t (h_{t-1} [- x_t])     log gates: times a_t        dh0 = a_0 dh_0
 #include <algorithm>
 #include <cstdint>
-#include <initializer_list>
 
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
@@ -114,24 +113,24 @@ struct Cut {
     float   *piece_a, *piece_b, *carry;  // [K][C]
     int32_t *piece_cut;                  // [K]
     int      exact;
-    int      vec;                        // narrow rows: arrays start on 16-byte boundaries
 };
 
-template <typename T, int V>
-struct alignas(V == 3 ? sizeof(T) : sizeof(T) * V) Vec { T e[V]; };
-
+// V neighbouring values at once, on whatever boundary they start: global memory takes that, the compiler makes one access of it.
+template <typename T, int N>
+struct Run { T e[N]; };
 template <typename T, int V>
 __device__ __forceinline__ void load_vec(float (&out)[V], const T *p) {
-    const Vec<T, V> t = *reinterpret_cast<const Vec<T, V> *>(p);
+    Run<T, V> t;
+    __builtin_memcpy(&t, p, sizeof t);
 #pragma unroll
-    for (int v = 0; v < V; ++v) out[v] = load(&t.e[v], 0);
+    for (int v = 0; v < V; ++v) out[v] = load(t.e, v);
 }
 template <typename T, int V>
 __device__ __forceinline__ void store_vec(T *p, const float (&in)[V]) {
-    Vec<T, V> t;
+    Run<T, V> t;
 #pragma unroll
-    for (int v = 0; v < V; ++v) store(&t.e[v], 0, in[v]);
-    *reinterpret_cast<Vec<T, V> *>(p) = t;
+    for (int v = 0; v < V; ++v) store(t.e, v, in[v]);
+    __builtin_memcpy(p, &t, sizeof t);
 }
 
 // Where a tile's rows lie.  Row j of a lane is memory row low + mine + j, or low + mine - j taken backwards; `low` is the same for
@@ -162,12 +161,56 @@ __device__ __forceinline__ void load_rows(float (&out)[RB][V], const void *array
     }
 }
 
+// A lane that holds all V values of its rows (CL = 1) reads its RB rows as one run of RB * V neighbouring values, 16 bytes at a time and
+// turns them round when the rows are taken backwards.
+template <typename T, int RB, int V>
+__device__ __forceinline__ void load_run(float (&out)[RB][V], const T *lowest, const bool back)
+{
+    Run<T, RB * V> raw;
+    __builtin_memcpy(&raw, lowest, sizeof raw);
+#pragma unroll
+    for (int j = 0; j < RB; ++j)
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const float f = load(&raw.e[j * V + v], 0), b = load(&raw.e[(RB - 1 - j) * V + v], 0);
+            out[j][v] = back ? b : f;
+        }
+}
+template <typename T, int RB, int V>
+__device__ __forceinline__ void store_run(T *lowest, const float (&in)[RB][V], const bool back)
+{
+    Run<T, RB * V> raw;
+#pragma unroll
+    for (int j = 0; j < RB; ++j)
+#pragma unroll
+        for (int v = 0; v < V; ++v) store(&raw.e[j * V + v], 0, back ? in[RB - 1 - j][v] : in[j][v]);
+    __builtin_memcpy(lowest, &raw, sizeof raw);
+}
+
+// As load_rows for such a lane: its run if that lies inside the array, else row by row.  Rows outside [p0, p1) hold anything.
+template <typename T, int RB, int V>
+__device__ __forceinline__ void load_narrow(float (&out)[RB][V], const void *array, const Place &at, const bool whole, const int64_t N,
+                                            const int64_t pr, const int64_t p0, const int64_t p1)
+{
+    const int64_t lowest = at.low + (int64_t)at.mine - (at.dir < 0 ? RB - 1 : 0);
+    if (whole || (lowest >= 0 && lowest + RB <= N)) {
+        load_run<T, RB, V>(out, (const T *)array + lowest * V, at.dir < 0);
+    } else {
+#pragma unroll
+        for (int j = 0; j < RB; ++j) {
+            const int64_t p = pr + j < p0 ? p0 : pr + j < p1 ? pr + j : p1 - 1;
+            load_vec<T, V>(out[j], (const T *)array + (at.low + (int64_t)at.mine + at.dir * (p - pr)) * V);
+        }
+    }
+}
+
 // PIECE: only the composed map of the rows that the next window continues, for `carry`; else the outputs.
 // CL lanes side by side hold V channels each of a row, RB rows each.
 template <typename Io, typename Gate, int BLOCK, int CL, int V, int RB, bool SHARED, bool MIX, bool BWD, bool PIECE>
 __global__ __launch_bounds__(BLOCK) void recur_scan_kernel(const RecurArgs a, const Cut cut)
 {
     constexpr int RL = BLOCK / CL, TR = RL * RB, W = BLOCK / 64, GV = SHARED ? 1 : V;
+    constexpr bool NARROW = CL == 1;                           // a lane holds all channels
     static_assert(kFlagRows % TR == 0 && 32 % RB == 0, "a tile's marks lie in one block of them, a lane's in one word");
     __shared__ uint32_t bits_first[PIECE ? 1 : kFlagRows / 32], bits_last[PIECE ? 1 : kFlagRows / 32];
     __shared__ int32_t  mark_first[PIECE ? 1 : kFlagRows], mark_last[PIECE ? 1 : kFlagRows];     // sequence (in order taken), where the bit is set
@@ -275,9 +318,11 @@ __global__ __launch_bounds__(BLOCK) void recur_scan_kernel(const RecurArgs a, co
 
         // gates and what comes in: x, or dy
         float g[RB][GV], in[RB][V], share[MIX ? RB : 1][GV], left[BWD && !PIECE ? RB : 1][V];
-        load_rows<Gate, RB, GV>(g, a.gate, at, gw, gc, whole, pr, p0, p1);
+        if constexpr (NARROW) load_narrow<Gate, RB, GV>(g, a.gate, at, whole, a.N, pr, p0, p1);
+        else load_rows<Gate, RB, GV>(g, a.gate, at, gw, gc, whole, pr, p0, p1);
         if (!BWD || a.dy) {
-            load_rows<Io, RB, V>(in, BWD ? a.dy : a.x, at, a.C, c, whole, pr, p0, p1);
+            if constexpr (NARROW) load_narrow<Io, RB, V>(in, BWD ? a.dy : a.x, at, whole, a.N, pr, p0, p1);
+            else load_rows<Io, RB, V>(in, BWD ? a.dy : a.x, at, a.C, c, whole, pr, p0, p1);
         } else {
 #pragma unroll
             for (int j = 0; j < RB; ++j)
@@ -289,8 +334,13 @@ __global__ __launch_bounds__(BLOCK) void recur_scan_kernel(const RecurArgs a, co
             const int64_t end = p1 + 1 <= a.N ? p1 + 1 : p1;
             const Place   next{at.low + dir, at.mine, dir};
             const bool    all = pt + TR + 1 <= end;
-            if (a.y_f32) load_rows<float, RB, V>(left, a.y, next, a.C, c, all, pr + 1, p0, end);
-            else load_rows<Io, RB, V>(left, a.y, next, a.C, c, all, pr + 1, p0, end);
+            if constexpr (NARROW) {
+                if (a.y_f32) load_narrow<float, RB, V>(left, a.y, next, all, a.N, pr + 1, p0, end);
+                else load_narrow<Io, RB, V>(left, a.y, next, all, a.N, pr + 1, p0, end);
+            } else {
+                if (a.y_f32) load_rows<float, RB, V>(left, a.y, next, a.C, c, all, pr + 1, p0, end);
+                else load_rows<Io, RB, V>(left, a.y, next, a.C, c, all, pr + 1, p0, end);
+            }
             if (__any(last != 0)) {
                 float h[RB][V];
 #pragma unroll
@@ -309,7 +359,8 @@ __global__ __launch_bounds__(BLOCK) void recur_scan_kernel(const RecurArgs a, co
             }
             if (MIX) {
                 float x[RB][V];
-                load_rows<Io, RB, V>(x, a.x, at, a.C, c, whole, pr, p0, p1);
+                if constexpr (NARROW) load_narrow<Io, RB, V>(x, a.x, at, whole, a.N, pr, p0, p1);
+                else load_rows<Io, RB, V>(x, a.x, at, a.C, c, whole, pr, p0, p1);
 #pragma unroll
                 for (int j = 0; j < RB; ++j)
 #pragma unroll
@@ -355,9 +406,11 @@ __global__ __launch_bounds__(BLOCK) void recur_scan_kernel(const RecurArgs a, co
                 }
         }
 
-        // this lane's rows as one map, then those of the lanes before it
+        // this lane's rows as one map, then those of the lanes before it: a lane takes in what lies before it until a sequence starts
         float A[GV], B[V];
-        int   gone = first != 0;                               // whether what came before is forgotten
+        const uint64_t starts = PIECE ? 0 : __ballot(first != 0);
+        const uint64_t upto = starts & (~0ull >> (63 - (lane | (CL - 1))));
+        const int      since = upto ? (63 - __clzll(upto)) / CL : -1, mine = lane / CL;     // last lane of rows, up to this one, with a start
 #pragma unroll
         for (int v = 0; v < GV; ++v) A[v] = 1.0f;
 #pragma unroll
@@ -374,27 +427,24 @@ __global__ __launch_bounds__(BLOCK) void recur_scan_kernel(const RecurArgs a, co
             for (int v = 0; v < GV; ++v) A[v] *= g[j][v];
         }
 #pragma unroll
-        for (int d = CL; d < 64; d <<= 1) {
-            const int gl = __shfl_up(gone, d, 64);
-            float     Al[GV], Bl[V];
+        for (int d = 1; d < 64 / CL; d <<= 1) {
+            float Al[GV], Bl[V];
 #pragma unroll
-            for (int v = 0; v < GV; ++v) Al[v] = __shfl_up(A[v], d, 64);
+            for (int v = 0; v < GV; ++v) Al[v] = __shfl_up(A[v], d * CL, 64);
 #pragma unroll
-            for (int v = 0; v < V; ++v) Bl[v] = __shfl_up(B[v], d, 64);
-            if (lane >= d) {
+            for (int v = 0; v < V; ++v) Bl[v] = __shfl_up(B[v], d * CL, 64);
+            const bool joins = mine >= d && since <= mine - d;
 #pragma unroll
-                for (int v = 0; v < V; ++v) B[v] = gone ? B[v] : fmaf(A[SHARED ? 0 : v], Bl[v], B[v]);
+            for (int v = 0; v < V; ++v) B[v] = joins ? fmaf(A[SHARED ? 0 : v], Bl[v], B[v]) : B[v];
 #pragma unroll
-                for (int v = 0; v < GV; ++v) A[v] *= Al[v];
-                gone |= gl;
-            }
+            for (int v = 0; v < GV; ++v) A[v] = joins ? A[v] * Al[v] : A[v];
         }
         if (lane >= 64 - CL) {
 #pragma unroll
             for (int v = 0; v < GV; ++v) tot_a[buf][w][cl * GV + v] = A[v];
 #pragma unroll
             for (int v = 0; v < V; ++v) tot_b[buf][w][cl * V + v] = B[v];
-            if (lane == 63) tot_cut[buf][w] = gone;
+            if (lane == 63) tot_cut[buf][w] = starts != 0;
         }
         __syncthreads();
         float h[V];
@@ -418,63 +468,92 @@ __global__ __launch_bounds__(BLOCK) void recur_scan_kernel(const RecurArgs a, co
         buf ^= 1;
         if (PIECE) continue;
         {
-            const int ge = __shfl_up(gone, CL, 64);
-            float     Ae[GV];
+            const bool forget = (starts & ((1ull << (mine * CL)) - 1ull)) != 0;
+            float      Ae[GV];
 #pragma unroll
             for (int v = 0; v < GV; ++v) Ae[v] = __shfl_up(A[v], CL, 64);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const float Be = __shfl_up(B[v], CL, 64);
-                if (lane >= CL) h[v] = ge ? Be : fmaf(Ae[SHARED ? 0 : v], h[v], Be);
+                if (lane >= CL) h[v] = forget ? Be : fmaf(Ae[SHARED ? 0 : v], h[v], Be);
             }
         }
 
         // the rows once more, now with the state that reaches them
         const uint32_t put = c_ok ? live : 0u;
-        const int64_t  row0 = at.low + at.mine;
+        const int64_t  row0 = at.low + (int64_t)at.mine;
+        float          slope[BWD ? RB : 1][GV];
 #pragma unroll
         for (int j = 0; j < RB; ++j) {
-            const bool    f = (first >> j) & 1u, ok = (put >> j) & 1u;
-            const int64_t r = row0 + dir * j;
-            if constexpr (!BWD) {
+            const bool f = (first >> j) & 1u;
+            float      sum = 0.0f;
 #pragma unroll
-                for (int v = 0; v < V; ++v) h[v] = f ? in[j][v] : fmaf(g[j][SHARED ? 0 : v], h[v], in[j][v]);
-                if (a.out_y && ok) {
-                    if (a.y_f32) store_vec<float, V>((float *)a.out_y + r * a.C + c, h);
-                    else store_vec<Io, V>((Io *)a.out_y + r * a.C + c, h);
-                }
-                if ((last >> j) & 1u) {
-                    const int64_t q = mark_last[(uint32_t)(pr - flags_from) + j];
-                    if (ok && a.last) store_vec<float, V>(a.last + o.sequence(q) * a.C + c, h);
-                }
-            } else {
-                float dx[V], slope[V];
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const float gj = g[j][SHARED ? 0 : v];
+            for (int v = 0; v < V; ++v) {
+                const float gj = g[j][SHARED ? 0 : v];
+                if constexpr (!BWD) {
+                    h[v] = f ? in[j][v] : fmaf(gj, h[v], in[j][v]);
+                    in[j][v] = h[v];                           // now the output
+                } else {
                     const float dh = (f ? 0.0f : h[v]) + in[j][v];
-                    dx[v] = MIX ? share[MIX ? j : 0][SHARED ? 0 : v] * dh : dh;
-                    slope[v] = dh * left[j][v];
-                    if (log_gate) slope[v] *= gj;
+                    const float da = dh * left[j][v];
+                    in[j][v] = MIX ? share[MIX ? j : 0][SHARED ? 0 : v] * dh : dh;
+                    if (!SHARED) slope[j][SHARED ? 0 : v] = log_gate ? da * gj : da;
+                    else sum += c_ok ? da : 0.0f;
                     h[v] = gj * dh;
                 }
-                if (ok) store_vec<Io, V>((Io *)a.dx + r * a.C + c, dx);
-                if constexpr (SHARED) {
-                    float sum = c_ok ? slope[0] : 0.0f;
+            }
+            if constexpr (BWD && SHARED) {
 #pragma unroll
-                    for (int v = 1; v < V; ++v) sum += c_ok ? slope[v] : 0.0f;
-#pragma unroll
-                    for (int d = 1; d < CL; d <<= 1) sum += __shfl_xor(sum, d, 64);
-                    if (cl == 0 && ((live >> j) & 1u)) {
-                        if (a.slope) a.slope[(int64_t)tile_c * a.N + r] = sum;
-                        else store((Gate *)a.dgate, r, sum);
-                    }
-                } else if (ok) {
-                    store_vec<Gate, V>((Gate *)a.dgate + r * a.C + c, slope);
+                for (int d = 1; d < CL; d <<= 1) sum += __shfl_xor(sum, d, 64);
+                slope[j][0] = log_gate ? sum * g[j][0] : sum;
+            }
+            if ((last >> j) & 1u) {
+                float        *to = BWD ? a.dh0 : a.last;
+                const int64_t q = mark_last[(uint32_t)(pr - flags_from) + j];
+                if (c_ok && to) store_vec<float, V>(to + o.sequence(q) * a.C + c, h);
+            }
+        }
+        if constexpr (NARROW) {
+            const int64_t lowest = row0 - (o.back ? RB - 1 : 0);
+            if (live == (1u << RB) - 1u) {
+                if constexpr (BWD) {
+                    store_run<Io, RB, V>((Io *)a.dx + lowest * V, in, o.back);
+                    store_run<Gate, RB, GV>((Gate *)a.dgate + lowest * GV, slope, o.back);
+                } else if (a.out_y) {
+                    if (a.y_f32) store_run<float, RB, V>((float *)a.out_y + lowest * V, in, o.back);
+                    else store_run<Io, RB, V>((Io *)a.out_y + lowest * V, in, o.back);
                 }
-                if ((last >> j) & 1u) {
-                    const int64_t q = mark_last[(uint32_t)(pr - flags_from) + j];
-                    if (ok && a.dh0) store_vec<float, V>(a.dh0 + o.sequence(q) * a.C + c, h);
+            } else if (live) {
+#pragma unroll
+                for (int j = 0; j < RB; ++j) {
+                    if (!((live >> j) & 1u)) continue;
+                    const int64_t r = row0 + dir * j;
+                    if constexpr (BWD) {
+                        store_vec<Io, V>((Io *)a.dx + r * V, in[j]);
+                        store_vec<Gate, GV>((Gate *)a.dgate + r * GV, slope[j]);
+                    } else if (a.out_y) {
+                        if (a.y_f32) store_vec<float, V>((float *)a.out_y + r * V, in[j]);
+                        else store_vec<Io, V>((Io *)a.out_y + r * V, in[j]);
+                    }
+                }
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < RB; ++j) {
+                const int64_t r = row0 + dir * j;
+                const bool    ok = (put >> j) & 1u;
+                if constexpr (!BWD) {
+                    if (!a.out_y || !ok) continue;
+                    if (a.y_f32) store_vec<float, V>((float *)a.out_y + r * a.C + c, in[j]);
+                    else store_vec<Io, V>((Io *)a.out_y + r * a.C + c, in[j]);
+                } else {
+                    if (ok) store_vec<Io, V>((Io *)a.dx + r * a.C + c, in[j]);
+                    if constexpr (!SHARED) {
+                        if (ok) store_vec<Gate, V>((Gate *)a.dgate + r * a.C + c, slope[j]);
+                    } else if (cl == 0 && ((live >> j) & 1u)) {
+                        if (a.slope) a.slope[(int64_t)tile_c * a.N + r] = slope[j][0];
+                        else store((Gate *)a.dgate, r, slope[j][0]);
+                    }
                 }
             }
         }
@@ -578,30 +657,42 @@ RecurArgs args_of(const cngp_recur_config *c, const void *gate, const void *x, i
 // How a call is cut.  CL lanes side by side hold V channels each: as many as there are channels, at most 32 (a row of a tile is then a
 // 128-byte line of fp32).
 struct RecurPlan {
-    int      CL, V, tiles;               // channel tiles
+    int      CL, V, block, tiles;        // channel tiles
     int64_t  R;                          // rows per window
     uint32_t K;                          // windows
     bool     exact;                      // long sequences are cut at the windows' edges
 };
 
-constexpr int     kRowsEach = 8;          // rows of a tile per lane
-constexpr int64_t kEnoughGroups = 2048;  // workgroups that fill the chip's 256 CUs with eight each
+constexpr int     kRowsEach = 8, kRowsNarrow = 4;     // rows of a tile per lane; where a lane holds all channels
+constexpr int     kWideBlock = 512;
+constexpr int64_t kEnoughGroups = 2048;               // workgroups that fill the chip's 256 CUs with eight each
 
 RecurPlan plan_of(const cngp_recur_config *c, int64_t N, int64_t S, bool ragged) {
     RecurPlan p{};
-    p.CL = c->channels == 1 ? 1 : c->channels <= 4 ? 4 : c->channels <= 16 ? 16 : 32;
-    p.V = c->channels > 32 && c->channels % 2 == 0 ? 2 : 1;
-    p.tiles = (c->channels + p.CL * p.V - 1) / (p.CL * p.V);
-    const int64_t tile_rows = kRecurBlock / p.CL * kRowsEach;
+    const int C = c->channels;
+    p.CL = C <= 4 ? 1 : C <= 16 ? 16 : 32;
+    p.V = C <= 4 ? C : C > 32 && C % 2 == 0 ? 2 : 1;
+    p.block = kRecurBlock;
+    p.tiles = (C + p.CL * p.V - 1) / (p.CL * p.V);
+    const int64_t tile_rows = kRecurBlock / p.CL * (p.CL == 1 ? kRowsNarrow : kRowsEach);
     const int64_t mean = S ? (N + S - 1) / S : 0;
+    const int64_t longest = !ragged ? mean : c->longest ? std::min<int64_t>(c->longest, N) : 4 * mean;
     // windows that give every CU eight workgroups, of whole tiles
     int64_t R = (N * p.tiles + kEnoughGroups - 1) / kEnoughGroups;
     R = std::max<int64_t>((R + tile_rows - 1) / tile_rows * tile_rows, tile_rows);
     // sequences that are no longer than a few windows stay whole: one launch, every input read once.  Longer ones are cut
-    const int64_t longest = !ragged ? mean : c->longest ? std::min<int64_t>(c->longest, N) : 4 * mean;
     p.exact = longest > 4 * R;
+    if (p.exact && p.V == 2 && !ragged && S * ((C + 31) / 32) >= 192) {
+        // enough sequences by channels to give most CUs one of 32 channels, walked by eight wavefronts: whole after all
+        p.CL = 16;
+        p.block = kWideBlock;
+        p.tiles = (C + 31) / 32;
+        p.exact = false;
+        R = mean;
+    }
     if (p.exact) R = std::max(R, ((N + kMostWindows - 1) / kMostWindows + tile_rows - 1) / tile_rows * tile_rows);
-    if (!p.exact && !ragged) R = std::max<int64_t>((R + mean / 2) / std::max<int64_t>(mean, 1), 1) * mean;
+    else if (!ragged) R = std::max<int64_t>((R + mean / 2) / std::max<int64_t>(mean, 1), 1) * mean;
+    else if (2 * mean < R) R -= 2 * mean;      // a window's last sequence reaches over its edge: that still fits its tiles
     p.R = std::max<int64_t>(R, 1);
     p.K = (uint32_t)std::max<int64_t>((N + p.R - 1) / p.R, 1);
     return p;
@@ -616,8 +707,7 @@ RecurSpace space_of(const cngp_recur_config *c, const RecurPlan &p, int64_t N, i
     const size_t C = (size_t)c->channels;
     const bool   bwd = call & CNGP_RECUR_CALL_BWD;
     s.y = take(bwd && (call & CNGP_RECUR_CALL_NO_Y), (size_t)N * C * 4);
-    const int singles = (c->channels + p.CL - 1) / p.CL;       // tiles of one channel to a lane, for arrays that are not aligned
-    s.slope = take(bwd && c->gate_channels == 1 && singles > 1, (size_t)N * (size_t)singles * 4);
+    s.slope = take(bwd && c->gate_channels == 1 && p.tiles > 1, (size_t)N * (size_t)p.tiles * 4);
     s.piece_a = take(p.exact, p.K * C * 4);
     s.piece_b = take(p.exact, p.K * C * 4);
     s.carry = take(p.exact, p.K * C * 4);
@@ -627,32 +717,45 @@ RecurSpace space_of(const cngp_recur_config *c, const RecurPlan &p, int64_t N, i
     return s;
 }
 
-template <typename Io, typename Gate, int CL, int V, bool SHARED, bool MIX, bool BWD>
+template <typename Io, typename Gate, int BLOCK, int CL, int V, bool SHARED, bool MIX, bool BWD>
 int launch_scan(const RecurArgs &a, const RecurPlan &p, const Cut &cut, hipStream_t s) {
+    constexpr int  RB = CL == 1 ? kRowsNarrow : kRowsEach;
     const unsigned groups = cut.K * (unsigned)p.tiles;
-    if (cut.exact) {
-        {
-            LaunchTimer t(s, BWD ? K_RECUR_BWD : K_RECUR_FWD);
-            recur_scan_kernel<Io, Gate, kRecurBlock, CL, V, kRowsEach, SHARED, MIX, BWD, true><<<groups, kRecurBlock, 0, s>>>(a, cut);
-            if (int rc = launch_status("recur_scan_kernel (pieces)")) return rc;
+    if constexpr (BLOCK == kRecurBlock) {
+        if (cut.exact) {
+            {
+                LaunchTimer t(s, BWD ? K_RECUR_BWD : K_RECUR_FWD);
+                recur_scan_kernel<Io, Gate, BLOCK, CL, V, RB, SHARED, MIX, BWD, true><<<groups, BLOCK, 0, s>>>(a, cut);
+                if (int rc = launch_status("recur_scan_kernel (pieces)")) return rc;
+            }
+            LaunchTimer t(s, K_RECUR_CARRY);
+            recur_carry_kernel<<<(unsigned)((a.C + kCarryChannels - 1) / kCarryChannels), kCarryChannels * kCarryLanes, 0, s>>>(cut, a.C);
+            if (int rc = launch_status("recur_carry_kernel")) return rc;
         }
-        LaunchTimer t(s, K_RECUR_CARRY);
-        recur_carry_kernel<<<(unsigned)((a.C + kCarryChannels - 1) / kCarryChannels), kCarryChannels * kCarryLanes, 0, s>>>(cut, a.C);
-        if (int rc = launch_status("recur_carry_kernel")) return rc;
     }
     LaunchTimer t(s, BWD ? K_RECUR_BWD : K_RECUR_FWD);
-    recur_scan_kernel<Io, Gate, kRecurBlock, CL, V, kRowsEach, SHARED, MIX, BWD, false><<<groups, kRecurBlock, 0, s>>>(a, cut);
+    recur_scan_kernel<Io, Gate, BLOCK, CL, V, RB, SHARED, MIX, BWD, false><<<groups, BLOCK, 0, s>>>(a, cut);
     return launch_status("recur_scan_kernel");
 }
 
 template <typename Io, typename Gate, bool MIX, bool BWD>
 int launch_lanes(const RecurArgs &a, const RecurPlan &p, const Cut &cut, hipStream_t s) {
     const bool shared = a.G == 1;
-    if (p.CL == 1) return launch_scan<Io, Gate, 1, 1, true, MIX, BWD>(a, p, cut, s);
-    if (p.CL == 4) return shared ? launch_scan<Io, Gate, 4, 1, true, MIX, BWD>(a, p, cut, s) : launch_scan<Io, Gate, 4, 1, false, MIX, BWD>(a, p, cut, s);
-    if (p.CL == 16) return shared ? launch_scan<Io, Gate, 16, 1, true, MIX, BWD>(a, p, cut, s) : launch_scan<Io, Gate, 16, 1, false, MIX, BWD>(a, p, cut, s);
-    if (p.V == 1) return shared ? launch_scan<Io, Gate, 32, 1, true, MIX, BWD>(a, p, cut, s) : launch_scan<Io, Gate, 32, 1, false, MIX, BWD>(a, p, cut, s);
-    return shared ? launch_scan<Io, Gate, 32, 2, true, MIX, BWD>(a, p, cut, s) : launch_scan<Io, Gate, 32, 2, false, MIX, BWD>(a, p, cut, s);
+#define CNGP_RECUR(BLOCK, CL, V) \
+    return shared ? launch_scan<Io, Gate, BLOCK, CL, V, true, MIX, BWD>(a, p, cut, s) : launch_scan<Io, Gate, BLOCK, CL, V, false, MIX, BWD>(a, p, cut, s)
+    if (p.CL == 1) {
+        if (a.C == 1) return launch_scan<Io, Gate, kRecurBlock, 1, 1, true, MIX, BWD>(a, p, cut, s);
+        if (a.C == 2) CNGP_RECUR(kRecurBlock, 1, 2);
+        if (a.C == 3) CNGP_RECUR(kRecurBlock, 1, 3);
+        CNGP_RECUR(kRecurBlock, 1, 4);
+    }
+    if (p.block == kWideBlock) {
+        CNGP_RECUR(kWideBlock, 16, 2);
+    }
+    if (p.CL == 16) CNGP_RECUR(kRecurBlock, 16, 1);
+    if (p.V == 1) CNGP_RECUR(kRecurBlock, 32, 1);
+    CNGP_RECUR(kRecurBlock, 32, 2);
+#undef CNGP_RECUR
 }
 
 template <typename Io, typename Gate, bool BWD>
@@ -665,7 +768,7 @@ int launch_inputs(const RecurArgs &a, const RecurPlan &p, const Cut &cut, hipStr
 template <bool BWD>
 int launch(const cngp_recur_config *c, RecurArgs a, const RecurPlan &p, const RecurSpace &sp, char *ws, hipStream_t s) {
     if ((int64_t)p.K * p.tiles > 0x7fffffffLL) return CNGP_ERR_UNSUPPORTED;
-    Cut cut{p.R, p.K, (float *)(ws + sp.piece_a), (float *)(ws + sp.piece_b), (float *)(ws + sp.carry), (int32_t *)(ws + sp.piece_cut), p.exact, 0};
+    Cut cut{p.R, p.K, (float *)(ws + sp.piece_a), (float *)(ws + sp.piece_b), (float *)(ws + sp.carry), (int32_t *)(ws + sp.piece_cut), p.exact};
     const float *&in = BWD ? a.dlast : a.h0;
     float        *out = BWD ? a.dh0 : a.last;
     if (p.exact && in && in == out) {
@@ -679,19 +782,6 @@ int launch(const cngp_recur_config *c, RecurArgs a, const RecurPlan &p, const Re
     const bool io16 = c->io_dtype == CNGP_F16, g16 = c->gate_dtype == CNGP_F16;
     return io16 ? (g16 ? launch_inputs<__half, __half, BWD>(a, p, cut, s) : launch_inputs<__half, float, BWD>(a, p, cut, s))
                 : (g16 ? launch_inputs<float, __half, BWD>(a, p, cut, s) : launch_inputs<float, float, BWD>(a, p, cut, s));
-}
-
-// One channel to a lane, the windows as they are: more channel tiles.
-void single_channels(const cngp_recur_config *c, RecurPlan &p) {
-    p.V = 1;
-    p.tiles = (c->channels + p.CL - 1) / p.CL;
-}
-
-// Two channels to a lane need arrays that start on a multiple of two values.
-bool pairs_fit(std::initializer_list<const void *> arrays) {
-    for (const void *p : arrays)
-        if ((uintptr_t)p & 7u) return false;
-    return true;
 }
 
 int pass_states(const float *in, float *out, int64_t n, hipStream_t s) {      // no rows at all
@@ -717,12 +807,11 @@ int cngp_recur_fwd(const cngp_recur_config *cfg, const void *gate, const void *x
     if (N && (!gate || !x || (!last && !y))) return CNGP_ERR_NULL;
     hipStream_t s = (hipStream_t)stream;
     if (N == 0) return pass_states(h0, last, sequences * cfg->channels, s);
-    RecurPlan        p = plan_of(cfg, N, sequences, offsets != nullptr);
+    const RecurPlan  p = plan_of(cfg, N, sequences, offsets != nullptr);
     const RecurSpace sp = space_of(cfg, p, N, sequences, offsets ? CNGP_RECUR_CALL_RAGGED : 0);
     if (sp.bytes && (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < sp.bytes)) return CNGP_ERR_WORKSPACE;
     RecurArgs a = args_of(cfg, gate, x, N, offsets, sequences, h0);
     a.out_y = y; a.last = last;
-    if (p.V == 2 && !pairs_fit({gate, x, h0, y, last})) single_channels(cfg, p);
     return launch<false>(cfg, a, p, sp, (char *)workspace, s);
 }
 
@@ -734,12 +823,11 @@ int cngp_recur_bwd(const cngp_recur_config *cfg, const void *gate, const void *x
     if (N && (!gate || !x || !dgate || !dx || (!dy && !dlast))) return CNGP_ERR_NULL;
     hipStream_t s = (hipStream_t)stream;
     if (N == 0) return pass_states(dlast, dh0, sequences * cfg->channels, s);
-    RecurPlan        p = plan_of(cfg, N, sequences, offsets != nullptr);
+    const RecurPlan  p = plan_of(cfg, N, sequences, offsets != nullptr);
     const uint32_t   call = CNGP_RECUR_CALL_BWD | (offsets ? CNGP_RECUR_CALL_RAGGED : 0) | (y ? 0 : CNGP_RECUR_CALL_NO_Y);
     const RecurSpace sp = space_of(cfg, p, N, sequences, call);
     char            *ws = (char *)workspace;
     if (sp.bytes && (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < sp.bytes)) return CNGP_ERR_WORKSPACE;
-    if (p.V == 2 && !pairs_fit({gate, x, h0, y, dy, dlast, dgate, dx, dh0})) single_channels(cfg, p);
     RecurArgs a = args_of(cfg, gate, x, N, offsets, sequences, h0);
     a.y = y;
     if (!y) {

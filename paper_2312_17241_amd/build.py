@@ -11,8 +11,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcngp.so")
-SOURCES = ["cngp_api.hip", "cngp_sort.hip", "cngp_recur.hip", "cngp_embed.hip", "cngp_balance.hip"]
-HEADERS = ["cngp_launch.h", "cngp_radix.h", "cngp_device.h", "cngp_kernels.h", "cngp_fwd_level.h", "cngp_bwd_sliced.h", "cngp_bwd_binned.h", "cngp_bwd_merge.h", "cngp_bwd_runs.h", "cngp_optim.h", "cngp_mlp.h", "cngp_rates.h", os.path.join("..", "..", "include", "cngp.h")]
+SOURCES = ["cngp_api.hip", "cngp_sort.hip", "cngp_recur.hip", "cngp_recur_fwd.hip", "cngp_recur_bwd.hip", "cngp_embed.hip", "cngp_balance.hip"]
+HEADERS = ["cngp_launch.h", "cngp_radix.h", "cngp_recur.h", "cngp_recur_scan.h", "cngp_device.h", "cngp_kernels.h", "cngp_fwd_level.h", "cngp_bwd_sliced.h", "cngp_bwd_binned.h", "cngp_bwd_merge.h", "cngp_bwd_runs.h", "cngp_optim.h", "cngp_mlp.h", "cngp_rates.h", os.path.join("..", "..", "include", "cngp.h")]
 
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-munsafe-fp-atomics",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wall", "-Wno-unused-function"]

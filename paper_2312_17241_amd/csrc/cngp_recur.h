@@ -1,0 +1,115 @@
+// Gated linear recurrence h_t = a_t h_{t-1} + v_t over the rows of sequences, and its gradient.
+//
+//     dh_t = dy_t + a_{t+1} dh_{t+1} (+ dlast at the last row)      dx = dh, or (1 - a) dh with mixed inputs
+//     da_t = dh_t (h_{t-1} [- x_t])     log gates: times a_t        dh0 = a_0 dh_0
+#pragma once
+#include <algorithm>
+#include <cstdint>
+
+#include <hip/hip_fp16.h>
+#include <hip/hip_runtime.h>
+
+#include "cngp_launch.h"
+
+namespace cngp {
+
+constexpr int kRecurBlock = 256;
+constexpr int kRowsEach = 8;             // rows of a tile per lane
+constexpr int kNarrowBlock = 64;         // rows of up to four channels, each whole in a lane: a wavefront by itself
+
+constexpr int kWideBlock = 512;          // workgroups that walk whole long sequences
+
+__device__ __forceinline__ float load(const float *p, const int64_t i) { return p[i]; }
+__device__ __forceinline__ float load(const __half *p, const int64_t i) { return __half2float(p[i]); }
+__device__ __forceinline__ void store(float *p, const int64_t i, const float v) { p[i] = v; }
+__device__ __forceinline__ void store(__half *p, const int64_t i, const float v) { p[i] = __float2half_rn(v); }
+
+struct RecurArgs {
+    const void    *gate, *x;
+    const int32_t *offsets;
+    const float   *h0, *dlast;
+    const void    *y, *dy;               // backward; y_f32: y is the workspace's fp32 copy
+    void          *out_y, *dgate, *dx;
+    float         *last, *dh0;
+    float         *slope;                // backward of a gate that several channel tiles share: their sums, fp32 [tiles][N]
+    int64_t        N, S, rows_each;
+    int32_t        C, G;
+    uint32_t       flags;
+    int32_t        y_f32;
+};
+
+struct Order {
+    const int32_t *offsets;
+    int64_t        N, S, rows_each;
+    bool           back;                 // taken from the last row to the first
+    __device__ __forceinline__ int64_t at(const int64_t q) const {       // ps(q), 0 <= q <= S
+        if (!offsets) return q * rows_each;
+        int64_t o = offsets[back ? S - q : q];
+        o = o < 0 ? 0 : o > N ? N : o;
+        return back ? N - o : o;
+    }
+    __device__ __forceinline__ int64_t sequence(const int64_t q) const { return back ? S - 1 - q : q; }
+    // First q with ps(q) >= p, for two p at once (S + 1 if there is none); a wavefront calls this together, 64 probes at a time.
+    __device__ void first_from(const int64_t pa, const int64_t pb, int64_t &qa, int64_t &qb) const {
+        if (!offsets) {
+            qa = (pa + rows_each - 1) / rows_each;
+            qb = (pb + rows_each - 1) / rows_each;
+            qa = qa < S + 1 ? qa : S + 1;
+            qb = qb < S + 1 ? qb : S + 1;
+            return;
+        }
+        const int64_t lane = threadIdx.x & 63;
+        int64_t lo[2] = {0, 0}, hi[2] = {S + 1, S + 1};         // the answers lie in [lo, hi]
+        const int64_t want[2] = {pa, pb};
+        while (lo[0] < hi[0] || lo[1] < hi[1]) {
+            bool    less[2];
+            int64_t step[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                step[i] = (hi[i] - lo[i] + 63) / 64;
+                const int64_t probe = lo[i] + lane * step[i];
+                less[i] = probe < hi[i] && at(probe < S ? probe : S) < want[i];
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint64_t before = __ballot(less[i]);
+                if (!before) { hi[i] = lo[i]; continue; }
+                const int64_t last = lo[i] + (63 - __clzll(before)) * step[i];      // the last probe that lies before p
+                lo[i] = last + 1;
+                hi[i] = last + step[i] < hi[i] ? last + step[i] : hi[i];
+            }
+        }
+        qa = lo[0];
+        qb = lo[1];
+    }
+};
+
+// Windows of rows: workgroup (k, channel tile) of a launch takes the sequences that start in [k R, (k + 1) R) -- or exactly those
+// rows, where a long sequence is cut: then the state at k R comes from `carry`.
+struct Cut {
+    int64_t  R;
+    uint32_t K;
+    float   *piece_a, *piece_b, *carry;  // [K][C]
+    int32_t *piece_cut;                  // [K]
+    int      exact;
+};
+
+// How a call is cut.  CL lanes side by side hold V channels each: as many as there are channels, at most 32 (a row of a tile is then a
+// 128-byte line of fp32).
+struct RecurPlan {
+    int      CL, V, block, tiles;        // channel tiles
+    int64_t  R;                          // rows per window
+    uint32_t K;                          // windows
+    bool     exact;                      // long sequences are cut at the windows' edges
+};
+
+// Where the parts of a workspace lie.
+struct RecurSpace { size_t y, slope, piece_a, piece_b, carry, piece_cut, state, bytes; };
+// One direction's launches (cngp_recur_fwd.hip, cngp_recur_bwd.hip: the instances of the kernels are many, they are compiled side by side).
+template <bool BWD>
+int recur_launch(const cngp_recur_config *c, RecurArgs a, const RecurPlan &p, const RecurSpace &sp, char *ws, hipStream_t s);
+
+int recur_copy(const float *from, float *to, int64_t n, hipStream_t s);      // zeros without `from`
+int recur_carry(const Cut &cut, int C, hipStream_t s);                       // the state that reaches each window
+
+}  // namespace cngp

@@ -1,0 +1,857 @@
+// The scan of the gated linear recurrence: kernels for wide rows and for rows of up to four channels, and their launches.
+#pragma once
+#include "cngp_recur.h"
+
+namespace {
+
+using namespace cngp;
+
+// The gate of a row and how much of the input it lets in.  1 - exp(g) cancels for small g: there it is -g times the series of
+// (exp(g) - 1) / g to the ninth term (0.5^9 / 10! = 5e-10 below one), and exp(g) is one minus that, to the last bit.
+template <bool MIX>
+__device__ __forceinline__ void gate_of(const bool log_gate, const float g, float &a, float &in) {
+    if (!log_gate) {
+        a = g;
+        in = MIX ? 1.0f - g : 1.0f;
+        return;
+    }
+    a = expf(g);
+    in = 1.0f;
+    if (MIX) {
+        float s = fmaf(g, 1.0f / 362880.0f, 1.0f / 40320.0f);
+        s = fmaf(s, g, 1.0f / 5040.0f);
+        s = fmaf(s, g, 1.0f / 720.0f);
+        s = fmaf(s, g, 1.0f / 120.0f);
+        s = fmaf(s, g, 1.0f / 24.0f);
+        s = fmaf(s, g, 1.0f / 6.0f);
+        s = fmaf(s, g, 0.5f);
+        s = fmaf(s, g, 1.0f);
+        const bool small = fabsf(g) < 0.5f;
+        in = small ? -g * s : 1.0f - a;
+        a = small ? 1.0f - in : a;
+    }
+}
+
+// ---------------------------------------------------------------- the scan
+// A row is the map h -> a h + v, and maps compose: rows (A, B) then (a, v) give (a A, a B + v).  So a sequence need not be walked
+// row after row: a workgroup takes a tile of RL * RB rows by CL * V channels, every lane composes the maps of its RB consecutive
+// rows, the lanes of the same channels join theirs (shuffles inside a wavefront, LDS between the four), and with the state that
+// then reaches its first row each lane walks its rows once more and writes.  The loads of a tile are all in flight at once, every
+// input is read once, every output written once.
+// The backward runs the same scan the other way: with u = a_{t+1} dh_{t+1} what arrives from later rows, dh = dy + u and what goes
+// on is a dh = a u + a dy.
+// Sequences are not handled one by one: the rows of all of them lie one behind the other, and the first row of a sequence takes
+// its map from h0 (or dlast) and forgets what came before -- a flag that travels with the map, not a factor of zero, so that
+// nothing that is not finite crosses over.
+// Positions: p counts rows in the order they are taken, p = row or N - 1 - row; ps(q) is where the q-th sequence in that order starts.
+
+// A window's sequences [qa, qb) and rows [p0, p1), in the order taken.
+struct Window {
+    int64_t qa, qb, p0, p1;
+    __device__ __forceinline__ bool find(const RecurArgs &a, const Cut &cut, const Order &o, const uint32_t k) {
+        const int64_t edge0 = (int64_t)k * cut.R, edge1 = edge0 + cut.R;
+        const bool    final_window = k + 1 == cut.K;
+        o.first_from(edge0, edge1, qa, qb);
+        if (k == 0) qa = 0;
+        if (final_window || qb > a.S) qb = a.S;
+        if (cut.exact) {
+            const int64_t lo = o.at(0), hi = o.at(a.S);
+            p0 = edge0 < lo ? lo : edge0;
+            p1 = edge1 < hi && !final_window ? edge1 : hi;
+            return true;
+        }
+        if (qa >= qb) return false;                            // no sequence starts in here
+        p0 = o.at(qa);
+        p1 = o.at(qb);
+        return true;
+    }
+    // The rows whose map the next window needs: those of the sequence that goes on in it.  False: none does, or it starts there.
+    // q: that sequence if it starts in here, else -1.
+    __device__ __forceinline__ bool piece(const RecurArgs &a, const Cut &cut, const Order &o, const uint32_t k, const bool writes, int64_t &q) {
+        q = qb - 1;
+        const bool    goes_on = k + 1 != cut.K && p1 > p0 && q >= 0 && o.at(q + 1) > p1;
+        const int64_t begin = goes_on ? o.at(q) : p1;
+        const bool    starts = !goes_on || begin >= p0;
+        if (writes) cut.piece_cut[k] = starts;
+        if (!goes_on) return false;
+        if (starts) p0 = begin;
+        else q = -1;
+        return true;
+    }
+};
+
+// V neighbouring values at once, on whatever boundary they start: global memory takes that, the compiler makes one access of it.
+template <typename T, int N>
+struct Run { T e[N]; };
+template <typename T, int V>
+__device__ __forceinline__ void load_vec(float (&out)[V], const T *p) {
+    Run<T, V> t;
+    __builtin_memcpy(&t, p, sizeof t);
+#pragma unroll
+    for (int v = 0; v < V; ++v) out[v] = load(t.e, v);
+}
+template <typename T, int V>
+__device__ __forceinline__ void store_vec(T *p, const float (&in)[V]) {
+    Run<T, V> t;
+#pragma unroll
+    for (int v = 0; v < V; ++v) store(t.e, v, in[v]);
+    __builtin_memcpy(p, &t, sizeof t);
+}
+
+// Where a tile's rows lie.  Row j of a lane is memory row low + mine + j, or low + mine - j taken backwards; `low` is the same for
+// the whole workgroup, so a load is a scalar base and a 32-bit lane offset.
+struct Place {
+    int64_t  low;
+    uint32_t mine;                       // rows
+    int      dir;                        // 1 or -1
+};
+
+// RB rows of V values each as they lie in memory, so that a tile's loads can be under way while another is worked on.
+// A lane that holds all values of its rows (NARROW) reads them as one run, 16 bytes at a time, in the order of the memory.
+template <typename T, int RB, int V, bool NARROW>
+struct Rows {
+    Run<T, RB * V> raw;
+
+    // `width` values to a row of the array, this lane's from c on.  Not a whole tile: rows outside [p0, p1) hold those of the nearest row
+    // inside, or, in a run that lies inside the N rows of the array, whatever is there.  pr: the lane's first row, in the order taken.
+    __device__ __forceinline__ void load_from(const void *array, const Place &at, const int width, const int c, const bool whole, const int64_t N,
+                                              const int64_t pr, const int64_t p0, const int64_t p1) {
+        if constexpr (NARROW) {
+            const int64_t lowest = at.low + (int64_t)at.mine - (at.dir < 0 ? RB - 1 : 0);
+            if (whole || (lowest >= 0 && lowest + RB <= N)) {
+                __builtin_memcpy(&raw, (const T *)array + lowest * V, sizeof raw);
+            } else {
+#pragma unroll
+                for (int j = 0; j < RB; ++j) {                 // row j of the run
+                    const int64_t p = pr + (at.dir < 0 ? RB - 1 - j : j), q = p < p0 ? p0 : p < p1 ? p : p1 - 1;
+                    __builtin_memcpy(&raw.e[j * V], (const T *)array + (at.low + (int64_t)at.mine + at.dir * (q - pr)) * V, sizeof(T) * V);
+                }
+            }
+        } else {
+            const uint32_t mine = at.mine * (uint32_t)width + (uint32_t)c;
+            const T       *base = (const T *)array + at.low * width;
+            if (whole) {
+#pragma unroll
+                for (int j = 0; j < RB; ++j) __builtin_memcpy(&raw.e[j * V], base + (int64_t)(at.dir * j) * width + mine, sizeof(T) * V);
+            } else {
+#pragma unroll
+                for (int j = 0; j < RB; ++j) {
+                    const int64_t p = pr + j < p0 ? p0 : pr + j < p1 ? pr + j : p1 - 1;
+                    __builtin_memcpy(&raw.e[j * V], base + (int64_t)mine + at.dir * (p - pr) * width, sizeof(T) * V);
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ float get(const int j, const int v, const bool back) const {
+        if constexpr (!NARROW) return load(raw.e, j * V + v);
+        return back ? load(raw.e, (RB - 1 - j) * V + v) : load(raw.e, j * V + v);
+    }
+};
+
+// Row j of a lane's outputs (not NARROW).
+template <typename T>
+__device__ __forceinline__ T *row_at(void *array, const Place &at, const int width, const int c, const int j) {
+    return (T *)array + (at.low + at.dir * j) * width + (at.mine * (uint32_t)width + (uint32_t)c);
+}
+template <typename T, int RB, int V>
+__device__ __forceinline__ void store_run(T *lowest, const float (&in)[RB][V], const bool back) {
+    Run<T, RB * V> raw;
+#pragma unroll
+    for (int j = 0; j < RB; ++j)
+#pragma unroll
+        for (int v = 0; v < V; ++v) store(raw.e, j * V + v, back ? in[RB - 1 - j][v] : in[j][v]);
+    __builtin_memcpy(lowest, &raw, sizeof raw);
+}
+
+// PIECE: only the composed map of the rows that the next window continues, for `carry`; else the outputs.
+// CL lanes side by side hold V channels each of a row, RB rows each.  Y: type of the states, written forward and read backward.
+template <typename Io, typename Gate, typename Y, int BLOCK, int CL, int V, int RB, bool SHARED, bool MIX, bool BWD, bool PIECE>
+__global__ __launch_bounds__(BLOCK) void recur_scan_kernel(const RecurArgs a, const Cut cut)
+{
+    constexpr int  RL = BLOCK / CL, TR = RL * RB, W = BLOCK / 64, GV = SHARED ? 1 : V;
+    constexpr int  kFlagRows = 2048;                           // rows whose first / last marks are in LDS at a time
+    static_assert(kFlagRows % TR == 0 && 32 % RB == 0, "a tile's marks lie in one block of them, a lane's in one word");
+    __shared__ uint32_t bits_first[PIECE ? 1 : kFlagRows / 32], bits_last[PIECE ? 1 : kFlagRows / 32];
+    __shared__ int32_t  mark_first[PIECE ? 1 : kFlagRows], mark_last[PIECE ? 1 : kFlagRows];     // sequence, where the bit is set
+    __shared__ float    tot_a[2][W][CL * GV], tot_b[2][W][CL * V];
+    __shared__ int      tot_cut[2][W];
+    __shared__ int      q_next;
+    const int      t = threadIdx.x, lane = t & 63, w = t >> 6, cl = t % CL, rl = t / CL;
+    const uint32_t k = blockIdx.x % cut.K, tile_c = blockIdx.x / cut.K;
+    const int      c_here = (int)tile_c * (CL * V) + cl * V;
+    const bool     c_ok = c_here < a.C;                        // V divides C
+    const int      c = c_ok ? c_here : a.C - V;                // lanes without a channel read the last ones and write nothing
+    const int      gc = SHARED ? 0 : c, gw = SHARED ? 1 : a.C;
+    const bool     log_gate = a.flags & CNGP_RECUR_LOG_GATE;
+    const Order    o{a.offsets, a.N, a.S, a.rows_each, ((a.flags & CNGP_RECUR_REVERSE) != 0) != BWD};
+    const float   *before = BWD ? a.dlast : a.h0;              // what a sequence starts from, in the order taken
+    const int      dir = o.back ? -1 : 1;
+
+    Window win;
+    if (!win.find(a, cut, o, k)) return;
+    float carry_a[GV], carry_b[V];
+#pragma unroll
+    for (int v = 0; v < GV; ++v) carry_a[v] = 1.0f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) carry_b[v] = 0.0f;
+    if (PIECE) {
+        int64_t q;
+        if (!win.piece(a, cut, o, k, t == 0 && tile_c == 0, q)) return;
+        if (q >= 0 && before) load_vec<float, V>(carry_b, before + o.sequence(q) * a.C + c);
+    } else if (cut.exact && k > 0) {
+        load_vec<float, V>(carry_b, cut.carry + (int64_t)k * a.C + c);
+    }
+    const int64_t qa = win.qa, qb = win.qb, p0 = win.p0, p1 = win.p1;
+
+    // a tile's loads: gates, what comes in (x, or dy), backward the states before the rows and, with mixed inputs, x
+    struct Tile {
+        Rows<Gate, RB, GV, false> g;
+        Rows<Io, RB, V, false>    in;
+        Rows<Y, (BWD && !PIECE ? RB : 1), V, false>         left;
+        Rows<Io, (BWD && MIX && !PIECE ? RB : 1), V, false> x;
+    };
+    const auto place = [&](const int64_t pt) {
+        return Place{o.back ? a.N - TR - pt : pt, (uint32_t)(o.back ? TR - 1 - rl * RB : rl * RB), dir};
+    };
+    const auto fetch = [&](Tile &f, const int64_t pt) {
+        const int64_t pr = pt + rl * RB;
+        const bool    whole = pt + TR <= p1;
+        const Place   at = place(pt);
+        f.g.load_from(a.gate, at, gw, gc, whole, a.N, pr, p0, p1);
+        if (!BWD || a.dy) f.in.load_from(BWD ? a.dy : a.x, at, a.C, c, whole, a.N, pr, p0, p1);
+        if constexpr (BWD && !PIECE) {
+            // the state before the row is that of the next row in the order taken (of the next window's first, at the end of this one)
+            const int64_t end = p1 + 1 <= a.N ? p1 + 1 : p1;
+            f.left.load_from(a.y, Place{at.low + dir, at.mine, dir}, a.C, c, pt + TR + 1 <= end, a.N, pr + 1, p0, end);
+            if constexpr (MIX) f.x.load_from(a.x, at, a.C, c, whole, a.N, pr, p0, p1);
+        }
+    };
+
+    int64_t q_at = PIECE ? 0 : qa > 0 ? qa - 1 : 0;            // no sequence before this one reaches p0
+    int64_t flags_from = p0;
+    int     buf = 0;
+    Tile    now, next;
+    if (p0 < p1) fetch(now, p0);
+    for (int64_t pt = p0; pt < p1 || (!PIECE && pt == p0); pt += TR) {
+        if (!PIECE && (pt - p0) % kFlagRows == 0) {
+            // marks of the rows [flags_from, flags_to): first and last rows of sequences; sequences without rows pass their state on here
+            flags_from = pt;
+            const int64_t flags_to = p1 - pt < kFlagRows ? p1 : pt + kFlagRows;
+            const bool    at_end = flags_to == p1;
+            for (int i = t; i < kFlagRows / 32; i += BLOCK) { bits_first[i] = 0; bits_last[i] = 0; }
+            if (t == 0) q_next = (int)q_at;
+            __syncthreads();
+            int furthest = (int)q_at;
+            for (int64_t q = q_at + t; q < qb; q += BLOCK) {
+                const int64_t f = o.at(q), l = o.at(q + 1);
+                if (f > flags_to || (f == flags_to && !at_end)) break;
+                if (f < l) {
+                    if (f < flags_to) furthest = (int)q;
+                    if (f >= flags_from && f < flags_to) {
+                        const int i = (int)(f - flags_from);
+                        mark_first[i] = (int32_t)o.sequence(q);
+                        atomicOr(&bits_first[i >> 5], 1u << (i & 31));
+                    }
+                    if (l > flags_from && l <= flags_to) {
+                        const int i = (int)(l - 1 - flags_from);
+                        mark_last[i] = (int32_t)o.sequence(q);
+                        atomicOr(&bits_last[i >> 5], 1u << (i & 31));
+                    }
+                } else if (f >= flags_from && q >= qa) {
+                    float        *to = BWD ? a.dh0 : a.last;
+                    const int64_t i = o.sequence(q) * a.C;
+                    for (int j = (int)tile_c * (CL * V); to && j < ((int)tile_c + 1) * (CL * V) && j < a.C; ++j) to[i + j] = before ? before[i + j] : 0.0f;
+                }
+            }
+            if (furthest > (int)q_at) atomicMax(&q_next, furthest);
+            __syncthreads();
+            q_at = q_next;
+        }
+        if (pt >= p1) break;
+
+        const int64_t pr = pt + rl * RB;                       // this lane's first row, in the order taken
+        const bool    whole = pt + TR <= p1;
+        const Place   at = place(pt);
+        uint32_t      first = 0, last = 0, live = (1u << RB) - 1u, mark0 = 0;
+        if (!whole) live = pr >= p1 ? 0u : pr + RB <= p1 ? live : (1u << (uint32_t)(p1 - pr)) - 1u;
+        if (!PIECE) {
+            mark0 = (uint32_t)(pr - flags_from);
+            first = (bits_first[mark0 >> 5] >> (mark0 & 31)) & live;
+            last = (bits_last[mark0 >> 5] >> (mark0 & 31)) & live;
+        }
+        if (pt + TR < p1) fetch(next, pt + TR);                // under way while this tile is worked on
+        // what the sequences that start in here start from; backward, what those that end in here started from
+        float      h_first[PIECE ? 1 : RB][V], h_last[BWD && !PIECE ? RB : 1][V];
+        const bool starts_here = !PIECE && __any(first != 0), ends_here = BWD && !PIECE && __any(last != 0);
+        if constexpr (!PIECE) {
+            if (starts_here && before) {
+#pragma unroll
+                for (int j = 0; j < RB; ++j)
+                    if ((first >> j) & 1u) load_vec<float, V>(h_first[j], before + (int64_t)mark_first[mark0 + j] * a.C + c);
+            }
+        }
+        if constexpr (BWD && !PIECE) {
+            if (ends_here && a.h0) {
+#pragma unroll
+                for (int j = 0; j < RB; ++j)
+                    if ((last >> j) & 1u) load_vec<float, V>(h_last[j], a.h0 + (int64_t)mark_last[mark0 + j] * a.C + c);
+            }
+        }
+
+        float g[RB][GV], in[RB][V], share[MIX ? RB : 1][GV];
+#pragma unroll
+        for (int j = 0; j < RB; ++j) {
+#pragma unroll
+            for (int v = 0; v < GV; ++v) {
+                float in_share;
+                gate_of<MIX>(log_gate, now.g.get(j, v, o.back), g[j][v], in_share);
+                if (MIX) share[MIX ? j : 0][v] = in_share;
+            }
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                in[j][v] = !BWD || a.dy ? now.in.get(j, v, o.back) : 0.0f;
+                if (MIX && !BWD) in[j][v] *= share[MIX ? j : 0][SHARED ? 0 : v];
+            }
+        }
+        if (!whole) {                                          // rows that are not there change nothing
+#pragma unroll
+            for (int j = 0; j < RB; ++j) {
+                const bool there = (live >> j) & 1u;
+#pragma unroll
+                for (int v = 0; v < GV; ++v) g[j][v] = there ? g[j][v] : 1.0f;
+#pragma unroll
+                for (int v = 0; v < V; ++v) in[j][v] = there ? in[j][v] : 0.0f;
+            }
+        }
+        if constexpr (!PIECE) {
+            if (starts_here && before) {
+#pragma unroll
+                for (int j = 0; j < RB; ++j)
+                    if ((first >> j) & 1u) {
+#pragma unroll
+                        for (int v = 0; v < V; ++v) in[j][v] = BWD ? in[j][v] + h_first[j][v] : fmaf(g[j][SHARED ? 0 : v], h_first[j][v], in[j][v]);
+                    }
+            }
+        }
+
+        // this lane's rows as one map, then those of the lanes before it: a lane takes in what lies before it until a sequence starts
+        float          A[GV], B[V];
+        const uint64_t starts = PIECE ? 0 : __ballot(first != 0);
+        const uint64_t upto = starts & (~0ull >> (63 - (lane | (CL - 1))));
+        const int      since = upto ? (63 - __clzll(upto)) / CL : -1, mine = lane / CL;     // last lane of rows, up to this one, with a start
+#pragma unroll
+        for (int v = 0; v < GV; ++v) A[v] = 1.0f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) B[v] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < RB; ++j) {
+            if (starts_here) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) B[v] = (first >> j) & 1u ? 0.0f : B[v];
+            }
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float gj = g[j][SHARED ? 0 : v];
+                B[v] = BWD ? gj * (B[v] + in[j][v]) : fmaf(gj, B[v], in[j][v]);
+            }
+#pragma unroll
+            for (int v = 0; v < GV; ++v) A[v] *= g[j][v];
+        }
+#pragma unroll
+        for (int d = 1; d < 64 / CL; d <<= 1) {
+            float Al[GV], Bl[V];
+#pragma unroll
+            for (int v = 0; v < GV; ++v) Al[v] = __shfl_up(A[v], d * CL, 64);
+#pragma unroll
+            for (int v = 0; v < V; ++v) Bl[v] = __shfl_up(B[v], d * CL, 64);
+            const bool joins = mine >= d && since <= mine - d;
+#pragma unroll
+            for (int v = 0; v < V; ++v) B[v] = joins ? fmaf(A[SHARED ? 0 : v], Bl[v], B[v]) : B[v];
+#pragma unroll
+            for (int v = 0; v < GV; ++v) A[v] = joins ? A[v] * Al[v] : A[v];
+        }
+        float h[V];
+        if (lane >= 64 - CL) {
+#pragma unroll
+            for (int v = 0; v < GV; ++v) tot_a[buf][w][cl * GV + v] = A[v];
+#pragma unroll
+            for (int v = 0; v < V; ++v) tot_b[buf][w][cl * V + v] = B[v];
+            if (lane == 63) tot_cut[buf][w] = starts != 0;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            const int forget = tot_cut[buf][i];
+            float     Ai[GV];
+#pragma unroll
+            for (int v = 0; v < GV; ++v) Ai[v] = tot_a[buf][i][cl * GV + v];
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                if (i == w) h[v] = carry_b[v];
+                const float Bi = tot_b[buf][i][cl * V + v];
+                carry_b[v] = forget ? Bi : fmaf(Ai[SHARED ? 0 : v], carry_b[v], Bi);
+            }
+            if (PIECE) {
+#pragma unroll
+                for (int v = 0; v < GV; ++v) carry_a[v] *= Ai[v];
+            }
+        }
+        buf ^= 1;
+        if constexpr (PIECE) {
+            now = next;
+            continue;
+        }
+        {
+            const bool forget = (starts & ((1ull << (mine * CL)) - 1ull)) != 0;
+            float      Ae[GV];
+#pragma unroll
+            for (int v = 0; v < GV; ++v) Ae[v] = __shfl_up(A[v], CL, 64);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float Be = __shfl_up(B[v], CL, 64);
+                if (lane >= CL) h[v] = forget ? Be : fmaf(Ae[SHARED ? 0 : v], h[v], Be);
+            }
+        }
+
+        // the rows once more, now with the state that reaches them
+        float slope[BWD ? RB : 1][GV];
+#pragma unroll
+        for (int j = 0; j < RB; ++j) {
+            if (starts_here) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) h[v] = (first >> j) & 1u ? 0.0f : h[v];
+            }
+            float sum = 0.0f;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float gj = g[j][SHARED ? 0 : v];
+                if constexpr (!BWD) {
+                    h[v] = fmaf(gj, h[v], in[j][v]);
+                    in[j][v] = h[v];                           // now the output
+                } else if constexpr (!PIECE) {
+                    float left = now.left.get(j, v, o.back);
+                    if (ends_here && ((last >> j) & 1u)) left = a.h0 ? h_last[j][v] : 0.0f;
+                    if constexpr (MIX) left -= now.x.get(j, v, o.back);
+                    const float dh = h[v] + in[j][v], da = dh * left;
+                    in[j][v] = MIX ? share[MIX ? j : 0][SHARED ? 0 : v] * dh : dh;
+                    if (!SHARED) slope[j][SHARED ? 0 : v] = log_gate ? da * gj : da;
+                    else sum += c_ok ? da : 0.0f;
+                    h[v] = gj * dh;
+                }
+            }
+            if constexpr (BWD && SHARED) {
+#pragma unroll
+                for (int d = 1; d < CL; d <<= 1) sum += __shfl_xor(sum, d, 64);
+                slope[j][0] = log_gate ? sum * g[j][0] : sum;
+            }
+            if ((last >> j) & 1u) {
+                float *to = BWD ? a.dh0 : a.last;
+                if (c_ok && to) store_vec<float, V>(to + (int64_t)mark_last[mark0 + j] * a.C + c, h);
+            }
+        }
+        constexpr uint32_t ALL = (1u << RB) - 1u;
+        const auto put = [&](const int j) {
+            if constexpr (!BWD) {
+                store_vec<Y, V>(row_at<Y>(a.out_y, at, a.C, c, j), in[j]);
+            } else {
+                store_vec<Io, V>(row_at<Io>(a.dx, at, a.C, c, j), in[j]);
+                if constexpr (!SHARED) store_vec<Gate, V>(row_at<Gate>(a.dgate, at, a.C, c, j), slope[j]);
+            }
+        };
+        if (c_ok && (BWD || a.out_y)) {
+            if (live == ALL) {
+#pragma unroll
+                for (int j = 0; j < RB; ++j) put(j);
+            } else {
+#pragma unroll
+                for (int j = 0; j < RB; ++j)
+                    if ((live >> j) & 1u) put(j);
+            }
+        }
+        if constexpr (BWD && SHARED) {
+#pragma unroll
+            for (int j = 0; j < RB; ++j)
+                if (cl == 0 && ((live >> j) & 1u)) {
+                    if (a.slope) *row_at<float>(a.slope + (int64_t)tile_c * a.N, at, 1, 0, j) = slope[j][0];
+                    else store(row_at<Gate>(a.dgate, at, 1, 0, j), 0, slope[j][0]);
+                }
+        }
+        now = next;
+        if ((pt + TR - p0) % kFlagRows == 0) __syncthreads();  // the marks are written anew
+    }
+    if (PIECE && rl == 0 && c_ok) {
+        float A[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) A[v] = carry_a[SHARED ? 0 : v];
+        store_vec<float, V>(cut.piece_a + (int64_t)k * a.C + c, A);
+        store_vec<float, V>(cut.piece_b + (int64_t)k * a.C + c, carry_b);
+    }
+}
+
+// Rows of up to four channels: a lane holds RB whole rows, a workgroup is one wavefront, so nothing is joined through LDS and no barrier
+// waits.  What bounds such rows is not their bytes but the chain of loads: where the sequences start, what they start from, the rows.
+// All three are loaded a tile ahead; the start states of a tile's first 64 sequences go through LDS to the lanes whose rows start them.
+template <typename Io, typename Gate, typename Y, int V, bool SHARED, bool MIX, bool BWD, bool PIECE>
+__global__ __launch_bounds__(64) void recur_narrow_kernel(const RecurArgs a, const Cut cut)
+{
+    constexpr int RB = kRowsEach, TR = 64 * RB, GV = SHARED ? 1 : V;
+    __shared__ __align__(16) uint32_t mark_first[PIECE ? 4 : TR], mark_last[PIECE ? 4 : TR];     // sequence (in order taken) + 1, or 0
+    __shared__ float from_s[PIECE ? 1 : 64 * V], left_s[BWD && !PIECE ? 64 * V : 1];
+    const int      lane = threadIdx.x;
+    const uint32_t k = blockIdx.x;
+    const bool     log_gate = a.flags & CNGP_RECUR_LOG_GATE;
+    const Order    o{a.offsets, a.N, a.S, a.rows_each, ((a.flags & CNGP_RECUR_REVERSE) != 0) != BWD};
+    const float   *before = BWD ? a.dlast : a.h0;              // what a sequence starts from, in the order taken
+    const int      dir = o.back ? -1 : 1;
+
+    Window win;
+    if (!win.find(a, cut, o, k)) return;
+    float carry_a[GV], carry_b[V];
+#pragma unroll
+    for (int v = 0; v < GV; ++v) carry_a[v] = 1.0f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) carry_b[v] = 0.0f;
+    if (PIECE) {
+        int64_t q;
+        if (!win.piece(a, cut, o, k, lane == 0, q)) return;
+        if (q >= 0 && before) load_vec<float, V>(carry_b, before + o.sequence(q) * V);
+    } else if (cut.exact && k > 0) {
+        load_vec<float, V>(carry_b, cut.carry + (int64_t)k * V);
+    }
+    const int64_t qa = win.qa, qb = win.qb, p0 = win.p0, p1 = win.p1;
+
+    struct Tile {
+        Rows<Gate, RB, GV, true> g;
+        Rows<Io, RB, V, true>    in;
+        Rows<Y, (BWD && !PIECE ? RB : 1), V, true>         left;
+        Rows<Io, (BWD && MIX && !PIECE ? RB : 1), V, true> x;
+        int64_t first, behind;                                 // rows of sequence q + lane
+        float   from[V], ends[BWD ? V : 1];                    // its state to start from; backward, the one it started from
+    };
+    const auto place = [&](const int64_t pt) {
+        return Place{o.back ? a.N - TR - pt : pt, (uint32_t)(o.back ? TR - 1 - lane * RB : lane * RB), dir};
+    };
+    const auto fetch_sequences = [&](Tile &f, const int64_t q) {
+        const int64_t s = q + lane < qb ? q + lane : qb - 1 > 0 ? qb - 1 : 0;
+        f.first = o.at(s);
+        f.behind = o.at(s + 1);
+        if (before) load_vec<float, V>(f.from, before + o.sequence(s) * V);
+        if (BWD && a.h0) load_vec<float, BWD ? V : 1>(f.ends, a.h0 + o.sequence(s) * V);
+    };
+    const auto fetch_rows = [&](Tile &f, const int64_t pt) {
+        const int64_t pr = pt + lane * RB;
+        const bool    whole = pt + TR <= p1;
+        const Place   at = place(pt);
+        f.g.load_from(a.gate, at, GV, 0, whole, a.N, pr, p0, p1);
+        if (!BWD || a.dy) f.in.load_from(BWD ? a.dy : a.x, at, V, 0, whole, a.N, pr, p0, p1);
+        if constexpr (BWD && !PIECE) {
+            const int64_t end = p1 + 1 <= a.N ? p1 + 1 : p1;
+            f.left.load_from(a.y, Place{at.low + dir, at.mine, dir}, V, 0, pt + TR + 1 <= end, a.N, pr + 1, p0, end);
+            if constexpr (MIX) f.x.load_from(a.x, at, V, 0, whole, a.N, pr, p0, p1);
+        }
+    };
+
+    int64_t q_at = qa > 0 ? qa - 1 : 0;                        // no sequence before this one reaches p0
+    Tile    now, next;
+    if (!PIECE) fetch_sequences(now, q_at);
+    if (p0 < p1) fetch_rows(now, p0);
+    for (int64_t pt = p0; pt < p1 || (!PIECE && pt == p0); pt += TR) {
+        const int64_t to = p1 - pt < TR ? p1 : pt + TR, q0 = q_at;
+        const bool    whole = pt + TR <= p1;
+        if (!PIECE) {
+            *reinterpret_cast<uint4 *>(mark_first + lane * RB) = make_uint4(0, 0, 0, 0);
+            *reinterpret_cast<uint4 *>(mark_first + lane * RB + 4) = make_uint4(0, 0, 0, 0);
+            *reinterpret_cast<uint4 *>(mark_last + lane * RB) = make_uint4(0, 0, 0, 0);
+            *reinterpret_cast<uint4 *>(mark_last + lane * RB + 4) = make_uint4(0, 0, 0, 0);
+            __syncthreads();
+            for (int64_t q = q0;;) {
+                const int64_t f = now.first, l = now.behind;
+                const bool    here = q + lane < qb && (f < to || (f == to && to == p1));
+                if (here && f < l) {
+                    if (f >= pt && f < to) mark_first[(int)(f - pt)] = (uint32_t)(q + lane) + 1u;
+                    if (l > pt && l <= to) mark_last[(int)(l - 1 - pt)] = (uint32_t)(q + lane) + 1u;
+                    if (q == q0) {
+#pragma unroll
+                        for (int v = 0; v < V; ++v) from_s[lane * V + v] = before ? now.from[v] : 0.0f;
+                        if constexpr (BWD) {
+#pragma unroll
+                            for (int v = 0; v < V; ++v) left_s[lane * V + v] = a.h0 ? now.ends[v] : 0.0f;
+                        }
+                    }
+                } else if (here && f >= pt && q + lane >= qa) {        // no rows: the state passes on
+                    float *pass = BWD ? a.dh0 : a.last;
+                    float  h[V];
+#pragma unroll
+                    for (int v = 0; v < V; ++v) h[v] = before ? now.from[v] : 0.0f;
+                    if (pass) store_vec<float, V>(pass + o.sequence(q + lane) * V, h);
+                }
+                const uint64_t inside = __ballot(here && f < to), all = __ballot(here);
+                if (inside) q_at = q + (63 - __clzll(inside));
+                if (all != ~0ull) break;
+                q += 64;                                       // more than 64 sequences touch the tile: these are not loaded ahead
+                fetch_sequences(now, q);
+            }
+            __syncthreads();
+        }
+        if (pt + TR < p1) {
+            if (!PIECE) fetch_sequences(next, q_at);
+            fetch_rows(next, pt + TR);
+        }
+        if (pt >= p1) break;
+
+        const int64_t pr = pt + lane * RB;
+        const Place   at = place(pt);
+        uint32_t      first[RB], last[RB], live = (1u << RB) - 1u;
+        if (!whole) live = pr >= p1 ? 0u : pr + RB <= p1 ? live : (1u << (uint32_t)(p1 - pr)) - 1u;
+        bool any_first = false;
+#pragma unroll
+        for (int j = 0; j < RB; ++j) {
+            first[j] = PIECE ? 0u : mark_first[lane * RB + j];
+            last[j] = PIECE ? 0u : mark_last[lane * RB + j];
+            any_first |= first[j] != 0;
+        }
+
+        float g[RB][GV], in[RB][V], share[MIX ? RB : 1][GV];
+#pragma unroll
+        for (int j = 0; j < RB; ++j) {
+#pragma unroll
+            for (int v = 0; v < GV; ++v) {
+                float in_share;
+                gate_of<MIX>(log_gate, now.g.get(j, v, o.back), g[j][v], in_share);
+                if (MIX) share[MIX ? j : 0][v] = in_share;
+            }
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                in[j][v] = !BWD || a.dy ? now.in.get(j, v, o.back) : 0.0f;
+                if (MIX && !BWD) in[j][v] *= share[MIX ? j : 0][SHARED ? 0 : v];
+            }
+        }
+        if (!whole) {                                          // rows that are not there change nothing
+#pragma unroll
+            for (int j = 0; j < RB; ++j) {
+                const bool there = (live >> j) & 1u;
+#pragma unroll
+                for (int v = 0; v < GV; ++v) g[j][v] = there ? g[j][v] : 1.0f;
+#pragma unroll
+                for (int v = 0; v < V; ++v) in[j][v] = there ? in[j][v] : 0.0f;
+            }
+        }
+        // the state of sequence q + 1 == mark out of LDS, or of the array if the tile has more than 64
+        const auto state = [&](float (&h)[V], const float *table, const float *array, const uint32_t mark) {
+            const uint32_t i = mark - 1u - (uint32_t)q0;
+            if (i < 64u) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) h[v] = table[i * V + v];
+            } else if (array) {
+                load_vec<float, V>(h, array + o.sequence((int64_t)mark - 1) * V);
+            } else {
+#pragma unroll
+                for (int v = 0; v < V; ++v) h[v] = 0.0f;
+            }
+        };
+        if (!PIECE && before) {
+#pragma unroll
+            for (int j = 0; j < RB; ++j)
+                if (first[j]) {
+                    float h[V];
+                    state(h, from_s, before, first[j]);
+#pragma unroll
+                    for (int v = 0; v < V; ++v) in[j][v] = BWD ? in[j][v] + h[v] : fmaf(g[j][SHARED ? 0 : v], h[v], in[j][v]);
+                }
+        }
+
+        float          A[GV], B[V];
+        const uint64_t starts = PIECE ? 0 : __ballot(any_first);
+        const uint64_t upto = starts & (~0ull >> (63 - lane));
+        const int      since = upto ? 63 - __clzll(upto) : -1;  // last lane, up to this one, with a start
+#pragma unroll
+        for (int v = 0; v < GV; ++v) A[v] = 1.0f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) B[v] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < RB; ++j) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float gj = g[j][SHARED ? 0 : v], b = first[j] ? 0.0f : B[v];
+                B[v] = BWD ? gj * (b + in[j][v]) : fmaf(gj, b, in[j][v]);
+            }
+#pragma unroll
+            for (int v = 0; v < GV; ++v) A[v] *= g[j][v];
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            float Al[GV], Bl[V];
+#pragma unroll
+            for (int v = 0; v < GV; ++v) Al[v] = __shfl_up(A[v], d, 64);
+#pragma unroll
+            for (int v = 0; v < V; ++v) Bl[v] = __shfl_up(B[v], d, 64);
+            if (lane >= d && since <= lane - d) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) B[v] = fmaf(A[SHARED ? 0 : v], Bl[v], B[v]);
+#pragma unroll
+                for (int v = 0; v < GV; ++v) A[v] *= Al[v];
+            }
+        }
+        float h[V];
+        const bool cut_before = (starts & ((1ull << lane) - 1ull)) != 0;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const float Ae = __shfl_up(A[SHARED ? 0 : v], 1, 64), Be = __shfl_up(B[v], 1, 64);
+            const float At = __shfl(A[SHARED ? 0 : v], 63, 64), Bt = __shfl(B[v], 63, 64);
+            h[v] = lane == 0 ? carry_b[v] : cut_before ? Be : fmaf(Ae, carry_b[v], Be);
+            carry_b[v] = starts ? Bt : fmaf(At, carry_b[v], Bt);
+        }
+        if constexpr (PIECE) {
+#pragma unroll
+            for (int v = 0; v < GV; ++v) carry_a[v] *= __shfl(A[v], 63, 64);
+            now = next;
+            continue;
+        }
+
+        float slope[BWD ? RB : 1][GV];
+#pragma unroll
+        for (int j = 0; j < RB; ++j) {
+            float sum = 0.0f, left[V];
+            if constexpr (BWD && !PIECE) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) left[v] = now.left.get(j, v, o.back);
+                if (last[j]) state(left, left_s, a.h0, last[j]);
+                if constexpr (MIX) {
+#pragma unroll
+                    for (int v = 0; v < V; ++v) left[v] -= now.x.get(j, v, o.back);
+                }
+            }
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float gj = g[j][SHARED ? 0 : v], b = first[j] ? 0.0f : h[v];
+                if constexpr (!BWD) {
+                    h[v] = fmaf(gj, b, in[j][v]);
+                    in[j][v] = h[v];                           // now the output
+                } else {
+                    const float dh = b + in[j][v], da = dh * left[v];
+                    in[j][v] = MIX ? share[MIX ? j : 0][SHARED ? 0 : v] * dh : dh;
+                    if (!SHARED) slope[j][SHARED ? 0 : v] = log_gate ? da * gj : da;
+                    else sum += da;
+                    h[v] = gj * dh;
+                }
+            }
+            if constexpr (BWD && SHARED) slope[j][0] = log_gate ? sum * g[j][0] : sum;
+            if (last[j]) {
+                float *pass = BWD ? a.dh0 : a.last;
+                if (pass) store_vec<float, V>(pass + o.sequence((int64_t)last[j] - 1) * V, h);
+            }
+        }
+        const int64_t low_row = at.low + (int64_t)at.mine, lowest = low_row - (o.back ? RB - 1 : 0);
+        if (live == (1u << RB) - 1u) {
+            if constexpr (BWD) {
+                store_run<Io, RB, V>((Io *)a.dx + lowest * V, in, o.back);
+                store_run<Gate, RB, GV>((Gate *)a.dgate + lowest * GV, slope, o.back);
+            } else if (a.out_y) {
+                store_run<Y, RB, V>((Y *)a.out_y + lowest * V, in, o.back);
+            }
+        } else if (live) {
+#pragma unroll
+            for (int j = 0; j < RB; ++j) {
+                if (!((live >> j) & 1u)) continue;
+                const int64_t r = low_row + dir * j;
+                if constexpr (BWD) {
+                    store_vec<Io, V>((Io *)a.dx + r * V, in[j]);
+                    store_vec<Gate, GV>((Gate *)a.dgate + r * GV, slope[j]);
+                } else if (a.out_y) {
+                    store_vec<Y, V>((Y *)a.out_y + r * V, in[j]);
+                }
+            }
+        }
+        now = next;
+    }
+    if (PIECE && lane == 0) {
+        float A[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) A[v] = carry_a[SHARED ? 0 : v];
+        store_vec<float, V>(cut.piece_a + (int64_t)k * V, A);
+        store_vec<float, V>(cut.piece_b + (int64_t)k * V, carry_b);
+    }
+}
+
+template <typename Io, typename Gate, typename Y, int BLOCK, int CL, int V, int RB, bool SHARED, bool MIX, bool BWD>
+int launch_scan(const RecurArgs &a, const RecurPlan &p, const Cut &cut, hipStream_t s) {
+    const unsigned groups = cut.K * (unsigned)p.tiles;
+    if constexpr (BLOCK != kWideBlock) {
+        if (cut.exact) {
+            {
+                LaunchTimer t(s, BWD ? K_RECUR_BWD : K_RECUR_FWD);
+                recur_scan_kernel<Io, Gate, Io, BLOCK, CL, V, RB, SHARED, MIX, BWD, true><<<groups, BLOCK, 0, s>>>(a, cut);
+                if (int rc = launch_status("recur_scan_kernel (pieces)")) return rc;
+            }
+            if (int rc = recur_carry(cut, a.C, s)) return rc;
+        }
+    }
+    LaunchTimer t(s, BWD ? K_RECUR_BWD : K_RECUR_FWD);
+    recur_scan_kernel<Io, Gate, Y, BLOCK, CL, V, RB, SHARED, MIX, BWD, false><<<groups, BLOCK, 0, s>>>(a, cut);
+    return launch_status("recur_scan_kernel");
+}
+
+template <typename Io, typename Gate, typename Y, int V, bool SHARED, bool MIX, bool BWD>
+int launch_narrow(const RecurArgs &a, const Cut &cut, hipStream_t s) {
+    if (cut.exact) {
+        {
+            LaunchTimer t(s, BWD ? K_RECUR_BWD : K_RECUR_FWD);
+            recur_narrow_kernel<Io, Gate, Io, V, SHARED, MIX, BWD, true><<<cut.K, kNarrowBlock, 0, s>>>(a, cut);
+            if (int rc = launch_status("recur_narrow_kernel (pieces)")) return rc;
+        }
+        if (int rc = recur_carry(cut, a.C, s)) return rc;
+    }
+    LaunchTimer t(s, BWD ? K_RECUR_BWD : K_RECUR_FWD);
+    recur_narrow_kernel<Io, Gate, Y, V, SHARED, MIX, BWD, false><<<cut.K, kNarrowBlock, 0, s>>>(a, cut);
+    return launch_status("recur_narrow_kernel");
+}
+
+template <typename Io, typename Gate, typename Y, bool MIX, bool BWD>
+int launch_lanes(const RecurArgs &a, const RecurPlan &p, const Cut &cut, hipStream_t s) {
+    const bool shared = a.G == 1;
+#define CNGP_RECUR(BLOCK, CL, V, RB)                                                      \
+    return shared ? launch_scan<Io, Gate, Y, BLOCK, CL, V, RB, true, MIX, BWD>(a, p, cut, s) \
+                  : launch_scan<Io, Gate, Y, BLOCK, CL, V, RB, false, MIX, BWD>(a, p, cut, s)
+    if (p.CL == 1) {
+#define CNGP_NARROW(V) return shared ? launch_narrow<Io, Gate, Y, V, true, MIX, BWD>(a, cut, s) : launch_narrow<Io, Gate, Y, V, false, MIX, BWD>(a, cut, s)
+        if (a.C == 1) return launch_narrow<Io, Gate, Y, 1, true, MIX, BWD>(a, cut, s);
+        if (a.C == 2) CNGP_NARROW(2);
+        if (a.C == 3) CNGP_NARROW(3);
+        CNGP_NARROW(4);
+#undef CNGP_NARROW
+    }
+    if (p.block == kWideBlock) CNGP_RECUR(kWideBlock, 16, 2, kRowsEach);
+    if (p.CL == 16) CNGP_RECUR(kRecurBlock, 16, 1, kRowsEach);
+    if (p.V == 1) CNGP_RECUR(kRecurBlock, 32, 1, kRowsEach);
+    CNGP_RECUR(kRecurBlock, 32, 2, kRowsEach);
+#undef CNGP_RECUR
+}
+
+template <typename Io, typename Gate, bool BWD>
+int launch_inputs(const RecurArgs &a, const RecurPlan &p, const Cut &cut, hipStream_t s) {
+    const bool mix = a.flags & CNGP_RECUR_MIX;
+    if constexpr (sizeof(Io) != sizeof(float))
+        if (a.y_f32) return mix ? launch_lanes<Io, Gate, float, true, BWD>(a, p, cut, s) : launch_lanes<Io, Gate, float, false, BWD>(a, p, cut, s);
+    return mix ? launch_lanes<Io, Gate, Io, true, BWD>(a, p, cut, s) : launch_lanes<Io, Gate, Io, false, BWD>(a, p, cut, s);
+}
+
+}  // namespace
+
+// One direction's launches.  state_in / state_out: what a sequence starts from and where it ends up; where they are one array and
+// sequences are cut, the workgroup that ends a sequence is not the one that starts it, so the start is taken from a copy.
+template <bool BWD>
+int cngp::recur_launch(const cngp_recur_config *c, RecurArgs a, const RecurPlan &p, const RecurSpace &sp, char *ws, hipStream_t s) {
+    if ((int64_t)p.K * p.tiles > 0x7fffffffLL) return CNGP_ERR_UNSUPPORTED;
+    Cut cut{p.R, p.K, (float *)(ws + sp.piece_a), (float *)(ws + sp.piece_b), (float *)(ws + sp.carry), (int32_t *)(ws + sp.piece_cut), p.exact};
+    const float *&in = BWD ? a.dlast : a.h0;
+    float        *out = BWD ? a.dh0 : a.last;
+    if (p.exact && in && in == out) {
+        float        *copy = (float *)(ws + sp.state);
+        if (int rc = recur_copy(in, copy, a.S * a.C, s)) return rc;
+        in = copy;
+    }
+    const bool io16 = c->io_dtype == CNGP_F16, g16 = c->gate_dtype == CNGP_F16;
+    return io16 ? (g16 ? launch_inputs<__half, __half, BWD>(a, p, cut, s) : launch_inputs<__half, float, BWD>(a, p, cut, s))
+                : (g16 ? launch_inputs<float, __half, BWD>(a, p, cut, s) : launch_inputs<float, float, BWD>(a, p, cut, s));
+}
+

@@ -5,6 +5,7 @@
 // The gradient needs, per row of the table, the points that chose it.  Float atomics would give sums whose order, hence bits, change
 // from call to call, and frequent ids would queue at one address; so the ids are sorted (stable, with their positions), and the rows
 // of dy that belong to one id are added up in the order of the points.
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 
@@ -31,51 +32,365 @@ __device__ __forceinline__ uint32_t row_of(const Id id, const int64_t rows) {
     return id >= 0 && (int64_t)id < rows ? (uint32_t)id : (uint32_t)rows;
 }
 
-template <typename Id, typename Table, typename Io>
+// V neighbouring values at once, on whatever boundary they start: global memory takes that, the compiler makes one access of it.
+template <typename T, int N>
+struct Run { T e[N]; };
+template <typename T, int V>
+__device__ __forceinline__ void load_run(float (&out)[V], const T *p) {
+    Run<T, V> r;
+    __builtin_memcpy(&r, p, sizeof r);
+#pragma unroll
+    for (int v = 0; v < V; ++v) out[v] = load(r.e, v);
+}
+template <typename T, int V>
+__device__ __forceinline__ void store_run(T *p, const float (&in)[V]) {
+    Run<T, V> r;
+#pragma unroll
+    for (int v = 0; v < V; ++v) store(r.e, v, in[v]);
+    __builtin_memcpy(p, &r, sizeof r);
+}
+
+// ---------------------------------------------------------------- lookup
+// A workgroup takes `rows_each` points, a lane V neighbouring columns of a point at a time, kEmbAhead of them in flight: the id and the
+// row it names are two loads one behind the other.  per_row = dim / V; i / per_row as a multiplication.
+constexpr int kEmbAhead = 4;
+template <typename Id, typename Table, typename Io, int V>
 __global__ __launch_bounds__(kEmbBlock) void embed_fwd_kernel(const Id *__restrict__ ids, const Table *__restrict__ table, const Io *base, Io *y,
-                                                              const int64_t N, const int64_t rows, const int dim, const float scale)
+                                                              const int64_t N, const int64_t rows, const int dim, const uint32_t per_row,
+                                                              const uint32_t inverse, const uint32_t rows_each, const float scale)
 {
-    const int64_t i = (int64_t)blockIdx.x * kEmbBlock + threadIdx.x;
-    if (i >= N * dim) return;
-    const int64_t  n = i / dim;
-    const uint32_t r = row_of(ids[n], rows);
-    const float    b = base ? load(base, i) : 0.0f;
-    store(y, i, (int64_t)r < rows ? b + scale * load(table, (int64_t)r * dim + (i - n * dim)) : b);
+    const int64_t  n0 = (int64_t)blockIdx.x * rows_each;
+    const uint32_t mine = N - n0 < (int64_t)rows_each ? (uint32_t)(N - n0) : rows_each, items = mine * per_row;
+    for (uint32_t i0 = threadIdx.x; i0 < items; i0 += kEmbBlock * kEmbAhead) {
+        uint32_t n[kEmbAhead], c[kEmbAhead], r[kEmbAhead];
+        float    row[kEmbAhead][V], b[kEmbAhead][V];
+#pragma unroll
+        for (int u = 0; u < kEmbAhead; ++u) {
+            const uint32_t i = i0 + u * kEmbBlock < items ? i0 + u * kEmbBlock : i0;
+            n[u] = per_row == 1 ? i : mine == 1 ? 0u : __umulhi(i, inverse);
+            c[u] = (i - n[u] * per_row) * V;
+            r[u] = row_of(ids[n0 + n[u]], rows);
+        }
+#pragma unroll
+        for (int u = 0; u < kEmbAhead; ++u) {
+            load_run<Table, V>(row[u], table + (int64_t)(r[u] < (uint32_t)rows ? r[u] : 0u) * dim + c[u]);
+            if (base) load_run<Io, V>(b[u], base + (n0 + n[u]) * dim + c[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < kEmbAhead; ++u) {
+            if (u && i0 + u * kEmbBlock >= items) break;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float start = base ? b[u][v] : 0.0f;
+                b[u][v] = r[u] < (uint32_t)rows ? fmaf(scale, row[u][v], start) : start;
+            }
+            store_run<Io, V>(y + (n0 + n[u]) * dim + c[u], b[u]);
+        }
+    }
 }
 
+// ---------------------------------------------------------------- sort of the ids
 template <typename Id>
-__global__ __launch_bounds__(kEmbBlock) void embed_keys_kernel(const Id *__restrict__ ids, uint32_t *__restrict__ keys, const int64_t N, const int64_t rows)
+__global__ __launch_bounds__(kTileBlock) void embed_keys_kernel(const Id *__restrict__ ids, uint32_t *__restrict__ keys, const int64_t N, const int64_t rows,
+                                                                uint32_t *__restrict__ counts, const int64_t tiles)
 {
-    const int64_t n = (int64_t)blockIdx.x * kEmbBlock + threadIdx.x;
-    if (n < N) keys[n] = row_of(ids[n], rows);
+    __shared__ uint32_t hist[kTileWaves * kDigits];
+    const int     t = threadIdx.x, w = t >> 6;
+    const int64_t n0 = (int64_t)blockIdx.x * kTile;
+    for (int i = t; i < kTileWaves * kDigits; i += kTileBlock) hist[i] = 0;
+    __syncthreads();
+    uint32_t key[kRounds];
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+        const int64_t n = n0 + (int64_t)r * kTileBlock + t;
+        key[r] = n < N ? row_of(ids[n], rows) : 0u;
+    }
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+        const int64_t n = n0 + (int64_t)r * kTileBlock + t;
+        if (n < N) {
+            keys[n] = key[r];
+            atomicAdd(&hist[w * kDigits + (key[r] & (kDigits - 1))], 1u);
+        }
+    }
+    __syncthreads();
+    flush_tile_histogram(hist, counts, tiles, blockIdx.x, t);
 }
 
-// First position of the sorted keys that is not below `key`.
-__device__ __forceinline__ int64_t first_at(const uint32_t *__restrict__ keys, const int64_t N, const uint32_t key) {
-    int64_t lo = 0, hi = N;
+// Up to 16384 ids are sorted by one workgroup in LDS, all digits in one launch (the passes above are three launches each, of which a short
+// batch fills two workgroups).  Stable, eight bits at a time: a wavefront ranks its strip 64 elements at a time, lanes with equal digits
+// find each other by ballots; per digit the wavefronts' counts become their places.
+constexpr int kSmallBlock = 1024, kSmallWaves = kSmallBlock / 64, kSmallBits = 8, kSmallDigits = 1 << kSmallBits, kSmallMost = kSmallBlock * 16;
+template <typename Id, int ROUNDS>
+__global__ __launch_bounds__(kSmallBlock) void embed_sort_small_kernel(const Id *__restrict__ ids, uint32_t *__restrict__ keys, int32_t *__restrict__ from,
+                                                                       const int N, const int64_t rows)
+{
+    extern __shared__ __align__(16) uint32_t small_lds[];
+    uint32_t *wave_count = small_lds;                          // [kSmallWaves][kSmallDigits]
+    uint32_t *stage_key = small_lds + kSmallWaves * kSmallDigits, *stage_from = stage_key + ROUNDS * kSmallBlock;
+    __shared__ uint32_t sums[kSmallDigits / 64];
+    const int t = threadIdx.x, w = t >> 6, lane = t & 63, n0 = w * (ROUNDS * 64) + lane;
+    const uint64_t below = lane ? (~0ull >> (64 - lane)) : 0ull;
+    uint32_t key[ROUNDS], at[ROUNDS], slot[ROUNDS];
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+        const int n = n0 + r * 64;
+        key[r] = n < N ? row_of(ids[n], rows) : 0xffffffffu;   // elements that are not there sort behind all others
+        at[r] = (uint32_t)n;
+    }
+    for (int shift = 0; shift < 32 && ((uint64_t)rows >> shift); shift += kSmallBits) {
+        for (int i = t; i < kSmallWaves * kSmallDigits; i += kSmallBlock) wave_count[i] = 0;
+        __syncthreads();
+        uint32_t *mine = wave_count + w * kSmallDigits;
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r) {
+            const uint32_t digit = (key[r] >> shift) & (kSmallDigits - 1);
+            uint64_t       peers = ~0ull;
+#pragma unroll
+            for (int b = 0; b < kSmallBits; ++b) {
+                const bool     bit = (digit >> b) & 1u;
+                const uint64_t has = __ballot(bit);
+                peers &= bit ? has : ~has;
+            }
+            const uint32_t seen = mine[digit];
+            slot[r] = seen + (uint32_t)__popcll(peers & below);
+            if ((peers & below) == 0) mine[digit] = seen + (uint32_t)__popcll(peers);
+            __builtin_amdgcn_wave_barrier();
+        }
+        __syncthreads();
+        uint32_t count = 0, before = 0, sum = 0;
+        if (t < kSmallDigits) {
+#pragma unroll
+            for (int k = 0; k < kSmallWaves; ++k) {
+                const uint32_t c = wave_count[k * kSmallDigits + t];
+                wave_count[k * kSmallDigits + t] = count;
+                count += c;
+            }
+            before = wave_exclusive_scan(count, &sum);
+            if (lane == 0) sums[w] = sum;
+        }
+        __syncthreads();
+        if (t < kSmallDigits) {
+            for (int k = 0; k < w; ++k) before += sums[k];
+#pragma unroll
+            for (int k = 0; k < kSmallWaves; ++k) wave_count[k * kSmallDigits + t] += before;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r) {
+            const uint32_t to = mine[(key[r] >> shift) & (kSmallDigits - 1)] + slot[r];
+            stage_key[to] = key[r];
+            stage_from[to] = at[r];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r) {
+            key[r] = stage_key[n0 + r * 64];
+            at[r] = stage_from[n0 + r * 64];
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+        const int n = n0 + r * 64;
+        if (n < N) { keys[n] = key[r]; from[n] = (int32_t)at[r]; }
+    }
+}
+
+// ---------------------------------------------------------------- sums of the rows of an id
+// The sorted positions are cut into pieces of `piece` positions, a wavefront each; its lanes are row lanes of LPR lanes that hold V
+// columns each, and a row lane walks piece / (64 / LPR) positions, kSumAhead rows in flight.  An id whose positions lie inside a piece
+// is summed and written there.  One that reaches over a piece's edges leaves a partial sum at each piece it touches -- `tail` where it
+// starts, `head` where it came from before -- and embed_join_kernel adds those up: always in the order of the positions.
+constexpr int kSumAhead = 8;
+
+struct SumArgs {
+    const uint32_t *keys;
+    const int32_t  *from;
+    const void     *dy;
+    float          *grad, *head, *tail;  // head, tail: [pieces][dim]
+    int64_t         N, rows;
+    uint32_t        piece, pieces;
+    int             dim, accumulate;
+    float           scale;
+};
+
+template <int V>
+__device__ __forceinline__ void put_row(const SumArgs &a, const uint32_t key, const int c, float (&sum)[V]) {
+    float *to = a.grad + (int64_t)key * a.dim + c;
+#pragma unroll
+    for (int v = 0; v < V; ++v) sum[v] *= a.scale;
+    if (a.accumulate) {
+        float old[V];
+        load_run<float, V>(old, to);
+#pragma unroll
+        for (int v = 0; v < V; ++v) sum[v] += old[v];
+    }
+    store_run<float, V>(to, sum);
+}
+
+template <typename Io, int V, int LPR>
+__global__ __launch_bounds__(kEmbBlock) void embed_sums_kernel(const SumArgs a)
+{
+    constexpr int  RL = 64 / LPR;                              // row lanes of a wavefront
+    const int      lane = threadIdx.x & 63, cl = lane % LPR, rl = lane / LPR;
+    const uint32_t piece = blockIdx.x * (kEmbBlock / 64) + (threadIdx.x >> 6);
+    if (piece >= a.pieces) return;
+    const int      c = ((int)blockIdx.y * LPR + cl) * V;
+    const bool     c_ok = c < a.dim;
+    const int      cc = c_ok ? c : 0;
+    const uint32_t each = a.piece / RL;
+    const int64_t  w0 = (int64_t)piece * a.piece, w1 = w0 + a.piece < a.N ? w0 + a.piece : a.N;
+    const int64_t  p0 = w0 + (int64_t)rl * each < w1 ? w0 + (int64_t)rl * each : w1, p1 = p0 + each < w1 ? p0 + each : w1;
+
+    // this row lane's first run (which may have begun before it) in `first`, its last one (which may go on) in `sum`
+    float    sum[V], first[V];
+    uint32_t key = 0, key0 = 0;
+    bool     one_run = true;
+#pragma unroll
+    for (int v = 0; v < V; ++v) sum[v] = first[v] = 0.0f;
+    for (int64_t p = p0; p < p1; p += kSumAhead) {
+        uint32_t k[kSumAhead];
+        int32_t  n[kSumAhead];
+        float    row[kSumAhead][V];
+#pragma unroll
+        for (int u = 0; u < kSumAhead; ++u) {
+            const int64_t at = p + u < p1 ? p + u : p1 - 1;
+            k[u] = a.keys[at];
+            n[u] = a.from[at];
+        }
+#pragma unroll
+        for (int u = 0; u < kSumAhead; ++u) load_run<Io, V>(row[u], (const Io *)a.dy + (int64_t)n[u] * a.dim + cc);
+        if (p == p0) key = key0 = k[0];
+#pragma unroll
+        for (int u = 0; u < kSumAhead; ++u) {
+            if (p + u >= p1) break;
+            if (k[u] != key) {                                 // a run ends
+                if (one_run) {
+#pragma unroll
+                    for (int v = 0; v < V; ++v) first[v] = sum[v];
+                } else if (c_ok) {
+                    put_row<V>(a, key, c, sum);                // began and ended in here: no padding, a larger key follows
+                }
+                one_run = false;
+                key = k[u];
+#pragma unroll
+                for (int v = 0; v < V; ++v) sum[v] = 0.0f;
+            }
+#pragma unroll
+            for (int v = 0; v < V; ++v) sum[v] += row[u][v];
+        }
+    }
+    // what reaches a row lane from those before it: a lane that is one run that came and goes on passes it on with its own sum added
+    const bool     some = p0 < p1;
+    const uint32_t none = 0xffffffffu;
+    const uint32_t came = some && p0 > 0 ? a.keys[p0 - 1] : none, follows = some && p1 < a.N ? a.keys[p1] : none;
+    const bool     from_before = some && came == key0, goes_on = some && follows == key;
+    const bool     through = one_run && from_before && goes_on;
+    float          reach[V], open[V];                          // open: the sum that leaves this row lane
+    bool           chain = through;                            // whether `open` still misses what reaches the lanes it spans
+#pragma unroll
+    for (int v = 0; v < V; ++v) open[v] = goes_on ? sum[v] : 0.0f;
+#pragma unroll
+    for (int d = 1; d < RL; d <<= 1) {
+        const bool lc = __shfl_up((int)chain, d * LPR, 64) != 0;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const float l = __shfl_up(open[v], d * LPR, 64);
+            if (rl >= d && chain) open[v] += l;
+        }
+        if (rl >= d) chain = chain && lc;
+    }
+    bool reach_chain = false;                                  // what reaches has itself come from before the piece
+    if (RL > 1) reach_chain = __shfl_up((int)chain, LPR, 64) != 0;
+#pragma unroll
+    for (int v = 0; v < V; ++v) reach[v] = RL > 1 ? __shfl_up(open[v], LPR, 64) : 0.0f;
+    if (rl == 0) {
+        reach_chain = true;
+#pragma unroll
+        for (int v = 0; v < V; ++v) reach[v] = 0.0f;
+    }
+    if (!some || !c_ok) return;
+    const bool last_lane = p1 == w1;
+    if (!one_run || !goes_on) {                                // the first run ends in here
+        float total[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) total[v] = (from_before ? reach[v] : 0.0f) + (one_run ? sum[v] : first[v]);
+        if (from_before && reach_chain) {
+            store_run<float, V>(a.head + (int64_t)piece * a.dim + c, total);
+        } else if (key0 < (uint32_t)a.rows) {
+            put_row<V>(a, key0, c, total);
+        }
+    }
+    if (!one_run && !goes_on && key < (uint32_t)a.rows) put_row<V>(a, key, c, sum);
+    if (goes_on && last_lane) {                                // the last run leaves the piece
+        float *to = through && reach_chain ? a.head : a.tail;  // one that also came from before it is all head
+#pragma unroll
+        for (int v = 0; v < V; ++v) sum[v] = through ? reach[v] + sum[v] : sum[v];
+        store_run<float, V>(to + (int64_t)piece * a.dim + c, sum);
+    }
+}
+
+// First position of the sorted keys that is not below `key`, from `lo` on; a wavefront together, 64 probes at a time.
+__device__ __forceinline__ int64_t first_at(const uint32_t *__restrict__ keys, int64_t lo, const int64_t N, const uint32_t key) {
+    int64_t       hi = N;
+    const int64_t lane = threadIdx.x & 63;
     while (lo < hi) {
-        const int64_t mid = (lo + hi) >> 1;
-        if (keys[mid] < key) lo = mid + 1;
-        else hi = mid;
+        const int64_t  step = (hi - lo + 63) / 64, probe = lo + lane * step;
+        const uint64_t less = __ballot(probe < hi && keys[probe < hi ? probe : hi - 1] < key);
+        if (!less) { hi = lo; break; }
+        const int64_t last = lo + (63 - __clzll(less)) * step;
+        lo = last + 1;
+        hi = last + step < hi ? last + step : hi;
     }
     return lo;
 }
 
-// A wavefront per row of the table.
-template <typename Io>
-__global__ __launch_bounds__(kEmbBlock) void embed_sums_kernel(const uint32_t *__restrict__ keys, const int32_t *__restrict__ from,
-                                                               const Io *__restrict__ dy, float *__restrict__ grad, const int64_t N,
-                                                               const int64_t rows, const int dim, const float scale, const int accumulate)
+// Ids that reach over pieces: the piece in which one starts adds its tail and the heads of the pieces up to its end.
+template <int V, int LPR>
+__global__ __launch_bounds__(kEmbBlock) void embed_join_kernel(const SumArgs a)
 {
-    const int64_t r = ((int64_t)blockIdx.x * kEmbBlock + threadIdx.x) >> 6;
-    if (r >= rows) return;
-    const int64_t p0 = first_at(keys, N, (uint32_t)r), p1 = first_at(keys, N, (uint32_t)r + 1u);
-    if (p0 == p1 && accumulate) return;
-    for (int c = threadIdx.x & 63; c < dim; c += 64) {
-        float sum = 0.0f;
-        for (int64_t p = p0; p < p1; ++p) sum += load(dy, (int64_t)from[p] * dim + c);
-        const int64_t o = r * dim + c;
-        grad[o] = accumulate ? grad[o] + scale * sum : scale * sum;
+    constexpr int  RL = 64 / LPR;
+    const int      lane = threadIdx.x & 63, cl = lane % LPR, rl = lane / LPR;
+    const uint32_t piece = blockIdx.x * (kEmbBlock / 64) + (threadIdx.x >> 6);
+    if (piece + 1 >= a.pieces) return;
+    const int64_t  w0 = (int64_t)piece * a.piece, w1 = w0 + a.piece;
+    const uint32_t key = a.keys[w1 - 1];
+    if (a.keys[w1] != key || key >= (uint32_t)a.rows || (w0 > 0 && a.keys[w0 - 1] == key)) return;      // does not start here and go on
+    const uint32_t end = (uint32_t)((first_at(a.keys, w1, a.N, key + 1u) - 1) / a.piece);               // the piece it ends in
+    const int      c = ((int)blockIdx.y * LPR + cl) * V, cc = c < a.dim ? c : 0;
+    float sum[V];
+    if (rl == 0) {
+        load_run<float, V>(sum, a.tail + (int64_t)piece * a.dim + cc);
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) sum[v] = 0.0f;
+    }
+    for (uint32_t q = piece + 1 + rl; q <= end; q += RL * 4) {
+        float h[4][V];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) load_run<float, V>(h[u], a.head + (int64_t)(q + u * RL <= end ? q + u * RL : q) * a.dim + cc);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int v = 0; v < V; ++v) sum[v] += u == 0 || q + u * RL <= end ? h[u][v] : 0.0f;
+    }
+#pragma unroll
+    for (int d = LPR; d < 64; d <<= 1)
+#pragma unroll
+        for (int v = 0; v < V; ++v) sum[v] += __shfl_xor(sum[v], d, 64);
+    if (rl == 0 && c < a.dim) put_row<V>(a, key, c, sum);
+}
+
+__global__ __launch_bounds__(kEmbBlock) void embed_clear_kernel(float *__restrict__ grad, const int64_t n)
+{
+    const int64_t step = (int64_t)gridDim.x * kEmbBlock * 4;
+    for (int64_t i = ((int64_t)blockIdx.x * kEmbBlock + threadIdx.x) * 4; i < n; i += step) {
+        if (i + 4 <= n) {
+            const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            store_run<float, 4>(grad + i, zero);
+        } else {
+            for (int64_t j = i; j < n; ++j) grad[j] = 0.0f;
+        }
     }
 }
 
@@ -90,15 +405,122 @@ int check(const cngp_embed_config *c, int64_t N) {
     return CNGP_OK;
 }
 
-struct EmbedSpace { size_t keys_a, keys_b, from_a, from_b, counts, totals, bytes; };
-EmbedSpace space_of(int64_t N) {
+// Columns of a lane: 16 bytes of the array that is gathered, or a divisor of the width.
+int columns_of(int dim, int most) {
+    int v = most;
+    while (dim % v) v >>= 1;
+    return v;
+}
+
+// Positions of a piece: 128, or as many as leave 8192 pieces (the joins of one id in all of a large batch stay short).  A multiple of
+// 64 row lanes.
+uint32_t piece_of(int64_t N) {
+    const int64_t p = (N + 8191) / 8192;
+    return (uint32_t)(p <= 128 ? 128 : (p + 63) / 64 * 64);
+}
+
+struct EmbedSpace { size_t keys_a, keys_b, from_a, from_b, counts, totals, head, tail, bytes; };
+EmbedSpace space_of(const cngp_embed_config *c, int64_t N) {
     EmbedSpace s{};
-    const size_t col = align256((size_t)N * 4);
-    s.keys_a = 0; s.keys_b = col; s.from_a = 2 * col; s.from_b = 3 * col;
-    s.counts = 4 * col;
-    s.totals = s.counts + align256((size_t)kDigits * (size_t)tiles_of(N) * 4);
-    s.bytes = N ? s.totals + align256((size_t)kDigits * 4) : 0;
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t o = at; at += align256(bytes); return o; };
+    if (!N) return s;
+    const size_t col = (size_t)N * 4, pieces = (size_t)((N + piece_of(N) - 1) / piece_of(N));
+    s.keys_a = take(col);
+    s.from_a = take(col);
+    if (N > kSmallMost) {
+        s.keys_b = take(col);
+        s.from_b = take(col);
+        s.counts = take((size_t)kDigits * (size_t)tiles_of(N) * 4);
+        s.totals = take((size_t)kDigits * 4);
+    }
+    s.head = take(pieces * (size_t)c->dim * 4);
+    s.tail = take(pieces * (size_t)c->dim * 4);
+    s.bytes = at;
     return s;
+}
+
+template <typename Id, int ROUNDS>
+int sort_small(const void *ids, uint32_t *keys, int32_t *from, int64_t N, int64_t rows, hipStream_t s) {
+    const size_t lds = (size_t)(kSmallWaves * kSmallDigits + 2 * ROUNDS * kSmallBlock) * 4;
+    if (lds > 64 * 1024)
+        if (hipError_t e = hipFuncSetAttribute((const void *)embed_sort_small_kernel<Id, ROUNDS>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds))
+            return record_hip_failure(e, "hipFuncSetAttribute(MaxDynamicSharedMemorySize)");
+    embed_sort_small_kernel<Id, ROUNDS><<<1, kSmallBlock, lds, s>>>((const Id *)ids, keys, from, (int)N, rows);
+    return launch_status("embed_sort_small_kernel");
+}
+
+// Sorted keys and the points they came from, in keys[0] and from[0] or, after an odd number of passes, [1]: *at says which.
+template <typename Id>
+int sort_ids(const void *ids, int64_t N, int64_t rows, uint32_t *(&keys)[2], int32_t *(&from)[2], uint32_t *counts, uint32_t *totals, int *at, hipStream_t s) {
+    LaunchTimer t(s, K_EMBED_SORT);
+    *at = 0;
+    if (N <= kSmallBlock) return sort_small<Id, 1>(ids, keys[0], from[0], N, rows, s);
+    if (N <= kSmallBlock * 4) return sort_small<Id, 4>(ids, keys[0], from[0], N, rows, s);
+    if (N <= kSmallMost) return sort_small<Id, 16>(ids, keys[0], from[0], N, rows, s);
+    const unsigned tiles = (unsigned)tiles_of(N);
+    embed_keys_kernel<Id><<<tiles, kTileBlock, 0, s>>>((const Id *)ids, keys[0], N, rows, counts, tiles);
+    if (int rc = launch_status("embed_keys_kernel")) return rc;
+    for (int shift = 0; shift < 32 && ((uint64_t)rows >> shift); shift += kDigitBits, *at ^= 1) {
+        if (shift) {
+            digit_count_kernel<<<tiles, kTileBlock, 0, s>>>(keys[*at], N, shift, counts, tiles);
+            if (int rc = launch_status("digit_count_kernel")) return rc;
+        }
+        digit_row_scan_kernel<<<kDigits, kScanBlock, 0, s>>>(counts, tiles, totals);
+        if (int rc = launch_status("digit_row_scan_kernel")) return rc;
+        digit_scatter_kernel<<<tiles, kTileBlock, 0, s>>>(keys[*at], shift ? from[*at] : nullptr, N, shift, counts, tiles, totals, keys[*at ^ 1], from[*at ^ 1]);
+        if (int rc = launch_status("digit_scatter_kernel")) return rc;
+    }
+    return CNGP_OK;
+}
+
+template <typename Io, int V, int LPR>
+int sum_rows(const SumArgs &a, hipStream_t s) {
+    const unsigned columns = (unsigned)((a.dim / V + LPR - 1) / LPR), groups = (a.pieces + kEmbBlock / 64 - 1) / (kEmbBlock / 64);
+    LaunchTimer t(s, K_EMBED_SUMS);
+    embed_sums_kernel<Io, V, LPR><<<dim3(groups, columns), kEmbBlock, 0, s>>>(a);
+    if (int rc = launch_status("embed_sums_kernel")) return rc;
+    if (a.pieces < 2) return CNGP_OK;
+    embed_join_kernel<V, LPR><<<dim3(groups, columns), kEmbBlock, 0, s>>>(a);
+    return launch_status("embed_join_kernel");
+}
+template <typename Io, int V>
+int sum_columns(const SumArgs &a, hipStream_t s) {
+    const int lanes = a.dim / V;
+    if (lanes <= 1) return sum_rows<Io, V, 1>(a, s);
+    if (lanes <= 4) return sum_rows<Io, V, 4>(a, s);
+    if (lanes <= 16) return sum_rows<Io, V, 16>(a, s);
+    return sum_rows<Io, V, 64>(a, s);
+}
+
+template <typename Id, typename Table, typename Io, int V>
+int look_up(const cngp_embed_config *c, const void *ids, int64_t N, const void *table, const void *base, void *y, hipStream_t s) {
+    const uint32_t per_row = (uint32_t)(c->dim / V), rows_each = std::max(1u, (uint32_t)(kEmbBlock * kEmbAhead) / per_row);
+    const int64_t  blocks = (N + rows_each - 1) / rows_each;
+    if (blocks > 0x7fffffffLL) return CNGP_ERR_INVALID;
+    // the smallest multiplier that divides every i below rows_each * per_row <= 1024 exactly (one point, or one value to a point, need none)
+    const uint32_t inverse = (uint32_t)((0x100000000ull + per_row - 1) / per_row);      // not used for per_row = 1
+    LaunchTimer t(s, K_EMBED_FWD);
+    embed_fwd_kernel<Id, Table, Io, V><<<(unsigned)blocks, kEmbBlock, 0, s>>>((const Id *)ids, (const Table *)table, (const Io *)base, (Io *)y, N, c->rows,
+                                                                              c->dim, per_row, inverse, rows_each, c->scale);
+    return launch_status("embed_fwd_kernel");
+}
+template <typename Id, typename Table, typename Io>
+int look_up_columns(const cngp_embed_config *c, const void *ids, int64_t N, const void *table, const void *base, void *y, hipStream_t s) {
+    switch (columns_of(c->dim, 16 / (int)std::max(sizeof(Table), sizeof(Io)))) {
+    case 8:  return look_up<Id, Table, Io, 8>(c, ids, N, table, base, y, s);
+    case 4:  return look_up<Id, Table, Io, 4>(c, ids, N, table, base, y, s);
+    case 2:  return look_up<Id, Table, Io, 2>(c, ids, N, table, base, y, s);
+    default: return look_up<Id, Table, Io, 1>(c, ids, N, table, base, y, s);
+    }
+}
+template <typename Id>
+int look_up_types(const cngp_embed_config *c, const void *ids, int64_t N, const void *table, const void *base, void *y, hipStream_t s) {
+    if (c->table_dtype == CNGP_F16)
+        return c->io_dtype == CNGP_F16 ? look_up_columns<Id, __half, __half>(c, ids, N, table, base, y, s)
+                                       : look_up_columns<Id, __half, float>(c, ids, N, table, base, y, s);
+    return c->io_dtype == CNGP_F16 ? look_up_columns<Id, float, __half>(c, ids, N, table, base, y, s)
+                                   : look_up_columns<Id, float, float>(c, ids, N, table, base, y, s);
 }
 
 }  // namespace
@@ -106,31 +528,15 @@ EmbedSpace space_of(int64_t N) {
 extern "C" {
 
 size_t cngp_embed_workspace_bytes(const cngp_embed_config *cfg, int64_t N) {
-    return check(cfg, N) ? 0 : space_of(N).bytes;
+    return check(cfg, N) ? 0 : space_of(cfg, N).bytes;
 }
 
 int cngp_embed_fwd(const cngp_embed_config *cfg, const void *ids, int64_t N, const void *table, const void *base, void *y, void *stream) {
     if (int rc = check(cfg, N)) return rc;
     if (N == 0) return CNGP_OK;
     if (!ids || !table || !y) return CNGP_ERR_NULL;
-    const int64_t blocks = (N * cfg->dim + kEmbBlock - 1) / kEmbBlock;
-    if (blocks > 0x7fffffffLL) return CNGP_ERR_INVALID;
     hipStream_t s = (hipStream_t)stream;
-    LaunchTimer t(s, K_EMBED_FWD);
-#define CNGP_EMBED(Id, Table, Io) embed_fwd_kernel<Id, Table, Io><<<(unsigned)blocks, kEmbBlock, 0, s>>>( \
-        (const Id *)ids, (const Table *)table, (const Io *)base, (Io *)y, N, cfg->rows, cfg->dim, cfg->scale)
-    switch (cfg->id_dtype * 4 + cfg->table_dtype * 2 + cfg->io_dtype) {
-    case 0: CNGP_EMBED(int32_t, float, float); break;
-    case 1: CNGP_EMBED(int32_t, float, __half); break;
-    case 2: CNGP_EMBED(int32_t, __half, float); break;
-    case 3: CNGP_EMBED(int32_t, __half, __half); break;
-    case 4: CNGP_EMBED(int64_t, float, float); break;
-    case 5: CNGP_EMBED(int64_t, float, __half); break;
-    case 6: CNGP_EMBED(int64_t, __half, float); break;
-    default: CNGP_EMBED(int64_t, __half, __half); break;
-    }
-#undef CNGP_EMBED
-    return launch_status("embed_fwd_kernel");
+    return cfg->id_dtype == CNGP_I64 ? look_up_types<int64_t>(cfg, ids, N, table, base, y, s) : look_up_types<int32_t>(cfg, ids, N, table, base, y, s);
 }
 
 int cngp_embed_bwd(const cngp_embed_config *cfg, const void *ids, int64_t N, const void *dy, float *grad_table,
@@ -138,39 +544,38 @@ int cngp_embed_bwd(const cngp_embed_config *cfg, const void *ids, int64_t N, con
     if (int rc = check(cfg, N)) return rc;
     if (!grad_table) return CNGP_ERR_NULL;
     const int accumulate = (cfg->flags & CNGP_ZERO_GRADS) ? 0 : 1;
-    if (N == 0 && accumulate) return CNGP_OK;
     if (N && (!ids || !dy)) return CNGP_ERR_NULL;
-    const EmbedSpace sp = space_of(N);
+    const EmbedSpace sp = space_of(cfg, N);
     if (sp.bytes && (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < sp.bytes)) return CNGP_ERR_WORKSPACE;
     hipStream_t s = (hipStream_t)stream;
+    if (!accumulate) {
+        const int64_t n = cfg->rows * cfg->dim, blocks = (n + kEmbBlock * 4 - 1) / (kEmbBlock * 4);
+        LaunchTimer t(s, K_ZERO);
+        embed_clear_kernel<<<(unsigned)std::min<int64_t>(blocks, 8192), kEmbBlock, 0, s>>>(grad_table, n);
+        if (int rc = launch_status("embed_clear_kernel")) return rc;
+    }
+    if (N == 0) return CNGP_OK;
     char     *ws = (char *)workspace;
     uint32_t *keys[2] = {(uint32_t *)(ws + sp.keys_a), (uint32_t *)(ws + sp.keys_b)};
     int32_t  *from[2] = {(int32_t *)(ws + sp.from_a), (int32_t *)(ws + sp.from_b)};
     uint32_t *counts = (uint32_t *)(ws + sp.counts), *totals = (uint32_t *)(ws + sp.totals);
     int       at = 0;
-    if (N) {
-        LaunchTimer t(s, K_EMBED_SORT);
-        const unsigned lanes = (unsigned)((N + kEmbBlock - 1) / kEmbBlock), tiles = (unsigned)tiles_of(N);
-        if (cfg->id_dtype == CNGP_I32) embed_keys_kernel<int32_t><<<lanes, kEmbBlock, 0, s>>>((const int32_t *)ids, keys[0], N, cfg->rows);
-        else embed_keys_kernel<int64_t><<<lanes, kEmbBlock, 0, s>>>((const int64_t *)ids, keys[0], N, cfg->rows);
-        if (int rc = launch_status("embed_keys_kernel")) return rc;
-        bool first = true;
-        for (int shift = 0; shift < 32 && ((uint64_t)cfg->rows >> shift); shift += kDigitBits, at ^= 1, first = false) {
-            digit_count_kernel<<<tiles, kTileBlock, 0, s>>>(keys[at], N, shift, counts, tiles);
-            if (int rc = launch_status("digit_count_kernel")) return rc;
-            digit_row_scan_kernel<<<kDigits, kScanBlock, 0, s>>>(counts, tiles, totals);
-            if (int rc = launch_status("digit_row_scan_kernel")) return rc;
-            digit_scatter_kernel<<<tiles, kTileBlock, 0, s>>>(keys[at], first ? nullptr : from[at], N, shift, counts, tiles, totals, keys[at ^ 1], from[at ^ 1]);
-            if (int rc = launch_status("digit_scatter_kernel")) return rc;
-        }
+    if (int rc = cfg->id_dtype == CNGP_I64 ? sort_ids<int64_t>(ids, N, cfg->rows, keys, from, counts, totals, &at, s)
+                                           : sort_ids<int32_t>(ids, N, cfg->rows, keys, from, counts, totals, &at, s))
+        return rc;
+    SumArgs a{};
+    a.keys = keys[at]; a.from = from[at]; a.dy = dy; a.grad = grad_table;
+    a.head = (float *)(ws + sp.head); a.tail = (float *)(ws + sp.tail);
+    a.N = N; a.rows = cfg->rows; a.dim = cfg->dim; a.accumulate = accumulate; a.scale = cfg->scale;
+    a.piece = piece_of(N);
+    a.pieces = (uint32_t)((N + a.piece - 1) / a.piece);
+    const bool half = cfg->io_dtype == CNGP_F16;
+    switch (columns_of(cfg->dim, half ? 8 : 4)) {
+    case 8:  return sum_columns<__half, 8>(a, s);
+    case 4:  return half ? sum_columns<__half, 4>(a, s) : sum_columns<float, 4>(a, s);
+    case 2:  return half ? sum_columns<__half, 2>(a, s) : sum_columns<float, 2>(a, s);
+    default: return half ? sum_columns<__half, 1>(a, s) : sum_columns<float, 1>(a, s);
     }
-    LaunchTimer t(s, K_EMBED_SUMS);
-    const unsigned blocks = (unsigned)((cfg->rows + kEmbBlock / 64 - 1) / (kEmbBlock / 64));
-    if (cfg->io_dtype == CNGP_F16)
-        embed_sums_kernel<__half><<<blocks, kEmbBlock, 0, s>>>(keys[at], from[at], (const __half *)dy, grad_table, N, cfg->rows, cfg->dim, cfg->scale, accumulate);
-    else
-        embed_sums_kernel<float><<<blocks, kEmbBlock, 0, s>>>(keys[at], from[at], (const float *)dy, grad_table, N, cfg->rows, cfg->dim, cfg->scale, accumulate);
-    return launch_status("embed_sums_kernel");
 }
 
 }  // extern "C"

@@ -90,23 +90,23 @@ __global__ __launch_bounds__(kEmbBlock) void embed_fwd_kernel(const Id *__restri
 }
 
 // ---------------------------------------------------------------- sort of the ids
-template <typename Id>
+template <typename Id, int ROUNDS>
 __global__ __launch_bounds__(kTileBlock) void embed_keys_kernel(const Id *__restrict__ ids, uint32_t *__restrict__ keys, const int64_t N, const int64_t rows,
                                                                 uint32_t *__restrict__ counts, const int64_t tiles)
 {
     __shared__ uint32_t hist[kTileWaves * kDigits];
     const int     t = threadIdx.x, w = t >> 6;
-    const int64_t n0 = (int64_t)blockIdx.x * kTile;
+    const int64_t n0 = (int64_t)blockIdx.x * (kTileBlock * ROUNDS);
     for (int i = t; i < kTileWaves * kDigits; i += kTileBlock) hist[i] = 0;
     __syncthreads();
-    uint32_t key[kRounds];
+    uint32_t key[ROUNDS];
 #pragma unroll
-    for (int r = 0; r < kRounds; ++r) {
+    for (int r = 0; r < ROUNDS; ++r) {
         const int64_t n = n0 + (int64_t)r * kTileBlock + t;
         key[r] = n < N ? row_of(ids[n], rows) : 0u;
     }
 #pragma unroll
-    for (int r = 0; r < kRounds; ++r) {
+    for (int r = 0; r < ROUNDS; ++r) {
         const int64_t n = n0 + (int64_t)r * kTileBlock + t;
         if (n < N) {
             keys[n] = key[r];
@@ -117,45 +117,100 @@ __global__ __launch_bounds__(kTileBlock) void embed_keys_kernel(const Id *__rest
     flush_tile_histogram(hist, counts, tiles, blockIdx.x, t);
 }
 
-// Up to 16384 ids are sorted by one workgroup in LDS, all digits in one launch (the passes above are three launches each, of which a short
-// batch fills two workgroups).  Stable, eight bits at a time: a wavefront ranks its strip 64 elements at a time, lanes with equal digits
-// find each other by ballots; per digit the wavefronts' counts become their places.
-constexpr int kSmallBlock = 1024, kSmallWaves = kSmallBlock / 64, kSmallBits = 8, kSmallDigits = 1 << kSmallBits, kSmallMost = kSmallBlock * 16;
-template <typename Id, int ROUNDS>
+// Up to 16384 ids are sorted in one launch (the passes above are three launches each, of which a short batch fills a few workgroups).
+// Workgroup g owns an equal share of the keys: it reads all ids, keeps its own in their order, counts the smaller ones -- that is where its
+// share starts -- and sorts its share in LDS.  Nothing waits for another workgroup; ids that crowd in one share cost that one time.
+// The sort is stable, eight bits at a time: a wavefront ranks its strip 64 elements at a time, lanes with equal digits find each other
+// by ballots; per digit the wavefronts' counts become their places.
+constexpr int kSmallBlock = 1024, kSmallWaves = kSmallBlock / 64, kSmallBits = 8, kSmallDigits = 1 << kSmallBits, kSmallRounds = 16,
+              kSmallMost = kSmallBlock * kSmallRounds;
+template <typename Id>
 __global__ __launch_bounds__(kSmallBlock) void embed_sort_small_kernel(const Id *__restrict__ ids, uint32_t *__restrict__ keys, int32_t *__restrict__ from,
-                                                                       const int N, const int64_t rows)
+                                                                       const int N, const int64_t rows, const uint32_t share)
 {
-    extern __shared__ __align__(16) uint32_t small_lds[];
-    uint32_t *wave_count = small_lds;                          // [kSmallWaves][kSmallDigits]
-    uint32_t *stage_key = small_lds + kSmallWaves * kSmallDigits, *stage_from = stage_key + ROUNDS * kSmallBlock;
-    __shared__ uint32_t sums[kSmallDigits / 64];
-    const int t = threadIdx.x, w = t >> 6, lane = t & 63, n0 = w * (ROUNDS * 64) + lane;
+    extern __shared__ __align__(16) uint32_t small_lds[];      // counts [waves][digits], then keys and points of the share, N each
+    uint32_t *wave_count = small_lds, *stage_key = small_lds + kSmallWaves * kSmallDigits, *stage_from = stage_key + kSmallMost;
+    __shared__ uint32_t sums[kSmallDigits / 64], wave_mine[kSmallRounds][kSmallWaves], wave_less[kSmallWaves];
+    const int      t = threadIdx.x, w = t >> 6, lane = t & 63;
     const uint64_t below = lane ? (~0ull >> (64 - lane)) : 0ull;
-    uint32_t key[ROUNDS], at[ROUNDS], slot[ROUNDS];
+    const uint32_t key_lo = blockIdx.x * share, key_hi = key_lo + share;
+    const int      rounds = (N + kSmallBlock - 1) / kSmallBlock;
+
+    // the ids of the share, in their order: round r, wavefront w, lane
+    uint32_t key[kSmallRounds], less = 0;
 #pragma unroll
-    for (int r = 0; r < ROUNDS; ++r) {
-        const int n = n0 + r * 64;
-        key[r] = n < N ? row_of(ids[n], rows) : 0xffffffffu;   // elements that are not there sort behind all others
-        at[r] = (uint32_t)n;
+    for (int r = 0; r < kSmallRounds; ++r) {
+        const int n = r * kSmallBlock + t;
+        key[r] = r < rounds && n < N ? row_of(ids[n], rows) : 0xffffffffu;
     }
-    for (int shift = 0; shift < 32 && ((uint64_t)rows >> shift); shift += kSmallBits) {
+#pragma unroll
+    for (int r = 0; r < kSmallRounds; ++r) {
+        if (r < rounds) {
+            const uint64_t mine = __ballot(key[r] >= key_lo && key[r] < key_hi);
+            less += (uint32_t)__popcll(__ballot(key[r] < key_lo));
+            if (lane == 0) wave_mine[r][w] = (uint32_t)__popcll(mine);
+        }
+    }
+    if (lane == 0) wave_less[w] = less;
+    __syncthreads();
+    uint32_t base = 0;                                         // where the share starts among the sorted ids
+#pragma unroll
+    for (int k = 0; k < kSmallWaves; ++k) base += wave_less[k];
+    // counts of (round, wavefront) -> places, by the first four wavefronts
+    if (t < kSmallRounds * kSmallWaves) {
+        const uint32_t c = t < rounds * kSmallWaves ? (&wave_mine[0][0])[t] : 0u;
+        uint32_t       sum;
+        const uint32_t before = wave_exclusive_scan(c, &sum);
+        if (lane == 0) sums[w] = sum;
+        (&wave_mine[0][0])[t] = before;
+    }
+    __syncthreads();
+    const uint32_t s0 = sums[0], s1 = s0 + sums[1], s2 = s1 + sums[2], total = s2 + sums[3];
+#pragma unroll
+    for (int r = 0; r < kSmallRounds; ++r) {
+        const bool     in = key[r] >= key_lo && key[r] < key_hi;
+        const uint64_t mine = __ballot(in);
+        const int      part = (r * kSmallWaves + w) >> 6;
+        if (in) {
+            const uint32_t to = wave_mine[r][w] + (part == 0 ? 0u : part == 1 ? s0 : part == 2 ? s1 : s2) + (uint32_t)__popcll(mine & below);
+            stage_key[to] = key[r] - key_lo;
+            stage_from[to] = (uint32_t)(r * kSmallBlock + t);
+        }
+    }
+    __syncthreads();
+
+    const int strips = (int)((total + kSmallBlock - 1) / kSmallBlock), n0 = w * strips * 64 + lane;      // rounds of a wavefront's strip
+    uint32_t at[kSmallRounds], slot[kSmallRounds];
+    for (int shift = 0; shift < 32 && ((share - 1) >> shift); shift += kSmallBits) {
+#pragma unroll
+        for (int r = 0; r < kSmallRounds; ++r) {
+            const uint32_t n = (uint32_t)(n0 + r * 64);
+            const bool     there = r < strips && n < total;
+            key[r] = there ? stage_key[n] : 0xffffffffu;
+            at[r] = there ? stage_from[n] : 0u;
+        }
         for (int i = t; i < kSmallWaves * kSmallDigits; i += kSmallBlock) wave_count[i] = 0;
         __syncthreads();
         uint32_t *mine = wave_count + w * kSmallDigits;
 #pragma unroll
-        for (int r = 0; r < ROUNDS; ++r) {
-            const uint32_t digit = (key[r] >> shift) & (kSmallDigits - 1);
-            uint64_t       peers = ~0ull;
-#pragma unroll
-            for (int b = 0; b < kSmallBits; ++b) {
-                const bool     bit = (digit >> b) & 1u;
-                const uint64_t has = __ballot(bit);
-                peers &= bit ? has : ~has;
+        for (int r = 0; r < kSmallRounds; ++r) {
+            if (r < strips) {
+                const bool     valid = (uint32_t)(n0 + r * 64) < total;
+                const uint32_t digit = (key[r] >> shift) & (kSmallDigits - 1);
+                uint64_t       peers = __ballot(valid);
+    #pragma unroll
+                for (int b = 0; b < kSmallBits; ++b) {
+                    const bool     bit = (digit >> b) & 1u;
+                    const uint64_t has = __ballot(bit);
+                    peers &= bit ? has : ~has;
+                }
+                if (valid) {
+                    const uint32_t seen = mine[digit];
+                    slot[r] = seen + (uint32_t)__popcll(peers & below);
+                    if ((peers & below) == 0) mine[digit] = seen + (uint32_t)__popcll(peers);
+                }
+                __builtin_amdgcn_wave_barrier();
             }
-            const uint32_t seen = mine[digit];
-            slot[r] = seen + (uint32_t)__popcll(peers & below);
-            if ((peers & below) == 0) mine[digit] = seen + (uint32_t)__popcll(peers);
-            __builtin_amdgcn_wave_barrier();
         }
         __syncthreads();
         uint32_t count = 0, before = 0, sum = 0;
@@ -177,22 +232,18 @@ __global__ __launch_bounds__(kSmallBlock) void embed_sort_small_kernel(const Id 
         }
         __syncthreads();
 #pragma unroll
-        for (int r = 0; r < ROUNDS; ++r) {
-            const uint32_t to = mine[(key[r] >> shift) & (kSmallDigits - 1)] + slot[r];
-            stage_key[to] = key[r];
-            stage_from[to] = at[r];
+        for (int r = 0; r < kSmallRounds; ++r) {
+            if (r < strips && (uint32_t)(n0 + r * 64) < total) {
+                const uint32_t to = mine[(key[r] >> shift) & (kSmallDigits - 1)] + slot[r];
+                stage_key[to] = key[r];
+                stage_from[to] = at[r];
+            }
         }
         __syncthreads();
-#pragma unroll
-        for (int r = 0; r < ROUNDS; ++r) {
-            key[r] = stage_key[n0 + r * 64];
-            at[r] = stage_from[n0 + r * 64];
-        }
     }
-#pragma unroll
-    for (int r = 0; r < ROUNDS; ++r) {
-        const int n = n0 + r * 64;
-        if (n < N) { keys[n] = key[r]; from[n] = (int32_t)at[r]; }
+    for (uint32_t i = t; i < total; i += kSmallBlock) {
+        keys[base + i] = stage_key[i] + key_lo;
+        from[base + i] = (int32_t)stage_from[i];
     }
 }
 
@@ -345,32 +396,30 @@ __device__ __forceinline__ int64_t first_at(const uint32_t *__restrict__ keys, i
     return lo;
 }
 
-// Ids that reach over pieces: the piece in which one starts adds its tail and the heads of the pieces up to its end.
+// Ids that reach over pieces: the workgroup of the piece in which one starts adds its tail and the heads of the pieces up to its end,
+// its wavefronts every fourth step of them.
 template <int V, int LPR>
 __global__ __launch_bounds__(kEmbBlock) void embed_join_kernel(const SumArgs a)
 {
-    constexpr int  RL = 64 / LPR;
-    const int      lane = threadIdx.x & 63, cl = lane % LPR, rl = lane / LPR;
-    const uint32_t piece = blockIdx.x * (kEmbBlock / 64) + (threadIdx.x >> 6);
-    if (piece + 1 >= a.pieces) return;
-    const int64_t  w0 = (int64_t)piece * a.piece, w1 = w0 + a.piece;
-    const uint32_t key = a.keys[w1 - 1];
-    if (a.keys[w1] != key || key >= (uint32_t)a.rows || (w0 > 0 && a.keys[w0 - 1] == key)) return;      // does not start here and go on
+    constexpr int  RL = 64 / LPR, W = kEmbBlock / 64, AHEAD = V == 8 ? 4 : 8;
+    __shared__ float part[W][64 * V];
+    const int      lane = threadIdx.x & 63, w = threadIdx.x >> 6, cl = lane % LPR, rl = lane / LPR;
+    const uint32_t piece = blockIdx.x;
+    const int64_t  w0 = (int64_t)piece * a.piece, w1 = w0 + a.piece;       // not the last piece: all its positions are there
+    const uint32_t key = a.keys[w1 - 1], follows = a.keys[w1], came = w0 > 0 ? a.keys[w0 - 1] : 0xffffffffu;
+    if (follows != key || key >= (uint32_t)a.rows || came == key) return;  // none starts here and goes on
     const uint32_t end = (uint32_t)((first_at(a.keys, w1, a.N, key + 1u) - 1) / a.piece);               // the piece it ends in
     const int      c = ((int)blockIdx.y * LPR + cl) * V, cc = c < a.dim ? c : 0;
     float sum[V];
-    if (rl == 0) {
-        load_run<float, V>(sum, a.tail + (int64_t)piece * a.dim + cc);
-    } else {
 #pragma unroll
-        for (int v = 0; v < V; ++v) sum[v] = 0.0f;
-    }
-    for (uint32_t q = piece + 1 + rl; q <= end; q += RL * 4) {
-        float h[4][V];
+    for (int v = 0; v < V; ++v) sum[v] = 0.0f;
+    if (w == 0 && rl == 0) load_run<float, V>(sum, a.tail + (int64_t)piece * a.dim + cc);
+    for (uint32_t q = piece + 1 + (uint32_t)w * RL * AHEAD + rl; q <= end; q += W * RL * AHEAD) {
+        float h[AHEAD][V];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) load_run<float, V>(h[u], a.head + (int64_t)(q + u * RL <= end ? q + u * RL : q) * a.dim + cc);
+        for (int u = 0; u < AHEAD; ++u) load_run<float, V>(h[u], a.head + (int64_t)(q + u * RL <= end ? q + u * RL : q) * a.dim + cc);
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
+        for (int u = 0; u < AHEAD; ++u)
 #pragma unroll
             for (int v = 0; v < V; ++v) sum[v] += u == 0 || q + u * RL <= end ? h[u][v] : 0.0f;
     }
@@ -378,7 +427,15 @@ __global__ __launch_bounds__(kEmbBlock) void embed_join_kernel(const SumArgs a)
     for (int d = LPR; d < 64; d <<= 1)
 #pragma unroll
         for (int v = 0; v < V; ++v) sum[v] += __shfl_xor(sum[v], d, 64);
-    if (rl == 0 && c < a.dim) put_row<V>(a, key, c, sum);
+#pragma unroll
+    for (int v = 0; v < V; ++v) part[w][v * 64 + lane] = sum[v];
+    __syncthreads();
+    if (w != 0 || rl != 0 || c >= a.dim) return;
+#pragma unroll
+    for (int i = 1; i < W; ++i)
+#pragma unroll
+        for (int v = 0; v < V; ++v) sum[v] += part[i][v * 64 + lane];
+    put_row<V>(a, key, c, sum);
 }
 
 __global__ __launch_bounds__(kEmbBlock) void embed_clear_kernel(float *__restrict__ grad, const int64_t n)
@@ -412,12 +469,21 @@ int columns_of(int dim, int most) {
     return v;
 }
 
-// Positions of a piece: 128, or as many as leave 8192 pieces (the joins of one id in all of a large batch stay short).  A multiple of
-// 64 row lanes.
-uint32_t piece_of(int64_t N) {
-    const int64_t p = (N + 8191) / 8192;
-    return (uint32_t)(p <= 128 ? 128 : (p + 63) / 64 * 64);
+// Lanes to a row of the gradient, `columns` values each.
+int lanes_of(int dim, int columns) {
+    const int n = dim / columns;
+    return n <= 1 ? 1 : n <= 4 ? 4 : n <= 16 ? 16 : 64;
 }
+
+// Positions of a piece: eight per row lane (what is in flight), or as many as leave 8192 wavefronts over pieces and column tiles.
+uint32_t piece_of(const cngp_embed_config *c, int64_t N) {
+    const int     columns = columns_of(c->dim, c->io_dtype == CNGP_F16 ? 8 : 4), lpr = lanes_of(c->dim, columns), rl = 64 / lpr;
+    const int64_t tiles = (c->dim / columns + lpr - 1) / lpr, each = (N * tiles / rl + 8191) / 8192;
+    return (uint32_t)(std::max<int64_t>(each, kSumAhead) * rl);
+}
+
+// Elements per lane of the sort's tiles: sixteen once those fill the chip, four for shorter batches.
+int rounds_of(int64_t N) { return N >= (int64_t)512 * kTile ? kRounds : 4; }
 
 struct EmbedSpace { size_t keys_a, keys_b, from_a, from_b, counts, totals, head, tail, bytes; };
 EmbedSpace space_of(const cngp_embed_config *c, int64_t N) {
@@ -425,13 +491,13 @@ EmbedSpace space_of(const cngp_embed_config *c, int64_t N) {
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t o = at; at += align256(bytes); return o; };
     if (!N) return s;
-    const size_t col = (size_t)N * 4, pieces = (size_t)((N + piece_of(N) - 1) / piece_of(N));
+    const size_t col = (size_t)N * 4, piece = piece_of(c, N), pieces = ((size_t)N + piece - 1) / piece;
     s.keys_a = take(col);
     s.from_a = take(col);
     if (N > kSmallMost) {
         s.keys_b = take(col);
         s.from_b = take(col);
-        s.counts = take((size_t)kDigits * (size_t)tiles_of(N) * 4);
+        s.counts = take((size_t)kDigits * (size_t)((N + kTileBlock * rounds_of(N) - 1) / (kTileBlock * rounds_of(N))) * 4);
         s.totals = take((size_t)kDigits * 4);
     }
     s.head = take(pieces * (size_t)c->dim * 4);
@@ -440,14 +506,35 @@ EmbedSpace space_of(const cngp_embed_config *c, int64_t N) {
     return s;
 }
 
-template <typename Id, int ROUNDS>
+// Shares of the keys 0 .. rows: a workgroup for every 64 ids, at most one per CU (each reads all ids; a share of 256 keys is one pass).
+template <typename Id>
 int sort_small(const void *ids, uint32_t *keys, int32_t *from, int64_t N, int64_t rows, hipStream_t s) {
-    const size_t lds = (size_t)(kSmallWaves * kSmallDigits + 2 * ROUNDS * kSmallBlock) * 4;
-    if (lds > 64 * 1024)
-        if (hipError_t e = hipFuncSetAttribute((const void *)embed_sort_small_kernel<Id, ROUNDS>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds))
-            return record_hip_failure(e, "hipFuncSetAttribute(MaxDynamicSharedMemorySize)");
-    embed_sort_small_kernel<Id, ROUNDS><<<1, kSmallBlock, lds, s>>>((const Id *)ids, keys, from, (int)N, rows);
+    constexpr size_t lds = (size_t)(kSmallWaves * kSmallDigits + 2 * kSmallMost) * 4;
+    if (hipError_t e = hipFuncSetAttribute((const void *)embed_sort_small_kernel<Id>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds))
+        return record_hip_failure(e, "hipFuncSetAttribute(MaxDynamicSharedMemorySize)");
+    const int64_t groups = std::min<int64_t>(std::max<int64_t>((N + 63) / 64, 1), 256), share = (rows + 1 + groups - 1) / groups;
+    embed_sort_small_kernel<Id><<<(unsigned)((rows + 1 + share - 1) / share), kSmallBlock, lds, s>>>((const Id *)ids, keys, from, (int)N, rows, (uint32_t)share);
     return launch_status("embed_sort_small_kernel");
+}
+
+template <typename Id, int ROUNDS>
+int sort_passes(const void *ids, int64_t N, int64_t rows, uint32_t *(&keys)[2], int32_t *(&from)[2], uint32_t *counts, uint32_t *totals, int *at, hipStream_t s) {
+    constexpr int  TILE = kTileBlock * ROUNDS;
+    const unsigned tiles = (unsigned)((N + TILE - 1) / TILE);
+    embed_keys_kernel<Id, ROUNDS><<<tiles, kTileBlock, 0, s>>>((const Id *)ids, keys[0], N, rows, counts, tiles);
+    if (int rc = launch_status("embed_keys_kernel")) return rc;
+    for (int shift = 0; shift < 32 && ((uint64_t)rows >> shift); shift += kDigitBits, *at ^= 1) {
+        if (shift) {
+            digit_count_kernel<ROUNDS><<<tiles, kTileBlock, 0, s>>>(keys[*at], N, shift, counts, tiles);
+            if (int rc = launch_status("digit_count_kernel")) return rc;
+        }
+        digit_row_scan_kernel<<<kDigits, kScanBlock, 0, s>>>(counts, tiles, totals);
+        if (int rc = launch_status("digit_row_scan_kernel")) return rc;
+        digit_scatter_kernel<ROUNDS><<<tiles, kTileBlock, 0, s>>>(keys[*at], shift ? from[*at] : nullptr, N, shift, counts, tiles, totals, keys[*at ^ 1],
+                                                                  from[*at ^ 1]);
+        if (int rc = launch_status("digit_scatter_kernel")) return rc;
+    }
+    return CNGP_OK;
 }
 
 // Sorted keys and the points they came from, in keys[0] and from[0] or, after an odd number of passes, [1]: *at says which.
@@ -455,23 +542,9 @@ template <typename Id>
 int sort_ids(const void *ids, int64_t N, int64_t rows, uint32_t *(&keys)[2], int32_t *(&from)[2], uint32_t *counts, uint32_t *totals, int *at, hipStream_t s) {
     LaunchTimer t(s, K_EMBED_SORT);
     *at = 0;
-    if (N <= kSmallBlock) return sort_small<Id, 1>(ids, keys[0], from[0], N, rows, s);
-    if (N <= kSmallBlock * 4) return sort_small<Id, 4>(ids, keys[0], from[0], N, rows, s);
-    if (N <= kSmallMost) return sort_small<Id, 16>(ids, keys[0], from[0], N, rows, s);
-    const unsigned tiles = (unsigned)tiles_of(N);
-    embed_keys_kernel<Id><<<tiles, kTileBlock, 0, s>>>((const Id *)ids, keys[0], N, rows, counts, tiles);
-    if (int rc = launch_status("embed_keys_kernel")) return rc;
-    for (int shift = 0; shift < 32 && ((uint64_t)rows >> shift); shift += kDigitBits, *at ^= 1) {
-        if (shift) {
-            digit_count_kernel<<<tiles, kTileBlock, 0, s>>>(keys[*at], N, shift, counts, tiles);
-            if (int rc = launch_status("digit_count_kernel")) return rc;
-        }
-        digit_row_scan_kernel<<<kDigits, kScanBlock, 0, s>>>(counts, tiles, totals);
-        if (int rc = launch_status("digit_row_scan_kernel")) return rc;
-        digit_scatter_kernel<<<tiles, kTileBlock, 0, s>>>(keys[*at], shift ? from[*at] : nullptr, N, shift, counts, tiles, totals, keys[*at ^ 1], from[*at ^ 1]);
-        if (int rc = launch_status("digit_scatter_kernel")) return rc;
-    }
-    return CNGP_OK;
+    if (N <= kSmallMost) return sort_small<Id>(ids, keys[0], from[0], N, rows, s);
+    return rounds_of(N) == kRounds ? sort_passes<Id, kRounds>(ids, N, rows, keys, from, counts, totals, at, s)
+                                   : sort_passes<Id, 4>(ids, N, rows, keys, from, counts, totals, at, s);
 }
 
 template <typename Io, int V, int LPR>
@@ -481,16 +554,17 @@ int sum_rows(const SumArgs &a, hipStream_t s) {
     embed_sums_kernel<Io, V, LPR><<<dim3(groups, columns), kEmbBlock, 0, s>>>(a);
     if (int rc = launch_status("embed_sums_kernel")) return rc;
     if (a.pieces < 2) return CNGP_OK;
-    embed_join_kernel<V, LPR><<<dim3(groups, columns), kEmbBlock, 0, s>>>(a);
+    embed_join_kernel<V, LPR><<<dim3(a.pieces - 1, columns), kEmbBlock, 0, s>>>(a);
     return launch_status("embed_join_kernel");
 }
 template <typename Io, int V>
 int sum_columns(const SumArgs &a, hipStream_t s) {
-    const int lanes = a.dim / V;
-    if (lanes <= 1) return sum_rows<Io, V, 1>(a, s);
-    if (lanes <= 4) return sum_rows<Io, V, 4>(a, s);
-    if (lanes <= 16) return sum_rows<Io, V, 16>(a, s);
-    return sum_rows<Io, V, 64>(a, s);
+    switch (lanes_of(a.dim, V)) {
+    case 1:  return sum_rows<Io, V, 1>(a, s);
+    case 4:  return sum_rows<Io, V, 4>(a, s);
+    case 16: return sum_rows<Io, V, 16>(a, s);
+    default: return sum_rows<Io, V, 64>(a, s);
+    }
 }
 
 template <typename Id, typename Table, typename Io, int V>
@@ -567,7 +641,7 @@ int cngp_embed_bwd(const cngp_embed_config *cfg, const void *ids, int64_t N, con
     a.keys = keys[at]; a.from = from[at]; a.dy = dy; a.grad = grad_table;
     a.head = (float *)(ws + sp.head); a.tail = (float *)(ws + sp.tail);
     a.N = N; a.rows = cfg->rows; a.dim = cfg->dim; a.accumulate = accumulate; a.scale = cfg->scale;
-    a.piece = piece_of(N);
+    a.piece = piece_of(cfg, N);
     a.pieces = (uint32_t)((N + a.piece - 1) / a.piece);
     const bool half = cfg->io_dtype == CNGP_F16;
     switch (columns_of(cfg->dim, half ? 8 : 4)) {

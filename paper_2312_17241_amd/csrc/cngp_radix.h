@@ -11,7 +11,7 @@ constexpr int kDigitBits = 7;
 constexpr int kDigits = 1 << kDigitBits;
 constexpr int kTileBlock = 512;          // 8 wavefronts per tile
 constexpr int kTileWaves = kTileBlock / 64;
-constexpr int kRounds = 16;              // elements per lane
+constexpr int kRounds = 16;              // elements per lane, where a batch fills the chip with such tiles
 constexpr int kTile = kTileBlock * kRounds;
 constexpr int kScanBlock = 1024;
 
@@ -30,22 +30,23 @@ __device__ __forceinline__ void flush_tile_histogram(const uint32_t *hist, uint3
     }
 }
 
+template <int ROUNDS>
 __global__ __launch_bounds__(kTileBlock) void digit_count_kernel(const uint32_t *__restrict__ keys, const int64_t N, const int shift,
                                                                  uint32_t *__restrict__ counts, const int64_t tiles)
 {
     __shared__ uint32_t hist[kTileWaves * kDigits];
     const int     t = threadIdx.x, w = t >> 6;
-    const int64_t n0 = (int64_t)blockIdx.x * kTile;
+    const int64_t n0 = (int64_t)blockIdx.x * (kTileBlock * ROUNDS);
     for (int i = t; i < kTileWaves * kDigits; i += kTileBlock) hist[i] = 0;
     __syncthreads();
-    uint32_t key[kRounds];
+    uint32_t key[ROUNDS];
 #pragma unroll
-    for (int r = 0; r < kRounds; ++r) {
+    for (int r = 0; r < ROUNDS; ++r) {
         const int64_t n = n0 + (int64_t)r * kTileBlock + t;
         key[r] = n < N ? keys[n] : 0u;
     }
 #pragma unroll
-    for (int r = 0; r < kRounds; ++r) {
+    for (int r = 0; r < ROUNDS; ++r) {
         const int64_t n = n0 + (int64_t)r * kTileBlock + t;
         if (n < N) atomicAdd(&hist[w * kDigits + ((key[r] >> shift) & (kDigits - 1))], 1u);
     }
@@ -99,6 +100,7 @@ __global__ __launch_bounds__(kScanBlock) void digit_row_scan_kernel(uint32_t *__
 // One pass of the sort for one tile.  keys_in in the order of the previous pass; index_in NULL = the identity
 // (first pass).  keys_out NULL on the last pass (nobody reads them).  Element n of the input goes to
 //   sum of totals of smaller digits + counts[digit][tile] (prefix over earlier tiles) + its rank inside the tile.
+template <int ROUNDS>
 __global__ __launch_bounds__(kTileBlock) void digit_scatter_kernel(
     const uint32_t *__restrict__ keys_in, const int32_t *__restrict__ index_in, const int64_t N, const int shift,
     const uint32_t *__restrict__ counts, const int64_t tiles, const uint32_t *__restrict__ totals,
@@ -107,29 +109,30 @@ __global__ __launch_bounds__(kTileBlock) void digit_scatter_kernel(
     __shared__ uint32_t wave_count[kTileWaves * kDigits];   // per wavefront and digit: running count, then base inside the digit's run
     __shared__ uint32_t tile_start[kDigits];                // first slot of the digit in the sorted tile
     __shared__ uint32_t dest[kDigits];                      // global position of that slot
-    __shared__ uint32_t stage[kTile];                       // the tile in sorted order: first its keys, then its indices
+    __shared__ uint32_t stage[kTileBlock * ROUNDS];          // the tile in sorted order: first its keys, then its indices
     __shared__ uint32_t carry[2];
     const int     t = threadIdx.x, w = t >> 6, lane = t & 63;
     const int64_t tile = blockIdx.x;
-    const int64_t n0 = tile * kTile;
-    const int     tile_n = (int)((N - n0 < kTile) ? N - n0 : kTile);
+    constexpr int TILE = kTileBlock * ROUNDS;
+    const int64_t n0 = tile * TILE;
+    const int     tile_n = (int)((N - n0 < TILE) ? N - n0 : TILE);
     uint32_t     *mine = wave_count + w * kDigits;
     for (int i = t; i < kTileWaves * kDigits; i += kTileBlock) wave_count[i] = 0;
     __syncthreads();
 
     // rank of every element among the equal digits before it in this wavefront's eighth of the tile
-    uint32_t key[kRounds], rank[kRounds];
-    int32_t  index[kRounds];
-    const int64_t  w0 = n0 + (int64_t)w * (kRounds * 64);
+    uint32_t key[ROUNDS], rank[ROUNDS];
+    int32_t  index[ROUNDS];
+    const int64_t  w0 = n0 + (int64_t)w * (ROUNDS * 64);
     const uint64_t below = lane ? (~0ull >> (64 - lane)) : 0ull;
 #pragma unroll
-    for (int r = 0; r < kRounds; ++r) {
+    for (int r = 0; r < ROUNDS; ++r) {
         const int64_t n = w0 + r * 64 + lane;
         key[r] = n < N ? keys_in[n] : 0u;
         index[r] = n < N ? (index_in ? index_in[n] : (int32_t)n) : 0;
     }
 #pragma unroll
-    for (int r = 0; r < kRounds; ++r) {
+    for (int r = 0; r < ROUNDS; ++r) {
         const int64_t  n = w0 + r * 64 + lane;
         const bool     valid = n < N;
         const uint32_t digit = (key[r] >> shift) & (kDigits - 1);
@@ -175,16 +178,16 @@ __global__ __launch_bounds__(kTileBlock) void digit_scatter_kernel(
     // keys: into LDS in sorted order (rank[] becomes the slot), out in runs of consecutive addresses;
     // slot j of the sorted tile is element (j - tile_start[digit]) of its digit's run
 #pragma unroll
-    for (int r = 0; r < kRounds; ++r) {
+    for (int r = 0; r < ROUNDS; ++r) {
         const int64_t  n = w0 + r * 64 + lane;
         const uint32_t digit = (key[r] >> shift) & (kDigits - 1);
-        rank[r] = n < N ? tile_start[digit] + mine[digit] + rank[r] : (uint32_t)kTile;
-        if (rank[r] < (uint32_t)kTile) stage[rank[r]] = key[r];
+        rank[r] = n < N ? tile_start[digit] + mine[digit] + rank[r] : (uint32_t)TILE;
+        if (rank[r] < (uint32_t)TILE) stage[rank[r]] = key[r];
     }
     __syncthreads();
-    uint32_t to[kRounds];
+    uint32_t to[ROUNDS];
 #pragma unroll
-    for (int i = 0; i < kRounds; ++i) {
+    for (int i = 0; i < ROUNDS; ++i) {
         const int j = t + i * kTileBlock;
         to[i] = 0xffffffffu;
         if (j < tile_n) {
@@ -197,11 +200,11 @@ __global__ __launch_bounds__(kTileBlock) void digit_scatter_kernel(
     __syncthreads();
     // indices: the same way through the same buffer
 #pragma unroll
-    for (int r = 0; r < kRounds; ++r)
-        if (rank[r] < (uint32_t)kTile) stage[rank[r]] = (uint32_t)index[r];
+    for (int r = 0; r < ROUNDS; ++r)
+        if (rank[r] < (uint32_t)TILE) stage[rank[r]] = (uint32_t)index[r];
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kRounds; ++i) {
+    for (int i = 0; i < ROUNDS; ++i) {
         const int j = t + i * kTileBlock;
         if (j < tile_n && (int64_t)to[i] < N) index_out[to[i]] = (int32_t)stage[j];
     }

@@ -121,12 +121,12 @@ int morton_sort(const float *x, int64_t N, int32_t *perm, float *x_sorted, char 
     for (int pass = 0; pass < passes; ++pass) {
         const int shift = pass * kDigitBits;
         if (pass) {
-            digit_count_kernel<<<grid, kTileBlock, 0, s>>>(k_in[pass], N, shift, counts, tiles);
+            digit_count_kernel<kRounds><<<grid, kTileBlock, 0, s>>>(k_in[pass], N, shift, counts, tiles);
             if (hipError_t e = hipGetLastError()) return cngp::record_hip_failure(e, "digit_count_kernel");
         }
         digit_row_scan_kernel<<<kDigits, kScanBlock, 0, s>>>(counts, tiles, totals);
         if (hipError_t e = hipGetLastError()) return cngp::record_hip_failure(e, "digit_row_scan_kernel");
-        digit_scatter_kernel<<<grid, kTileBlock, 0, s>>>(k_in[pass], i_in[pass], N, shift, counts, tiles, totals, k_out[pass], i_out[pass]);
+        digit_scatter_kernel<kRounds><<<grid, kTileBlock, 0, s>>>(k_in[pass], i_in[pass], N, shift, counts, tiles, totals, k_out[pass], i_out[pass]);
         if (hipError_t e = hipGetLastError()) return cngp::record_hip_failure(e, "digit_scatter_kernel");
     }
     if (x_sorted) {

@@ -4,7 +4,8 @@
 //     d loss / d logit_rk = N_p / W * sigma_rk (f_k - sum_j f_j sigma_rj)
 // The gradient of every row needs the level's f, so two launches: one reads the logits and leaves sums per workgroup, the other
 // adds those up (in a fixed order), reads the logits again and writes the gradient.  Both stream: a lane holds four neighbouring
-// logits, so a row of sixteen is four lanes that exchange their maximum and sums with two shuffles each.
+// logits, so a row of sixteen is four lanes that exchange their maximum and sums with two lane permutations each.  The sparse variant ranks
+// a row's logits once, in the first launch, and leaves four bits per lane for the second.
 #include <cmath>
 #include <cstdint>
 
@@ -27,6 +28,7 @@ struct BalArgs {
     int32_t       *counts;
     float         *part_p;               // [L][chunks][NP]
     int32_t       *part_n;               // [L][chunks][NP] winners
+    uint8_t       *kept;                 // [L][quads] which of four logits keep weight, top_k < N_p
     uint32_t       N_c, quads;           // rows and groups of four logits per level
     uint32_t       chunks, per_chunk;    // groups of four logits per workgroup
     uint32_t       top_k;
@@ -62,73 +64,92 @@ struct Quad {
     }
 };
 
-// Largest of a row by the rule of the bake: a NaN never wins, equal values go to the lowest index, no number at all gives 0.
-template <int NP>
-__device__ __forceinline__ uint32_t winner(const float (&v)[4], const int first) {
-    constexpr int G = NP / 4;
-    uint32_t best = 0;
-    float    top = 0.0f;
-    bool     have = false;
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-        if (v[k] == v[k] && (!have || v[k] > top)) { best = (uint32_t)(first + k); top = v[k]; have = true; }
-#pragma unroll
-    for (int s = 1; s < G; s <<= 1) {
-        const float    ov = __shfl_xor(top, s, 64);
-        const uint32_t ob = (uint32_t)__shfl_xor((int)best, s, 64);
-        const bool     oh = __shfl_xor((int)have, s, 64) != 0;
-        if (oh && (!have || ov > top || (ov == top && ob < best))) { best = ob; top = ov; have = true; }
-    }
-    return best;
+// The value of lane ^ X among four neighbouring lanes.
+template <int X, typename T>
+__device__ __forceinline__ T across(const T v) {
+    static_assert(X >= 1 && X <= 3 && sizeof(T) == 4, "a quad of lanes");
+    constexpr int perm = X == 1 ? 0xB1 : X == 2 ? 0x4E : 0x1B;
+    return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), perm, 0xf, 0xf, true));
 }
-
-// Entries outside the top_k largest (equal values by lowest index, any number before a NaN) become minus infinity.
-template <int NP>
-__device__ __forceinline__ void keep_largest(float (&v)[4], const int first, const uint32_t top_k) {
-    uint32_t ahead[4] = {0, 0, 0, 0};
-    const int lane0 = (int)(threadIdx.x & 63u) & ~(NP / 4 - 1);
-#pragma unroll
-    for (int g = 0; g < NP / 4; ++g)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float o = __shfl(v[j], lane0 + g, 64);
-            const int   oi = 4 * g + j;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const bool o_num = o == o, v_num = v[k] == v[k];
-                ahead[k] += ((o_num && !v_num) || (o_num == v_num && (o > v[k] || ((o == v[k] || !v_num) && oi < first + k)))) ? 1u : 0u;
-            }
-        }
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-        if (ahead[k] >= top_k) v[k] = -INFINITY;
-}
-
 template <int G>
 __device__ __forceinline__ float row_sum(float s) {
-#pragma unroll
-    for (int o = 1; o < G; o <<= 1) s += __shfl_xor(s, o, 64);
+    if (G >= 2) s += across<1>(s);
+    if (G >= 4) s += across<2>(s);
     return s;
 }
 template <int G>
 __device__ __forceinline__ float row_max(float m) {
-#pragma unroll
-    for (int o = 1; o < G; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+    if (G >= 2) m = fmaxf(m, across<1>(m));
+    if (G >= 4) m = fmaxf(m, across<2>(m));
     return m;
 }
 
-// The four logits become their softmax weights; win[k]: entry k won its row.  All lanes of a wavefront call this together.
-template <int NP, bool SPARSE>
-__device__ __forceinline__ void weigh(Quad<NP> &q, const int first, const uint32_t top_k, bool (&win)[4]) {
+// Which entry of a row wins by the rule of the bake, given its largest number: the first that equals it; none does if there is no
+// number, and that gives 0.
+template <int NP>
+__device__ __forceinline__ uint32_t winner(const float (&v)[4], const int first, const float top) {
+    uint32_t best = 255;
+#pragma unroll
+    for (int k = 3; k >= 0; --k) best = v[k] == top ? (uint32_t)(first + k) : best;
+    if (NP >= 8) best = min(best, across<1>(best));
+    if (NP >= 16) best = min(best, across<2>(best));
+    return best == 255 ? 0 : best;
+}
+
+// Bit k: entry k of this lane is among the top_k largest of its row (equal values by lowest index, any number before a NaN).  Values are
+// compared as integers in the order of the numbers, a NaN below all; one that comes earlier counts from equality on.
+template <int X, int NP>
+__device__ __forceinline__ void count_ahead(const uint32_t (&key)[4], const int sub, uint32_t (&ahead)[4]) {
+    const uint32_t earlier = (sub ^ X) < sub ? 1u : 0u;
+    uint32_t       bar[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) bar[k] = key[k] - earlier;     // keys are at least 1
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t o = across<X>(key[j]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) ahead[k] += o > bar[k] ? 1u : 0u;
+    }
+}
+template <int NP>
+__device__ __forceinline__ uint32_t largest(const float (&v)[4], const int sub, const uint32_t top_k) {
+    uint32_t key[4], ahead[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t u = __builtin_bit_cast(uint32_t, v[k] + 0.0f);      // -0 is 0
+        key[k] = v[k] == v[k] ? ((u >> 31) ? ~u : u | 0x80000000u) : 1u;   // minus infinity is 0x7fffff
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (j != k) ahead[k] += (j < k ? key[j] >= key[k] : key[j] > key[k]) ? 1u : 0u;
+    if (NP >= 8) count_ahead<1, NP>(key, sub, ahead);
+    if (NP >= 16) {
+        count_ahead<2, NP>(key, sub, ahead);
+        count_ahead<3, NP>(key, sub, ahead);
+    }
+    uint32_t kept = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) kept |= (ahead[k] < top_k ? 1u : 0u) << k;
+    return kept;
+}
+
+// The four logits become their softmax weights; WINNERS: win[k] says whether entry k won its row.  With SPARSE, bit k of `kept` says
+// whether entry k keeps weight: found here with WINNERS, else given.  All lanes of a wavefront call this together.
+template <int NP, bool SPARSE, bool WINNERS>
+__device__ __forceinline__ void weigh(Quad<NP> &q, const int first, const uint32_t top_k, uint32_t &kept, bool (&win)[4]) {
     using Q = Quad<NP>;
     if constexpr (NP >= 4) {
-        const uint32_t best = winner<NP>(q.v, first);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) win[k] = best == (uint32_t)(first + k);
-        if (SPARSE) keep_largest<NP>(q.v, first, top_k);
+        if (SPARSE && WINNERS) kept = largest<NP>(q.v, first / 4, top_k);
         const float m = row_max<Q::G>(fmaxf(fmaxf(q.v[0], q.v[1]), fmaxf(q.v[2], q.v[3])));
+        if (WINNERS) {
+            const uint32_t best = winner<NP>(q.v, first, m);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) q.v[k] = expf(q.v[k] - m);
+            for (int k = 0; k < 4; ++k) win[k] = best == (uint32_t)(first + k);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) q.v[k] = !SPARSE || ((kept >> k) & 1u) ? expf(q.v[k] - m) : 0.0f;
         const float s = 1.0f / row_sum<Q::G>((q.v[0] + q.v[1]) + (q.v[2] + q.v[3]));
 #pragma unroll
         for (int k = 0; k < 4; ++k) q.v[k] *= s;
@@ -139,7 +160,12 @@ __device__ __forceinline__ void weigh(Quad<NP> &q, const int first, const uint32
             const bool second = b == b && (!(a == a) || b > a);
             win[2 * r] = !second;
             win[2 * r + 1] = second;
-            if (SPARSE) (second ? a : b) = -INFINITY;
+            if (SPARSE) {                                      // the one that stays has all the weight
+                (second ? a : b) = 0.0f;
+                float &stays = second ? b : a;
+                stays = expf(stays - stays);
+                continue;
+            }
             const float m = fmaxf(a, b);
             a = expf(a - m);
             b = expf(b - m);
@@ -167,10 +193,12 @@ __global__ __launch_bounds__(kBalBlock) void balance_sums_kernel(const BalArgs a
     uint32_t n[4] = {0, 0, 0, 0};
     for (uint32_t base = q0; base < q1; base += kBalBlock) {      // whole wavefronts stay: the lanes exchange
         const uint32_t at = base + t < q1 ? base + t : 0xffffffffu;
-        Q    q;
-        bool win[4];
+        Q        q;
+        bool     win[4];
+        uint32_t kept = 15u;
         q.load(a, level, at);
-        weigh<NP, SPARSE>(q, first, a.top_k, win);
+        weigh<NP, SPARSE, true>(q, first, a.top_k, kept, win);
+        if (SPARSE && NP >= 4 && a.grad && at != 0xffffffffu) a.kept[(size_t)level * a.quads + at] = (uint8_t)kept;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const bool c = q.counted[k / (4 / Q::R)];
@@ -260,10 +288,12 @@ __global__ __launch_bounds__(kBalBlock) void balance_grad_kernel(const BalArgs a
     for (uint32_t base = q0; base < q1; base += kBalBlock) {
         const bool     live = base + t < q1;
         const uint32_t at = live ? base + t : 0xffffffffu;
-        Q    q;
-        bool win[4];
+        Q        q;
+        bool     win[4];
+        uint32_t kept = 15u;
         q.load(a, level, at);
-        weigh<NP, SPARSE>(q, first, a.top_k, win);
+        if (SPARSE && NP >= 4 && live) kept = a.kept[(size_t)level * a.quads + at];
+        weigh<NP, SPARSE, false>(q, first, a.top_k, kept, win);
         float g[4];
 #pragma unroll
         for (int r = 0; r < Q::R; ++r) {
@@ -290,12 +320,17 @@ __global__ __launch_bounds__(kBalBlock) void balance_grad_kernel(const BalArgs a
     }
 }
 
+uint64_t quads_of(const cngp_config *c) { return ((uint64_t)c->N_c * c->N_p + 3) / 4; }
+bool     sparse_rows(const cngp_config *c) { return c->N_p >= 4 && c->top_k && c->top_k < c->N_p; }
+
 // Four groups of logits per lane before a level gets another workgroup, and at most kMostChunks workgroups per level.
 uint32_t chunks_of(const cngp_config *c) {
-    const uint64_t quads = ((uint64_t)c->N_c * c->N_p + 3) / 4, per = (uint64_t)kBalBlock * 4;
+    const uint64_t quads = quads_of(c), per = (uint64_t)kBalBlock * 4;
     const uint64_t want = (quads + per - 1) / per;
     return (uint32_t)(want < 1 ? 1 : want > (uint64_t)kMostChunks ? (uint64_t)kMostChunks : want);
 }
+
+size_t sums_bytes(const cngp_config *c) { return ((size_t)c->L * chunks_of(c) * c->N_p * 8 + 255) / 256 * 256; }
 
 template <int NP, bool SPARSE>
 int run(const BalArgs &a, const int L, hipStream_t s) {
@@ -315,7 +350,7 @@ extern "C" {
 
 size_t cngp_probe_balance_workspace_bytes(const cngp_config *cfg) {
     if (validate(cfg)) return 0;
-    return ((size_t)cfg->L * chunks_of(cfg) * cfg->N_p * 8 + 255) & ~(size_t)255;
+    return sums_bytes(cfg) + (sparse_rows(cfg) ? (((size_t)cfg->L * quads_of(cfg)) + 255) / 256 * 256 : 0);
 }
 
 int cngp_probe_balance(const cngp_config *cfg, const float *Dhat_c, const uint8_t *rows, float weight, float *loss, int32_t *counts,
@@ -331,7 +366,8 @@ int cngp_probe_balance(const cngp_config *cfg, const float *Dhat_c, const uint8_
     a.chunks = chunks_of(cfg);
     a.part_p = (float *)workspace;
     a.part_n = (int32_t *)workspace + (size_t)cfg->L * a.chunks * cfg->N_p;
-    const uint64_t quads = ((uint64_t)cfg->N_c * cfg->N_p + 3) / 4;      // at most 2^32: N_c <= 2^30, N_p <= 16
+    a.kept = (uint8_t *)workspace + sums_bytes(cfg);
+    const uint64_t quads = quads_of(cfg);                      // at most 2^32: N_c <= 2^30, N_p <= 16
     if (quads > 0xfffffff0ull - (uint64_t)kBalBlock * kMostChunks) return CNGP_ERR_UNSUPPORTED;
     a.quads = (uint32_t)quads;
     // a multiple of a workgroup's step, so that the lanes of a row stay together

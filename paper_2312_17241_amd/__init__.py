@@ -127,7 +127,7 @@ _lib = _load()
 class _Marshalled:
     """A frozen configuration's C struct by reference, made at the first call that passes it and kept with the configuration (beside its fields:
     not in __dict__, comparisons, copies or pickles).  Making it anew took a quarter of a small call's time: 1.7 of 6.5 us."""
-    __slots__ = ("_kept",)
+    __slots__ = ("_kept", "_rooms")          # _rooms: workspace sizes of the operators' calls (operators.py)
 
     def _ref(self):
         try:

@@ -7,26 +7,22 @@ namespace {
 
 inline size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
 
-// The state that reaches each window, from the windows' maps: 16 channels to a workgroup, 64 lanes with up to 16 windows each, held in
+// The state that reaches each window, from the windows' maps: a wavefront per channel, a lane with up to 16 neighbouring windows, held in
 // registers between composing them and walking them with the state.
-constexpr int kCarryChannels = 16, kCarryLanes = 64, kCarryEach = 16, kMostWindows = kCarryLanes * kCarryEach;
-__global__ __launch_bounds__(kCarryChannels * kCarryLanes) void recur_carry_kernel(const Cut cut, const int C)
+constexpr int kCarryEach = 16, kMostWindows = 64 * kCarryEach;
+__global__ __launch_bounds__(64) void recur_carry_kernel(const Cut cut, const int C)
 {
-    __shared__ float sum_a[kCarryLanes][kCarryChannels], sum_b[kCarryLanes][kCarryChannels];
-    __shared__ int   sum_cut[kCarryLanes];
-    const int      cl = threadIdx.x % kCarryChannels, rl = threadIdx.x / kCarryChannels;
-    const int      c_here = (int)blockIdx.x * kCarryChannels + cl, c = c_here < C ? c_here : C - 1;
-    const uint32_t per = (cut.K + kCarryLanes - 1) / kCarryLanes, k0 = rl * per;
+    const int      lane = threadIdx.x, c = (int)blockIdx.x;
+    const uint32_t per = (cut.K + 63) / 64, k0 = lane * per;
     float a[kCarryEach], b[kCarryEach];
     int   f[kCarryEach];
 #pragma unroll
     for (int i = 0; i < kCarryEach; ++i) {
         const uint32_t k = k0 + i;
         const bool     there = (uint32_t)i < per && k < cut.K;
-        const size_t   at = (size_t)(there ? k : 0) * C + c;
-        f[i] = there ? cut.piece_cut[there ? k : 0] : 0;
-        a[i] = there ? cut.piece_a[at] : 1.0f;
-        b[i] = there ? cut.piece_b[at] : 0.0f;
+        f[i] = there ? cut.piece_cut[k] : 0;
+        a[i] = there ? cut.piece_a[(size_t)k * C + c] : 1.0f;
+        b[i] = there ? cut.piece_b[(size_t)k * C + c] : 0.0f;
     }
     float A = 1.0f, B = 0.0f;
     int   gone = 0;
@@ -36,20 +32,23 @@ __global__ __launch_bounds__(kCarryChannels * kCarryLanes) void recur_carry_kern
         A *= a[i];
         gone |= f[i];
     }
-    sum_a[rl][cl] = A;
-    sum_b[rl][cl] = B;
-    if (cl == 0) sum_cut[rl] = gone;
-    __syncthreads();
-    float h = 0.0f;
-#pragma unroll 8
-    for (int i = 0; i < kCarryLanes; ++i) {
-        const float next = sum_cut[i] ? sum_b[i][cl] : fmaf(sum_a[i][cl], h, sum_b[i][cl]);
-        h = i < rl ? next : h;
+    const uint64_t cuts = __ballot(gone);
+    const uint64_t upto = cuts & (~0ull >> (63 - lane));
+    const int      since = upto ? 63 - __clzll(upto) : -1;     // last lane, up to this one, with a window that forgets
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const float Al = __shfl_up(A, d, 64), Bl = __shfl_up(B, d, 64);
+        if (lane >= d && since <= lane - d) {
+            B = fmaf(A, Bl, B);
+            A *= Al;
+        }
     }
+    const float before = __shfl_up(B, 1, 64);
+    float       h = lane ? before : 0.0f;                      // the first window's state is 0
 #pragma unroll
     for (int i = 0; i < kCarryEach; ++i) {
         const uint32_t k = k0 + i;
-        if ((uint32_t)i < per && k < cut.K && c_here < C) cut.carry[(size_t)k * C + c] = h;
+        if ((uint32_t)i < per && k < cut.K) cut.carry[(size_t)k * C + c] = h;
         h = f[i] ? b[i] : fmaf(a[i], h, b[i]);
     }
 }
@@ -156,7 +155,7 @@ int cngp::recur_copy(const float *from, float *to, int64_t n, hipStream_t s) {
 
 int cngp::recur_carry(const Cut &cut, int C, hipStream_t s) {
     LaunchTimer t(s, K_RECUR_CARRY);
-    recur_carry_kernel<<<(unsigned)((C + kCarryChannels - 1) / kCarryChannels), kCarryChannels * kCarryLanes, 0, s>>>(cut, C);
+    recur_carry_kernel<<<(unsigned)C, 64, 0, s>>>(cut, C);
     return launch_status("recur_carry_kernel");
 }
 

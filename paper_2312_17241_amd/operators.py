@@ -73,9 +73,12 @@ class EmbedConfig(_Marshalled):
         return CEmbedConfig(self.rows, self.dim, self.table_dtype, self.io_dtype, self.id_dtype, self.scale, self.flags)
 
 
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)      # the number alone: 0.1 us against 0.6
+
+
 def _on_current_device(*tensors):
     """The kernels go to the current device's stream: a tensor of another device would be reached through the wrong one."""
-    here = torch.cuda.current_device()
+    here = _device()
     for t in tensors:
         if t is not None and t.get_device() != here:
             raise ValueError(f"tensors must lie on the current device (cuda:{here}), got one on {t.device}")
@@ -90,6 +93,21 @@ def _room(need, workspace, like):
     if workspace is None and need:
         workspace = torch.empty(need, dtype=torch.uint8, device=like.device)
     return workspace
+
+
+def _need(query, cfg, *sizes):
+    """Bytes of a call's workspace, kept with the configuration: host arithmetic, but a microsecond through ctypes."""
+    try:
+        rooms = cfg._rooms
+    except AttributeError:
+        rooms = {}
+        object.__setattr__(cfg, "_rooms", rooms)
+    need = rooms.get((query, sizes))
+    if need is None:
+        if len(rooms) >= 256:
+            rooms.clear()
+        need = rooms[query, sizes] = int(getattr(_lib, query)(cfg._ref(), *sizes))
+    return need
 
 
 def _out(given, shape, dtype, like, name):
@@ -114,7 +132,7 @@ def _sequences(N, offsets, sequences):
 
 def recur_workspace_bytes(cfg: RecurConfig, N, sequences, backward=False, ragged=False, with_y=True) -> int:
     call = (_CALL_BWD if backward else 0) | (_CALL_RAGGED if ragged else 0) | (0 if with_y or not backward else _CALL_NO_Y)
-    return int(_lib.cngp_recur_workspace_bytes(cfg._ref(), N, sequences, call))
+    return _need("cngp_recur_workspace_bytes", cfg, N, sequences, call)
 
 
 def recur_fwd(cfg: RecurConfig, gate, x, h0=None, offsets=None, sequences=None, y=True, last=True, workspace=None):
@@ -152,7 +170,7 @@ def recur_bwd(cfg: RecurConfig, gate, x, dy=None, dlast=None, h0=None, y=None, o
 
 
 def embed_workspace_bytes(cfg: EmbedConfig, N) -> int:
-    return int(_lib.cngp_embed_workspace_bytes(cfg._ref(), N))
+    return _need("cngp_embed_workspace_bytes", cfg, N)
 
 
 def embed_fwd(cfg: EmbedConfig, ids, table, base=None, y=None):
@@ -181,7 +199,7 @@ def embed_bwd(cfg: EmbedConfig, ids, dy, grad_table=None, workspace=None):
 
 
 def probe_balance_workspace_bytes(cfg) -> int:
-    return int(_lib.cngp_probe_balance_workspace_bytes(cfg._ref()))
+    return _need("cngp_probe_balance_workspace_bytes", cfg)
 
 
 def probe_balance(cfg, Dhat_c, weight=1.0, rows=None, grad_Dhat_c=True, loss=None, counts=None, workspace=None):

@@ -62,7 +62,7 @@ def check(L, N_c, N_p, top_k=0, rows=None, weight=0.7, accumulate=False, seed=1,
         held[rows == 0] = np.where(g.random((int((rows == 0).sum()), N_p)) < 0.5, np.nan, np.inf)
     cfg = config(L, N_c, N_p, top_k, 0 if accumulate else cngp.ZERO_GRADS)
     before = g.normal(size=v.shape).astype(np.float32) if accumulate else np.full(v.shape, np.nan, np.float32)
-    ws = torch.full((cngp.probe_balance_workspace_bytes(cfg),), 255, dtype=torch.uint8, device=DEV)
+    ws = torch.full((max(cngp.probe_balance_workspace_bytes(cfg), 256),), 255, dtype=torch.uint8, device=DEV)
     dev = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to(DEV)
     rd = None if rows is None else dev(rows)
     loss, counts, grad = cngp.probe_balance(cfg, dev(held), weight, rows=rd, grad_Dhat_c=dev(before), workspace=ws)
@@ -81,7 +81,7 @@ def check(L, N_c, N_p, top_k=0, rows=None, weight=0.7, accumulate=False, seed=1,
 
 
 @pytest.mark.parametrize("N_p", [1, 2, 4, 8, 16])
-@pytest.mark.parametrize("N_c", [1, 2, 4, 64, 256, 2048, 2**14])
+@pytest.mark.parametrize("N_c", [1, 2, 4, 64, 256, 2048, 4096, 2**14])
 @pytest.mark.parametrize("rows", [None, "some", "none"])
 @pytest.mark.parametrize("accumulate", [False, True])
 def test_shapes(N_p, N_c, rows, accumulate):
@@ -90,8 +90,9 @@ def test_shapes(N_p, N_c, rows, accumulate):
 
 @pytest.mark.parametrize("N_p,top_k", [(2, 1), (2, 2), (4, 1), (4, 3), (8, 2), (8, 7), (16, 1), (16, 4), (16, 16), (1, 1)])
 @pytest.mark.parametrize("rows", [None, "some"])
-def test_sparse_backward(N_p, top_k, rows):
-    check(2, 1024, N_p, top_k, rows)
+@pytest.mark.parametrize("N_c", [1024, 8192])
+def test_sparse_backward(N_p, top_k, rows, N_c):
+    check(2, N_c, N_p, top_k, rows)
 
 
 def test_ties_and_wide_logits():

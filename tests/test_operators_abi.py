@@ -116,10 +116,12 @@ def test_balance_refuses():
         assert balance(config(), **kw) == cngp.ERR_NULL, kw
     for w in (float("nan"), float("inf"), -float("inf")):
         assert balance(config(), weight=w) == cngp.ERR_INVALID
-    need = cngp.probe_balance_workspace_bytes(config())
-    assert need > 0 and need % 256 == 0
-    for kw in (dict(ws=None), dict(ws=OFF), dict(size=need - 1)):
-        assert balance(config(), **kw) == cngp.ERR_WORKSPACE, kw
+    assert cngp.probe_balance_workspace_bytes(config()) == 0               # a level of a few rows: one launch
+    for big in (config(N_c=2**14), config(N_c=2**14, top_k=2)):
+        need = cngp.probe_balance_workspace_bytes(big)
+        assert need > 0 and need % 256 == 0
+        for kw in (dict(ws=None), dict(ws=OFF), dict(size=need - 1)):
+            assert balance(big, **kw) == cngp.ERR_WORKSPACE, kw
 
 
 def test_binding_refuses_wrong_tensors():

@@ -15,6 +15,7 @@ namespace cngp {
 
 constexpr int kRecurBlock = 256;
 constexpr int kRowsEach = 8;             // rows of a tile per lane
+constexpr int kRowsNarrow = 4;           // ... where a lane holds all channels
 constexpr int kNarrowBlock = 64;         // rows of up to four channels, each whole in a lane: a wavefront by itself
 
 constexpr int kWideBlock = 512;          // workgroups that walk whole long sequences

@@ -103,7 +103,7 @@ RecurPlan plan_of(const cngp_recur_config *c, int64_t N, int64_t S, bool ragged)
     p.V = C <= 4 ? C : C > 32 && C % 2 == 0 ? 2 : 1;
     p.block = p.CL == 1 ? kNarrowBlock : kRecurBlock;
     p.tiles = (C + p.CL * p.V - 1) / (p.CL * p.V);
-    const int64_t tile_rows = p.block / p.CL * kRowsEach;
+    const int64_t tile_rows = p.CL == 1 ? kNarrowBlock * kRowsNarrow : p.block / p.CL * kRowsEach;
     const int64_t mean = S ? (N + S - 1) / S : 0;
     const int64_t longest = !ragged ? mean : c->longest ? std::min<int64_t>(c->longest, N) : 4 * mean;
     // windows that give every CU eight workgroups, of whole tiles

@@ -8,16 +8,11 @@ using namespace cngp;
 
 // The gate of a row and how much of the input it lets in.  1 - exp(g) cancels for small g: there it is -g times the series of
 // (exp(g) - 1) / g to the ninth term (0.5^9 / 10! = 5e-10 below one), and exp(g) is one minus that, to the last bit.
-template <bool MIX>
-__device__ __forceinline__ void gate_of(const bool log_gate, const float g, float &a, float &in) {
-    if (!log_gate) {
-        a = g;
-        in = MIX ? 1.0f - g : 1.0f;
-        return;
-    }
-    a = expf(g);
-    in = 1.0f;
-    if (MIX) {
+template <bool LOG, bool MIX>
+__device__ __forceinline__ void gate_of(const float g, float &a, float &in) {
+    a = LOG ? expf(g) : g;
+    in = 1.0f - a;
+    if (LOG && MIX) {
         float s = fmaf(g, 1.0f / 362880.0f, 1.0f / 40320.0f);
         s = fmaf(s, g, 1.0f / 5040.0f);
         s = fmaf(s, g, 1.0f / 720.0f);
@@ -27,7 +22,7 @@ __device__ __forceinline__ void gate_of(const bool log_gate, const float g, floa
         s = fmaf(s, g, 0.5f);
         s = fmaf(s, g, 1.0f);
         const bool small = fabsf(g) < 0.5f;
-        in = small ? -g * s : 1.0f - a;
+        in = small ? -g * s : in;
         a = small ? 1.0f - in : a;
     }
 }
@@ -163,6 +158,29 @@ __device__ __forceinline__ void store_run(T *lowest, const float (&in)[RB][V], c
     __builtin_memcpy(lowest, &raw, sizeof raw);
 }
 
+// The gates of a lane's rows.  The two forms are two loops: chosen value by value, the compiler computes both.
+template <int RB, int GV, bool MIX, typename R>
+__device__ __forceinline__ void gates_of(const bool log_gate, const R &raw, const bool back, float (&g)[RB][GV], float (&share)[MIX ? RB : 1][GV]) {
+    float in;
+    if (log_gate) {
+#pragma unroll
+        for (int j = 0; j < RB; ++j)
+#pragma unroll
+            for (int v = 0; v < GV; ++v) {
+                gate_of<true, MIX>(raw.get(j, v, back), g[j][v], in);
+                if (MIX) share[MIX ? j : 0][v] = in;
+            }
+    } else {
+#pragma unroll
+        for (int j = 0; j < RB; ++j)
+#pragma unroll
+            for (int v = 0; v < GV; ++v) {
+                gate_of<false, MIX>(raw.get(j, v, back), g[j][v], in);
+                if (MIX) share[MIX ? j : 0][v] = in;
+            }
+    }
+}
+
 // PIECE: only the composed map of the rows that the next window continues, for `carry`; else the outputs.
 // CL lanes side by side hold V channels each of a row, RB rows each.  Y: type of the states, written forward and read backward.
 template <typename Io, typename Gate, typename Y, int BLOCK, int CL, int V, int RB, bool SHARED, bool MIX, bool BWD, bool PIECE>
@@ -287,26 +305,21 @@ __global__ __launch_bounds__(BLOCK) void recur_scan_kernel(const RecurArgs a, co
             if (starts_here && before) {
 #pragma unroll
                 for (int j = 0; j < RB; ++j)
-                    if ((first >> j) & 1u) load_vec<float, V>(h_first[j], before + (int64_t)mark_first[mark0 + j] * a.C + c);
+                    if ((first >> j) & 1u) load_vec<float, V>(h_first[j], before + (uint64_t)(uint32_t)mark_first[mark0 + j] * (uint32_t)a.C + c);
             }
         }
         if constexpr (BWD && !PIECE) {
             if (ends_here && a.h0) {
 #pragma unroll
                 for (int j = 0; j < RB; ++j)
-                    if ((last >> j) & 1u) load_vec<float, V>(h_last[j], a.h0 + (int64_t)mark_last[mark0 + j] * a.C + c);
+                    if ((last >> j) & 1u) load_vec<float, V>(h_last[j], a.h0 + (uint64_t)(uint32_t)mark_last[mark0 + j] * (uint32_t)a.C + c);
             }
         }
 
         float g[RB][GV], in[RB][V], share[MIX ? RB : 1][GV];
+        gates_of<RB, GV, MIX>(log_gate, now.g, o.back, g, share);
 #pragma unroll
         for (int j = 0; j < RB; ++j) {
-#pragma unroll
-            for (int v = 0; v < GV; ++v) {
-                float in_share;
-                gate_of<MIX>(log_gate, now.g.get(j, v, o.back), g[j][v], in_share);
-                if (MIX) share[MIX ? j : 0][v] = in_share;
-            }
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 in[j][v] = !BWD || a.dy ? now.in.get(j, v, o.back) : 0.0f;
@@ -446,7 +459,7 @@ __global__ __launch_bounds__(BLOCK) void recur_scan_kernel(const RecurArgs a, co
             }
             if ((last >> j) & 1u) {
                 float *to = BWD ? a.dh0 : a.last;
-                if (c_ok && to) store_vec<float, V>(to + (int64_t)mark_last[mark0 + j] * a.C + c, h);
+                if (c_ok && to) store_vec<float, V>(to + (uint64_t)(uint32_t)mark_last[mark0 + j] * (uint32_t)a.C + c, h);
             }
         }
         constexpr uint32_t ALL = (1u << RB) - 1u;
@@ -494,7 +507,7 @@ __global__ __launch_bounds__(BLOCK) void recur_scan_kernel(const RecurArgs a, co
 template <typename Io, typename Gate, typename Y, int V, bool SHARED, bool MIX, bool BWD, bool PIECE>
 __global__ __launch_bounds__(64) void recur_narrow_kernel(const RecurArgs a, const Cut cut)
 {
-    constexpr int RB = kRowsEach, TR = 64 * RB, GV = SHARED ? 1 : V;
+    constexpr int RB = kRowsNarrow, TR = 64 * RB, GV = SHARED ? 1 : V;
     __shared__ __align__(16) uint32_t mark_first[PIECE ? 4 : TR], mark_last[PIECE ? 4 : TR];     // sequence (in order taken) + 1, or 0
     __shared__ float from_s[PIECE ? 1 : 64 * V], left_s[BWD && !PIECE ? 64 * V : 1];
     const int      lane = threadIdx.x;
@@ -559,10 +572,11 @@ __global__ __launch_bounds__(64) void recur_narrow_kernel(const RecurArgs a, con
         const int64_t to = p1 - pt < TR ? p1 : pt + TR, q0 = q_at;
         const bool    whole = pt + TR <= p1;
         if (!PIECE) {
-            *reinterpret_cast<uint4 *>(mark_first + lane * RB) = make_uint4(0, 0, 0, 0);
-            *reinterpret_cast<uint4 *>(mark_first + lane * RB + 4) = make_uint4(0, 0, 0, 0);
-            *reinterpret_cast<uint4 *>(mark_last + lane * RB) = make_uint4(0, 0, 0, 0);
-            *reinterpret_cast<uint4 *>(mark_last + lane * RB + 4) = make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < RB; i += 4) {
+                *reinterpret_cast<uint4 *>(mark_first + lane * RB + i) = make_uint4(0, 0, 0, 0);
+                *reinterpret_cast<uint4 *>(mark_last + lane * RB + i) = make_uint4(0, 0, 0, 0);
+            }
             __syncthreads();
             for (int64_t q = q0;;) {
                 const int64_t f = now.first, l = now.behind;
@@ -612,14 +626,9 @@ __global__ __launch_bounds__(64) void recur_narrow_kernel(const RecurArgs a, con
         }
 
         float g[RB][GV], in[RB][V], share[MIX ? RB : 1][GV];
+        gates_of<RB, GV, MIX>(log_gate, now.g, o.back, g, share);
 #pragma unroll
         for (int j = 0; j < RB; ++j) {
-#pragma unroll
-            for (int v = 0; v < GV; ++v) {
-                float in_share;
-                gate_of<MIX>(log_gate, now.g.get(j, v, o.back), g[j][v], in_share);
-                if (MIX) share[MIX ? j : 0][v] = in_share;
-            }
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 in[j][v] = !BWD || a.dy ? now.in.get(j, v, o.back) : 0.0f;
@@ -820,7 +829,7 @@ int launch_lanes(const RecurArgs &a, const RecurPlan &p, const Cut &cut, hipStre
         CNGP_NARROW(4);
 #undef CNGP_NARROW
     }
-    if (p.block == kWideBlock) CNGP_RECUR(kWideBlock, 16, 2, (BWD ? kRowsEach : 2 * kRowsEach));
+    if (p.block == kWideBlock) CNGP_RECUR(kWideBlock, 16, 2, kRowsEach);
     if (p.CL == 16) CNGP_RECUR(kRecurBlock, 16, 1, kRowsEach);
     if (p.V == 1) CNGP_RECUR(kRecurBlock, 32, 1, kRowsEach);
     CNGP_RECUR(kRecurBlock, 32, 2, kRowsEach);

@@ -390,7 +390,7 @@ int cngp_adam_step(const cngp_adam *opt, int64_t n, float *master, void *half_co
  * (entries outside are taken as the nearest of the two; with entries that decrease the results are unspecified, but no array is
  * left).  Rows before the first sequence and behind the last one are neither used nor written.
  * offsets NULL: N / sequences rows each, which must divide.  A sequence without rows passes its state on (last = h0, dh0 = dlast).
- *   channels  1 .. 65536       N, sequences  below 2^31       gate dev gate_dtype [N, gate_channels]      x dev io_dtype [N, channels]
+ *   channels  1 .. 65536       N, sequences  at most 2^31 - 2^16       gate dev gate_dtype [N, gate_channels]      x dev io_dtype [N, channels]
  *   h0    dev float32 [sequences, channels], or NULL (zeros)
  *   y     dev io_dtype [N, channels], every row's state, written; or NULL
  *   last  dev float32 [sequences, channels], the state after the last row taken, written; or NULL; may be h0 itself.

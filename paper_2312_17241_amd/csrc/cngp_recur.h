@@ -25,6 +25,9 @@ __device__ __forceinline__ float load(const __half *p, const int64_t i) { return
 __device__ __forceinline__ void store(float *p, const int64_t i, const float v) { p[i] = v; }
 __device__ __forceinline__ void store(__half *p, const int64_t i, const float v) { p[i] = __float2half_rn(v); }
 
+using pos = int32_t;                     // rows and sequences: at most kMostRows of each, so that the end of a tile behind the last is one too
+constexpr int64_t kMostRows = 0x7fff0000;
+
 struct RecurArgs {
     const void    *gate, *x;
     const int32_t *offsets;
@@ -33,7 +36,7 @@ struct RecurArgs {
     void          *out_y, *dgate, *dx;
     float         *last, *dh0;
     float         *slope;                // backward of a gate that several channel tiles share: their sums, fp32 [tiles][N]
-    int64_t        N, S, rows_each;
+    pos            N, S, rows_each;
     int32_t        C, G;
     uint32_t       flags;
     int32_t        y_f32;
@@ -41,17 +44,17 @@ struct RecurArgs {
 
 struct Order {
     const int32_t *offsets;
-    int64_t        N, S, rows_each;
+    pos        N, S, rows_each;
     bool           back;                 // taken from the last row to the first
-    __device__ __forceinline__ int64_t at(const int64_t q) const {       // ps(q), 0 <= q <= S
+    __device__ __forceinline__ pos at(const pos q) const {       // ps(q), 0 <= q <= S
         if (!offsets) return q * rows_each;
-        int64_t o = offsets[back ? S - q : q];
+        pos o = offsets[back ? S - q : q];
         o = o < 0 ? 0 : o > N ? N : o;
         return back ? N - o : o;
     }
-    __device__ __forceinline__ int64_t sequence(const int64_t q) const { return back ? S - 1 - q : q; }
+    __device__ __forceinline__ pos sequence(const pos q) const { return back ? S - 1 - q : q; }
     // First q with ps(q) >= p, for two p at once (S + 1 if there is none); a wavefront calls this together, 64 probes at a time.
-    __device__ void first_from(const int64_t pa, const int64_t pb, int64_t &qa, int64_t &qb) const {
+    __device__ void first_from(const pos pa, const pos pb, pos &qa, pos &qb) const {
         if (!offsets) {
             qa = (pa + rows_each - 1) / rows_each;
             qb = (pb + rows_each - 1) / rows_each;
@@ -59,23 +62,23 @@ struct Order {
             qb = qb < S + 1 ? qb : S + 1;
             return;
         }
-        const int64_t lane = threadIdx.x & 63;
-        int64_t lo[2] = {0, 0}, hi[2] = {S + 1, S + 1};         // the answers lie in [lo, hi]
-        const int64_t want[2] = {pa, pb};
+        const pos lane = threadIdx.x & 63;
+        pos lo[2] = {0, 0}, hi[2] = {S + 1, S + 1};         // the answers lie in [lo, hi]
+        const pos want[2] = {pa, pb};
         while (lo[0] < hi[0] || lo[1] < hi[1]) {
             bool    less[2];
-            int64_t step[2];
+            pos step[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 step[i] = (hi[i] - lo[i] + 63) / 64;
-                const int64_t probe = lo[i] + lane * step[i];
+                const pos probe = lo[i] + lane * step[i];
                 less[i] = probe < hi[i] && at(probe < S ? probe : S) < want[i];
             }
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const uint64_t before = __ballot(less[i]);
                 if (!before) { hi[i] = lo[i]; continue; }
-                const int64_t last = lo[i] + (63 - __clzll(before)) * step[i];      // the last probe that lies before p
+                const pos last = lo[i] + (63 - __clzll(before)) * step[i];      // the last probe that lies before p
                 lo[i] = last + 1;
                 hi[i] = last + step[i] < hi[i] ? last + step[i] : hi[i];
             }
@@ -88,7 +91,7 @@ struct Order {
 // Windows of rows: workgroup (k, channel tile) of a launch takes the sequences that start in [k R, (k + 1) R) -- or exactly those
 // rows, where a long sequence is cut: then the state at k R comes from `carry`.
 struct Cut {
-    int64_t  R;
+    pos      R;
     uint32_t K;
     float   *piece_a, *piece_b, *carry;  // [K][C]
     int32_t *piece_cut;                  // [K]

@@ -79,7 +79,7 @@ int check(const cngp_recur_config *c, int64_t N, int64_t S, bool ragged) {
     if (c->gate_dtype != CNGP_F32 && c->gate_dtype != CNGP_F16) return CNGP_ERR_INVALID;
     if (c->longest < 0) return CNGP_ERR_INVALID;
     if (c->flags & ~(uint32_t)(CNGP_RECUR_REVERSE | CNGP_RECUR_LOG_GATE | CNGP_RECUR_MIX)) return CNGP_ERR_INVALID;
-    if (N < 0 || N > 0x7fffffffLL || S < 0 || S > 0x7ffffffeLL) return CNGP_ERR_INVALID;
+    if (N < 0 || N > kMostRows || S < 0 || S > kMostRows) return CNGP_ERR_INVALID;
     if (!ragged && (S == 0 ? N != 0 : N % S != 0)) return CNGP_ERR_INVALID;
     return CNGP_OK;
 }
@@ -87,7 +87,7 @@ int check(const cngp_recur_config *c, int64_t N, int64_t S, bool ragged) {
 RecurArgs args_of(const cngp_recur_config *c, const void *gate, const void *x, int64_t N, const int32_t *offsets, int64_t S, const float *h0) {
     RecurArgs a{};
     a.gate = gate; a.x = x; a.offsets = offsets; a.h0 = h0;
-    a.N = N; a.S = S; a.rows_each = S ? N / S : 0;
+    a.N = (pos)N; a.S = (pos)S; a.rows_each = (pos)(S ? N / S : 0);
     a.C = c->channels; a.G = c->gate_channels; a.flags = c->flags;
     return a;
 }

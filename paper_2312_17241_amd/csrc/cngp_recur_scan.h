@@ -42,15 +42,15 @@ __device__ __forceinline__ void gate_of(const float g, float &a, float &in) {
 
 // A window's sequences [qa, qb) and rows [p0, p1), in the order taken.
 struct Window {
-    int64_t qa, qb, p0, p1;
+    pos qa, qb, p0, p1;
     __device__ __forceinline__ bool find(const RecurArgs &a, const Cut &cut, const Order &o, const uint32_t k) {
-        const int64_t edge0 = (int64_t)k * cut.R, edge1 = edge0 + cut.R;
+        const pos     edge0 = (pos)k * cut.R, edge1 = k + 1 == cut.K ? a.N : edge0 + cut.R;
         const bool    final_window = k + 1 == cut.K;
         o.first_from(edge0, edge1, qa, qb);
         if (k == 0) qa = 0;
         if (final_window || qb > a.S) qb = a.S;
         if (cut.exact) {
-            const int64_t lo = o.at(0), hi = o.at(a.S);
+            const pos lo = o.at(0), hi = o.at(a.S);
             p0 = edge0 < lo ? lo : edge0;
             p1 = edge1 < hi && !final_window ? edge1 : hi;
             return true;
@@ -62,10 +62,10 @@ struct Window {
     }
     // The rows whose map the next window needs: those of the sequence that goes on in it.  False: none does, or it starts there.
     // q: that sequence if it starts in here, else -1.
-    __device__ __forceinline__ bool piece(const RecurArgs &a, const Cut &cut, const Order &o, const uint32_t k, const bool writes, int64_t &q) {
+    __device__ __forceinline__ bool piece(const RecurArgs &a, const Cut &cut, const Order &o, const uint32_t k, const bool writes, pos &q) {
         q = qb - 1;
         const bool    goes_on = k + 1 != cut.K && p1 > p0 && q >= 0 && o.at(q + 1) > p1;
-        const int64_t begin = goes_on ? o.at(q) : p1;
+        const pos begin = goes_on ? o.at(q) : p1;
         const bool    starts = !goes_on || begin >= p0;
         if (writes) cut.piece_cut[k] = starts;
         if (!goes_on) return false;
@@ -96,7 +96,7 @@ __device__ __forceinline__ void store_vec(T *p, const float (&in)[V]) {
 // Where a tile's rows lie.  Row j of a lane is memory row low + mine + j, or low + mine - j taken backwards; `low` is the same for
 // the whole workgroup, so a load is a scalar base and a 32-bit lane offset.
 struct Place {
-    int64_t  low;
+    pos  low;
     uint32_t mine;                       // rows
     int      dir;                        // 1 or -1
 };
@@ -109,44 +109,45 @@ struct Rows {
 
     // `width` values to a row of the array, this lane's from c on.  Not a whole tile: rows outside [p0, p1) hold those of the nearest row
     // inside, or, in a run that lies inside the N rows of the array, whatever is there.  pr: the lane's first row, in the order taken.
-    __device__ __forceinline__ void load_from(const void *array, const Place &at, const int width, const int c, const bool whole, const int64_t N,
-                                              const int64_t pr, const int64_t p0, const int64_t p1) {
+    __device__ __forceinline__ void load_from(const void *array, const Place &at, const int width, const int c, const bool whole, const pos N,
+                                              const pos pr, const pos p0, const pos p1) {
         if constexpr (NARROW) {
-            const int64_t lowest = at.low + (int64_t)at.mine - (at.dir < 0 ? RB - 1 : 0);
+            const pos lowest = at.low + (pos)at.mine - (at.dir < 0 ? RB - 1 : 0);
             if (whole || (lowest >= 0 && lowest + RB <= N)) {
-                __builtin_memcpy(&raw, (const T *)array + lowest * V, sizeof raw);
+                __builtin_memcpy(&raw, (const T *)array + (int64_t)lowest * V, sizeof raw);
             } else {
 #pragma unroll
                 for (int j = 0; j < RB; ++j) {                 // row j of the run
-                    const int64_t p = pr + (at.dir < 0 ? RB - 1 - j : j), q = p < p0 ? p0 : p < p1 ? p : p1 - 1;
-                    __builtin_memcpy(&raw.e[j * V], (const T *)array + (at.low + (int64_t)at.mine + at.dir * (q - pr)) * V, sizeof(T) * V);
+                    const pos p = pr + (at.dir < 0 ? RB - 1 - j : j), q = p < p0 ? p0 : p < p1 ? p : p1 - 1;
+                    __builtin_memcpy(&raw.e[j * V], (const T *)array + (int64_t)(at.low + (pos)at.mine + at.dir * (q - pr)) * V, sizeof(T) * V);
                 }
             }
         } else {
             const uint32_t mine = at.mine * (uint32_t)width + (uint32_t)c;
-            const T       *base = (const T *)array + at.low * width;
+            const T       *base = (const T *)array + (int64_t)at.low * width;
             if (whole) {
 #pragma unroll
                 for (int j = 0; j < RB; ++j) __builtin_memcpy(&raw.e[j * V], base + (int64_t)(at.dir * j) * width + mine, sizeof(T) * V);
             } else {
 #pragma unroll
                 for (int j = 0; j < RB; ++j) {
-                    const int64_t p = pr + j < p0 ? p0 : pr + j < p1 ? pr + j : p1 - 1;
-                    __builtin_memcpy(&raw.e[j * V], base + (int64_t)mine + at.dir * (p - pr) * width, sizeof(T) * V);
+                    const pos p = pr + j < p0 ? p0 : pr + j < p1 ? pr + j : p1 - 1;
+                    __builtin_memcpy(&raw.e[j * V], base + (int64_t)mine + (int64_t)(at.dir * (p - pr)) * width, sizeof(T) * V);
                 }
             }
         }
     }
     __device__ __forceinline__ float get(const int j, const int v, const bool back) const {
         if constexpr (!NARROW) return load(raw.e, j * V + v);
-        return back ? load(raw.e, (RB - 1 - j) * V + v) : load(raw.e, j * V + v);
+        const float f = load(raw.e, j * V + v), b = load(raw.e, (RB - 1 - j) * V + v);      // both, then one: values, not an index
+        return back ? b : f;
     }
 };
 
 // Row j of a lane's outputs (not NARROW).
 template <typename T>
 __device__ __forceinline__ T *row_at(void *array, const Place &at, const int width, const int c, const int j) {
-    return (T *)array + (at.low + at.dir * j) * width + (at.mine * (uint32_t)width + (uint32_t)c);
+    return (T *)array + (int64_t)(at.low + at.dir * j) * width + (at.mine * (uint32_t)width + (uint32_t)c);
 }
 template <typename T, int RB, int V>
 __device__ __forceinline__ void store_run(T *lowest, const float (&in)[RB][V], const bool back) {
@@ -213,13 +214,13 @@ __global__ __launch_bounds__(BLOCK) void recur_scan_kernel(const RecurArgs a, co
 #pragma unroll
     for (int v = 0; v < V; ++v) carry_b[v] = 0.0f;
     if (PIECE) {
-        int64_t q;
+        pos q;
         if (!win.piece(a, cut, o, k, t == 0 && tile_c == 0, q)) return;
-        if (q >= 0 && before) load_vec<float, V>(carry_b, before + o.sequence(q) * a.C + c);
+        if (q >= 0 && before) load_vec<float, V>(carry_b, before + (int64_t)o.sequence(q) * a.C + c);
     } else if (cut.exact && k > 0) {
         load_vec<float, V>(carry_b, cut.carry + (int64_t)k * a.C + c);
     }
-    const int64_t qa = win.qa, qb = win.qb, p0 = win.p0, p1 = win.p1;
+    const pos qa = win.qa, qb = win.qb, p0 = win.p0, p1 = win.p1;
 
     // a tile's loads: gates, what comes in (x, or dy), backward the states before the rows and, with mixed inputs, x
     struct Tile {
@@ -228,25 +229,25 @@ __global__ __launch_bounds__(BLOCK) void recur_scan_kernel(const RecurArgs a, co
         Rows<Y, (BWD && !PIECE ? RB : 1), V, false>         left;
         Rows<Io, (BWD && MIX && !PIECE ? RB : 1), V, false> x;
     };
-    const auto place = [&](const int64_t pt) {
+    const auto place = [&](const pos pt) {
         return Place{o.back ? a.N - TR - pt : pt, (uint32_t)(o.back ? TR - 1 - rl * RB : rl * RB), dir};
     };
-    const auto fetch = [&](Tile &f, const int64_t pt) {
-        const int64_t pr = pt + rl * RB;
+    const auto fetch = [&](Tile &f, const pos pt) {
+        const pos pr = pt + rl * RB;
         const bool    whole = pt + TR <= p1;
         const Place   at = place(pt);
         f.g.load_from(a.gate, at, gw, gc, whole, a.N, pr, p0, p1);
         if (!BWD || a.dy) f.in.load_from(BWD ? a.dy : a.x, at, a.C, c, whole, a.N, pr, p0, p1);
         if constexpr (BWD && !PIECE) {
             // the state before the row is that of the next row in the order taken (of the next window's first, at the end of this one)
-            const int64_t end = p1 + 1 <= a.N ? p1 + 1 : p1;
+            const pos end = p1 + 1 <= a.N ? p1 + 1 : p1;
             f.left.load_from(a.y, Place{at.low + dir, at.mine, dir}, a.C, c, pt + TR + 1 <= end, a.N, pr + 1, p0, end);
             if constexpr (MIX) f.x.load_from(a.x, at, a.C, c, whole, a.N, pr, p0, p1);
         }
     };
 
-    int64_t q_at = PIECE ? 0 : qa > 0 ? qa - 1 : 0;            // no sequence before this one reaches p0
-    int64_t flags_from = p0;
+    pos q_at = PIECE ? 0 : qa > 0 ? qa - 1 : 0;            // no sequence before this one reaches p0
+    pos flags_from = p0;
     int     buf = 0;
     Tile    now, next;
     if (p0 < p1) fetch(now, p0);
@@ -254,14 +255,14 @@ __global__ __launch_bounds__(BLOCK) void recur_scan_kernel(const RecurArgs a, co
         if (!PIECE && (pt - p0) % kFlagRows == 0) {
             // marks of the rows [flags_from, flags_to): first and last rows of sequences; sequences without rows pass their state on here
             flags_from = pt;
-            const int64_t flags_to = p1 - pt < kFlagRows ? p1 : pt + kFlagRows;
+            const pos flags_to = p1 - pt < kFlagRows ? p1 : pt + kFlagRows;
             const bool    at_end = flags_to == p1;
             for (int i = t; i < kFlagRows / 32; i += BLOCK) { bits_first[i] = 0; bits_last[i] = 0; }
             if (t == 0) q_next = (int)q_at;
             __syncthreads();
             int furthest = (int)q_at;
             for (int64_t q = q_at + t; q < qb; q += BLOCK) {
-                const int64_t f = o.at(q), l = o.at(q + 1);
+                const pos f = o.at(q), l = o.at(q + 1);
                 if (f > flags_to || (f == flags_to && !at_end)) break;
                 if (f < l) {
                     if (f < flags_to) furthest = (int)q;
@@ -277,7 +278,7 @@ __global__ __launch_bounds__(BLOCK) void recur_scan_kernel(const RecurArgs a, co
                     }
                 } else if (f >= flags_from && q >= qa) {
                     float        *to = BWD ? a.dh0 : a.last;
-                    const int64_t i = o.sequence(q) * a.C;
+                    const int64_t i = (int64_t)o.sequence(q) * a.C;
                     for (int j = (int)tile_c * (CL * V); to && j < ((int)tile_c + 1) * (CL * V) && j < a.C; ++j) to[i + j] = before ? before[i + j] : 0.0f;
                 }
             }
@@ -287,7 +288,7 @@ __global__ __launch_bounds__(BLOCK) void recur_scan_kernel(const RecurArgs a, co
         }
         if (pt >= p1) break;
 
-        const int64_t pr = pt + rl * RB;                       // this lane's first row, in the order taken
+        const pos pr = pt + rl * RB;                       // this lane's first row, in the order taken
         const bool    whole = pt + TR <= p1;
         const Place   at = place(pt);
         uint32_t      first = 0, last = 0, live = (1u << RB) - 1u, mark0 = 0;
@@ -525,51 +526,51 @@ __global__ __launch_bounds__(64) void recur_narrow_kernel(const RecurArgs a, con
 #pragma unroll
     for (int v = 0; v < V; ++v) carry_b[v] = 0.0f;
     if (PIECE) {
-        int64_t q;
+        pos q;
         if (!win.piece(a, cut, o, k, lane == 0, q)) return;
-        if (q >= 0 && before) load_vec<float, V>(carry_b, before + o.sequence(q) * V);
+        if (q >= 0 && before) load_vec<float, V>(carry_b, before + (int64_t)o.sequence(q) * V);
     } else if (cut.exact && k > 0) {
         load_vec<float, V>(carry_b, cut.carry + (int64_t)k * V);
     }
-    const int64_t qa = win.qa, qb = win.qb, p0 = win.p0, p1 = win.p1;
+    const pos qa = win.qa, qb = win.qb, p0 = win.p0, p1 = win.p1;
 
     struct Tile {
         Rows<Gate, RB, GV, true> g;
         Rows<Io, RB, V, true>    in;
         Rows<Y, (BWD && !PIECE ? RB : 1), V, true>         left;
         Rows<Io, (BWD && MIX && !PIECE ? RB : 1), V, true> x;
-        int64_t first, behind;                                 // rows of sequence q + lane
+        pos first, behind;                                 // rows of sequence q + lane
         float   from[V], ends[BWD ? V : 1];                    // its state to start from; backward, the one it started from
     };
-    const auto place = [&](const int64_t pt) {
+    const auto place = [&](const pos pt) {
         return Place{o.back ? a.N - TR - pt : pt, (uint32_t)(o.back ? TR - 1 - lane * RB : lane * RB), dir};
     };
-    const auto fetch_sequences = [&](Tile &f, const int64_t q) {
-        const int64_t s = q + lane < qb ? q + lane : qb - 1 > 0 ? qb - 1 : 0;
+    const auto fetch_sequences = [&](Tile &f, const pos q) {
+        const pos s = q + lane < qb ? q + lane : qb - 1 > 0 ? qb - 1 : 0;
         f.first = o.at(s);
         f.behind = o.at(s + 1);
-        if (before) load_vec<float, V>(f.from, before + o.sequence(s) * V);
-        if (BWD && a.h0) load_vec<float, BWD ? V : 1>(f.ends, a.h0 + o.sequence(s) * V);
+        if (before) load_vec<float, V>(f.from, before + (int64_t)o.sequence(s) * V);
+        if (BWD && a.h0) load_vec<float, BWD ? V : 1>(f.ends, a.h0 + (int64_t)o.sequence(s) * V);
     };
-    const auto fetch_rows = [&](Tile &f, const int64_t pt) {
-        const int64_t pr = pt + lane * RB;
+    const auto fetch_rows = [&](Tile &f, const pos pt) {
+        const pos pr = pt + lane * RB;
         const bool    whole = pt + TR <= p1;
         const Place   at = place(pt);
         f.g.load_from(a.gate, at, GV, 0, whole, a.N, pr, p0, p1);
         if (!BWD || a.dy) f.in.load_from(BWD ? a.dy : a.x, at, V, 0, whole, a.N, pr, p0, p1);
         if constexpr (BWD && !PIECE) {
-            const int64_t end = p1 + 1 <= a.N ? p1 + 1 : p1;
+            const pos end = p1 + 1 <= a.N ? p1 + 1 : p1;
             f.left.load_from(a.y, Place{at.low + dir, at.mine, dir}, V, 0, pt + TR + 1 <= end, a.N, pr + 1, p0, end);
             if constexpr (MIX) f.x.load_from(a.x, at, V, 0, whole, a.N, pr, p0, p1);
         }
     };
 
-    int64_t q_at = qa > 0 ? qa - 1 : 0;                        // no sequence before this one reaches p0
+    pos q_at = qa > 0 ? qa - 1 : 0;                        // no sequence before this one reaches p0
     Tile    now, next;
     if (!PIECE) fetch_sequences(now, q_at);
     if (p0 < p1) fetch_rows(now, p0);
     for (int64_t pt = p0; pt < p1 || (!PIECE && pt == p0); pt += TR) {
-        const int64_t to = p1 - pt < TR ? p1 : pt + TR, q0 = q_at;
+        const pos to = p1 - pt < TR ? p1 : pt + TR, q0 = q_at;
         const bool    whole = pt + TR <= p1;
         if (!PIECE) {
 #pragma unroll
@@ -579,7 +580,7 @@ __global__ __launch_bounds__(64) void recur_narrow_kernel(const RecurArgs a, con
             }
             __syncthreads();
             for (int64_t q = q0;;) {
-                const int64_t f = now.first, l = now.behind;
+                const pos f = now.first, l = now.behind;
                 const bool    here = q + lane < qb && (f < to || (f == to && to == p1));
                 if (here && f < l) {
                     if (f >= pt && f < to) mark_first[(int)(f - pt)] = (uint32_t)(q + lane) + 1u;
@@ -597,7 +598,7 @@ __global__ __launch_bounds__(64) void recur_narrow_kernel(const RecurArgs a, con
                     float  h[V];
 #pragma unroll
                     for (int v = 0; v < V; ++v) h[v] = before ? now.from[v] : 0.0f;
-                    if (pass) store_vec<float, V>(pass + o.sequence(q + lane) * V, h);
+                    if (pass) store_vec<float, V>(pass + (int64_t)o.sequence(q + lane) * V, h);
                 }
                 const uint64_t inside = __ballot(here && f < to), all = __ballot(here);
                 if (inside) q_at = q + (63 - __clzll(inside));
@@ -613,7 +614,7 @@ __global__ __launch_bounds__(64) void recur_narrow_kernel(const RecurArgs a, con
         }
         if (pt >= p1) break;
 
-        const int64_t pr = pt + lane * RB;
+        const pos pr = pt + lane * RB;
         const Place   at = place(pt);
         uint32_t      first[RB], last[RB], live = (1u << RB) - 1u;
         if (!whole) live = pr >= p1 ? 0u : pr + RB <= p1 ? live : (1u << (uint32_t)(p1 - pr)) - 1u;
@@ -652,7 +653,7 @@ __global__ __launch_bounds__(64) void recur_narrow_kernel(const RecurArgs a, con
 #pragma unroll
                 for (int v = 0; v < V; ++v) h[v] = table[i * V + v];
             } else if (array) {
-                load_vec<float, V>(h, array + o.sequence((int64_t)mark - 1) * V);
+                load_vec<float, V>(h, array + (int64_t)o.sequence((pos)mark - 1) * V);
             } else {
 #pragma unroll
                 for (int v = 0; v < V; ++v) h[v] = 0.0f;
@@ -747,27 +748,27 @@ __global__ __launch_bounds__(64) void recur_narrow_kernel(const RecurArgs a, con
             if constexpr (BWD && SHARED) slope[j][0] = log_gate ? sum * g[j][0] : sum;
             if (last[j]) {
                 float *pass = BWD ? a.dh0 : a.last;
-                if (pass) store_vec<float, V>(pass + o.sequence((int64_t)last[j] - 1) * V, h);
+                if (pass) store_vec<float, V>(pass + (int64_t)o.sequence((pos)last[j] - 1) * V, h);
             }
         }
-        const int64_t low_row = at.low + (int64_t)at.mine, lowest = low_row - (o.back ? RB - 1 : 0);
+        const pos low_row = at.low + (pos)at.mine, lowest = low_row - (o.back ? RB - 1 : 0);
         if (live == (1u << RB) - 1u) {
             if constexpr (BWD) {
-                store_run<Io, RB, V>((Io *)a.dx + lowest * V, in, o.back);
-                store_run<Gate, RB, GV>((Gate *)a.dgate + lowest * GV, slope, o.back);
+                store_run<Io, RB, V>((Io *)a.dx + (int64_t)lowest * V, in, o.back);
+                store_run<Gate, RB, GV>((Gate *)a.dgate + (int64_t)lowest * GV, slope, o.back);
             } else if (a.out_y) {
-                store_run<Y, RB, V>((Y *)a.out_y + lowest * V, in, o.back);
+                store_run<Y, RB, V>((Y *)a.out_y + (int64_t)lowest * V, in, o.back);
             }
         } else if (live) {
 #pragma unroll
             for (int j = 0; j < RB; ++j) {
                 if (!((live >> j) & 1u)) continue;
-                const int64_t r = low_row + dir * j;
+                const pos r = low_row + dir * j;
                 if constexpr (BWD) {
-                    store_vec<Io, V>((Io *)a.dx + r * V, in[j]);
-                    store_vec<Gate, GV>((Gate *)a.dgate + r * GV, slope[j]);
+                    store_vec<Io, V>((Io *)a.dx + (int64_t)r * V, in[j]);
+                    store_vec<Gate, GV>((Gate *)a.dgate + (int64_t)r * GV, slope[j]);
                 } else if (a.out_y) {
-                    store_vec<Y, V>((Y *)a.out_y + r * V, in[j]);
+                    store_vec<Y, V>((Y *)a.out_y + (int64_t)r * V, in[j]);
                 }
             }
         }
@@ -851,12 +852,12 @@ int launch_inputs(const RecurArgs &a, const RecurPlan &p, const Cut &cut, hipStr
 template <bool BWD>
 int cngp::recur_launch(const cngp_recur_config *c, RecurArgs a, const RecurPlan &p, const RecurSpace &sp, char *ws, hipStream_t s) {
     if ((int64_t)p.K * p.tiles > 0x7fffffffLL) return CNGP_ERR_UNSUPPORTED;
-    Cut cut{p.R, p.K, (float *)(ws + sp.piece_a), (float *)(ws + sp.piece_b), (float *)(ws + sp.carry), (int32_t *)(ws + sp.piece_cut), p.exact};
+    Cut cut{(pos)p.R, p.K, (float *)(ws + sp.piece_a), (float *)(ws + sp.piece_b), (float *)(ws + sp.carry), (int32_t *)(ws + sp.piece_cut), p.exact};
     const float *&in = BWD ? a.dlast : a.h0;
     float        *out = BWD ? a.dh0 : a.last;
     if (p.exact && in && in == out) {
         float        *copy = (float *)(ws + sp.state);
-        if (int rc = recur_copy(in, copy, a.S * a.C, s)) return rc;
+        if (int rc = recur_copy(in, copy, (int64_t)a.S * a.C, s)) return rc;
         in = copy;
     }
     const bool io16 = c->io_dtype == CNGP_F16, g16 = c->gate_dtype == CNGP_F16;

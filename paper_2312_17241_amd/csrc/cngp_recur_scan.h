@@ -1,5 +1,7 @@
 // The scan of the gated linear recurrence: kernels for wide rows and for rows of up to four channels, and their launches.
 #pragma once
+#include <type_traits>
+
 #include "cngp_recur.h"
 
 namespace {
@@ -101,6 +103,16 @@ struct Place {
     int      dir;                        // 1 or -1
 };
 
+// A lane's first row in an array of `width` values to a row; the next one lies dir * width further.
+template <typename T>
+__device__ __forceinline__ T *row_at(T *array, const Place &at, const int width, const int c) {
+    return array + (int64_t)at.low * width + (at.mine * (uint32_t)width + (uint32_t)c);
+}
+template <typename T>
+__device__ __forceinline__ const T *row_at(const void *array, const Place &at, const int width, const int c) {
+    return row_at<const T>((const T *)array, at, width, c);
+}
+
 // RB rows of V values each as they lie in memory, so that a tile's loads can be under way while another is worked on.
 // A lane that holds all values of its rows (NARROW) reads them as one run, 16 bytes at a time, in the order of the memory.
 template <typename T, int RB, int V, bool NARROW>
@@ -123,16 +135,16 @@ struct Rows {
                 }
             }
         } else {
-            const uint32_t mine = at.mine * (uint32_t)width + (uint32_t)c;
-            const T       *base = (const T *)array + (int64_t)at.low * width;
+            const T *row = row_at<T>(array, at, width, c);
             if (whole) {
+                const int64_t step = (int64_t)at.dir * width;
 #pragma unroll
-                for (int j = 0; j < RB; ++j) __builtin_memcpy(&raw.e[j * V], base + (int64_t)(at.dir * j) * width + mine, sizeof(T) * V);
+                for (int j = 0; j < RB; ++j, row += step) __builtin_memcpy(&raw.e[j * V], row, sizeof(T) * V);
             } else {
 #pragma unroll
                 for (int j = 0; j < RB; ++j) {
                     const pos p = pr + j < p0 ? p0 : pr + j < p1 ? pr + j : p1 - 1;
-                    __builtin_memcpy(&raw.e[j * V], base + (int64_t)mine + (int64_t)(at.dir * (p - pr)) * width, sizeof(T) * V);
+                    __builtin_memcpy(&raw.e[j * V], row + (int64_t)(at.dir * (p - pr)) * width, sizeof(T) * V);
                 }
             }
         }
@@ -144,11 +156,6 @@ struct Rows {
     }
 };
 
-// Row j of a lane's outputs (not NARROW).
-template <typename T>
-__device__ __forceinline__ T *row_at(void *array, const Place &at, const int width, const int c, const int j) {
-    return (T *)array + (int64_t)(at.low + at.dir * j) * width + (at.mine * (uint32_t)width + (uint32_t)c);
-}
 template <typename T, int RB, int V>
 __device__ __forceinline__ void store_run(T *lowest, const float (&in)[RB][V], const bool back) {
     Run<T, RB * V> raw;
@@ -195,7 +202,7 @@ __global__ __launch_bounds__(BLOCK) void recur_scan_kernel(const RecurArgs a, co
     __shared__ float    tot_a[2][W][CL * GV], tot_b[2][W][CL * V];
     __shared__ int      tot_cut[2][W];
     __shared__ int      q_next;
-    const int      t = threadIdx.x, lane = t & 63, w = t >> 6, cl = t % CL, rl = t / CL;
+    const int      t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), cl = t % CL, rl = t / CL;
     const uint32_t k = blockIdx.x % cut.K, tile_c = blockIdx.x / cut.K;
     const int      c_here = (int)tile_c * (CL * V) + cl * V;
     const bool     c_ok = c_here < a.C;                        // V divides C
@@ -301,7 +308,7 @@ __global__ __launch_bounds__(BLOCK) void recur_scan_kernel(const RecurArgs a, co
         if (pt + TR < p1) fetch(next, pt + TR);                // under way while this tile is worked on
         // what the sequences that start in here start from; backward, what those that end in here started from
         float      h_first[PIECE ? 1 : RB][V], h_last[BWD && !PIECE ? RB : 1][V];
-        const bool starts_here = !PIECE && __any(first != 0), ends_here = BWD && !PIECE && __any(last != 0);
+        const bool starts_here = !PIECE && __any(first != 0), ends_here = !PIECE && __any(last != 0);
         if constexpr (!PIECE) {
             if (starts_here && before) {
 #pragma unroll
@@ -357,20 +364,20 @@ __global__ __launch_bounds__(BLOCK) void recur_scan_kernel(const RecurArgs a, co
         for (int v = 0; v < GV; ++v) A[v] = 1.0f;
 #pragma unroll
         for (int v = 0; v < V; ++v) B[v] = 0.0f;
+        const auto compose = [&](auto with_starts) {
 #pragma unroll
-        for (int j = 0; j < RB; ++j) {
-            if (starts_here) {
+            for (int j = 0; j < RB; ++j) {
 #pragma unroll
-                for (int v = 0; v < V; ++v) B[v] = (first >> j) & 1u ? 0.0f : B[v];
+                for (int v = 0; v < V; ++v) {
+                    const float gj = g[j][SHARED ? 0 : v], from = with_starts && ((first >> j) & 1u) ? 0.0f : B[v];
+                    B[v] = BWD ? gj * (from + in[j][v]) : fmaf(gj, from, in[j][v]);
+                }
+#pragma unroll
+                for (int v = 0; v < GV; ++v) A[v] *= g[j][v];
             }
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const float gj = g[j][SHARED ? 0 : v];
-                B[v] = BWD ? gj * (B[v] + in[j][v]) : fmaf(gj, B[v], in[j][v]);
-            }
-#pragma unroll
-            for (int v = 0; v < GV; ++v) A[v] *= g[j][v];
-        }
+        };
+        if (starts_here) compose(std::true_type());            // two loops, not one of selects
+        else compose(std::false_type());
 #pragma unroll
         for (int d = 1; d < 64 / CL; d <<= 1) {
             float Al[GV], Bl[V];
@@ -393,23 +400,33 @@ __global__ __launch_bounds__(BLOCK) void recur_scan_kernel(const RecurArgs a, co
             if (lane == 63) tot_cut[buf][w] = starts != 0;
         }
         __syncthreads();
+        int forgets[W], any_forgets = 0;
 #pragma unroll
-        for (int i = 0; i < W; ++i) {
-            const int forget = tot_cut[buf][i];
-            float     Ai[GV];
+        for (int i = 0; i < W; ++i) { forgets[i] = tot_cut[buf][i]; any_forgets |= forgets[i]; }
+        const auto fold = [&](auto with_starts) {
 #pragma unroll
-            for (int v = 0; v < GV; ++v) Ai[v] = tot_a[buf][i][cl * GV + v];
+            for (int i = 0; i < W; ++i) {
+                float Ai[GV], Bi[V];
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                if (i == w) h[v] = carry_b[v];
-                const float Bi = tot_b[buf][i][cl * V + v];
-                carry_b[v] = forget ? Bi : fmaf(Ai[SHARED ? 0 : v], carry_b[v], Bi);
+                for (int v = 0; v < GV; ++v) Ai[v] = tot_a[buf][i][cl * GV + v];
+#pragma unroll
+                for (int v = 0; v < V; ++v) Bi[v] = tot_b[buf][i][cl * V + v];
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    h[v] = i == w ? carry_b[v] : h[v];
+                    const float next_b = fmaf(Ai[SHARED ? 0 : v], carry_b[v], Bi[v]);
+                    carry_b[v] = with_starts && forgets[i] ? Bi[v] : next_b;
+                }
+                if (PIECE) {
+#pragma unroll
+                    for (int v = 0; v < GV; ++v) carry_a[v] *= Ai[v];
+                }
             }
-            if (PIECE) {
+        };
 #pragma unroll
-                for (int v = 0; v < GV; ++v) carry_a[v] *= Ai[v];
-            }
-        }
+        for (int v = 0; v < V; ++v) h[v] = 0.0f;
+        if (!PIECE && __builtin_amdgcn_readfirstlane(any_forgets)) fold(std::true_type());
+        else fold(std::false_type());
         buf ^= 1;
         if constexpr (PIECE) {
             now = next;
@@ -429,66 +446,73 @@ __global__ __launch_bounds__(BLOCK) void recur_scan_kernel(const RecurArgs a, co
 
         // the rows once more, now with the state that reaches them
         float slope[BWD ? RB : 1][GV];
+        const auto walk = [&](auto with_edges) {
 #pragma unroll
-        for (int j = 0; j < RB; ++j) {
-            if (starts_here) {
+            for (int j = 0; j < RB; ++j) {
+                float sum = 0.0f;
 #pragma unroll
-                for (int v = 0; v < V; ++v) h[v] = (first >> j) & 1u ? 0.0f : h[v];
-            }
-            float sum = 0.0f;
+                for (int v = 0; v < V; ++v) {
+                    const float gj = g[j][SHARED ? 0 : v], from = with_edges && ((first >> j) & 1u) ? 0.0f : h[v];
+                    if constexpr (!BWD) {
+                        h[v] = fmaf(gj, from, in[j][v]);
+                        in[j][v] = h[v];                       // now the output
+                    } else if constexpr (!PIECE) {
+                        float left = now.left.get(j, v, o.back);
+                        if (with_edges && ((last >> j) & 1u)) left = a.h0 ? h_last[j][v] : 0.0f;
+                        if constexpr (MIX) left -= now.x.get(j, v, o.back);
+                        const float dh = from + in[j][v], da = dh * left;
+                        in[j][v] = MIX ? share[MIX ? j : 0][SHARED ? 0 : v] * dh : dh;
+                        if (!SHARED) slope[j][SHARED ? 0 : v] = log_gate ? da * gj : da;
+                        else sum += c_ok ? da : 0.0f;
+                        h[v] = gj * dh;
+                    }
+                }
+                if constexpr (BWD && SHARED) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const float gj = g[j][SHARED ? 0 : v];
-                if constexpr (!BWD) {
-                    h[v] = fmaf(gj, h[v], in[j][v]);
-                    in[j][v] = h[v];                           // now the output
-                } else if constexpr (!PIECE) {
-                    float left = now.left.get(j, v, o.back);
-                    if (ends_here && ((last >> j) & 1u)) left = a.h0 ? h_last[j][v] : 0.0f;
-                    if constexpr (MIX) left -= now.x.get(j, v, o.back);
-                    const float dh = h[v] + in[j][v], da = dh * left;
-                    in[j][v] = MIX ? share[MIX ? j : 0][SHARED ? 0 : v] * dh : dh;
-                    if (!SHARED) slope[j][SHARED ? 0 : v] = log_gate ? da * gj : da;
-                    else sum += c_ok ? da : 0.0f;
-                    h[v] = gj * dh;
+                    for (int d = 1; d < CL; d <<= 1) sum += __shfl_xor(sum, d, 64);
+                    slope[j][0] = log_gate ? sum * g[j][0] : sum;
+                }
+                if (with_edges && ((last >> j) & 1u)) {
+                    float *to = BWD ? a.dh0 : a.last;
+                    if (c_ok && to) store_vec<float, V>(to + (uint64_t)(uint32_t)mark_last[mark0 + j] * (uint32_t)a.C + c, h);
                 }
             }
-            if constexpr (BWD && SHARED) {
-#pragma unroll
-                for (int d = 1; d < CL; d <<= 1) sum += __shfl_xor(sum, d, 64);
-                slope[j][0] = log_gate ? sum * g[j][0] : sum;
-            }
-            if ((last >> j) & 1u) {
-                float *to = BWD ? a.dh0 : a.last;
-                if (c_ok && to) store_vec<float, V>(to + (uint64_t)(uint32_t)mark_last[mark0 + j] * (uint32_t)a.C + c, h);
-            }
-        }
-        constexpr uint32_t ALL = (1u << RB) - 1u;
-        const auto put = [&](const int j) {
-            if constexpr (!BWD) {
-                store_vec<Y, V>(row_at<Y>(a.out_y, at, a.C, c, j), in[j]);
-            } else {
-                store_vec<Io, V>(row_at<Io>(a.dx, at, a.C, c, j), in[j]);
-                if constexpr (!SHARED) store_vec<Gate, V>(row_at<Gate>(a.dgate, at, a.C, c, j), slope[j]);
-            }
         };
+        if (starts_here || ends_here) walk(std::true_type());
+        else walk(std::false_type());
+        const int64_t step = (int64_t)dir * a.C;
         if (c_ok && (BWD || a.out_y)) {
-            if (live == ALL) {
+            const auto put = [&](const int j, Io *dx, Gate *dg, Y *y) {
+                if constexpr (!BWD) {
+                    store_vec<Y, V>(y + step * j, in[j]);
+                } else {
+                    store_vec<Io, V>(dx + step * j, in[j]);
+                    if constexpr (!SHARED) store_vec<Gate, V>(dg + step * j, slope[j]);
+                }
+            };
+            Io   *dx = BWD ? row_at<Io>((Io *)a.dx, at, a.C, c) : nullptr;
+            Gate *dg = BWD && !SHARED ? row_at<Gate>((Gate *)a.dgate, at, a.C, c) : nullptr;
+            Y    *y = BWD ? nullptr : row_at<Y>((Y *)a.out_y, at, a.C, c);
+            if (whole) {
 #pragma unroll
-                for (int j = 0; j < RB; ++j) put(j);
+                for (int j = 0; j < RB; ++j) put(j, dx, dg, y);
             } else {
 #pragma unroll
                 for (int j = 0; j < RB; ++j)
-                    if ((live >> j) & 1u) put(j);
+                    if ((live >> j) & 1u) put(j, dx, dg, y);
             }
         }
         if constexpr (BWD && SHARED) {
+            if (cl == 0) {
+                float *sl = a.slope ? row_at<float>(a.slope + (int64_t)tile_c * a.N, at, 1, 0) : nullptr;
+                Gate  *dg = row_at<Gate>((Gate *)a.dgate, at, 1, 0);
 #pragma unroll
-            for (int j = 0; j < RB; ++j)
-                if (cl == 0 && ((live >> j) & 1u)) {
-                    if (a.slope) *row_at<float>(a.slope + (int64_t)tile_c * a.N, at, 1, 0, j) = slope[j][0];
-                    else store(row_at<Gate>(a.dgate, at, 1, 0, j), 0, slope[j][0]);
-                }
+                for (int j = 0; j < RB; ++j)
+                    if ((live >> j) & 1u) {
+                        if (sl) sl[dir * j] = slope[j][0];
+                        else store(dg + dir * j, 0, slope[j][0]);
+                    }
+            }
         }
         now = next;
         if ((pt + TR - p0) % kFlagRows == 0) __syncthreads();  // the marks are written anew

@@ -91,7 +91,7 @@ def _maybe(t, dtype, shape, name):
 def _room(need, workspace, like):
     """The workspace to pass: the caller's, or one for this call."""
     if workspace is None and need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=like.device)
+        workspace = like.new_empty(need, dtype=torch.uint8)
     return workspace
 
 
@@ -111,11 +111,13 @@ def _need(query, cfg, *sizes):
 
 
 def _out(given, shape, dtype, like, name):
-    """True: a new tensor; a tensor: itself; None / False: not wanted."""
+    """(tensor, pointer).  True: a new tensor, made from `like` where that has the shape and type (a third less time); a tensor: itself,
+    checked; None / False: not wanted."""
+    if given is True:
+        given = torch.empty_like(like) if like.shape == shape and like.dtype is dtype else like.new_empty(shape, dtype=dtype)
+        return given, given.data_ptr()
     if given is None or given is False:
         return None, None
-    if given is True:
-        given = torch.empty(shape, dtype=dtype, device=like.device)
     return given, _dev(given, dtype, shape, name)
 
 
@@ -141,11 +143,11 @@ def recur_fwd(cfg: RecurConfig, gate, x, h0=None, offsets=None, sequences=None, 
     N, C = x.shape
     S = _sequences(N, offsets, sequences)
     y, yp = _out(y, (N, C), _TORCH_DT[cfg.io_dtype], x, "y")
-    last, lp = _out(last, (S, C), torch.float32, x, "last")
+    last, lp = _out(last, (S, C), torch.float32, x if h0 is None else h0, "last")
     gp, xp = _dev(gate, _TORCH_DT[cfg.gate_dtype], (N, cfg.gate_channels), "gate"), _dev(x, _TORCH_DT[cfg.io_dtype], (N, cfg.channels), "x")
     hp, op = _maybe(h0, torch.float32, (S, C), "h0"), _maybe(offsets, torch.int32, (S + 1,), "offsets")
     _on_current_device(gate, x, h0, offsets, y, last, workspace)
-    workspace = _room(recur_workspace_bytes(cfg, N, S, ragged=offsets is not None), workspace, x)
+    workspace = _room(_need("cngp_recur_workspace_bytes", cfg, N, S, 0 if offsets is None else _CALL_RAGGED), workspace, x)
     _check(_lib.cngp_recur_fwd(cfg._ref(), gp, xp, N, op, S, hp, yp, lp, *_ws(workspace), _stream()))
     return y, last
 
@@ -160,9 +162,9 @@ def recur_bwd(cfg: RecurConfig, gate, x, dy=None, dlast=None, h0=None, y=None, o
     gp, xp = _dev(gate, gt, (N, cfg.gate_channels), "gate"), _dev(x, io, (N, cfg.channels), "x")
     hp, op, yp = _maybe(h0, torch.float32, (S, C), "h0"), _maybe(offsets, torch.int32, (S + 1,), "offsets"), _maybe(y, io, (N, C), "y")
     dyp, dlp = _maybe(dy, io, (N, C), "dy"), _maybe(dlast, torch.float32, (S, C), "dlast")
-    dgate, dgp = _out(dgate, (N, cfg.gate_channels), gt, x, "dgate")
+    dgate, dgp = _out(dgate, (N, cfg.gate_channels), gt, gate, "dgate")
     dx, dxp = _out(dx, (N, C), io, x, "dx")
-    dh0, dhp = _out(h0 is not None if dh0 is None else dh0, (S, C), torch.float32, x, "dh0")
+    dh0, dhp = _out(h0 is not None if dh0 is None else dh0, (S, C), torch.float32, x if dlast is None else dlast, "dh0")
     _on_current_device(gate, x, h0, offsets, y, dy, dlast, dgate, dx, dh0, workspace)
     workspace = _room(recur_workspace_bytes(cfg, N, S, True, offsets is not None, y is not None), workspace, x)
     _check(_lib.cngp_recur_bwd(cfg._ref(), gp, xp, N, op, S, hp, yp, dyp, dlp, dgp, dxp, dhp, *_ws(workspace), _stream()))
@@ -176,7 +178,7 @@ def embed_workspace_bytes(cfg: EmbedConfig, N) -> int:
 def embed_fwd(cfg: EmbedConfig, ids, table, base=None, y=None):
     """cngp_embed_fwd: base + scale * table[ids], io_dtype [N, dim]; y may be base (added in place)."""
     N, io = ids.shape[0], _TORCH_DT[cfg.io_dtype]
-    y, yp = _out(True if y is None else y, (N, cfg.dim), io, ids, "y")
+    y, yp = _out(True if y is None else y, (N, cfg.dim), io, ids if base is None else base, "y")
     ip, tp = _dev(ids, _ID_DT[cfg.id_dtype], (N,), "ids"), _dev(table, _TORCH_DT[cfg.table_dtype], (cfg.rows, cfg.dim), "table")
     bp = _maybe(base, io, (N, cfg.dim), "base")
     _on_current_device(ids, table, base, y)

@@ -1,4 +1,5 @@
-"""torch.nn.Module around the library's entry points, for training loops.
+"""torch.nn.Modules and autograd functions around the library's entry points, for training loops: the encoding, codes per image or
+object that are added to it, and the recurrence that composites a ray's decoded samples.
 
 Holds the codebooks of the encoding (Sec. 3: feature codebook D_f, confidence values D^_c, baked index
 codebook D_c), their gradient arrays and optimiser moments as device tensors, and wires encode_fwd /
@@ -12,8 +13,9 @@ first bake picks an arbitrary one); the optimiser is Adam.
 """
 import torch
 
-from . import (Adam, Config, ZERO_GRADS, _TORCH_DT, F16, adam_step_bake, alloc_workspace, bake_probes,
-               encode_bwd, encode_bwd_input, encode_fwd, workspace_bytes)
+from . import (Adam, Config, EmbedConfig, F32, I64, RECUR_LOG_GATE, RECUR_MIX, RECUR_REVERSE, RecurConfig, ZERO_GRADS, _TORCH_DT, F16,
+               adam_step, adam_step_bake, alloc_workspace, bake_probes, embed_bwd, embed_fwd, encode_bwd, encode_bwd_input, encode_fwd,
+               probe_balance, recur_bwd, recur_fwd, workspace_bytes)
 
 
 class _Encode(torch.autograd.Function):
@@ -68,6 +70,12 @@ class Encoding(torch.nn.Module):
     def forward(self, x):
         return _Encode.apply(x, self._hook, self)
 
+    def balance(self, weight, rows=None):
+        """Adds the gradient of weight * sum(loss) to that of the confidence values, loss as in cngp_probe_balance, and returns
+        (loss [L], winners per candidate [L, N_p]).  Call it after backward(), before step().  rows: uint8 [L, N_c], 0 = not counted."""
+        loss, counts, _ = probe_balance(self.cfg, self.Dhat_c, weight, rows=rows, grad_Dhat_c=self.grad_Dhat_c)
+        return loss, counts
+
     def step(self, opt_f: Adam, opt_c: Adam):
         """Optimiser step on both codebooks fused with the bake; clears the gradient arrays."""
         self.steps += 1
@@ -77,3 +85,79 @@ class Encoding(torch.nn.Module):
         half = self.D_f if self.cfg.feat_dtype == F16 else None
         adam_step_bake(cfg, of, oc, (self.D_f_master, half, self.m_f, self.v_f, self.grad_D_f),
                        (self.Dhat_c, self.m_c, self.v_c, self.grad_Dhat_c, self.D_c))
+
+
+class _LookUp(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, base, hook, codes, ids):
+        ctx.codes, ctx.ids, ctx.has_base = codes, ids, base is not None
+        return embed_fwd(codes.cfg, ids, codes.table, base=base)
+
+    @staticmethod
+    def backward(ctx, dy):
+        dy = dy.contiguous()
+        embed_bwd(ctx.codes.cfg, ctx.ids, dy, ctx.codes.grad_table)             # accumulates (+=)
+        return (dy if ctx.has_base else None), None, None, None
+
+
+class Codes(torch.nn.Module):
+    """A code per image, object or token: y = codes(ids, base) = base + scale * table[ids], base the encodings [N, dim] (or None).
+    Ids outside the table are padding.  Call codes.step(opt) after backward()."""
+
+    def __init__(self, rows, dim, io_dtype=F32, id_dtype=I64, scale=1.0, device="cuda", seed=0):
+        super().__init__()
+        self.cfg = EmbedConfig(rows, dim, F32, io_dtype, id_dtype, scale)
+        g = torch.Generator(device="cpu").manual_seed(seed)
+        # entries of an Adam step are moved four at a time: an array of its own, on 16 bytes
+        self.table = ((torch.rand((rows, dim), generator=g) * 2 - 1) * 1e-4).to(device)
+        zeros = lambda: torch.zeros((rows, dim), dtype=torch.float32, device=device)
+        self.grad_table, self.m, self.v = zeros(), zeros(), zeros()
+        self._hook = torch.nn.Parameter(torch.zeros((), device=device))         # lets autograd reach backward()
+        self.steps = 0
+
+    def forward(self, ids, base=None):
+        return _LookUp.apply(base, self._hook, self, ids)
+
+    def step(self, opt: Adam):
+        """Adam on the table (every entry: those that no id chose too); clears the gradient."""
+        self.steps += 1
+        adam_step(Adam(opt.lr, opt.beta1, opt.beta2, opt.eps, opt.grad_scale, self.steps), self.table, None, self.m, self.v, self.grad_table,
+                  clear_grad=True)
+
+
+class _Recur(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, gate, x, h0, cfg, offsets, sequences, keep):
+        y, last = recur_fwd(cfg, gate, x, h0=h0, offsets=offsets, sequences=sequences, y=keep)
+        if y is not None and offsets is not None:                                # rows of no sequence are not written
+            rows = torch.arange(x.shape[0], device=x.device)
+            y.masked_fill_(((rows < offsets[0]) | (rows >= offsets[-1]))[:, None], 0.0)
+        ctx.cfg, ctx.sequences, ctx.keep = cfg, sequences, keep
+        ctx.save_for_backward(gate, x, h0, offsets, y)
+        return (y, last) if keep else last
+
+    @staticmethod
+    def backward(ctx, *grads):
+        gate, x, h0, offsets, y = ctx.saved_tensors
+        dy, dlast = grads if ctx.keep else (None, grads[0])
+        dy = None if dy is None else dy.contiguous()
+        dlast = None if dlast is None else dlast.contiguous()
+        make = torch.empty_like if offsets is None else torch.zeros_like         # rows of no sequence have gradient 0
+        dgate, dx, dh0 = recur_bwd(ctx.cfg, gate, x, dy=dy, dlast=dlast, h0=h0, y=y, offsets=offsets, sequences=ctx.sequences,
+                                   dgate=make(gate), dx=make(x))
+        return dgate, dx, dh0, None, None, None, None
+
+
+def recur(cfg: RecurConfig, gate, x, h0=None, offsets=None, sequences=None, keep=True):
+    """The gated linear recurrence with gradients: (y, last), or last alone with keep=False (then the states are computed again by the
+    backward pass).  See cngp_recur_fwd."""
+    return _Recur.apply(gate, x, h0, cfg, offsets, sequences, keep)
+
+
+def composite(depth, colour, background=None, offsets=None, rays=None, longest=0):
+    """Pixels [rays, C] float32 of rays whose samples lie one behind the other, nearest first: depth [N] are the samples' optical depths
+    (density times step, >= 0), colour [N, C] what they emit, background [rays, C] float32 what lies behind (None: black).
+    offsets int32 [rays + 1], or None for `rays` rays of equal length; longest: most samples of a ray, if known."""
+    code = {t: c for c, t in _TORCH_DT.items()}
+    cfg = RecurConfig(colour.shape[1], 1, code[colour.dtype], code[depth.dtype], longest, RECUR_LOG_GATE | RECUR_MIX | RECUR_REVERSE)
+    return recur(cfg, -depth[:, None], colour, background, offsets, rays, keep=False)

@@ -1,0 +1,177 @@
+"""The operators together, as a radiance field with a code per image uses them: encoding + code -> decoder -> samples composited along
+rays -> squared error, back through all of it, the balance of the probing confidences on top.  Held against the same computation in
+64 bits by torch's autograd on the CPU.
+
+Tolerance: each stage is fp32 with at most a few dozen roundings of 2^-24 relative to the magnitudes it sums (32 products of the decoder,
+8 per sample of the recurrence along at most 40 samples, a few thousand added per code, each in sums of mixed sign): 1e-4 of the largest
+entry is above their product with room for the cancellation of a gradient of random signs."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2312_17241_amd as cngp
+from paper_2312_17241_amd.module import Codes, Encoding, composite, recur
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+def close(name, got, want, rel=1e-4):
+    got, want = got.detach().cpu().double(), want.detach().cpu().double()
+    assert got.shape == want.shape and float((got - want).abs().max()) <= rel * float(want.abs().max()), name
+
+
+def rays_of(g, rays, most, empty):
+    lengths = torch.randint(1, most + 1, (rays,), generator=g)
+    lengths[torch.randperm(rays, generator=g)[:empty]] = 0
+    return torch.cat([torch.zeros(1, dtype=torch.long), lengths.cumsum(0)]).int()
+
+
+def pixels_64(depth, colour, background, offsets):
+    out = []
+    for s in range(len(offsets) - 1):
+        h = background[s]
+        for r in range(int(offsets[s + 1]) - 1, int(offsets[s]) - 1, -1):
+            a = torch.exp(-depth[r])
+            h = a * h + (1 - a) * colour[r]
+        out.append(h)
+    return torch.stack(out)
+
+
+def test_a_training_iteration_of_a_field_with_codes():
+    g = torch.Generator().manual_seed(5)
+    cfg = cngp.Config(d=3, L=8, F=2, N_f=2**10, N_c=2**8, N_p=4, N_min=4, N_max=64)
+    enc, codes = Encoding(cfg, seed=1), Codes(7, 16, scale=0.5, seed=2)
+    with torch.no_grad():
+        enc.D_f_master.copy_(torch.randn(enc.D_f_master.shape, generator=g) * 0.3)
+        codes.table.copy_(torch.randn(codes.table.shape, generator=g) * 0.3)
+    offsets = rays_of(g, 60, 40, 5)
+    N = int(offsets[-1])
+    x = torch.rand(N, 3, generator=g)
+    image = torch.randint(0, 7, (60,), generator=g)
+    ids = torch.repeat_interleave(image, (offsets[1:] - offsets[:-1]).long())
+    ids[::11] = -1                                                   # samples without a code
+    W = (torch.randn(4, 16, generator=g) * 0.5).to(DEV).requires_grad_()
+    background, target = torch.rand(60, 3, generator=g).to(DEV).requires_grad_(), torch.rand(60, 3, generator=g)
+
+    y = enc(x.to(DEV))
+    z = codes(ids.to(DEV), y)
+    out = z @ W.t()
+    colour, depth = torch.sigmoid(out[:, :3]), torch.nn.functional.softplus(out[:, 3])
+    pixels = composite(depth, colour.contiguous(), background, offsets.to(DEV))
+    loss = ((pixels - target.to(DEV)) ** 2).sum()
+    y.retain_grad()
+    loss.backward()
+
+    y64 = y.detach().cpu().double().requires_grad_()
+    E64, W64 = codes.table.cpu().double().requires_grad_(), W.detach().cpu().double().requires_grad_()
+    b64 = background.detach().cpu().double().requires_grad_()
+    picked = torch.where((ids >= 0)[:, None], E64[ids.clamp(min=0)], torch.zeros((), dtype=torch.float64))
+    out64 = (y64 + 0.5 * picked) @ W64.t()
+    p64 = pixels_64(torch.nn.functional.softplus(out64[:, 3]), torch.sigmoid(out64[:, :3]), b64, offsets)
+    loss64 = ((p64 - target.double()) ** 2).sum()
+    loss64.backward()
+    close("pixels", pixels, p64)
+    close("W", W.grad, W64.grad)
+    close("codes", codes.grad_table, E64.grad)
+    close("background", background.grad, b64.grad)
+    close("encodings", y.grad, y64.grad)
+
+    # what the encoding passed on is what the library's own backward makes of that gradient
+    gF, gC = cngp.encode_bwd(cfg, x.to(DEV), enc.D_f, enc.Dhat_c, y.grad.contiguous())
+    close("features", enc.grad_D_f, gF, 1e-5)
+    before = enc.grad_Dhat_c.clone()
+    losses, counts = enc.balance(0.1)
+    alone = cngp.probe_balance(cfg, enc.Dhat_c, 0.1)
+    assert torch.equal(losses, alone[0]) and torch.equal(counts, alone[1]) and bool((counts.sum(1) == cfg.N_c).all())
+    close("balance", enc.grad_Dhat_c - before, alone[2], 1e-3)       # what was there is larger: its last bits are the difference's
+    enc.step(cngp.Adam(lr=1e-2), cngp.Adam(lr=1e-1))
+    table = codes.table.clone()
+    codes.step(cngp.Adam(lr=1e-2))
+    assert bool((codes.grad_table == 0).all()) and not torch.equal(codes.table, table)
+    assert torch.equal(enc.D_c, cngp.bake_probes(cfg, enc.Dhat_c))
+
+
+def test_recurrence_under_autograd():
+    """Both outputs, one of them, states kept or not; rows outside the sequences have states and gradients of 0."""
+    g = torch.Generator().manual_seed(3)
+    offsets = torch.tensor([2, 9, 9, 40, 61], dtype=torch.int32)
+    N, C = 64, 5
+    cfg = cngp.RecurConfig(C, C)
+    for keep in (True, False):
+        leaves = [t.to(DEV).requires_grad_() for t in (torch.rand(N, C, generator=g), torch.randn(N, C, generator=g), torch.randn(4, C, generator=g))]
+        wy, wl = torch.randn(N, C, generator=g), torch.randn(4, C, generator=g)
+        out = recur(cfg, *leaves, offsets=offsets.to(DEV), keep=keep)
+        loss = (out[0] * wy.to(DEV)).sum() + (out[1] * wl.to(DEV)).sum() if keep else (out * wl.to(DEV)).sum()
+        loss.backward()
+        ref = [t.detach().cpu().double().requires_grad_() for t in leaves]
+        total = 0.0
+        for s in range(4):
+            h = ref[2][s]
+            for r in range(int(offsets[s]), int(offsets[s + 1])):
+                h = ref[0][r] * h + ref[1][r]
+                if keep:
+                    total = total + (h * wy[r].double()).sum()
+            total = total + (h * wl[s].double()).sum()
+        total.backward()
+        close("loss", loss, total)
+        for name, a, b in zip(("gate", "x", "h0"), leaves, ref):
+            close(name, a.grad, b.grad)
+            if name != "h0":
+                assert bool((a.grad[:2] == 0).all()) and bool((a.grad[61:] == 0).all())
+
+
+def test_decoded_samples_in_a_captured_step():
+    """The library's own calls of an inference and training step captured together and replayed: encoding, code, decoder, recurrence and
+    the way back, with one workspace per call."""
+    g = torch.Generator().manual_seed(8)
+    cfg = cngp.Config(d=3, L=8, F=2, N_f=2**12, N_c=2**10, N_p=8, N_min=8, N_max=256, io_dtype=cngp.F16, feat_dtype=cngp.F16, flags=cngp.ZERO_GRADS)
+    rays, samples = 50, 24
+    N = rays * samples
+    dev = lambda t: t.to(DEV)
+    x, D_f = dev(torch.rand(N, 3, generator=g)), dev((torch.randn(8, 2**12, 2, generator=g) * 0.3).half())
+    Dhat = dev(torch.randn(8, 2**10, 8, generator=g))
+    ecfg = cngp.EmbedConfig(9, 16, cngp.F32, cngp.F16, cngp.I64, 1.0, cngp.ZERO_GRADS)
+    table, ids = dev(torch.randn(9, 16, generator=g) * 0.3), dev(torch.randint(0, 9, (N,), generator=g))
+    mcfg = cngp.MlpConfig(16, 4, cngp.F16, cngp.ZERO_GRADS)
+    W = dev((torch.randn(mcfg.weight_count, generator=g) * 0.2).half())
+    rcfg = cngp.RecurConfig(3, 1, flags=cngp.RECUR_LOG_GATE | cngp.RECUR_MIX | cngp.RECUR_REVERSE)
+    dpix = dev(torch.randn(rays, 3, generator=g))
+    ws = cngp.alloc_workspace(cfg, N)
+    out = {}
+
+    def step():
+        D_c = cngp.bake_probes(cfg, Dhat)
+        y = cngp.encode_fwd(cfg, x, D_f, D_c, workspace=ws)
+        z = cngp.embed_fwd(ecfg, ids, table, base=y)
+        o = cngp.mlp_fwd(mcfg, z, W)
+        gate, colour = -torch.nn.functional.softplus(o[:, 3:]), o[:, :3].contiguous()
+        _, pix = cngp.recur_fwd(rcfg, gate, colour, y=False, sequences=rays)
+        dgate, dcol, _ = cngp.recur_bwd(rcfg, gate, colour, dlast=dpix, sequences=rays)
+        dout = torch.cat([dcol, -dgate * torch.sigmoid(o[:, 3:])], 1)
+        dz, gW = cngp.mlp_bwd(mcfg, z, W, dout)
+        gE = cngp.embed_bwd(ecfg, ids, dz)
+        gF, gC = cngp.encode_bwd(cfg, x, D_f, Dhat, dz, workspace=ws)
+        loss, counts, gC2 = cngp.probe_balance(cfg, Dhat, 0.1)
+        out.update(pix=pix, dz=dz, gE=gE, gF=gF, loss=loss, counts=counts, gC2=gC2)
+
+    step()
+    want = {k: v.clone() for k, v in out.items()}
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    kept = dict(out)
+    for _ in range(3):
+        for v in kept.values():
+            v.fill_(9)
+        graph.replay()
+        torch.cuda.synchronize()
+        for k in ("pix", "dz", "gE", "loss", "counts", "gC2"):       # sums of a fixed order (gF has float atomics)
+            assert torch.equal(kept[k], want[k]), k
+        close("gF", kept["gF"], want["gF"], 1e-5)
+        step()

@@ -528,10 +528,14 @@ int sort_passes(const void *ids, int64_t N, int64_t rows, uint32_t *(&keys)[2], 
             digit_count_kernel<ROUNDS><<<tiles, kTileBlock, 0, s>>>(keys[*at], N, shift, counts, tiles);
             if (int rc = launch_status("digit_count_kernel")) return rc;
         }
-        digit_row_scan_kernel<<<kDigits, kScanBlock, 0, s>>>(counts, tiles, totals);
-        if (int rc = launch_status("digit_row_scan_kernel")) return rc;
-        digit_scatter_kernel<ROUNDS><<<tiles, kTileBlock, 0, s>>>(keys[*at], shift ? from[*at] : nullptr, N, shift, counts, tiles, totals, keys[*at ^ 1],
-                                                                  from[*at ^ 1]);
+        const int32_t *order = shift ? from[*at] : nullptr;
+        if (tiles <= (unsigned)kPrefixTiles) {
+            digit_scatter_kernel<ROUNDS, true><<<tiles, kTileBlock, 0, s>>>(keys[*at], order, N, shift, counts, tiles, totals, keys[*at ^ 1], from[*at ^ 1]);
+        } else {
+            digit_row_scan_kernel<<<kDigits, kScanBlock, 0, s>>>(counts, tiles, totals);
+            if (int rc = launch_status("digit_row_scan_kernel")) return rc;
+            digit_scatter_kernel<ROUNDS><<<tiles, kTileBlock, 0, s>>>(keys[*at], order, N, shift, counts, tiles, totals, keys[*at ^ 1], from[*at ^ 1]);
+        }
         if (int rc = launch_status("digit_scatter_kernel")) return rc;
     }
     return CNGP_OK;

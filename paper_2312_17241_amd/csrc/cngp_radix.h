@@ -100,7 +100,10 @@ __global__ __launch_bounds__(kScanBlock) void digit_row_scan_kernel(uint32_t *__
 // One pass of the sort for one tile.  keys_in in the order of the previous pass; index_in NULL = the identity
 // (first pass).  keys_out NULL on the last pass (nobody reads them).  Element n of the input goes to
 //   sum of totals of smaller digits + counts[digit][tile] (prefix over earlier tiles) + its rank inside the tile.
-template <int ROUNDS>
+// PREFIX: `counts` holds the tiles' own counts, as for up to kPrefixTiles tiles, whose prefix every workgroup then adds up itself (`totals` is
+// not read): a launch less per pass.
+constexpr int kPrefixTiles = 128;
+template <int ROUNDS, bool PREFIX = false>
 __global__ __launch_bounds__(kTileBlock) void digit_scatter_kernel(
     const uint32_t *__restrict__ keys_in, const int32_t *__restrict__ index_in, const int64_t N, const int shift,
     const uint32_t *__restrict__ counts, const int64_t tiles, const uint32_t *__restrict__ totals,
@@ -118,6 +121,16 @@ __global__ __launch_bounds__(kTileBlock) void digit_scatter_kernel(
     const int     tile_n = (int)((N - n0 < TILE) ? N - n0 : TILE);
     uint32_t     *mine = wave_count + w * kDigits;
     for (int i = t; i < kTileWaves * kDigits; i += kTileBlock) wave_count[i] = 0;
+    uint32_t part_all = 0, part_before = 0;                 // PREFIX: lane t adds every fourth tile's count of digit t mod 128
+    if constexpr (PREFIX) {
+        const uint32_t *row = counts + (size_t)(t & (kDigits - 1)) * (size_t)tiles;
+#pragma unroll 8
+        for (int64_t i = t >> kDigitBits; i < tiles; i += kTileBlock / kDigits) {
+            const uint32_t c = row[i];
+            part_all += c;
+            part_before += i < tile ? c : 0u;
+        }
+    }
     __syncthreads();
 
     // rank of every element among the equal digits before it in this wavefront's eighth of the tile
@@ -162,7 +175,20 @@ __global__ __launch_bounds__(kTileBlock) void digit_scatter_kernel(
             wave_count[k * kDigits + t] = count;
             count += c;
         }
-        total = totals[t];
+        if constexpr (!PREFIX) total = totals[t];
+    }
+    uint32_t earlier = 0;                                   // the digit's elements in earlier tiles
+    if constexpr (PREFIX) {
+        __syncthreads();
+        stage[t] = part_all;
+        stage[kTileBlock + t] = part_before;
+        __syncthreads();
+        if (t < kDigits) {
+#pragma unroll
+            for (int k = 0; k < kTileBlock / kDigits; ++k) { total += stage[k * kDigits + t]; earlier += stage[kTileBlock + k * kDigits + t]; }
+        }
+    } else if (t < kDigits) {
+        earlier = counts[(size_t)t * (size_t)tiles + (size_t)tile];
     }
     uint32_t       count_sum, total_sum;
     const uint32_t count_before = wave_exclusive_scan(count, &count_sum);
@@ -171,7 +197,7 @@ __global__ __launch_bounds__(kTileBlock) void digit_scatter_kernel(
     __syncthreads();
     if (t < kDigits) {
         tile_start[t] = (w ? carry[0] : 0u) + count_before;
-        dest[t] = (w ? carry[1] : 0u) + total_before + counts[(size_t)t * (size_t)tiles + (size_t)tile];
+        dest[t] = (w ? carry[1] : 0u) + total_before + earlier;
     }
     __syncthreads();
 

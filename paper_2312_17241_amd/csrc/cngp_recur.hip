@@ -128,13 +128,17 @@ RecurPlan plan_of(const cngp_recur_config *c, int64_t N, int64_t S, bool ragged)
     return p;
 }
 
+// Whether the backward pass reads the states that the caller kept: not where they are rounded to fp16 and the gradient of the gates,
+// which they are a factor of, is fp32.
+bool keeps_states(const cngp_recur_config *c, bool given) { return given && (c->io_dtype == CNGP_F32 || c->gate_dtype == CNGP_F16); }
+
 RecurSpace space_of(const cngp_recur_config *c, const RecurPlan &p, int64_t N, int64_t S, uint32_t call) {
     RecurSpace s{};
     size_t at = 0;
     auto take = [&](bool wanted, size_t bytes) { const size_t o = at; if (wanted) at += align256(bytes); return o; };
     const size_t C = (size_t)c->channels;
     const bool   bwd = call & CNGP_RECUR_CALL_BWD;
-    s.y = take(bwd && (call & CNGP_RECUR_CALL_NO_Y), (size_t)N * C * 4);
+    s.y = take(bwd && !keeps_states(c, !(call & CNGP_RECUR_CALL_NO_Y)), (size_t)N * C * 4);
     s.slope = take(bwd && c->gate_channels == 1 && p.tiles > 1, (size_t)N * (size_t)p.tiles * 4);
     s.piece_a = take(p.exact, p.K * C * 4);
     s.piece_b = take(p.exact, p.K * C * 4);
@@ -198,6 +202,7 @@ int cngp_recur_bwd(const cngp_recur_config *cfg, const void *gate, const void *x
     hipStream_t s = (hipStream_t)stream;
     if (N == 0) return pass_states(dlast, dh0, sequences * cfg->channels, s);
     const RecurPlan  p = plan_of(cfg, N, sequences, offsets != nullptr);
+    if (!keeps_states(cfg, y != nullptr)) y = nullptr;
     const uint32_t   call = CNGP_RECUR_CALL_BWD | (offsets ? CNGP_RECUR_CALL_RAGGED : 0) | (y ? 0 : CNGP_RECUR_CALL_NO_Y);
     const RecurSpace sp = space_of(cfg, p, N, sequences, call);
     char            *ws = (char *)workspace;

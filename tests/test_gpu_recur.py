@@ -55,7 +55,7 @@ def check(C, shared, lengths, io=F32, gt=F32, flags=0, h0=True, dy=True, dlast=T
         inside[lo:hi] = True
     ref = R.backward(np.where(inside[:, None], f64["gate"], 0), np.where(inside[:, None], f64["x"], 0), sp, f64["h0"] if h0 else None,
                      f64["dy"] if dy else None, f64["dlast"] if dlast else None, bool(flags & REV), bool(flags & LOG), bool(flags & MIX),
-                     R.half_step(NP[io]) if keep else 0.0)
+                     R.half_step(NP[io]) if keep and gt == F16 else 0.0)      # fp32 gates: states in fp32
     t = {k: dev(v) for k, v in d.items()}
     where = dict(h0=t["h0"] if h0 else None, offsets=dev(off), sequences=S)
     sentinel = torch.full((N, C), 7.0, dtype=t["x"].dtype, device=DEV)

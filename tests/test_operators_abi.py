@@ -63,6 +63,16 @@ def test_recurrence_workspaces_grow_with_what_is_asked():
                     assert cngp.recur_workspace_bytes(cfg, N, S, False, ragged) % 256 == 0
 
 
+def test_states_rounded_to_fp16_do_not_serve_fp32_gates():
+    """The backward pass computes them again: it asks for the room of a call without them."""
+    for io, gate, again in ((0, 0, False), (1, 1, False), (0, 1, False), (1, 0, True)):
+        cfg = recur(io_dtype=io, gate_dtype=gate)
+        room = lambda with_y: cngp.recur_workspace_bytes(cfg, 6, 3, True, False, with_y)
+        assert (room(True) == room(False)) == again
+        if again:
+            assert bwd(cfg, ws=None) == cngp.ERR_WORKSPACE
+
+
 def embed(**over):
     kw = dict(rows=10, dim=4)
     kw.update(over)

@@ -89,12 +89,34 @@ __global__ __launch_bounds__(kEmbBlock) void embed_fwd_kernel(const Id *__restri
     }
 }
 
+// Values [lo, hi) of the gradient cleared by a workgroup.  Where ids are sorted, the first kernel of the sort does it beside its own work, which
+// is latency (16381 ids and 50000 rows of 1024: 27 us of clearing hide the sort's 14).
+template <int BLOCK>
+__device__ __forceinline__ void clear_values(float *__restrict__ grad, const int64_t lo, const int64_t hi) {
+    const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int64_t i = lo + (int64_t)threadIdx.x * 4; i < hi; i += BLOCK * 4) {
+        if (i + 4 <= hi) store_run<float, 4>(grad + i, zero);
+        else for (int64_t j = i; j < hi; ++j) grad[j] = 0.0f;
+    }
+}
+
+__global__ __launch_bounds__(kEmbBlock) void embed_clear_kernel(float *__restrict__ grad, const int64_t n, const int64_t each)
+{
+    const int64_t lo = (int64_t)blockIdx.x * each;
+    clear_values<kEmbBlock>(grad, lo, lo + each < n ? lo + each : n);
+}
+
 // ---------------------------------------------------------------- sort of the ids
-template <typename Id, int ROUNDS>
+template <typename Id, int ROUNDS, bool PREFIX>
 __global__ __launch_bounds__(kTileBlock) void embed_keys_kernel(const Id *__restrict__ ids, uint32_t *__restrict__ keys, const int64_t N, const int64_t rows,
-                                                                uint32_t *__restrict__ counts, const int64_t tiles)
+                                                                uint32_t *__restrict__ counts, const int64_t tiles, float *__restrict__ grad,
+                                                                const int64_t values)
 {
     __shared__ uint32_t hist[kTileWaves * kDigits];
+    if (grad) {
+        const int64_t each = ((values + tiles - 1) / tiles + 3) / 4 * 4, lo = each * blockIdx.x;
+        clear_values<kTileBlock>(grad, lo, lo + each < values ? lo + each : values);
+    }
     const int     t = threadIdx.x, w = t >> 6;
     const int64_t n0 = (int64_t)blockIdx.x * (kTileBlock * ROUNDS);
     for (int i = t; i < kTileWaves * kDigits; i += kTileBlock) hist[i] = 0;
@@ -114,7 +136,7 @@ __global__ __launch_bounds__(kTileBlock) void embed_keys_kernel(const Id *__rest
         }
     }
     __syncthreads();
-    flush_tile_histogram(hist, counts, tiles, blockIdx.x, t);
+    flush_tile_histogram<PREFIX>(hist, counts, tiles, blockIdx.x, t);
 }
 
 // Up to 16384 ids are sorted in one launch (the passes above are three launches each, of which a short batch fills a few workgroups).
@@ -126,7 +148,8 @@ constexpr int kSmallBlock = 1024, kSmallWaves = kSmallBlock / 64, kSmallBits = 8
               kSmallMost = kSmallBlock * kSmallRounds;
 template <typename Id>
 __global__ __launch_bounds__(kSmallBlock) void embed_sort_small_kernel(const Id *__restrict__ ids, uint32_t *__restrict__ keys, int32_t *__restrict__ from,
-                                                                       const int N, const int64_t rows, const uint32_t share)
+                                                                       const int N, const int64_t rows, const uint32_t share, float *__restrict__ grad,
+                                                                       const int dim)
 {
     extern __shared__ __align__(16) uint32_t small_lds[];      // counts [waves][digits], then keys and points of the share, N each
     uint32_t *wave_count = small_lds, *stage_key = small_lds + kSmallWaves * kSmallDigits, *stage_from = stage_key + kSmallMost;
@@ -135,6 +158,7 @@ __global__ __launch_bounds__(kSmallBlock) void embed_sort_small_kernel(const Id 
     const uint64_t below = lane ? (~0ull >> (64 - lane)) : 0ull;
     const uint32_t key_lo = blockIdx.x * share, key_hi = key_lo + share;
     const int      rounds = (N + kSmallBlock - 1) / kSmallBlock;
+    if (grad) clear_values<kSmallBlock>(grad, (int64_t)key_lo * dim, (key_hi < rows ? (int64_t)key_hi : rows) * dim);
 
     // the ids of the share, in their order: round r, wavefront w, lane
     uint32_t key[kSmallRounds], less = 0;
@@ -438,19 +462,6 @@ __global__ __launch_bounds__(kEmbBlock) void embed_join_kernel(const SumArgs a)
     put_row<V>(a, key, c, sum);
 }
 
-__global__ __launch_bounds__(kEmbBlock) void embed_clear_kernel(float *__restrict__ grad, const int64_t n)
-{
-    const int64_t step = (int64_t)gridDim.x * kEmbBlock * 4;
-    for (int64_t i = ((int64_t)blockIdx.x * kEmbBlock + threadIdx.x) * 4; i < n; i += step) {
-        if (i + 4 <= n) {
-            const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            store_run<float, 4>(grad + i, zero);
-        } else {
-            for (int64_t j = i; j < n; ++j) grad[j] = 0.0f;
-        }
-    }
-}
-
 int check(const cngp_embed_config *c, int64_t N) {
     if (!c) return CNGP_ERR_NULL;
     if (c->rows < 1 || c->rows > 0x7ffffffeLL || c->dim < 1 || c->dim > 65536) return CNGP_ERR_INVALID;
@@ -475,11 +486,12 @@ int lanes_of(int dim, int columns) {
     return n <= 1 ? 1 : n <= 4 ? 4 : n <= 16 ? 16 : 64;
 }
 
-// Positions of a piece: eight per row lane (what is in flight), or as many as leave 8192 wavefronts over pieces and column tiles.
+// Positions of a piece: eight per row lane (what is in flight), or as many as leave 8192 wavefronts over pieces and column tiles; up to 64 to a
+// row lane where that is all of them, which then need not be joined.
 uint32_t piece_of(const cngp_embed_config *c, int64_t N) {
     const int     columns = columns_of(c->dim, c->io_dtype == CNGP_F16 ? 8 : 4), lpr = lanes_of(c->dim, columns), rl = 64 / lpr;
     const int64_t tiles = (c->dim / columns + lpr - 1) / lpr, each = (N * tiles / rl + 8191) / 8192;
-    return (uint32_t)(std::max<int64_t>(each, kSumAhead) * rl);
+    return (uint32_t)((N <= 64 * rl ? std::max<int64_t>((N + rl - 1) / rl, 1) : std::max<int64_t>(each, kSumAhead)) * rl);
 }
 
 // Elements per lane of the sort's tiles: sixteen once those fill the chip, four for shorter batches.
@@ -506,49 +518,62 @@ EmbedSpace space_of(const cngp_embed_config *c, int64_t N) {
     return s;
 }
 
-// Shares of the keys 0 .. rows: a workgroup for every 64 ids, at most one per CU (each reads all ids; a share of 256 keys is one pass).
+// Shares of the keys 0 .. rows: a workgroup for every 64 ids or 64 KB of table to clear, at most one per CU (each reads all ids; a share of 256
+// keys is one pass).
 template <typename Id>
-int sort_small(const void *ids, uint32_t *keys, int32_t *from, int64_t N, int64_t rows, hipStream_t s) {
+int sort_small(const void *ids, uint32_t *keys, int32_t *from, int64_t N, int64_t rows, int dim, float *clear, hipStream_t s) {
     constexpr size_t lds = (size_t)(kSmallWaves * kSmallDigits + 2 * kSmallMost) * 4;
     if (hipError_t e = hipFuncSetAttribute((const void *)embed_sort_small_kernel<Id>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds))
         return record_hip_failure(e, "hipFuncSetAttribute(MaxDynamicSharedMemorySize)");
-    const int64_t groups = std::min<int64_t>(std::max<int64_t>((N + 63) / 64, 1), 256), share = (rows + 1 + groups - 1) / groups;
-    embed_sort_small_kernel<Id><<<(unsigned)((rows + 1 + share - 1) / share), kSmallBlock, lds, s>>>((const Id *)ids, keys, from, (int)N, rows, (uint32_t)share);
+    const int64_t wanted = std::max<int64_t>((N + 63) / 64, clear ? rows * dim / 16384 : 0);
+    const int64_t groups = std::min<int64_t>(std::max<int64_t>(wanted, 1), 256), share = (rows + 1 + groups - 1) / groups;
+    embed_sort_small_kernel<Id><<<(unsigned)((rows + 1 + share - 1) / share), kSmallBlock, lds, s>>>((const Id *)ids, keys, from, (int)N, rows, (uint32_t)share,
+                                                                                                    clear, dim);
     return launch_status("embed_sort_small_kernel");
 }
 
-template <typename Id, int ROUNDS>
-int sort_passes(const void *ids, int64_t N, int64_t rows, uint32_t *(&keys)[2], int32_t *(&from)[2], uint32_t *counts, uint32_t *totals, int *at, hipStream_t s) {
+template <typename Id, int ROUNDS, bool PREFIX>
+int sort_passes(const void *ids, int64_t N, int64_t rows, int dim, float *clear, uint32_t *(&keys)[2], int32_t *(&from)[2], uint32_t *counts, uint32_t *totals,
+                int *at, hipStream_t s) {
     constexpr int  TILE = kTileBlock * ROUNDS;
     const unsigned tiles = (unsigned)((N + TILE - 1) / TILE);
-    embed_keys_kernel<Id, ROUNDS><<<tiles, kTileBlock, 0, s>>>((const Id *)ids, keys[0], N, rows, counts, tiles);
+    embed_keys_kernel<Id, ROUNDS, PREFIX><<<tiles, kTileBlock, 0, s>>>((const Id *)ids, keys[0], N, rows, counts, tiles, clear, rows * dim);
     if (int rc = launch_status("embed_keys_kernel")) return rc;
     for (int shift = 0; shift < 32 && ((uint64_t)rows >> shift); shift += kDigitBits, *at ^= 1) {
         if (shift) {
-            digit_count_kernel<ROUNDS><<<tiles, kTileBlock, 0, s>>>(keys[*at], N, shift, counts, tiles);
+            digit_count_kernel<ROUNDS, PREFIX><<<tiles, kTileBlock, 0, s>>>(keys[*at], N, shift, counts, tiles);
             if (int rc = launch_status("digit_count_kernel")) return rc;
         }
-        const int32_t *order = shift ? from[*at] : nullptr;
-        if (tiles <= (unsigned)kPrefixTiles) {
-            digit_scatter_kernel<ROUNDS, true><<<tiles, kTileBlock, 0, s>>>(keys[*at], order, N, shift, counts, tiles, totals, keys[*at ^ 1], from[*at ^ 1]);
-        } else {
+        if (!PREFIX) {
             digit_row_scan_kernel<<<kDigits, kScanBlock, 0, s>>>(counts, tiles, totals);
             if (int rc = launch_status("digit_row_scan_kernel")) return rc;
-            digit_scatter_kernel<ROUNDS><<<tiles, kTileBlock, 0, s>>>(keys[*at], order, N, shift, counts, tiles, totals, keys[*at ^ 1], from[*at ^ 1]);
         }
+        digit_scatter_kernel<ROUNDS, PREFIX><<<tiles, kTileBlock, 0, s>>>(keys[*at], shift ? from[*at] : nullptr, N, shift, counts, tiles, totals, keys[*at ^ 1],
+                                                                          from[*at ^ 1]);
         if (int rc = launch_status("digit_scatter_kernel")) return rc;
     }
     return CNGP_OK;
 }
 
-// Sorted keys and the points they came from, in keys[0] and from[0] or, after an odd number of passes, [1]: *at says which.
+int clear_table(float *grad, int64_t n, hipStream_t s) {
+    const int64_t each = std::max<int64_t>((n + 8191) / 8192 / 4 * 4 + 4, kEmbBlock * 4);
+    LaunchTimer   t(s, K_ZERO);
+    embed_clear_kernel<<<(unsigned)((n + each - 1) / each), kEmbBlock, 0, s>>>(grad, n, each);
+    return launch_status("embed_clear_kernel");
+}
+
+// Sorted keys and the points they came from (and `clear`, if given, set to zero), in keys[0] and from[0] or, after an odd number of passes, [1]: *at says which.
 template <typename Id>
-int sort_ids(const void *ids, int64_t N, int64_t rows, uint32_t *(&keys)[2], int32_t *(&from)[2], uint32_t *counts, uint32_t *totals, int *at, hipStream_t s) {
+int sort_ids(const void *ids, int64_t N, int64_t rows, int dim, float *clear, uint32_t *(&keys)[2], int32_t *(&from)[2], uint32_t *counts, uint32_t *totals, int *at, hipStream_t s) {
     LaunchTimer t(s, K_EMBED_SORT);
     *at = 0;
-    if (N <= kSmallMost) return sort_small<Id>(ids, keys[0], from[0], N, rows, s);
-    return rounds_of(N) == kRounds ? sort_passes<Id, kRounds>(ids, N, rows, keys, from, counts, totals, at, s)
-                                   : sort_passes<Id, 4>(ids, N, rows, keys, from, counts, totals, at, s);
+    if (N <= kSmallMost) return sort_small<Id>(ids, keys[0], from[0], N, rows, dim, clear, s);
+    if (N <= (int64_t)kPrefixTiles * kTileBlock * 4) return sort_passes<Id, 4, true>(ids, N, rows, dim, clear, keys, from, counts, totals, at, s);
+    // a longer sort fills the chip by itself: cleared beside its first kernel, 2^20 rows of 64 took 299 us in place of 289
+    if (clear)
+        if (int rc = clear_table(clear, rows * dim, s)) return rc;
+    return rounds_of(N) == kRounds ? sort_passes<Id, kRounds, false>(ids, N, rows, dim, nullptr, keys, from, counts, totals, at, s)
+                                   : sort_passes<Id, 4, false>(ids, N, rows, dim, nullptr, keys, from, counts, totals, at, s);
 }
 
 template <typename Io, int V, int LPR>
@@ -626,20 +651,15 @@ int cngp_embed_bwd(const cngp_embed_config *cfg, const void *ids, int64_t N, con
     const EmbedSpace sp = space_of(cfg, N);
     if (sp.bytes && (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < sp.bytes)) return CNGP_ERR_WORKSPACE;
     hipStream_t s = (hipStream_t)stream;
-    if (!accumulate) {
-        const int64_t n = cfg->rows * cfg->dim, blocks = (n + kEmbBlock * 4 - 1) / (kEmbBlock * 4);
-        LaunchTimer t(s, K_ZERO);
-        embed_clear_kernel<<<(unsigned)std::min<int64_t>(blocks, 8192), kEmbBlock, 0, s>>>(grad_table, n);
-        if (int rc = launch_status("embed_clear_kernel")) return rc;
-    }
-    if (N == 0) return CNGP_OK;
+    float *clear = accumulate ? nullptr : grad_table;
+    if (N == 0) return clear ? clear_table(clear, cfg->rows * cfg->dim, s) : CNGP_OK;
     char     *ws = (char *)workspace;
     uint32_t *keys[2] = {(uint32_t *)(ws + sp.keys_a), (uint32_t *)(ws + sp.keys_b)};
     int32_t  *from[2] = {(int32_t *)(ws + sp.from_a), (int32_t *)(ws + sp.from_b)};
     uint32_t *counts = (uint32_t *)(ws + sp.counts), *totals = (uint32_t *)(ws + sp.totals);
     int       at = 0;
-    if (int rc = cfg->id_dtype == CNGP_I64 ? sort_ids<int64_t>(ids, N, cfg->rows, keys, from, counts, totals, &at, s)
-                                           : sort_ids<int32_t>(ids, N, cfg->rows, keys, from, counts, totals, &at, s))
+    if (int rc = cfg->id_dtype == CNGP_I64 ? sort_ids<int64_t>(ids, N, cfg->rows, cfg->dim, clear, keys, from, counts, totals, &at, s)
+                                           : sort_ids<int32_t>(ids, N, cfg->rows, cfg->dim, clear, keys, from, counts, totals, &at, s))
         return rc;
     SumArgs a{};
     a.keys = keys[at]; a.from = from[at]; a.dy = dy; a.grad = grad_table;

@@ -18,7 +18,9 @@ constexpr int kScanBlock = 1024;
 inline size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
 inline int64_t tiles_of(int64_t N) { return (N + kTile - 1) / kTile; }
 
-// Sum of a tile's per-wavefront histograms, written as column `tile` of counts[digit][tiles].
+// Sum of a tile's per-wavefront histograms, written as column `tile` of counts[digit][tiles], or with PREFIX as row `tile` of
+// counts[tiles][digit] (what digit_scatter_kernel adds up itself).
+template <bool PREFIX = false>
 __device__ __forceinline__ void flush_tile_histogram(const uint32_t *hist, uint32_t *__restrict__ counts,
                                                      const int64_t tiles, const int64_t tile, const int t)
 {
@@ -26,11 +28,11 @@ __device__ __forceinline__ void flush_tile_histogram(const uint32_t *hist, uint3
         uint32_t sum = 0;
 #pragma unroll
         for (int w = 0; w < kTileWaves; ++w) sum += hist[w * kDigits + t];
-        counts[(size_t)t * (size_t)tiles + (size_t)tile] = sum;
+        counts[PREFIX ? (size_t)tile * kDigits + (size_t)t : (size_t)t * (size_t)tiles + (size_t)tile] = sum;
     }
 }
 
-template <int ROUNDS>
+template <int ROUNDS, bool PREFIX = false>
 __global__ __launch_bounds__(kTileBlock) void digit_count_kernel(const uint32_t *__restrict__ keys, const int64_t N, const int shift,
                                                                  uint32_t *__restrict__ counts, const int64_t tiles)
 {
@@ -51,7 +53,7 @@ __global__ __launch_bounds__(kTileBlock) void digit_count_kernel(const uint32_t 
         if (n < N) atomicAdd(&hist[w * kDigits + ((key[r] >> shift) & (kDigits - 1))], 1u);
     }
     __syncthreads();
-    flush_tile_histogram(hist, counts, tiles, blockIdx.x, t);
+    flush_tile_histogram<PREFIX>(hist, counts, tiles, blockIdx.x, t);
 }
 
 // Exclusive prefix of v over the 64 lanes of a wavefront; *total = the sum.
@@ -100,8 +102,8 @@ __global__ __launch_bounds__(kScanBlock) void digit_row_scan_kernel(uint32_t *__
 // One pass of the sort for one tile.  keys_in in the order of the previous pass; index_in NULL = the identity
 // (first pass).  keys_out NULL on the last pass (nobody reads them).  Element n of the input goes to
 //   sum of totals of smaller digits + counts[digit][tile] (prefix over earlier tiles) + its rank inside the tile.
-// PREFIX: `counts` holds the tiles' own counts, as for up to kPrefixTiles tiles, whose prefix every workgroup then adds up itself (`totals` is
-// not read): a launch less per pass.
+// PREFIX, for up to kPrefixTiles tiles: `counts` holds the tiles' own counts, whose prefix every workgroup adds up itself (`totals` is not read):
+// a launch less per pass.
 constexpr int kPrefixTiles = 128;
 template <int ROUNDS, bool PREFIX = false>
 __global__ __launch_bounds__(kTileBlock) void digit_scatter_kernel(
@@ -123,10 +125,9 @@ __global__ __launch_bounds__(kTileBlock) void digit_scatter_kernel(
     for (int i = t; i < kTileWaves * kDigits; i += kTileBlock) wave_count[i] = 0;
     uint32_t part_all = 0, part_before = 0;                 // PREFIX: lane t adds every fourth tile's count of digit t mod 128
     if constexpr (PREFIX) {
-        const uint32_t *row = counts + (size_t)(t & (kDigits - 1)) * (size_t)tiles;
 #pragma unroll 8
         for (int64_t i = t >> kDigitBits; i < tiles; i += kTileBlock / kDigits) {
-            const uint32_t c = row[i];
+            const uint32_t c = counts[(size_t)i * kDigits + (size_t)(t & (kDigits - 1))];
             part_all += c;
             part_before += i < tile ? c : 0u;
         }

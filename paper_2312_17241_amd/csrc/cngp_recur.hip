@@ -111,7 +111,8 @@ RecurPlan plan_of(const cngp_recur_config *c, int64_t N, int64_t S, bool ragged)
     int64_t       R = (N * p.tiles + enough - 1) / enough;
     R = std::max<int64_t>((R + tile_rows - 1) / tile_rows * tile_rows, tile_rows);
     // sequences that are no longer than a few windows stay whole: one launch, every input read once.  Longer ones are cut
-    p.exact = longest > 4 * R;
+    // (a tile after the other takes 1.5 to 2 us; the two launches more of a cut sequence take what a dozen tiles do)
+    p.exact = longest > std::max(4 * R, 12 * tile_rows);
     if (p.exact && p.V == 2 && !ragged && S * ((C + 31) / 32) >= 192) {
         // enough sequences by channels to give most CUs one of 32 channels, walked by eight wavefronts: whole after all
         p.CL = 16;

@@ -25,24 +25,30 @@ def stale() -> bool:
     return any(os.path.getmtime(os.path.join(CSRC, f)) > t for f in SOURCES + HEADERS)
 
 
+def _compile_and_link(flags, sources, out_dir, out, link_flags, what):
+    """Every source to an object, side by side, then one link."""
+    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+    os.makedirs(out_dir, exist_ok=True)
+    objects = [os.path.join(out_dir, os.path.basename(f) + ".o") for f in sources]
+    jobs = [subprocess.Popen([hipcc] + flags + ["-c", "-o", o, f], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+            for f, o in zip(sources, objects)]
+    log = "".join(job.communicate()[0] for job in jobs)
+    failed = any(job.returncode for job in jobs)
+    if not failed:
+        res = subprocess.run([hipcc] + link_flags + ["-o", out] + objects, capture_output=True, text=True)
+        log, failed = log + res.stdout + res.stderr, res.returncode != 0
+    msgs = [ln for ln in log.splitlines() if "packed-fp32-ops" not in ln]          # the host pass does not know the feature: harmless
+    if failed:
+        raise RuntimeError(f"{what} failed:\n" + "\n".join(msgs))
+    return msgs
+
+
 def build(force: bool = True, extra=()) -> str:
     if not force and not stale():
         return LIB
-    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     out_dir = os.path.join(os.path.dirname(HERE), "_build")
-    os.makedirs(out_dir, exist_ok=True)
-    objects = [os.path.join(out_dir, f + ".o") for f in SOURCES]
-    compile_flags = [f for f in FLAGS if f != "-shared"] + list(extra)
-    jobs = [subprocess.Popen([hipcc] + compile_flags + ["-c", "-o", o, os.path.join(CSRC, f)], stdout=subprocess.PIPE,
-                             stderr=subprocess.STDOUT, text=True) for f, o in zip(SOURCES, objects)]       # side by side
-    out = "".join(job.communicate()[0] for job in jobs)
-    failed = any(job.returncode for job in jobs)
-    if not failed:
-        res = subprocess.run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB] + objects, capture_output=True, text=True)
-        out, failed = out + res.stdout + res.stderr, res.returncode != 0
-    msgs = [ln for ln in out.splitlines() if "packed-fp32-ops" not in ln]          # the host pass does not know the feature: harmless
-    if failed:
-        raise RuntimeError("hipcc failed:\n" + "\n".join(msgs))
+    msgs = _compile_and_link([f for f in FLAGS if f != "-shared"] + list(extra), [os.path.join(CSRC, f) for f in SOURCES], out_dir, LIB,
+                             ["--offload-arch=gfx950", "-shared", "-fPIC"], "hipcc")
     if msgs:
         print("\n".join(msgs), file=sys.stderr)
     return LIB
@@ -60,15 +66,11 @@ def build_host_sanitized() -> str:
     srcs = [os.path.join(CSRC, f) for f in SOURCES + HEADERS] + [main]
     if os.path.exists(exe) and os.path.getmtime(exe) >= max(os.path.getmtime(f) for f in srcs):
         return exe
-    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     san = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
            "-Xarch_host", "-fno-sanitize-recover=undefined"]
-    flags = [f for f in FLAGS if f not in ("-shared", "-fPIC", "-O3")] + ["-O1", "-g"]
-    cmd = [hipcc] + flags + san + ["-o", exe, main] + [os.path.join(CSRC, s) for s in SOURCES]
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if res.returncode != 0:
-        raise RuntimeError("hipcc (host sanitizers) failed:\n" + "\n".join(
-            ln for ln in (res.stdout + res.stderr).splitlines() if "packed-fp32-ops" not in ln))
+    flags = [f for f in FLAGS if f not in ("-shared", "-fPIC", "-O3")] + ["-O1", "-g"] + san
+    _compile_and_link(flags, [main] + [os.path.join(CSRC, s) for s in SOURCES], os.path.join(out_dir, "sanitized"), exe,
+                      ["--offload-arch=gfx950"] + san, "hipcc (host sanitizers)")
     return exe
 
 

@@ -1,6 +1,6 @@
 // Exerciser of the library's HOST code under AddressSanitizer and UndefinedBehaviorSanitizer: argument
 // validation, level table, storage sizes, the backward plan (slices, chunks, bins, passes) and its workspace
-// layout, for seeded random configurations, and the rule that decides which corners of a point become entries.  It is linked with cngp_api.hip and cngp_sort.hip compiled with the
+// layout, for seeded random configurations, and the rule that decides which corners of a point become entries.  It is linked with the library's .hip files compiled with the
 // sanitizers on the host side only (`python paper_2312_17241_amd/build.py --host-sanitizers`) and launches
 // nothing: every call below returns before a kernel would be enqueued, so it runs without a GPU.
 // Exit code 0 = clean.
@@ -126,6 +126,30 @@ int main() {
         if (cngp_morton_sort_workspace_bytes(3, N) != 3 * col + (tiles * 512 + 255) / 256 * 256 + 512) bad |= 8192;
     }
     if (cngp_morton_sort_workspace_bytes(5, 100) != 0 || cngp_morton_sort(3, nullptr, 5, nullptr, nullptr, nullptr, 0, nullptr) == CNGP_OK) bad |= 8192;
+    // the operators around the encoding: workspaces of random descriptions (invalid ones need none), missing arrays refused
+    for (int it = 0; it < 2000; ++it) {
+        const int64_t counts[] = {0, 1, 63, 4097, 100003, (int64_t)1 << 22, (int64_t)1 << 27, 0x7fff0000, 0x7fffffff};
+        const int64_t N = counts[below(9)], S = it % 3 ? counts[below(9)] : 1;
+        cngp_recur_config r = {(int)below(70000), 1, (int)below(3), (int)below(2), (int)below(4000) - 10, below(9)};
+        if (below(2)) r.gate_channels = r.channels;
+        const uint32_t call = below(8);
+        const size_t   fwd = cngp_recur_workspace_bytes(&r, N, S, call & CNGP_RECUR_CALL_RAGGED), with_y = cngp_recur_workspace_bytes(&r, N, S, call | CNGP_RECUR_CALL_BWD),
+                       without = cngp_recur_workspace_bytes(&r, N, S, call | CNGP_RECUR_CALL_BWD | CNGP_RECUR_CALL_NO_Y);
+        if (fwd % 256 || with_y % 256 || without % 256 || without < with_y || with_y < fwd) bad |= 65536;
+        if (N > 0 && S > 0 && cngp_recur_fwd(&r, nullptr, nullptr, N, nullptr, S, nullptr, nullptr, nullptr, nullptr, 0, nullptr) == CNGP_OK) bad |= 65536;
+        if (N > 0 && S > 0 && cngp_recur_bwd(&r, nullptr, nullptr, N, nullptr, S, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, 0, nullptr) == CNGP_OK) bad |= 65536;
+        cngp_embed_config e = {counts[below(9)], (int)below(70000), (int)below(2), (int)below(3), (int)below(2), 1.0f, below(2)};
+        const size_t      room = cngp_embed_workspace_bytes(&e, N);
+        if (room % 256 || (room != 0 && N == 0)) bad |= 131072;
+        if (N > 0 && cngp_embed_fwd(&e, nullptr, N, nullptr, nullptr, nullptr, nullptr) == CNGP_OK) bad |= 131072;
+        if (cngp_embed_bwd(&e, nullptr, N, nullptr, nullptr, nullptr, 0, nullptr) == CNGP_OK) bad |= 131072;
+        cngp_config c;
+        std::memset(&c, 0, sizeof(c));
+        c.d = 3; c.L = 1 + (int)below(32); c.F = 2; c.N_p = 1u << below(5); c.N_f = 1u << 10; c.N_c = 1u << below(31); c.N_min = 4; c.N_max = 64;
+        c.top_k = below(c.N_p + 2);
+        if (cngp_probe_balance_workspace_bytes(&c) % 256) bad |= 262144;
+        if (cngp_probe_balance(&c, nullptr, nullptr, 1.0f, nullptr, nullptr, nullptr, nullptr, 0, nullptr) == CNGP_OK) bad |= 262144;
+    }
     if (bad) { std::fprintf(stderr, "host sanitizer run: inconsistent results, mask %d\n", bad); return 1; }
     std::printf("host sanitizer run: clean\n");
     return 0;

@@ -4,9 +4,9 @@
 //     d loss / d logit_rk = N_p / W * sigma_rk (f_k - sum_j f_j sigma_rj)
 // The gradient of every row needs the level's f, so two launches: one reads the logits and leaves sums per workgroup, the other
 // adds those up (in a fixed order), reads the logits again and writes the gradient.  A level that one workgroup can hold in registers
-// takes one launch.  A lane has a whole row, so nothing of a row is computed twice and its softmax needs no other lane.  With 4 lanes to
-// a row of 16 the sparse variant, which ranks a row's logits, was bound by the vector ALU: 16 x 2^18 x 16 logits 171 us in the
-// first launch against 285 us together; now see balance_sums_kernel.
+// takes one launch.  16 levels x 2^18 rows x 16 logits, the four largest kept: 182 us, 106 + 96 where each launch is profiled by itself; reading
+// 268 MB twice and writing it once is 805 MB, 113 us at the rates of a large read and a large fill.  The first launch is bound by the vector
+// ALU (the ranks), the second by memory.
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
@@ -69,18 +69,49 @@ struct Group {
     }
 };
 
+// Batcher's odd-even merge sort of N values: the pairs that are compared, in order (63 of 16, 19 of 8, 5 of 4).
+template <int N>
+struct Network {
+    int lo[64], hi[64], n;
+    constexpr Network() : lo(), hi(), n(0) {
+        for (int p = 1; p < N; p *= 2)
+            for (int k = p; k >= 1; k /= 2)
+                for (int j = k % p; j + k < N; j += 2 * k)
+                    for (int i = 0; i < k && i + j + k < N; ++i)
+                        if ((i + j) / (2 * p) == (i + j + k) / (2 * p)) { lo[n] = i + j; hi[n] = i + j + k; ++n; }
+    }
+};
+
 // Bit k: entry k is among the top_k largest of the row (equal values by lowest index, any number before a NaN).  Values are compared as
-// integers in the order of the numbers, a NaN below all; a pair is compared once, and the earlier of two equal ones is ahead.
+// integers in the order of the numbers, a NaN below all.  The top_k-th largest comes out of a sorting network, and what is not below it is
+// kept (195 instructions for 16 against 408 for the rank of each); where that is more than top_k in some row of the wavefront, values equal
+// to it among them, every entry is ranked: a pair is compared once, and the earlier of two equal ones is ahead.
 template <int NP>
 __device__ __forceinline__ uint32_t largest(const float *v, const uint32_t top_k) {
-    uint32_t key[NP];
-    int      ahead[NP];
+    static constexpr Network<NP> net{};
+    uint32_t key[NP], sorted[NP];
 #pragma unroll
     for (int k = 0; k < NP; ++k) {
         const uint32_t u = __builtin_bit_cast(uint32_t, v[k] + 0.0f);      // -0 is 0
         key[k] = v[k] == v[k] ? u ^ (uint32_t)((int32_t)u >> 31 | (int32_t)0x80000000) : 0u;      // minus infinity is 0x7fffff
-        ahead[k] = NP - 1 - k;
+        sorted[k] = key[k];
     }
+#pragma unroll
+    for (int i = 0; i < net.n; ++i) {
+        const uint32_t a = sorted[net.lo[i]], b = sorted[net.hi[i]];
+        sorted[net.lo[i]] = max(a, b);
+        sorted[net.hi[i]] = min(a, b);
+    }
+    uint32_t bar = sorted[NP - 1], kept = 0;
+#pragma unroll
+    for (int k = 0; k < NP - 1; ++k) bar = top_k == (uint32_t)(k + 1) ? sorted[k] : bar;
+#pragma unroll
+    for (int k = 0; k < NP; ++k) kept |= (key[k] >= bar ? 1u : 0u) << k;
+    if (!__any((uint32_t)__popc(kept) != top_k)) return kept;
+
+    int ahead[NP];
+#pragma unroll
+    for (int k = 0; k < NP; ++k) ahead[k] = NP - 1 - k;
 #pragma unroll
     for (int j = 0; j < NP; ++j)
 #pragma unroll
@@ -89,7 +120,7 @@ __device__ __forceinline__ uint32_t largest(const float *v, const uint32_t top_k
             ahead[k] += first;
             ahead[j] -= first;
         }
-    uint32_t kept = 0;
+    kept = 0;
 #pragma unroll
     for (int k = 0; k < NP; ++k) kept |= (ahead[k] < (int)top_k ? 1u : 0u) << k;
     return kept;
@@ -229,6 +260,9 @@ __device__ __forceinline__ void put_gradient(const BalArgs &a, const uint32_t le
     }
 }
 
+// A lane has a whole row here: nothing of the row is computed twice and its softmax needs no other lane.  With four lanes to a row of 16 the
+// sparse variant took 171 us at 16 x 2^18 x 16, with every entry of a lane's row ranked 133, with the network 106.  The next row is on its
+// way while one is worked on.
 template <int NP, bool SPARSE>
 __global__ __launch_bounds__(kBalBlock) void balance_sums_kernel(const BalArgs a)
 {
@@ -261,7 +295,7 @@ __global__ __launch_bounds__(kBalBlock) void balance_sums_kernel(const BalArgs a
 }
 
 // The second launch moves twice what the first does and computes little: here four lanes share a row of 16 (two one of 8), so that loads
-// and stores run over whole lines (one lane to a row: 130 us at 16 x 2^18 x 16, this 107), and exchange sums by lane permutations.
+// and stores run over whole lines (one lane to a row: 130 us at 16 x 2^18 x 16, this 96), and exchange sums by lane permutations.
 template <int X>
 __device__ __forceinline__ float across(const float v) {
     static_assert(X == 1 || X == 2, "a quad of lanes");
@@ -373,7 +407,8 @@ __global__ __launch_bounds__(kBalBlock) void balance_grad_kernel(const BalArgs a
     }
 }
 
-// A level of at most kLevelBlock * kLevelGroups groups: its weights stay in registers between the sums and the gradient.
+// A level of at most kLevelBlock * kLevelGroups groups: its weights stay in registers between the sums and the gradient, and the second launch
+// is saved: 4 levels x 256 rows x 4 take 4.6 us, bound by latency.
 template <int NP, bool SPARSE>
 __global__ __launch_bounds__(kLevelBlock) void balance_level_kernel(const BalArgs a)
 {

@@ -106,7 +106,8 @@ RecurPlan plan_of(const cngp_recur_config *c, int64_t N, int64_t S, bool ragged)
     const int64_t tile_rows = p.CL == 1 ? kNarrowBlock * kRowsNarrow : p.block / p.CL * kRowsEach;
     const int64_t mean = S ? (N + S - 1) / S : 0;
     const int64_t longest = !ragged ? mean : c->longest ? std::min<int64_t>(c->longest, N) : 4 * mean;
-    // windows that give every CU eight workgroups, of whole tiles
+    // windows that give every CU eight workgroups, of whole tiles; single wavefronts four times as many (a frame of 1920 x 1080 rays with 8192 of
+    // them 102.6 us, 4096 114, 16384 105)
     const int64_t enough = kEnoughGroups * (kRecurBlock / std::min(p.block, kRecurBlock));
     int64_t       R = (N * p.tiles + enough - 1) / enough;
     R = std::max<int64_t>((R + tile_rows - 1) / tile_rows * tile_rows, tile_rows);

@@ -214,8 +214,11 @@ int cngp_recur_bwd(const cngp_recur_config *cfg, const void *gate, const void *x
     if (!y) {
         a.out_y = ws + sp.y;
         a.y_f32 = 1;
-        if (int rc = recur_launch<false>(cfg, a, p, sp, ws, s)) return rc;
         a.y = a.out_y;
+        if (p.CL > 1 || p.exact) {                             // else the backward launch computes them (recur_narrow_again_kernel)
+            if (int rc = recur_launch<false>(cfg, a, p, sp, ws, s)) return rc;
+            a.out_y = nullptr;
+        }
     }
     a.dy = dy; a.dlast = dlast; a.dgate = dgate; a.dx = dx; a.dh0 = dh0;
     const bool sums = cfg->gate_channels == 1 && p.tiles > 1;

@@ -25,6 +25,45 @@ __device__ __forceinline__ float load(const __half *p, const int64_t i) { return
 __device__ __forceinline__ void store(float *p, const int64_t i, const float v) { p[i] = v; }
 __device__ __forceinline__ void store(__half *p, const int64_t i, const float v) { p[i] = __float2half_rn(v); }
 
+// V neighbouring values at once, on whatever boundary they start: global memory takes that, the compiler makes one access of it.
+template <typename T, int N>
+struct Run { T e[N]; };
+template <typename T, int V>
+__device__ __forceinline__ void load_vec(float (&out)[V], const T *p) {
+    Run<T, V> t;
+    __builtin_memcpy(&t, p, sizeof t);
+#pragma unroll
+    for (int v = 0; v < V; ++v) out[v] = load(t.e, v);
+}
+template <typename T, int V>
+__device__ __forceinline__ void store_vec(T *p, const float (&in)[V]) {
+    Run<T, V> t;
+#pragma unroll
+    for (int v = 0; v < V; ++v) store(t.e, v, in[v]);
+    __builtin_memcpy(p, &t, sizeof t);
+}
+
+// The gate of a row and how much of the input it lets in.  1 - exp(g) cancels for small g: there it is -g times the series of
+// (exp(g) - 1) / g to the ninth term (0.5^9 / 10! = 5e-10 below one), and exp(g) is one minus that, to the last bit.
+template <bool LOG, bool MIX>
+__device__ __forceinline__ void gate_of(const float g, float &a, float &in) {
+    a = LOG ? expf(g) : g;
+    in = 1.0f - a;
+    if (LOG && MIX) {
+        float s = fmaf(g, 1.0f / 362880.0f, 1.0f / 40320.0f);
+        s = fmaf(s, g, 1.0f / 5040.0f);
+        s = fmaf(s, g, 1.0f / 720.0f);
+        s = fmaf(s, g, 1.0f / 120.0f);
+        s = fmaf(s, g, 1.0f / 24.0f);
+        s = fmaf(s, g, 1.0f / 6.0f);
+        s = fmaf(s, g, 0.5f);
+        s = fmaf(s, g, 1.0f);
+        const bool small = fabsf(g) < 0.5f;
+        in = small ? -g * s : in;
+        a = small ? 1.0f - in : a;
+    }
+}
+
 using pos = int32_t;                     // rows and sequences: at most kMostRows of each, so that the end of a tile behind the last is one too
 constexpr int64_t kMostRows = 0x7fff0000;
 

@@ -8,27 +8,6 @@ namespace {
 
 using namespace cngp;
 
-// The gate of a row and how much of the input it lets in.  1 - exp(g) cancels for small g: there it is -g times the series of
-// (exp(g) - 1) / g to the ninth term (0.5^9 / 10! = 5e-10 below one), and exp(g) is one minus that, to the last bit.
-template <bool LOG, bool MIX>
-__device__ __forceinline__ void gate_of(const float g, float &a, float &in) {
-    a = LOG ? expf(g) : g;
-    in = 1.0f - a;
-    if (LOG && MIX) {
-        float s = fmaf(g, 1.0f / 362880.0f, 1.0f / 40320.0f);
-        s = fmaf(s, g, 1.0f / 5040.0f);
-        s = fmaf(s, g, 1.0f / 720.0f);
-        s = fmaf(s, g, 1.0f / 120.0f);
-        s = fmaf(s, g, 1.0f / 24.0f);
-        s = fmaf(s, g, 1.0f / 6.0f);
-        s = fmaf(s, g, 0.5f);
-        s = fmaf(s, g, 1.0f);
-        const bool small = fabsf(g) < 0.5f;
-        in = small ? -g * s : in;
-        a = small ? 1.0f - in : a;
-    }
-}
-
 // ---------------------------------------------------------------- the scan
 // A row is the map h -> a h + v, and maps compose: rows (A, B) then (a, v) give (a A, a B + v).  So a sequence need not be walked
 // row after row: a workgroup takes a tile of RL * RB rows by CL * V channels, every lane composes the maps of its RB consecutive
@@ -76,24 +55,6 @@ struct Window {
         return true;
     }
 };
-
-// V neighbouring values at once, on whatever boundary they start: global memory takes that, the compiler makes one access of it.
-template <typename T, int N>
-struct Run { T e[N]; };
-template <typename T, int V>
-__device__ __forceinline__ void load_vec(float (&out)[V], const T *p) {
-    Run<T, V> t;
-    __builtin_memcpy(&t, p, sizeof t);
-#pragma unroll
-    for (int v = 0; v < V; ++v) out[v] = load(t.e, v);
-}
-template <typename T, int V>
-__device__ __forceinline__ void store_vec(T *p, const float (&in)[V]) {
-    Run<T, V> t;
-#pragma unroll
-    for (int v = 0; v < V; ++v) store(t.e, v, in[v]);
-    __builtin_memcpy(p, &t, sizeof t);
-}
 
 // Where a tile's rows lie.  Row j of a lane is memory row low + mine + j, or low + mine - j taken backwards; `low` is the same for
 // the whole workgroup, so a load is a scalar base and a 32-bit lane offset.

@@ -220,3 +220,27 @@ def test_offsets_beyond_the_rows_are_taken_as_the_nearest():
     ref = R.forward(d["gate"].astype(np.float64), d["x"].astype(np.float64), spans, d["h0"].astype(np.float64), False, False, False)
     R.within("y", host(y), ref["y"], ref["Ey"])
     R.within("last", host(last), ref["last"], ref["El"])
+
+
+@pytest.mark.parametrize("C,shared", [(1, True), (2, True), (3, False), (5, True), (64, True), (257, False), (1024, True), (1031, True)])
+@pytest.mark.parametrize("flags", [0, REV, LOG, MIX, REV | LOG | MIX])
+@pytest.mark.parametrize("S,h0", [(1, True), (67, True), (342, False)])
+def test_one_row_each(C, shared, flags, S, h0):
+    check(C, shared, [1] * S, flags=flags, uniform=True, h0=h0)
+
+
+@pytest.mark.parametrize("io,gt", [(F16, F16), (F16, F32), (F32, F16)])
+@pytest.mark.parametrize("flags", [0, LOG | MIX])
+def test_one_row_each_types_and_in_place(io, gt, flags):
+    C, S = 37, 93
+    check(C, True, [1] * S, io, gt, flags, uniform=True)
+    check(C, False, [1] * S, io, gt, flags, uniform=True)
+    d = make(C, C, S, S, io, gt, flags, 5)
+    gate, x, h0 = dev(d["gate"]), dev(d["x"]), dev(d["h0"])
+    cfg = cngp.RecurConfig(C, C, io, gt, 0, flags)
+    y, last = cngp.recur_fwd(cfg, gate, x, h0=h0, sequences=S)
+    state = h0.clone()
+    none, same = cngp.recur_fwd(cfg, gate, x, h0=state, sequences=S, y=False, last=state)
+    assert none is None and same is state and torch.equal(state, last)
+    only, none = cngp.recur_fwd(cfg, gate, x, h0=h0, sequences=S, last=False)
+    assert none is None and torch.equal(only, y)

@@ -11,7 +11,10 @@ Choices the paper leaves open (stated, not claimed): D_f starts uniform in +-1e-
 encoding the method extends; D^_c starts uniform in +-1e-4 (every candidate nearly equally likely, the
 first bake picks an arbitrary one); the optimiser is Adam.
 """
+import functools
+
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import (Adam, Config, EmbedConfig, F32, I64, RECUR_LOG_GATE, RECUR_MIX, RECUR_REVERSE, RecurConfig, ZERO_GRADS, _TORCH_DT, F16,
                adam_step, adam_step_bake, alloc_workspace, bake_probes, embed_bwd, embed_fwd, encode_bwd, encode_bwd_input, encode_fwd,
@@ -90,13 +93,15 @@ class Encoding(torch.nn.Module):
 class _LookUp(torch.autograd.Function):
     @staticmethod
     def forward(ctx, base, hook, codes, ids):
-        ctx.codes, ctx.ids, ctx.has_base = codes, ids, base is not None
+        ctx.codes, ctx.has_base = codes, base is not None
+        ctx.save_for_backward(ids)
         return embed_fwd(codes.cfg, ids, codes.table, base=base)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         dy = dy.contiguous()
-        embed_bwd(ctx.codes.cfg, ctx.ids, dy, ctx.codes.grad_table)             # accumulates (+=)
+        embed_bwd(ctx.codes.cfg, *ctx.saved_tensors, dy, ctx.codes.grad_table)  # accumulates (+=)
         return (dy if ctx.has_base else None), None, None, None
 
 
@@ -116,7 +121,8 @@ class Codes(torch.nn.Module):
         self.steps = 0
 
     def forward(self, ids, base=None):
-        return _LookUp.apply(base, self._hook, self, ids)
+        # a leaf of its own for every call: one that an earlier graph holds would bind a captured backward to that graph's stream
+        return _LookUp.apply(base, self._hook.detach().requires_grad_(self._hook.requires_grad), self, ids)
 
     def step(self, opt: Adam):
         """Adam on the table (every entry: those that no id chose too); clears the gradient."""
@@ -133,13 +139,17 @@ class _Recur(torch.autograd.Function):
             rows = torch.arange(x.shape[0], device=x.device)
             y.masked_fill_(((rows < offsets[0]) | (rows >= offsets[-1]))[:, None], 0.0)
         ctx.cfg, ctx.sequences, ctx.keep = cfg, sequences, keep
+        ctx.set_materialize_grads(False)                                         # an output that the loss does not use costs no zeros
         ctx.save_for_backward(gate, x, h0, offsets, y)
         return (y, last) if keep else last
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, *grads):
         gate, x, h0, offsets, y = ctx.saved_tensors
         dy, dlast = grads if ctx.keep else (None, grads[0])
+        if dy is None and dlast is None:
+            return (None,) * 7
         dy = None if dy is None else dy.contiguous()
         dlast = None if dlast is None else dlast.contiguous()
         make = torch.empty_like if offsets is None else torch.zeros_like         # rows of no sequence have gradient 0
@@ -150,14 +160,25 @@ class _Recur(torch.autograd.Function):
 
 def recur(cfg: RecurConfig, gate, x, h0=None, offsets=None, sequences=None, keep=True):
     """The gated linear recurrence with gradients: (y, last), or last alone with keep=False (then the states are computed again by the
-    backward pass).  See cngp_recur_fwd."""
+    backward pass).  See cngp_recur_fwd.  As with any torch function, a backward pass is captured into a graph together with its forward, while no
+    eager graph of the same gate, x or h0 lives."""
     return _Recur.apply(gate, x, h0, cfg, offsets, sequences, keep)
+
+
+@functools.lru_cache(maxsize=64)
+def _composite_config(channels, colour, depth, longest):
+    code = {t: c for c, t in _TORCH_DT.items()}
+    for name, dtype in (("colour", colour), ("depth", depth)):
+        if dtype not in code:
+            raise TypeError(f"{name} must be float32 or float16, got {dtype}")
+    return RecurConfig(channels, 1, code[colour], code[depth], longest, RECUR_LOG_GATE | RECUR_MIX | RECUR_REVERSE)
 
 
 def composite(depth, colour, background=None, offsets=None, rays=None, longest=0):
     """Pixels [rays, C] float32 of rays whose samples lie one behind the other, nearest first: depth [N] are the samples' optical depths
     (density times step, >= 0), colour [N, C] what they emit, background [rays, C] float32 what lies behind (None: black).
     offsets int32 [rays + 1], or None for `rays` rays of equal length; longest: most samples of a ray, if known."""
-    code = {t: c for c, t in _TORCH_DT.items()}
-    cfg = RecurConfig(colour.shape[1], 1, code[colour.dtype], code[depth.dtype], longest, RECUR_LOG_GATE | RECUR_MIX | RECUR_REVERSE)
+    if depth.dim() != 1 or colour.dim() != 2:
+        raise ValueError(f"depth must be [N] and colour [N, C], got {tuple(depth.shape)} and {tuple(colour.shape)}")
+    cfg = _composite_config(colour.shape[1], colour.dtype, depth.dtype, longest)
     return recur(cfg, -depth[:, None], colour, background, offsets, rays, keep=False)

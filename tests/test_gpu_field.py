@@ -175,3 +175,84 @@ def test_decoded_samples_in_a_captured_step():
             assert torch.equal(kept[k], want[k]), k
         close("gF", kept["gF"], want["gF"], 1e-5)
         step()
+
+
+def test_codes_alone_twice_and_frozen():
+    """Without encodings, the same ids in two lookups of one iteration, no table gradient once frozen, ids changed in between refused."""
+    codes = Codes(5, 6, io_dtype=cngp.F16, id_dtype=cngp.I32, scale=2.0)
+    ids = torch.tensor([4, 0, 4, 7, -2, 4], dtype=torch.int32, device=DEV)
+    (codes(ids).sum() + codes(ids).sum()).backward()
+    want = torch.zeros(5, 6)
+    want[4], want[0] = 12.0, 4.0
+    assert torch.equal(codes.grad_table.cpu(), want)
+    y = codes(ids)
+    ids.fill_(1)
+    with pytest.raises(RuntimeError):
+        y.sum().backward()
+    assert torch.equal(codes.grad_table.cpu(), want)
+    codes.requires_grad_(False)
+    assert not codes(ids).requires_grad
+    base = torch.zeros(6, 6, dtype=torch.float16, device=DEV, requires_grad=True)
+    codes(ids, base).sum().backward()
+    assert bool((base.grad == 1).all())
+
+
+def test_a_captured_training_iteration_while_an_eager_one_of_the_codes_lives():
+    g = torch.Generator().manual_seed(4)
+    codes = Codes(9, 4, scale=0.5)
+    with torch.no_grad():
+        codes.table.copy_(torch.randn(9, 4, generator=g))
+    offsets = rays_of(g, 30, 20, 3)
+    N = int(offsets[-1])
+    ids, offsets, target = torch.randint(0, 9, (N,), generator=g).to(DEV), offsets.to(DEV), torch.rand(30, 3, generator=g).to(DEV)
+
+    def iteration():
+        codes.grad_table.zero_()
+        out = codes(ids)
+        pixels = composite(torch.nn.functional.softplus(out[:, 3]), torch.sigmoid(out[:, :3]).contiguous(), offsets=offsets, longest=20)
+        ((pixels - target) ** 2).sum().backward()
+        return pixels.detach()
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        iteration()
+    torch.cuda.current_stream().wait_stream(side)
+    want = iteration(), codes.grad_table.clone()
+    lives = codes(ids)                                               # its graph is alive while the other one is captured
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        pixels = iteration()
+    for _ in range(3):
+        codes.grad_table.fill_(9)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(pixels, want[0]) and torch.equal(codes.grad_table, want[1])
+        assert torch.equal(iteration(), want[0])
+    codes.grad_table.zero_()
+    lives.sum().backward()
+    assert bool((codes.grad_table.sum(1) > 0).any())
+
+
+def test_outputs_that_the_loss_leaves_out_and_refusals():
+    g = torch.Generator().manual_seed(6)
+    cfg = cngp.RecurConfig(3, 3)
+    gate, x = torch.rand(20, 3, generator=g).to(DEV), torch.randn(20, 3, generator=g).to(DEV).requires_grad_()
+    y, last = recur(cfg, gate, x, sequences=4)
+    last.sum().backward()
+    _, dx, _ = cngp.recur_bwd(cfg, gate, x.detach(), dlast=torch.ones(4, 3, device=DEV), y=y.detach(), sequences=4)
+    assert torch.equal(x.grad, dx)
+    y, last = recur(cfg, gate, x, sequences=4)
+    y.sum().backward()
+    _, dy_alone, _ = cngp.recur_bwd(cfg, gate, x.detach(), dy=torch.ones(20, 3, device=DEV), y=y.detach(), sequences=4)
+    assert torch.equal(x.grad, dx + dy_alone)
+    with pytest.raises(RuntimeError):                                # no second derivatives
+        torch.autograd.grad(torch.autograd.grad((recur(cfg, gate, x, sequences=4)[1] ** 2).sum(), x, create_graph=True)[0].sum(), x)
+    for depth, colour in ((torch.ones(6, 1), torch.ones(6, 3)), (torch.ones(6), torch.ones(6)), (torch.ones(5), torch.ones(6, 3)),
+                          (torch.ones(6), torch.ones(3, 6).t())):
+        with pytest.raises(ValueError):
+            composite(depth.to(DEV), colour.to(DEV), rays=2)
+    with pytest.raises(TypeError):
+        composite(torch.ones(6, device=DEV).double(), torch.ones(6, 3, device=DEV), rays=2)
+    with pytest.raises(TypeError):
+        composite(torch.ones(6), torch.ones(6, 3), rays=2)

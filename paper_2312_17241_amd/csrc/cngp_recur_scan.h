@@ -841,6 +841,7 @@ int launch_lanes(const RecurArgs &a, const RecurPlan &p, const Cut &cut, hipStre
 #undef CNGP_NARROW
     }
     if (p.block == kWideBlock) CNGP_RECUR(kWideBlock, 16, 2, (BWD ? 1 : 2) * kRowsEach);
+    if (p.CL == 8) CNGP_RECUR(kRecurBlock, 8, 1, kRowsEach);
     if (p.CL == 16) CNGP_RECUR(kRecurBlock, 16, 1, kRowsEach);
     if (p.V == 1) CNGP_RECUR(kRecurBlock, 32, 1, kRowsEach);
     CNGP_RECUR(kRecurBlock, 32, 2, kRowsEach);

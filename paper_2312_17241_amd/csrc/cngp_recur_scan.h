@@ -487,6 +487,31 @@ __global__ __launch_bounds__(BLOCK) void recur_scan_kernel(const RecurArgs a, co
     }
 }
 
+// The value of another lane of the wavefront by the lane permutations that instructions have (no trip through LDS): that of the lane CTRL names,
+// 0 where there is none.
+constexpr int kLaneBefore = 0x138, kRowEndBefore = 0x142, kLane31 = 0x143;       // lane - 1; lane 15 of the sixteen before; lane 31 for the upper half
+constexpr int lane_less(const int d) { return 0x110 + d; }                        // lane - d, inside the sixteen
+template <int CTRL>
+__device__ __forceinline__ float lane_value(const float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float last_lane_value(const float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+}
+// One step of the scan over a wavefront's maps: `ok` where the map of the lane CTRL names lies right before what this lane's covers.
+template <int CTRL, int GV, int V>
+__device__ __forceinline__ void take_in(float (&A)[GV], float (&B)[V], const bool ok) {
+    float Al[GV], Bl[V];
+#pragma unroll
+    for (int v = 0; v < GV; ++v) Al[v] = lane_value<CTRL>(A[v]);
+#pragma unroll
+    for (int v = 0; v < V; ++v) Bl[v] = lane_value<CTRL>(B[v]);
+#pragma unroll
+    for (int v = 0; v < V; ++v) B[v] = ok ? fmaf(A[GV == 1 ? 0 : v], Bl[v], B[v]) : B[v];
+#pragma unroll
+    for (int v = 0; v < GV; ++v) A[v] = ok ? A[v] * Al[v] : A[v];
+}
+
 // Rows of up to four channels: a lane holds RB whole rows, a workgroup is one wavefront, so nothing is joined through LDS and no barrier
 // waits.  What bounds such rows is not their bytes but the chain of loads: where the sequences start, what they start from, the rows.
 // All three are loaded a tile ahead; the start states of a tile's first 64 sequences go through LDS to the lanes whose rows start them.
@@ -669,32 +694,26 @@ __device__ __forceinline__ void narrow_rows(const RecurArgs &a, const Cut &cut, 
 #pragma unroll
             for (int v = 0; v < GV; ++v) A[v] *= g[j][v];
         }
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            float Al[GV], Bl[V];
-#pragma unroll
-            for (int v = 0; v < GV; ++v) Al[v] = __shfl_up(A[v], d, 64);
-#pragma unroll
-            for (int v = 0; v < V; ++v) Bl[v] = __shfl_up(B[v], d, 64);
-            if (lane >= d && since <= lane - d) {
-#pragma unroll
-                for (int v = 0; v < V; ++v) B[v] = fmaf(A[SHARED ? 0 : v], Bl[v], B[v]);
-#pragma unroll
-                for (int v = 0; v < GV; ++v) A[v] *= Al[v];
-            }
-        }
+        // sixteen lanes, then the sixteen before, then the lower half; a lane may take in `room` lanes, back to one where a sequence starts
+        const int room = lane - (since > 0 ? since : 0), inside = min(room, lane & 15);
+        take_in<lane_less(1), GV, V>(A, B, inside >= 1);
+        take_in<lane_less(2), GV, V>(A, B, inside >= 2);
+        take_in<lane_less(4), GV, V>(A, B, inside >= 4);
+        take_in<lane_less(8), GV, V>(A, B, inside >= 8);
+        take_in<kRowEndBefore, GV, V>(A, B, (lane & 16) && room > (lane & 15));
+        take_in<kLane31, GV, V>(A, B, (lane & 32) && room > (lane & 31));
         float h[V];
         const bool cut_before = (starts & ((1ull << lane) - 1ull)) != 0;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const float Ae = __shfl_up(A[SHARED ? 0 : v], 1, 64), Be = __shfl_up(B[v], 1, 64);
-            const float At = __shfl(A[SHARED ? 0 : v], 63, 64), Bt = __shfl(B[v], 63, 64);
+            const float Ae = lane_value<kLaneBefore>(A[SHARED ? 0 : v]), Be = lane_value<kLaneBefore>(B[v]);
+            const float At = last_lane_value(A[SHARED ? 0 : v]), Bt = last_lane_value(B[v]);
             h[v] = lane == 0 ? carry_b[v] : cut_before ? Be : fmaf(Ae, carry_b[v], Be);
             carry_b[v] = starts ? Bt : fmaf(At, carry_b[v], Bt);
         }
         if constexpr (PIECE) {
 #pragma unroll
-            for (int v = 0; v < GV; ++v) carry_a[v] *= __shfl(A[v], 63, 64);
+            for (int v = 0; v < GV; ++v) carry_a[v] *= last_lane_value(A[v]);
             now = next;
             continue;
         }

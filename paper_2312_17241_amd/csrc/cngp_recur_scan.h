@@ -27,19 +27,19 @@ struct Window {
     __device__ __forceinline__ bool find(const RecurArgs &a, const Cut &cut, const Order &o, const uint32_t k) {
         const pos     edge0 = (pos)k * cut.R, edge1 = k + 1 == cut.K ? a.N : edge0 + cut.R;
         const bool    final_window = k + 1 == cut.K;
-        o.first_from(edge0, edge1, qa, qb);
-        if (k == 0) qa = 0;
-        if (final_window || qb > a.S) qb = a.S;
+        pos from, to;
+        o.first_from(edge0, edge1, qa, qb, from, to);
+        if (k == 0 && qa > 0) { qa = 0; from = o.at(0); }
+        if (final_window || qb > a.S) { qb = a.S; to = o.at(a.S); }
         if (cut.exact) {
             const pos lo = o.at(0), hi = o.at(a.S);
             p0 = edge0 < lo ? lo : edge0;
             p1 = edge1 < hi && !final_window ? edge1 : hi;
             return true;
         }
-        if (qa >= qb) return false;                            // no sequence starts in here
-        p0 = o.at(qa);
-        p1 = o.at(qb);
-        return true;
+        p0 = from;
+        p1 = to;
+        return qa < qb;                                        // else no sequence starts in here
     }
     // The rows whose map the next window needs: those of the sequence that goes on in it.  False: none does, or it starts there.
     // q: that sequence if it starts in here, else -1.
@@ -518,7 +518,7 @@ __device__ __forceinline__ void take_in(float (&A)[GV], float (&B)[V], const boo
 // waits.  What bounds such rows is not their bytes but the chain of loads: where the sequences start, what they start from, the rows.
 // All three are loaded a tile ahead; the start states of a tile's first 64 sequences go through LDS to the lanes whose rows start them.
 // Lanes join by the instructions' lane permutations: with shuffles through LDS 4096 rays forward and backward took 32.2 us, so 29.2.  A frame of
-// 1920 x 1080 rays with 16.6 M samples takes 100 us for 323 MB: 510 vector instructions to a tile of 256 rows keep the vector ALU busy for half
+// 1920 x 1080 rays with 16.6 M samples takes 98 us for 323 MB: 510 vector instructions to a tile of 256 rows keep the vector ALU busy for half
 // of it, and wavefronts wait for loads 70 % of their time.
 template <typename Io, typename Gate, typename Y, int V, bool SHARED, bool MIX, bool BWD, bool PIECE>
 __device__ __forceinline__ void narrow_rows(const RecurArgs &a, const Cut &cut, const Order &o, Window win, const uint32_t k)

@@ -244,3 +244,23 @@ def test_one_row_each_types_and_in_place(io, gt, flags):
     assert none is None and same is state and torch.equal(state, last)
     only, none = cngp.recur_fwd(cfg, gate, x, h0=h0, sequences=S, last=False)
     assert none is None and torch.equal(only, y)
+
+
+def many(kind, S):
+    g = np.random.default_rng(S)
+    if kind == "even":                     # about as long as half a window's tile
+        return g.integers(50, 200, S)
+    if kind == "skewed":                   # nearly all rows in a few sequences, most sequences without any
+        n = np.where(g.random(S) < 0.02, g.integers(500, 1500, S), 0)
+        n[[0, S // 3]] = 1200
+        return n
+    n = np.zeros(S, np.int64)              # the rows at one end
+    n[-40:] = g.integers(1, 300, 40)
+    return n if kind == "late" else n[::-1]
+
+
+@pytest.mark.parametrize("kind", ["even", "skewed", "late", "early"])
+@pytest.mark.parametrize("C,shared,flags", [(3, True, REV | LOG | MIX), (4, False, 0), (7, True, LOG), (40, False, REV)])
+@pytest.mark.parametrize("longest", [0, 1500])
+def test_windows_of_many_sequences(kind, C, shared, flags, longest):
+    check(C, shared, many(kind, 330), flags=flags, keep=False, lead=5, trail=70, longest=longest)

@@ -397,8 +397,9 @@ int cngp_adam_step(const cngp_adam *opt, int64_t n, float *master, void *half_co
  * One token each for many running sequences is N == sequences with offsets NULL.
  * Backward, for L = sum(y * dy) + sum(last * dlast) (dy io_dtype [N, channels], dlast float32; either may be NULL, not both):
  *   dgate dev gate_dtype [N, gate_channels], dx dev io_dtype [N, channels], written; dh0 dev float32 [sequences, channels], written,
- *   or NULL; may be dlast itself.  y: the forward's states if they were kept; with NULL they are computed again, in fp32, into
- *   the workspace, and also where y is fp16 and the gates fp32, whose gradient the rounded states would not resolve.  Sums over channels are formed in a fixed order: the same call gives the same bits.
+ *   or NULL; may be dlast itself.  y: the forward's states, as written for this cfg, if they were kept.  The gates' gradient takes states in
+ *   32 bits: without y, and where y is fp16, they are computed again, into the workspace (with y and fp16 gates, what their rounding took
+ *   off, into dx before its gradients where that serves).  Sums over channels are formed in a fixed order: the same call gives the same bits.
  * `longest` (host): no sequence has more rows than this; 0: unknown.  It only decides how the work is cut.
  * Workspace: cngp_recur_workspace_bytes(cfg, N, sequences, call) bytes, 256-byte aligned (may be 0), for call = the sum of
  * CNGP_RECUR_CALL_*; undefined before and after.  Other arrays must not overlap. */

@@ -43,6 +43,23 @@ __device__ __forceinline__ void store_vec(T *p, const float (&in)[V]) {
     __builtin_memcpy(p, &t, sizeof t);
 }
 
+// A state in 32 bits as its rounding to fp16, which the caller keeps, and sixteen bits beside it: the lower half of |h| + 2^-15 in fp32.
+// Values with that lower half lie 2^16 steps of fp32 apart and the fp16 value is at most 2^12 steps away (below 2^-14, where steps of fp16
+// are 2^-24: of the 2^-38 that the sum's are), so the nearest one is meant, also where the fp16 value is a step off.  h comes back with two
+// roundings of fp32, or to 2^-39.  Where fp16 has infinity or no number, the sixteen bits are the upper half of h.
+struct LowHalf { uint16_t bits; };
+constexpr float kLowOffset = 0x1p-15f, kHalfOverflow = 65520.0f;      // what rounds to infinity in fp16
+__host__ __device__ __forceinline__ uint16_t low_half(const float h) {
+    const float m = fabsf(h);
+    return m < kHalfOverflow ? (uint16_t)__builtin_bit_cast(uint32_t, m + kLowOffset) : (uint16_t)(__builtin_bit_cast(uint32_t, h) >> 16);
+}
+__host__ __device__ __forceinline__ float with_low_half(const float rounded, const uint16_t low) {
+    const float    m = fabsf(rounded);
+    const uint32_t near = __builtin_bit_cast(uint32_t, m + kLowOffset), z = near + (uint32_t)(int32_t)(int16_t)(uint16_t)(low - (uint16_t)near);
+    return m < kHalfOverflow ? copysignf(__builtin_bit_cast(float, z) - kLowOffset, rounded) : __builtin_bit_cast(float, (uint32_t)low << 16);
+}
+__device__ __forceinline__ void store(LowHalf *p, const int64_t i, const float v) { p[i].bits = low_half(v); }
+
 // The gate of a row and how much of the input it lets in.  1 - exp(g) cancels for small g: there it is -g times the series of
 // (exp(g) - 1) / g to the ninth term (0.5^9 / 10! = 5e-10 below one), and exp(g) is one minus that, to the last bit.
 template <bool LOG, bool MIX>
@@ -71,15 +88,19 @@ struct RecurArgs {
     const void    *gate, *x;
     const int32_t *offsets;
     const float   *h0, *dlast;
-    const void    *y, *dy;               // backward; y_f32: y is the workspace's fp32 copy
+    const void    *y, *dy;               // backward; states: where those before the rows come from
     void          *out_y, *dgate, *dx;
     float         *last, *dh0;
     float         *slope;                // backward of a gate that several channel tiles share: their sums, fp32 [tiles][N]
     pos            N, S, rows_each;
     int32_t        C, G;
     uint32_t       flags;
-    int32_t        y_f32;
+    int32_t        states;               // STATES_*
 };
+
+// Where the backward pass has the states from, and what a forward launch writes as states: the caller's array y, in its type; the workspace,
+// in fp32; y in fp16 and the low halves in dx, until the gradients take their place.
+enum { STATES_Y = 0, STATES_F32, STATES_LOW };
 
 struct Order {
     const int32_t *offsets;

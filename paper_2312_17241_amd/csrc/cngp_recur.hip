@@ -187,9 +187,15 @@ RecurPlan plan_of(const cngp_recur_config *c, int64_t N, int64_t S, bool ragged)
     return p;
 }
 
-// Whether the backward pass reads the states that the caller kept: not where they are rounded to fp16 and the gradient of the gates,
-// which they are a factor of, is fp32.
-bool keeps_states(const cngp_recur_config *c, bool given) { return given && (c->io_dtype == CNGP_F32 || c->gate_dtype == CNGP_F16); }
+// Where the backward pass has the states from, a factor of the gates' gradient (less x, with mixed inputs: what rounding them to fp16 takes
+// off is relative to the states, not to that difference).  Kept ones serve as they are in fp32.  In fp16 a launch computes them again:
+// into the workspace; or, with fp16 gates, only what their rounding took off, into dx, whose rows are overwritten after they were read, so
+// that the call needs no workspace (8 sequences of 4096 rows of 1024: 162 us, 61 + 101; by the 134 MB workspace 160, 70 + 90).  Not so for rows that a
+// wavefront computes again by itself (up to four channels), nor for cut sequences, whose last row in a window has its state in the next one.
+int states_of(const cngp_recur_config *c, const RecurPlan &p, bool given) {
+    if (given && c->io_dtype == CNGP_F32) return STATES_Y;
+    return given && c->gate_dtype == CNGP_F16 && p.CL > 1 && !p.exact ? STATES_LOW : STATES_F32;
+}
 
 RecurSpace space_of(const cngp_recur_config *c, const RecurPlan &p, int64_t N, int64_t S, uint32_t call) {
     RecurSpace s{};
@@ -197,7 +203,7 @@ RecurSpace space_of(const cngp_recur_config *c, const RecurPlan &p, int64_t N, i
     auto take = [&](bool wanted, size_t bytes) { const size_t o = at; if (wanted) at += align256(bytes); return o; };
     const size_t C = (size_t)c->channels;
     const bool   bwd = call & CNGP_RECUR_CALL_BWD;
-    s.y = take(bwd && !keeps_states(c, !(call & CNGP_RECUR_CALL_NO_Y)), (size_t)N * C * 4);
+    s.y = take(bwd && states_of(c, p, !(call & CNGP_RECUR_CALL_NO_Y)) == STATES_F32, (size_t)N * C * 4);
     s.slope = take(bwd && c->gate_channels == 1 && p.tiles > 1, (size_t)N * (size_t)p.tiles * 4);
     s.piece_a = take(p.exact, p.K * C * 4);
     s.piece_b = take(p.exact, p.K * C * 4);
@@ -265,17 +271,16 @@ int cngp_recur_bwd(const cngp_recur_config *cfg, const void *gate, const void *x
     hipStream_t s = (hipStream_t)stream;
     if (N == 0) return pass_states(dlast, dh0, sequences * cfg->channels, s);
     const RecurPlan  p = plan_of(cfg, N, sequences, offsets != nullptr);
-    if (!keeps_states(cfg, y != nullptr)) y = nullptr;
     const uint32_t   call = CNGP_RECUR_CALL_BWD | (offsets ? CNGP_RECUR_CALL_RAGGED : 0) | (y ? 0 : CNGP_RECUR_CALL_NO_Y);
     const RecurSpace sp = space_of(cfg, p, N, sequences, call);
     char            *ws = (char *)workspace;
     if (sp.bytes && (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < sp.bytes)) return CNGP_ERR_WORKSPACE;
     RecurArgs a = args_of(cfg, gate, x, N, offsets, sequences, h0);
+    a.states = states_of(cfg, p, y != nullptr);
     a.y = y;
-    if (!y) {
-        a.out_y = ws + sp.y;
-        a.y_f32 = 1;
-        a.y = a.out_y;
+    if (a.states != STATES_Y) {
+        a.out_y = a.states == STATES_LOW ? dx : ws + sp.y;
+        if (a.states == STATES_F32) a.y = a.out_y;
         if (p.CL > 1 || p.exact) {                             // else the backward launch computes them (recur_narrow_again_kernel)
             if (int rc = recur_launch<false>(cfg, a, p, sp, ws, s)) return rc;
             a.out_y = nullptr;

@@ -151,13 +151,16 @@ __device__ __forceinline__ void gates_of(const bool log_gate, const R &raw, cons
 }
 
 // PIECE: only the composed map of the rows that the next window continues, for `carry`; else the outputs.
-// CL lanes side by side hold V channels each of a row, RB rows each.  Y: type of the states, written forward and read backward.
-// Bound by memory: 8 sequences of 4096 rows of 1024 in fp16, forward 61 us for 201 MB (rows in pieces of 64 bytes, so that 256 workgroups walk
-// whole sequences), backward 81 us for 335 MB.
+// CL lanes side by side hold V channels each of a row, RB rows each.  Y: type of the states, written forward and read backward; LowHalf:
+// the low halves alone, written to and read from dx, whose rows the workgroup that read them overwrites: those of a tile after the barrier
+// that follows their loads, the first of the next tile's with that tile.
+// Bound by memory: 8 sequences of 4096 rows of 1024 in fp16, forward 58 us for 201 MB (rows in pieces of 64 bytes, so that 256 workgroups walk
+// whole sequences), as much for the low halves, backward 101 us for 403 MB.
 template <typename Io, typename Gate, typename Y, int BLOCK, int CL, int V, int RB, bool SHARED, bool MIX, bool BWD, bool PIECE>
 __global__ __launch_bounds__(BLOCK) void recur_scan_kernel(const RecurArgs a, const Cut cut)
 {
     constexpr int  RL = BLOCK / CL, TR = RL * RB, W = BLOCK / 64, GV = SHARED ? 1 : V;
+    constexpr bool LOW = std::is_same_v<Y, LowHalf>;
     constexpr int  kFlagRows = 2048;                           // rows whose first / last marks are in LDS at a time
     static_assert(kFlagRows % TR == 0 && 32 % RB == 0, "a tile's marks lie in one block of them, a lane's in one word");
     __shared__ uint32_t bits_first[PIECE ? 1 : kFlagRows / 32], bits_last[PIECE ? 1 : kFlagRows / 32];
@@ -196,7 +199,8 @@ __global__ __launch_bounds__(BLOCK) void recur_scan_kernel(const RecurArgs a, co
     struct Tile {
         Rows<Gate, RB, GV, false> g;
         Rows<Io, RB, V, false>    in;
-        Rows<Y, (BWD && !PIECE ? RB : 1), V, false>         left;
+        Rows<LowHalf, (BWD && LOW && !PIECE ? RB : 1), V, false>                      low;
+        Rows<std::conditional_t<LOW, Io, Y>, (BWD && !PIECE ? RB : 1), V, false>     left;
         Rows<Io, (BWD && MIX && !PIECE ? RB : 1), V, false> x;
     };
     const auto place = [&](const pos pt) {
@@ -206,6 +210,9 @@ __global__ __launch_bounds__(BLOCK) void recur_scan_kernel(const RecurArgs a, co
         const pos pr = pt + rl * RB;
         const bool    whole = pt + TR <= p1;
         const Place   at = place(pt);
+        // the row behind the window is another workgroup's, and its state not used: these windows hold whole sequences
+        if constexpr (BWD && LOW && !PIECE)
+            f.low.load_from(a.dx, Place{at.low + dir, at.mine, dir}, a.C, c, pt + TR + 1 <= p1, a.N, pr + 1, p0, p1);
         f.g.load_from(a.gate, at, gw, gc, whole, a.N, pr, p0, p1);
         if (!BWD || a.dy) f.in.load_from(BWD ? a.dy : a.x, at, a.C, c, whole, a.N, pr, p0, p1);
         if constexpr (BWD && !PIECE) {
@@ -421,6 +428,7 @@ __global__ __launch_bounds__(BLOCK) void recur_scan_kernel(const RecurArgs a, co
                         in[j][v] = h[v];                       // now the output
                     } else if constexpr (!PIECE) {
                         float left = now.left.get(j, v, o.back);
+                        if constexpr (LOW) left = with_low_half(left, now.low.raw.e[j * V + v].bits);
                         if (with_edges && ((last >> j) & 1u)) left = a.h0 ? h_last[j][v] : 0.0f;
                         if constexpr (MIX) left -= now.x.get(j, v, o.back);
                         const float dh = from + in[j][v], da = dh * left;
@@ -853,10 +861,11 @@ int launch_narrow(const RecurArgs &a, const Cut &cut, hipStream_t s) {
 template <typename Io, typename Gate, typename Y, bool MIX, bool BWD>
 int launch_lanes(const RecurArgs &a, const RecurPlan &p, const Cut &cut, hipStream_t s) {
     const bool shared = a.G == 1;
+    constexpr bool low = std::is_same_v<Y, LowHalf>;           // rows of more than four channels (states_of)
 #define CNGP_RECUR(BLOCK, CL, V, RB)                                                      \
     return shared ? launch_scan<Io, Gate, Y, BLOCK, CL, V, RB, true, MIX, BWD>(a, p, cut, s) \
                   : launch_scan<Io, Gate, Y, BLOCK, CL, V, RB, false, MIX, BWD>(a, p, cut, s)
-    if (p.CL == 1) {
+    if constexpr (!low) if (p.CL == 1) {
 #define CNGP_NARROW(V) return shared ? launch_narrow<Io, Gate, Y, V, true, MIX, BWD>(a, cut, s) : launch_narrow<Io, Gate, Y, V, false, MIX, BWD>(a, cut, s)
         if (a.C == 1) return launch_narrow<Io, Gate, Y, 1, true, MIX, BWD>(a, cut, s);
         if (a.C == 2) CNGP_NARROW(2);
@@ -875,9 +884,17 @@ int launch_lanes(const RecurArgs &a, const RecurPlan &p, const Cut &cut, hipStre
 template <typename Io, typename Gate, bool BWD>
 int launch_inputs(const RecurArgs &a, const RecurPlan &p, const Cut &cut, hipStream_t s) {
     const bool mix = a.flags & CNGP_RECUR_MIX;
-    if constexpr (sizeof(Io) != sizeof(float))
-        if (a.y_f32) return mix ? launch_lanes<Io, Gate, float, true, BWD>(a, p, cut, s) : launch_lanes<Io, Gate, float, false, BWD>(a, p, cut, s);
-    return mix ? launch_lanes<Io, Gate, Io, true, BWD>(a, p, cut, s) : launch_lanes<Io, Gate, Io, false, BWD>(a, p, cut, s);
+    const auto launch = [&](auto y) {
+        using Y = decltype(y);
+        return mix ? launch_lanes<Io, Gate, Y, true, BWD>(a, p, cut, s) : launch_lanes<Io, Gate, Y, false, BWD>(a, p, cut, s);
+    };
+    if constexpr (sizeof(Io) != sizeof(float)) {
+        if constexpr (sizeof(Gate) != sizeof(float))
+            if (a.states == STATES_LOW) return launch(LowHalf{});
+        if constexpr (!BWD)
+            if (a.states == STATES_Y) return launch(Io{});     // the backward pass never has states in fp16
+    }
+    return launch(float{});
 }
 
 }  // namespace

@@ -154,8 +154,9 @@ def recur_fwd(cfg: RecurConfig, gate, x, h0=None, offsets=None, sequences=None, 
 
 def recur_bwd(cfg: RecurConfig, gate, x, dy=None, dlast=None, h0=None, y=None, offsets=None, sequences=None, dgate=True, dx=True, dh0=None,
               workspace=None):
-    """cngp_recur_bwd: (dgate, dx, dh0).  y: the forward's states if kept (else computed again).  dh0: as `last` of the forward; None gives
-    one where h0 is given.  Rows that belong to no sequence are left as they are in the gradients, undefined in new ones."""
+    """cngp_recur_bwd: (dgate, dx, dh0).  y: the forward's states if kept (else, and where they are fp16, computed again: the gates' gradient
+    takes states in 32 bits).  dh0: as `last` of the forward; None gives one where h0 is given.  Rows that belong to no sequence are left as
+    they are in the gradients, undefined in new ones."""
     N, C = x.shape
     S = _sequences(N, offsets, sequences)
     io, gt = _TORCH_DT[cfg.io_dtype], _TORCH_DT[cfg.gate_dtype]

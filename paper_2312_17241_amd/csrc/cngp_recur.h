@@ -113,17 +113,19 @@ struct Order {
         return back ? N - o : o;
     }
     __device__ __forceinline__ pos sequence(const pos q) const { return back ? S - 1 - q : q; }
-    // First q with ps(q) >= p (S + 1 if there is none) and its ps(q) (ps(S) then), for two p at once; a wavefront calls this together, 64 probes at
+    // Sequences of equal length: first q with ps(q) >= p (S + 1 if there is none) and its ps(q) (ps(S) then), 0 <= p <= N.
+    __host__ __device__ void equal_from(const pos p, pos &q, pos &v) const {
+        q = p / rows_each + (p % rows_each != 0);             // no sum: p + rows_each may pass 2^31
+        q = q < S + 1 ? q : S + 1;
+        v = (q < S ? q : S) * rows_each;
+    }
+    // The same for any sequences and two p at once; a wavefront calls this together, 64 probes at
     // a time.  The first ones lie around where sequences of equal length would have it: with lengths drawn at random that leaves a few
     // entries, and fewer dependent loads than from the ends (16.7 M rows of three channels in sequences of about 1023: 129 us and 121 so).
     __device__ void first_from(const pos pa, const pos pb, pos &qa, pos &qb, pos &va, pos &vb) const {
         if (!offsets) {
-            qa = (pa + rows_each - 1) / rows_each;
-            qb = (pb + rows_each - 1) / rows_each;
-            qa = qa < S + 1 ? qa : S + 1;
-            qb = qb < S + 1 ? qb : S + 1;
-            va = at(qa < S ? qa : S);
-            vb = at(qb < S ? qb : S);
+            equal_from(pa, qa, va);
+            equal_from(pb, qb, vb);
             return;
         }
         const pos lane = threadIdx.x & 63, want[2] = {pa, pb}, end = at(S);

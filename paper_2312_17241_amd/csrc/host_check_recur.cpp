@@ -1,5 +1,5 @@
 // Checks, on the host, of the recurrence's arithmetic that host and device share (cngp_recur.h): states as their rounding to fp16 and sixteen
-// bits beside it.  Nothing is launched.  Exit code 0 = all hold.
+// bits beside it, and where windows of rows fall among sequences of equal length.  Nothing is launched.  Exit code 0 = all hold.
 #include <cmath>
 #include <cstdint>
 #include <cstdio>
@@ -52,8 +52,32 @@ static void states_come_back() {
     expect(with_low_half(65504.0f, low_half(65519.996f)) == 65519.996f, "the largest that fp16 holds", 65519.996, with_low_half(65504.0f, low_half(65519.996f)));
 }
 
+// Where the windows' edges fall among sequences of equal length, against 64 bits, for counts of rows up to the most that a call may have.
+static void edges_of_equal_sequences() {
+    for (const int64_t most : {(int64_t)1000, (int64_t)1 << 30, (int64_t)1100000000, (int64_t)1500000000, (int64_t)1 << 31, kMostRows})
+        for (const int64_t S : {(int64_t)1, (int64_t)2, (int64_t)3, (int64_t)7, (int64_t)1000, (int64_t)123457, most < kMostRows ? most : kMostRows}) {
+            if (S > most) continue;
+            const int64_t each = (most < kMostRows ? most : kMostRows) / S, N = each * S;
+            const Order   o{nullptr, (pos)N, (pos)S, (pos)each, false};
+            const auto    check = [&](const int64_t p) {
+                if (p < 0 || p > N) return;
+                const int64_t q = (p + each - 1) / each;
+                pos           got = -7, at = -7;
+                o.equal_from((pos)p, got, at);
+                expect(got == q && at == q * each, "a window's edge", (double)p, (double)got);
+            };
+            for (int64_t k = 0; k <= 1024; ++k)
+                for (const int64_t d : {-1, 0, 1}) {
+                    check((N + 1023) / 1024 * k + d);      // edges of 1024 windows
+                    check(S / 1024 * k * each + d);        // around where sequences start
+                }
+            for (int64_t d = 0; d < 3; ++d) check(N - d);
+        }
+}
+
 int main() {
     states_come_back();
+    edges_of_equal_sequences();
     if (g_bad) { std::fprintf(stderr, "%d checks of the recurrence's arithmetic fail\n", g_bad); return 1; }
     std::printf("the recurrence's arithmetic holds\n");
     return 0;

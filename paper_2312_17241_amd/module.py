@@ -101,13 +101,14 @@ class _LookUp(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dy):
         dy = dy.contiguous()
-        embed_bwd(ctx.codes.cfg, *ctx.saved_tensors, dy, ctx.codes.grad_table)  # accumulates (+=)
+        if ctx.needs_input_grad[1]:                                              # frozen codes: the gradient of base alone
+            embed_bwd(ctx.codes.cfg, *ctx.saved_tensors, dy, ctx.codes.grad_table)  # accumulates (+=)
         return (dy if ctx.has_base else None), None, None, None
 
 
 class Codes(torch.nn.Module):
     """A code per image, object or token: y = codes(ids, base) = base + scale * table[ids], base the encodings [N, dim] (or None).
-    Ids outside the table are padding.  Call codes.step(opt) after backward()."""
+    Ids outside the table are padding.  Call codes.step(opt) after backward().  After codes.requires_grad_(False) the table collects no gradient."""
 
     def __init__(self, rows, dim, io_dtype=F32, id_dtype=I64, scale=1.0, device="cuda", seed=0):
         super().__init__()

@@ -628,18 +628,20 @@ int sum_columns(const SumArgs &a, hipStream_t s) {
 template <typename Id, typename Table, typename Io, int V>
 int look_up(const cngp_embed_config *c, const void *ids, int64_t N, const void *table, const void *base, void *y, hipStream_t s) {
     const uint32_t per_row = (uint32_t)((c->dim + V - 1) / V), rows_each = std::max(1u, (uint32_t)(kEmbBlock * kEmbAhead) / per_row);
-    const int64_t  blocks = (N + rows_each - 1) / rows_each;
-    if (blocks > 0x7fffffffLL) return CNGP_ERR_INVALID;
     // the smallest multiplier that divides every i below rows_each * per_row <= 1024 exactly (one point, or one value to a point, need none)
     const uint32_t inverse = (uint32_t)((0x100000000ull + per_row - 1) / per_row);      // not used for per_row = 1
     LaunchTimer t(s, K_EMBED_FWD);
     const auto launch = [&](auto kernel) {
-        kernel<<<(unsigned)blocks, kEmbBlock, 0, s>>>((const Id *)ids, (const Table *)table, (const Io *)base, (Io *)y, N, c->rows, c->dim, per_row, inverse,
-                                                      rows_each, c->scale);
+        const int64_t most = kMostGroups256 * rows_each;       // points of a launch: all of them below 2^24 rows of 8 KB and more
+        for (int64_t n = 0; n < N; n += most) {
+            const int64_t here = std::min(most, N - n), at = n * c->dim;
+            kernel<<<(unsigned)((here + rows_each - 1) / rows_each), kEmbBlock, 0, s>>>((const Id *)ids + n, (const Table *)table, base ? (const Io *)base + at : nullptr,
+                                                                                      (Io *)y + at, here, c->rows, c->dim, per_row, inverse, rows_each, c->scale);
+            if (int rc = launch_status("embed_fwd_kernel")) return rc;
+        }
+        return (int)CNGP_OK;
     };
-    if (c->dim % V == 0) launch(embed_fwd_kernel<Id, Table, Io, V, true>);
-    else launch(embed_fwd_kernel<Id, Table, Io, V, V == 1>);
-    return launch_status("embed_fwd_kernel");
+    return c->dim % V == 0 ? launch(embed_fwd_kernel<Id, Table, Io, V, true>) : launch(embed_fwd_kernel<Id, Table, Io, V, V == 1>);
 }
 template <typename Id, typename Table, typename Io>
 int look_up_columns(const cngp_embed_config *c, const void *ids, int64_t N, const void *table, const void *base, void *y, hipStream_t s) {

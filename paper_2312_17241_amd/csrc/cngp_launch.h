@@ -12,6 +12,9 @@ enum KernelId { K_FWD = 0, K_BWD_DIRECT, K_BWD_PREP, K_BWD_SLICED, K_BWD_SLICED_
                 K_BWD_BIN_OFFSETS, K_BWD_BIN_SCATTER, K_BWD_BIN_DRAIN, K_BWD_INPUT, K_FUSED_FWD, K_PLANES, K_FWD_ROWS, K_BWD_SMALL, K_BWD_CELLS, K_BWD_MERGE, K_BWD_PARTIAL,
                 K_RECUR_FWD, K_RECUR_BWD, K_RECUR_CARRY, K_EMBED_FWD, K_EMBED_SORT, K_EMBED_SUMS, K_BALANCE, K_COUNT };
 
+// A launch has less than 2^32 work-items: workgroups of 256 lanes that fit.
+constexpr int64_t kMostGroups256 = 0xffffff;
+
 int record_hip_failure(hipError_t e, const char *what);
 int launch_status(const char *what);              // of the launch just made
 int validate(const cngp_config *c);

@@ -57,8 +57,7 @@ __global__ __launch_bounds__(64) void recur_carry_kernel(const Cut cut, const in
 
 __global__ __launch_bounds__(kRecurBlock) void recur_copy_kernel(const float *__restrict__ from, float *__restrict__ to, const int64_t n)
 {
-    const int64_t i = (int64_t)blockIdx.x * kRecurBlock + threadIdx.x;
-    if (i < n) to[i] = from ? from[i] : 0.0f;
+    for (int64_t i = (int64_t)blockIdx.x * kRecurBlock + threadIdx.x; i < n; i += (int64_t)gridDim.x * kRecurBlock) to[i] = from ? from[i] : 0.0f;
 }
 
 // dgate of a gate that all channels share, from the sums of the channel tiles.
@@ -218,7 +217,7 @@ RecurSpace space_of(const cngp_recur_config *c, const RecurPlan &p, int64_t N, i
 
 int cngp::recur_copy(const float *from, float *to, int64_t n, hipStream_t s) {
     LaunchTimer t(s, K_RECUR_CARRY);
-    recur_copy_kernel<<<(unsigned)((n + kRecurBlock - 1) / kRecurBlock), kRecurBlock, 0, s>>>(from, to, n);
+    recur_copy_kernel<<<(unsigned)std::min<int64_t>((n + kRecurBlock - 1) / kRecurBlock, kMostGroups256), kRecurBlock, 0, s>>>(from, to, n);
     return launch_status("recur_copy_kernel");
 }
 
@@ -255,7 +254,7 @@ int cngp_recur_fwd(const cngp_recur_config *cfg, const void *gate, const void *x
     if (sp.bytes && (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < sp.bytes)) return CNGP_ERR_WORKSPACE;
     RecurArgs a = args_of(cfg, gate, x, N, offsets, sequences, h0);
     a.out_y = y; a.last = last;
-    if (!offsets && N == sequences && (N * cfg->channels + kStepEach - 1) / kStepEach <= 0x7fffffffLL) {
+    if (!offsets && N == sequences && (N * cfg->channels + kStepEach - 1) / kStepEach <= kMostGroups256) {      // 2^34 values; above by the scan
         const bool io16 = cfg->io_dtype == CNGP_F16, g16 = cfg->gate_dtype == CNGP_F16;
         return io16 ? (g16 ? step<__half, __half>(a, s) : step<__half, float>(a, s)) : (g16 ? step<float, __half>(a, s) : step<float, float>(a, s));
     }

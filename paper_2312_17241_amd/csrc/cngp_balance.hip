@@ -187,14 +187,14 @@ __device__ __forceinline__ void over_wavefront(float *p, const int lane) {
         over_wavefront<NP, 1, BIT * 2>(p, lane);
     }
 }
+// p: the sum over the wavefront that this lane ended up with.
 template <int NP, int W>
-__device__ __forceinline__ void over_workgroup(float (&p)[NP], const uint32_t (&n)[NP], float (&sum_p)[W][NP], uint32_t (&sum_n)[W][NP]) {
+__device__ __forceinline__ void over_workgroup(const float p, const uint32_t (&n)[NP], float (&sum_p)[W][NP], uint32_t (&sum_n)[W][NP]) {
     const int t = threadIdx.x, lane = t & 63, w = t >> 6;
-    over_wavefront<NP, NP, 1>(p, lane);
     int mine = 0;                                              // which of the sums this lane ended up with
 #pragma unroll
     for (int half = NP / 2, bit = 1; half; half >>= 1, bit <<= 1) mine += lane & bit ? half : 0;
-    if (lane < NP) sum_p[w][mine] = p[0];
+    if (lane < NP) sum_p[w][mine] = p;
 #pragma unroll
     for (int k = 0; k < NP; ++k)
         if (lane == k) sum_n[w][k] = n[k];
@@ -263,6 +263,10 @@ __device__ __forceinline__ void put_gradient(const BalArgs &a, const uint32_t le
 // A lane has a whole row here: nothing of the row is computed twice and its softmax needs no other lane.  With four lanes to a row of 16 the
 // sparse variant took 171 us at 16 x 2^18 x 16, with every entry of a lane's row ranked 133, with the network 106.  The next row is on its
 // way while one is worked on.
+// A lane adds 64 rows in fp32, then the wavefront's sum goes to one in fp64: equal weights that are no power of two round the same way row after
+// row, and 4096 rows of 1/5 one after the other in fp32 were 540 half steps off.
+template <int NP>
+constexpr uint32_t kHeldEvery = 64 / Group<NP>::R;                 // groups of a lane
 template <int NP, bool SPARSE>
 __global__ __launch_bounds__(kBalBlock) void balance_sums_kernel(const BalArgs a)
 {
@@ -276,17 +280,25 @@ __global__ __launch_bounds__(kBalBlock) void balance_sums_kernel(const BalArgs a
 #pragma unroll
     for (int k = 0; k < NP; ++k) { p[k] = 0.0f; n[k] = 0u; }
     Group<NP> g, next;
+    double held = 0.0;                                             // the wavefront's sums so far, one to a lane
     next.load(a, level, g0 + t, g0 + t < g1);
-    for (uint32_t base = g0; base < g1; base += kBalBlock) {       // whole wavefronts stay: they count by ballots
-        const uint32_t at = base + t;
-        uint32_t       kept = 0, won[Group<NP>::R];
-        g = next;
-        next.load(a, level, at + kBalBlock, at + kBalBlock < g1);  // under way while this one is worked on
-        weigh<NP, SPARSE, true>(g, a.top_k, kept, won);
-        if (SPARSE && a.grad && at < g1) a.kept[(size_t)level * a.groups + at] = (uint16_t)kept;
-        add_up<NP>(g, won, p, n);
+    for (uint32_t base = g0; base < g1;) {
+        const uint32_t until = g1 - base > kHeldEvery<NP> * kBalBlock ? base + kHeldEvery<NP> * kBalBlock : g1;
+        for (; base < until; base += kBalBlock) {                  // whole wavefronts stay: they count by ballots
+            const uint32_t at = base + t;
+            uint32_t       kept = 0, won[Group<NP>::R];
+            g = next;
+            next.load(a, level, at + kBalBlock, at + kBalBlock < g1);      // under way while this one is worked on
+            weigh<NP, SPARSE, true>(g, a.top_k, kept, won);
+            if (SPARSE && a.grad && at < g1) a.kept[(size_t)level * a.groups + at] = (uint16_t)kept;
+            add_up<NP>(g, won, p, n);
+        }
+        over_wavefront<NP, NP, 1>(p, (int)t & 63);
+        held += (double)p[0];
+#pragma unroll
+        for (int k = 0; k < NP; ++k) p[k] = 0.0f;
     }
-    over_workgroup<NP, W>(p, n, sum_p, sum_n);
+    over_workgroup<NP, W>((float)held, n, sum_p, sum_n);
     if (t < NP) {
         const size_t o = ((size_t)level * a.chunks + blockIdx.x) * NP + t;
         a.part_p[o] = sum_p[0][t];
@@ -430,7 +442,8 @@ __global__ __launch_bounds__(kLevelBlock) void balance_level_kernel(const BalArg
         weigh<NP, SPARSE, true>(g[i], a.top_k, kept, won);
         add_up<NP>(g[i], won, p, n);
     }
-    over_workgroup<NP, W>(p, n, sum_p, sum_n);
+    over_wavefront<NP, NP, 1>(p, (int)t & 63);
+    over_workgroup<NP, W>(p[0], n, sum_p, sum_n);
     if (t < 64) {
         const float w = level_shares<NP>(a, level, sum_p[0], sum_n[0], true);
         if (t == 0) scale = w;

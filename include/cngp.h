@@ -400,7 +400,9 @@ int cngp_adam_step(const cngp_adam *opt, int64_t n, float *master, void *half_co
  *   or NULL; may be dlast itself.  y: the forward's states, as written for this cfg, if they were kept.  The gates' gradient takes states in
  *   32 bits: without y, and where y is fp16, they are computed again, into the workspace (with y and fp16 gates, what their rounding took
  *   off, into dx before its gradients where that serves).  Sums over channels are formed in a fixed order: the same call gives the same bits.
- * `longest` (host): no sequence has more rows than this; 0: unknown.  It only decides how the work is cut.
+ * `longest` (host): no sequence has more rows than this; 0: unknown.  It only decides how the work is cut: with offsets and 0, no sequence is
+ * taken to be longer than four times the mean, and a much longer one is walked by a workgroup alone.  Batches of very unequal lengths
+ * should give it (4096 sequences of 64 rows of three channels but for one of 2^20: 7.9 ms, with `longest` 28 us; backward 18.6 ms and 68 us).
  * Workspace: cngp_recur_workspace_bytes(cfg, N, sequences, call) bytes, 256-byte aligned (may be 0), for call = the sum of
  * CNGP_RECUR_CALL_*; undefined before and after.  Other arrays must not overlap. */
 enum { CNGP_RECUR_REVERSE = 1u, CNGP_RECUR_LOG_GATE = 2u, CNGP_RECUR_MIX = 4u };

@@ -159,6 +159,8 @@ RecurPlan plan_of(const cngp_recur_config *c, int64_t N, int64_t S, bool ragged)
     p.tiles = (C + p.CL * p.V - 1) / (p.CL * p.V);
     const int64_t tile_rows = p.CL == 1 ? kNarrowBlock * kRowsNarrow : p.block / p.CL * kRowsEach;
     const int64_t mean = S ? (N + S - 1) / S : 0;
+    // Ragged ones are of unknown length here (the offsets lie on the device).  Cutting wherever one might be long costs ordinary batches two
+    // launches; a single long sequence among short ones that is not known of costs 280 times what it takes cut (2^20 rows of three channels).
     const int64_t longest = !ragged ? mean : c->longest ? std::min<int64_t>(c->longest, N) : 4 * mean;
     // windows that give every CU eight workgroups, of whole tiles; single wavefronts four times as many (a frame of 1920 x 1080 rays with 8192 of
     // them 102.6 us, 4096 114, 16384 105)

@@ -178,7 +178,8 @@ def _composite_config(channels, colour, depth, longest):
 def composite(depth, colour, background=None, offsets=None, rays=None, longest=0):
     """Pixels [rays, C] float32 of rays whose samples lie one behind the other, nearest first: depth [N] are the samples' optical depths
     (density times step, >= 0), colour [N, C] what they emit, background [rays, C] float32 what lies behind (None: black).
-    offsets int32 [rays + 1], or None for `rays` rays of equal length; longest: most samples of a ray, if known."""
+    offsets int32 [rays + 1], or None for `rays` rays of equal length; longest: most samples of a ray, to be given where a few rays may have
+    very many (without it a ray of 2^20 samples among 4095 of 64 takes 8 ms in place of 30 us)."""
     if depth.dim() != 1 or colour.dim() != 2:
         raise ValueError(f"depth must be [N] and colour [N, C], got {tuple(depth.shape)} and {tuple(colour.shape)}")
     cfg = _composite_config(colour.shape[1], colour.dtype, depth.dtype, longest)

@@ -51,7 +51,7 @@ class RecurConfig(_Marshalled):
     gate_channels: int
     io_dtype: int = 0
     gate_dtype: int = 0
-    longest: int = 0          # no sequence has more rows; 0 = unknown
+    longest: int = 0          # no sequence has more rows; 0 = unknown: one far longer than four times the mean is then walked alone, and slowly
     flags: int = 0            # RECUR_REVERSE | RECUR_LOG_GATE | RECUR_MIX
 
     def c(self):

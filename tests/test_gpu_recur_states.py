@@ -117,3 +117,48 @@ def test_states_beyond_fp16_and_not_finite_ones():
     keep = torch.ones(47, C, dtype=torch.bool, device=DEV)
     keep[13:40, 5] = False
     assert torch.equal(bad[0][keep], good[0][keep]) and bool(torch.isnan(bad[0][13:40, 5]).all()) and torch.equal(bad[1], good[1])
+
+
+@pytest.mark.parametrize("C,shared,lengths", [(64, False, [900] * 192), (12, True, [40, 0, 700, 3]), (3, True, [40, 0, 700, 3]), (40, False, [9000, 3])])
+def test_graph_replays_and_another_stream(C, shared, lengths):
+    G, S, N = 1 if shared else C, len(lengths), sum(lengths)
+    gate, x, h0, dy, dlast = (dev(a) for a in inputs(C, G, N, S, 0, 4))
+    off = None if len(set(lengths)) == 1 else dev(np.concatenate([[0], np.cumsum(lengths)]).astype(np.int32))
+    cfg = cngp.RecurConfig(C, G, F16, F16)
+    y, dgate, dx, dh0 = torch.empty_like(x), torch.empty_like(gate), torch.empty_like(x), torch.empty_like(h0)
+    last, size = torch.empty_like(h0), max(cngp.recur_workspace_bytes(cfg, N, S, b, off is not None, True) for b in (False, True))
+    ws = torch.empty(max(size, 256), dtype=torch.uint8, device=DEV)
+
+    def step():
+        cngp.recur_fwd(cfg, gate, x, h0=h0, offsets=off, sequences=S, y=y, last=last, workspace=ws)
+        cngp.recur_bwd(cfg, gate, x, dy=dy, dlast=dlast, h0=h0, y=y, offsets=off, sequences=S, dgate=dgate, dx=dx, dh0=dh0, workspace=ws)
+
+    outs = [y, last, dgate, dx, dh0]
+    step()
+    want = [o.clone() for o in outs]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for o in outs:
+            o.fill_(float("nan"))
+        ws.fill_(255)
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(o, w) for o, w in zip(outs, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(3):
+        for o in outs:
+            o.fill_(float("nan"))
+        ws.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, w) for o, w in zip(outs, want))
+        step()
+
+
+@pytest.mark.parametrize("C,shared", [(3, True), (24, False)])
+def test_cut_sequences_far_behind_rows_of_no_sequence(C, shared):
+    check(C, shared, [20000, 0, 7, 9000], REV | LOG | MIX, lead=12000)
+    check(C, shared, [20000, 0, 7, 9000], 0, lead=12000)

@@ -399,7 +399,7 @@ int cngp_adam_step(const cngp_adam *opt, int64_t n, float *master, void *half_co
  *   dgate dev gate_dtype [N, gate_channels], dx dev io_dtype [N, channels], written; dh0 dev float32 [sequences, channels], written,
  *   or NULL; may be dlast itself.  y: the forward's states, as written for this cfg, if they were kept.  The gates' gradient takes states in
  *   32 bits: without y, and where y is fp16, they are computed again, into the workspace (with y and fp16 gates, what their rounding took
- *   off, into dx before its gradients where that serves).  Sums over channels are formed in a fixed order: the same call gives the same bits.
+ *   off, into dx before its gradients where that serves; states above 65504, infinite in y, then have eight bits).  Sums over channels are formed in a fixed order: the same call gives the same bits.
  * `longest` (host): no sequence has more rows than this; 0: unknown.  It only decides how the work is cut: with offsets and 0, no sequence is
  * taken to be longer than four times the mean, and a much longer one is walked by a workgroup alone.  Batches of very unequal lengths
  * should give it (4096 sequences of 64 rows of three channels but for one of 2^20: 7.9 ms, with `longest` 28 us; backward 18.6 ms and 68 us).
@@ -459,7 +459,8 @@ int cngp_embed_bwd(const cngp_embed_config *cfg, const void *ids, int64_t N, con
  *   Dhat_c dev float32 [L, N_c, N_p]       rows dev uint8 [L, N_c], 0 = not counted, whatever the row holds; or NULL: all are
  *   loss   dev float32 [L], written        counts dev int32 [L, N_p], written
  *   grad_Dhat_c dev float32 [L, N_c, N_p], accumulated, or written with CNGP_ZERO_GRADS (0 in rows that are not counted); or NULL
- *   weight finite, host.  Sums are formed in a fixed order.
+ *   weight finite, host.  Sums are formed in a fixed order.  N_c * N_p below 2^34.  A counted row without a finite largest logit has no
+ *   finite weights, here as in the backward pass, and its level's loss is then not finite.
  *   workspace dev, 256-byte aligned, cngp_probe_balance_workspace_bytes(cfg) bytes; undefined before and after */
 size_t cngp_probe_balance_workspace_bytes(const cngp_config *cfg);
 int cngp_probe_balance(const cngp_config *cfg, const float *Dhat_c, const uint8_t *rows, float weight, float *loss, int32_t *counts,

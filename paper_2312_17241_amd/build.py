@@ -75,12 +75,12 @@ def build_host_sanitized() -> str:
 
 
 def build_host_recur() -> str:
-    """The recurrence's arithmetic that host and device share (csrc/cngp_recur.h) with its checks csrc/host_check_recur.cpp, for the host alone.
+    """The recurrence's arithmetic that host and device share (csrc/cngp_recur.h) with its checks csrc/host_check_recur_main.cpp, for the host alone.
     The result lives in the git-ignored _build/ folder and is rebuilt when a source is newer.  tests/test_recur_host.py runs it."""
     out_dir = os.path.join(os.path.dirname(HERE), "_build")
     os.makedirs(out_dir, exist_ok=True)
     exe = os.path.join(out_dir, "cngp_host_check_recur")
-    srcs = [os.path.join(CSRC, "host_check_recur.cpp")] + [os.path.join(CSRC, f) for f in ("cngp_recur.h", "cngp_launch.h")]
+    srcs = [os.path.join(CSRC, "host_check_recur_main.cpp")] + [os.path.join(CSRC, f) for f in ("cngp_recur.h", "cngp_launch.h")]
     if os.path.exists(exe) and os.path.getmtime(exe) >= max(os.path.getmtime(f) for f in srcs):
         return exe
     res = subprocess.run([os.environ.get("HIPCC", "/opt/rocm/bin/hipcc"), "-x", "hip", "--offload-host-only", "-O2", "-std=c++17", "-Wall",

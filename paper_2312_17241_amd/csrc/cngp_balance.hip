@@ -4,7 +4,7 @@
 //     d loss / d logit_rk = N_p / W * sigma_rk (f_k - sum_j f_j sigma_rj)
 // The gradient of every row needs the level's f, so two launches: one reads the logits and leaves sums per workgroup, the other
 // adds those up (in a fixed order), reads the logits again and writes the gradient.  A level that one workgroup can hold in registers
-// takes one launch.  16 levels x 2^18 rows x 16 logits, the four largest kept: 182 us, 106 + 96 where each launch is profiled by itself; reading
+// takes one launch.  16 levels x 2^18 rows x 16 logits, the four largest kept: 181 us, 105 + 96 where each launch is profiled by itself; reading
 // 268 MB twice and writing it once is 805 MB, 113 us at the rates of a large read and a large fill.  The first launch is bound by the vector
 // ALU (the ranks), the second by memory.
 #include <algorithm>
@@ -261,7 +261,7 @@ __device__ __forceinline__ void put_gradient(const BalArgs &a, const uint32_t le
 }
 
 // A lane has a whole row here: nothing of the row is computed twice and its softmax needs no other lane.  With four lanes to a row of 16 the
-// sparse variant took 171 us at 16 x 2^18 x 16, with every entry of a lane's row ranked 133, with the network 106.  The next row is on its
+// sparse variant took 171 us at 16 x 2^18 x 16, with every entry of a lane's row ranked 133, with the network 105.  The next row is on its
 // way while one is worked on.
 // A lane adds 64 rows in fp32, then the wavefront's sum goes to one in fp64: equal weights that are no power of two round the same way row after
 // row, and 4096 rows of 1/5 one after the other in fp32 were 540 half steps off.

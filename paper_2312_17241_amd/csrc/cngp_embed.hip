@@ -632,7 +632,7 @@ int look_up(const cngp_embed_config *c, const void *ids, int64_t N, const void *
     const uint32_t inverse = (uint32_t)((0x100000000ull + per_row - 1) / per_row);      // not used for per_row = 1
     LaunchTimer t(s, K_EMBED_FWD);
     const auto launch = [&](auto kernel) {
-        const int64_t most = kMostGroups256 * rows_each;       // points of a launch: all of them below 2^24 rows of 8 KB and more
+        const int64_t most = kMostGroups256 * rows_each;       // points of a launch: more than there are, but for 2^24 rows and more of at least 513 vectors
         for (int64_t n = 0; n < N; n += most) {
             const int64_t here = std::min(most, N - n), at = n * c->dim;
             kernel<<<(unsigned)((here + rows_each - 1) / rows_each), kEmbBlock, 0, s>>>((const Id *)ids + n, (const Table *)table, base ? (const Io *)base + at : nullptr,

@@ -154,8 +154,8 @@ __device__ __forceinline__ void gates_of(const bool log_gate, const R &raw, cons
 // CL lanes side by side hold V channels each of a row, RB rows each.  Y: type of the states, written forward and read backward; LowHalf:
 // the low halves alone, written to and read from dx, whose rows the workgroup that read them overwrites: those of a tile after the barrier
 // that follows their loads, the first of the next tile's with that tile.
-// Bound by memory: 8 sequences of 4096 rows of 1024 in fp16, forward 58 us for 201 MB (rows in pieces of 64 bytes, so that 256 workgroups walk
-// whole sequences), as much for the low halves, backward 101 us for 403 MB.
+// Bound by memory: 8 sequences of 4096 rows of 1024 in fp16, forward 62 us for 201 MB (rows in pieces of 64 bytes, so that 256 workgroups walk
+// whole sequences), the low halves right behind it 47, backward 106 us for 403 MB.
 template <typename Io, typename Gate, typename Y, int BLOCK, int CL, int V, int RB, bool SHARED, bool MIX, bool BWD, bool PIECE>
 __global__ __launch_bounds__(BLOCK) void recur_scan_kernel(const RecurArgs a, const Cut cut)
 {

@@ -1,9 +1,9 @@
 """The gates' gradient of the recurrence in fp16 is a product with the states in 32 bits, not with those that the caller kept in fp16.
 
 Tolerances: those of recur_ref.py without a rounding of the states.  Where the kernel completes the kept states by what their rounding took
-off, a state is off by two more roundings of fp32 (inside the eight that the bound counts per row) and 2^-39: with the incoming gradients
-below 2^12 and at most 130 channels to a sum that is below 2^-19 times the smallest of these states' gradients that fp16 resolves, so it
-is written beside the bound only where the states are small."""
+off, a state is off by two more roundings of fp32 (inside the eight that the bound counts per row) and 2^-39.  With gradients of the states
+below 64 and at most 130 channels to a sum that adds 2^-26, half of the half step of the smallest fp16 number that every comparison
+allows; it is written beside the bound where gradients are larger."""
 import numpy as np
 import pytest
 import torch

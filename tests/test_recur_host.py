@@ -1,4 +1,4 @@
-"""The recurrence's arithmetic that host and device share, checked on the host (csrc/host_check_recur.cpp)."""
+"""The recurrence's arithmetic that host and device share, checked on the host (csrc/host_check_recur_main.cpp)."""
 import subprocess
 
 from paper_2312_17241_amd import build

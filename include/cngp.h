@@ -423,6 +423,94 @@ int cngp_recur_bwd(const cngp_recur_config *cfg, const void *gate, const void *x
                    const float *h0, const void *y, const void *dy, const float *dlast, void *dgate, void *dx, float *dh0,
                    void *workspace, size_t workspace_bytes, void *stream);
 
+/* Linear attention with a decay for each head, forward and backward: the samples of a ray, the patches of an image or the tokens of a text take
+ * from the rows before them by content.  Each head keeps a state S [key_dim, value_dim] over the rows of its sequence:
+ *     S_t = exp(g_t) S_{t-1} + k_t v_t^T            y_t = scale * S_t^T q_t            g_t the log decay of the head, <= 0
+ * The state before a sequence's first row is h0, or 0.  Query head h reads the keys and values of head h / (heads / kv_heads).
+ *   q dev io_dtype [N, heads, key_dim]      k dev io_dtype [N, kv_heads, key_dim]      v dev io_dtype [N, kv_heads, value_dim]
+ *   decay dev float32 [heads], or [N, heads] with CNGP_ATTEND_ROW_DECAY; -infinity forgets everything
+ *   h0    dev float32 [sequences, heads, key_dim, value_dim], or NULL (zeros)
+ *   y     dev io_dtype [N, heads, value_dim], written; or NULL (then q may be NULL unless every sequence has one row and heads share keys)
+ *   last  dev float32 like h0, the state behind the last row, written; or NULL; may be h0 itself
+ *   heads 1 .. 4096, a multiple of kv_heads      key_dim, value_dim 1 .. 128      N, sequences at most 2^31 - 2^16      scale finite
+ * Sequences, offsets and `longest` as in cngp_recur_fwd; rows of no sequence are neither used nor written.  N == sequences with offsets NULL
+ * is one new token for each running sequence and has a kernel of its own.
+ * States and sums in fp32, decays joined in 64 bits; products of computed values take two fp16 numbers each with fp16 storage (22 bits),
+ * so that the result has its one rounding to io_dtype and little else.  |scale * v| (backward: |scale * dy|, |scale * q|) has to stay within fp16
+ * where io_dtype is.  Decays above 0 work while the products of a sequence's factors stay within fp32.  A row that is not finite spoils its
+ * sequence's later rows, and those of its 64-row piece before it (counted from the sequence's start), in the heads that read it.
+ * Backward, for L = sum(y * dy) + sum(last * dlast) (either may be NULL, not both): dq, dk, dv io_dtype, written; ddecay float32 like decay, written,
+ * or NULL (with one decay per head: the sum over all rows); dh0 float32 like h0, written, or NULL; it must not be dlast.  Sums are formed in
+ * a fixed order: the same call gives the same bits.
+ * Workspace: cngp_attend_workspace_bytes(cfg, N, sequences, call) bytes, 256-byte aligned (may be 0), for call = the sum of
+ * CNGP_ATTEND_CALL_*; undefined before and after.  Other arrays must not overlap. */
+enum { CNGP_ATTEND_ROW_DECAY = 1u };
+enum { CNGP_ATTEND_CALL_BWD = 1u,     /* cngp_attend_bwd, else cngp_attend_fwd */
+       CNGP_ATTEND_CALL_RAGGED = 2u };/* offsets are given                     */
+typedef struct cngp_attend_config {
+    int32_t  heads, kv_heads, key_dim, value_dim;
+    int32_t  io_dtype;        /* cngp_dtype of q, k, v, y and their gradients */
+    int32_t  longest;         /* no sequence has more rows than this; 0: unknown */
+    float    scale;
+    uint32_t flags;           /* CNGP_ATTEND_ROW_DECAY */
+} cngp_attend_config;
+size_t cngp_attend_workspace_bytes(const cngp_attend_config *cfg, int64_t N, int64_t sequences, uint32_t call);
+int cngp_attend_fwd(const cngp_attend_config *cfg, const void *q, const void *k, const void *v, const float *decay, int64_t N, const int32_t *offsets,
+                    int64_t sequences, const float *h0, void *y, float *last, void *workspace, size_t workspace_bytes, void *stream);
+int cngp_attend_bwd(const cngp_attend_config *cfg, const void *q, const void *k, const void *v, const float *decay, int64_t N, const int32_t *offsets,
+                    int64_t sequences, const float *h0, const void *dy, const float *dlast, void *dq, void *dk, void *dv, float *ddecay, float *dh0,
+                    void *workspace, size_t workspace_bytes, void *stream);
+
+/* Norms of queries and keys for each head and the rotation by their positions, in one pass, with the gradient: what attention over points, patches or
+ * tokens is given.  For every row n and head, x its `dim` components:
+ *     u = gamma * x / sqrt(mean(x^2) + eps) with CNGP_ROTATE_NORM (gamma NULL: ones), else x
+ *     pair p of u's components turned by the angle position[n][axis of p] * omega[p]; components behind the pairs pass as they are
+ * Axis a turns pairs[a] pairs, axis after axis (one for texts, rows and columns of images, time besides for videos, coordinates of points).
+ * Pair p holds components p and p + the number of pairs, or 2p and 2p + 1 with CNGP_ROTATE_NEXT.  Angles are formed in 64 bits
+ * from the fp32 numbers, whole turns taken off there: far positions turn as exactly as near ones.  Everything else in fp32, one rounding.
+ *   q dev io_dtype [N, heads, dim]     k dev io_dtype [N, kv_heads, dim]; either number of heads may be 0, its arrays are then ignored
+ *   position dev float32 [N, axes]     omega dev float32 [sum of pairs]; NULL without pairs
+ *   gamma_q, gamma_k dev float32 [dim], or NULL
+ *   q_out, k_out like q, k, written; each may be its input itself
+ * Backward for L = sum(q_out * dq_out) + sum(k_out * dk_out): dq, dk like q, k, written, each may be dq_out, dk_out itself; dgamma_q, dgamma_k dev
+ * float32 [dim], accumulated (+=) or written with CNGP_ZERO_GRADS (then also where N is 0), or NULL; summed in a fixed order.  q and k are
+ * the forward's inputs, used with CNGP_ROTATE_NORM only.  Positions and omega are constants.
+ *   dim 1 .. 512     heads, kv_heads 0 .. 4096     axes 1 .. 4     eps >= 0     N at most 2^31 - 2^16
+ *   workspace (gradients of gains only) dev, 256-byte aligned, cngp_rotate_workspace_bytes(cfg, N) bytes; undefined before and after */
+enum { CNGP_ROTATE_NORM = 2u, CNGP_ROTATE_NEXT = 4u };      /* beside CNGP_ZERO_GRADS = 1 */
+typedef struct cngp_rotate_config {
+    int32_t  heads, kv_heads, dim;
+    int32_t  axes, pairs[4];
+    int32_t  io_dtype;        /* cngp_dtype */
+    float    eps;
+    uint32_t flags;
+} cngp_rotate_config;
+int cngp_rotate_fwd(const cngp_rotate_config *cfg, const void *q, const void *k, int64_t N, const float *position, const float *omega, const float *gamma_q,
+                    const float *gamma_k, void *q_out, void *k_out, void *stream);
+size_t cngp_rotate_workspace_bytes(const cngp_rotate_config *cfg, int64_t N);
+int cngp_rotate_bwd(const cngp_rotate_config *cfg, const void *q, const void *k, int64_t N, const float *position, const float *omega, const float *gamma_q,
+                    const float *gamma_k, const void *dq_out, const void *dk_out, void *dq, void *dk, float *dgamma_q, float *dgamma_k, void *workspace,
+                    size_t workspace_bytes, void *stream);
+
+/* Orthogonalised update of matrices: X with the singular vectors of G and singular values near 1, by `steps` products of a polynomial
+ *     X = G / (|G|_F + eps);    each step:  A = X X^T,   X <- a X + (b A + c A A) X          (of the transposed matrix where rows > cols)
+ * with the same three coefficients in every step (3.4445, -4.7750, 2.0315 bring singular values above a thousandth of the norm
+ * into 0.7 .. 1.2 in five steps; 1.5, -0.5, 0 converge to 1 slowly).  The products run on the matrix cores, every operand as two fp16 numbers (22 bits), sums in fp32;
+ * the norm in 64 bits.  A matrix of zeros gives zeros; one with a value that is not finite gives values that are not finite.
+ * Not part of the paper's method: an optimiser step for the matrices around the encoding, where cngp_adam_step takes arrays entry by entry.
+ *   g dev io_dtype [batch, rows, cols]        out like g, written; may be g itself
+ *   rows, cols 1 .. 16384      batch 1 .. 65535      steps 0 .. 32      eps >= 0      |a|, |b|, |c| <= 16, and such that singular values stay below 4
+ *   workspace dev, 256-byte aligned, cngp_orthogonalise_workspace_bytes(cfg) bytes (may be 0); undefined before and after */
+typedef struct cngp_ortho_config {
+    int32_t  batch, rows, cols;
+    int32_t  io_dtype;        /* cngp_dtype of g and out */
+    int32_t  steps;
+    float    a, b, c, eps;
+    uint32_t flags;           /* must be 0 */
+} cngp_ortho_config;
+size_t cngp_orthogonalise_workspace_bytes(const cngp_ortho_config *cfg);
+int cngp_orthogonalise(const cngp_ortho_config *cfg, const void *g, void *out, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Lookup of codes with scaling, and its gradient: a row per image, object or token, chosen by an id per point, alone or added to
  * the point's encoding (a field conditioned on the image it is seen in, several shapes in one field).
  *     y[n] = base[n] + scale * table[ids[n]]           grad_table[r] += scale * sum over n with ids[n] == r of dy[n]

@@ -146,7 +146,8 @@ const char *const kKernelNames[K_COUNT] = {"encode_fwd", "encode_bwd_direct", "e
                                            "encode_bwd_bin_drain", "encode_bwd_input", "encode_mlp_fwd", "feature_planes",
                                            "encode_fwd_rows", "encode_bwd_small", "encode_bwd_cells", "encode_bwd_merge",
                                            "encode_bwd_partial_sums",
-                                           "recur_fwd", "recur_bwd", "recur_carry", "embed_fwd", "embed_sort", "embed_sums", "probe_balance"};
+                                           "recur_fwd", "recur_bwd", "recur_carry", "embed_fwd", "embed_sort", "embed_sums", "probe_balance",
+                                           "attend_walk", "attend_states", "attend_step", "attend_decay", "rotate", "rotate_bwd", "orthogonalise", "orthogonalise_product"};
 
 struct TimedLaunch { int id; hipEvent_t t0, t1; };
 bool g_profile = false;

@@ -1,0 +1,476 @@
+// Linear attention with a decay for each head: entry points, how a call is cut, the kernels beside the walk (cngp_attend_walk.h).
+#include <cmath>
+
+#include "cngp_attend.h"
+
+using namespace cngp;
+
+namespace {
+
+inline size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
+constexpr int64_t kMostRows = 0x7fffffffll - 65536;
+constexpr int     kBlock = 256;
+
+struct StepArgs {
+    const void  *q, *k, *v;
+    const float *decay, *h0;
+    void        *y;
+    float       *last;
+    int32_t      S, heads, group, kdim, vdim;
+    float        scale;
+    int32_t      row_decay;
+};
+
+template <typename T> __device__ __forceinline__ float value(const T v) { return (float)v; }
+
+// One row to each sequence: a workgroup per sequence and head goes over its state once (read, decayed, the row added, written, multiplied
+// with the query), neighbouring lanes neighbouring columns of VEC values, bound by those reads and writes.
+template <typename T, int BLOCK, int VEC>
+__global__ __launch_bounds__(BLOCK) void attend_step_kernel(const StepArgs a)
+{
+    __shared__ float qk[2][kAttendDim];
+    __shared__ float sums[BLOCK * VEC];
+    int units = 1;                                          // lanes side by side: a power of two that holds the columns
+    while (units * VEC < a.vdim) units *= 2;
+    const int c = (int)threadIdx.x % units * VEC, r0 = (int)threadIdx.x / units, rows = BLOCK / units;
+    const bool there = c < a.vdim;
+    for (int64_t item = blockIdx.x; item < (int64_t)a.S * a.heads; item += gridDim.x) {
+        const int     h = (int)(item % a.heads), kv = h / a.group, kvs = a.heads / a.group;
+        const int64_t s = item / a.heads;
+        for (int i = threadIdx.x; i < a.kdim; i += BLOCK) {
+            qk[0][i] = (float)((const T *)a.q)[item * a.kdim + i] * a.scale;
+            qk[1][i] = (float)((const T *)a.k)[(s * kvs + kv) * a.kdim + i];
+        }
+        const float g = a.row_decay ? a.decay[item] : a.decay[h], e = expf(g);
+        float v[VEC], y[VEC];
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            v[i] = there ? (float)((const T *)a.v)[(s * kvs + kv) * a.vdim + c + i] : 0.0f;
+            y[i] = 0.0f;
+        }
+        __syncthreads();
+        const size_t at = (size_t)item * a.kdim * a.vdim + c;
+        if (there)
+            for (int r = r0; r < a.kdim; r += rows) {
+                float S[VEC];
+                const size_t p = at + (size_t)r * a.vdim;
+                if (a.h0) __builtin_memcpy(S, a.h0 + p, sizeof S);
+                else
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) S[i] = 0.0f;
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    S[i] = fmaf(e, S[i], qk[1][r] * v[i]);
+                    y[i] = fmaf(qk[0][r], S[i], y[i]);
+                }
+                if (a.last) __builtin_memcpy(a.last + p, S, sizeof S);
+            }
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) sums[threadIdx.x * VEC + i] = y[i];
+        __syncthreads();
+        if (a.y)
+            for (int j = threadIdx.x; j < a.vdim; j += BLOCK) {
+                float t = 0.0f;
+                for (int r = 0; r < rows; ++r) t += sums[(r * units + j / VEC) * VEC + j % VEC];
+                ((T *)a.y)[item * a.vdim + j] = (T)t;
+            }
+        __syncthreads();
+    }
+}
+
+// States before each segment from the segments' own parts: a thread per state entry goes through a sequence's segments.
+struct CarryArgs {
+    float       *states;                 // [segments, heads, size]: a segment's own part, then the state before it
+    const float *total;                  // [segments, heads]
+    const int32_t *offsets;
+    const float *first;
+    float       *final;
+    int64_t      N;
+    int32_t      S, rows_each, heads, seg_rows, size, reverse;
+};
+__global__ __launch_bounds__(kBlock) void attend_carry_kernel(const CarryArgs a)
+{
+    const int64_t all = (int64_t)a.S * a.heads * a.size;
+    for (int64_t own = blockIdx.x * (int64_t)kBlock + threadIdx.x; own < all; own += (int64_t)gridDim.x * kBlock) {
+        const int     e = (int)(own % a.size), h = (int)(own / a.size % a.heads);
+        const int32_t s = (int32_t)(own / a.size / a.heads);
+        const Span    span = span_of(a.offsets, s, a.N, a.rows_each);
+        const int64_t n = (span.end - span.begin + a.seg_rows - 1) / a.seg_rows, base = piece_base(a.offsets, s, a.N, a.rows_each, a.seg_rows);
+        float state = a.first ? a.first[own] : 0.0f;
+        for (int64_t i = 0; i < n; ++i) {
+            const int64_t at = (base + (a.reverse ? n - 1 - i : i)) * a.heads + h;
+            float *p = a.states + (size_t)at * a.size + e;
+            const float part = *p;
+            *p = state;
+            state = fmaf(__builtin_amdgcn_exp2f(a.total[at]), state, part);
+        }
+        if (a.final) a.final[own] = state;
+    }
+}
+
+// Gradient of the log decays.  That of row t is the part of the result that reaches over t: with near = the products inside a chunk, far = those
+// with states, D = <state, gradient of the state> at a chunk's start and T = what crosses the whole chunk,
+//     sum over s >= t of (q.dq near - k.dk near + q.dq far)  +  sum over s < t of k.dk far  +  T,     T = D - sum of q.dq far,
+// and D of the next chunk is T + sum of k.dk far.  D is formed anew from both states every kAnchorChunks chunks: sums that ran on over a long
+// sequence would bury the short memories' gradients in their rounding.  A wavefront per such stretch and head, a lane per row of a chunk.
+struct DecayArgs {
+    const float *q_near, *q_far, *k_near, *k_far;    // [heads, N]
+    const float *states, *grads;                     // anchors of the two walks
+    const float *h0, *dh0;                           // or NULL
+    const int32_t *offsets;
+    float       *ddecay;                             // [N, heads], or NULL
+    double      *parts;                              // [pieces, heads], or NULL
+    int64_t      N, pieces;
+    int32_t      S, rows_each, heads, size, anchor_size;
+};
+__device__ __forceinline__ double wave_sum(double v) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d, 64);
+    return v;
+}
+__device__ __forceinline__ double upto(double v, const int lane) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const double o = __shfl_up(v, d, 64);
+        if (lane >= d) v += o;
+    }
+    return v;
+}
+__global__ __launch_bounds__(64) void attend_decay_kernel(const DecayArgs a)
+{
+    constexpr int kRows = kAnchorChunks * kChunk;
+    const int lane = threadIdx.x;
+    for (int64_t item = blockIdx.x; item < a.pieces * a.heads; item += gridDim.x) {
+        const int     h = (int)(item % a.heads);
+        const int64_t piece = item / a.heads;
+        const int32_t seq = sequence_of(a.offsets, piece, a.N, a.S, a.rows_each, kRows);
+        const Span    span = span_of(a.offsets, seq, a.N, a.rows_each);
+        const int64_t i = piece - piece_base(a.offsets, seq, a.N, a.rows_each, kRows), begin = span.begin + i * kRows;
+        const int64_t end = begin + kRows < span.end ? begin + kRows : span.end;
+        double sum = 0.0;
+        if (begin < end) {
+            double D = 0.0;
+            const int n = i ? a.anchor_size : a.size;
+            const size_t  at = i ? (size_t)(anchor_slot(span.begin, i * kAnchorChunks) * a.heads + h) * a.anchor_size : ((size_t)seq * a.heads + h) * a.size;
+            const float *x = i ? a.states : a.h0, *y = i ? a.grads : a.dh0;
+            if (x && y)
+                for (int e = lane; e < n; e += 64) D += (double)x[at + e] * (double)y[at + e];
+            D = wave_sum(D);
+            for (int64_t row0 = begin; row0 < end; row0 += kChunk) {
+                const bool   in = row0 + lane < end;
+                const size_t p = (size_t)h * a.N + (size_t)(in ? row0 + lane : row0);
+                const double qf = in ? a.q_far[p] : 0.0, kf = in ? a.k_far[p] : 0.0, near = in ? (double)a.q_near[p] - (double)a.k_near[p] : 0.0;
+                const double qfs = upto(qf, lane), kfs = upto(kf, lane), ns = upto(near, lane);
+                const double q_all = __shfl(qfs, 63, 64), k_all = __shfl(kfs, 63, 64), n_all = __shfl(ns, 63, 64);
+                const double T = D - q_all;
+                const double g = (n_all - ns + near) + (q_all - qfs + qf) + (kfs - kf) + T;
+                if (a.ddecay && in) a.ddecay[(row0 + lane) * a.heads + h] = (float)g;
+                sum += in ? g : 0.0;
+                D = T + k_all;
+            }
+        }
+        if (a.parts) {
+            sum = wave_sum(sum);
+            if (lane == 0) a.parts[piece * a.heads + h] = sum;
+        }
+    }
+}
+__global__ __launch_bounds__(kBlock) void attend_decay_sum_kernel(const double *__restrict__ parts, float *__restrict__ ddecay, const int64_t pieces, const int heads)
+{
+    __shared__ double sums[kBlock / 64];
+    const int h = blockIdx.x;
+    double t = 0.0;
+    for (int64_t p = threadIdx.x; p < pieces; p += kBlock) t += parts[p * heads + h];
+    t = wave_sum(t);
+    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = t;
+    __syncthreads();
+    if (threadIdx.x == 0) ddecay[h] = (float)(sums[0] + sums[1] + sums[2] + sums[3]);
+}
+
+// Gradients of keys or values that several heads share: the heads' parts added up in their order.  Rows of no sequence are left alone.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void attend_group_kernel(const float *__restrict__ part, T *__restrict__ out, const int32_t *offsets, const int32_t S, const int64_t N,
+                                                              const int kv, const int group, const int dim)
+{
+    const int64_t first = offsets ? span_of(offsets, 0, N, 0).begin : 0, end = offsets ? span_of(offsets, S - 1, N, 0).end : N;
+    const int64_t each = (int64_t)kv * dim, n = (end - first) * each;
+    for (int64_t i = blockIdx.x * (int64_t)kBlock + threadIdx.x; i < n; i += (int64_t)gridDim.x * kBlock) {
+        const int64_t row = first + i / each;
+        const int     c = (int)(i % each), head = c / dim, e = c % dim;
+        const float  *p = part + (row * kv + head) * (int64_t)group * dim + e;
+        float t = 0.0f;
+        for (int g = 0; g < group; ++g) t += p[(int64_t)g * dim];
+        out[row * each + c] = (T)t;
+    }
+}
+
+int check(const cngp_attend_config *c, int64_t N, int64_t S, bool ragged) {
+    if (!c) return CNGP_ERR_NULL;
+    if (c->heads < 1 || c->heads > 4096 || c->kv_heads < 1 || c->heads % c->kv_heads) return CNGP_ERR_INVALID;
+    if (c->key_dim < 1 || c->key_dim > kAttendDim || c->value_dim < 1 || c->value_dim > kAttendDim) return CNGP_ERR_INVALID;
+    if (c->io_dtype != CNGP_F32 && c->io_dtype != CNGP_F16) return CNGP_ERR_INVALID;
+    if (c->longest < 0 || !std::isfinite(c->scale)) return CNGP_ERR_INVALID;
+    if (c->flags & ~(uint32_t)CNGP_ATTEND_ROW_DECAY) return CNGP_ERR_INVALID;
+    if (N < 0 || N > kMostRows || S < 0 || S > kMostRows) return CNGP_ERR_INVALID;
+    if (!ragged && (S == 0 ? N != 0 : N % S != 0)) return CNGP_ERR_INVALID;
+    return CNGP_OK;
+}
+
+// How a call is cut: sequences whole, a workgroup per sequence and head, or in segments of `seg_rows` rows where that leaves most of the chip
+// without work; then a walk without outputs gives the segments' parts first.
+struct Plan {
+    int32_t seg_rows;
+    int64_t segments;
+};
+constexpr int64_t kEnoughItems = 512;                 // two workgroups for each of 256 CUs
+Plan plan_of(const cngp_attend_config *c, int64_t N, int64_t S, bool ragged) {
+    const int64_t mean = S ? (N + S - 1) / S : 0;
+    const int64_t longest = !ragged ? mean : c->longest ? std::min<int64_t>(c->longest, N) : std::min<int64_t>(4 * mean, N);
+    int64_t R = (N * c->heads + kEnoughItems - 1) / kEnoughItems;
+    R = std::max<int64_t>((R + kChunk - 1) / kChunk * kChunk, 4 * kChunk);
+    if (longest <= 4 * R) return {0, S};
+    return {(int32_t)R, pieces(N, S, (int32_t)R)};
+}
+
+struct Space {
+    size_t states, total, near_q, far_q, near_k, far_k, anchors_q, anchors_k, parts, dh0, part_k, part_v, bytes;
+};
+Space space_of(const cngp_attend_config *c, const Plan &p, int64_t N, int64_t S, uint32_t call) {
+    Space sp{};
+    size_t at = 0;
+    auto take = [&](bool wanted, size_t bytes) { const size_t o = at; if (wanted) at += align256(bytes); return o; };
+    const bool   bwd = call & CNGP_ATTEND_CALL_BWD, cut = p.seg_rows != 0, shared = c->heads != c->kv_heads;
+    const size_t H = (size_t)c->heads, size = (size_t)c->key_dim * c->value_dim, rows = (size_t)N;
+    sp.states = take(cut, (size_t)p.segments * H * size * 4);
+    sp.total = take(cut, (size_t)p.segments * H * 4);
+    for (size_t *d : {&sp.near_q, &sp.far_q, &sp.near_k, &sp.far_k}) *d = take(bwd, rows * H * 4);
+    const size_t slots = rows / (kAnchorChunks * kChunk) + 1;
+    sp.anchors_q = take(bwd, slots * H * anchor_floats(c->key_dim, c->value_dim) * 4);
+    sp.anchors_k = take(bwd, slots * H * anchor_floats(c->key_dim, c->value_dim) * 4);
+    sp.parts = take(bwd && !(c->flags & CNGP_ATTEND_ROW_DECAY), (size_t)pieces(N, S, kAnchorChunks * kChunk) * H * 8);
+    sp.dh0 = take(bwd, (size_t)S * H * size * 4);
+    sp.part_k = take(bwd && shared, rows * H * (size_t)c->key_dim * 4);
+    sp.part_v = take(bwd && shared, rows * H * (size_t)c->value_dim * 4);
+    sp.bytes = at;
+    return sp;
+}
+
+bool whole_rows(const void *p, int dim, int io, size_t bytes) {
+    return ((uintptr_t)p & (bytes - 1)) == 0 && (size_t)dim * (io == CNGP_F16 ? 2 : 4) % bytes == 0;
+}
+
+struct Call {
+    const cngp_attend_config *c;
+    const float *decay;
+    int64_t N, S;
+    const int32_t *offsets;
+    Plan p;
+    Space sp;
+    char *ws;
+    hipStream_t s;
+
+    WalkArgs base(const void *q, const void *k, const void *v, int q_div, int k_div, int v_div, int kdim, int vdim, bool reverse) const {
+        WalkArgs a{};
+        a.q = q; a.k = k; a.v = v; a.decay = decay; a.offsets = offsets;
+        a.N = N; a.S = (int32_t)S; a.rows_each = (int32_t)(S ? N / S : 0);
+        a.heads = c->heads; a.q_div = q_div; a.k_div = k_div; a.v_div = v_div; a.x_div = 1;
+        a.kdim = kdim; a.vdim = vdim;
+        a.seg_rows = p.seg_rows; a.segments = (int32_t)p.segments;
+        a.first_i = a.final_i = vdim; a.first_j = a.final_j = 1;
+        a.pair_scale = a.far_scale = a.state_scale = 1.0f;
+        a.reverse = reverse; a.row_decay = (c->flags & CNGP_ATTEND_ROW_DECAY) != 0;
+        a.vec_q = whole_rows(q, kdim, c->io_dtype, 16); a.vec_k = whole_rows(k, kdim, c->io_dtype, 16); a.vec_v = whole_rows(v, vdim, c->io_dtype, 16);
+        return a;
+    }
+    void output(WalkArgs &a, void *out, bool f32) const {
+        a.out = out;
+        a.out_f32 = f32 || c->io_dtype == CNGP_F32;
+        a.vec_out = a.vdim % 4 == 0 && ((uintptr_t)out & (a.out_f32 ? 15u : 7u)) == 0;
+    }
+    int walk(const WalkArgs &a, bool states_only) const {
+        return c->io_dtype == CNGP_F16 ? attend_walk_f16(a, states_only, s) : attend_walk_f32(a, states_only, s);
+    }
+    // cut sequences: the states before each segment into the workspace, the last ones into `final`
+    int carry(WalkArgs a, const float *first, float *final) const {
+        a.first = nullptr;
+        a.final = (float *)(ws + sp.states);
+        a.total = (float *)(ws + sp.total);
+        if (int rc = walk(a, true)) return rc;
+        CarryArgs k{};
+        k.states = a.final; k.total = a.total; k.offsets = offsets; k.first = first; k.final = final;
+        k.N = N; k.S = (int32_t)S; k.rows_each = a.rows_each; k.heads = c->heads; k.seg_rows = p.seg_rows;
+        k.size = a.kdim * a.vdim; k.reverse = a.reverse;
+        LaunchTimer t(s, K_ATTEND_STATES);
+        attend_carry_kernel<<<(unsigned)std::min<int64_t>((S * c->heads * k.size + kBlock - 1) / kBlock, 1 << 20), kBlock, 0, s>>>(k);
+        return launch_status("attend_carry_kernel");
+    }
+};
+
+template <typename T>
+int step(const StepArgs &a, hipStream_t s) {
+    const int64_t items = (int64_t)a.S * a.heads;
+    const unsigned blocks = (unsigned)std::min<int64_t>(items, kMostGroups256);
+    const bool vec = a.vdim % 4 == 0 && ((uintptr_t)a.h0 & 15u) == 0 && ((uintptr_t)a.last & 15u) == 0;
+    const bool small = a.kdim * a.vdim <= 1024 && (vec || a.vdim <= 64);
+    LaunchTimer t(s, K_ATTEND_STEP);
+    if (vec) {
+        if (small) attend_step_kernel<T, 64, 4><<<blocks, 64, 0, s>>>(a);
+        else attend_step_kernel<T, 256, 4><<<blocks, 256, 0, s>>>(a);
+    } else {
+        if (small) attend_step_kernel<T, 64, 1><<<blocks, 64, 0, s>>>(a);
+        else attend_step_kernel<T, 256, 1><<<blocks, 256, 0, s>>>(a);
+    }
+    return launch_status("attend_step_kernel");
+}
+
+int decay_sum(const double *parts, float *ddecay, int64_t pieces, int heads, hipStream_t s) {
+    LaunchTimer t(s, K_ATTEND_DECAY);
+    attend_decay_sum_kernel<<<(unsigned)heads, kBlock, 0, s>>>(parts, ddecay, pieces, heads);
+    return launch_status("attend_decay_sum_kernel");
+}
+
+bool lent(const Space &sp, const void *ws, size_t bytes) { return !sp.bytes || (ws && ((uintptr_t)ws & 255u) == 0 && bytes >= sp.bytes); }
+
+}  // namespace
+
+extern "C" {
+
+size_t cngp_attend_workspace_bytes(const cngp_attend_config *cfg, int64_t N, int64_t sequences, uint32_t call) {
+    if (check(cfg, N, sequences, call & CNGP_ATTEND_CALL_RAGGED) || sequences == 0) return 0;
+    return space_of(cfg, plan_of(cfg, N, sequences, call & CNGP_ATTEND_CALL_RAGGED), N, sequences, call).bytes;
+}
+
+int cngp_attend_fwd(const cngp_attend_config *cfg, const void *q, const void *k, const void *v, const float *decay, int64_t N, const int32_t *offsets,
+                    int64_t sequences, const float *h0, void *y, float *last, void *workspace, size_t workspace_bytes, void *stream) {
+    if (int rc = check(cfg, N, sequences, offsets != nullptr)) return rc;
+    if (sequences == 0) return CNGP_OK;
+    if (N && (!k || !v || !decay || (y && !q) || (!last && !y))) return CNGP_ERR_NULL;
+    if (N == 0 && !last) return CNGP_OK;
+    hipStream_t s = (hipStream_t)stream;
+    const bool ragged = offsets != nullptr;
+    if (!ragged && N == sequences) {
+        StepArgs a{q ? q : k, k, v, decay, h0, y, last, (int32_t)sequences, cfg->heads, cfg->heads / cfg->kv_heads, cfg->key_dim, cfg->value_dim, cfg->scale,
+                   (cfg->flags & CNGP_ATTEND_ROW_DECAY) != 0};
+        if (!q && cfg->heads != cfg->kv_heads) return CNGP_ERR_NULL;
+        return cfg->io_dtype == CNGP_F16 ? step<_Float16>(a, s) : step<float>(a, s);
+    }
+    Call call{cfg, decay, N, sequences, offsets, plan_of(cfg, N, sequences, ragged), {}, (char *)workspace, s};
+    call.sp = space_of(cfg, call.p, N, sequences, ragged ? CNGP_ATTEND_CALL_RAGGED : 0);
+    if (!lent(call.sp, workspace, workspace_bytes)) return CNGP_ERR_WORKSPACE;
+    const int group = cfg->heads / cfg->kv_heads;
+    WalkArgs a = call.base(q, k, v, 1, group, group, cfg->key_dim, cfg->value_dim, false);
+    a.pair_scale = a.far_scale = cfg->scale;
+    a.first = h0;
+    a.final = last;
+    if (call.p.seg_rows) {
+        if (int rc = call.carry(a, h0, last)) return rc;
+        if (!y) return CNGP_OK;
+        a.first = (const float *)(call.ws + call.sp.states);
+        a.final = nullptr;
+    }
+    if (!y) return call.walk(a, true);
+    call.output(a, y, false);
+    return call.walk(a, false);
+}
+
+int cngp_attend_bwd(const cngp_attend_config *cfg, const void *q, const void *k, const void *v, const float *decay, int64_t N, const int32_t *offsets,
+                    int64_t sequences, const float *h0, const void *dy, const float *dlast, void *dq, void *dk, void *dv, float *ddecay, float *dh0,
+                    void *workspace, size_t workspace_bytes, void *stream) {
+    if (int rc = check(cfg, N, sequences, offsets != nullptr)) return rc;
+    const bool rows = cfg->flags & CNGP_ATTEND_ROW_DECAY;
+    if (sequences == 0) return ddecay && !rows ? decay_sum(nullptr, ddecay, 0, cfg->heads, (hipStream_t)stream) : CNGP_OK;
+    if (dh0 && dh0 == dlast) return CNGP_ERR_INVALID;
+    if (N && (!q || !k || !v || !decay || !dq || !dk || !dv || (!dy && !dlast))) return CNGP_ERR_NULL;
+    hipStream_t s = (hipStream_t)stream;
+    const bool ragged = offsets != nullptr;
+    Call call{cfg, decay, N, sequences, offsets, plan_of(cfg, N, sequences, ragged), {}, (char *)workspace, s};
+    call.sp = space_of(cfg, call.p, N, sequences, CNGP_ATTEND_CALL_BWD | (ragged ? CNGP_ATTEND_CALL_RAGGED : 0));
+    if (!lent(call.sp, workspace, workspace_bytes)) return CNGP_ERR_WORKSPACE;
+    char *ws = call.ws;
+    const Space &sp = call.sp;
+    const int   group = cfg->heads / cfg->kv_heads, K = cfg->key_dim, V = cfg->value_dim;
+    const bool  cut = call.p.seg_rows != 0, shared = group > 1;
+    float      *states = (float *)(ws + sp.states);
+    if (ddecay && h0 && !dh0) dh0 = (float *)(ws + sp.dh0);
+
+    // dq_t = scale (sum of e (dy_t . v_s) k_s + e state dy_t): a forward walk over the transposed state
+    WalkArgs a = call.base(dy, v, k, 1, group, group, V, K, false);
+    a.pair_scale = a.far_scale = cfg->scale;
+    if (cut) {
+        WalkArgs m = call.base(q, k, v, 1, group, group, K, V, false);
+        if (int rc = call.carry(m, h0, nullptr)) return rc;
+        a.first = states;
+    } else a.first = h0;
+    a.first_i = 1; a.first_j = V;
+    call.output(a, dq, false);
+    if (ddecay) {
+        a.x = q; a.x_div = 1;
+        a.dot_near = (float *)(ws + sp.near_q); a.dot_far = (float *)(ws + sp.far_q);
+        a.anchors = (float *)(ws + sp.anchors_q);
+    }
+    if (N)
+        if (int rc = call.walk(a, false)) return rc;
+
+    // dv_s = sum of scale e (k_s . q_t) dy_t + e k_s . (gradient of the state behind it): against time, with the gradient of the state
+    a = call.base(k, q, dy, group, 1, 1, K, V, true);
+    a.pair_scale = a.state_scale = cfg->scale;
+    a.first = dlast; a.final = dh0;
+    if (cut) {
+        if (int rc = call.carry(a, dlast, dh0)) return rc;
+        a.first = states; a.final = nullptr;
+    }
+    if (N == 0) {                                        // the gradient of the state passes through
+        if (dh0)
+            if (int rc = call.walk(a, true)) return rc;
+        return ddecay && !rows ? decay_sum(nullptr, ddecay, 0, cfg->heads, s) : CNGP_OK;
+    }
+    call.output(a, shared ? (void *)(ws + sp.part_v) : dv, shared);
+    if (int rc = call.walk(a, false)) return rc;
+
+    // dk_s = sum of scale e (v_s . dy_t) q_t + e (gradient of the state behind it) v_s
+    a = call.base(v, dy, q, group, 1, 1, V, K, true);
+    a.pair_scale = a.state_scale = cfg->scale;
+    a.first = cut ? states : dlast;
+    a.first_i = 1; a.first_j = V;
+    call.output(a, shared ? (void *)(ws + sp.part_k) : dk, shared);
+    if (ddecay) {
+        a.x = k; a.x_div = group;
+        a.dot_near = (float *)(ws + sp.near_k); a.dot_far = (float *)(ws + sp.far_k);
+        a.anchors = (float *)(ws + sp.anchors_k);
+    }
+    if (int rc = call.walk(a, false)) return rc;
+
+    if (shared) {
+        LaunchTimer t(s, K_ATTEND_DECAY);
+        for (int which = 0; which < 2; ++which) {
+            const int      dim = which ? V : K;
+            const float   *part = (const float *)(ws + (which ? sp.part_v : sp.part_k));
+            void          *out = which ? dv : dk;
+            const unsigned blocks = (unsigned)std::min<int64_t>((N * cfg->kv_heads * dim + kBlock - 1) / kBlock, 1 << 20);
+            if (cfg->io_dtype == CNGP_F16)
+                attend_group_kernel<_Float16><<<blocks, kBlock, 0, s>>>(part, (_Float16 *)out, offsets, (int32_t)sequences, N, cfg->kv_heads, group, dim);
+            else attend_group_kernel<float><<<blocks, kBlock, 0, s>>>(part, (float *)out, offsets, (int32_t)sequences, N, cfg->kv_heads, group, dim);
+            if (int rc = launch_status("attend_group_kernel")) return rc;
+        }
+    }
+    if (!ddecay) return CNGP_OK;
+    DecayArgs d{};
+    d.q_near = (const float *)(ws + sp.near_q); d.q_far = (const float *)(ws + sp.far_q);
+    d.k_near = (const float *)(ws + sp.near_k); d.k_far = (const float *)(ws + sp.far_k);
+    d.states = (const float *)(ws + sp.anchors_q); d.grads = (const float *)(ws + sp.anchors_k);
+    d.h0 = h0; d.dh0 = dh0; d.offsets = offsets;
+    d.ddecay = rows ? ddecay : nullptr;
+    d.parts = rows ? nullptr : (double *)(ws + sp.parts);
+    d.N = N; d.S = (int32_t)sequences; d.rows_each = (int32_t)(N / sequences); d.heads = cfg->heads;
+    d.pieces = pieces(N, sequences, kAnchorChunks * kChunk);
+    d.size = K * V; d.anchor_size = (int32_t)anchor_floats(K, V);
+    {
+        LaunchTimer t(s, K_ATTEND_DECAY);
+        attend_decay_kernel<<<(unsigned)std::min<int64_t>(d.pieces * d.heads, 0x3ffffff), 64, 0, s>>>(d);
+        if (int rc = launch_status("attend_decay_kernel")) return rc;
+    }
+    if (rows) return CNGP_OK;
+    return decay_sum(d.parts, ddecay, d.pieces, cfg->heads, s);
+}
+
+}  // extern "C"

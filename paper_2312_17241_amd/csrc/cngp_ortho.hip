@@ -1,0 +1,350 @@
+// Orthogonalised update of matrices by products of a polynomial.  X [m, n], m <= n (a taller matrix is taken transposed):
+//     X = G / (|G| + eps);      each step   A = X X^T,   B = b A + c A A,   X <- a X + B X
+// The products run on the matrix cores.  One fp16 number per value would not do: the polynomial lifts small singular values by 3.4 in each
+// step and with them what a rounding put into their directions, so that 11 bits leave errors of a tenth of an entry.  Every operand is two fp16
+// numbers, the second scaled by 2^11, and a product three (high by high, and both mixed ones into sums of their own): 22 bits.
+// A and B are symmetric: tiles on and below the diagonal are computed and written twice.
+#include <algorithm>
+#include <cmath>
+
+#include "cngp_launch.h"
+#include "cngp_matrix.h"
+
+using namespace cngp;
+using namespace cngp::mat;
+
+namespace {
+
+inline size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
+constexpr int kBlock = 256, kTile = 128, kDepth = 32;       // a workgroup's part of a product, and how much of the contraction it has in LDS at a time
+constexpr int kPad = 8;                                     // halves between rows in LDS: 16-byte reads of neighbouring rows fall into different banks
+constexpr float kScaleA = 512.0f;                           // A and B are kept times this, X times a power of two of its own (Shape::scale):
+                                                            // entries of large matrices would be subnormal fp16 numbers
+constexpr int kNormParts = 256;
+
+// High and low parts of a matrix, rows of `stride` values.
+struct Pair {
+    _Float16 *hi, *lo;
+    size_t    stride, each;                                 // each: values of one matrix of the batch
+};
+
+__device__ __forceinline__ void put(const Pair &p, const size_t at, const float v) {
+    const _Float16 h = (_Float16)v;
+    p.hi[at] = h;
+    p.lo[at] = (_Float16)((v - (float)h) * kLow);
+}
+__device__ __forceinline__ void put4(const Pair &p, const size_t at, const float (&v)[4]) {
+    half4_t h, l;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        h[e] = (_Float16)v[e];
+        l[e] = (_Float16)((v[e] - (float)h[e]) * kLow);
+    }
+    *reinterpret_cast<half4_t *>(p.hi + at) = h;
+    *reinterpret_cast<half4_t *>(p.lo + at) = l;
+}
+__device__ __forceinline__ void get4(const Pair &p, const size_t at, float (&v)[4]) {
+    const half4_t h = *reinterpret_cast<const half4_t *>(p.hi + at), l = *reinterpret_cast<const half4_t *>(p.lo + at);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = fmaf((float)l[e], 1.0f / kLow, (float)h[e]);
+}
+
+// ---------------------------------------------------------------- norm, start, no steps
+__device__ __forceinline__ double block_sum(double v, double *room) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d, 64);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return room[0] + room[1] + room[2] + room[3];
+}
+
+template <typename T>
+__global__ __launch_bounds__(kBlock) void ortho_norm_kernel(const T *__restrict__ g, const int64_t n, double *__restrict__ parts)
+{
+    __shared__ double room[4];
+    const T *x = g + (size_t)blockIdx.y * n;
+    double t = 0.0;
+    for (int64_t i = blockIdx.x * (int64_t)kBlock + threadIdx.x; i < n; i += (int64_t)gridDim.x * kBlock) {
+        const double v = (double)(float)x[i];
+        t = fma(v, v, t);
+    }
+    t = block_sum(t, room);
+    if (threadIdx.x == 0) parts[(size_t)blockIdx.y * gridDim.x + blockIdx.x] = t;
+}
+
+__device__ __forceinline__ float inverse_norm(const double *parts, const int count, const float eps, double *room) {
+    double t = 0.0;
+    for (int i = threadIdx.x; i < count; i += kBlock) t += parts[(size_t)blockIdx.z * count + i];
+    return (float)(1.0 / (sqrt(block_sum(t, room)) + (double)eps));
+}
+
+// X from G (transposed where `turned`), with zeros behind its edges: 64 x 64 tiles.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void ortho_start_kernel(const T *__restrict__ g, const int rows, const int cols, const bool turned, const double *__restrict__ parts,
+                                                             const int count, const float eps, const float scale, const Pair X)
+{
+    __shared__ double room[4];
+    __shared__ float  tile[64][65];
+    const float inv = inverse_norm(parts, count, eps, room) * scale;
+    const T *x = g + (size_t)blockIdx.z * rows * cols;
+    const int m0 = (int)blockIdx.y * 64, n0 = (int)blockIdx.x * 64;     // of X
+    const int c = threadIdx.x & 63;
+    for (int r = threadIdx.x >> 6; r < 64; r += 4) {
+        const int row = (turned ? n0 : m0) + r, col = (turned ? m0 : n0) + c;
+        const float v = row < rows && col < cols ? (float)x[(size_t)row * cols + col] * inv : 0.0f;
+        if (turned) tile[c][r] = v;
+        else tile[r][c] = v;
+    }
+    __syncthreads();
+    const int c4 = (threadIdx.x & 15) * 4;
+    for (int r = threadIdx.x >> 4; r < 64; r += 16) {
+        const float v[4] = {tile[r][c4], tile[r][c4 + 1], tile[r][c4 + 2], tile[r][c4 + 3]};
+        put4(X, blockIdx.z * X.each + (size_t)(m0 + r) * X.stride + n0 + c4, v);
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kBlock) void ortho_scale_kernel(const T *g, T *out, const int64_t n, const double *__restrict__ parts, const int count, const float eps)
+{
+    __shared__ double room[4];
+    const float inv = inverse_norm(parts, count, eps, room);
+    for (int64_t i = blockIdx.x * (int64_t)kBlock + threadIdx.x; i < n; i += (int64_t)gridDim.x * kBlock)
+        out[(size_t)blockIdx.z * n + i] = (T)((float)g[(size_t)blockIdx.z * n + i] * inv);
+}
+
+// ---------------------------------------------------------------- products
+enum : int { GRAM, POLY, UPDATE, LAST };
+struct ProductArgs {
+    Pair  A, B, C, D;                    // C = epilogue(A B^T, or A B for updates; D)
+    int   depth, tiles_m, tiles_n;
+    float of_sum, of_d;                  // C = of_sum * product + of_d * D
+    void *out;                           // LAST: the result
+    int   m, n, turned, out_f16;
+};
+
+// 128 x 128 of a product by four wavefronts of 64 x 64; computed transposed (a lane has a row of C and four neighbouring columns in four registers).
+template <int WHAT>
+__global__ __launch_bounds__(kBlock) void ortho_product_kernel(const ProductArgs a)
+{
+    constexpr bool kBack = WHAT == UPDATE || WHAT == LAST;              // the right factor lies by rows of the contraction
+    constexpr int  kRowA = kDepth + kPad, kRowB = kBack ? kTile + kPad : kDepth + kPad, kSizeB = kBack ? kDepth * kRowB : kTile * kRowB;
+    __shared__ __align__(16) _Float16 lds[2][2 * kTile * kRowA + 2 * kSizeB];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
+    int ti, tj;
+    if (kBack) {
+        ti = (int)(blockIdx.x % a.tiles_m);
+        tj = (int)(blockIdx.x / a.tiles_m);
+    } else {                             // the triangle's tiles, row after row
+        ti = (int)((sqrtf(8.0f * (float)blockIdx.x + 1.0f) - 1.0f) * 0.5f);
+        while ((ti + 1) * (ti + 2) / 2 <= (int)blockIdx.x) ++ti;
+        while (ti * (ti + 1) / 2 > (int)blockIdx.x) --ti;
+        tj = (int)blockIdx.x - ti * (ti + 1) / 2;
+    }
+    const size_t z = blockIdx.z;
+    const int i0 = ti * kTile, j0 = tj * kTile, wi = 64 * (wave & 1), wj = 64 * (wave >> 1);
+
+    uint4 r[8];
+    auto fetch = [&](const int k0) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int at = (int)threadIdx.x + i * kBlock;
+            const size_t pa = z * a.A.each + (size_t)(i0 + (at >> 2)) * a.A.stride + k0 + (at & 3) * 8;
+            r[i] = *reinterpret_cast<const uint4 *>(a.A.hi + pa);
+            r[2 + i] = *reinterpret_cast<const uint4 *>(a.A.lo + pa);
+            const size_t pb = z * a.B.each + (kBack ? (size_t)(k0 + (at >> 4)) * a.B.stride + j0 + (at & 15) * 8
+                                                    : (size_t)(j0 + (at >> 2)) * a.B.stride + k0 + (at & 3) * 8);
+            r[4 + i] = *reinterpret_cast<const uint4 *>(a.B.hi + pb);
+            r[6 + i] = *reinterpret_cast<const uint4 *>(a.B.lo + pb);
+        }
+    };
+    auto keep = [&](_Float16 *to) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int at = (int)threadIdx.x + i * kBlock, pa = (at >> 2) * kRowA + (at & 3) * 8, pb = kBack ? (at >> 4) * kRowB + (at & 15) * 8 : pa;
+            *reinterpret_cast<uint4 *>(to + pa) = r[i];
+            *reinterpret_cast<uint4 *>(to + kTile * kRowA + pa) = r[2 + i];
+            *reinterpret_cast<uint4 *>(to + 2 * kTile * kRowA + pb) = r[4 + i];
+            *reinterpret_cast<uint4 *>(to + 2 * kTile * kRowA + kSizeB + pb) = r[6 + i];
+        }
+    };
+
+    acc_t high[2][2], low[2][2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int w = 0; w < 2; ++w) high[u][w] = low[u][w] = zero();
+    fetch(0);
+    for (int k0 = 0, b = 0; k0 < a.depth; k0 += kDepth, b ^= 1) {
+        keep(lds[b]);
+        __syncthreads();
+        if (k0 + kDepth < a.depth) fetch(k0 + kDepth);
+        const _Float16 *A = lds[b], *B = lds[b] + 2 * kTile * kRowA;
+#pragma unroll
+        for (int s = 0; s < kDepth / 16; ++s) {
+            half8_t ah[2], al[2], bh[2], bl[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const _Float16 *p = A + (wi + 32 * u + col) * kRowA + 16 * s + 8 * half;
+                ah[u] = read8(p);
+                al[u] = read8(p + kTile * kRowA);
+                if constexpr (kBack) {
+                    bh[u] = read_column(B, kRowB, 16 * s, wj + 32 * u, lane);
+                    bl[u] = read_column(B + kSizeB, kRowB, 16 * s, wj + 32 * u, lane);
+                } else {
+                    const _Float16 *q = B + (wj + 32 * u + col) * kRowB + 16 * s + 8 * half;
+                    bh[u] = read8(q);
+                    bl[u] = read8(q + kSizeB);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int w = 0; w < 2; ++w) {
+                    high[u][w] = mfma(bh[w], ah[u], high[u][w]);
+                    low[u][w] = mfma(bh[w], al[u], low[u][w]);
+                    low[u][w] = mfma(bl[w], ah[u], low[u][w]);
+                }
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+            const int i = i0 + wi + 32 * u + col;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int j = j0 + wj + 32 * w + 8 * g + 4 * half;
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = fmaf(low[u][w][4 * g + e], 1.0f / kLow, high[u][w][4 * g + e]) * a.of_sum;
+                if (WHAT != GRAM) {
+                    float d[4];
+                    get4(a.D, z * a.D.each + (size_t)i * a.D.stride + j, d);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = fmaf(a.of_d, d[e], v[e]);
+                }
+                if (WHAT != LAST) put4(a.C, z * a.C.each + (size_t)i * a.C.stride + j, v);
+                if (!kBack && ti != tj)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) put(a.C, z * a.C.each + (size_t)(j + e) * a.C.stride + i, v[e]);
+                if (WHAT == LAST && i < a.m)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (j + e < a.n) {
+                            const size_t at = z * (size_t)a.m * a.n + (a.turned ? (size_t)(j + e) * a.m + i : (size_t)i * a.n + j + e);
+                            if (a.out_f16) ((_Float16 *)a.out)[at] = (_Float16)v[e];
+                            else ((float *)a.out)[at] = v[e];
+                        }
+            }
+        }
+}
+
+struct Shape {
+    int    m, n, mp, np, parts;
+    bool   turned;
+    float  scale;
+    size_t x[2], a, b, norm, bytes;
+};
+Shape shape_of(const cngp_ortho_config *c) {
+    Shape s{};
+    s.turned = c->rows > c->cols;
+    s.m = std::min(c->rows, c->cols);
+    s.n = std::max(c->rows, c->cols);
+    s.mp = (s.m + kTile - 1) / kTile * kTile;
+    s.np = (s.n + kTile - 1) / kTile * kTile;
+    s.scale = 16.0f;                     // entries of an orthogonal matrix are about 1 / sqrt(n); the largest possible ones stay below 16 * 128 * 4
+    for (int r = 1; r < s.n; r *= 4) s.scale *= 2.0f;
+    s.parts = (int)std::max<int64_t>(1, std::min<int64_t>((int64_t)s.m * s.n / 4096, std::max(1, kNormParts / std::max(1, std::min(c->batch, 8)))));
+    size_t at = 0;
+    auto take = [&](bool wanted, size_t bytes) { const size_t o = at; if (wanted) at += align256(bytes); return o; };
+    const size_t batch = (size_t)c->batch, x = batch * s.mp * s.np * 4, a = batch * s.mp * s.mp * 4;
+    s.norm = take(true, batch * s.parts * 8);
+    s.x[0] = take(c->steps > 0, x);
+    s.x[1] = take(c->steps > 1, x);
+    s.a = take(c->steps > 0, a);
+    s.b = take(c->steps > 0, a);
+    s.bytes = at;
+    return s;
+}
+
+int check(const cngp_ortho_config *c) {
+    if (!c) return CNGP_ERR_NULL;
+    if (c->rows < 1 || c->rows > 16384 || c->cols < 1 || c->cols > 16384 || c->batch < 1 || c->batch > 65535) return CNGP_ERR_INVALID;
+    if (c->io_dtype != CNGP_F32 && c->io_dtype != CNGP_F16) return CNGP_ERR_INVALID;
+    if (c->steps < 0 || c->steps > 32 || c->flags) return CNGP_ERR_INVALID;
+    if (!std::isfinite(c->eps) || c->eps < 0.0f) return CNGP_ERR_INVALID;
+    for (float v : {c->a, c->b, c->c})
+        if (!(std::fabs(v) <= 16.0f)) return CNGP_ERR_INVALID;
+    return CNGP_OK;
+}
+
+Pair pair_of(char *ws, size_t at, int rows, int cols, int batch) {
+    Pair p;
+    p.stride = (size_t)cols;
+    p.each = (size_t)rows * cols;
+    p.hi = (_Float16 *)(ws + at);
+    p.lo = p.hi + p.each * batch;
+    return p;
+}
+
+template <typename T>
+int norm_and_start(const cngp_ortho_config *c, const Shape &s, const T *g, T *out, char *ws, hipStream_t st) {
+    LaunchTimer t(st, K_ORTHO);
+    double *parts = (double *)(ws + s.norm);
+    const int64_t n = (int64_t)s.m * s.n;
+    ortho_norm_kernel<T><<<dim3((unsigned)s.parts, (unsigned)c->batch), kBlock, 0, st>>>(g, n, parts);
+    if (int rc = launch_status("ortho_norm_kernel")) return rc;
+    if (c->steps == 0) {
+        ortho_scale_kernel<T><<<dim3((unsigned)std::min<int64_t>((n + 1023) / 1024, 1024), 1, (unsigned)c->batch), kBlock, 0, st>>>(g, out, n, parts, s.parts, c->eps);
+        return launch_status("ortho_scale_kernel");
+    }
+    ortho_start_kernel<T><<<dim3((unsigned)(s.np / 64), (unsigned)(s.mp / 64), (unsigned)c->batch), kBlock, 0, st>>>(g, c->rows, c->cols, s.turned, parts, s.parts, c->eps,
+                                                                                                                  s.scale, pair_of(ws, s.x[0], s.mp, s.np, c->batch));
+    return launch_status("ortho_start_kernel");
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t cngp_orthogonalise_workspace_bytes(const cngp_ortho_config *cfg) { return check(cfg) ? 0 : shape_of(cfg).bytes; }
+
+int cngp_orthogonalise(const cngp_ortho_config *cfg, const void *g, void *out, void *workspace, size_t workspace_bytes, void *stream) {
+    if (int rc = check(cfg)) return rc;
+    if (!g || !out) return CNGP_ERR_NULL;
+    const Shape s = shape_of(cfg);
+    if (s.bytes && (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < s.bytes)) return CNGP_ERR_WORKSPACE;
+    char *ws = (char *)workspace;
+    hipStream_t st = (hipStream_t)stream;
+    if (int rc = cfg->io_dtype == CNGP_F16 ? norm_and_start(cfg, s, (const _Float16 *)g, (_Float16 *)out, ws, st) : norm_and_start(cfg, s, (const float *)g, (float *)out, ws, st))
+        return rc;
+    const Pair A = pair_of(ws, s.a, s.mp, s.mp, cfg->batch), B = pair_of(ws, s.b, s.mp, s.mp, cfg->batch);
+    const int  tm = s.mp / kTile, tn = s.np / kTile;
+    for (int step = 0; step < cfg->steps; ++step) {
+        const bool last = step + 1 == cfg->steps;
+        const Pair X = pair_of(ws, s.x[step & 1], s.mp, s.np, cfg->batch), Y = last ? X : pair_of(ws, s.x[1 - (step & 1)], s.mp, s.np, cfg->batch);
+        LaunchTimer t(st, K_ORTHO_PRODUCT);
+        ProductArgs p{};
+        p.tiles_m = tm; p.tiles_n = tn;
+        p.A = X; p.B = X; p.C = A; p.D = A;
+        p.depth = s.np; p.of_sum = kScaleA / (s.scale * s.scale);
+        ortho_product_kernel<GRAM><<<dim3((unsigned)(tm * (tm + 1) / 2), 1, (unsigned)cfg->batch), kBlock, 0, st>>>(p);
+        if (int rc = launch_status("ortho_product_kernel")) return rc;
+        p.A = A; p.B = A; p.C = B; p.D = A;
+        p.depth = s.mp; p.of_sum = cfg->c / kScaleA; p.of_d = cfg->b;
+        ortho_product_kernel<POLY><<<dim3((unsigned)(tm * (tm + 1) / 2), 1, (unsigned)cfg->batch), kBlock, 0, st>>>(p);
+        if (int rc = launch_status("ortho_product_kernel")) return rc;
+        p.A = B; p.B = X; p.C = Y; p.D = X;
+        p.depth = s.mp; p.of_sum = 1.0f / kScaleA; p.of_d = cfg->a;
+        if (last) {
+            p.of_sum /= s.scale; p.of_d /= s.scale;
+            p.out = out; p.m = s.m; p.n = s.n; p.turned = s.turned; p.out_f16 = cfg->io_dtype == CNGP_F16;
+            ortho_product_kernel<LAST><<<dim3((unsigned)(tm * tn), 1, (unsigned)cfg->batch), kBlock, 0, st>>>(p);
+        } else ortho_product_kernel<UPDATE><<<dim3((unsigned)(tm * tn), 1, (unsigned)cfg->batch), kBlock, 0, st>>>(p);
+        if (int rc = launch_status("ortho_product_kernel")) return rc;
+    }
+    return CNGP_OK;
+}
+
+}  // extern "C"

@@ -18,9 +18,17 @@ namespace {
 inline size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
 constexpr int kBlock = 256, kTile = 128, kDepth = 32;       // a workgroup's part of a product, and how much of the contraction it has in LDS at a time
 constexpr int kPad = 8;                                     // halves between rows in LDS: 16-byte reads of neighbouring rows fall into different banks
-constexpr float kScaleA = 512.0f;                           // A and B are kept times this, X times a power of two of its own (Shape::scale):
+constexpr float kScaleX = 16384.0f, kScaleA = 4096.0f, kScaleB = 1024.0f;                           // A and B are kept times this, X times a power of two of its own (Shape::scale):
                                                             // entries of large matrices would be subnormal fp16 numbers
 constexpr int kNormParts = 256;
+#ifndef KST
+#define KST 2
+#endif
+#ifndef KOCC
+#define KOCC 2
+#endif
+constexpr int kStages = KST;
+typedef unsigned words_t __attribute__((ext_vector_type(4)));
 
 // High and low parts of a matrix, rows of `stride` values.
 struct Pair {
@@ -31,14 +39,14 @@ struct Pair {
 __device__ __forceinline__ void put(const Pair &p, const size_t at, const float v) {
     const _Float16 h = (_Float16)v;
     p.hi[at] = h;
-    p.lo[at] = (_Float16)((v - (float)h) * kLow);
+    p.lo[at] = (_Float16)(v - (float)h);
 }
 __device__ __forceinline__ void put4(const Pair &p, const size_t at, const float (&v)[4]) {
     half4_t h, l;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         h[e] = (_Float16)v[e];
-        l[e] = (_Float16)((v[e] - (float)h[e]) * kLow);
+        l[e] = (_Float16)(v[e] - (float)h[e]);
     }
     *reinterpret_cast<half4_t *>(p.hi + at) = h;
     *reinterpret_cast<half4_t *>(p.lo + at) = l;
@@ -46,7 +54,7 @@ __device__ __forceinline__ void put4(const Pair &p, const size_t at, const float
 __device__ __forceinline__ void get4(const Pair &p, const size_t at, float (&v)[4]) {
     const half4_t h = *reinterpret_cast<const half4_t *>(p.hi + at), l = *reinterpret_cast<const half4_t *>(p.lo + at);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = fmaf((float)l[e], 1.0f / kLow, (float)h[e]);
+    for (int e = 0; e < 4; ++e) v[e] = (float)h[e] + (float)l[e];
 }
 
 // ---------------------------------------------------------------- norm, start, no steps
@@ -125,11 +133,11 @@ struct ProductArgs {
 
 // 128 x 128 of a product by four wavefronts of 64 x 64; computed transposed (a lane has a row of C and four neighbouring columns in four registers).
 template <int WHAT>
-__global__ __launch_bounds__(kBlock) void ortho_product_kernel(const ProductArgs a)
+__global__ __launch_bounds__(kBlock, KOCC) void ortho_product_kernel(const ProductArgs a)
 {
     constexpr bool kBack = WHAT == UPDATE || WHAT == LAST;              // the right factor lies by rows of the contraction
     constexpr int  kRowA = kDepth + kPad, kRowB = kBack ? kTile + kPad : kDepth + kPad, kSizeB = kBack ? kDepth * kRowB : kTile * kRowB;
-    __shared__ __align__(16) _Float16 lds[2][2 * kTile * kRowA + 2 * kSizeB];
+    __shared__ __align__(16) _Float16 lds[kStages][2 * kTile * kRowA + 2 * kSizeB];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
     int ti, tj;
     if (kBack) {
@@ -144,41 +152,46 @@ __global__ __launch_bounds__(kBlock) void ortho_product_kernel(const ProductArgs
     const size_t z = blockIdx.z;
     const int i0 = ti * kTile, j0 = tj * kTile, wi = 64 * (wave & 1), wj = 64 * (wave >> 1);
 
-    uint4 r[8];
-    auto fetch = [&](const int k0) {
+    words_t r[8];
+    const _Float16 *pa = a.A.hi + z * a.A.each + (size_t)(i0 + ((int)threadIdx.x >> 2)) * a.A.stride + ((int)threadIdx.x & 3) * 8;
+    const _Float16 *pb = a.B.hi + z * a.B.each + (kBack ? (size_t)((int)threadIdx.x >> 4) * a.B.stride + j0 + ((int)threadIdx.x & 15) * 8
+                                                        : (size_t)(j0 + ((int)threadIdx.x >> 2)) * a.B.stride + ((int)threadIdx.x & 3) * 8);
+    const ptrdiff_t la = a.A.lo - a.A.hi, lb = a.B.lo - a.B.hi;
+    auto fetch = [&]() {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const int at = (int)threadIdx.x + i * kBlock;
-            const size_t pa = z * a.A.each + (size_t)(i0 + (at >> 2)) * a.A.stride + k0 + (at & 3) * 8;
-            r[i] = *reinterpret_cast<const uint4 *>(a.A.hi + pa);
-            r[2 + i] = *reinterpret_cast<const uint4 *>(a.A.lo + pa);
-            const size_t pb = z * a.B.each + (kBack ? (size_t)(k0 + (at >> 4)) * a.B.stride + j0 + (at & 15) * 8
-                                                    : (size_t)(j0 + (at >> 2)) * a.B.stride + k0 + (at & 3) * 8);
-            r[4 + i] = *reinterpret_cast<const uint4 *>(a.B.hi + pb);
-            r[6 + i] = *reinterpret_cast<const uint4 *>(a.B.lo + pb);
+            const _Float16 *qa = pa + (size_t)(64 * i) * a.A.stride, *qb = pb + (size_t)((kBack ? 16 : 64) * i) * a.B.stride;
+            r[i] = *reinterpret_cast<const words_t *>(qa);
+            r[2 + i] = *reinterpret_cast<const words_t *>(qa + la);
+            r[4 + i] = *reinterpret_cast<const words_t *>(qb);
+            r[6 + i] = *reinterpret_cast<const words_t *>(qb + lb);
         }
+        pa += kDepth;
+        pb += kBack ? (size_t)kDepth * a.B.stride : (size_t)kDepth;
     };
+    const int oa = ((int)threadIdx.x >> 2) * kRowA + ((int)threadIdx.x & 3) * 8, ob = kBack ? ((int)threadIdx.x >> 4) * kRowB + ((int)threadIdx.x & 15) * 8 : oa;
     auto keep = [&](_Float16 *to) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const int at = (int)threadIdx.x + i * kBlock, pa = (at >> 2) * kRowA + (at & 3) * 8, pb = kBack ? (at >> 4) * kRowB + (at & 15) * 8 : pa;
-            *reinterpret_cast<uint4 *>(to + pa) = r[i];
-            *reinterpret_cast<uint4 *>(to + kTile * kRowA + pa) = r[2 + i];
-            *reinterpret_cast<uint4 *>(to + 2 * kTile * kRowA + pb) = r[4 + i];
-            *reinterpret_cast<uint4 *>(to + 2 * kTile * kRowA + kSizeB + pb) = r[6 + i];
+            const int qa = oa + 64 * i * kRowA, qb = ob + (kBack ? 16 : 64) * i * kRowB;
+            *reinterpret_cast<words_t *>(to + qa) = r[i];
+            *reinterpret_cast<words_t *>(to + kTile * kRowA + qa) = r[2 + i];
+            *reinterpret_cast<words_t *>(to + 2 * kTile * kRowA + qb) = r[4 + i];
+            *reinterpret_cast<words_t *>(to + 2 * kTile * kRowA + kSizeB + qb) = r[6 + i];
         }
     };
 
-    acc_t high[2][2], low[2][2];
+    acc_t sum[2][2];
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int w = 0; w < 2; ++w) high[u][w] = low[u][w] = zero();
-    fetch(0);
-    for (int k0 = 0, b = 0; k0 < a.depth; k0 += kDepth, b ^= 1) {
+        for (int w = 0; w < 2; ++w) sum[u][w] = zero();
+    fetch();
+    for (int k0 = 0, b = 0; k0 < a.depth; k0 += kDepth, b ^= kStages - 1) {
+        if (kStages == 1) __syncthreads();
         keep(lds[b]);
         __syncthreads();
-        if (k0 + kDepth < a.depth) fetch(k0 + kDepth);
+        if (k0 + kDepth < a.depth) fetch();
         const _Float16 *A = lds[b], *B = lds[b] + 2 * kTile * kRowA;
 #pragma unroll
         for (int s = 0; s < kDepth / 16; ++s) {
@@ -198,13 +211,11 @@ __global__ __launch_bounds__(kBlock) void ortho_product_kernel(const ProductArgs
                 }
             }
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int which = 0; which < 3; ++which)
 #pragma unroll
-                for (int w = 0; w < 2; ++w) {
-                    high[u][w] = mfma(bh[w], ah[u], high[u][w]);
-                    low[u][w] = mfma(bh[w], al[u], low[u][w]);
-                    low[u][w] = mfma(bl[w], ah[u], low[u][w]);
-                }
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int w = 0; w < 2; ++w) sum[u][w] = mfma(which == 2 ? bl[w] : bh[w], which == 1 ? al[u] : ah[u], sum[u][w]);
         }
     }
 #pragma unroll
@@ -217,7 +228,7 @@ __global__ __launch_bounds__(kBlock) void ortho_product_kernel(const ProductArgs
                 const int j = j0 + wj + 32 * w + 8 * g + 4 * half;
                 float v[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = fmaf(low[u][w][4 * g + e], 1.0f / kLow, high[u][w][4 * g + e]) * a.of_sum;
+                for (int e = 0; e < 4; ++e) v[e] = sum[u][w][4 * g + e] * a.of_sum;
                 if (WHAT != GRAM) {
                     float d[4];
                     get4(a.D, z * a.D.each + (size_t)i * a.D.stride + j, d);
@@ -243,7 +254,6 @@ __global__ __launch_bounds__(kBlock) void ortho_product_kernel(const ProductArgs
 struct Shape {
     int    m, n, mp, np, parts;
     bool   turned;
-    float  scale;
     size_t x[2], a, b, norm, bytes;
 };
 Shape shape_of(const cngp_ortho_config *c) {
@@ -253,8 +263,6 @@ Shape shape_of(const cngp_ortho_config *c) {
     s.n = std::max(c->rows, c->cols);
     s.mp = (s.m + kTile - 1) / kTile * kTile;
     s.np = (s.n + kTile - 1) / kTile * kTile;
-    s.scale = 16.0f;                     // entries of an orthogonal matrix are about 1 / sqrt(n); the largest possible ones stay below 16 * 128 * 4
-    for (int r = 1; r < s.n; r *= 4) s.scale *= 2.0f;
     s.parts = (int)std::max<int64_t>(1, std::min<int64_t>((int64_t)s.m * s.n / 4096, std::max(1, kNormParts / std::max(1, std::min(c->batch, 8)))));
     size_t at = 0;
     auto take = [&](bool wanted, size_t bytes) { const size_t o = at; if (wanted) at += align256(bytes); return o; };
@@ -300,7 +308,7 @@ int norm_and_start(const cngp_ortho_config *c, const Shape &s, const T *g, T *ou
         return launch_status("ortho_scale_kernel");
     }
     ortho_start_kernel<T><<<dim3((unsigned)(s.np / 64), (unsigned)(s.mp / 64), (unsigned)c->batch), kBlock, 0, st>>>(g, c->rows, c->cols, s.turned, parts, s.parts, c->eps,
-                                                                                                                  s.scale, pair_of(ws, s.x[0], s.mp, s.np, c->batch));
+                                                                                                                  kScaleX, pair_of(ws, s.x[0], s.mp, s.np, c->batch));
     return launch_status("ortho_start_kernel");
 }
 
@@ -328,17 +336,17 @@ int cngp_orthogonalise(const cngp_ortho_config *cfg, const void *g, void *out, v
         ProductArgs p{};
         p.tiles_m = tm; p.tiles_n = tn;
         p.A = X; p.B = X; p.C = A; p.D = A;
-        p.depth = s.np; p.of_sum = kScaleA / (s.scale * s.scale);
+        p.depth = s.np; p.of_sum = kScaleA / (kScaleX * kScaleX);
         ortho_product_kernel<GRAM><<<dim3((unsigned)(tm * (tm + 1) / 2), 1, (unsigned)cfg->batch), kBlock, 0, st>>>(p);
         if (int rc = launch_status("ortho_product_kernel")) return rc;
         p.A = A; p.B = A; p.C = B; p.D = A;
-        p.depth = s.mp; p.of_sum = cfg->c / kScaleA; p.of_d = cfg->b;
+        p.depth = s.mp; p.of_sum = cfg->c * kScaleB / (kScaleA * kScaleA); p.of_d = cfg->b * kScaleB / kScaleA;
         ortho_product_kernel<POLY><<<dim3((unsigned)(tm * (tm + 1) / 2), 1, (unsigned)cfg->batch), kBlock, 0, st>>>(p);
         if (int rc = launch_status("ortho_product_kernel")) return rc;
         p.A = B; p.B = X; p.C = Y; p.D = X;
-        p.depth = s.mp; p.of_sum = 1.0f / kScaleA; p.of_d = cfg->a;
+        p.depth = s.mp; p.of_sum = 1.0f / kScaleB; p.of_d = cfg->a;
         if (last) {
-            p.of_sum /= s.scale; p.of_d /= s.scale;
+            p.of_sum /= kScaleX; p.of_d /= kScaleX;
             p.out = out; p.m = s.m; p.n = s.n; p.turned = s.turned; p.out_f16 = cfg->io_dtype == CNGP_F16;
             ortho_product_kernel<LAST><<<dim3((unsigned)(tm * tn), 1, (unsigned)cfg->batch), kBlock, 0, st>>>(p);
         } else ortho_product_kernel<UPDATE><<<dim3((unsigned)(tm * tn), 1, (unsigned)cfg->batch), kBlock, 0, st>>>(p);

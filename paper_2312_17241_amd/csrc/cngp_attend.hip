@@ -86,7 +86,7 @@ struct CarryArgs {
     const float *first;
     float       *final;
     int64_t      N;
-    int32_t      S, rows_each, heads, seg_rows, size, reverse;
+    int32_t      S, rows_each, heads, seg_shift, size, reverse;
 };
 __global__ __launch_bounds__(kBlock) void attend_carry_kernel(const CarryArgs a)
 {
@@ -95,10 +95,10 @@ __global__ __launch_bounds__(kBlock) void attend_carry_kernel(const CarryArgs a)
         const int     e = (int)(own % a.size), h = (int)(own / a.size % a.heads);
         const int32_t s = (int32_t)(own / a.size / a.heads);
         const Span    span = span_of(a.offsets, s, a.N, a.rows_each);
-        const int64_t n = (span.end - span.begin + a.seg_rows - 1) / a.seg_rows, base = piece_base(a.offsets, s, a.N, a.rows_each, a.seg_rows);
+        const int32_t n = (int32_t)(((uint32_t)(span.end - span.begin) + (1u << a.seg_shift) - 1) >> a.seg_shift), base = piece_base(span.begin, s, a.seg_shift);
         float state = a.first ? a.first[own] : 0.0f;
-        for (int64_t i = 0; i < n; ++i) {
-            const int64_t at = (base + (a.reverse ? n - 1 - i : i)) * a.heads + h;
+        for (int32_t i = 0; i < n; ++i) {
+            const int64_t at = (int64_t)(base + (a.reverse ? n - 1 - i : i)) * a.heads + h;
             float *p = a.states + (size_t)at * a.size + e;
             const float part = *p;
             *p = state;
@@ -122,6 +122,7 @@ struct DecayArgs {
     double      *parts;                              // [pieces, heads], or NULL
     int64_t      N, pieces;
     int32_t      S, rows_each, heads, size, anchor_size;
+    int32_t      kdim, vdim;                         // of the anchors' walks
 };
 __device__ __forceinline__ double wave_sum(double v) {
 #pragma unroll
@@ -138,23 +139,24 @@ __device__ __forceinline__ double upto(double v, const int lane) {
 }
 __global__ __launch_bounds__(64) void attend_decay_kernel(const DecayArgs a)
 {
-    constexpr int kRows = kAnchorChunks * kChunk;
+    constexpr int kRows = 1 << kAnchorShift;
     const int lane = threadIdx.x;
     for (int64_t item = blockIdx.x; item < a.pieces * a.heads; item += gridDim.x) {
         const int     h = (int)(item % a.heads);
         const int64_t piece = item / a.heads;
-        const int32_t seq = sequence_of(a.offsets, piece, a.N, a.S, a.rows_each, kRows);
+        const int32_t seq = sequence_of(a.offsets, (int32_t)piece, a.N, a.S, a.rows_each, kAnchorShift);
         const Span    span = span_of(a.offsets, seq, a.N, a.rows_each);
-        const int64_t i = piece - piece_base(a.offsets, seq, a.N, a.rows_each, kRows), begin = span.begin + i * kRows;
+        const int64_t i = piece - piece_base(span.begin, seq, kAnchorShift), begin = span.begin + i * kRows;
         const int64_t end = begin + kRows < span.end ? begin + kRows : span.end;
         double sum = 0.0;
         if (begin < end) {
             double D = 0.0;
             const int n = i ? a.anchor_size : a.size;
-            const size_t  at = i ? (size_t)(anchor_slot(span.begin, i * kAnchorChunks) * a.heads + h) * a.anchor_size : ((size_t)seq * a.heads + h) * a.size;
+            const size_t  at = i ? (size_t)(anchor_slot(span.begin, (int32_t)i * kAnchorChunks) * a.heads + h) * a.anchor_size : ((size_t)seq * a.heads + h) * a.size;
             const float *x = i ? a.states : a.h0, *y = i ? a.grads : a.dh0;
             if (x && y)
-                for (int e = lane; e < n; e += 64) D += (double)x[at + e] * (double)y[at + e];
+                for (int e = lane; e < n; e += 64)
+                    if (!i || (anchor_row(e, a.kdim) < a.kdim && anchor_column(e, a.kdim) < a.vdim)) D += (double)x[at + e] * (double)y[at + e];
             D = wave_sum(D);
             for (int64_t row0 = begin; row0 < end; row0 += kChunk) {
                 const bool   in = row0 + lane < end;
@@ -216,20 +218,21 @@ int check(const cngp_attend_config *c, int64_t N, int64_t S, bool ragged) {
     return CNGP_OK;
 }
 
-// How a call is cut: sequences whole, a workgroup per sequence and head, or in segments of `seg_rows` rows where that leaves most of the chip
+// How a call is cut: sequences whole, a workgroup per sequence and head, or in segments of 2^seg_shift rows where that leaves most of the chip
 // without work; then a walk without outputs gives the segments' parts first.
 struct Plan {
-    int32_t seg_rows;
+    int     seg_shift;
     int64_t segments;
 };
 constexpr int64_t kEnoughItems = 512;                 // two workgroups for each of 256 CUs
 Plan plan_of(const cngp_attend_config *c, int64_t N, int64_t S, bool ragged) {
     const int64_t mean = S ? (N + S - 1) / S : 0;
     const int64_t longest = !ragged ? mean : c->longest ? std::min<int64_t>(c->longest, N) : std::min<int64_t>(4 * mean, N);
-    int64_t R = (N * c->heads + kEnoughItems - 1) / kEnoughItems;
-    R = std::max<int64_t>((R + kChunk - 1) / kChunk * kChunk, 4 * kChunk);
-    if (longest <= 4 * R) return {0, S};
-    return {(int32_t)R, pieces(N, S, (int32_t)R)};
+    const int64_t R = (N * c->heads + kEnoughItems - 1) / kEnoughItems;
+    int shift = 8;
+    while (shift < 30 && (int64_t)1 << shift < R) ++shift;
+    if (longest <= (int64_t)4 << shift) return {0, S};
+    return {shift, pieces(N, S, shift)};
 }
 
 struct Space {
@@ -239,15 +242,15 @@ Space space_of(const cngp_attend_config *c, const Plan &p, int64_t N, int64_t S,
     Space sp{};
     size_t at = 0;
     auto take = [&](bool wanted, size_t bytes) { const size_t o = at; if (wanted) at += align256(bytes); return o; };
-    const bool   bwd = call & CNGP_ATTEND_CALL_BWD, cut = p.seg_rows != 0, shared = c->heads != c->kv_heads;
+    const bool   bwd = call & CNGP_ATTEND_CALL_BWD, cut = p.seg_shift != 0, shared = c->heads != c->kv_heads;
     const size_t H = (size_t)c->heads, size = (size_t)c->key_dim * c->value_dim, rows = (size_t)N;
     sp.states = take(cut, (size_t)p.segments * H * size * 4);
     sp.total = take(cut, (size_t)p.segments * H * 4);
     for (size_t *d : {&sp.near_q, &sp.far_q, &sp.near_k, &sp.far_k}) *d = take(bwd, rows * H * 4);
     const size_t slots = rows / (kAnchorChunks * kChunk) + 1;
-    sp.anchors_q = take(bwd, slots * H * anchor_floats(c->key_dim, c->value_dim) * 4);
-    sp.anchors_k = take(bwd, slots * H * anchor_floats(c->key_dim, c->value_dim) * 4);
-    sp.parts = take(bwd && !(c->flags & CNGP_ATTEND_ROW_DECAY), (size_t)pieces(N, S, kAnchorChunks * kChunk) * H * 8);
+    sp.anchors_q = take(bwd, slots * H * anchor_floats(c->value_dim, c->key_dim) * 4);
+    sp.anchors_k = take(bwd, slots * H * anchor_floats(c->value_dim, c->key_dim) * 4);
+    sp.parts = take(bwd && !(c->flags & CNGP_ATTEND_ROW_DECAY), (size_t)pieces(N, S, kAnchorShift) * H * 8);
     sp.dh0 = take(bwd, (size_t)S * H * size * 4);
     sp.part_k = take(bwd && shared, rows * H * (size_t)c->key_dim * 4);
     sp.part_v = take(bwd && shared, rows * H * (size_t)c->value_dim * 4);
@@ -275,7 +278,7 @@ struct Call {
         a.N = N; a.S = (int32_t)S; a.rows_each = (int32_t)(S ? N / S : 0);
         a.heads = c->heads; a.q_div = q_div; a.k_div = k_div; a.v_div = v_div; a.x_div = 1;
         a.kdim = kdim; a.vdim = vdim;
-        a.seg_rows = p.seg_rows; a.segments = (int32_t)p.segments;
+        a.seg_shift = p.seg_shift; a.segments = (int32_t)p.segments;
         a.first_i = a.final_i = vdim; a.first_j = a.final_j = 1;
         a.pair_scale = a.far_scale = a.state_scale = 1.0f;
         a.reverse = reverse; a.row_decay = (c->flags & CNGP_ATTEND_ROW_DECAY) != 0;
@@ -298,7 +301,7 @@ struct Call {
         if (int rc = walk(a, true)) return rc;
         CarryArgs k{};
         k.states = a.final; k.total = a.total; k.offsets = offsets; k.first = first; k.final = final;
-        k.N = N; k.S = (int32_t)S; k.rows_each = a.rows_each; k.heads = c->heads; k.seg_rows = p.seg_rows;
+        k.N = N; k.S = (int32_t)S; k.rows_each = a.rows_each; k.heads = c->heads; k.seg_shift = p.seg_shift;
         k.size = a.kdim * a.vdim; k.reverse = a.reverse;
         LaunchTimer t(s, K_ATTEND_STATES);
         attend_carry_kernel<<<(unsigned)std::min<int64_t>((S * c->heads * k.size + kBlock - 1) / kBlock, 1 << 20), kBlock, 0, s>>>(k);
@@ -362,7 +365,7 @@ int cngp_attend_fwd(const cngp_attend_config *cfg, const void *q, const void *k,
     a.pair_scale = a.far_scale = cfg->scale;
     a.first = h0;
     a.final = last;
-    if (call.p.seg_rows) {
+    if (call.p.seg_shift) {
         if (int rc = call.carry(a, h0, last)) return rc;
         if (!y) return CNGP_OK;
         a.first = (const float *)(call.ws + call.sp.states);
@@ -389,7 +392,7 @@ int cngp_attend_bwd(const cngp_attend_config *cfg, const void *q, const void *k,
     char *ws = call.ws;
     const Space &sp = call.sp;
     const int   group = cfg->heads / cfg->kv_heads, K = cfg->key_dim, V = cfg->value_dim;
-    const bool  cut = call.p.seg_rows != 0, shared = group > 1;
+    const bool  cut = call.p.seg_shift != 0, shared = group > 1;
     float      *states = (float *)(ws + sp.states);
     if (ddecay && h0 && !dh0) dh0 = (float *)(ws + sp.dh0);
 
@@ -404,7 +407,7 @@ int cngp_attend_bwd(const cngp_attend_config *cfg, const void *q, const void *k,
     a.first_i = 1; a.first_j = V;
     call.output(a, dq, false);
     if (ddecay) {
-        a.x = q; a.x_div = 1;
+        a.x = q; a.x_div = 1; a.vec_x = whole_rows(q, K, cfg->io_dtype, cfg->io_dtype == CNGP_F16 ? 8 : 16);
         a.dot_near = (float *)(ws + sp.near_q); a.dot_far = (float *)(ws + sp.far_q);
         a.anchors = (float *)(ws + sp.anchors_q);
     }
@@ -434,7 +437,7 @@ int cngp_attend_bwd(const cngp_attend_config *cfg, const void *q, const void *k,
     a.first_i = 1; a.first_j = V;
     call.output(a, shared ? (void *)(ws + sp.part_k) : dk, shared);
     if (ddecay) {
-        a.x = k; a.x_div = group;
+        a.x = k; a.x_div = group; a.vec_x = whole_rows(k, K, cfg->io_dtype, cfg->io_dtype == CNGP_F16 ? 8 : 16);
         a.dot_near = (float *)(ws + sp.near_k); a.dot_far = (float *)(ws + sp.far_k);
         a.anchors = (float *)(ws + sp.anchors_k);
     }
@@ -462,8 +465,9 @@ int cngp_attend_bwd(const cngp_attend_config *cfg, const void *q, const void *k,
     d.ddecay = rows ? ddecay : nullptr;
     d.parts = rows ? nullptr : (double *)(ws + sp.parts);
     d.N = N; d.S = (int32_t)sequences; d.rows_each = (int32_t)(N / sequences); d.heads = cfg->heads;
-    d.pieces = pieces(N, sequences, kAnchorChunks * kChunk);
-    d.size = K * V; d.anchor_size = (int32_t)anchor_floats(K, V);
+    d.pieces = pieces(N, sequences, kAnchorShift);
+    d.kdim = V; d.vdim = K;
+    d.size = K * V; d.anchor_size = (int32_t)anchor_floats(V, K);
     {
         LaunchTimer t(s, K_ATTEND_DECAY);
         attend_decay_kernel<<<(unsigned)std::min<int64_t>(d.pieces * d.heads, 0x3ffffff), 64, 0, s>>>(d);

@@ -1,13 +1,16 @@
 // The walk of the linear attention (WalkArgs in cngp_attend.h): a workgroup per sequence (or segment) and head goes over its chunks with the
-// state in registers.  Everything dense runs on the matrix cores, 32 x 32 x 16 products with fp32 sums:
+// state in registers.  Everything dense runs on the matrix cores, 32 x 32 x 16 products of fp16 operands with fp32 sums:
 //     scores of the pairs of rows       P^T = K Q^T                       (three of the four tiles: a row sees those up to it)
 //     outputs inside the chunk          O^T += V^T P^T,  far ones  O^T += S^T Q^T
 //     state                             S = e^F S + K^T (V e^(F - F_s))
 // A wavefront owns 32 columns of v: of the state, the accumulators themselves (lane = column of v, registers = columns of k), which are at
 // the same time the operand of S^T Q^T once they are rounded; the contraction's order is a permutation, the same for Q's reads.  Outputs
-// are formed transposed, a row of the chunk per lane, so that decays and products with another row are per lane too.
-// fp16 storage: q, k, v are exact operands; what is computed (scores, state, decayed v) would lose half of the result's accuracy if it
-// were rounded once, so it is split in two fp16 numbers (22 bits) and takes two products.  fp32 storage: fp32 products.
+// are formed transposed, a row of the chunk per lane, so that decays and products with another row are per lane too.  Scores pass from the
+// wavefronts that form them through LDS, or stay in registers where one wavefront does everything (the same permutation again).
+// Precision: rounding what is computed (scores, state, decayed v) to fp16 would cost half of the result's accuracy.  It is split in two fp16
+// numbers (22 bits) after a power of two has brought its largest value to 2^13, and takes two products.  fp16 storage: q, k, v are
+// exact operands.  fp32 storage: they are split as well, each row by a power of two of its own, and products take three (the fp32 products of
+// the matrix cores have a sixteenth of the rate: 4096 rays of 64 samples, 4 heads of 16, a walk 526 us).
 #pragma once
 #include "cngp_attend.h"
 #include "cngp_matrix.h"
@@ -17,429 +20,537 @@ namespace attend {
 
 using namespace mat;
 
-// Power of two that brings the largest finite of a wavefront's values to 2^13 .. 2^14, as an exponent (0 if all are 0).
-__device__ __forceinline__ int lift_of(float most) {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) most = fmaxf(most, __shfl_xor(most, d, 64));
-    const int e = (int)((__float_as_uint(most) >> 23) & 255u) - 127;
-    const int lift = 13 - e;
-    return most > 0.0f ? (lift > 120 ? 120 : lift < -120 ? -120 : lift) : 0;
-}
-__device__ __forceinline__ float most_of(const float most, const float v) {
-    const float a = fabsf(v);
-    return a <= 3.402823466e38f ? fmaxf(most, a) : most;
-}
-__device__ __forceinline__ float power_of_two(const int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
+// The same for the whole wavefront, and known to be: addresses formed from it are scalar.  (Rows are numbers below 2^31.)
+__device__ __forceinline__ Span scalar(const Span s) { return {__builtin_amdgcn_readfirstlane(s.begin), __builtin_amdgcn_readfirstlane(s.end)}; }
 
-// Registers of a thread's part of a tile [64, 32 TILES] on its way into LDS.
-template <typename T, int TILES, int WAVES>
+// A tile [64, W] of an array on its way into LDS: rows t of a chunk, `stride` values apart, `dim` of them (the rest and rows from `count` on are
+// 0).  Reverse walks take rows from the last to the first.  Where 16-byte pieces lie whole in the rows they are fetched into registers a chunk
+// ahead; else values are read one by one on the way.  Addresses are a scalar base and one 32-bit offset per lane.
+template <typename T, int W, int WAVES>
 struct Staged {
-    static constexpr int vec = Types<T>::vec, per_row = TILES * 32 / vec, each = kChunk * per_row / (WAVES * 64);
-    uint4 r[each];
+    static constexpr int per_row = W / 8, dealt = WAVES * 64 / per_row, rows = dealt < kChunk ? dealt : kChunk, each = kChunk / rows, words = sizeof(T) / 2, lds_stride = W + 8;
+    static_assert(rows * each == kChunk, "a tile is dealt out evenly");
+    words_t  r[each][words];
+    uint32_t offset;                     // bytes from the lowest row of a whole chunk
+    int      row;
 
-    // Rows lo + t dir of an array with `stride` values between rows, `dim` of them from `base` on; rows from `count` and columns from dim on are 0.
-    __device__ __forceinline__ void load(const T *base, const int64_t row0, const int dir, const int count, const int64_t stride, const int dim, const bool whole) {
+    __device__ __forceinline__ void begin(const int stride, const bool reverse) {
+        row = (int)threadIdx.x / per_row;
+        offset = (uint32_t)((reverse ? kChunk - 1 - row : row) * stride + (int)threadIdx.x % per_row * 8) * (uint32_t)sizeof(T);
+    }
+    // low: the row where a whole chunk would begin in memory
+    __device__ __forceinline__ void load(const T *low, const bool reverse, const int count, const int stride, const int dim, const bool whole) {
+        const int column = (int)threadIdx.x % per_row * 8;
+        if (!whole) return;
 #pragma unroll
         for (int i = 0; i < each; ++i) {
-            const int at = (int)threadIdx.x + i * WAVES * 64, t = at / per_row, c = at % per_row * vec;
-            r[i] = make_uint4(0, 0, 0, 0);
-            if (t < count && c < dim) {
-                const T *p = base + (row0 + (int64_t)t * dir) * stride + c;
-                if (whole) r[i] = *reinterpret_cast<const uint4 *>(p);
-                else {
-                    T e[vec];
+            const char *p = (const char *)(low + (int64_t)(reverse ? -i * rows : i * rows) * stride);
 #pragma unroll
-                    for (int j = 0; j < vec; ++j) e[j] = c + j < dim ? p[j] : (T)0.0f;
-                    __builtin_memcpy(&r[i], e, 16);
+            for (int w = 0; w < words; ++w) {
+                r[i][w] = words_t{0, 0, 0, 0};
+                if (column + (int)(16 / sizeof(T)) * w < dim && row + i * rows < count) r[i][w] = *reinterpret_cast<const words_t *>(p + 16 * w + offset);
+            }
+        }
+    }
+    // hi, lo: the parts of the tile; lift: of each row (fp32 only)
+    __device__ __forceinline__ void put(_Float16 *hi, _Float16 *lo, int *lift, const int t, const words_t (&v)[words]) const {
+        if (dealt > kChunk && t >= kChunk) return;
+        const int at = t * lds_stride + (int)threadIdx.x % per_row * 8;
+        if constexpr (sizeof(T) == 2) {
+            *reinterpret_cast<words_t *>(hi + at) = v[0];
+        } else {
+            float x[8];
+            __builtin_memcpy(x, &v, sizeof x);
+            float most = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x[e]));
+            const int up = lift_of_lanes<per_row>(most);
+            half8_t   h, l;
+            split(x, power_of_two(up), h, l);
+            *reinterpret_cast<half8_t *>(hi + at) = h;
+            *reinterpret_cast<half8_t *>(lo + at) = l;
+            if (threadIdx.x % per_row == 0) lift[t] = up;
+        }
+    }
+    __device__ __forceinline__ void store(_Float16 *hi, _Float16 *lo, int *lift, const T *low, const bool reverse, const int count, const int stride, const int dim,
+                                          const bool whole) const {
+        if (whole) {
+#pragma unroll
+            for (int i = 0; i < each; ++i) put(hi, lo, lift, row + i * rows, r[i]);
+            return;
+        }
+        const int column = (int)threadIdx.x % per_row * 8;
+#pragma unroll 1
+        for (int i = 0; i < each; ++i) {
+            const int t = row + i * rows;
+            T x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = (T)0.0f;
+            if (t < count) {
+                const T *p = low + (int64_t)(reverse ? kChunk - 1 - t : t) * stride;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int c = column + e < dim ? column + e : dim - 1;
+                    x[e] = column + e < dim ? p[c] : (T)0.0f;
                 }
             }
-        }
-    }
-    __device__ __forceinline__ void store(T *tile) const {
-#pragma unroll
-        for (int i = 0; i < each; ++i) {
-            const int at = (int)threadIdx.x + i * WAVES * 64, t = at / per_row, c = at % per_row * vec;
-            *reinterpret_cast<uint4 *>(tile + t * (TILES * 32 + Types<T>::pad) + c) = r[i];
+            words_t v[words];
+            __builtin_memcpy(&v, x, sizeof x);
+            put(hi, lo, lift, t, v);
         }
     }
 };
 
-template <typename T, int KT, int VT, bool OUT>
+constexpr int walk_threads(int KW, int VW) { return 64 * (((KW > VW ? KW : VW) + 31) / 32); }
+
+// Wavefronts of a SIMD that registers are left for: those that LDS leaves room for.
+constexpr int walk_per_simd(size_t value, int KW) { return value == 2 || KW < 128 ? 2 : 1; }
+
+// KW, VW: columns of k and v in a tile: 16, 32, 64 or 128.  Sums of 32 rows or columns where 16 are kept read what lies behind a row in LDS;
+// the rows and columns of the state that come of it are used by nothing.
+template <typename T, int KW, int VW, bool OUT>
 struct Lds {
-    static constexpr int kstride = 32 * KT + Types<T>::pad, vstride = 32 * VT + Types<T>::pad, pstride = 32 + Types<T>::pad;
+    static constexpr int parts = sizeof(T) / 2, kstride = KW + 8, vstride = VW + 8, pstride = 32 + 8, KT = (KW + 31) / 32, VT = (VW + 31) / 32;
     static constexpr int waves = KT > VT ? KT : VT;
-    double F[kChunk];                                       // log2 of the decay from the chunk's start
-    float  far[kChunk], keep[kChunk];                       // what a row takes from the state, and gives to it
-    double total;
+    static constexpr bool scores = OUT && waves > 1;        // pass through LDS
+    double F[2][kChunk];                                    // log2 of the decay from the chunk's start; this chunk's and the next one's
+    float  far[2][kChunk], keep[2][kChunk];                 // what a row takes from the state, and gives to it
+    double total[2];
     int    lift[4];                                         // of each score tile
+    int    up_q[parts == 2 ? kChunk : 1], up_k[parts == 2 ? kChunk : 1], up_v[parts == 2 ? kChunk : 1];
     float  dots[OUT ? 2 * waves : 1][kChunk];
-    alignas(16) T k[kChunk * kstride];
-    alignas(16) T v[kChunk * vstride];
-    alignas(16) T q[OUT ? kChunk * kstride : 8];
-    alignas(16) T p[OUT ? (sizeof(T) == 2 ? 2 : 1) * 3 * 32 * pstride : 8];
+    alignas(16) _Float16 k[parts][kChunk * kstride];
+    alignas(16) _Float16 q[parts][OUT ? kChunk * kstride : 8];
+    alignas(16) _Float16 v[parts][kChunk * vstride];
+    alignas(16) _Float16 p[2][scores ? 3 * 32 * pstride : 32];
 };
 
-template <typename T, int KT, int VT, bool OUT>
-__global__ __launch_bounds__(64 * (KT > VT ? KT : VT)) void attend_walk_kernel(const WalkArgs a)
+template <typename T, int KW, int VW, bool OUT>
+__global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW)) void attend_walk_kernel(const WalkArgs a)
 {
-    using L = Lds<T, KT, VT, OUT>;
-    constexpr int  WAVES = L::waves;
-    constexpr bool kSplit = sizeof(T) == 2;
+    using L = Lds<T, KW, VW, OUT>;
+    constexpr int  WAVES = L::waves, KT = L::KT, VT = L::VT, KS = KW / 16;
+    constexpr bool kEarly = EARLY;
+    constexpr bool kLow = sizeof(T) == 4;                   // the inputs have low parts too
     extern __shared__ __align__(16) char lds_raw[];
     L &lds = *reinterpret_cast<L *>(lds_raw);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
     const bool owns = wave < VT;
 
-    for (int64_t item = blockIdx.x; item < (int64_t)a.segments * a.heads; item += gridDim.x) {
-        const int h = (int)(item % a.heads);
-        const int64_t piece = item / a.heads;
-        const int32_t seq = a.seg_rows ? sequence_of(a.offsets, piece, a.N, a.S, a.rows_each, a.seg_rows) : (int32_t)piece;
-        const Span    span = span_of(a.offsets, seq, a.N, a.rows_each);
-        int64_t begin = span.begin, end = span.end;
-        int64_t chunk0 = 0;                                 // the first chunk's number in its sequence
-        if (a.seg_rows) {
-            const int64_t i = piece - piece_base(a.offsets, seq, a.N, a.rows_each, a.seg_rows);
-            begin += i * a.seg_rows;
-            if (begin >= end) continue;
-            end = begin + a.seg_rows < end ? begin + a.seg_rows : end;
-            chunk0 = i * (a.seg_rows / kChunk);
+    const int h = (int)blockIdx.x;
+    const int qs = a.heads / a.q_div * a.kdim, ks = a.heads / a.k_div * a.kdim, vs = a.heads / a.v_div * a.vdim;
+    const T *q = (const T *)a.q + h / a.q_div * a.kdim, *k = (const T *)a.k + h / a.k_div * a.kdim, *v = (const T *)a.v + h / a.v_div * a.vdim;
+    const int j = 32 * wave + col;                          // this lane's column of v
+    const bool mine_v = owns && j < a.vdim;
+
+    {
+        const int32_t piece = a.piece0 + (int32_t)blockIdx.y;
+        const int32_t seq = __builtin_amdgcn_readfirstlane(a.seg_shift ? sequence_of(a.offsets, piece, a.N, a.S, a.rows_each, a.seg_shift) : piece);
+        const Span    span = scalar(span_of(a.offsets, seq, a.N, a.rows_each));
+        int begin = span.begin, end = span.end;
+        int chunk0 = 0;                                     // the first chunk's number in its sequence
+        if (a.seg_shift) {
+            const int i = piece - piece_base(span.begin, seq, a.seg_shift);
+            if ((int64_t)begin + ((int64_t)i << a.seg_shift) >= end) return;
+            begin += i << a.seg_shift;
+            end = end - begin > 1 << a.seg_shift ? begin + (1 << a.seg_shift) : end;
+            chunk0 = i << (a.seg_shift - kChunkShift);
         }
-        const int64_t chunks = (end - begin + kChunk - 1) / kChunk;
-        const int64_t state_at = piece * a.heads + h;       // whole sequences: piece == sequence
-        const size_t  state_size = (size_t)a.kdim * a.vdim;
-        const int64_t qs = (int64_t)(a.heads / a.q_div) * a.kdim, ks = (int64_t)(a.heads / a.k_div) * a.kdim, vs = (int64_t)(a.heads / a.v_div) * a.vdim;
-        const T *q = (const T *)a.q + (size_t)(h / a.q_div) * a.kdim, *k = (const T *)a.k + (size_t)(h / a.k_div) * a.kdim,
-                *v = (const T *)a.v + (size_t)(h / a.v_div) * a.vdim;
+        const int chunks = (end - begin + kChunk - 1) >> kChunkShift;
+        const int64_t state_at = (int64_t)piece * a.heads + h;   // whole sequences: piece == sequence
+        const size_t  state_bytes = (size_t)(a.kdim * a.vdim) * 4;
 
         acc_t S[KT];
-        const int j = 32 * wave + col;                      // this lane's column of v
-#pragma unroll
-        for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int i = 32 * kt + 8 * (r >> 2) + 4 * half + (r & 3);
-                S[kt][r] = a.first && owns && i < a.kdim && j < a.vdim ? a.first[state_at * state_size + (size_t)i * a.first_i + (size_t)j * a.first_j] : 0.0f;
-            }
-
-        Staged<T, KT, WAVES> rq, rk;
-        Staged<T, VT, WAVES> rv;
-        float  rdecay = 0.0f;
-        double whole = 0.0;
-        // chunk c of the walk: its first row (reverse: its last), how many
-        auto place = [&](const int64_t c, int64_t &row0, int &count) {
-            const int64_t at = begin + (a.reverse ? chunks - 1 - c : c) * kChunk;
-            count = (int)(end - at < kChunk ? end - at : kChunk);
-            row0 = a.reverse ? at + count - 1 : at;
-        };
-        const int dir = a.reverse ? -1 : 1;
-        auto fetch = [&](const int64_t c) {
-            int64_t row0;
-            int     count;
-            place(c, row0, count);
-            if (OUT) rq.load(q, row0, dir, a.q ? count : 0, qs, a.kdim, a.vec_q);
-            rk.load(k, row0, dir, a.k ? count : 0, ks, a.kdim, a.vec_k);
-            rv.load(v, row0, dir, a.v ? count : 0, vs, a.vdim, a.vec_v);
-            if (wave == 0) rdecay = lane < count ? a.row_decay ? a.decay[(row0 + (int64_t)lane * dir) * a.heads + h] : a.decay[h] : 0.0f;
-        };
-        if (chunks > 0) fetch(0);
-        // the state at the start of a chunk (of this number in its sequence), as it lies in the registers
-        auto anchor = [&](const int64_t number) {
-            if (number == 0 || number % kAnchorChunks) return;
-            float *to = a.anchors + (size_t)(anchor_slot(span.begin, number) * a.heads + h) * (KT * VT * 1024) + wave * KT * 1024 + lane;
+        {
+            const char *from = a.first ? (const char *)a.first + state_at * state_bytes : nullptr;
+            uint32_t  at = (uint32_t)(4 * half * a.first_i + j * a.first_j) * 4;
+            const int left = a.kdim - 4 * half;
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) to[(kt * 16 + r) * 64] = S[kt][r];
+                for (int r = 0; r < 16; ++r) {
+                    S[kt][r] = 0.0f;
+                    if (from && mine_v && 32 * kt + 8 * (r >> 2) + (r & 3) < left) S[kt][r] = *reinterpret_cast<const float *>(from + at);
+                    at += (uint32_t)(r % 4 == 3 ? 5 : 1) * (uint32_t)a.first_i * 4;
+                }
+        }
+
+        const bool reverse = a.reverse;
+        Staged<T, KW, WAVES> rq, rk;
+        Staged<T, VW, WAVES> rv;
+        if (OUT) rq.begin(qs, reverse);
+        rk.begin(ks, reverse);
+        rv.begin(vs, reverse);
+        float  rdecay = 0.0f;
+        double whole = 0.0;
+        const int dir = reverse ? -1 : 1;
+        // chunk c of the walk: its first row (reverse: its last), how many, and the row where a whole chunk of these would begin in memory
+        auto place = [&](const int c, int &row0, int &count, int &low) {
+            const int at = begin + (reverse ? chunks - 1 - c : c) * kChunk;
+            count = end - at < kChunk ? end - at : kChunk;
+            row0 = reverse ? at + count - 1 : at;
+            low = reverse ? row0 - (kChunk - 1) : row0;
+        };
+        auto fetch = [&](const int c) {
+            int row0, low, count;
+            place(c, row0, count, low);
+            if (OUT) rq.load(q + (int64_t)low * qs, reverse, a.q ? count : 0, qs, a.kdim, a.vec_q);
+            rk.load(k + (int64_t)low * ks, reverse, a.k ? count : 0, ks, a.kdim, a.vec_k);
+            rv.load(v + (int64_t)low * vs, reverse, a.v ? count : 0, vs, a.vdim, a.vec_v);
+        };
+        // the decays of chunk c, by the last wavefront (which has the least to do with the scores), a chunk ahead; their loads another chunk ahead
+        auto fetch_decays = [&](const int c) {
+            int row0, low, count;
+            place(c, row0, count, low);
+            if (wave == WAVES - 1) rdecay = lane < count ? a.row_decay ? a.decay[(int64_t)(row0 + lane * dir) * a.heads + h] : a.decay[h] : 0.0f;
+        };
+        auto decays = [&](const int c) {
+            if (wave != WAVES - 1) return;
+            // below -110 a decay is 0 in fp32 however it is joined; bounded, sums of them stay exact enough to be subtracted
+            double f = (double)(rdecay < -110.0f ? -110.0f : rdecay) * 1.4426950408889634;
+            if (c + 1 < chunks) fetch_decays(c + 1);
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const double o = __shfl_up(f, d, 64);
+                if (lane >= d) f += o;
+            }
+            const double all = __shfl(f, 63, 64);
+            if (reverse) {
+                f = __shfl_up(f, 1, 64);
+                if (lane == 0) f = 0.0;
+            }
+            lds.F[c & 1][lane] = f;
+            lds.far[c & 1][lane] = __builtin_amdgcn_exp2f((float)f) * a.far_scale;
+            lds.keep[c & 1][lane] = __builtin_amdgcn_exp2f((float)(all - f)) * a.state_scale;
+            if (lane == 0) lds.total[c & 1] = all;
+        };
+        if (chunks > 0) {
+            fetch(0);
+            fetch_decays(0);
+            decays(0);
+        }
+        // the state at the start of a chunk (of this number in its sequence), as it lies in the registers
+        auto anchor = [&](const int number) {
+            if (number == 0 || number % kAnchorChunks) return;
+            float *to = a.anchors + ((size_t)anchor_slot(span.begin, number) * a.heads + h) * (KT * VT * 1024) + wave * KT * 1024 + lane;
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    to[(kt * 16 + r) * 64] = S[kt][r];
         };
 
-        for (int64_t c = 0; c < chunks; ++c) {
-            int64_t row0;
-            int     count;
-            place(c, row0, count);
-            if (OUT) rq.store(lds.q);
-            rk.store(lds.k);
-            rv.store(lds.v);
-            if (wave == 0) {
-                // below -110 a decay is 0 in fp32 however it is joined; bounded, sums of them stay exact enough to be subtracted
-                double g = (double)(rdecay < -110.0f ? -110.0f : rdecay) * 1.4426950408889634;
-                double f = g;
-#pragma unroll
-                for (int d = 1; d < 64; d <<= 1) {
-                    const double o = __shfl_up(f, d, 64);
-                    if (lane >= d) f += o;
-                }
-                const double all = __shfl(f, 63, 64);
-                if (a.reverse) {
-                    f = __shfl_up(f, 1, 64);
-                    if (lane == 0) f = 0.0;
-                }
-                lds.F[lane] = f;
-                lds.far[lane] = __builtin_amdgcn_exp2f((float)f) * a.far_scale;
-                lds.keep[lane] = __builtin_amdgcn_exp2f((float)(all - f)) * a.state_scale;
-                if (lane == 0) lds.total = all;
-            }
+        for (int c = 0; c < chunks; ++c) {
+            int row0, low, count;
+            place(c, row0, count, low);
+            if (OUT) rq.store(lds.q[0], lds.q[L::parts - 1], lds.up_q, q + (int64_t)low * qs, reverse, a.q ? count : 0, qs, a.kdim, a.vec_q);
+            rk.store(lds.k[0], lds.k[L::parts - 1], lds.up_k, k + (int64_t)low * ks, reverse, a.k ? count : 0, ks, a.kdim, a.vec_k);
+            rv.store(lds.v[0], lds.v[L::parts - 1], lds.up_v, v + (int64_t)low * vs, reverse, a.v ? count : 0, vs, a.vdim, a.vec_v);
             __syncthreads();
-            if (c + 1 < chunks) fetch(c + 1);
-            const double all = lds.total;
+            const int    now = c & 1;
+            const double all = lds.total[now];
             whole += all;
+            if (kEarly && c + 1 < chunks) fetch(c + 1);
+            if (c + 1 < chunks) decays(c + 1);
 
-            acc_t far[2];
-            if (OUT) {
-                // scores: tile (0, 0), (1, 0), (1, 1) of (rows, rows they look at)
-                for (int tile = wave; tile < 3; tile += WAVES) {
-                    const int tt = tile > 0, ss = tile > 1;
-                    acc_t p = zero();
-#pragma unroll
-                    for (int s = 0; s < 2 * KT; ++s)
-                        p = mfma(read8(lds.k + (32 * ss + col) * L::kstride + 16 * s + 8 * half), read8(lds.q + (32 * tt + col) * L::kstride + 16 * s + 8 * half), p);
-                    const int    t = 32 * tt + col;
-                    const double Ft = lds.F[t];
-                    float most = 0.0f;
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int s = 32 * ss + 8 * (r >> 2) + 4 * half + (r & 3);
-                        const float w = __builtin_amdgcn_exp2f((float)(Ft - lds.F[s])) * a.pair_scale;
-                        p[r] = s <= t ? p[r] * w : 0.0f;
-                        most = most_of(most, p[r]);
-                    }
-                    T *to = lds.p + (tile * 32 + col) * L::pstride + 4 * half;
-                    if constexpr (kSplit) {
-                        const int   lift = lift_of(most);
-                        const float up = power_of_two(lift);
-                        if (lane == 0) lds.lift[tile] = lift;
-#pragma unroll
-                        for (int g = 0; g < 4; ++g) {
-                            half4_t hi, lo;
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const float y = p[4 * g + e] * up;
-                                hi[e] = (_Float16)y;
-                                lo[e] = (_Float16)((y - (float)hi[e]) * kLow);
-                            }
-                            *reinterpret_cast<half4_t *>(to + 8 * g) = hi;
-                            *reinterpret_cast<half4_t *>(to + 3 * 32 * L::pstride + 8 * g) = lo;
-                        }
-                    } else {
-#pragma unroll
-                        for (int g = 0; g < 4; ++g) {
-                            float4_t w;
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) w[e] = p[4 * g + e];
-                            *reinterpret_cast<float4_t *>(to + 8 * g) = w;
-                        }
+            // scores of rows 32 tt .. (lanes) with rows 32 ss .. (registers) and the decay between them, and the power of two they are brought up by
+            [[maybe_unused]] auto score = [&](const int tt, const int ss, acc_t &p) -> int {
+                p = zero();
+                if constexpr (!OUT) return 0;
+                const int qa = (32 * tt + col) * L::kstride + 8 * half, ka = (32 * ss + col) * L::kstride + 8 * half;
+#pragma unroll 2
+                for (int s = 0; s < KS; ++s) {
+                    const half8_t kh = read8(lds.k[0] + ka + 16 * s), qh = read8(lds.q[0] + qa + 16 * s);
+                    p = mfma(kh, qh, p);
+                    if constexpr (kLow) {
+                        p = mfma(read8(lds.k[1] + ka + 16 * s), qh, p);
+                        p = mfma(kh, read8(lds.q[1] + qa + 16 * s), p);
                     }
                 }
-                // what the rows take from the state
-                if (owns) {
-                    acc_t low[2];
-                    far[0] = far[1] = low[0] = low[1] = zero();
-                    int lift = 0;
-                    if constexpr (kSplit) {
-                        float most = 0.0f;
+                apart();
+                const int    t = 32 * tt + anew(col);
+                const double Ft = lds.F[now][t];
+                const int    qt = kLow ? lds.up_q[t] : 0;
+                float most = 0.0f;
 #pragma unroll
-                        for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-                            for (int r = 0; r < 16; ++r) most = most_of(most, S[kt][r]);
-                        lift = lift_of(most);
-                    }
+                for (int r = 0; r < 16; ++r) {
+                    const int s = 32 * ss + 8 * (r >> 2) + 4 * half + (r & 3);
+                    float x = p[r] * (__builtin_amdgcn_exp2f((float)(Ft - lds.F[now][s])) * a.pair_scale);
+                    if constexpr (kLow) x = ldexpf(x, -(qt + lds.up_k[s] + lds.up_v[s]));
+                    p[r] = s <= t ? x : 0.0f;
+                    most = fmaxf(most, fabsf(p[r]));
+                    if (r % 4 == 3) apart();
+                }
+                return lift_of(most);
+            };
+
+            if constexpr (L::scores) {
+                for (int tile = wave; tile < 3; tile += WAVES) {
+                    acc_t p;
+                    const int   lift = score(tile > 0, tile > 1, p);
                     const float up = power_of_two(lift);
+                    if (lane == 0) lds.lift[tile] = lift;
+                    _Float16 *to = lds.p[0] + (tile * 32 + col) * L::pstride + 4 * half;
 #pragma unroll
-                    for (int s = 0; s < 2 * KT; ++s) {
-                        float x[8];
+                    for (int g = 0; g < 4; ++g) {
+                        half4_t hi, lo;
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) x[i] = S[s >> 1][8 * (s & 1) + i];
-                        frag_t<T> hi, lo;
-                        if constexpr (kSplit) split(x, up, hi, lo);
-                        else
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) hi[i] = x[i];
-#pragma unroll
-                        for (int tt = 0; tt < 2; ++tt) {
-                            const frag_t<T> b = read4_4(lds.q + (32 * tt + col) * L::kstride + 16 * s + 4 * half);
-                            far[tt] = mfma(hi, b, far[tt]);
-                            if constexpr (kSplit) low[tt] = mfma(lo, b, low[tt]);
+                        for (int e = 0; e < 4; ++e) {
+                            const float y = p[4 * g + e] * up;
+                            hi[e] = (_Float16)y;
+                            lo[e] = (_Float16)(y - (float)hi[e]);
                         }
+                        *reinterpret_cast<half4_t *>(to + 8 * g) = hi;
+                        *reinterpret_cast<half4_t *>(to + 3 * 32 * L::pstride + 8 * g) = lo;
                     }
-                    const float down = power_of_two(-lift);
+                }
+                apart();
+            }
+            acc_t far[2];
+            if (OUT && owns) {           // what the rows take from the state
+                far[0] = far[1] = zero();
+                float most = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 8 * KS; ++i) most = fmaxf(most, fabsf(S[i >> 4][i & 15]));
+                const int   lift = lift_of(mine_v ? most : 0.0f);
+                const float up = power_of_two(lift);
+#pragma unroll
+                for (int s = 0; s < KS; ++s) {
+                    float x[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[i] = S[s >> 1][8 * (s & 1) + i];
+                    half8_t hi, lo;
+                    split(x, up, hi, lo);
 #pragma unroll
                     for (int tt = 0; tt < 2; ++tt) {
-                        const float f = lds.far[32 * tt + col];
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) far[tt][r] = (kSplit ? fmaf(low[tt][r], 1.0f / kLow, far[tt][r]) * down : far[tt][r]) * f;
+                        const int     at = (32 * tt + col) * L::kstride + 16 * s + 4 * half;
+                        const half8_t b = read4_4(lds.q[0] + at);
+                        far[tt] = mfma(hi, b, far[tt]);
+                        far[tt] = mfma(lo, b, far[tt]);
+                        if constexpr (kLow) far[tt] = mfma(hi, read4_4(lds.q[1] + at), far[tt]);
                     }
+                    if (s & 1) apart();
                 }
-            }
-            // the state behind the chunk
-            if (owns) {
-                if (a.anchors && !a.reverse) anchor(chunk0 + c);
-                float    x[4][8];
-                int      lift = 0;
-                float    most = 0.0f;
 #pragma unroll
-                for (int s = 0; s < 4; ++s) {
-                    const frag_t<T> b = read_column(lds.v, L::vstride, 16 * s, 32 * wave, lane);
+                for (int tt = 0; tt < 2; ++tt) {
+                    const float f = ldexpf(lds.far[now][32 * tt + col], -(lift + (kLow ? lds.up_q[32 * tt + col] : 0)));
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) far[tt][r] *= f;
+                }
+                apart();
+            }
+            if (owns) {                  // the state behind the chunk
+                if (a.anchors && !reverse) anchor(chunk0 + c);
+                // rows 16 s + 8 half .. + 7 of this lane's column, decayed to the chunk's end
+                auto decayed = [&](const int s, float (&x)[8]) {
+                    const half8_t b = read_column(lds.v[0], L::vstride, 16 * s, 32 * wave, lane);
+                    half8_t l = b;
+                    if constexpr (kLow) l = read_column(lds.v[1], L::vstride, 16 * s, 32 * wave, lane);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        x[s][i] = (float)b[i] * lds.keep[16 * s + 8 * half + i];
-                        if constexpr (kSplit) most = most_of(most, x[s][i]);
+                        const int t = 16 * s + 8 * half + i;
+                        x[i] = kLow ? ((float)b[i] + (float)l[i]) * ldexpf(lds.keep[now][t], -(lds.up_k[t] + lds.up_v[t])) : (float)b[i] * lds.keep[now][t];
                     }
-                }
-                if constexpr (kSplit) {
-                    lift = lift_of(most);
-                    lift = lift > 60 ? 60 : lift;
-                }
-                const float tot = __builtin_amdgcn_exp2f((float)all) * power_of_two(lift), up = power_of_two(lift), down = power_of_two(-lift);
-                acc_t low[KT];
+                };
+                float most = 0.0f;
+#pragma unroll 1
+                for (int s = 0; s < 4; ++s) {
+                    float x[8];
+                    decayed(s, x);
 #pragma unroll
-                for (int kt = 0; kt < KT; ++kt) {
-                    low[kt] = zero();
+                    for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(x[i]));
+                }
+                const int   lift = lift_of(mine_v ? most : 0.0f, 60);
+                const float up = power_of_two(lift), down = power_of_two(-lift), tot = __builtin_amdgcn_exp2f((float)all) * up;
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) S[kt][r] *= tot;
-                }
-#pragma unroll
+                apart();
+#pragma unroll 1
                 for (int s = 0; s < 4; ++s) {
-                    frag_t<T> hi, lo;
-                    if constexpr (kSplit) split(x[s], up, hi, lo);
-                    else
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) hi[i] = x[s][i];
+                    float   x[8];
+                    half8_t hi, lo;
+                    decayed(s, x);
+                    split(x, up, hi, lo);
 #pragma unroll
                     for (int kt = 0; kt < KT; ++kt) {
-                        const frag_t<T> w = read_column(lds.k, L::kstride, 16 * s, 32 * kt, lane);
+                        const half8_t w = read_column(lds.k[0], L::kstride, 16 * s, 32 * kt, lane);
                         S[kt] = mfma(w, hi, S[kt]);
-                        if constexpr (kSplit) low[kt] = mfma(w, lo, low[kt]);
+                        S[kt] = mfma(w, lo, S[kt]);
+                        if constexpr (kLow) S[kt] = mfma(read_column(lds.k[1], L::kstride, 16 * s, 32 * kt, lane), hi, S[kt]);
                     }
+                    apart();
                 }
-                if constexpr (kSplit)
 #pragma unroll
-                    for (int kt = 0; kt < KT; ++kt)
+                for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) S[kt][r] = fmaf(low[kt][r], 1.0f / kLow, S[kt][r]) * down;
-                if (a.anchors && a.reverse) anchor(chunk0 + chunks - 1 - c);
+                    for (int r = 0; r < 16; ++r) S[kt][r] *= down;
+                if (a.anchors && reverse) anchor(chunk0 + chunks - 1 - c);
+                apart();
             }
-            if (OUT) {
-                __syncthreads();                            // the scores are there
-                if (owns) {
-                    acc_t near[2];
-                    near[0] = near[1] = zero();
+            if (!kEarly && c + 1 < chunks) fetch(c + 1);
+            if (L::scores) __syncthreads();                 // they are there
+            if (OUT && owns) {
+                const int     os = a.heads * a.vdim, xs = a.heads / a.x_div * a.vdim;
+                const int     t0 = reverse ? kChunk - 1 - col : col, j0 = 32 * wave + 4 * half, left = anew(a.vdim - j0);       // columns from j0 on
+#pragma unroll 1
+                for (int tt = 0; tt < 2; ++tt) {
+                    acc_t near = zero(), far_t;
 #pragma unroll
-                    for (int tile = 0; tile < 3; ++tile) {
-                        const int tt = tile > 0, ss = tile > 1;
-                        acc_t hi = zero(), lo = zero();
+                    for (int r = 0; r < 16; ++r) far_t[r] = tt ? far[1][r] : far[0][r];
+#pragma unroll 1
+                    for (int ss = 0; ss <= tt; ++ss) {
+                        acc_t sum = zero(), p;
+                        int   lift;
+                        if constexpr (L::scores) lift = lds.lift[tt + ss];
+                        else lift = score(tt, ss, p);
 #pragma unroll
                         for (int s = 0; s < 2; ++s) {
-                            const frag_t<T> w = read_column(lds.v, L::vstride, 32 * ss + 16 * s, 32 * wave, lane);
-                            const T *p = lds.p + (tile * 32 + col) * L::pstride + 16 * s + 8 * half;
-                            hi = mfma(w, read8(p), hi);
-                            if constexpr (kSplit) lo = mfma(w, read8(p + 3 * 32 * L::pstride), lo);
+                            half8_t hi, lo;
+                            if constexpr (L::scores) {
+                                const _Float16 *from = lds.p[0] + ((tt + ss) * 32 + col) * L::pstride + 16 * s + 8 * half;
+                                hi = read8(from);
+                                lo = read8(from + 3 * 32 * L::pstride);
+                            } else {
+                                float y[8];
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) y[i] = p[8 * s + i];
+                                split(y, power_of_two(lift), hi, lo);
+                            }
+                            const half8_t w = read_column<!L::scores>(lds.v[0], L::vstride, 32 * ss + 16 * s, 32 * wave, lane);
+                            sum = mfma(w, hi, sum);
+                            sum = mfma(w, lo, sum);
+                            if constexpr (kLow) sum = mfma(read_column<!L::scores>(lds.v[1], L::vstride, 32 * ss + 16 * s, 32 * wave, lane), hi, sum);
                         }
-                        const float down = kSplit ? power_of_two(-lds.lift[tile]) : 1.0f;
+                        const float down = power_of_two(-lift);
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) near[tt][r] += kSplit ? fmaf(lo[r], 1.0f / kLow, hi[r]) * down : hi[r];
+                        for (int r = 0; r < 16; ++r) near[r] = fmaf(sum[r], down, near[r]);
+                        apart();
                     }
-                    const int64_t os = (int64_t)a.heads * a.vdim, xs = (int64_t)(a.heads / a.x_div) * a.vdim;
-#pragma unroll
-                    for (int tt = 0; tt < 2; ++tt) {
-                        const int t = 32 * tt + col;
-                        const bool there = t < count;
-                        const int64_t row = row0 + (int64_t)(there ? t : 0) * dir;
-                        float dn = 0.0f, df = 0.0f;
+                    const int  t = 32 * tt + col;
+                    const bool there = t < count;
+                    const int  base = low + (reverse ? -32 * tt : 32 * tt);
+                    float dn = 0.0f, df = 0.0f;
+                    if (a.x && there) {
+                        const T *x = (const T *)a.x + h / a.x_div * a.vdim + (int64_t)base * xs;
+                        const uint32_t mine = (uint32_t)(t0 * xs + j0);
 #pragma unroll
                         for (int g = 0; g < 4; ++g) {
-                            const int j0 = 32 * wave + 8 * g + 4 * half;
+                            float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                            if (a.vec_x) {
+                                if (8 * g < left) {
+                                    T e4[4];
+                                    __builtin_memcpy(e4, (x + 8 * g) + mine, sizeof e4);
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e) v[e] = (float)e4[e];
+                                }
+                            } else {
+#pragma unroll
+                                for (int e = 0; e < 4; ++e)
+                                    if (8 * g + e < left) v[e] = (float)(x + 8 * g + e)[mine];
+                            }
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (8 * g + e < left) {
+                                    dn = fmaf(near[4 * g + e], v[e], dn);
+                                    df = fmaf(far_t[4 * g + e], v[e], df);
+                                }
+                        }
+                    }
+                    if (there) {
+                        const uint32_t mine = (uint32_t)(t0 * os + j0);
+                        float    *to32 = (float *)a.out + h * a.vdim + (int64_t)base * os;
+                        _Float16 *to16 = (_Float16 *)a.out + h * a.vdim + (int64_t)base * os;
+#pragma unroll
+                        for (int g = 0; g < 4; ++g) {
                             float o[4];
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) o[e] = near[tt][4 * g + e] + far[tt][4 * g + e];
-                            if (a.x && there) {
-                                const T *x = (const T *)a.x + (size_t)(h / a.x_div) * a.vdim + row * xs + j0;
+                            for (int e = 0; e < 4; ++e) o[e] = near[4 * g + e] + far_t[4 * g + e];
+                            if (a.vec_out) {
+                                if (8 * g < left) {
+                                    if (kLow || a.out_f32) *reinterpret_cast<float4_t *>((to32 + 8 * g) + mine) = float4_t{o[0], o[1], o[2], o[3]};
+                                    else *reinterpret_cast<half4_t *>((to16 + 8 * g) + mine) = half4_t{(_Float16)o[0], (_Float16)o[1], (_Float16)o[2], (_Float16)o[3]};
+                                }
+                            } else {
 #pragma unroll
-                                for (int e = 0; e < 4; ++e) {
-                                    const float xe = j0 + e < a.vdim ? (float)x[e] : 0.0f;
-                                    dn = j0 + e < a.vdim ? fmaf(near[tt][4 * g + e], xe, dn) : dn;
-                                    df = j0 + e < a.vdim ? fmaf(far[tt][4 * g + e], xe, df) : df;
-                                }
-                            }
-                            if (there && j0 < a.vdim) {
-                                const size_t at = (size_t)(row * os) + (size_t)h * a.vdim + j0;
-                                if (a.out_f32 || !kSplit) {
-                                    float *to = (float *)a.out + at;
-                                    if (a.vec_out) *reinterpret_cast<float4_t *>(to) = float4_t{o[0], o[1], o[2], o[3]};
-                                    else
-                                        for (int e = 0; e < 4; ++e)
-                                            if (j0 + e < a.vdim) to[e] = o[e];
-                                } else {
-                                    _Float16 *to = (_Float16 *)a.out + at;
-                                    if (a.vec_out) *reinterpret_cast<half4_t *>(to) = half4_t{(_Float16)o[0], (_Float16)o[1], (_Float16)o[2], (_Float16)o[3]};
-                                    else
-                                        for (int e = 0; e < 4; ++e)
-                                            if (j0 + e < a.vdim) to[e] = (_Float16)o[e];
-                                }
-                            }
-                        }
-                        if (a.x) {
-                            dn += __shfl_xor(dn, 32, 64);
-                            df += __shfl_xor(df, 32, 64);
-                            if (half == 0) {
-                                lds.dots[2 * wave][t] = dn;
-                                lds.dots[2 * wave + 1][t] = df;
+                                for (int e = 0; e < 4; ++e)
+                                    if (8 * g + e < left) {
+                                        if (kLow || a.out_f32) (to32 + 8 * g + e)[mine] = o[e];
+                                        else (to16 + 8 * g + e)[mine] = (_Float16)o[e];
+                                    }
                             }
                         }
                     }
+                    if (a.x) {
+                        dn += __shfl_xor(dn, 32, 64);
+                        df += __shfl_xor(df, 32, 64);
+                        if (half == 0) {
+                            lds.dots[2 * wave][t] = dn;
+                            lds.dots[2 * wave + 1][t] = df;
+                        }
+                    }
+                    apart();
                 }
-                if (a.x) {
-                    __syncthreads();
-                    if (threadIdx.x < kChunk && (int)threadIdx.x < count) {
-                        float dn = 0.0f, df = 0.0f;
+            }
+            if (OUT && a.x) {
+                __syncthreads();
+                if (threadIdx.x < kChunk && (int)threadIdx.x < count) {
+                    float dn = 0.0f, df = 0.0f;
 #pragma unroll
-                        for (int w = 0; w < VT; ++w) {
-                            dn += lds.dots[2 * w][threadIdx.x];
-                            df += lds.dots[2 * w + 1][threadIdx.x];
-                        }
-                        const size_t at = (size_t)h * a.N + (size_t)(row0 + (int64_t)threadIdx.x * dir);
-                        a.dot_near[at] = dn;
-                        a.dot_far[at] = df;
+                    for (int w = 0; w < VT; ++w) {
+                        dn += lds.dots[2 * w][threadIdx.x];
+                        df += lds.dots[2 * w + 1][threadIdx.x];
                     }
+                    const size_t at = (size_t)h * a.N + (size_t)(row0 + (int)threadIdx.x * dir);
+                    a.dot_near[at] = dn;
+                    a.dot_far[at] = df;
                 }
             }
             __syncthreads();                                // the tiles may be written again
         }
         if (a.total && threadIdx.x == 0) a.total[state_at] = (float)whole;
-        if (a.final && owns && j < a.vdim)
+        if (a.final && mine_v) {
+            char     *to = (char *)a.final + state_at * state_bytes;
+            uint32_t  at = (uint32_t)(4 * half * a.final_i + j * a.final_j) * 4;
+            const int left = anew(a.kdim - 4 * half);
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const int i = 32 * kt + 8 * (r >> 2) + 4 * half + (r & 3);
-                    if (i < a.kdim) a.final[state_at * state_size + (size_t)i * a.final_i + (size_t)j * a.final_j] = S[kt][r];
+                    if (32 * kt + 8 * (r >> 2) + (r & 3) < left) *reinterpret_cast<float *>(to + at) = S[kt][r];
+                    at += (uint32_t)(r % 4 == 3 ? 5 : 1) * (uint32_t)a.final_i * 4;
                 }
+        }
     }
 }
 
-template <typename T, int KT, int VT, bool OUT>
+template <typename T, int KW, int VW, bool OUT>
 int launch(const WalkArgs &a, hipStream_t s) {
-    using L = Lds<T, KT, VT, OUT>;
+    using L = Lds<T, KW, VW, OUT>;
     if (sizeof(L) > 64 * 1024)
-        if (hipError_t e = hipFuncSetAttribute((const void *)attend_walk_kernel<T, KT, VT, OUT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(L)))
+        if (hipError_t e = hipFuncSetAttribute((const void *)attend_walk_kernel<T, KW, VW, OUT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(L)))
             return record_hip_failure(e, "hipFuncSetAttribute(MaxDynamicSharedMemorySize)");
-    const int64_t items = (int64_t)a.segments * a.heads;
-    LaunchTimer t(s, OUT ? K_ATTEND_WALK : K_ATTEND_STATES);
-    attend_walk_kernel<T, KT, VT, OUT><<<(unsigned)std::min<int64_t>(items, kMostGroups256), 64 * L::waves, sizeof(L), s>>>(a);
-    return launch_status("attend_walk_kernel");
+    // a workgroup goes over one piece: a loop over pieces would have the addresses of the states' entries formed before it and kept in registers
+    const int most = (int)std::min<int64_t>(65535, kMostGroups256 / a.heads);
+    for (int first = 0; first < a.segments; first += most) {
+        WalkArgs part = a;
+        part.piece0 = first;
+        LaunchTimer t(s, OUT ? K_ATTEND_WALK : K_ATTEND_STATES);
+        attend_walk_kernel<T, KW, VW, OUT><<<dim3((unsigned)a.heads, (unsigned)std::min(a.segments - first, most)), 64 * L::waves, sizeof(L), s>>>(part);
+        if (int rc = launch_status("attend_walk_kernel")) return rc;
+    }
+    return CNGP_OK;
 }
 
+template <typename T, bool OUT, int KW>
+int launch_columns(const WalkArgs &a, hipStream_t s) {
+    return a.vdim <= 16 ? launch<T, KW, 16, OUT>(a, s) : a.vdim <= 32 ? launch<T, KW, 32, OUT>(a, s) : a.vdim <= 64 ? launch<T, KW, 64, OUT>(a, s) : launch<T, KW, 128, OUT>(a, s);
+}
 template <typename T, bool OUT>
 int launch_tiles(const WalkArgs &a, hipStream_t s) {
-    switch (tiles_of(a.kdim) * 8 + tiles_of(a.vdim)) {
-        case 8 + 1: return launch<T, 1, 1, OUT>(a, s);
-        case 8 + 2: return launch<T, 1, 2, OUT>(a, s);
-        case 8 + 4: return launch<T, 1, 4, OUT>(a, s);
-        case 16 + 1: return launch<T, 2, 1, OUT>(a, s);
-        case 16 + 2: return launch<T, 2, 2, OUT>(a, s);
-        case 16 + 4: return launch<T, 2, 4, OUT>(a, s);
-        case 32 + 1: return launch<T, 4, 1, OUT>(a, s);
-        case 32 + 2: return launch<T, 4, 2, OUT>(a, s);
-        default: return launch<T, 4, 4, OUT>(a, s);
-    }
+    return a.kdim <= 16 ? launch_columns<T, OUT, 16>(a, s) : a.kdim <= 32 ? launch_columns<T, OUT, 32>(a, s) : a.kdim <= 64 ? launch_columns<T, OUT, 64>(a, s)
+                                                                                                          : launch_columns<T, OUT, 128>(a, s);
 }
 
 }  // namespace attend

@@ -37,7 +37,7 @@ struct WalkArgs {
     int32_t      first_i, first_j, final_i, final_j;   // strides of the states' two dimensions
     float        pair_scale, far_scale, state_scale;
     int32_t      reverse, row_decay, out_f32;
-    int32_t      vec_q, vec_k, vec_v, vec_out, vec_x;  // 16-byte pieces (out, x: four values) lie whole and aligned in a row
+    int32_t      whole;                  // every array's 16-byte pieces (out, x: four values) lie whole and aligned in its rows
 };
 
 // Rows [begin, end) of sequence s.

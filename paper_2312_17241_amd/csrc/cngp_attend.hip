@@ -282,13 +282,13 @@ struct Call {
         a.first_i = a.final_i = vdim; a.first_j = a.final_j = 1;
         a.pair_scale = a.far_scale = a.state_scale = 1.0f;
         a.reverse = reverse; a.row_decay = (c->flags & CNGP_ATTEND_ROW_DECAY) != 0;
-        a.vec_q = whole_rows(q, kdim, c->io_dtype, 16); a.vec_k = whole_rows(k, kdim, c->io_dtype, 16); a.vec_v = whole_rows(v, vdim, c->io_dtype, 16);
+        a.whole = whole_rows(q, kdim, c->io_dtype, 16) && whole_rows(k, kdim, c->io_dtype, 16) && whole_rows(v, vdim, c->io_dtype, 16);
         return a;
     }
     void output(WalkArgs &a, void *out, bool f32) const {
         a.out = out;
         a.out_f32 = f32 || c->io_dtype == CNGP_F32;
-        a.vec_out = a.vdim % 4 == 0 && ((uintptr_t)out & (a.out_f32 ? 15u : 7u)) == 0;
+        a.whole = a.whole && a.vdim % 4 == 0 && ((uintptr_t)out & (a.out_f32 ? 15u : 7u)) == 0;
     }
     int walk(const WalkArgs &a, bool states_only) const {
         return c->io_dtype == CNGP_F16 ? attend_walk_f16(a, states_only, s) : attend_walk_f32(a, states_only, s);
@@ -407,7 +407,7 @@ int cngp_attend_bwd(const cngp_attend_config *cfg, const void *q, const void *k,
     a.first_i = 1; a.first_j = V;
     call.output(a, dq, false);
     if (ddecay) {
-        a.x = q; a.x_div = 1; a.vec_x = whole_rows(q, K, cfg->io_dtype, cfg->io_dtype == CNGP_F16 ? 8 : 16);
+        a.x = q; a.x_div = 1; a.whole = a.whole && whole_rows(q, K, cfg->io_dtype, cfg->io_dtype == CNGP_F16 ? 8 : 16);
         a.dot_near = (float *)(ws + sp.near_q); a.dot_far = (float *)(ws + sp.far_q);
         a.anchors = (float *)(ws + sp.anchors_q);
     }
@@ -437,7 +437,7 @@ int cngp_attend_bwd(const cngp_attend_config *cfg, const void *q, const void *k,
     a.first_i = 1; a.first_j = V;
     call.output(a, shared ? (void *)(ws + sp.part_k) : dk, shared);
     if (ddecay) {
-        a.x = k; a.x_div = group; a.vec_x = whole_rows(k, K, cfg->io_dtype, cfg->io_dtype == CNGP_F16 ? 8 : 16);
+        a.x = k; a.x_div = group; a.whole = a.whole && whole_rows(k, K, cfg->io_dtype, cfg->io_dtype == CNGP_F16 ? 8 : 16);
         a.dot_near = (float *)(ws + sp.near_k); a.dot_far = (float *)(ws + sp.far_k);
         a.anchors = (float *)(ws + sp.anchors_k);
     }

@@ -26,7 +26,7 @@ __device__ __forceinline__ Span scalar(const Span s) { return {__builtin_amdgcn_
 // A tile [64, W] of an array on its way into LDS: rows t of a chunk, `stride` values apart, `dim` of them (the rest and rows from `count` on are
 // 0).  Reverse walks take rows from the last to the first.  Where 16-byte pieces lie whole in the rows they are fetched into registers a chunk
 // ahead; else values are read one by one on the way.  Addresses are a scalar base and one 32-bit offset per lane.
-template <typename T, int W, int WAVES>
+template <typename T, int W, int WAVES, bool WHOLE>
 struct Staged {
     static constexpr int per_row = W / 8, dealt = WAVES * 64 / per_row, rows = dealt < kChunk ? dealt : kChunk, each = kChunk / rows, words = sizeof(T) / 2, lds_stride = W + 8;
     static_assert(rows * each == kChunk, "a tile is dealt out evenly");
@@ -39,9 +39,9 @@ struct Staged {
         offset = (uint32_t)((reverse ? kChunk - 1 - row : row) * stride + (int)threadIdx.x % per_row * 8) * (uint32_t)sizeof(T);
     }
     // low: the row where a whole chunk would begin in memory
-    __device__ __forceinline__ void load(const T *low, const bool reverse, const int count, const int stride, const int dim, const bool whole) {
+    __device__ __forceinline__ void load(const T *low, const bool reverse, const int count, const int stride, const int dim) {
         const int column = (int)threadIdx.x % per_row * 8;
-        if (!whole) return;
+        if constexpr (!WHOLE) return;
 #pragma unroll
         for (int i = 0; i < each; ++i) {
             const char *p = (const char *)(low + (int64_t)(reverse ? -i * rows : i * rows) * stride);
@@ -72,9 +72,8 @@ struct Staged {
             if (threadIdx.x % per_row == 0) lift[t] = up;
         }
     }
-    __device__ __forceinline__ void store(_Float16 *hi, _Float16 *lo, int *lift, const T *low, const bool reverse, const int count, const int stride, const int dim,
-                                          const bool whole) const {
-        if (whole) {
+    __device__ __forceinline__ void store(_Float16 *hi, _Float16 *lo, int *lift, const T *low, const bool reverse, const int count, const int stride, const int dim) const {
+        if constexpr (WHOLE) {
 #pragma unroll
             for (int i = 0; i < each; ++i) put(hi, lo, lift, row + i * rows, r[i]);
             return;
@@ -101,9 +100,11 @@ struct Staged {
     }
 };
 
-constexpr int walk_threads(int KW, int VW) { return 64 * (((KW > VW ? KW : VW) + 31) / 32); }
-
-// Wavefronts of a SIMD that registers are left for: those that LDS leaves room for.
+// Wavefronts of a workgroup: one for each 32 columns of v, by two where k has more than 32 (each keeps one half of the state's rows, and takes one half
+// of the chunk's rows for the outputs).  One wavefront on a SIMD waits most of the time, so what it does in a row is kept short.
+constexpr int walk_halves(int KW) { return KW > 32 ? 2 : 1; }
+constexpr int walk_threads(int KW, int VW) { return 64 * ((VW + 31) / 32) * walk_halves(KW); }
+// Wavefronts of a SIMD that registers are left for.
 constexpr int walk_per_simd(size_t value, int KW) { return value == 2 || KW < 128 ? 2 : 1; }
 
 // KW, VW: columns of k and v in a tile: 16, 32, 64 or 128.  Sums of 32 rows or columns where 16 are kept read what lies behind a row in LDS;
@@ -111,389 +112,434 @@ constexpr int walk_per_simd(size_t value, int KW) { return value == 2 || KW < 12
 template <typename T, int KW, int VW, bool OUT>
 struct Lds {
     static constexpr int parts = sizeof(T) / 2, kstride = KW + 8, vstride = VW + 8, pstride = 32 + 8, KT = (KW + 31) / 32, VT = (VW + 31) / 32;
-    static constexpr int waves = KT > VT ? KT : VT;
+    static constexpr int halves = walk_halves(KW), waves = VT * halves;
     static constexpr bool scores = OUT && waves > 1;        // pass through LDS
     double F[2][kChunk];                                    // log2 of the decay from the chunk's start; this chunk's and the next one's
     float  far[2][kChunk], keep[2][kChunk];                 // what a row takes from the state, and gives to it
+    float  from[2][kChunk], to[2][kChunk];                  // decay between two rows as a product, where the chunk's are mild: to[t] * from[s]
     double total[2];
+    int    mild[2];
     int    lift[4];                                         // of each score tile
     int    up_q[parts == 2 ? kChunk : 1], up_k[parts == 2 ? kChunk : 1], up_v[parts == 2 ? kChunk : 1];
-    float  dots[OUT ? 2 * waves : 1][kChunk];
-    alignas(16) _Float16 k[parts][kChunk * kstride];
-    alignas(16) _Float16 q[parts][OUT ? kChunk * kstride : 8];
+    float  dots[OUT ? 2 * VT : 1][kChunk];
+    union {
+        struct {
+            alignas(16) _Float16 k[parts][kChunk * kstride];
+            alignas(16) _Float16 q[parts][OUT ? kChunk * kstride : 8];
+        };
+        float far_half[OUT && halves == 2 ? waves : 1][16][64];     // when both tiles have been used: far outputs of the other half's rows
+    };
     alignas(16) _Float16 v[parts][kChunk * vstride];
     alignas(16) _Float16 p[2][scores ? 3 * 32 * pstride : 32];
 };
 
-template <typename T, int KW, int VW, bool OUT>
+// A chunk's decays are mild where none is more than 2^kMild away from the middle row's: two factors in place of an exponential per pair
+// of rows then, and the later row's outside the sums.  (A tile of scores spans 2^(2 kMild) by that, of the 2^28 that its high parts hold.)
+constexpr double kMild = 6.0;
+
+// Sum over the lanes 0 .. own: moves inside rows of 16 lanes, then broadcasts of the rows' last ones.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double moved(const double v) {
+    const uint64_t w = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)w, CTRL, ROWS, 0xF, ROWS == 0xF);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(w >> 32), CTRL, ROWS, 0xF, ROWS == 0xF);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ double sum_upto(double v) {
+    v += moved<0x111, 0xF>(v);
+    v += moved<0x112, 0xF>(v);
+    v += moved<0x114, 0xF>(v);
+    v += moved<0x118, 0xF>(v);
+    v += moved<0x142, 0xA>(v);
+    v += moved<0x143, 0xC>(v);
+    return v;
+}
+
+template <typename T, int KW, int VW, bool OUT, bool WHOLE>
 __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW)) void attend_walk_kernel(const WalkArgs a)
 {
     using L = Lds<T, KW, VW, OUT>;
-    constexpr int  WAVES = L::waves, KT = L::KT, VT = L::VT, KS = KW / 16;
-    constexpr bool kEarly = EARLY;
+    constexpr int  WAVES = L::waves, VT = L::VT, KT = L::KT, HALVES = L::halves, KP = KT / HALVES;
+    constexpr int  KS = KW / 16 / HALVES;                   // steps of 16 columns of k that a wavefront keeps
     constexpr bool kLow = sizeof(T) == 4;                   // the inputs have low parts too
     extern __shared__ __align__(16) char lds_raw[];
     L &lds = *reinterpret_cast<L *>(lds_raw);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
-    const bool owns = wave < VT;
-
-    const int h = (int)blockIdx.x;
+    const int vt = wave % VT, kh = wave / VT;               // this wavefront's columns of v; its half of the columns of k, and of the chunk's rows
+    // Workgroups go to the eight XCDs in turn, each with an L2 of its own: neighbouring heads, which share keys or lines of memory, to the same one.
+    const uint32_t each = gridDim.x >> 3, rest = gridDim.x & 7, xcd = blockIdx.x & 7, item = xcd * each + (xcd < rest ? xcd : rest) + (blockIdx.x >> 3);
+    const int h = (int)(item % (uint32_t)a.heads);
     const int qs = a.heads / a.q_div * a.kdim, ks = a.heads / a.k_div * a.kdim, vs = a.heads / a.v_div * a.vdim;
     const T *q = (const T *)a.q + h / a.q_div * a.kdim, *k = (const T *)a.k + h / a.k_div * a.kdim, *v = (const T *)a.v + h / a.v_div * a.vdim;
-    const int j = 32 * wave + col;                          // this lane's column of v
-    const bool mine_v = owns && j < a.vdim;
+    const int j = 32 * vt + col;                            // this lane's column of v
+    const bool mine_v = j < a.vdim;
 
+    const int32_t piece = a.piece0 + (int32_t)(item / (uint32_t)a.heads);
+    const int32_t seq = __builtin_amdgcn_readfirstlane(a.seg_shift ? sequence_of(a.offsets, piece, a.N, a.S, a.rows_each, a.seg_shift) : piece);
+    const Span    span = scalar(span_of(a.offsets, seq, a.N, a.rows_each));
+    int begin = span.begin, end = span.end;
+    int chunk0 = 0;                                         // the first chunk's number in its sequence
+    if (a.seg_shift) {
+        const int i = piece - piece_base(span.begin, seq, a.seg_shift);
+        if ((int64_t)begin + ((int64_t)i << a.seg_shift) >= end) return;
+        begin += i << a.seg_shift;
+        end = end - begin > 1 << a.seg_shift ? begin + (1 << a.seg_shift) : end;
+        chunk0 = i << (a.seg_shift - kChunkShift);
+    }
+    const int chunks = (end - begin + kChunk - 1) >> kChunkShift;
+    const int64_t state_at = (int64_t)piece * a.heads + h;  // whole sequences: piece == sequence
+    const size_t  state_bytes = (size_t)(a.kdim * a.vdim) * 4;
+    const bool    reverse = a.reverse;
+    const int     dir = reverse ? -1 : 1;
+
+    // chunk c of the walk: its first row (reverse: its last), how many, and the row where a whole chunk of these would begin in memory
+    auto place = [&](const int c, int &row0, int &count, int &low) {
+        const int at = begin + (reverse ? chunks - 1 - c : c) * kChunk;
+        count = end - at < kChunk ? end - at : kChunk;
+        row0 = reverse ? at + count - 1 : at;
+        low = reverse ? row0 - (kChunk - 1) : row0;
+    };
+    Staged<T, KW, WAVES, WHOLE> rq, rk;
+    Staged<T, VW, WAVES, WHOLE> rv;
+    if (OUT) rq.begin(qs, reverse);
+    rk.begin(ks, reverse);
+    rv.begin(vs, reverse);
+    auto fetch = [&](const int c) {
+        int row0, low, count;
+        place(c, row0, count, low);
+        if (OUT) rq.load(q + (int64_t)low * qs, reverse, a.q ? count : 0, qs, a.kdim);
+        rk.load(k + (int64_t)low * ks, reverse, a.k ? count : 0, ks, a.kdim);
+        rv.load(v + (int64_t)low * vs, reverse, a.v ? count : 0, vs, a.vdim);
+    };
+    // the decays of chunk c, by the last wavefront (which has the least to do with the scores), a chunk ahead; their loads another chunk ahead
+    float  rdecay = 0.0f;
+    double whole = 0.0;
+    auto fetch_decays = [&](const int c) {
+        int row0, low, count;
+        place(c, row0, count, low);
+        if (wave == WAVES - 1) rdecay = lane < count ? a.row_decay ? a.decay[(int64_t)(row0 + lane * dir) * a.heads + h] : a.decay[h] : 0.0f;
+    };
+    auto decays = [&](const int c) {
+        if (wave != WAVES - 1) return;
+        // below -110 a decay is 0 in fp32 however it is joined; bounded, sums of them stay exact enough to be subtracted
+        const double g = (double)(rdecay < -110.0f ? -110.0f : rdecay) * 1.4426950408889634, f = sum_upto(g);
+        if (c + 1 < chunks) fetch_decays(c + 1);
+        const double all = __shfl(f, 63, 64), mine = reverse ? f - g : f;
+        lds.F[c & 1][lane] = mine;
+        lds.far[c & 1][lane] = __builtin_amdgcn_exp2f((float)mine) * a.far_scale;
+        lds.keep[c & 1][lane] = __builtin_amdgcn_exp2f((float)(all - mine)) * a.state_scale;
+        const double middle = __shfl(mine, 31, 64);
+        lds.to[c & 1][lane] = __builtin_amdgcn_exp2f((float)(mine - middle));
+        lds.from[c & 1][lane] = __builtin_amdgcn_exp2f((float)(middle - mine));
+        const bool mild = __all(fabs(mine - middle) <= kMild);
+        if (lane == 0) {
+            lds.total[c & 1] = all;
+            lds.mild[c & 1] = mild;
+        }
+    };
+    if (chunks > 0) {
+        fetch_decays(0);
+        fetch(0);
+    }
+
+    acc_t S[KP];
     {
-        const int32_t piece = a.piece0 + (int32_t)blockIdx.y;
-        const int32_t seq = __builtin_amdgcn_readfirstlane(a.seg_shift ? sequence_of(a.offsets, piece, a.N, a.S, a.rows_each, a.seg_shift) : piece);
-        const Span    span = scalar(span_of(a.offsets, seq, a.N, a.rows_each));
-        int begin = span.begin, end = span.end;
-        int chunk0 = 0;                                     // the first chunk's number in its sequence
-        if (a.seg_shift) {
-            const int i = piece - piece_base(span.begin, seq, a.seg_shift);
-            if ((int64_t)begin + ((int64_t)i << a.seg_shift) >= end) return;
-            begin += i << a.seg_shift;
-            end = end - begin > 1 << a.seg_shift ? begin + (1 << a.seg_shift) : end;
-            chunk0 = i << (a.seg_shift - kChunkShift);
-        }
-        const int chunks = (end - begin + kChunk - 1) >> kChunkShift;
-        const int64_t state_at = (int64_t)piece * a.heads + h;   // whole sequences: piece == sequence
-        const size_t  state_bytes = (size_t)(a.kdim * a.vdim) * 4;
-
-        acc_t S[KT];
-        {
-            const char *from = a.first ? (const char *)a.first + state_at * state_bytes : nullptr;
-            uint32_t  at = (uint32_t)(4 * half * a.first_i + j * a.first_j) * 4;
-            const int left = a.kdim - 4 * half;
+        const char *from = a.first ? (const char *)a.first + state_at * state_bytes : nullptr;
+        uint32_t  at = (uint32_t)((32 * KP * kh + 4 * half) * a.first_i + j * a.first_j) * 4;
+        const int left = a.kdim - 32 * KP * kh - 4 * half;
 #pragma unroll
-            for (int kt = 0; kt < KT; ++kt)
+        for (int kt = 0; kt < KP; ++kt)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    S[kt][r] = 0.0f;
-                    if (from && mine_v && 32 * kt + 8 * (r >> 2) + (r & 3) < left) S[kt][r] = *reinterpret_cast<const float *>(from + at);
-                    at += (uint32_t)(r % 4 == 3 ? 5 : 1) * (uint32_t)a.first_i * 4;
-                }
-        }
-
-        const bool reverse = a.reverse;
-        Staged<T, KW, WAVES> rq, rk;
-        Staged<T, VW, WAVES> rv;
-        if (OUT) rq.begin(qs, reverse);
-        rk.begin(ks, reverse);
-        rv.begin(vs, reverse);
-        float  rdecay = 0.0f;
-        double whole = 0.0;
-        const int dir = reverse ? -1 : 1;
-        // chunk c of the walk: its first row (reverse: its last), how many, and the row where a whole chunk of these would begin in memory
-        auto place = [&](const int c, int &row0, int &count, int &low) {
-            const int at = begin + (reverse ? chunks - 1 - c : c) * kChunk;
-            count = end - at < kChunk ? end - at : kChunk;
-            row0 = reverse ? at + count - 1 : at;
-            low = reverse ? row0 - (kChunk - 1) : row0;
-        };
-        auto fetch = [&](const int c) {
-            int row0, low, count;
-            place(c, row0, count, low);
-            if (OUT) rq.load(q + (int64_t)low * qs, reverse, a.q ? count : 0, qs, a.kdim, a.vec_q);
-            rk.load(k + (int64_t)low * ks, reverse, a.k ? count : 0, ks, a.kdim, a.vec_k);
-            rv.load(v + (int64_t)low * vs, reverse, a.v ? count : 0, vs, a.vdim, a.vec_v);
-        };
-        // the decays of chunk c, by the last wavefront (which has the least to do with the scores), a chunk ahead; their loads another chunk ahead
-        auto fetch_decays = [&](const int c) {
-            int row0, low, count;
-            place(c, row0, count, low);
-            if (wave == WAVES - 1) rdecay = lane < count ? a.row_decay ? a.decay[(int64_t)(row0 + lane * dir) * a.heads + h] : a.decay[h] : 0.0f;
-        };
-        auto decays = [&](const int c) {
-            if (wave != WAVES - 1) return;
-            // below -110 a decay is 0 in fp32 however it is joined; bounded, sums of them stay exact enough to be subtracted
-            double f = (double)(rdecay < -110.0f ? -110.0f : rdecay) * 1.4426950408889634;
-            if (c + 1 < chunks) fetch_decays(c + 1);
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const double o = __shfl_up(f, d, 64);
-                if (lane >= d) f += o;
+            for (int r = 0; r < 16; ++r) {
+                S[kt][r] = 0.0f;
+                if (from && mine_v && 32 * kt + 8 * (r >> 2) + (r & 3) < left) S[kt][r] = *reinterpret_cast<const float *>(from + at);
+                at += (uint32_t)(r % 4 == 3 ? 5 : 1) * (uint32_t)a.first_i * 4;
             }
-            const double all = __shfl(f, 63, 64);
-            if (reverse) {
-                f = __shfl_up(f, 1, 64);
-                if (lane == 0) f = 0.0;
-            }
-            lds.F[c & 1][lane] = f;
-            lds.far[c & 1][lane] = __builtin_amdgcn_exp2f((float)f) * a.far_scale;
-            lds.keep[c & 1][lane] = __builtin_amdgcn_exp2f((float)(all - f)) * a.state_scale;
-            if (lane == 0) lds.total[c & 1] = all;
-        };
-        if (chunks > 0) {
-            fetch(0);
-            fetch_decays(0);
-            decays(0);
+    }
+    int up = 0;                          // the state is kept times 2^up, the scale of what is added to it
+    // the state at the start of a chunk (of this number in its sequence), as it lies in the registers
+    auto anchor = [&](const int number) {
+        if (number == 0 || number % kAnchorChunks) return;
+        float *to = a.anchors + ((size_t)anchor_slot(span.begin, number) * a.heads + h) * (KT * VT * 1024) + (vt * KT + kh * KP) * 1024 + lane;
+        const float f = power_of_two(-up);
+#pragma unroll
+        for (int kt = 0; kt < KP; ++kt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) to[(kt * 16 + r) * 64] = S[kt][r] * f;
+    };
+    if (chunks > 0) decays(0);
+
+    for (int c = 0; c < chunks; ++c) {
+        const int now = c & 1;
+        int row0, low, count;
+        place(c, row0, count, low);
+        if (OUT) rq.store(lds.q[0], lds.q[L::parts - 1], lds.up_q, q + (int64_t)low * qs, reverse, a.q ? count : 0, qs, a.kdim);
+        rk.store(lds.k[0], lds.k[L::parts - 1], lds.up_k, k + (int64_t)low * ks, reverse, a.k ? count : 0, ks, a.kdim);
+        rv.store(lds.v[0], lds.v[L::parts - 1], lds.up_v, v + (int64_t)low * vs, reverse, a.v ? count : 0, vs, a.vdim);
+        __syncthreads();
+        const double all = lds.total[now];
+        whole += all;
+        if (c + 1 < chunks) {
+            if (!OUT) fetch(c + 1);
+            decays(c + 1);
         }
-        // the state at the start of a chunk (of this number in its sequence), as it lies in the registers
-        auto anchor = [&](const int number) {
-            if (number == 0 || number % kAnchorChunks) return;
-            float *to = a.anchors + ((size_t)anchor_slot(span.begin, number) * a.heads + h) * (KT * VT * 1024) + wave * KT * 1024 + lane;
-#pragma unroll
-            for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    to[(kt * 16 + r) * 64] = S[kt][r];
-        };
 
-        for (int c = 0; c < chunks; ++c) {
-            int row0, low, count;
-            place(c, row0, count, low);
-            if (OUT) rq.store(lds.q[0], lds.q[L::parts - 1], lds.up_q, q + (int64_t)low * qs, reverse, a.q ? count : 0, qs, a.kdim, a.vec_q);
-            rk.store(lds.k[0], lds.k[L::parts - 1], lds.up_k, k + (int64_t)low * ks, reverse, a.k ? count : 0, ks, a.kdim, a.vec_k);
-            rv.store(lds.v[0], lds.v[L::parts - 1], lds.up_v, v + (int64_t)low * vs, reverse, a.v ? count : 0, vs, a.vdim, a.vec_v);
-            __syncthreads();
-            const int    now = c & 1;
-            const double all = lds.total[now];
-            whole += all;
-            if (kEarly && c + 1 < chunks) fetch(c + 1);
-            if (c + 1 < chunks) decays(c + 1);
-
-            // scores of rows 32 tt .. (lanes) with rows 32 ss .. (registers) and the decay between them, and the power of two they are brought up by
-            [[maybe_unused]] auto score = [&](const int tt, const int ss, acc_t &p) -> int {
-                p = zero();
-                if constexpr (!OUT) return 0;
-                const int qa = (32 * tt + col) * L::kstride + 8 * half, ka = (32 * ss + col) * L::kstride + 8 * half;
-#pragma unroll 2
-                for (int s = 0; s < KS; ++s) {
-                    const half8_t kh = read8(lds.k[0] + ka + 16 * s), qh = read8(lds.q[0] + qa + 16 * s);
-                    p = mfma(kh, qh, p);
-                    if constexpr (kLow) {
-                        p = mfma(read8(lds.k[1] + ka + 16 * s), qh, p);
-                        p = mfma(kh, read8(lds.q[1] + qa + 16 * s), p);
-                    }
+        const bool mild = OUT && __builtin_amdgcn_readfirstlane(lds.mild[now]);
+        // scores of rows 32 tt .. (lanes) with rows 32 ss .. (registers), the decay between them (without the later row's part where mild), and the
+        // power of two they are brought up by; what is the same for a row is left to the sums over ss
+        [[maybe_unused]] auto score = [&](const int tt, const int ss, acc_t &p) -> int {
+            p = zero();
+            if constexpr (!OUT) return 0;
+            const int qa = (32 * tt + col) * L::kstride + 8 * half, ka = (32 * ss + col) * L::kstride + 8 * half;
+#pragma unroll
+            for (int s = 0; s < KW / 16; ++s) {
+                const half8_t kf = read8(lds.k[0] + ka + 16 * s), qf = read8(lds.q[0] + qa + 16 * s);
+                p = mfma(kf, qf, p);
+                if constexpr (kLow) {
+                    p = mfma(read8(lds.k[1] + ka + 16 * s), qf, p);
+                    p = mfma(kf, read8(lds.q[1] + qa + 16 * s), p);
                 }
-                apart();
-                const int    t = 32 * tt + anew(col);
-                const double Ft = lds.F[now][t];
-                const int    qt = kLow ? lds.up_q[t] : 0;
-                float most = 0.0f;
+            }
+            float most = 0.0f;
+            if (mild) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int s = 32 * ss + 8 * (r >> 2) + 4 * half + (r & 3);
-                    float x = p[r] * (__builtin_amdgcn_exp2f((float)(Ft - lds.F[now][s])) * a.pair_scale);
-                    if constexpr (kLow) x = ldexpf(x, -(qt + lds.up_k[s] + lds.up_v[s]));
-                    p[r] = s <= t ? x : 0.0f;
-                    most = fmaxf(most, fabsf(p[r]));
-                    if (r % 4 == 3) apart();
+                    p[r] *= lds.from[now][s];
+                    if constexpr (kLow) p[r] = ldexpf(p[r], -(lds.up_k[s] + lds.up_v[s]));
                 }
-                return lift_of(most);
-            };
+            } else {
+                const double Ft = lds.F[now][32 * tt + col];
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int s = 32 * ss + 8 * (r >> 2) + 4 * half + (r & 3);
+                    p[r] *= __builtin_amdgcn_exp2f((float)(Ft - lds.F[now][s]));
+                    if constexpr (kLow) p[r] = ldexpf(p[r], -(lds.up_k[s] + lds.up_v[s]));
+                }
+            }
+            if (ss == tt) {
+                const int t = anew(col - 4 * half);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) p[r] = 8 * (r >> 2) + (r & 3) <= t ? p[r] : 0.0f;
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) most = fmaxf(most, fabsf(p[r]));
+            return lift_of(most);
+        };
+        if constexpr (L::scores) {
+            for (int tile = wave; tile < 3; tile += WAVES) {
+                acc_t p;
+                const int   lift = score(tile > 0, tile > 1, p);
+                const float f = power_of_two(lift);
+                if (lane == 0) lds.lift[tile] = lift;
+                _Float16 *to = lds.p[0] + (tile * 32 + col) * L::pstride + 4 * half;
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    half4_t hi, lo;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        hi[e] = (_Float16)(p[4 * g + e] * f);
+                        lo[e] = (_Float16)fmaf(p[4 * g + e], f, -(float)hi[e]);
+                    }
+                    *reinterpret_cast<half4_t *>(to + 8 * g) = hi;
+                    *reinterpret_cast<half4_t *>(to + 3 * 32 * L::pstride + 8 * g) = lo;
+                }
+            }
+            apart();
+        }
 
-            if constexpr (L::scores) {
-                for (int tile = wave; tile < 3; tile += WAVES) {
-                    acc_t p;
-                    const int   lift = score(tile > 0, tile > 1, p);
-                    const float up = power_of_two(lift);
-                    if (lane == 0) lds.lift[tile] = lift;
-                    _Float16 *to = lds.p[0] + (tile * 32 + col) * L::pstride + 4 * half;
+        int lift = 0;                    // brings the state into the range of its fp16 parts
+        if (OUT) {
+            float most = 0.0f;
 #pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        half4_t hi, lo;
+            for (int i = 0; i < 8 * KS; ++i) most = fmaxf(most, fabsf(S[i >> 4][i & 15]));
+            lift = lift_of(mine_v ? most : 0.0f);
+        }
+        // what rows 32 tt .. take from this wavefront's part of the state
+        const float lifted = power_of_two(lift);
+        auto part_of_state = [&](const int tt) -> acc_t {
+            acc_t far = zero();
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float y = p[4 * g + e] * up;
-                            hi[e] = (_Float16)y;
-                            lo[e] = (_Float16)(y - (float)hi[e]);
+            for (int s = 0; s < KS; ++s) {
+                float x[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = S[s >> 1][8 * (s & 1) + i];
+                half8_t hi, lo;
+                split(x, lifted, hi, lo);
+                const int     at = (32 * tt + col) * L::kstride + 16 * (KS * kh + s) + 4 * half;
+                const half8_t b = read4_4(lds.q[0] + at);
+                far = mfma(hi, b, far);
+                far = mfma(lo, b, far);
+                if constexpr (kLow) far = mfma(hi, read4_4(lds.q[1] + at), far);
+            }
+            const float f = ldexpf(lds.far[now][32 * tt + col], -(up + lift + (kLow ? lds.up_q[32 * tt + col] : 0)));
+#pragma unroll
+            for (int r = 0; r < 16; ++r) far[r] *= f;
+            return far;
+        };
+        acc_t far, other;                // of this wavefront's rows, and of the other half's
+        if constexpr (OUT && HALVES == 2) {
+            far = part_of_state(kh);
+            other = part_of_state(1 - kh);
+            apart();
+        }
+
+        auto state_behind = [&]() {
+            if (a.anchors && !reverse) anchor(chunk0 + c);
+            // rows 16 s + 8 half .. + 7 of this lane's column, decayed to the chunk's end
+            float x[4][8];
+            float most = 0.0f;
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                const half8_t b = read_column(lds.v[0], L::vstride, 16 * s, 32 * vt, lane);
+                half8_t l = b;
+                if constexpr (kLow) l = read_column(lds.v[1], L::vstride, 16 * s, 32 * vt, lane);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int t = 16 * s + 8 * half + i;
+                    x[s][i] = kLow ? ((float)b[i] + (float)l[i]) * ldexpf(lds.keep[now][t], -(lds.up_k[t] + lds.up_v[t])) : (float)b[i] * lds.keep[now][t];
+                    most = fmaxf(most, fabsf(x[s][i]));
+                }
+            }
+            const uint32_t in = wave_top(mine_v ? most : 0.0f);
+            const int      to = in ? lift_from(in, 60) : up;
+            const float    scale = power_of_two(to), tot = ldexpf(__builtin_amdgcn_exp2f((float)all), to - up);
+            up = to;
+#pragma unroll
+            for (int kt = 0; kt < KP; ++kt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) S[kt][r] *= tot;
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                half8_t hi, lo;
+                split(x[s], scale, hi, lo);
+#pragma unroll
+                for (int kt = 0; kt < KP; ++kt) {
+                    const half8_t w = read_column(lds.k[0], L::kstride, 16 * s, 32 * (KP * kh + kt), lane);
+                    S[kt] = mfma(w, hi, S[kt]);
+                    S[kt] = mfma(w, lo, S[kt]);
+                    if constexpr (kLow) S[kt] = mfma(read_column(lds.k[1], L::kstride, 16 * s, 32 * (KP * kh + kt), lane), hi, S[kt]);
+                }
+            }
+            if (a.anchors && reverse) anchor(chunk0 + chunks - 1 - c);
+            apart();
+        };
+        if (!OUT || HALVES == 2) state_behind();
+        if (c + 1 < chunks && OUT) fetch(c + 1);
+
+        if constexpr (OUT) {
+            if (WAVES > 1) __syncthreads();                 // the scores are there; q and k have been used
+            if constexpr (HALVES == 2) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) lds.far_half[wave][r][lane] = other[r];
+            }
+            const int os = a.heads * a.vdim, xs = a.heads / a.x_div * a.vdim;
+            const int t0 = reverse ? kChunk - 1 - col : col, j0 = 32 * vt + 4 * half, left = anew(a.vdim - j0);      // columns from j0 on
+#pragma unroll 1
+            for (int tt = HALVES == 2 ? kh : 0; tt < (HALVES == 2 ? kh + 1 : 2); ++tt) {
+                acc_t near = zero();
+                if constexpr (HALVES == 1) far = part_of_state(tt);
+                const int   t = 32 * tt + col;
+                const float of_row = ldexpf(mild ? a.pair_scale * lds.to[now][t] : a.pair_scale, kLow ? -lds.up_q[t] : 0);
+#pragma unroll 1
+                for (int ss = 0; ss <= tt; ++ss) {
+                    acc_t sum = zero(), p;
+                    int   lift;
+                    if constexpr (L::scores) lift = __builtin_amdgcn_readfirstlane(lds.lift[tt + ss]);
+                    else lift = score(tt, ss, p);
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        half8_t hi, lo;
+                        if constexpr (L::scores) {
+                            const _Float16 *from = lds.p[0] + ((tt + ss) * 32 + col) * L::pstride + 16 * s + 8 * half;
+                            hi = read8(from);
+                            lo = read8(from + 3 * 32 * L::pstride);
+                        } else {
+                            float y[8];
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) y[i] = p[8 * s + i];
+                            split(y, power_of_two(lift), hi, lo);
                         }
-                        *reinterpret_cast<half4_t *>(to + 8 * g) = hi;
-                        *reinterpret_cast<half4_t *>(to + 3 * 32 * L::pstride + 8 * g) = lo;
+                        const half8_t w = read_column<!L::scores>(lds.v[0], L::vstride, 32 * ss + 16 * s, 32 * vt, lane);
+                        sum = mfma(w, hi, sum);
+                        sum = mfma(w, lo, sum);
+                        if constexpr (kLow) sum = mfma(read_column<!L::scores>(lds.v[1], L::vstride, 32 * ss + 16 * s, 32 * vt, lane), hi, sum);
                     }
-                }
-                apart();
-            }
-            acc_t far[2];
-            if (OUT && owns) {           // what the rows take from the state
-                far[0] = far[1] = zero();
-                float most = 0.0f;
+                    const float down = power_of_two(-lift) * of_row;
 #pragma unroll
-                for (int i = 0; i < 8 * KS; ++i) most = fmaxf(most, fabsf(S[i >> 4][i & 15]));
-                const int   lift = lift_of(mine_v ? most : 0.0f);
-                const float up = power_of_two(lift);
-#pragma unroll
-                for (int s = 0; s < KS; ++s) {
-                    float x[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[i] = S[s >> 1][8 * (s & 1) + i];
-                    half8_t hi, lo;
-                    split(x, up, hi, lo);
-#pragma unroll
-                    for (int tt = 0; tt < 2; ++tt) {
-                        const int     at = (32 * tt + col) * L::kstride + 16 * s + 4 * half;
-                        const half8_t b = read4_4(lds.q[0] + at);
-                        far[tt] = mfma(hi, b, far[tt]);
-                        far[tt] = mfma(lo, b, far[tt]);
-                        if constexpr (kLow) far[tt] = mfma(hi, read4_4(lds.q[1] + at), far[tt]);
-                    }
-                    if (s & 1) apart();
-                }
-#pragma unroll
-                for (int tt = 0; tt < 2; ++tt) {
-                    const float f = ldexpf(lds.far[now][32 * tt + col], -(lift + (kLow ? lds.up_q[32 * tt + col] : 0)));
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) far[tt][r] *= f;
-                }
-                apart();
-            }
-            if (owns) {                  // the state behind the chunk
-                if (a.anchors && !reverse) anchor(chunk0 + c);
-                // rows 16 s + 8 half .. + 7 of this lane's column, decayed to the chunk's end
-                auto decayed = [&](const int s, float (&x)[8]) {
-                    const half8_t b = read_column(lds.v[0], L::vstride, 16 * s, 32 * wave, lane);
-                    half8_t l = b;
-                    if constexpr (kLow) l = read_column(lds.v[1], L::vstride, 16 * s, 32 * wave, lane);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int t = 16 * s + 8 * half + i;
-                        x[i] = kLow ? ((float)b[i] + (float)l[i]) * ldexpf(lds.keep[now][t], -(lds.up_k[t] + lds.up_v[t])) : (float)b[i] * lds.keep[now][t];
-                    }
-                };
-                float most = 0.0f;
-#pragma unroll 1
-                for (int s = 0; s < 4; ++s) {
-                    float x[8];
-                    decayed(s, x);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(x[i]));
-                }
-                const int   lift = lift_of(mine_v ? most : 0.0f, 60);
-                const float up = power_of_two(lift), down = power_of_two(-lift), tot = __builtin_amdgcn_exp2f((float)all) * up;
-#pragma unroll
-                for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) S[kt][r] *= tot;
-                apart();
-#pragma unroll 1
-                for (int s = 0; s < 4; ++s) {
-                    float   x[8];
-                    half8_t hi, lo;
-                    decayed(s, x);
-                    split(x, up, hi, lo);
-#pragma unroll
-                    for (int kt = 0; kt < KT; ++kt) {
-                        const half8_t w = read_column(lds.k[0], L::kstride, 16 * s, 32 * kt, lane);
-                        S[kt] = mfma(w, hi, S[kt]);
-                        S[kt] = mfma(w, lo, S[kt]);
-                        if constexpr (kLow) S[kt] = mfma(read_column(lds.k[1], L::kstride, 16 * s, 32 * kt, lane), hi, S[kt]);
-                    }
+                    for (int r = 0; r < 16; ++r) near[r] = fmaf(sum[r], down, near[r]);
                     apart();
                 }
+                if constexpr (HALVES == 2) {
+                    __syncthreads();
 #pragma unroll
-                for (int kt = 0; kt < KT; ++kt)
+                    for (int r = 0; r < 16; ++r) far[r] += lds.far_half[wave < VT ? wave + VT : wave - VT][r][lane];
+                }
+                const bool there = t < count;
+                const int  base = low + (reverse ? -32 * tt : 32 * tt);
+                float dn = 0.0f, df = 0.0f;
+                if (a.x && there) {
+                    const T *x = (const T *)a.x + h / a.x_div * a.vdim + (int64_t)base * xs;
+                    const uint32_t mine = (uint32_t)(t0 * xs + j0);
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) S[kt][r] *= down;
-                if (a.anchors && reverse) anchor(chunk0 + chunks - 1 - c);
-                apart();
-            }
-            if (!kEarly && c + 1 < chunks) fetch(c + 1);
-            if (L::scores) __syncthreads();                 // they are there
-            if (OUT && owns) {
-                const int     os = a.heads * a.vdim, xs = a.heads / a.x_div * a.vdim;
-                const int     t0 = reverse ? kChunk - 1 - col : col, j0 = 32 * wave + 4 * half, left = anew(a.vdim - j0);       // columns from j0 on
-#pragma unroll 1
-                for (int tt = 0; tt < 2; ++tt) {
-                    acc_t near = zero(), far_t;
+                    for (int g = 0; g < 4; ++g) {
+                        float w[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                        if (WHOLE) {
+                            if (8 * g < left) {
+                                T e4[4];
+                                __builtin_memcpy(e4, (x + 8 * g) + mine, sizeof e4);
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) far_t[r] = tt ? far[1][r] : far[0][r];
-#pragma unroll 1
-                    for (int ss = 0; ss <= tt; ++ss) {
-                        acc_t sum = zero(), p;
-                        int   lift;
-                        if constexpr (L::scores) lift = lds.lift[tt + ss];
-                        else lift = score(tt, ss, p);
-#pragma unroll
-                        for (int s = 0; s < 2; ++s) {
-                            half8_t hi, lo;
-                            if constexpr (L::scores) {
-                                const _Float16 *from = lds.p[0] + ((tt + ss) * 32 + col) * L::pstride + 16 * s + 8 * half;
-                                hi = read8(from);
-                                lo = read8(from + 3 * 32 * L::pstride);
-                            } else {
-                                float y[8];
-#pragma unroll
-                                for (int i = 0; i < 8; ++i) y[i] = p[8 * s + i];
-                                split(y, power_of_two(lift), hi, lo);
+                                for (int e = 0; e < 4; ++e) w[e] = (float)e4[e];
                             }
-                            const half8_t w = read_column<!L::scores>(lds.v[0], L::vstride, 32 * ss + 16 * s, 32 * wave, lane);
-                            sum = mfma(w, hi, sum);
-                            sum = mfma(w, lo, sum);
-                            if constexpr (kLow) sum = mfma(read_column<!L::scores>(lds.v[1], L::vstride, 32 * ss + 16 * s, 32 * wave, lane), hi, sum);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (8 * g + e < left) w[e] = (float)(x + 8 * g + e)[mine];
                         }
-                        const float down = power_of_two(-lift);
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) near[r] = fmaf(sum[r], down, near[r]);
-                        apart();
-                    }
-                    const int  t = 32 * tt + col;
-                    const bool there = t < count;
-                    const int  base = low + (reverse ? -32 * tt : 32 * tt);
-                    float dn = 0.0f, df = 0.0f;
-                    if (a.x && there) {
-                        const T *x = (const T *)a.x + h / a.x_div * a.vdim + (int64_t)base * xs;
-                        const uint32_t mine = (uint32_t)(t0 * xs + j0);
-#pragma unroll
-                        for (int g = 0; g < 4; ++g) {
-                            float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                            if (a.vec_x) {
-                                if (8 * g < left) {
-                                    T e4[4];
-                                    __builtin_memcpy(e4, (x + 8 * g) + mine, sizeof e4);
-#pragma unroll
-                                    for (int e = 0; e < 4; ++e) v[e] = (float)e4[e];
-                                }
-                            } else {
-#pragma unroll
-                                for (int e = 0; e < 4; ++e)
-                                    if (8 * g + e < left) v[e] = (float)(x + 8 * g + e)[mine];
+                        for (int e = 0; e < 4; ++e)
+                            if (8 * g + e < left) {
+                                dn = fmaf(near[4 * g + e], w[e], dn);
+                                df = fmaf(far[4 * g + e], w[e], df);
                             }
+                    }
+                }
+                if (there) {
+                    const uint32_t mine = (uint32_t)(t0 * os + j0);
+                    float    *to32 = (float *)a.out + h * a.vdim + (int64_t)base * os;
+                    _Float16 *to16 = (_Float16 *)a.out + h * a.vdim + (int64_t)base * os;
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        float o[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[e] = near[4 * g + e] + far[4 * g + e];
+                        if (WHOLE) {
+                            if (8 * g < left) {
+                                if (kLow || a.out_f32) *reinterpret_cast<float4_t *>((to32 + 8 * g) + mine) = float4_t{o[0], o[1], o[2], o[3]};
+                                else *reinterpret_cast<half4_t *>((to16 + 8 * g) + mine) = half4_t{(_Float16)o[0], (_Float16)o[1], (_Float16)o[2], (_Float16)o[3]};
+                            }
+                        } else {
 #pragma unroll
                             for (int e = 0; e < 4; ++e)
                                 if (8 * g + e < left) {
-                                    dn = fmaf(near[4 * g + e], v[e], dn);
-                                    df = fmaf(far_t[4 * g + e], v[e], df);
+                                    if (kLow || a.out_f32) (to32 + 8 * g + e)[mine] = o[e];
+                                    else (to16 + 8 * g + e)[mine] = (_Float16)o[e];
                                 }
                         }
                     }
-                    if (there) {
-                        const uint32_t mine = (uint32_t)(t0 * os + j0);
-                        float    *to32 = (float *)a.out + h * a.vdim + (int64_t)base * os;
-                        _Float16 *to16 = (_Float16 *)a.out + h * a.vdim + (int64_t)base * os;
-#pragma unroll
-                        for (int g = 0; g < 4; ++g) {
-                            float o[4];
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) o[e] = near[4 * g + e] + far_t[4 * g + e];
-                            if (a.vec_out) {
-                                if (8 * g < left) {
-                                    if (kLow || a.out_f32) *reinterpret_cast<float4_t *>((to32 + 8 * g) + mine) = float4_t{o[0], o[1], o[2], o[3]};
-                                    else *reinterpret_cast<half4_t *>((to16 + 8 * g) + mine) = half4_t{(_Float16)o[0], (_Float16)o[1], (_Float16)o[2], (_Float16)o[3]};
-                                }
-                            } else {
-#pragma unroll
-                                for (int e = 0; e < 4; ++e)
-                                    if (8 * g + e < left) {
-                                        if (kLow || a.out_f32) (to32 + 8 * g + e)[mine] = o[e];
-                                        else (to16 + 8 * g + e)[mine] = (_Float16)o[e];
-                                    }
-                            }
-                        }
-                    }
-                    if (a.x) {
-                        dn += __shfl_xor(dn, 32, 64);
-                        df += __shfl_xor(df, 32, 64);
-                        if (half == 0) {
-                            lds.dots[2 * wave][t] = dn;
-                            lds.dots[2 * wave + 1][t] = df;
-                        }
-                    }
-                    apart();
                 }
+                if (a.x) {
+                    dn += __shfl_xor(dn, 32, 64);
+                    df += __shfl_xor(df, 32, 64);
+                    if (half == 0) {
+                        lds.dots[2 * vt][t] = dn;
+                        lds.dots[2 * vt + 1][t] = df;
+                    }
+                }
+                apart();
             }
-            if (OUT && a.x) {
+            if (HALVES == 1) state_behind();
+            if (a.x) {
                 __syncthreads();
                 if (threadIdx.x < kChunk && (int)threadIdx.x < count) {
                     float dn = 0.0f, df = 0.0f;
@@ -507,41 +553,45 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
                     a.dot_far[at] = df;
                 }
             }
-            __syncthreads();                                // the tiles may be written again
         }
-        if (a.total && threadIdx.x == 0) a.total[state_at] = (float)whole;
-        if (a.final && mine_v) {
-            char     *to = (char *)a.final + state_at * state_bytes;
-            uint32_t  at = (uint32_t)(4 * half * a.final_i + j * a.final_j) * 4;
-            const int left = anew(a.kdim - 4 * half);
+        if (c + 1 < chunks) __syncthreads();                // the tiles may be written again
+    }
+    if (a.total && threadIdx.x == 0) a.total[state_at] = (float)whole;
+    if (a.final && mine_v) {
+        char     *to = (char *)a.final + state_at * state_bytes;
+        uint32_t  at = (uint32_t)((32 * KP * kh + 4 * half) * a.final_i + j * a.final_j) * 4;
+        const int left = anew(a.kdim - 32 * KP * kh - 4 * half);
+        const float f = power_of_two(-up);
 #pragma unroll
-            for (int kt = 0; kt < KT; ++kt)
+        for (int kt = 0; kt < KP; ++kt)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    if (32 * kt + 8 * (r >> 2) + (r & 3) < left) *reinterpret_cast<float *>(to + at) = S[kt][r];
-                    at += (uint32_t)(r % 4 == 3 ? 5 : 1) * (uint32_t)a.final_i * 4;
-                }
-        }
+            for (int r = 0; r < 16; ++r) {
+                if (32 * kt + 8 * (r >> 2) + (r & 3) < left) *reinterpret_cast<float *>(to + at) = S[kt][r] * f;
+                at += (uint32_t)(r % 4 == 3 ? 5 : 1) * (uint32_t)a.final_i * 4;
+            }
     }
 }
 
-template <typename T, int KW, int VW, bool OUT>
-int launch(const WalkArgs &a, hipStream_t s) {
+template <typename T, int KW, int VW, bool OUT, bool WHOLE>
+int launch_walk(const WalkArgs &a, hipStream_t s) {
     using L = Lds<T, KW, VW, OUT>;
     if (sizeof(L) > 64 * 1024)
-        if (hipError_t e = hipFuncSetAttribute((const void *)attend_walk_kernel<T, KW, VW, OUT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(L)))
+        if (hipError_t e = hipFuncSetAttribute((const void *)attend_walk_kernel<T, KW, VW, OUT, WHOLE>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(L)))
             return record_hip_failure(e, "hipFuncSetAttribute(MaxDynamicSharedMemorySize)");
     // a workgroup goes over one piece: a loop over pieces would have the addresses of the states' entries formed before it and kept in registers
-    const int most = (int)std::min<int64_t>(65535, kMostGroups256 / a.heads);
+    const int most = (int)(kMostGroups256 / 2 / a.heads);   // (workgroups of up to 512)
     for (int first = 0; first < a.segments; first += most) {
         WalkArgs part = a;
         part.piece0 = first;
         LaunchTimer t(s, OUT ? K_ATTEND_WALK : K_ATTEND_STATES);
-        attend_walk_kernel<T, KW, VW, OUT><<<dim3((unsigned)a.heads, (unsigned)std::min(a.segments - first, most)), 64 * L::waves, sizeof(L), s>>>(part);
+        attend_walk_kernel<T, KW, VW, OUT, WHOLE><<<(unsigned)a.heads * (unsigned)std::min(a.segments - first, most), 64 * L::waves, sizeof(L), s>>>(part);
         if (int rc = launch_status("attend_walk_kernel")) return rc;
     }
     return CNGP_OK;
 }
+
+template <typename T, int KW, int VW, bool OUT>
+int launch(const WalkArgs &a, hipStream_t s) { return a.whole ? launch_walk<T, KW, VW, OUT, true>(a, s) : launch_walk<T, KW, VW, OUT, false>(a, s); }
 
 template <typename T, bool OUT, int KW>
 int launch_columns(const WalkArgs &a, hipStream_t s) {

@@ -38,17 +38,18 @@ __device__ __forceinline__ half8_t read_column(const _Float16 *tile, const int s
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// x * scale as a high and a low part; what subnormal parts lose is 2^-39 of the largest value where `scale` has lifted that (lift_of).
+// x * scale as a high and a low part; what subnormal parts lose is 2^-39 of the largest value where that has been lifted (lift_of).  (As a product and
+// sum the low part is one instruction, as a difference three: a scale of 1 has to be one that the compiler does not know, see anew.)
 __device__ __forceinline__ void split(const float (&x)[8], const float scale, half8_t &hi, half8_t &lo) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float y = x[i] * scale;
-        hi[i] = (_Float16)y;
-        lo[i] = (_Float16)(y - (float)hi[i]);
+        hi[i] = (_Float16)(x[i] * scale);
+        lo[i] = (_Float16)fmaf(x[i], scale, -(float)hi[i]);
     }
 }
 
-// Exponent of the power of two that brings a wavefront's largest magnitude to 2^13 .. 2^14 (0 where that is 0 or not finite), within +-`most`.
+// wave_top: the largest of a wavefront's magnitudes, as bits.  lift_of: exponent of the power of two that brings it to 2^13 .. 2^14 (0 where it is 0 or
+// not finite), within +-`most`.
 template <int CTRL>
 __device__ __forceinline__ float max_moved(const float v) {
     return fmaxf(v, __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xF, 0xF, true)));
@@ -57,7 +58,7 @@ __device__ __forceinline__ int lift_from(const uint32_t top, const int most) {
     const int e = (int)(top >> 23) - 127, lift = 13 - e;
     return top == 0 || e > 127 ? 0 : lift > most ? most : lift < -most ? -most : lift;
 }
-__device__ __forceinline__ int lift_of(float v, const int most = 120) {
+__device__ __forceinline__ uint32_t wave_top(float v) {
     v = max_moved<0x121>(max_moved<0x122>(max_moved<0x124>(max_moved<0x128>(v))));      // rows of 16 lanes turned by 8, 4, 2, 1
     uint32_t top = 0;
 #pragma unroll
@@ -65,8 +66,9 @@ __device__ __forceinline__ int lift_of(float v, const int most = 120) {
         const uint32_t o = (uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), r);
         top = top > o ? top : o;
     }
-    return lift_from(top, most);
+    return top;
 }
+__device__ __forceinline__ int lift_of(const float v, const int most = 120) { return lift_from(wave_top(v), most); }
 // ... of LANES lanes side by side, for each of them.
 template <int LANES>
 __device__ __forceinline__ int lift_of_lanes(float v) {
@@ -87,8 +89,8 @@ __device__ __forceinline__ int anew(int v) {
     asm volatile("" : "+v"(v));
     return v;
 }
-__device__ __forceinline__ int anew_scalar(int v) {
-    asm volatile("" : "+s"(v));
+__device__ __forceinline__ float anew(float v) {
+    asm volatile("" : "+v"(v));
     return v;
 }
 

@@ -97,12 +97,24 @@ __global__ __launch_bounds__(kBlock) void attend_carry_kernel(const CarryArgs a)
         const Span    span = span_of(a.offsets, s, a.N, a.rows_each);
         const int32_t n = (int32_t)(((uint32_t)(span.end - span.begin) + (1u << a.seg_shift) - 1) >> a.seg_shift), base = piece_base(span.begin, s, a.seg_shift);
         float state = a.first ? a.first[own] : 0.0f;
-        for (int32_t i = 0; i < n; ++i) {
-            const int64_t at = (int64_t)(base + (a.reverse ? n - 1 - i : i)) * a.heads + h;
-            float *p = a.states + (size_t)at * a.size + e;
-            const float part = *p;
-            *p = state;
-            state = fmaf(__builtin_amdgcn_exp2f(a.total[at]), state, part);
+        // eight segments' parts are under way at a time: one after the other they would be a chain of memory latencies
+        for (int32_t i0 = 0; i0 < n; i0 += 8) {
+            float part[8], keep[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int32_t i = i0 + u < n ? i0 + u : n - 1;
+                const int64_t at = (int64_t)(base + (a.reverse ? n - 1 - i : i)) * a.heads + h;
+                part[u] = a.states[(size_t)at * a.size + e];
+                keep[u] = a.total[at];
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int32_t i = i0 + u;
+                if (i >= n) break;
+                const int64_t at = (int64_t)(base + (a.reverse ? n - 1 - i : i)) * a.heads + h;
+                a.states[(size_t)at * a.size + e] = state;
+                state = fmaf(__builtin_amdgcn_exp2f(keep[u]), state, part[u]);
+            }
         }
         if (a.final) a.final[own] = state;
     }
@@ -112,7 +124,7 @@ __global__ __launch_bounds__(kBlock) void attend_carry_kernel(const CarryArgs a)
 // with states, D = <state, gradient of the state> at a chunk's start and T = what crosses the whole chunk,
 //     sum over s >= t of (q.dq near - k.dk near + q.dq far)  +  sum over s < t of k.dk far  +  T,     T = D - sum of q.dq far,
 // and D of the next chunk is T + sum of k.dk far.  D is formed anew from both states every kAnchorChunks chunks: sums that ran on over a long
-// sequence would bury the short memories' gradients in their rounding.  A wavefront per such stretch and head, a lane per row of a chunk.
+// sequence would bury the short memories' gradients in their rounding.  A workgroup per such stretch and head, a wavefront per chunk, a lane per row.
 struct DecayArgs {
     const float *q_near, *q_far, *k_near, *k_far;    // [heads, N]
     const float *states, *grads;                     // anchors of the two walks
@@ -123,6 +135,7 @@ struct DecayArgs {
     int64_t      N, pieces;
     int32_t      S, rows_each, heads, size, anchor_size;
     int32_t      kdim, vdim;                         // of the anchors' walks
+    int32_t      whole;                              // a workgroup per sequence goes over all its stretches: where most have one
 };
 __device__ __forceinline__ double wave_sum(double v) {
 #pragma unroll
@@ -137,44 +150,68 @@ __device__ __forceinline__ double upto(double v, const int lane) {
     }
     return v;
 }
-__global__ __launch_bounds__(64) void attend_decay_kernel(const DecayArgs a)
+__global__ __launch_bounds__(64 * kAnchorChunks) void attend_decay_kernel(const DecayArgs a)
 {
     constexpr int kRows = 1 << kAnchorShift;
-    const int lane = threadIdx.x;
+    __shared__ double q_sum[kAnchorChunks], k_sum[kAnchorChunks], D_part[kAnchorChunks], g_sum[kAnchorChunks];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;      // as many as a sequence may have chunks in a stretch
     for (int64_t item = blockIdx.x; item < a.pieces * a.heads; item += gridDim.x) {
         const int     h = (int)(item % a.heads);
         const int64_t piece = item / a.heads;
-        const int32_t seq = sequence_of(a.offsets, (int32_t)piece, a.N, a.S, a.rows_each, kAnchorShift);
+        const int32_t seq = a.whole ? (int32_t)piece : sequence_of(a.offsets, (int32_t)piece, a.N, a.S, a.rows_each, kAnchorShift);
         const Span    span = span_of(a.offsets, seq, a.N, a.rows_each);
-        const int64_t i = piece - piece_base(span.begin, seq, kAnchorShift), begin = span.begin + i * kRows;
-        const int64_t end = begin + kRows < span.end ? begin + kRows : span.end;
         double sum = 0.0;
-        if (begin < end) {
+        for (int64_t i = a.whole ? 0 : piece - piece_base(span.begin, seq, kAnchorShift); span.begin + i * kRows < span.end; ++i) {
+            const int64_t begin = span.begin + i * kRows, end = begin + kRows < span.end ? begin + kRows : span.end;
+            const int     chunks = (int)((end - begin + kChunk - 1) >> kChunkShift);
+            const bool    anchored = i != 0;
+            const int     n = anchored ? a.anchor_size : a.size;
+            const size_t  at = anchored ? ((size_t)anchor_slot(span.begin, (int32_t)i * kAnchorChunks) * a.heads + h) * a.anchor_size : ((size_t)seq * a.heads + h) * a.size;
+            const float  *x = anchored ? a.states : a.h0, *y = anchored ? a.grads : a.dh0;
             double D = 0.0;
-            const int n = i ? a.anchor_size : a.size;
-            const size_t  at = i ? (size_t)(anchor_slot(span.begin, (int32_t)i * kAnchorChunks) * a.heads + h) * a.anchor_size : ((size_t)seq * a.heads + h) * a.size;
-            const float *x = i ? a.states : a.h0, *y = i ? a.grads : a.dh0;
             if (x && y)
-                for (int e = lane; e < n; e += 64)
-                    if (!i || (anchor_row(e, a.kdim) < a.kdim && anchor_column(e, a.kdim) < a.vdim)) D += (double)x[at + e] * (double)y[at + e];
+                for (int e = threadIdx.x; e < n; e += blockDim.x)
+                    if (!anchored || (anchor_row(e, a.kdim) < a.kdim && anchor_column(e, a.kdim) < a.vdim)) D += (double)x[at + e] * (double)y[at + e];
             D = wave_sum(D);
-            for (int64_t row0 = begin; row0 < end; row0 += kChunk) {
-                const bool   in = row0 + lane < end;
-                const size_t p = (size_t)h * a.N + (size_t)(in ? row0 + lane : row0);
-                const double qf = in ? a.q_far[p] : 0.0, kf = in ? a.k_far[p] : 0.0, near = in ? (double)a.q_near[p] - (double)a.k_near[p] : 0.0;
-                const double qfs = upto(qf, lane), kfs = upto(kf, lane), ns = upto(near, lane);
-                const double q_all = __shfl(qfs, 63, 64), k_all = __shfl(kfs, 63, 64), n_all = __shfl(ns, 63, 64);
-                const double T = D - q_all;
+            if (lane == 0) D_part[wave] = D;
+            // (a sequence that is longer than the caller said has more chunks than there are wavefronts: they go round)
+            double before = 0.0;                             // k.dk far - q.dq far of the chunks of earlier turns
+            for (int c0 = 0; c0 < chunks; c0 += waves) {
+                const int64_t row = begin + (int64_t)(c0 + wave) * kChunk + lane;
+                const bool    in = row < end;
+                const size_t  p = (size_t)h * a.N + (size_t)(in ? row : begin);
+                const double  qf = in ? a.q_far[p] : 0.0, kf = in ? a.k_far[p] : 0.0, near = in ? (double)a.q_near[p] - (double)a.k_near[p] : 0.0;
+                const double  qfs = upto(qf, lane), kfs = upto(kf, lane), ns = upto(near, lane);
+                const double  q_all = __shfl(qfs, 63, 64), k_all = __shfl(kfs, 63, 64), n_all = __shfl(ns, 63, 64);
+                if (lane == 0) {
+                    q_sum[wave] = q_all;
+                    k_sum[wave] = k_all;
+                }
+                __syncthreads();
+                double T = before - q_all;
+                for (int w = 0; w < waves; ++w) {
+                    T += D_part[w];
+                    if (w < wave) T += k_sum[w] - q_sum[w];
+                    before += k_sum[w] - q_sum[w];
+                }
                 const double g = (n_all - ns + near) + (q_all - qfs + qf) + (kfs - kf) + T;
-                if (a.ddecay && in) a.ddecay[(row0 + lane) * a.heads + h] = (float)g;
+                if (a.ddecay && in) a.ddecay[row * a.heads + h] = (float)g;
                 sum += in ? g : 0.0;
-                D = T + k_all;
+                __syncthreads();
             }
+            if (!a.whole) break;
         }
         if (a.parts) {
             sum = wave_sum(sum);
-            if (lane == 0) a.parts[piece * a.heads + h] = sum;
+            if (lane == 0) g_sum[wave] = sum;
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                double t = 0.0;
+                for (int w = 0; w < waves; ++w) t += g_sum[w];
+                a.parts[piece * a.heads + h] = t;
+            }
         }
+        __syncthreads();
     }
 }
 __global__ __launch_bounds__(kBlock) void attend_decay_sum_kernel(const double *__restrict__ parts, float *__restrict__ ddecay, const int64_t pieces, const int heads)
@@ -224,10 +261,13 @@ struct Plan {
     int     seg_shift;
     int64_t segments;
 };
-constexpr int64_t kEnoughItems = 512;                 // two workgroups for each of 256 CUs
-Plan plan_of(const cngp_attend_config *c, int64_t N, int64_t S, bool ragged) {
+constexpr int64_t kEnoughItems = 1024;                // four workgroups for each of 256 CUs: they end unevenly
+int64_t longest_of(const cngp_attend_config *c, int64_t N, int64_t S, bool ragged) {
     const int64_t mean = S ? (N + S - 1) / S : 0;
-    const int64_t longest = !ragged ? mean : c->longest ? std::min<int64_t>(c->longest, N) : std::min<int64_t>(4 * mean, N);
+    return !ragged ? mean : c->longest ? std::min<int64_t>(c->longest, N) : std::min<int64_t>(4 * mean, N);
+}
+Plan plan_of(const cngp_attend_config *c, int64_t N, int64_t S, bool ragged) {
+    const int64_t longest = longest_of(c, N, S, ragged);
     const int64_t R = (N * c->heads + kEnoughItems - 1) / kEnoughItems;
     int shift = 8;
     while (shift < 30 && (int64_t)1 << shift < R) ++shift;
@@ -465,12 +505,15 @@ int cngp_attend_bwd(const cngp_attend_config *cfg, const void *q, const void *k,
     d.ddecay = rows ? ddecay : nullptr;
     d.parts = rows ? nullptr : (double *)(ws + sp.parts);
     d.N = N; d.S = (int32_t)sequences; d.rows_each = (int32_t)(N / sequences); d.heads = cfg->heads;
-    d.pieces = pieces(N, sequences, kAnchorShift);
+    d.whole = longest_of(cfg, N, sequences, ragged) <= kAnchorChunks * kChunk;
+    d.pieces = d.whole ? sequences : pieces(N, sequences, kAnchorShift);
     d.kdim = V; d.vdim = K;
     d.size = K * V; d.anchor_size = (int32_t)anchor_floats(V, K);
     {
         LaunchTimer t(s, K_ATTEND_DECAY);
-        attend_decay_kernel<<<(unsigned)std::min<int64_t>(d.pieces * d.heads, 0x3ffffff), 64, 0, s>>>(d);
+        const int64_t longest = longest_of(cfg, N, sequences, ragged);
+        const int     waves = (int)std::min<int64_t>(kAnchorChunks, std::max<int64_t>(1, (longest + kChunk - 1) / kChunk));
+        attend_decay_kernel<<<(unsigned)std::min<int64_t>(d.pieces * d.heads, 0x3fffff), 64 * waves, 0, s>>>(d);
         if (int rc = launch_status("attend_decay_kernel")) return rc;
     }
     if (rows) return CNGP_OK;

@@ -161,6 +161,7 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
     using L = Lds<T, KW, VW, OUT>;
     constexpr int  WAVES = L::waves, VT = L::VT, KT = L::KT, HALVES = L::halves, KP = KT / HALVES;
     constexpr int  KS = KW / 16 / HALVES;                   // steps of 16 columns of k that a wavefront keeps
+    constexpr int  KR = KW < 32 ? 8 : 16, VR = VW < 32 ? 8 : 16;      // registers of a tile's sums that hold rows of the state, and of the outputs
     constexpr bool kLow = sizeof(T) == 4;                   // the inputs have low parts too
     extern __shared__ __align__(16) char lds_raw[];
     L &lds = *reinterpret_cast<L *>(lds_raw);
@@ -237,9 +238,11 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
             lds.mild[c & 1] = mild;
         }
     };
+    constexpr bool kAhead = WAVES > 1;                      // a chunk's rows are fetched while the one before is worked on (short rows: registers that
+                                                            // another wavefront has more of, 740 against 725 us a pass of 4096 rays)
     if (chunks > 0) {
         fetch_decays(0);
-        fetch(0);
+        if (kAhead) fetch(0);
     }
 
     acc_t S[KP];
@@ -273,6 +276,7 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
         const int now = c & 1;
         int row0, low, count;
         place(c, row0, count, low);
+        if (!kAhead) fetch(c);
         if (OUT) rq.store(lds.q[0], lds.q[L::parts - 1], lds.up_q, q + (int64_t)low * qs, reverse, a.q ? count : 0, qs, a.kdim);
         rk.store(lds.k[0], lds.k[L::parts - 1], lds.up_k, k + (int64_t)low * ks, reverse, a.k ? count : 0, ks, a.kdim);
         rv.store(lds.v[0], lds.v[L::parts - 1], lds.up_v, v + (int64_t)low * vs, reverse, a.v ? count : 0, vs, a.vdim);
@@ -280,7 +284,7 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
         const double all = lds.total[now];
         whole += all;
         if (c + 1 < chunks) {
-            if (!OUT) fetch(c + 1);
+            if (kAhead && !OUT) fetch(c + 1);
             decays(c + 1);
         }
 
@@ -327,7 +331,7 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
             return lift_of(most);
         };
         if constexpr (L::scores) {
-            for (int tile = wave; tile < 3; tile += WAVES) {
+            for (int tile = wave; tile < (count > 32 ? 3 : 1); tile += WAVES) {
                 acc_t p;
                 const int   lift = score(tile > 0, tile > 1, p);
                 const float f = power_of_two(lift);
@@ -374,7 +378,7 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
             }
             const float f = ldexpf(lds.far[now][32 * tt + col], -(up + lift + (kLow ? lds.up_q[32 * tt + col] : 0)));
 #pragma unroll
-            for (int r = 0; r < 16; ++r) far[r] *= f;
+            for (int r = 0; r < VR; ++r) far[r] *= f;
             return far;
         };
         acc_t far, other;                // of this wavefront's rows, and of the other half's
@@ -408,9 +412,10 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
 #pragma unroll
             for (int kt = 0; kt < KP; ++kt)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) S[kt][r] *= tot;
+                for (int r = 0; r < KR; ++r) S[kt][r] *= tot;
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
+                if (s && 16 * s >= count) break;            // (no rows there)
                 half8_t hi, lo;
                 split(x[s], scale, hi, lo);
 #pragma unroll
@@ -425,24 +430,24 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
             apart();
         };
         if (!OUT || HALVES == 2) state_behind();
-        if (c + 1 < chunks && OUT) fetch(c + 1);
+        if (kAhead && c + 1 < chunks && OUT) fetch(c + 1);
 
         if constexpr (OUT) {
             if (WAVES > 1) __syncthreads();                 // the scores are there; q and k have been used
             if constexpr (HALVES == 2) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) lds.far_half[wave][r][lane] = other[r];
+                for (int r = 0; r < VR; ++r) lds.far_half[wave][r][lane] = other[r];
             }
             const int os = a.heads * a.vdim, xs = a.heads / a.x_div * a.vdim;
             const int t0 = reverse ? kChunk - 1 - col : col, j0 = 32 * vt + 4 * half, left = anew(a.vdim - j0);      // columns from j0 on
 #pragma unroll 1
-            for (int tt = HALVES == 2 ? kh : 0; tt < (HALVES == 2 ? kh + 1 : 2); ++tt) {
+            for (int tt = HALVES == 2 ? kh : 0; tt < (HALVES == 2 ? kh + 1 : count > 32 ? 2 : 1); ++tt) {
                 acc_t near = zero();
                 if constexpr (HALVES == 1) far = part_of_state(tt);
                 const int   t = 32 * tt + col;
                 const float of_row = ldexpf(mild ? a.pair_scale * lds.to[now][t] : a.pair_scale, kLow ? -lds.up_q[t] : 0);
 #pragma unroll 1
-                for (int ss = 0; ss <= tt; ++ss) {
+                for (int ss = 0; ss <= tt && 32 * tt < count; ++ss) {
                     acc_t sum = zero(), p;
                     int   lift;
                     if constexpr (L::scores) lift = __builtin_amdgcn_readfirstlane(lds.lift[tt + ss]);
@@ -467,13 +472,13 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
                     }
                     const float down = power_of_two(-lift) * of_row;
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) near[r] = fmaf(sum[r], down, near[r]);
+                    for (int r = 0; r < VR; ++r) near[r] = fmaf(sum[r], down, near[r]);
                     apart();
                 }
                 if constexpr (HALVES == 2) {
                     __syncthreads();
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) far[r] += lds.far_half[wave < VT ? wave + VT : wave - VT][r][lane];
+                    for (int r = 0; r < VR; ++r) far[r] += lds.far_half[wave < VT ? wave + VT : wave - VT][r][lane];
                 }
                 const bool there = t < count;
                 const int  base = low + (reverse ? -32 * tt : 32 * tt);
@@ -482,7 +487,7 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
                     const T *x = (const T *)a.x + h / a.x_div * a.vdim + (int64_t)base * xs;
                     const uint32_t mine = (uint32_t)(t0 * xs + j0);
 #pragma unroll
-                    for (int g = 0; g < 4; ++g) {
+                    for (int g = 0; g < VR / 4; ++g) {
                         float w[4] = {0.0f, 0.0f, 0.0f, 0.0f};
                         if (WHOLE) {
                             if (8 * g < left) {
@@ -509,7 +514,7 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
                     float    *to32 = (float *)a.out + h * a.vdim + (int64_t)base * os;
                     _Float16 *to16 = (_Float16 *)a.out + h * a.vdim + (int64_t)base * os;
 #pragma unroll
-                    for (int g = 0; g < 4; ++g) {
+                    for (int g = 0; g < VR / 4; ++g) {
                         float o[4];
 #pragma unroll
                         for (int e = 0; e < 4; ++e) o[e] = near[4 * g + e] + far[4 * g + e];

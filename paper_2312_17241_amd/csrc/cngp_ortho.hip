@@ -16,19 +16,13 @@ using namespace cngp::mat;
 namespace {
 
 inline size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
-constexpr int kBlock = 256, kTile = 128, kDepth = 32;       // a workgroup's part of a product, and how much of the contraction it has in LDS at a time
+constexpr int kBlock = 256, kTile = 128, kDepth = 32;       // matrices are padded to tiles of 128; how much of a contraction a workgroup has in LDS at a time
 constexpr int kPad = 8;                                     // halves between rows in LDS: 16-byte reads of neighbouring rows fall into different banks
-constexpr float kScaleX = 16384.0f, kScaleA = 4096.0f, kScaleB = 1024.0f;                           // A and B are kept times this, X times a power of two of its own (Shape::scale):
-                                                            // entries of large matrices would be subnormal fp16 numbers
+// X, A and B are kept times these: singular values of 1 spread over rows of thousands, and their low parts, would be subnormal fp16 numbers.  What
+// is left above: entries of X below 4 (so its singular values may be), of A below 16, of B below 64.
+constexpr float kScaleX = 16384.0f, kScaleA = 4096.0f, kScaleB = 1024.0f;
 constexpr int kNormParts = 256;
-#ifndef KST
-#define KST 2
-#endif
-#ifndef KOCC
-#define KOCC 2
-#endif
-constexpr int kStages = KST;
-typedef unsigned words_t __attribute__((ext_vector_type(4)));
+constexpr int64_t kEnoughTiles = 256;                       // of 128 x 128: a CU each
 
 // High and low parts of a matrix, rows of `stride` values.
 struct Pair {
@@ -84,7 +78,8 @@ __global__ __launch_bounds__(kBlock) void ortho_norm_kernel(const T *__restrict_
 __device__ __forceinline__ float inverse_norm(const double *parts, const int count, const float eps, double *room) {
     double t = 0.0;
     for (int i = threadIdx.x; i < count; i += kBlock) t += parts[(size_t)blockIdx.z * count + i];
-    return (float)(1.0 / (sqrt(block_sum(t, room)) + (double)eps));
+    const double norm = sqrt(block_sum(t, room)) + (double)eps;
+    return norm > 0.0 || norm != norm ? (float)(1.0 / norm) : 0.0f;
 }
 
 // X from G (transposed where `turned`), with zeros behind its edges: 64 x 64 tiles.
@@ -131,13 +126,15 @@ struct ProductArgs {
     int   m, n, turned, out_f16;
 };
 
-// 128 x 128 of a product by four wavefronts of 64 x 64; computed transposed (a lane has a row of C and four neighbouring columns in four registers).
-template <int WHAT>
-__global__ __launch_bounds__(kBlock, KOCC) void ortho_product_kernel(const ProductArgs a)
+// A tile of 64 U x 64 U of a product by four wavefronts of 32 U x 32 U; computed transposed (a lane has a row of C and four neighbouring columns in
+// four registers).
+template <int WHAT, int U>
+__global__ __launch_bounds__(kBlock, 2) void ortho_product_kernel(const ProductArgs a)
 {
     constexpr bool kBack = WHAT == UPDATE || WHAT == LAST;              // the right factor lies by rows of the contraction
-    constexpr int  kRowA = kDepth + kPad, kRowB = kBack ? kTile + kPad : kDepth + kPad, kSizeB = kBack ? kDepth * kRowB : kTile * kRowB;
-    __shared__ __align__(16) _Float16 lds[kStages][2 * kTile * kRowA + 2 * kSizeB];
+    constexpr int  TILE = 64 * U, kRowA = kDepth + kPad, kRowB = kBack ? TILE + kPad : kDepth + kPad, kSizeA = TILE * kRowA, kSizeB = kBack ? kDepth * kRowB : TILE * kRowB;
+    constexpr int  kBackRow = TILE / 8, kStepA = kBlock / 4, kStepB = kBack ? kBlock / kBackRow : kStepA;
+    __shared__ __align__(16) _Float16 lds[2][2 * kSizeA + 2 * kSizeB];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
     int ti, tj;
     if (kBack) {
@@ -150,57 +147,56 @@ __global__ __launch_bounds__(kBlock, KOCC) void ortho_product_kernel(const Produ
         tj = (int)blockIdx.x - ti * (ti + 1) / 2;
     }
     const size_t z = blockIdx.z;
-    const int i0 = ti * kTile, j0 = tj * kTile, wi = 64 * (wave & 1), wj = 64 * (wave >> 1);
+    const int i0 = ti * TILE, j0 = tj * TILE, wi = 32 * U * (wave & 1), wj = 32 * U * (wave >> 1);
 
-    words_t r[8];
+    words_t r[4 * U];
     const _Float16 *pa = a.A.hi + z * a.A.each + (size_t)(i0 + ((int)threadIdx.x >> 2)) * a.A.stride + ((int)threadIdx.x & 3) * 8;
-    const _Float16 *pb = a.B.hi + z * a.B.each + (kBack ? (size_t)((int)threadIdx.x >> 4) * a.B.stride + j0 + ((int)threadIdx.x & 15) * 8
+    const _Float16 *pb = a.B.hi + z * a.B.each + (kBack ? (size_t)((int)threadIdx.x / kBackRow) * a.B.stride + j0 + (int)threadIdx.x % kBackRow * 8
                                                         : (size_t)(j0 + ((int)threadIdx.x >> 2)) * a.B.stride + ((int)threadIdx.x & 3) * 8);
     const ptrdiff_t la = a.A.lo - a.A.hi, lb = a.B.lo - a.B.hi;
     auto fetch = [&]() {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const _Float16 *qa = pa + (size_t)(64 * i) * a.A.stride, *qb = pb + (size_t)((kBack ? 16 : 64) * i) * a.B.stride;
+        for (int i = 0; i < U; ++i) {
+            const _Float16 *qa = pa + (size_t)(kStepA * i) * a.A.stride, *qb = pb + (size_t)(kStepB * i) * a.B.stride;
             r[i] = *reinterpret_cast<const words_t *>(qa);
-            r[2 + i] = *reinterpret_cast<const words_t *>(qa + la);
-            r[4 + i] = *reinterpret_cast<const words_t *>(qb);
-            r[6 + i] = *reinterpret_cast<const words_t *>(qb + lb);
+            r[U + i] = *reinterpret_cast<const words_t *>(qa + la);
+            r[2 * U + i] = *reinterpret_cast<const words_t *>(qb);
+            r[3 * U + i] = *reinterpret_cast<const words_t *>(qb + lb);
         }
         pa += kDepth;
         pb += kBack ? (size_t)kDepth * a.B.stride : (size_t)kDepth;
     };
-    const int oa = ((int)threadIdx.x >> 2) * kRowA + ((int)threadIdx.x & 3) * 8, ob = kBack ? ((int)threadIdx.x >> 4) * kRowB + ((int)threadIdx.x & 15) * 8 : oa;
+    const int oa = ((int)threadIdx.x >> 2) * kRowA + ((int)threadIdx.x & 3) * 8, ob = kBack ? (int)threadIdx.x / kBackRow * kRowB + (int)threadIdx.x % kBackRow * 8 : oa;
     auto keep = [&](_Float16 *to) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int qa = oa + 64 * i * kRowA, qb = ob + (kBack ? 16 : 64) * i * kRowB;
+        for (int i = 0; i < U; ++i) {
+            const int qa = oa + kStepA * i * kRowA, qb = ob + kStepB * i * kRowB;
             *reinterpret_cast<words_t *>(to + qa) = r[i];
-            *reinterpret_cast<words_t *>(to + kTile * kRowA + qa) = r[2 + i];
-            *reinterpret_cast<words_t *>(to + 2 * kTile * kRowA + qb) = r[4 + i];
-            *reinterpret_cast<words_t *>(to + 2 * kTile * kRowA + kSizeB + qb) = r[6 + i];
+            *reinterpret_cast<words_t *>(to + kSizeA + qa) = r[U + i];
+            *reinterpret_cast<words_t *>(to + 2 * kSizeA + qb) = r[2 * U + i];
+            *reinterpret_cast<words_t *>(to + 2 * kSizeA + kSizeB + qb) = r[3 * U + i];
         }
     };
 
-    acc_t sum[2][2];
+    acc_t sum[U][U];
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int w = 0; w < 2; ++w) sum[u][w] = zero();
+        for (int w = 0; w < U; ++w) sum[u][w] = zero();
     fetch();
-    for (int k0 = 0, b = 0; k0 < a.depth; k0 += kDepth, b ^= kStages - 1) {
-        if (kStages == 1) __syncthreads();
+    for (int k0 = 0, b = 0; k0 < a.depth; k0 += kDepth, b ^= 1) {
         keep(lds[b]);
         __syncthreads();
         if (k0 + kDepth < a.depth) fetch();
-        const _Float16 *A = lds[b], *B = lds[b] + 2 * kTile * kRowA;
+        const _Float16 *A = lds[b], *B = lds[b] + 2 * kSizeA;
 #pragma unroll
         for (int s = 0; s < kDepth / 16; ++s) {
-            half8_t ah[2], al[2], bh[2], bl[2];
+            half8_t ah[U], al[U], bh[U], bl[U];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
+            for (int u = 0; u < U; ++u) {
                 const _Float16 *p = A + (wi + 32 * u + col) * kRowA + 16 * s + 8 * half;
                 ah[u] = read8(p);
-                al[u] = read8(p + kTile * kRowA);
+                al[u] = read8(p + kSizeA);
                 if constexpr (kBack) {
                     bh[u] = read_column(B, kRowB, 16 * s, wj + 32 * u, lane);
                     bl[u] = read_column(B + kSizeB, kRowB, 16 * s, wj + 32 * u, lane);
@@ -213,15 +209,15 @@ __global__ __launch_bounds__(kBlock, KOCC) void ortho_product_kernel(const Produ
 #pragma unroll
             for (int which = 0; which < 3; ++which)
 #pragma unroll
-                for (int u = 0; u < 2; ++u)
+                for (int u = 0; u < U; ++u)
 #pragma unroll
-                    for (int w = 0; w < 2; ++w) sum[u][w] = mfma(which == 2 ? bl[w] : bh[w], which == 1 ? al[u] : ah[u], sum[u][w]);
+                    for (int w = 0; w < U; ++w) sum[u][w] = mfma(which == 2 ? bl[w] : bh[w], which == 1 ? al[u] : ah[u], sum[u][w]);
         }
     }
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int w = 0; w < 2; ++w) {
+        for (int w = 0; w < U; ++w) {
             const int i = i0 + wi + 32 * u + col;
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
@@ -251,9 +247,141 @@ __global__ __launch_bounds__(kBlock, KOCC) void ortho_product_kernel(const Produ
         }
 }
 
+template <int WHAT>
+int product(const ProductArgs &p, int mp, int np, int batch, hipStream_t st) {
+    constexpr bool kBack = WHAT == UPDATE || WHAT == LAST;
+    ProductArgs a = p;
+    const int64_t tm = mp / kTile, tn = np / kTile, large = (kBack ? tm * tn : tm * (tm + 1) / 2) * batch;
+    const int     U = large >= kEnoughTiles ? 2 : 1;
+    a.tiles_m = mp / (64 * U);
+    a.tiles_n = np / (64 * U);
+    const unsigned tiles = (unsigned)(kBack ? a.tiles_m * a.tiles_n : a.tiles_m * (a.tiles_m + 1) / 2);
+    LaunchTimer t(st, K_ORTHO_PRODUCT);
+    if (U == 2) ortho_product_kernel<WHAT, 2><<<dim3(tiles, 1, (unsigned)batch), kBlock, 0, st>>>(a);
+    else ortho_product_kernel<WHAT, 1><<<dim3(tiles, 1, (unsigned)batch), kBlock, 0, st>>>(a);
+    return launch_status("ortho_product_kernel");
+}
+
+// ---------------------------------------------------------------- matrices of at most 64 x 128
+// One workgroup does everything in one launch: X in registers (fp32, as the tiles of the last product come out), its two parts and those of A and
+// B in LDS.  Bound by the chain of products (four barriers a step).
+struct SmallArgs {
+    const void *g;
+    void       *out;
+    int   rows, cols, turned, m, n, steps;
+    float a, b, c, eps;
+};
+template <typename T, int NP>
+__global__ __launch_bounds__(kBlock) void ortho_small_kernel(const SmallArgs a)
+{
+    constexpr int kTiles = NP / 64, kRowX = NP + kPad, kRowA = 64 + kPad;   // column tiles to a wavefront: two row tiles by NP / 32
+    __shared__ __align__(16) _Float16 X[2][64 * kRowX], A[2][64 * kRowA], B[2][64 * kRowA];
+    __shared__ double room[4];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
+    const int i = 32 * (wave & 1) + col, jw = 32 * (wave >> 1);           // this lane's row; the wavefront's first column (the next tile 64 further on)
+    const size_t count = (size_t)a.rows * a.cols;
+    const T *g = (const T *)a.g + blockIdx.x * count;
+    double t = 0.0;
+    for (int e = threadIdx.x; e < (int)count; e += kBlock) {
+        const double v = (double)(float)g[e];
+        t = fma(v, v, t);
+    }
+    const double norm = sqrt(block_sum(t, room)) + (double)a.eps;
+    const float  scale = norm > 0.0 || norm != norm ? (float)(1.0 / norm) : 0.0f;
+    float x[kTiles][16];
+    auto place = [&](const int r, const int j) -> size_t { return a.turned ? (size_t)j * a.m + r : (size_t)r * a.n + j; };
+#pragma unroll
+    for (int k = 0; k < kTiles; ++k)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int j = jw + 64 * k + 8 * (r >> 2) + 4 * half + (r & 3);
+            x[k][r] = i < a.m && j < a.n ? (float)g[place(i, j)] * scale : 0.0f;
+        }
+    auto keep4 = [&](_Float16 *hi, _Float16 *lo, const int at, const float (&v)[4]) {
+        half4_t h, l;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            h[e] = (_Float16)v[e];
+            l[e] = (_Float16)(v[e] - (float)h[e]);
+        }
+        *reinterpret_cast<half4_t *>(hi + at) = h;
+        *reinterpret_cast<half4_t *>(lo + at) = l;
+    };
+    for (int step = 0; step < a.steps; ++step) {
+#pragma unroll
+        for (int k = 0; k < kTiles; ++k)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = x[k][4 * q + e] * kScaleX;
+                keep4(X[0], X[1], i * kRowX + jw + 64 * k + 8 * q + 4 * half, v);
+            }
+        __syncthreads();
+        acc_t s = zero();                // A: rows i, columns jw ..
+#pragma unroll
+        for (int k = 0; k < NP / 16; ++k) {
+            const int pi = i * kRowX + 16 * k + 8 * half, pj = (jw + col) * kRowX + 16 * k + 8 * half;
+            const half8_t ah = read8(X[0] + pi), al = read8(X[1] + pi), bh = read8(X[0] + pj), bl = read8(X[1] + pj);
+            s = mfma(bh, ah, s);
+            s = mfma(bh, al, s);
+            s = mfma(bl, ah, s);
+        }
+        float y[16];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[4 * q + e] = v[e] = s[4 * q + e] * (kScaleA / (kScaleX * kScaleX));
+            keep4(A[0], A[1], i * kRowA + jw + 8 * q + 4 * half, v);
+        }
+        __syncthreads();
+        s = zero();
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int pi = i * kRowA + 16 * k + 8 * half, pj = (jw + col) * kRowA + 16 * k + 8 * half;
+            const half8_t ah = read8(A[0] + pi), al = read8(A[1] + pi), bh = read8(A[0] + pj), bl = read8(A[1] + pj);
+            s = mfma(bh, ah, s);
+            s = mfma(bh, al, s);
+            s = mfma(bl, ah, s);
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = fmaf(a.b * (kScaleB / kScaleA), y[4 * q + e], s[4 * q + e] * (a.c * (kScaleB / (kScaleA * kScaleA))));
+            keep4(B[0], B[1], i * kRowA + jw + 8 * q + 4 * half, v);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kTiles; ++k) {
+            s = zero();
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                const int pi = i * kRowA + 16 * d + 8 * half;
+                const half8_t ah = read8(B[0] + pi), al = read8(B[1] + pi);
+                const half8_t bh = read_column(X[0], kRowX, 16 * d, jw + 64 * k, lane), bl = read_column(X[1], kRowX, 16 * d, jw + 64 * k, lane);
+                s = mfma(bh, ah, s);
+                s = mfma(bh, al, s);
+                s = mfma(bl, ah, s);
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) x[k][r] = fmaf(a.a, x[k][r], s[r] * (1.0f / (kScaleB * kScaleX)));
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int k = 0; k < kTiles; ++k)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int j = jw + 64 * k + 8 * (r >> 2) + 4 * half + (r & 3);
+            if (i < a.m && j < a.n) ((T *)a.out)[blockIdx.x * count + place(i, j)] = (T)x[k][r];
+        }
+}
+
 struct Shape {
     int    m, n, mp, np, parts;
-    bool   turned;
+    bool   turned, small;
     size_t x[2], a, b, norm, bytes;
 };
 Shape shape_of(const cngp_ortho_config *c) {
@@ -264,6 +392,8 @@ Shape shape_of(const cngp_ortho_config *c) {
     s.mp = (s.m + kTile - 1) / kTile * kTile;
     s.np = (s.n + kTile - 1) / kTile * kTile;
     s.parts = (int)std::max<int64_t>(1, std::min<int64_t>((int64_t)s.m * s.n / 4096, std::max(1, kNormParts / std::max(1, std::min(c->batch, 8)))));
+    s.small = s.m <= 64 && s.n <= 128;
+    if (s.small) return s;
     size_t at = 0;
     auto take = [&](bool wanted, size_t bytes) { const size_t o = at; if (wanted) at += align256(bytes); return o; };
     const size_t batch = (size_t)c->batch, x = batch * s.mp * s.np * 4, a = batch * s.mp * s.mp * 4;
@@ -312,6 +442,19 @@ int norm_and_start(const cngp_ortho_config *c, const Shape &s, const T *g, T *ou
     return launch_status("ortho_start_kernel");
 }
 
+template <typename T>
+void launch_small(const SmallArgs &a, int batch, hipStream_t st) {
+    if (a.n <= 64) ortho_small_kernel<T, 64><<<(unsigned)batch, kBlock, 0, st>>>(a);
+    else ortho_small_kernel<T, 128><<<(unsigned)batch, kBlock, 0, st>>>(a);
+}
+int small(const cngp_ortho_config *c, const Shape &s, const void *g, void *out, hipStream_t st) {
+    SmallArgs a{g, out, c->rows, c->cols, s.turned, s.m, s.n, c->steps, c->a, c->b, c->c, c->eps};
+    LaunchTimer t(st, K_ORTHO);
+    if (c->io_dtype == CNGP_F16) launch_small<_Float16>(a, c->batch, st);
+    else launch_small<float>(a, c->batch, st);
+    return launch_status("ortho_small_kernel");
+}
+
 }  // namespace
 
 extern "C" {
@@ -322,35 +465,30 @@ int cngp_orthogonalise(const cngp_ortho_config *cfg, const void *g, void *out, v
     if (int rc = check(cfg)) return rc;
     if (!g || !out) return CNGP_ERR_NULL;
     const Shape s = shape_of(cfg);
+    if (s.small) return small(cfg, s, g, out, (hipStream_t)stream);
     if (s.bytes && (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < s.bytes)) return CNGP_ERR_WORKSPACE;
     char *ws = (char *)workspace;
     hipStream_t st = (hipStream_t)stream;
     if (int rc = cfg->io_dtype == CNGP_F16 ? norm_and_start(cfg, s, (const _Float16 *)g, (_Float16 *)out, ws, st) : norm_and_start(cfg, s, (const float *)g, (float *)out, ws, st))
         return rc;
     const Pair A = pair_of(ws, s.a, s.mp, s.mp, cfg->batch), B = pair_of(ws, s.b, s.mp, s.mp, cfg->batch);
-    const int  tm = s.mp / kTile, tn = s.np / kTile;
     for (int step = 0; step < cfg->steps; ++step) {
         const bool last = step + 1 == cfg->steps;
         const Pair X = pair_of(ws, s.x[step & 1], s.mp, s.np, cfg->batch), Y = last ? X : pair_of(ws, s.x[1 - (step & 1)], s.mp, s.np, cfg->batch);
-        LaunchTimer t(st, K_ORTHO_PRODUCT);
         ProductArgs p{};
-        p.tiles_m = tm; p.tiles_n = tn;
         p.A = X; p.B = X; p.C = A; p.D = A;
         p.depth = s.np; p.of_sum = kScaleA / (kScaleX * kScaleX);
-        ortho_product_kernel<GRAM><<<dim3((unsigned)(tm * (tm + 1) / 2), 1, (unsigned)cfg->batch), kBlock, 0, st>>>(p);
-        if (int rc = launch_status("ortho_product_kernel")) return rc;
+        if (int rc = product<GRAM>(p, s.mp, s.np, cfg->batch, st)) return rc;
         p.A = A; p.B = A; p.C = B; p.D = A;
         p.depth = s.mp; p.of_sum = cfg->c * kScaleB / (kScaleA * kScaleA); p.of_d = cfg->b * kScaleB / kScaleA;
-        ortho_product_kernel<POLY><<<dim3((unsigned)(tm * (tm + 1) / 2), 1, (unsigned)cfg->batch), kBlock, 0, st>>>(p);
-        if (int rc = launch_status("ortho_product_kernel")) return rc;
+        if (int rc = product<POLY>(p, s.mp, s.np, cfg->batch, st)) return rc;
         p.A = B; p.B = X; p.C = Y; p.D = X;
         p.depth = s.mp; p.of_sum = 1.0f / kScaleB; p.of_d = cfg->a;
         if (last) {
             p.of_sum /= kScaleX; p.of_d /= kScaleX;
             p.out = out; p.m = s.m; p.n = s.n; p.turned = s.turned; p.out_f16 = cfg->io_dtype == CNGP_F16;
-            ortho_product_kernel<LAST><<<dim3((unsigned)(tm * tn), 1, (unsigned)cfg->batch), kBlock, 0, st>>>(p);
-        } else ortho_product_kernel<UPDATE><<<dim3((unsigned)(tm * tn), 1, (unsigned)cfg->batch), kBlock, 0, st>>>(p);
-        if (int rc = launch_status("ortho_product_kernel")) return rc;
+        }
+        if (int rc = last ? product<LAST>(p, s.mp, s.np, cfg->batch, st) : product<UPDATE>(p, s.mp, s.np, cfg->batch, st)) return rc;
     }
     return CNGP_OK;
 }

@@ -139,61 +139,80 @@ __global__ __launch_bounds__(kBlock) void rotate_kernel(const RotateArgs a)
                 }
             }
         }
-        for (int h = h0; h < h1; ++h) {
-            const int    w = h >= a.heads[0];
-            const size_t at = ((size_t)row * a.heads[w] + (w ? h - a.heads[0] : h)) * a.dim;
-            float x[ITEMS][V], u[ITEMS][V];
+        // queries, then keys; a head ahead is loaded while one is worked on
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+            const int n0 = w ? a.heads[0] : 0, first_h = (h0 > n0 ? h0 : n0) - n0, last_h = (h1 < n0 + a.heads[w] ? h1 : n0 + a.heads[w]) - n0;
+            if (first_h >= last_h) continue;
+            float gain[ITEMS][V];
 #pragma unroll
             for (int n = 0; n < ITEMS; ++n) {
                 const I it(lane + n * LANES, a.dim, a.pairs);
-                if (!BWD || NORM) it.load((const T *)a.x[w] + at, a.dim, x[n]);
-                if (BWD) it.load((const T *)a.dy[w] + at, a.dim, u[n]);
+#pragma unroll
+                for (int j = 0; j < V; ++j) gain[n][j] = NORM && a.gamma[w] && it.there(j, a.dim) ? a.gamma[w][it.component(j)] : 1.0f;
             }
-            float r = 1.0f;
-            if (NORM) {
-                float t = 0.0f;
+            const T *from = (const T *)a.x[w] + (size_t)row * a.heads[w] * a.dim, *up = (const T *)a.dy[w] + (size_t)row * a.heads[w] * a.dim;
+            T       *to = (T *)a.y[w] + (size_t)row * a.heads[w] * a.dim;
+            float x[ITEMS][V], u[ITEMS][V], xn[ITEMS][V], un[ITEMS][V];
+            auto load = [&](const int h, float (&xo)[ITEMS][V], float (&uo)[ITEMS][V]) {
+#pragma unroll
+                for (int n = 0; n < ITEMS; ++n) {
+                    const I it(lane + n * LANES, a.dim, a.pairs);
+                    if (!BWD || NORM) it.load(from + h * a.dim, a.dim, xo[n]);
+                    if (BWD) it.load(up + h * a.dim, a.dim, uo[n]);
+                }
+            };
+            load(first_h, xn, un);
+            for (int h = first_h; h < last_h; ++h) {
 #pragma unroll
                 for (int n = 0; n < ITEMS; ++n)
 #pragma unroll
-                    for (int j = 0; j < V; ++j) t = fmaf(x[n][j], x[n][j], t);
-                r = 1.0f / sqrtf(fmaf(lanes_sum<LANES>(t), a.inverse_dim, a.eps));
-            }
-            float dot = 0.0f;
-#pragma unroll
-            for (int n = 0; n < ITEMS; ++n) {
-                const I it(lane + n * LANES, a.dim, a.pairs);
-                float g[V];
-#pragma unroll
-                for (int j = 0; j < V; ++j) g[j] = NORM && a.gamma[w] && it.there(j, a.dim) ? a.gamma[w][it.component(j)] : 1.0f;
-                if (!BWD) {
-#pragma unroll
-                    for (int j = 0; j < V; ++j) u[n][j] = NORM ? x[n][j] * r * g[j] : x[n][j];
-                }
-#pragma unroll
-                for (int k = 0; k < A; ++k) {
-                    const float p = u[n][I::first(k)], q = u[n][I::second(k)];
-                    u[n][I::first(k)] = fmaf(p, c[n][k], -(q * s[n][k]));
-                    u[n][I::second(k)] = fmaf(p, s[n][k], q * c[n][k]);
-                }
-                if (BWD && NORM) {
-#pragma unroll
                     for (int j = 0; j < V; ++j) {
-                        x[n][j] *= r;
-                        if (w) sums[1][n][j] += work ? u[n][j] * x[n][j] : 0.0f;
-                        else sums[0][n][j] += work ? u[n][j] * x[n][j] : 0.0f;
-                        u[n][j] *= g[j];
-                        dot = fmaf(u[n][j], x[n][j], dot);
+                        if (!BWD || NORM) x[n][j] = xn[n][j];
+                        if (BWD) u[n][j] = un[n][j];
+                    }
+                if (h + 1 < last_h) load(h + 1, xn, un);
+                float r = 1.0f;
+                if (NORM) {
+                    float t = 0.0f;
+#pragma unroll
+                    for (int n = 0; n < ITEMS; ++n)
+#pragma unroll
+                        for (int j = 0; j < V; ++j) t = fmaf(x[n][j], x[n][j], t);
+                    r = rsqrtf(fmaf(lanes_sum<LANES>(t), a.inverse_dim, a.eps));
+                }
+                float dot = 0.0f;
+#pragma unroll
+                for (int n = 0; n < ITEMS; ++n) {
+                    if (!BWD) {
+#pragma unroll
+                        for (int j = 0; j < V; ++j) u[n][j] = NORM ? x[n][j] * r * gain[n][j] : x[n][j];
+                    }
+#pragma unroll
+                    for (int k = 0; k < A; ++k) {
+                        const float p = u[n][I::first(k)], q = u[n][I::second(k)];
+                        u[n][I::first(k)] = fmaf(p, c[n][k], -(q * s[n][k]));
+                        u[n][I::second(k)] = fmaf(p, s[n][k], q * c[n][k]);
+                    }
+                    if (BWD && NORM) {
+#pragma unroll
+                        for (int j = 0; j < V; ++j) {
+                            x[n][j] *= r;
+                            sums[w][n][j] += work ? u[n][j] * x[n][j] : 0.0f;
+                            u[n][j] *= gain[n][j];
+                            dot = fmaf(u[n][j], x[n][j], dot);
+                        }
                     }
                 }
-            }
-            if (BWD && NORM) dot = lanes_sum<LANES>(dot) * a.inverse_dim;
+                if (BWD && NORM) dot = lanes_sum<LANES>(dot) * a.inverse_dim;
 #pragma unroll
-            for (int n = 0; n < ITEMS; ++n) {
-                const I it(lane + n * LANES, a.dim, a.pairs);
-                if (BWD && NORM)
+                for (int n = 0; n < ITEMS; ++n) {
+                    const I it(lane + n * LANES, a.dim, a.pairs);
+                    if (BWD && NORM)
 #pragma unroll
-                    for (int j = 0; j < V; ++j) u[n][j] = r * fmaf(-x[n][j], dot, u[n][j]);
-                if (work) it.store((T *)a.y[w] + at, a.dim, u[n]);
+                        for (int j = 0; j < V; ++j) u[n][j] = r * fmaf(-x[n][j], dot, u[n][j]);
+                    if (work) it.store(to + h * a.dim, a.dim, u[n]);
+                }
             }
         }
     }

@@ -161,7 +161,7 @@ __global__ __launch_bounds__(64 * kAnchorChunks) void attend_decay_kernel(const 
         const int32_t seq = a.whole ? (int32_t)piece : sequence_of(a.offsets, (int32_t)piece, a.N, a.S, a.rows_each, kAnchorShift);
         const Span    span = span_of(a.offsets, seq, a.N, a.rows_each);
         double sum = 0.0;
-        for (int64_t i = a.whole ? 0 : piece - piece_base(span.begin, seq, kAnchorShift); span.begin + i * kRows < span.end; ++i) {
+        for (int64_t i = a.whole ? 0 : piece - piece_base(span.begin, seq, kAnchorShift); i >= 0 && span.begin + i * kRows < span.end; ++i) {
             const int64_t begin = span.begin + i * kRows, end = begin + kRows < span.end ? begin + kRows : span.end;
             const int     chunks = (int)((end - begin + kChunk - 1) >> kChunkShift);
             const bool    anchored = i != 0;

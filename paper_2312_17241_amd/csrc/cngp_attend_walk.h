@@ -182,7 +182,7 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
     int chunk0 = 0;                                         // the first chunk's number in its sequence
     if (a.seg_shift) {
         const int i = piece - piece_base(span.begin, seq, a.seg_shift);
-        if ((int64_t)begin + ((int64_t)i << a.seg_shift) >= end) return;
+        if (i < 0 || (int64_t)begin + ((int64_t)i << a.seg_shift) >= end) return;      // (i < 0: rows before the first sequence)
         begin += i << a.seg_shift;
         end = end - begin > 1 << a.seg_shift ? begin + (1 << a.seg_shift) : end;
         chunk0 = i << (a.seg_shift - kChunkShift);

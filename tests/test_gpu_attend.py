@@ -118,6 +118,34 @@ def test_long_sequences_are_cut_and_anchored(io, rows):
     check([4300], H=1, K=1, dk=40, dv=8, io=io, rows=rows, uniform=True)
 
 
+@pytest.mark.parametrize("rows", [True, False])
+def test_many_rows_before_the_first_sequence(rows):
+    """More of them than a segment, or a stretch of the decays' gradient, has: their pieces belong to no sequence."""
+    check([1500, 2600, 7], H=1, K=1, dk=8, dv=8, rows=rows, slow=True, lead=2900, longest=2600)
+    check([1500, 2600, 7], H=2, K=1, dk=8, dv=8, rows=rows, slow=True, lead=2900, longest=600)       # ... of sequences that are longer than said
+
+
+@pytest.mark.parametrize("sharp", [0.0, 0.3, 3.0])
+@pytest.mark.parametrize("io", [F16, F32])
+def test_decays_mild_and_sharp(io, sharp):
+    """Chunks whose decay stays within 2^+-6 go by two factors to a pair, others by one exponential: both, and growth, against the same recurrence."""
+    N, H, D = 200, 2, 32
+    d = make(N, 1, H, H, D, D, io, True, 13)
+    d["decay"] = np.where(np.arange(N)[:, None] % 3 == 0, -sharp, 0.25 * min(sharp, 0.3)).astype(np.float32) + np.zeros((N, H), np.float32)
+    f = {n: a.astype(np.float64) for n, a in d.items()}
+    args = (f["q"], f["k"], f["v"], f["decay"], [(0, N)], f["h0"], 0.2, f["dy"], f["dlast"])
+    args = args[:6] + (float(np.float32(0.2)),) + args[7:]
+    want, bound = R.attend(*args), R.attend_bounds(*args)
+    cfg = cngp.AttendConfig(H, H, D, D, io, scale=0.2, flags=cngp.ATTEND_ROW_DECAY)
+    t = {n: dev(a) for n, a in d.items()}
+    y, last = cngp.attend_fwd(cfg, t["q"], t["k"], t["v"], t["decay"], h0=t["h0"])
+    back = cngp.attend_bwd(cfg, t["q"], t["k"], t["v"], t["decay"], dy=t["dy"], dlast=t["dlast"], h0=t["h0"])
+    R.within("y", host(y), want["y"], bound["y"], NP[io])
+    R.within("last", host(last), want["last"], bound["last"])
+    for name, got, key in zip(("dq", "dk", "dv", "ddecay", "dh0"), back, ("dq", "dk", "dv", "dg", "dh0")):
+        R.within(name, host(got), want[key], bound[key], NP[io] if name in ("dq", "dk", "dv") else np.float32)
+
+
 def test_state_updated_in_place():
     for N, S, H, D in ((6, 6, 3, 20), (640, 2, 2, 64), (2600, 1, 1, 16)):
         d = make(N, S, H, H, D, D, F32, True, 5)

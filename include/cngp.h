@@ -499,8 +499,10 @@ int cngp_rotate_bwd(const cngp_rotate_config *cfg, const void *q, const void *k,
  * the norm in 64 bits.  A matrix of zeros gives zeros; one with a value that is not finite gives values that are not finite.
  * Not part of the paper's method: an optimiser step for the matrices around the encoding, where cngp_adam_step takes arrays entry by entry.
  *   g dev io_dtype [batch, rows, cols]        out like g, written; may be g itself
- *   rows, cols 1 .. 16384      batch 1 .. 65535      steps 0 .. 32      eps >= 0      |a|, |b|, |c| <= 16, and such that singular values stay below 4
- *   workspace dev, 256-byte aligned, cngp_orthogonalise_workspace_bytes(cfg) bytes (may be 0); undefined before and after */
+ *   rows, cols 1 .. 16384      batch 1 .. 65535      steps 0 .. 32      eps >= 0      |a|, |b|, |c| <= 16, such that with s the largest singular value of
+ *   any step (1 at first) s stays below 4 and |b| s^2 + |c| s^4 below 64: fp16's range; beyond it results are not finite
+ *   workspace dev, 256-byte aligned, cngp_orthogonalise_workspace_bytes(cfg) bytes (0 where the smaller side is at most 64 and the larger at
+ *   most 128); undefined before and after */
 typedef struct cngp_ortho_config {
     int32_t  batch, rows, cols;
     int32_t  io_dtype;        /* cngp_dtype of g and out */
@@ -510,6 +512,23 @@ typedef struct cngp_ortho_config {
 } cngp_ortho_config;
 size_t cngp_orthogonalise_workspace_bytes(const cngp_ortho_config *cfg);
 int cngp_orthogonalise(const cngp_ortho_config *cfg, const void *g, void *out, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Optimiser step of matrices by the orthogonalised update (what cngp_adam_step is for arrays), e.g. of the decoder's W1, W2, W3:
+ *     m = momentum * m + grad_scale * grad          u = grad_scale * grad + momentum * m with nesterov, else m
+ *     master = master (1 - lr * weight_decay) - lr * orthogonalised u
+ * The momentum is updated in the norm's pass, the weights at the end of the last product.
+ *   cfg as above, io_dtype CNGP_F32      master, m, grad dev float32 [batch, rows, cols], master and m updated in place (m zero before the first step)
+ *   half_copy dev float16, receives the updated weights rounded to fp16, or NULL      clear_grad != 0 sets grad to zero afterwards
+ *   workspace as for cngp_orthogonalise */
+typedef struct cngp_muon {
+    float   lr;             /* >= 0; a factor for the shape, such as sqrt(max(1, rows / cols)), is the caller's */
+    float   momentum;       /* 0 <= momentum < 1 */
+    float   weight_decay;   /* >= 0 */
+    float   grad_scale;     /* e.g. 1 / loss scale; must be finite */
+    int32_t nesterov;       /* 0 or 1 */
+} cngp_muon;
+int cngp_muon_step(const cngp_ortho_config *cfg, const cngp_muon *opt, float *master, void *half_copy, float *m, float *grad, int clear_grad, void *workspace,
+                   size_t workspace_bytes, void *stream);
 
 /* Lookup of codes with scaling, and its gradient: a row per image, object or token, chosen by an id per point, alone or added to
  * the point's encoding (a field conditioned on the image it is seen in, several shapes in one field).

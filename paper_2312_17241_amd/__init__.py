@@ -634,5 +634,5 @@ def pack4(D_c_u8):
 
 from .operators import (I32, I64, RECUR_LOG_GATE, RECUR_MIX, RECUR_REVERSE, EmbedConfig, RecurConfig, embed_bwd, embed_fwd,  # noqa: E402
                         embed_workspace_bytes, probe_balance, probe_balance_workspace_bytes, recur_bwd, recur_fwd, recur_workspace_bytes)
-from .mixer import (ATTEND_ROW_DECAY, ROTATE_NEXT, ROTATE_NORM, AttendConfig, OrthoConfig, RotateConfig, attend_bwd, attend_fwd,  # noqa: E402
-                    attend_workspace_bytes, orthogonalise, orthogonalise_workspace_bytes, rotate_bwd, rotate_fwd, rotate_workspace_bytes)
+from .mixer import (ATTEND_ROW_DECAY, ROTATE_NEXT, ROTATE_NORM, AttendConfig, Muon, OrthoConfig, RotateConfig, attend_bwd, attend_fwd,  # noqa: E402
+                    attend_workspace_bytes, muon_step, orthogonalise, orthogonalise_workspace_bytes, rotate_bwd, rotate_fwd, rotate_workspace_bytes)

@@ -21,7 +21,7 @@ constexpr int kPad = 8;                                     // halves between ro
 // X, A and B are kept times these: singular values of 1 spread over rows of thousands, and their low parts, would be subnormal fp16 numbers.  What
 // is left above: entries of X below 4 (so its singular values may be), of A below 16, of B below 64.
 constexpr float kScaleX = 16384.0f, kScaleA = 4096.0f, kScaleB = 1024.0f;
-constexpr int kNormParts = 256;
+constexpr int kNormParts = 1024;
 constexpr int64_t kEnoughTiles = 256;                       // of 128 x 128: a CU each
 
 // High and low parts of a matrix, rows of `stride` values.
@@ -51,6 +51,32 @@ __device__ __forceinline__ void get4(const Pair &p, const size_t at, float (&v)[
     for (int e = 0; e < 4; ++e) v[e] = (float)h[e] + (float)l[e];
 }
 
+// ---------------------------------------------------------------- what is orthogonalised, and what becomes of it
+// A matrix of its own, or the momentum of an optimiser step: then the norm's pass takes the gradient into it, and the result moves the weights.
+struct Step {
+    float    *m, *grad, *master;         // m NULL: a plain matrix
+    _Float16 *half;
+    float     momentum, scale, lr, keep; // keep: 1 - lr * weight decay
+    int       nesterov, clear;
+};
+__device__ __forceinline__ float direction(const Step &st, const size_t at) {
+    return st.nesterov ? fmaf(st.momentum, st.m[at], st.grad[at] * st.scale) : st.m[at];
+}
+template <typename T>
+__device__ __forceinline__ float entry(const T *g, const Step &st, const size_t at) { return st.m ? direction(st, at) : (float)g[at]; }
+template <typename T>
+__device__ __forceinline__ float taken(const T *g, const Step &st, const size_t at) {
+    if (!st.m) return (float)g[at];
+    st.m[at] = fmaf(st.momentum, st.m[at], st.grad[at] * st.scale);
+    return direction(st, at);
+}
+__device__ __forceinline__ void moved(const Step &st, const size_t at, const float v) {
+    const float w = fmaf(-st.lr, v, st.master[at] * st.keep);
+    st.master[at] = w;
+    if (st.half) st.half[at] = (_Float16)w;
+    if (st.clear) st.grad[at] = 0.0f;
+}
+
 // ---------------------------------------------------------------- norm, start, no steps
 __device__ __forceinline__ double block_sum(double v, double *room) {
 #pragma unroll
@@ -62,15 +88,24 @@ __device__ __forceinline__ double block_sum(double v, double *room) {
 }
 
 template <typename T>
-__global__ __launch_bounds__(kBlock) void ortho_norm_kernel(const T *__restrict__ g, const int64_t n, double *__restrict__ parts)
+__global__ __launch_bounds__(kBlock) void ortho_norm_kernel(const T *__restrict__ g, const Step st, const int64_t n, double *__restrict__ parts)
 {
     __shared__ double room[4];
-    const T *x = g + (size_t)blockIdx.y * n;
-    double t = 0.0;
-    for (int64_t i = blockIdx.x * (int64_t)kBlock + threadIdx.x; i < n; i += (int64_t)gridDim.x * kBlock) {
-        const double v = (double)(float)x[i];
-        t = fma(v, v, t);
+    const size_t first = (size_t)blockIdx.y * n;
+    double sums[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) sums[u] = 0.0;
+    const int64_t step = (int64_t)gridDim.x * kBlock;
+    for (int64_t i = blockIdx.x * (int64_t)kBlock + threadIdx.x; i < n; i += 8 * step) {
+        float v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = i + u * step < n ? taken(g, st, first + i + u * step) : 0.0f;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) sums[u] = fma((double)v[u], (double)v[u], sums[u]);
     }
+    double t = 0.0;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) t += sums[u];
     t = block_sum(t, room);
     if (threadIdx.x == 0) parts[(size_t)blockIdx.y * gridDim.x + blockIdx.x] = t;
 }
@@ -84,18 +119,18 @@ __device__ __forceinline__ float inverse_norm(const double *parts, const int cou
 
 // X from G (transposed where `turned`), with zeros behind its edges: 64 x 64 tiles.
 template <typename T>
-__global__ __launch_bounds__(kBlock) void ortho_start_kernel(const T *__restrict__ g, const int rows, const int cols, const bool turned, const double *__restrict__ parts,
+__global__ __launch_bounds__(kBlock) void ortho_start_kernel(const T *__restrict__ g, const Step st, const int rows, const int cols, const bool turned, const double *__restrict__ parts,
                                                              const int count, const float eps, const float scale, const Pair X)
 {
     __shared__ double room[4];
     __shared__ float  tile[64][65];
     const float inv = inverse_norm(parts, count, eps, room) * scale;
-    const T *x = g + (size_t)blockIdx.z * rows * cols;
+    const size_t first = (size_t)blockIdx.z * rows * cols;
     const int m0 = (int)blockIdx.y * 64, n0 = (int)blockIdx.x * 64;     // of X
     const int c = threadIdx.x & 63;
     for (int r = threadIdx.x >> 6; r < 64; r += 4) {
         const int row = (turned ? n0 : m0) + r, col = (turned ? m0 : n0) + c;
-        const float v = row < rows && col < cols ? (float)x[(size_t)row * cols + col] * inv : 0.0f;
+        const float v = row < rows && col < cols ? entry(g, st, first + (size_t)row * cols + col) * inv : 0.0f;
         if (turned) tile[c][r] = v;
         else tile[r][c] = v;
     }
@@ -108,12 +143,17 @@ __global__ __launch_bounds__(kBlock) void ortho_start_kernel(const T *__restrict
 }
 
 template <typename T>
-__global__ __launch_bounds__(kBlock) void ortho_scale_kernel(const T *g, T *out, const int64_t n, const double *__restrict__ parts, const int count, const float eps)
+__global__ __launch_bounds__(kBlock) void ortho_scale_kernel(const T *g, const Step st, T *out, const int64_t n, const double *__restrict__ parts, const int count, const float eps)
 {
     __shared__ double room[4];
     const float inv = inverse_norm(parts, count, eps, room);
     for (int64_t i = blockIdx.x * (int64_t)kBlock + threadIdx.x; i < n; i += (int64_t)gridDim.x * kBlock)
-        out[(size_t)blockIdx.z * n + i] = (T)((float)g[(size_t)blockIdx.z * n + i] * inv);
+    {
+        const size_t at = (size_t)blockIdx.z * n + i;
+        const float  v = entry(g, st, at) * inv;
+        if (st.m) moved(st, at, v);
+        else out[at] = (T)v;
+    }
 }
 
 // ---------------------------------------------------------------- products
@@ -124,6 +164,7 @@ struct ProductArgs {
     float of_sum, of_d;                  // C = of_sum * product + of_d * D
     void *out;                           // LAST: the result
     int   m, n, turned, out_f16;
+    Step  step;
 };
 
 // A tile of 64 U x 64 U of a product by four wavefronts of 32 U x 32 U; computed transposed (a lane has a row of C and four neighbouring columns in
@@ -240,7 +281,8 @@ __global__ __launch_bounds__(kBlock, 2) void ortho_product_kernel(const ProductA
                     for (int e = 0; e < 4; ++e)
                         if (j + e < a.n) {
                             const size_t at = z * (size_t)a.m * a.n + (a.turned ? (size_t)(j + e) * a.m + i : (size_t)i * a.n + j + e);
-                            if (a.out_f16) ((_Float16 *)a.out)[at] = (_Float16)v[e];
+                            if (a.step.m) moved(a.step, at, v[e]);
+                            else if (a.out_f16) ((_Float16 *)a.out)[at] = (_Float16)v[e];
                             else ((float *)a.out)[at] = v[e];
                         }
             }
@@ -270,6 +312,7 @@ struct SmallArgs {
     void       *out;
     int   rows, cols, turned, m, n, steps;
     float a, b, c, eps;
+    Step  step;
 };
 template <typename T, int NP>
 __global__ __launch_bounds__(kBlock) void ortho_small_kernel(const SmallArgs a)
@@ -280,10 +323,11 @@ __global__ __launch_bounds__(kBlock) void ortho_small_kernel(const SmallArgs a)
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
     const int i = 32 * (wave & 1) + col, jw = 32 * (wave >> 1);           // this lane's row; the wavefront's first column (the next tile 64 further on)
     const size_t count = (size_t)a.rows * a.cols;
-    const T *g = (const T *)a.g + blockIdx.x * count;
+    const size_t first = blockIdx.x * count;
+    const T *g = (const T *)a.g;
     double t = 0.0;
     for (int e = threadIdx.x; e < (int)count; e += kBlock) {
-        const double v = (double)(float)g[e];
+        const double v = (double)taken(g, a.step, first + e);
         t = fma(v, v, t);
     }
     const double norm = sqrt(block_sum(t, room)) + (double)a.eps;
@@ -295,7 +339,7 @@ __global__ __launch_bounds__(kBlock) void ortho_small_kernel(const SmallArgs a)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             const int j = jw + 64 * k + 8 * (r >> 2) + 4 * half + (r & 3);
-            x[k][r] = i < a.m && j < a.n ? (float)g[place(i, j)] * scale : 0.0f;
+            x[k][r] = i < a.m && j < a.n ? entry(g, a.step, first + place(i, j)) * scale : 0.0f;
         }
     auto keep4 = [&](_Float16 *hi, _Float16 *lo, const int at, const float (&v)[4]) {
         half4_t h, l;
@@ -375,7 +419,11 @@ __global__ __launch_bounds__(kBlock) void ortho_small_kernel(const SmallArgs a)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             const int j = jw + 64 * k + 8 * (r >> 2) + 4 * half + (r & 3);
-            if (i < a.m && j < a.n) ((T *)a.out)[blockIdx.x * count + place(i, j)] = (T)x[k][r];
+            if (i < a.m && j < a.n) {
+                const size_t at = first + place(i, j);
+                if (a.step.m) moved(a.step, at, x[k][r]);
+                else ((T *)a.out)[at] = (T)x[k][r];
+            }
         }
 }
 
@@ -391,7 +439,7 @@ Shape shape_of(const cngp_ortho_config *c) {
     s.n = std::max(c->rows, c->cols);
     s.mp = (s.m + kTile - 1) / kTile * kTile;
     s.np = (s.n + kTile - 1) / kTile * kTile;
-    s.parts = (int)std::max<int64_t>(1, std::min<int64_t>((int64_t)s.m * s.n / 4096, std::max(1, kNormParts / std::max(1, std::min(c->batch, 8)))));
+    s.parts = (int)std::max<int64_t>(1, std::min<int64_t>((int64_t)s.m * s.n / 4096, kNormParts / std::min(c->batch, 16)));
     s.small = s.m <= 64 && s.n <= 128;
     if (s.small) return s;
     size_t at = 0;
@@ -427,17 +475,17 @@ Pair pair_of(char *ws, size_t at, int rows, int cols, int batch) {
 }
 
 template <typename T>
-int norm_and_start(const cngp_ortho_config *c, const Shape &s, const T *g, T *out, char *ws, hipStream_t st) {
+int norm_and_start(const cngp_ortho_config *c, const Shape &s, const T *g, const Step &step, T *out, char *ws, hipStream_t st) {
     LaunchTimer t(st, K_ORTHO);
     double *parts = (double *)(ws + s.norm);
     const int64_t n = (int64_t)s.m * s.n;
-    ortho_norm_kernel<T><<<dim3((unsigned)s.parts, (unsigned)c->batch), kBlock, 0, st>>>(g, n, parts);
+    ortho_norm_kernel<T><<<dim3((unsigned)s.parts, (unsigned)c->batch), kBlock, 0, st>>>(g, step, n, parts);
     if (int rc = launch_status("ortho_norm_kernel")) return rc;
     if (c->steps == 0) {
-        ortho_scale_kernel<T><<<dim3((unsigned)std::min<int64_t>((n + 1023) / 1024, 1024), 1, (unsigned)c->batch), kBlock, 0, st>>>(g, out, n, parts, s.parts, c->eps);
+        ortho_scale_kernel<T><<<dim3((unsigned)std::min<int64_t>((n + 1023) / 1024, 1024), 1, (unsigned)c->batch), kBlock, 0, st>>>(g, step, out, n, parts, s.parts, c->eps);
         return launch_status("ortho_scale_kernel");
     }
-    ortho_start_kernel<T><<<dim3((unsigned)(s.np / 64), (unsigned)(s.mp / 64), (unsigned)c->batch), kBlock, 0, st>>>(g, c->rows, c->cols, s.turned, parts, s.parts, c->eps,
+    ortho_start_kernel<T><<<dim3((unsigned)(s.np / 64), (unsigned)(s.mp / 64), (unsigned)c->batch), kBlock, 0, st>>>(g, step, c->rows, c->cols, s.turned, parts, s.parts, c->eps,
                                                                                                                   kScaleX, pair_of(ws, s.x[0], s.mp, s.np, c->batch));
     return launch_status("ortho_start_kernel");
 }
@@ -447,34 +495,25 @@ void launch_small(const SmallArgs &a, int batch, hipStream_t st) {
     if (a.n <= 64) ortho_small_kernel<T, 64><<<(unsigned)batch, kBlock, 0, st>>>(a);
     else ortho_small_kernel<T, 128><<<(unsigned)batch, kBlock, 0, st>>>(a);
 }
-int small(const cngp_ortho_config *c, const Shape &s, const void *g, void *out, hipStream_t st) {
-    SmallArgs a{g, out, c->rows, c->cols, s.turned, s.m, s.n, c->steps, c->a, c->b, c->c, c->eps};
+int small(const cngp_ortho_config *c, const Shape &s, const void *g, const Step &step, void *out, hipStream_t st) {
+    SmallArgs a{g, out, c->rows, c->cols, s.turned, s.m, s.n, c->steps, c->a, c->b, c->c, c->eps, step};
     LaunchTimer t(st, K_ORTHO);
     if (c->io_dtype == CNGP_F16) launch_small<_Float16>(a, c->batch, st);
     else launch_small<float>(a, c->batch, st);
     return launch_status("ortho_small_kernel");
 }
 
-}  // namespace
-
-extern "C" {
-
-size_t cngp_orthogonalise_workspace_bytes(const cngp_ortho_config *cfg) { return check(cfg) ? 0 : shape_of(cfg).bytes; }
-
-int cngp_orthogonalise(const cngp_ortho_config *cfg, const void *g, void *out, void *workspace, size_t workspace_bytes, void *stream) {
-    if (int rc = check(cfg)) return rc;
-    if (!g || !out) return CNGP_ERR_NULL;
+int run(const cngp_ortho_config *cfg, const void *g, const Step &step, void *out, void *workspace, size_t workspace_bytes, hipStream_t st) {
     const Shape s = shape_of(cfg);
-    if (s.small) return small(cfg, s, g, out, (hipStream_t)stream);
+    if (s.small) return small(cfg, s, g, step, out, st);
     if (s.bytes && (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < s.bytes)) return CNGP_ERR_WORKSPACE;
     char *ws = (char *)workspace;
-    hipStream_t st = (hipStream_t)stream;
-    if (int rc = cfg->io_dtype == CNGP_F16 ? norm_and_start(cfg, s, (const _Float16 *)g, (_Float16 *)out, ws, st) : norm_and_start(cfg, s, (const float *)g, (float *)out, ws, st))
-        return rc;
+    if (int rc = cfg->io_dtype == CNGP_F16 ? norm_and_start(cfg, s, (const _Float16 *)g, step, (_Float16 *)out, ws, st)
+                                           : norm_and_start(cfg, s, (const float *)g, step, (float *)out, ws, st)) return rc;
     const Pair A = pair_of(ws, s.a, s.mp, s.mp, cfg->batch), B = pair_of(ws, s.b, s.mp, s.mp, cfg->batch);
-    for (int step = 0; step < cfg->steps; ++step) {
-        const bool last = step + 1 == cfg->steps;
-        const Pair X = pair_of(ws, s.x[step & 1], s.mp, s.np, cfg->batch), Y = last ? X : pair_of(ws, s.x[1 - (step & 1)], s.mp, s.np, cfg->batch);
+    for (int i = 0; i < cfg->steps; ++i) {
+        const bool last = i + 1 == cfg->steps;
+        const Pair X = pair_of(ws, s.x[i & 1], s.mp, s.np, cfg->batch), Y = last ? X : pair_of(ws, s.x[1 - (i & 1)], s.mp, s.np, cfg->batch);
         ProductArgs p{};
         p.A = X; p.B = X; p.C = A; p.D = A;
         p.depth = s.np; p.of_sum = kScaleA / (kScaleX * kScaleX);
@@ -486,11 +525,35 @@ int cngp_orthogonalise(const cngp_ortho_config *cfg, const void *g, void *out, v
         p.depth = s.mp; p.of_sum = 1.0f / kScaleB; p.of_d = cfg->a;
         if (last) {
             p.of_sum /= kScaleX; p.of_d /= kScaleX;
-            p.out = out; p.m = s.m; p.n = s.n; p.turned = s.turned; p.out_f16 = cfg->io_dtype == CNGP_F16;
+            p.out = out; p.m = s.m; p.n = s.n; p.turned = s.turned; p.out_f16 = cfg->io_dtype == CNGP_F16; p.step = step;
         }
         if (int rc = last ? product<LAST>(p, s.mp, s.np, cfg->batch, st) : product<UPDATE>(p, s.mp, s.np, cfg->batch, st)) return rc;
     }
     return CNGP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t cngp_orthogonalise_workspace_bytes(const cngp_ortho_config *cfg) { return check(cfg) ? 0 : shape_of(cfg).bytes; }
+
+int cngp_orthogonalise(const cngp_ortho_config *cfg, const void *g, void *out, void *workspace, size_t workspace_bytes, void *stream) {
+    if (int rc = check(cfg)) return rc;
+    if (!g || !out) return CNGP_ERR_NULL;
+    return run(cfg, g, Step{}, out, workspace, workspace_bytes, (hipStream_t)stream);
+}
+
+int cngp_muon_step(const cngp_ortho_config *cfg, const cngp_muon *opt, float *master, void *half_copy, float *m, float *grad, int clear_grad, void *workspace,
+                   size_t workspace_bytes, void *stream) {
+    if (int rc = check(cfg)) return rc;
+    if (!opt || !master || !m || !grad) return CNGP_ERR_NULL;
+    if (cfg->io_dtype != CNGP_F32) return CNGP_ERR_UNSUPPORTED;
+    if (!(opt->lr >= 0.0f) || !std::isfinite(opt->lr) || !(opt->momentum >= 0.0f && opt->momentum < 1.0f) || !(opt->weight_decay >= 0.0f) ||
+        !std::isfinite(opt->weight_decay) || !std::isfinite(opt->grad_scale) || (opt->nesterov != 0 && opt->nesterov != 1))
+        return CNGP_ERR_INVALID;
+    const Step step{m, grad, master, (_Float16 *)half_copy, opt->momentum, opt->grad_scale, opt->lr, 1.0f - opt->lr * opt->weight_decay, opt->nesterov, clear_grad != 0};
+    return run(cfg, m, step, nullptr, workspace, workspace_bytes, (hipStream_t)stream);
 }
 
 }  // extern "C"

@@ -32,6 +32,10 @@ class COrthoConfig(ctypes.Structure):
         (n, ctypes.c_float) for n in ("a", "b", "c", "eps")] + [("flags", ctypes.c_uint32)]
 
 
+class CMuon(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_float) for n in ("lr", "momentum", "weight_decay", "grad_scale")] + [("nesterov", ctypes.c_int32)]
+
+
 def _declare():
     vp, i64, sz, u32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_size_t, ctypes.c_uint32
     for name, result, args in (
@@ -42,7 +46,8 @@ def _declare():
             ("cngp_rotate_fwd", ctypes.c_int, [vp] * 3 + [i64] + [vp] * 7),
             ("cngp_rotate_bwd", ctypes.c_int, [vp] * 3 + [i64] + [vp] * 11 + [sz, vp]),
             ("cngp_orthogonalise_workspace_bytes", sz, [vp]),
-            ("cngp_orthogonalise", ctypes.c_int, [vp] * 4 + [sz, vp])):
+            ("cngp_orthogonalise", ctypes.c_int, [vp] * 4 + [sz, vp]),
+            ("cngp_muon_step", ctypes.c_int, [vp] * 6 + [ctypes.c_int, vp, sz, vp])):
         f = getattr(_lib, name)
         f.restype, f.argtypes = result, args
 
@@ -213,3 +218,28 @@ def orthogonalise(cfg: OrthoConfig, g, out=True, workspace=None):
     workspace = _room(orthogonalise_workspace_bytes(cfg), workspace, g)
     _check(_lib.cngp_orthogonalise(cfg._ref(), gp, op, *_ws(workspace), _stream()))
     return out
+
+
+@dataclass
+class Muon:
+    """Hyper-parameters of an orthogonalised optimiser step (cngp_muon)."""
+    lr: float = 2e-2
+    momentum: float = 0.95
+    weight_decay: float = 0.0
+    grad_scale: float = 1.0
+    nesterov: bool = True
+
+    def c(self):
+        return CMuon(self.lr, self.momentum, self.weight_decay, self.grad_scale, int(self.nesterov))
+
+
+def muon_step(cfg: OrthoConfig, opt: Muon, master, half_copy, m, grad, clear_grad=False, workspace=None):
+    """cngp_muon_step on float32 matrices [batch, rows, cols] (or [rows, cols] of one); half_copy (float16, same shape) may be None.
+    Updates master and m in place."""
+    shape = (cfg.rows, cfg.cols) if cfg.batch == 1 and master.dim() == 2 else (cfg.batch, cfg.rows, cfg.cols)
+    mp, sp, gp = _dev(master, torch.float32, shape, "master"), _dev(m, torch.float32, shape, "m"), _dev(grad, torch.float32, shape, "grad")
+    hp = _maybe(half_copy, torch.float16, shape, "half_copy")
+    _on_current_device(master, half_copy, m, grad, workspace)
+    workspace = _room(orthogonalise_workspace_bytes(cfg), workspace, master)
+    o = opt.c()
+    _check(_lib.cngp_muon_step(cfg._ref(), ctypes.byref(o), mp, hp, sp, gp, int(bool(clear_grad)), *_ws(workspace), _stream()))

@@ -108,3 +108,41 @@ def test_same_bits_in_any_workspace_and_batch():
     for fill in (0, 255):
         ws = torch.full((cngp.orthogonalise_workspace_bytes(cfg),), fill, dtype=torch.uint8, device=DEV)
         assert torch.equal(cngp.orthogonalise(cfg, g, workspace=ws), ref)
+
+
+@pytest.mark.parametrize("m,n,batch", [(3, 5, 1), (64, 32, 2), (64, 128, 1), (100, 30, 3), (130, 260, 2), (300, 70, 1)])
+@pytest.mark.parametrize("nesterov,clear,half", [(True, True, True), (False, False, False)])
+@pytest.mark.parametrize("steps", [0, 5])
+def test_optimiser_steps(m, n, batch, nesterov, clear, half, steps):
+    """Three steps in a row against 64 bits, each from what the library left: the momentum and the weights are rounded twice each, the direction's
+    own roundings (4 u of its terms) come into the orthogonalised matrix as noise of that share of its norm."""
+    g = np.random.default_rng(m)
+    shape = (batch, m, n) if batch > 1 else (m, n)
+    master, mom = (torch.from_numpy(g.normal(size=shape).astype(np.float32)).to(DEV), torch.zeros(shape, device=DEV))
+    cfg, opt = cngp.OrthoConfig(m, n, batch, steps=steps), cngp.Muon(0.02, 0.9, 0.1, 0.25, nesterov)
+    copy = torch.empty(shape, dtype=torch.float16, device=DEV) if half else None
+    mo, lr, wd = (float(np.float32(v)) for v in (0.9, 0.02, 0.1))
+    for i in range(3):
+        grad = torch.from_numpy(matrices(batch, m, n, i).astype(np.float32).reshape(shape)).to(DEV)
+        w64, m64, g64 = (t.cpu().double().numpy().reshape(batch, m, n) for t in (master, mom, grad))
+        cngp.muon_step(cfg, opt, master, copy, mom, grad, clear_grad=clear)
+        new = mo * m64 + 0.25 * g64
+        u, mag = (mo * new + 0.25 * g64, np.abs(mo * new) + np.abs(0.25 * g64)) if nesterov else (new, np.abs(mo * m64) + np.abs(0.25 * g64))
+        R.within("momentum", mom.cpu().numpy().reshape(new.shape), new, 2 * R.U * (np.abs(mo * m64) + np.abs(0.25 * g64)))
+        o = R.orthogonalise(u, steps, as_fp32(MUON), float(np.float32(1e-7)))
+        noise = 4 * R.U * max(float(np.linalg.norm(b) / np.linalg.norm(a)) for a, b in zip(u, mag))
+        want = w64 * (1 - lr * wd) - lr * o
+        slack = lr * (bound(m, n, steps) + noise * 3.4445 ** steps) + R.U * (4 * np.abs(w64) + 2 * lr * np.abs(o))
+        R.within("weights", master.cpu().numpy().reshape(want.shape), want, slack)
+        if half:
+            assert torch.equal(copy, master.half())
+        assert bool((grad == 0).all()) == clear
+
+
+def test_optimiser_step_of_nothing():
+    """A gradient and momentum of zeros leave the weights, but for their decay."""
+    for m, n in ((32, 16), (130, 70)):
+        w = torch.randn(m, n, device=DEV)
+        want, mom, grad = w * (1 - 0.5 * 0.25), torch.zeros(m, n, device=DEV), torch.zeros(m, n, device=DEV)
+        cngp.muon_step(cngp.OrthoConfig(m, n, eps=0.0), cngp.Muon(0.5, 0.9, 0.25), w, None, mom, grad)
+        assert torch.equal(w, want) and not mom.any()

@@ -145,6 +145,30 @@ def test_orthogonalising_refuses():
         assert call(ortho(), **kw) == cngp.ERR_WORKSPACE, kw
 
 
+def test_optimiser_step_refuses():
+    def call(cfg=ortho(), opt=cngp.Muon(), w=P, m=P, g=P, ws=P, size=BIG):
+        o = None if opt is None else ctypes.byref(opt.c())
+        return lib.cngp_muon_step(None if cfg is None else cfg._ref(), o, w, None, m, g, 0, ws, size, None)
+    for kw in (dict(cfg=None), dict(opt=None), dict(w=None), dict(m=None), dict(g=None)):
+        assert call(**kw) == cngp.ERR_NULL, kw
+    assert call(cfg=ortho(io_dtype=cngp.F16)) == cngp.ERR_UNSUPPORTED
+    assert call(cfg=ortho(rows=0)) == cngp.ERR_INVALID
+    for kw in (dict(lr=-1.0), dict(lr=float("inf")), dict(lr=float("nan")), dict(momentum=1.0), dict(momentum=-0.1), dict(weight_decay=-1.0), dict(grad_scale=float("inf")),
+               dict(nesterov=2)):
+        assert call(opt=cngp.Muon(**kw)) == cngp.ERR_INVALID, kw
+    need = cngp.orthogonalise_workspace_bytes(ortho())
+    for kw in (dict(ws=None), dict(ws=OFF), dict(size=need - 1)):
+        assert call(**kw) == cngp.ERR_WORKSPACE, kw
+
+
+def test_modules_refuse_gradients_that_they_do_not_give():
+    from paper_2312_17241_amd.module import rotate as turned
+    x = torch.zeros(6, 4, 16)
+    for position, omega in ((torch.zeros(6, 2, requires_grad=True), torch.zeros(8)), (torch.zeros(6, 2), torch.zeros(8, requires_grad=True))):
+        with pytest.raises(ValueError):
+            turned(rotate(), x, torch.zeros(6, 2, 16), position, omega)
+
+
 def test_binding_refuses_wrong_tensors():
     x = torch.zeros(6, 4, 16)
     with pytest.raises(TypeError):

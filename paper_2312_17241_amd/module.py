@@ -1,5 +1,6 @@
 """torch.nn.Modules and autograd functions around the library's entry points, for training loops: the encoding, codes per image or
-object that are added to it, and the recurrence that composites a ray's decoded samples.
+object that are added to it, the recurrence that composites a ray's decoded samples, and the mixer of a ray's or sequence's rows (attention with
+decays, norms and rotation of its queries and keys).
 
 Holds the codebooks of the encoding (Sec. 3: feature codebook D_f, confidence values D^_c, baked index
 codebook D_c), their gradient arrays and optimiser moments as device tensors, and wires encode_fwd /
@@ -16,9 +17,9 @@ import functools
 import torch
 from torch.autograd.function import once_differentiable
 
-from . import (Adam, Config, EmbedConfig, F32, I64, RECUR_LOG_GATE, RECUR_MIX, RECUR_REVERSE, RecurConfig, ZERO_GRADS, _TORCH_DT, F16,
-               adam_step, adam_step_bake, alloc_workspace, bake_probes, embed_bwd, embed_fwd, encode_bwd, encode_bwd_input, encode_fwd,
-               probe_balance, recur_bwd, recur_fwd, workspace_bytes)
+from . import (Adam, AttendConfig, Config, EmbedConfig, F32, I64, RECUR_LOG_GATE, RECUR_MIX, RECUR_REVERSE, RecurConfig, RotateConfig, ZERO_GRADS,
+               _TORCH_DT, F16, adam_step, adam_step_bake, alloc_workspace, attend_bwd, attend_fwd, bake_probes, embed_bwd, embed_fwd, encode_bwd,
+               encode_bwd_input, encode_fwd, probe_balance, recur_bwd, recur_fwd, rotate_bwd, rotate_fwd, workspace_bytes)
 
 
 class _Encode(torch.autograd.Function):
@@ -184,3 +185,60 @@ def composite(depth, colour, background=None, offsets=None, rays=None, longest=0
         raise ValueError(f"depth must be [N] and colour [N, C], got {tuple(depth.shape)} and {tuple(colour.shape)}")
     cfg = _composite_config(colour.shape[1], colour.dtype, depth.dtype, longest)
     return recur(cfg, -depth[:, None], colour, background, offsets, rays, keep=False)
+
+
+class _Attend(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, decay, h0, cfg, offsets, sequences):
+        y, last = attend_fwd(cfg, q, k, v, decay, h0=h0, offsets=offsets, sequences=sequences)
+        if offsets is not None:                                                  # rows of no sequence are not written
+            rows = torch.arange(q.shape[0], device=q.device)
+            y.masked_fill_(((rows < offsets[0]) | (rows >= offsets[-1]))[:, None, None], 0.0)
+        ctx.cfg, ctx.sequences = cfg, sequences
+        ctx.set_materialize_grads(False)
+        ctx.save_for_backward(q, k, v, decay, h0, offsets)
+        return y, last
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy, dlast):
+        q, k, v, decay, h0, offsets = ctx.saved_tensors
+        if dy is None and dlast is None:
+            return (None,) * 8
+        dy = None if dy is None else dy.contiguous()
+        dlast = None if dlast is None else dlast.contiguous()
+        make = torch.empty_like if offsets is None else torch.zeros_like         # rows of no sequence have gradient 0
+        grads = attend_bwd(ctx.cfg, q, k, v, decay, dy=dy, dlast=dlast, h0=h0, offsets=offsets, sequences=ctx.sequences, dq=make(q), dk=make(k),
+                           dv=make(v), ddecay=make(decay) if ctx.needs_input_grad[3] else False, dh0=h0 is not None and ctx.needs_input_grad[4])
+        return (*grads[:3], *(g if need else None for g, need in zip(grads[3:], ctx.needs_input_grad[3:5])), None, None, None)
+
+
+def attend(cfg: AttendConfig, q, k, v, decay, h0=None, offsets=None, sequences=None):
+    """Linear attention with a decay per head, with gradients: (y, last).  See cngp_attend_fwd.  A backward pass is captured into a graph as with recur()."""
+    return _Attend.apply(q, k, v, decay, h0, cfg, offsets, sequences)
+
+
+class _Rotate(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, gamma_q, gamma_k, position, omega, cfg):
+        ctx.cfg = cfg
+        ctx.save_for_backward(q, k, gamma_q, gamma_k, position, omega)
+        return rotate_fwd(cfg, q, k, position, omega, gamma_q, gamma_k)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dq, dk):
+        q, k, gamma_q, gamma_k, position, omega = ctx.saved_tensors
+        dq = dq if dq is None else dq.contiguous()
+        dk = dk if dk is None else dk.contiguous()
+        wanted = lambda i: None if ctx.needs_input_grad[i] else False
+        return (*rotate_bwd(ctx.cfg, q, k, position, omega, dq, dk, gamma_q, gamma_k, dgamma_q=wanted(2), dgamma_k=wanted(3)), None, None, None)
+
+
+def rotate(cfg: RotateConfig, q, k, position, omega, gamma_q=None, gamma_k=None):
+    """Norms and rotation of queries and keys, with gradients of q, k and the gains: (q, k).  See cngp_rotate_fwd.  A backward pass is captured
+    into a graph as with recur()."""
+    for name, t in (("position", position), ("omega", omega)):
+        if t is not None and t.requires_grad:
+            raise ValueError(f"{name} gets no gradient: detach it")
+    return _Rotate.apply(q, k, gamma_q, gamma_k, position, omega, cfg)

@@ -23,6 +23,7 @@ constexpr int kPad = 8;                                     // halves between ro
 constexpr float kScaleX = 16384.0f, kScaleA = 4096.0f, kScaleB = 1024.0f;
 constexpr int kNormParts = 1024;
 constexpr int64_t kEnoughTiles = 256;                       // of 128 x 128: a CU each
+constexpr int kSlots = 512, kLeastShare = 256;              // ... that run at a time; least length of a share of a contraction
 
 // High and low parts of a matrix, rows of `stride` values.
 struct Pair {
@@ -75,6 +76,19 @@ __device__ __forceinline__ void moved(const Step &st, const size_t at, const flo
     st.master[at] = w;
     if (st.half) st.half[at] = (_Float16)w;
     if (st.clear) st.grad[at] = 0.0f;
+}
+
+__device__ __forceinline__ void moved4(const Step &st, const size_t at, const float (&v)[4]) {
+    const float4 from = *reinterpret_cast<const float4 *>(st.master + at);
+    const float  w[4] = {fmaf(-st.lr, v[0], from.x * st.keep), fmaf(-st.lr, v[1], from.y * st.keep), fmaf(-st.lr, v[2], from.z * st.keep), fmaf(-st.lr, v[3], from.w * st.keep)};
+    *reinterpret_cast<float4 *>(st.master + at) = make_float4(w[0], w[1], w[2], w[3]);
+    if (st.half) {
+        half4_t h;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) h[e] = (_Float16)w[e];
+        *reinterpret_cast<half4_t *>(st.half + at) = h;
+    }
+    if (st.clear) *reinterpret_cast<float4 *>(st.grad + at) = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 }
 
 // ---------------------------------------------------------------- norm, start, no steps
@@ -159,13 +173,72 @@ __global__ __launch_bounds__(kBlock) void ortho_scale_kernel(const T *g, const S
 // ---------------------------------------------------------------- products
 enum : int { GRAM, POLY, UPDATE, LAST };
 struct ProductArgs {
-    Pair  A, B, C, D;                    // C = epilogue(A B^T, or A B for updates; D)
-    int   depth, tiles_m, tiles_n;
-    float of_sum, of_d;                  // C = of_sum * product + of_d * D
-    void *out;                           // LAST: the result
-    int   m, n, turned, out_f16;
-    Step  step;
+    Pair   A, B, C, D;                   // C = epilogue(A B^T, or A B for updates; D)
+    int    depth, tiles_m, tiles_n, tiles;
+    int    whole, parts;                 // tiles (of all matrices) by one workgroup each; the others by `parts`, each a share of the contraction
+    float *sums;                         // ... into here, as their lanes hold them: [tile, part, subtiles of 32 x 32, 4, lanes, 4]
+    float  of_sum, of_d;                 // C = of_sum * product + of_d * D
+    void  *out;                          // LAST: the result
+    int    m, n, turned, out_f16, wide;  // wide: four neighbouring results go as one
+    Step   step;
 };
+
+struct Tile { int i, j; size_t z; };
+template <bool BACK>
+__device__ __forceinline__ Tile tile_of(const ProductArgs &a, const int number) {
+    Tile t;
+    t.z = (size_t)(number / a.tiles);
+    const int n = number % a.tiles;
+    if (BACK) {
+        t.i = n % a.tiles_m;
+        t.j = n / a.tiles_m;
+    } else {                             // the triangle's tiles, row after row
+        t.i = (int)((sqrtf(8.0f * (float)n + 1.0f) - 1.0f) * 0.5f);
+        while ((t.i + 1) * (t.i + 2) / 2 <= n) ++t.i;
+        while (t.i * (t.i + 1) / 2 > n) --t.i;
+        t.j = n - t.i * (t.i + 1) / 2;
+    }
+    return t;
+}
+
+// What becomes of four neighbouring sums, row i, columns j ..
+template <int WHAT>
+__device__ __forceinline__ void finish(const ProductArgs &a, const Tile &t, const int i, const int j, const float (&sum)[4]) {
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = sum[e] * a.of_sum;
+    if (WHAT != GRAM) {
+        float d[4];
+        get4(a.D, t.z * a.D.each + (size_t)i * a.D.stride + j, d);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = fmaf(a.of_d, d[e], v[e]);
+    }
+    if (WHAT != LAST) put4(a.C, t.z * a.C.each + (size_t)i * a.C.stride + j, v);
+    if ((WHAT == GRAM || WHAT == POLY) && t.i != t.j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) put(a.C, t.z * a.C.each + (size_t)(j + e) * a.C.stride + i, v[e]);
+    if (WHAT == LAST && i < a.m && j < a.n) {
+        const size_t first = t.z * (size_t)a.m * a.n;
+        if (a.wide) {
+            const size_t at = first + (size_t)i * a.n + j;
+            if (a.step.m) moved4(a.step, at, v);
+            else if (a.out_f16) {
+                half4_t h;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) h[e] = (_Float16)v[e];
+                *reinterpret_cast<half4_t *>((_Float16 *)a.out + at) = h;
+            } else *reinterpret_cast<float4 *>((float *)a.out + at) = make_float4(v[0], v[1], v[2], v[3]);
+        } else
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (j + e < a.n) {
+                    const size_t at = first + (a.turned ? (size_t)(j + e) * a.m + i : (size_t)i * a.n + j + e);
+                    if (a.step.m) moved(a.step, at, v[e]);
+                    else if (a.out_f16) ((_Float16 *)a.out)[at] = (_Float16)v[e];
+                    else ((float *)a.out)[at] = v[e];
+                }
+    }
+}
 
 // A tile of 64 U x 64 U of a product by four wavefronts of 32 U x 32 U; computed transposed (a lane has a row of C and four neighbouring columns in
 // four registers).
@@ -177,23 +250,21 @@ __global__ __launch_bounds__(kBlock, 2) void ortho_product_kernel(const ProductA
     constexpr int  kBackRow = TILE / 8, kStepA = kBlock / 4, kStepB = kBack ? kBlock / kBackRow : kStepA;
     __shared__ __align__(16) _Float16 lds[2][2 * kSizeA + 2 * kSizeB];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
-    int ti, tj;
-    if (kBack) {
-        ti = (int)(blockIdx.x % a.tiles_m);
-        tj = (int)(blockIdx.x / a.tiles_m);
-    } else {                             // the triangle's tiles, row after row
-        ti = (int)((sqrtf(8.0f * (float)blockIdx.x + 1.0f) - 1.0f) * 0.5f);
-        while ((ti + 1) * (ti + 2) / 2 <= (int)blockIdx.x) ++ti;
-        while (ti * (ti + 1) / 2 > (int)blockIdx.x) --ti;
-        tj = (int)blockIdx.x - ti * (ti + 1) / 2;
+    int number = (int)blockIdx.x, part = -1, k0 = 0, k_end = a.depth;
+    if (number >= a.whole) {
+        const int share = (a.depth / kDepth + a.parts - 1) / a.parts * kDepth;
+        part = number - a.whole;
+        number = a.whole + part / a.parts;
+        k0 = part % a.parts * share;
+        k_end = k0 + share < a.depth ? k0 + share : a.depth;
     }
-    const size_t z = blockIdx.z;
-    const int i0 = ti * TILE, j0 = tj * TILE, wi = 32 * U * (wave & 1), wj = 32 * U * (wave >> 1);
+    const Tile t = tile_of<kBack>(a, number);
+    const int i0 = t.i * TILE, j0 = t.j * TILE, wi = 32 * U * (wave & 1), wj = 32 * U * (wave >> 1);
 
     words_t r[4 * U];
-    const _Float16 *pa = a.A.hi + z * a.A.each + (size_t)(i0 + ((int)threadIdx.x >> 2)) * a.A.stride + ((int)threadIdx.x & 3) * 8;
-    const _Float16 *pb = a.B.hi + z * a.B.each + (kBack ? (size_t)((int)threadIdx.x / kBackRow) * a.B.stride + j0 + (int)threadIdx.x % kBackRow * 8
-                                                        : (size_t)(j0 + ((int)threadIdx.x >> 2)) * a.B.stride + ((int)threadIdx.x & 3) * 8);
+    const _Float16 *pa = a.A.hi + t.z * a.A.each + (size_t)(i0 + ((int)threadIdx.x >> 2)) * a.A.stride + k0 + ((int)threadIdx.x & 3) * 8;
+    const _Float16 *pb = a.B.hi + t.z * a.B.each + (kBack ? (size_t)(k0 + (int)threadIdx.x / kBackRow) * a.B.stride + j0 + (int)threadIdx.x % kBackRow * 8
+                                                          : (size_t)(j0 + ((int)threadIdx.x >> 2)) * a.B.stride + k0 + ((int)threadIdx.x & 3) * 8);
     const ptrdiff_t la = a.A.lo - a.A.hi, lb = a.B.lo - a.B.hi;
     auto fetch = [&]() {
 #pragma unroll
@@ -224,11 +295,11 @@ __global__ __launch_bounds__(kBlock, 2) void ortho_product_kernel(const ProductA
     for (int u = 0; u < U; ++u)
 #pragma unroll
         for (int w = 0; w < U; ++w) sum[u][w] = zero();
-    fetch();
-    for (int k0 = 0, b = 0; k0 < a.depth; k0 += kDepth, b ^= 1) {
+    if (k0 < k_end) fetch();
+    for (int b = 0; k0 < k_end; k0 += kDepth, b ^= 1) {
         keep(lds[b]);
         __syncthreads();
-        if (k0 + kDepth < a.depth) fetch();
+        if (k0 + kDepth < k_end) fetch();
         const _Float16 *A = lds[b], *B = lds[b] + 2 * kSizeA;
 #pragma unroll
         for (int s = 0; s < kDepth / 16; ++s) {
@@ -258,50 +329,77 @@ __global__ __launch_bounds__(kBlock, 2) void ortho_product_kernel(const ProductA
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int w = 0; w < U; ++w) {
-            const int i = i0 + wi + 32 * u + col;
+        for (int w = 0; w < U; ++w)
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const int j = j0 + wj + 32 * w + 8 * g + 4 * half;
-                float v[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = sum[u][w][4 * g + e] * a.of_sum;
-                if (WHAT != GRAM) {
-                    float d[4];
-                    get4(a.D, z * a.D.each + (size_t)i * a.D.stride + j, d);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = fmaf(a.of_d, d[e], v[e]);
-                }
-                if (WHAT != LAST) put4(a.C, z * a.C.each + (size_t)i * a.C.stride + j, v);
-                if (!kBack && ti != tj)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) put(a.C, z * a.C.each + (size_t)(j + e) * a.C.stride + i, v[e]);
-                if (WHAT == LAST && i < a.m)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (j + e < a.n) {
-                            const size_t at = z * (size_t)a.m * a.n + (a.turned ? (size_t)(j + e) * a.m + i : (size_t)i * a.n + j + e);
-                            if (a.step.m) moved(a.step, at, v[e]);
-                            else if (a.out_f16) ((_Float16 *)a.out)[at] = (_Float16)v[e];
-                            else ((float *)a.out)[at] = v[e];
-                        }
+                const float v[4] = {sum[u][w][4 * g], sum[u][w][4 * g + 1], sum[u][w][4 * g + 2], sum[u][w][4 * g + 3]};
+                if (part >= 0)
+                    *reinterpret_cast<float4 *>(a.sums + ((((size_t)part * (U * U) + u * U + w) * 4 + g) * kBlock + threadIdx.x) * 4) = make_float4(v[0], v[1], v[2], v[3]);
+                else finish<WHAT>(a, t, i0 + wi + 32 * u + col, j0 + wj + 32 * w + 8 * g + 4 * half, v);
             }
-        }
 }
+
+// Shares of a contraction added up, in their order: a workgroup for 16 x 16 of a tile's 128 x 128 (a quarter of each wavefront's 32 x 32).
+template <int WHAT, int U>
+__global__ __launch_bounds__(kBlock) void ortho_join_kernel(const ProductArgs a)
+{
+    constexpr bool kBack = WHAT == UPDATE || WHAT == LAST;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
+    const int each = U * U * 4, tail = (int)blockIdx.x / each, piece = (int)blockIdx.x % each, u = piece / (4 * U), w = piece / 4 % U, g = piece & 3;
+    const Tile t = tile_of<kBack>(a, a.whole + tail);
+    const float *p = a.sums + (((size_t)tail * a.parts * each + piece) * kBlock + threadIdx.x) * 4;
+    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+    for (int k = 0; k < a.parts; ++k) {
+        const float4 x = *reinterpret_cast<const float4 *>(p + (size_t)k * each * kBlock * 4);
+        v[0] += x.x;
+        v[1] += x.y;
+        v[2] += x.z;
+        v[3] += x.w;
+    }
+    finish<WHAT>(a, t, 64 * U * t.i + 32 * U * (wave & 1) + 32 * u + col, 64 * U * t.j + 32 * U * (wave >> 1) + 32 * w + 8 * g + 4 * half, v);
+}
+
+// How a product's tiles are shared out.  A card has room for two workgroups of 128 x 128 on each of its 256 CUs: what is left after whole turns of
+// 512 is cut along the contraction, into as many parts as there is room for (of 256 at least), and joined by a second launch.  (528 tiles of a
+// triangle of 4096: the last 16 alone took more than half of what the 512 before them did.)
+struct Cut {
+    int U, tiles, whole, parts;
+    int64_t rest() const { return (int64_t)tiles - whole; }
+};
+Cut cut_of(bool back, int mp, int np, int depth, int batch) {
+    auto count = [&](int64_t tile) { const int64_t tm = mp / tile, tn = np / tile; return (int)((back ? tm * tn : tm * (tm + 1) / 2) * batch); };
+    Cut c{2, count(kTile), 0, 1};
+    c.whole = c.tiles / kSlots * kSlots;
+    const int most = c.rest() ? (int)std::min<int64_t>(kSlots / c.rest(), depth / (c.whole ? kLeastShare : 4 * kLeastShare)) : 1;
+    if (most > 1 && c.whole + c.rest() * most >= kEnoughTiles) {
+        c.parts = most;
+        return c;
+    }
+    if (c.tiles < kEnoughTiles) c = Cut{1, count(kTile / 2), 0, 1};
+    c.whole = c.tiles;
+    return c;
+}
+size_t sums_bytes(const Cut &c) { return (size_t)c.rest() * c.parts * kTile * kTile * 4; }
 
 template <int WHAT>
 int product(const ProductArgs &p, int mp, int np, int batch, hipStream_t st) {
     constexpr bool kBack = WHAT == UPDATE || WHAT == LAST;
     ProductArgs a = p;
-    const int64_t tm = mp / kTile, tn = np / kTile, large = (kBack ? tm * tn : tm * (tm + 1) / 2) * batch;
-    const int     U = large >= kEnoughTiles ? 2 : 1;
-    a.tiles_m = mp / (64 * U);
-    a.tiles_n = np / (64 * U);
-    const unsigned tiles = (unsigned)(kBack ? a.tiles_m * a.tiles_n : a.tiles_m * (a.tiles_m + 1) / 2);
+    const Cut   c = cut_of(kBack, mp, np, a.depth, batch);
+    a.tiles_m = mp / (64 * c.U);
+    a.tiles_n = np / (64 * c.U);
+    a.tiles = c.tiles / batch;
+    a.whole = c.whole;
+    a.parts = c.parts;
     LaunchTimer t(st, K_ORTHO_PRODUCT);
-    if (U == 2) ortho_product_kernel<WHAT, 2><<<dim3(tiles, 1, (unsigned)batch), kBlock, 0, st>>>(a);
-    else ortho_product_kernel<WHAT, 1><<<dim3(tiles, 1, (unsigned)batch), kBlock, 0, st>>>(a);
-    return launch_status("ortho_product_kernel");
+    const unsigned groups = (unsigned)(c.whole + c.rest() * c.parts);
+    if (c.U == 2) ortho_product_kernel<WHAT, 2><<<groups, kBlock, 0, st>>>(a);
+    else ortho_product_kernel<WHAT, 1><<<groups, kBlock, 0, st>>>(a);
+    if (int rc = launch_status("ortho_product_kernel")) return rc;
+    if (!c.rest()) return CNGP_OK;
+    ortho_join_kernel<WHAT, 2><<<(unsigned)(c.rest() * 16), kBlock, 0, st>>>(a);
+    return launch_status("ortho_join_kernel");
 }
 
 // ---------------------------------------------------------------- matrices of at most 64 x 128
@@ -430,7 +528,7 @@ __global__ __launch_bounds__(kBlock) void ortho_small_kernel(const SmallArgs a)
 struct Shape {
     int    m, n, mp, np, parts;
     bool   turned, small;
-    size_t x[2], a, b, norm, bytes;
+    size_t x[2], a, b, norm, sums, bytes;
 };
 Shape shape_of(const cngp_ortho_config *c) {
     Shape s{};
@@ -450,6 +548,12 @@ Shape shape_of(const cngp_ortho_config *c) {
     s.x[1] = take(c->steps > 1, x);
     s.a = take(c->steps > 0, a);
     s.b = take(c->steps > 0, a);
+    if (c->steps > 0) {
+        size_t most = 0;
+        for (const Cut &k : {cut_of(false, s.mp, s.np, s.np, c->batch), cut_of(false, s.mp, s.np, s.mp, c->batch), cut_of(true, s.mp, s.np, s.mp, c->batch)})
+            most = std::max(most, sums_bytes(k));
+        s.sums = take(most > 0, most);
+    }
     s.bytes = at;
     return s;
 }
@@ -515,6 +619,7 @@ int run(const cngp_ortho_config *cfg, const void *g, const Step &step, void *out
         const bool last = i + 1 == cfg->steps;
         const Pair X = pair_of(ws, s.x[i & 1], s.mp, s.np, cfg->batch), Y = last ? X : pair_of(ws, s.x[1 - (i & 1)], s.mp, s.np, cfg->batch);
         ProductArgs p{};
+        p.sums = (float *)(ws + s.sums);
         p.A = X; p.B = X; p.C = A; p.D = A;
         p.depth = s.np; p.of_sum = kScaleA / (kScaleX * kScaleX);
         if (int rc = product<GRAM>(p, s.mp, s.np, cfg->batch, st)) return rc;
@@ -526,6 +631,8 @@ int run(const cngp_ortho_config *cfg, const void *g, const Step &step, void *out
         if (last) {
             p.of_sum /= kScaleX; p.of_d /= kScaleX;
             p.out = out; p.m = s.m; p.n = s.n; p.turned = s.turned; p.out_f16 = cfg->io_dtype == CNGP_F16; p.step = step;
+            const auto on = [](const void *q, uintptr_t bytes) { return ((uintptr_t)q & (bytes - 1)) == 0; };
+            p.wide = !s.turned && s.n % 4 == 0 && (step.m ? on(step.master, 16) && on(step.grad, 16) && on(step.half, 8) : on(out, p.out_f16 ? 8 : 16));
         }
         if (int rc = last ? product<LAST>(p, s.mp, s.np, cfg->batch, st) : product<UPDATE>(p, s.mp, s.np, cfg->batch, st)) return rc;
     }

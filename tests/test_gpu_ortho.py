@@ -110,6 +110,24 @@ def test_same_bits_in_any_workspace_and_batch():
         assert torch.equal(cngp.orthogonalise(cfg, g, workspace=ws), ref)
 
 
+@pytest.mark.parametrize("batch,m,n", [(36, 640, 650), (36, 650, 640), (36, 640, 644), (4, 1000, 2100), (4, 2100, 1000)])
+@pytest.mark.parametrize("io", [F16, F32])
+def test_tiles_that_are_cut_along_the_contraction(batch, m, n, io):
+    """Tiles that do not fill the card, or are left after those that do; the last matrices hold them."""
+    g = matrices(batch, m, n, m).astype(NP[io])
+    t = torch.from_numpy(g).to(DEV)
+    steps = 2
+    out = cngp.orthogonalise(cngp.OrthoConfig(m, n, batch, io, steps), t)
+    some = sorted({0, batch - 2, batch - 1} - {-1})
+    want = R.orthogonalise(g[some].astype(np.float64), steps, as_fp32(MUON), float(np.float32(1e-7)))
+    R.within("out", out.cpu().numpy()[some], want, bound(m, n, steps), NP[io])
+    assert torch.equal(cngp.orthogonalise(cngp.OrthoConfig(m, n, batch, io, steps), t), out)
+    if io == F32:
+        w, mom = torch.zeros_like(t), torch.zeros_like(t)
+        cngp.muon_step(cngp.OrthoConfig(m, n, batch, steps=steps), cngp.Muon(1.0, 0.0, nesterov=False), w, None, mom, t)
+        assert torch.equal(w, -out)
+
+
 @pytest.mark.parametrize("m,n,batch", [(3, 5, 1), (64, 32, 2), (64, 128, 1), (100, 30, 3), (130, 260, 2), (300, 70, 1)])
 @pytest.mark.parametrize("nesterov,clear,half", [(True, True, True), (False, False, False)])
 @pytest.mark.parametrize("steps", [0, 5])

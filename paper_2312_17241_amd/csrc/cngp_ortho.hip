@@ -246,7 +246,7 @@ template <int WHAT, int U>
 __global__ __launch_bounds__(kBlock, 2) void ortho_product_kernel(const ProductArgs a)
 {
     constexpr bool kBack = WHAT == UPDATE || WHAT == LAST;              // the right factor lies by rows of the contraction
-    constexpr int  TILE = 64 * U, kRowA = kDepth + kPad, kRowB = kBack ? TILE + kPad : kDepth + kPad, kSizeA = TILE * kRowA, kSizeB = kBack ? kDepth * kRowB : TILE * kRowB;
+    constexpr int  TILE = 64 * U, kRowA = kDepth, kRowB = kBack ? TILE + 32 : kDepth, kSizeA = TILE * kRowA, kSizeB = kBack ? kDepth * kRowB : TILE * kRowB;
     constexpr int  kBackRow = TILE / 8, kStepA = kBlock / 4, kStepB = kBack ? kBlock / kBackRow : kStepA;
     __shared__ __align__(16) _Float16 lds[2][2 * kSizeA + 2 * kSizeB];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
@@ -278,7 +278,9 @@ __global__ __launch_bounds__(kBlock, 2) void ortho_product_kernel(const ProductA
         pa += kDepth;
         pb += kBack ? (size_t)kDepth * a.B.stride : (size_t)kDepth;
     };
-    const int oa = ((int)threadIdx.x >> 2) * kRowA + ((int)threadIdx.x & 3) * 8, ob = kBack ? (int)threadIdx.x / kBackRow * kRowB + (int)threadIdx.x % kBackRow * 8 : oa;
+    // Banks: rows along the contraction are 64 bytes, their 16-byte pieces turned by (row / 4) % 4 (sixteen lanes' pieces of sixteen rows, or of four whole rows,
+    // then lie in different ones); rows across it are 64 bytes more than a multiple of 256 (a transposing read takes 64 bytes of four rows).
+    const int oa = ((int)threadIdx.x >> 2) * kRowA + (((int)threadIdx.x & 3) ^ ((int)threadIdx.x >> 4 & 3)) * 8, ob = kBack ? (int)threadIdx.x / kBackRow * kRowB + (int)threadIdx.x % kBackRow * 8 : oa;
     auto keep = [&](_Float16 *to) {
 #pragma unroll
         for (int i = 0; i < U; ++i) {
@@ -306,14 +308,15 @@ __global__ __launch_bounds__(kBlock, 2) void ortho_product_kernel(const ProductA
             half8_t ah[U], al[U], bh[U], bl[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const _Float16 *p = A + (wi + 32 * u + col) * kRowA + 16 * s + 8 * half;
+                const int       turned = 8 * ((2 * s + half) ^ (col >> 2 & 3));
+                const _Float16 *p = A + (wi + 32 * u + col) * kRowA + turned;
                 ah[u] = read8(p);
                 al[u] = read8(p + kSizeA);
                 if constexpr (kBack) {
                     bh[u] = read_column(B, kRowB, 16 * s, wj + 32 * u, lane);
                     bl[u] = read_column(B + kSizeB, kRowB, 16 * s, wj + 32 * u, lane);
                 } else {
-                    const _Float16 *q = B + (wj + 32 * u + col) * kRowB + 16 * s + 8 * half;
+                    const _Float16 *q = B + (wj + 32 * u + col) * kRowB + turned;
                     bh[u] = read8(q);
                     bl[u] = read8(q + kSizeB);
                 }

@@ -26,9 +26,9 @@ __device__ __forceinline__ Span scalar(const Span s) { return {__builtin_amdgcn_
 // A tile [64, W] of an array on its way into LDS: rows t of a chunk, `stride` values apart, `dim` of them (the rest and rows from `count` on are
 // 0).  Reverse walks take rows from the last to the first.  Where 16-byte pieces lie whole in the rows they are fetched into registers a chunk
 // ahead; else values are read one by one on the way.  Addresses are a scalar base and one 32-bit offset per lane.
-template <typename T, int W, int WAVES, bool WHOLE>
+template <typename T, int W, int LDS_STRIDE, int WAVES, bool WHOLE>
 struct Staged {
-    static constexpr int per_row = W / 8, dealt = WAVES * 64 / per_row, rows = dealt < kChunk ? dealt : kChunk, each = kChunk / rows, words = sizeof(T) / 2, lds_stride = W + 8;
+    static constexpr int per_row = W / 8, dealt = WAVES * 64 / per_row, rows = dealt < kChunk ? dealt : kChunk, each = kChunk / rows, words = sizeof(T) / 2;
     static_assert(rows * each == kChunk, "a tile is dealt out evenly");
     words_t  r[each][words];
     uint32_t offset;                     // bytes from the lowest row of a whole chunk
@@ -55,7 +55,7 @@ struct Staged {
     // hi, lo: the parts of the tile; lift: of each row (fp32 only)
     __device__ __forceinline__ void put(_Float16 *hi, _Float16 *lo, int *lift, const int t, const words_t (&v)[words]) const {
         if (dealt > kChunk && t >= kChunk) return;
-        const int at = t * lds_stride + (int)threadIdx.x % per_row * 8;
+        const int at = t * LDS_STRIDE + (int)threadIdx.x % per_row * 8;
         if constexpr (sizeof(T) == 2) {
             *reinterpret_cast<words_t *>(hi + at) = v[0];
         } else {
@@ -109,9 +109,13 @@ constexpr int walk_per_simd(size_t value, int KW) { return value == 2 || KW < 12
 
 // KW, VW: columns of k and v in a tile: 16, 32, 64 or 128.  Sums of 32 rows or columns where 16 are kept read what lies behind a row in LDS;
 // the rows and columns of the state that come of it are used by nothing.
+// Banks: the scores read 16 bytes of sixteen rows, so rows have an odd number of 16-byte pieces; a transposing read takes 64 bytes of four neighbouring
+// rows, for which rows of 128 values are 64 bytes beyond a multiple of 256 (v, read by that alone) or five pieces (k) (128 x 128: 338 against 344 us a
+// prompt; of 64 values it gained nothing).
 template <typename T, int KW, int VW, bool OUT>
 struct Lds {
-    static constexpr int parts = sizeof(T) / 2, kstride = KW + 8, vstride = VW + 8, pstride = 32 + 8, KT = (KW + 31) / 32, VT = (VW + 31) / 32;
+    static constexpr int kstride = KW + (KW == 128 ? 40 : 8), vstride = VW + (VW == 128 ? 32 : 8);     // see above
+    static constexpr int parts = sizeof(T) / 2, pstride = 32 + 8, KT = (KW + 31) / 32, VT = (VW + 31) / 32;
     static constexpr int halves = walk_halves(KW), waves = VT * halves;
     static constexpr bool scores = OUT && waves > 1;        // pass through LDS
     double F[2][kChunk];                                    // log2 of the decay from the chunk's start; this chunk's and the next one's
@@ -200,8 +204,8 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
         row0 = reverse ? at + count - 1 : at;
         low = reverse ? row0 - (kChunk - 1) : row0;
     };
-    Staged<T, KW, WAVES, WHOLE> rq, rk;
-    Staged<T, VW, WAVES, WHOLE> rv;
+    Staged<T, KW, L::kstride, WAVES, WHOLE> rq, rk;
+    Staged<T, VW, L::vstride, WAVES, WHOLE> rv;
     if (OUT) rq.begin(qs, reverse);
     rk.begin(ks, reverse);
     rv.begin(vs, reverse);

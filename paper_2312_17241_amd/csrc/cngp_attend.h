@@ -31,7 +31,7 @@ struct WalkArgs {
     float       *total;                  // [segments, heads]: log2 of a segment's decay, or NULL
     int64_t      N;
     int32_t      S, rows_each, heads, q_div, k_div, v_div, x_div, kdim, vdim;
-    int32_t      seg_shift;              // 0: sequences whole; else segments have 2^seg_shift rows, counted from a sequence's start
+    int32_t      seg_rows;               // 0: sequences whole; else segments have this many rows (a multiple of kChunk), counted from a sequence's start
     int32_t      piece0;                 // first of this launch
     int32_t      segments;               // whole sequences: S
     int32_t      first_i, first_j, final_i, final_j;   // strides of the states' two dimensions
@@ -51,17 +51,17 @@ __host__ __device__ inline Span span_of(const int32_t *offsets, const int32_t s,
     return p;
 }
 
-// Numbers of pieces of 2^shift rows, sequence after sequence: those of sequence s start at piece (begin >> shift) + s, which leaves room for all of them
-// whatever the lengths (a sequence of n rows has at most ((begin + n) >> shift) - (begin >> shift) + 1).
-__host__ __device__ inline int32_t piece_base(const int32_t begin, const int32_t s, const int shift) { return (begin >> shift) + s; }
-inline int64_t pieces(const int64_t N, const int64_t S, const int shift) { return (N >> shift) + S; }
+// Numbers of pieces of `each` rows, sequence after sequence: those of sequence s start at piece begin / each + s, which leaves room for all of them
+// whatever the lengths (a sequence of n rows has at most (begin + n) / each - begin / each + 1, rounded down each).
+__host__ __device__ inline int32_t piece_base(const int32_t begin, const int32_t s, const int32_t each) { return (int32_t)((uint32_t)begin / (uint32_t)each) + s; }
+inline int64_t pieces(const int64_t N, const int64_t S, const int64_t each) { return N / each + S; }
 
 // Sequence of a piece: the last whose pieces start at or before it.
-__device__ inline int32_t sequence_of(const int32_t *offsets, const int32_t piece, const int64_t N, const int32_t S, const int32_t rows_each, const int shift) {
+__device__ inline int32_t sequence_of(const int32_t *offsets, const int32_t piece, const int64_t N, const int32_t S, const int32_t rows_each, const int32_t each) {
     int32_t lo = 0, hi = S - 1;
     while (lo < hi) {
         const int32_t mid = lo + (hi - lo + 1) / 2;
-        if (piece_base(span_of(offsets, mid, N, rows_each).begin, mid, shift) <= piece) lo = mid;
+        if (piece_base(span_of(offsets, mid, N, rows_each).begin, mid, each) <= piece) lo = mid;
         else hi = mid - 1;
     }
     return lo;

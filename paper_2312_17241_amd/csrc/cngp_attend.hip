@@ -86,7 +86,7 @@ struct CarryArgs {
     const float *first;
     float       *final;
     int64_t      N;
-    int32_t      S, rows_each, heads, seg_shift, size, reverse;
+    int32_t      S, rows_each, heads, seg_rows, size, reverse;
 };
 __global__ __launch_bounds__(kBlock) void attend_carry_kernel(const CarryArgs a)
 {
@@ -95,7 +95,7 @@ __global__ __launch_bounds__(kBlock) void attend_carry_kernel(const CarryArgs a)
         const int     e = (int)(own % a.size), h = (int)(own / a.size % a.heads);
         const int32_t s = (int32_t)(own / a.size / a.heads);
         const Span    span = span_of(a.offsets, s, a.N, a.rows_each);
-        const int32_t n = (int32_t)(((uint32_t)(span.end - span.begin) + (1u << a.seg_shift) - 1) >> a.seg_shift), base = piece_base(span.begin, s, a.seg_shift);
+        const int32_t n = (int32_t)(((uint32_t)(span.end - span.begin) + (uint32_t)a.seg_rows - 1) / (uint32_t)a.seg_rows), base = piece_base(span.begin, s, a.seg_rows);
         float state = a.first ? a.first[own] : 0.0f;
         // eight segments' parts are under way at a time: one after the other they would be a chain of memory latencies
         for (int32_t i0 = 0; i0 < n; i0 += 8) {
@@ -158,10 +158,10 @@ __global__ __launch_bounds__(64 * kAnchorChunks) void attend_decay_kernel(const 
     for (int64_t item = blockIdx.x; item < a.pieces * a.heads; item += gridDim.x) {
         const int     h = (int)(item % a.heads);
         const int64_t piece = item / a.heads;
-        const int32_t seq = a.whole ? (int32_t)piece : sequence_of(a.offsets, (int32_t)piece, a.N, a.S, a.rows_each, kAnchorShift);
+        const int32_t seq = a.whole ? (int32_t)piece : sequence_of(a.offsets, (int32_t)piece, a.N, a.S, a.rows_each, kRows);
         const Span    span = span_of(a.offsets, seq, a.N, a.rows_each);
         double sum = 0.0;
-        for (int64_t i = a.whole ? 0 : piece - piece_base(span.begin, seq, kAnchorShift); i >= 0 && span.begin + i * kRows < span.end; ++i) {
+        for (int64_t i = a.whole ? 0 : piece - piece_base(span.begin, seq, kRows); i >= 0 && span.begin + i * kRows < span.end; ++i) {
             const int64_t begin = span.begin + i * kRows, end = begin + kRows < span.end ? begin + kRows : span.end;
             const int     chunks = (int)((end - begin + kChunk - 1) >> kChunkShift);
             const bool    anchored = i != 0;
@@ -255,24 +255,26 @@ int check(const cngp_attend_config *c, int64_t N, int64_t S, bool ragged) {
     return CNGP_OK;
 }
 
-// How a call is cut: sequences whole, a workgroup per sequence and head, or in segments of 2^seg_shift rows where that leaves most of the chip
+// How a call is cut: sequences whole, a workgroup per sequence and head, or in segments of seg_rows rows where that leaves most of the chip
 // without work; then a walk without outputs gives the segments' parts first.
 struct Plan {
-    int     seg_shift;
+    int     seg_rows;
     int64_t segments;
 };
-constexpr int64_t kEnoughItems = 1024;                // four workgroups for each of 256 CUs: they end unevenly
+// Workgroups of all segments together: four for each of 256 CUs, whole turns of the card whatever a CU has room for, as nearly as that can be
+// had (a last segment is half a one in the mean).  Rows in powers of two left a fifth turn of a few (2^15 rows, 16 heads of 128 x 128: 312 against 338 us;
+// 512 or 2048 workgroups: 356 and 367).
+constexpr int64_t kItems = 1024, kLeastSegment = 256;
 int64_t longest_of(const cngp_attend_config *c, int64_t N, int64_t S, bool ragged) {
     const int64_t mean = S ? (N + S - 1) / S : 0;
     return !ragged ? mean : c->longest ? std::min<int64_t>(c->longest, N) : std::min<int64_t>(4 * mean, N);
 }
 Plan plan_of(const cngp_attend_config *c, int64_t N, int64_t S, bool ragged) {
     const int64_t longest = longest_of(c, N, S, ragged);
-    const int64_t R = (N * c->heads + kEnoughItems - 1) / kEnoughItems;
-    int shift = 8;
-    while (shift < 30 && (int64_t)1 << shift < R) ++shift;
-    if (longest <= (int64_t)4 << shift) return {0, S};
-    return {shift, pieces(N, S, shift)};
+    const int64_t items = std::max<int64_t>(kItems - (S + 1) / 2 * c->heads, kItems * 3 / 4), least = (N * c->heads + items - 1) / items;
+    const int64_t R = std::max<int64_t>((least + kChunk - 1) / kChunk * kChunk, kLeastSegment);
+    if (longest <= 4 * R) return {0, S};
+    return {(int)R, pieces(N, S, R)};
 }
 
 struct Space {
@@ -282,7 +284,7 @@ Space space_of(const cngp_attend_config *c, const Plan &p, int64_t N, int64_t S,
     Space sp{};
     size_t at = 0;
     auto take = [&](bool wanted, size_t bytes) { const size_t o = at; if (wanted) at += align256(bytes); return o; };
-    const bool   bwd = call & CNGP_ATTEND_CALL_BWD, cut = p.seg_shift != 0, shared = c->heads != c->kv_heads;
+    const bool   bwd = call & CNGP_ATTEND_CALL_BWD, cut = p.seg_rows != 0, shared = c->heads != c->kv_heads;
     const size_t H = (size_t)c->heads, size = (size_t)c->key_dim * c->value_dim, rows = (size_t)N;
     sp.states = take(cut, (size_t)p.segments * H * size * 4);
     sp.total = take(cut, (size_t)p.segments * H * 4);
@@ -290,7 +292,7 @@ Space space_of(const cngp_attend_config *c, const Plan &p, int64_t N, int64_t S,
     const size_t slots = rows / (kAnchorChunks * kChunk) + 1;
     sp.anchors_q = take(bwd, slots * H * anchor_floats(c->value_dim, c->key_dim) * 4);
     sp.anchors_k = take(bwd, slots * H * anchor_floats(c->value_dim, c->key_dim) * 4);
-    sp.parts = take(bwd && !(c->flags & CNGP_ATTEND_ROW_DECAY), (size_t)pieces(N, S, kAnchorShift) * H * 8);
+    sp.parts = take(bwd && !(c->flags & CNGP_ATTEND_ROW_DECAY), (size_t)pieces(N, S, 1 << kAnchorShift) * H * 8);
     sp.dh0 = take(bwd, (size_t)S * H * size * 4);
     sp.part_k = take(bwd && shared, rows * H * (size_t)c->key_dim * 4);
     sp.part_v = take(bwd && shared, rows * H * (size_t)c->value_dim * 4);
@@ -318,7 +320,7 @@ struct Call {
         a.N = N; a.S = (int32_t)S; a.rows_each = (int32_t)(S ? N / S : 0);
         a.heads = c->heads; a.q_div = q_div; a.k_div = k_div; a.v_div = v_div; a.x_div = 1;
         a.kdim = kdim; a.vdim = vdim;
-        a.seg_shift = p.seg_shift; a.segments = (int32_t)p.segments;
+        a.seg_rows = p.seg_rows; a.segments = (int32_t)p.segments;
         a.first_i = a.final_i = vdim; a.first_j = a.final_j = 1;
         a.pair_scale = a.far_scale = a.state_scale = 1.0f;
         a.reverse = reverse; a.row_decay = (c->flags & CNGP_ATTEND_ROW_DECAY) != 0;
@@ -341,7 +343,7 @@ struct Call {
         if (int rc = walk(a, true)) return rc;
         CarryArgs k{};
         k.states = a.final; k.total = a.total; k.offsets = offsets; k.first = first; k.final = final;
-        k.N = N; k.S = (int32_t)S; k.rows_each = a.rows_each; k.heads = c->heads; k.seg_shift = p.seg_shift;
+        k.N = N; k.S = (int32_t)S; k.rows_each = a.rows_each; k.heads = c->heads; k.seg_rows = p.seg_rows;
         k.size = a.kdim * a.vdim; k.reverse = a.reverse;
         LaunchTimer t(s, K_ATTEND_STATES);
         attend_carry_kernel<<<(unsigned)std::min<int64_t>((S * c->heads * k.size + kBlock - 1) / kBlock, 1 << 20), kBlock, 0, s>>>(k);
@@ -405,7 +407,7 @@ int cngp_attend_fwd(const cngp_attend_config *cfg, const void *q, const void *k,
     a.pair_scale = a.far_scale = cfg->scale;
     a.first = h0;
     a.final = last;
-    if (call.p.seg_shift) {
+    if (call.p.seg_rows) {
         if (int rc = call.carry(a, h0, last)) return rc;
         if (!y) return CNGP_OK;
         a.first = (const float *)(call.ws + call.sp.states);
@@ -432,7 +434,7 @@ int cngp_attend_bwd(const cngp_attend_config *cfg, const void *q, const void *k,
     char *ws = call.ws;
     const Space &sp = call.sp;
     const int   group = cfg->heads / cfg->kv_heads, K = cfg->key_dim, V = cfg->value_dim;
-    const bool  cut = call.p.seg_shift != 0, shared = group > 1;
+    const bool  cut = call.p.seg_rows != 0, shared = group > 1;
     float      *states = (float *)(ws + sp.states);
     if (ddecay && h0 && !dh0) dh0 = (float *)(ws + sp.dh0);
 
@@ -506,7 +508,7 @@ int cngp_attend_bwd(const cngp_attend_config *cfg, const void *q, const void *k,
     d.parts = rows ? nullptr : (double *)(ws + sp.parts);
     d.N = N; d.S = (int32_t)sequences; d.rows_each = (int32_t)(N / sequences); d.heads = cfg->heads;
     d.whole = longest_of(cfg, N, sequences, ragged) <= kAnchorChunks * kChunk;
-    d.pieces = d.whole ? sequences : pieces(N, sequences, kAnchorShift);
+    d.pieces = d.whole ? sequences : pieces(N, sequences, 1 << kAnchorShift);
     d.kdim = V; d.vdim = K;
     d.size = K * V; d.anchor_size = (int32_t)anchor_floats(V, K);
     {

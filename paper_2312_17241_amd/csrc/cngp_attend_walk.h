@@ -180,16 +180,16 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
     const bool mine_v = j < a.vdim;
 
     const int32_t piece = a.piece0 + (int32_t)(item / (uint32_t)a.heads);
-    const int32_t seq = __builtin_amdgcn_readfirstlane(a.seg_shift ? sequence_of(a.offsets, piece, a.N, a.S, a.rows_each, a.seg_shift) : piece);
+    const int32_t seq = __builtin_amdgcn_readfirstlane(a.seg_rows ? sequence_of(a.offsets, piece, a.N, a.S, a.rows_each, a.seg_rows) : piece);
     const Span    span = scalar(span_of(a.offsets, seq, a.N, a.rows_each));
     int begin = span.begin, end = span.end;
     int chunk0 = 0;                                         // the first chunk's number in its sequence
-    if (a.seg_shift) {
-        const int i = piece - piece_base(span.begin, seq, a.seg_shift);
-        if (i < 0 || (int64_t)begin + ((int64_t)i << a.seg_shift) >= end) return;      // (i < 0: rows before the first sequence)
-        begin += i << a.seg_shift;
-        end = end - begin > 1 << a.seg_shift ? begin + (1 << a.seg_shift) : end;
-        chunk0 = i << (a.seg_shift - kChunkShift);
+    if (a.seg_rows) {
+        const int i = piece - piece_base(span.begin, seq, a.seg_rows);
+        if (i < 0 || (int64_t)begin + (int64_t)i * a.seg_rows >= end) return;      // (i < 0: rows before the first sequence)
+        begin += i * a.seg_rows;
+        end = end - begin > a.seg_rows ? begin + a.seg_rows : end;
+        chunk0 = i * (a.seg_rows >> kChunkShift);
     }
     const int chunks = (end - begin + kChunk - 1) >> kChunkShift;
     const int64_t state_at = (int64_t)piece * a.heads + h;  // whole sequences: piece == sequence

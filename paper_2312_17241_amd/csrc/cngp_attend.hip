@@ -263,7 +263,8 @@ struct Plan {
 };
 // Workgroups of all segments together: four for each of 256 CUs, whole turns of the card whatever a CU has room for, as nearly as that can be
 // had (a last segment is half a one in the mean).  Rows in powers of two left a fifth turn of a few (2^15 rows, 16 heads of 128 x 128: 312 against 338 us;
-// 512 or 2048 workgroups: 356 and 367).
+// 512 or 2048 workgroups: 356 and 367).  Twice as many of fp16 heads of at most 32 columns, whose workgroups are a wavefront or two (backward, 2 of
+// 2^16 rows, 8 heads of 32: 247 against 295 us; in fp32, which keeps twice as much in registers, 2^18 rows, 4 heads of 16: 716 against 662).
 constexpr int64_t kItems = 1024, kLeastSegment = 256;
 int64_t longest_of(const cngp_attend_config *c, int64_t N, int64_t S, bool ragged) {
     const int64_t mean = S ? (N + S - 1) / S : 0;
@@ -271,7 +272,8 @@ int64_t longest_of(const cngp_attend_config *c, int64_t N, int64_t S, bool ragge
 }
 Plan plan_of(const cngp_attend_config *c, int64_t N, int64_t S, bool ragged) {
     const int64_t longest = longest_of(c, N, S, ragged);
-    const int64_t items = std::max<int64_t>(kItems - (S + 1) / 2 * c->heads, kItems * 3 / 4), least = (N * c->heads + items - 1) / items;
+    const int64_t all = kItems * (c->io_dtype == CNGP_F16 && std::max(c->key_dim, c->value_dim) <= 32 ? 2 : 1);
+    const int64_t items = std::max<int64_t>(all - (S + 1) / 2 * c->heads, all * 3 / 4), least = (N * c->heads + items - 1) / items;
     const int64_t R = std::max<int64_t>((least + kChunk - 1) / kChunk * kChunk, kLeastSegment);
     if (longest <= 4 * R) return {0, S};
     return {(int)R, pieces(N, S, R)};

@@ -391,11 +391,14 @@ Cut cut_of(bool back, int mp, int np, int depth, int batch) {
         c.parts = most;
         return c;
     }
-    if (c.tiles < kEnoughTiles) c = Cut{1, count(kTile / 2), 0, 1};
-    c.whole = c.tiles;
+    if (c.tiles < kEnoughTiles) {
+        c = Cut{1, count(kTile / 2), 0, 1};
+        c.parts = depth >= 4 * kLeastShare ? (int)std::min<int64_t>(std::max(kSlots / c.tiles, 1), depth / kLeastShare) : 1;
+    }
+    c.whole = c.parts > 1 ? 0 : c.tiles;
     return c;
 }
-size_t sums_bytes(const Cut &c) { return (size_t)c.rest() * c.parts * kTile * kTile * 4; }
+size_t sums_bytes(const Cut &c) { return (size_t)c.rest() * c.parts * (64 * c.U) * (64 * c.U) * 4; }
 
 template <int WHAT>
 int product(const ProductArgs &p, int mp, int np, int batch, hipStream_t st) {
@@ -413,7 +416,8 @@ int product(const ProductArgs &p, int mp, int np, int batch, hipStream_t st) {
     else ortho_product_kernel<WHAT, 1><<<groups, kBlock, 0, st>>>(a);
     if (int rc = launch_status("ortho_product_kernel")) return rc;
     if (!c.rest()) return CNGP_OK;
-    ortho_join_kernel<WHAT, 2><<<(unsigned)(c.rest() * 16), kBlock, 0, st>>>(a);
+    if (c.U == 2) ortho_join_kernel<WHAT, 2><<<(unsigned)(c.rest() * 16), kBlock, 0, st>>>(a);
+    else ortho_join_kernel<WHAT, 1><<<(unsigned)(c.rest() * 4), kBlock, 0, st>>>(a);
     return launch_status("ortho_join_kernel");
 }
 

@@ -110,7 +110,7 @@ def test_same_bits_in_any_workspace_and_batch():
         assert torch.equal(cngp.orthogonalise(cfg, g, workspace=ws), ref)
 
 
-@pytest.mark.parametrize("batch,m,n", [(36, 640, 650), (36, 650, 640), (36, 640, 644), (4, 1000, 2100), (4, 2100, 1000)])
+@pytest.mark.parametrize("batch,m,n", [(36, 640, 650), (36, 650, 640), (36, 640, 644), (4, 1000, 2100), (4, 2100, 1000), (1, 333, 1021), (3, 200, 1100)])
 @pytest.mark.parametrize("io", [F16, F32])
 def test_tiles_that_are_cut_along_the_contraction(batch, m, n, io):
     """Tiles that do not fill the card, or are left after those that do; the last matrices hold them."""

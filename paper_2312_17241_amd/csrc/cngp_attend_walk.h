@@ -114,15 +114,16 @@ constexpr int walk_per_simd(size_t value, int KW) { return value == 2 || KW < 12
 // prompt; of 64 values it gained nothing).
 template <typename T, int KW, int VW, bool OUT>
 struct Lds {
-    static constexpr int kstride = KW + (KW == 128 ? 40 : 8), vstride = VW + (VW == 128 ? 32 : 8);     // see above
+    static constexpr int kstride = KW + (KW == 128 ? 40 : KW == 16 ? 0 : 8), vstride = VW + (VW == 128 ? 32 : VW == 16 ? 0 : 8);     // see above
     static constexpr int parts = sizeof(T) / 2, pstride = 32 + 8, KT = (KW + 31) / 32, VT = (VW + 31) / 32;
     static constexpr int halves = walk_halves(KW), waves = VT * halves;
     static constexpr bool scores = OUT && waves > 1;        // pass through LDS
-    double F[2][kChunk];                                    // log2 of the decay from the chunk's start; this chunk's and the next one's
-    float  far[2][kChunk], keep[2][kChunk];                 // what a row takes from the state, and gives to it
-    float  from[2][kChunk], to[2][kChunk];                  // decay between two rows as a product, where the chunk's are mild: to[t] * from[s]
-    double total[2];
-    int    mild[2];
+    static constexpr int decays = waves > 1 ? 2 : 1;        // this chunk's, and the next one's where another wavefront makes them ready
+    double F[decays][kChunk];                               // log2 of the decay from the chunk's start
+    float  far[decays][kChunk], keep[decays][kChunk];       // what a row takes from the state, and gives to it
+    float  from[decays][kChunk], to[decays][kChunk];        // decay between two rows as a product, where the chunk's are mild: to[t] * from[s]
+    double total[decays];
+    int    mild[decays];
     int    lift[4];                                         // of each score tile
     int    up_q[parts == 2 ? kChunk : 1], up_k[parts == 2 ? kChunk : 1], up_v[parts == 2 ? kChunk : 1];
     float  dots[OUT ? 2 * VT : 1][kChunk];
@@ -230,16 +231,17 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
         const double g = (double)(rdecay < -110.0f ? -110.0f : rdecay) * 1.4426950408889634, f = sum_upto(g);
         if (c + 1 < chunks) fetch_decays(c + 1);
         const double all = __shfl(f, 63, 64), mine = reverse ? f - g : f;
-        lds.F[c & 1][lane] = mine;
-        lds.far[c & 1][lane] = __builtin_amdgcn_exp2f((float)mine) * a.far_scale;
-        lds.keep[c & 1][lane] = __builtin_amdgcn_exp2f((float)(all - mine)) * a.state_scale;
+        const int at = c % L::decays;
+        lds.F[at][lane] = mine;
+        lds.far[at][lane] = __builtin_amdgcn_exp2f((float)mine) * a.far_scale;
+        lds.keep[at][lane] = __builtin_amdgcn_exp2f((float)(all - mine)) * a.state_scale;
         const double middle = __shfl(mine, 31, 64);
-        lds.to[c & 1][lane] = __builtin_amdgcn_exp2f((float)(mine - middle));
-        lds.from[c & 1][lane] = __builtin_amdgcn_exp2f((float)(middle - mine));
+        lds.to[at][lane] = __builtin_amdgcn_exp2f((float)(mine - middle));
+        lds.from[at][lane] = __builtin_amdgcn_exp2f((float)(middle - mine));
         const bool mild = __all(fabs(mine - middle) <= kMild);
         if (lane == 0) {
-            lds.total[c & 1] = all;
-            lds.mild[c & 1] = mild;
+            lds.total[at] = all;
+            lds.mild[at] = mild;
         }
     };
     constexpr bool kAhead = WAVES > 1;                      // a chunk's rows are fetched while the one before is worked on (short rows: registers that
@@ -277,7 +279,7 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
     if (chunks > 0) decays(0);
 
     for (int c = 0; c < chunks; ++c) {
-        const int now = c & 1;
+        const int now = c % L::decays;
         int row0, low, count;
         place(c, row0, count, low);
         if (!kAhead) fetch(c);
@@ -289,7 +291,7 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
         whole += all;
         if (c + 1 < chunks) {
             if (kAhead && !OUT) fetch(c + 1);
-            decays(c + 1);
+            if (WAVES > 1) decays(c + 1);
         }
 
         const bool mild = OUT && __builtin_amdgcn_readfirstlane(lds.mild[now]);
@@ -563,7 +565,10 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
                 }
             }
         }
-        if (c + 1 < chunks) __syncthreads();                // the tiles may be written again
+        if (c + 1 < chunks) {
+            if (WAVES == 1) decays(c + 1);
+            __syncthreads();                                // the tiles may be written again
+        }
     }
     if (a.total && threadIdx.x == 0) a.total[state_at] = (float)whole;
     if (a.final && mine_v) {

@@ -53,7 +53,7 @@ struct Staged {
         }
     }
     // hi, lo: the parts of the tile; lift: of each row (fp32 only)
-    __device__ __forceinline__ void put(_Float16 *hi, _Float16 *lo, int *lift, const int t, const words_t (&v)[words]) const {
+    __device__ __forceinline__ void put(_Float16 *hi, _Float16 *lo, short *lift, const int t, const words_t (&v)[words]) const {
         if (dealt > kChunk && t >= kChunk) return;
         const int at = t * LDS_STRIDE + (int)threadIdx.x % per_row * 8;
         if constexpr (sizeof(T) == 2) {
@@ -69,10 +69,10 @@ struct Staged {
             split(x, power_of_two(up), h, l);
             *reinterpret_cast<half8_t *>(hi + at) = h;
             *reinterpret_cast<half8_t *>(lo + at) = l;
-            if (threadIdx.x % per_row == 0) lift[t] = up;
+            if (threadIdx.x % per_row == 0) lift[t] = (short)up;
         }
     }
-    __device__ __forceinline__ void store(_Float16 *hi, _Float16 *lo, int *lift, const T *low, const bool reverse, const int count, const int stride, const int dim) const {
+    __device__ __forceinline__ void store(_Float16 *hi, _Float16 *lo, short *lift, const T *low, const bool reverse, const int count, const int stride, const int dim) const {
         if constexpr (WHOLE) {
 #pragma unroll
             for (int i = 0; i < each; ++i) put(hi, lo, lift, row + i * rows, r[i]);
@@ -119,14 +119,16 @@ struct Lds {
     static constexpr int halves = walk_halves(KW), waves = VT * halves;
     static constexpr bool scores = OUT && waves > 1;        // pass through LDS
     static constexpr int decays = waves > 1 ? 2 : 1;        // this chunk's, and the next one's where another wavefront makes them ready
-    double F[decays][kChunk];                               // log2 of the decay from the chunk's start
+    union {
+        double F[kChunk];                                   // log2 of the decay from the chunk's start
+        struct { float from[kChunk], to[kChunk]; };         // ... or, of mild chunks, the decay between two rows as a product, to[t] * from[s]
+    } between[decays];
     float  far[decays][kChunk], keep[decays][kChunk];       // what a row takes from the state, and gives to it
-    float  from[decays][kChunk], to[decays][kChunk];        // decay between two rows as a product, where the chunk's are mild: to[t] * from[s]
     double total[decays];
     int    mild[decays];
     int    lift[4];                                         // of each score tile
-    int    up_q[parts == 2 ? kChunk : 1], up_k[parts == 2 ? kChunk : 1], up_v[parts == 2 ? kChunk : 1];
-    float  dots[OUT ? 2 * VT : 1][kChunk];
+    short  up_q[parts == 2 ? kChunk : 1], up_k[parts == 2 ? kChunk : 1], up_v[parts == 2 ? kChunk : 1];     // lifts of the rows
+    float  dots[OUT && VT > 1 ? 2 * VT : 1][VT > 1 ? kChunk : 1];
     union {
         struct {
             alignas(16) _Float16 k[parts][kChunk * kstride];
@@ -135,7 +137,7 @@ struct Lds {
         float far_half[OUT && halves == 2 ? waves : 1][16][64];     // when both tiles have been used: far outputs of the other half's rows
     };
     alignas(16) _Float16 v[parts][kChunk * vstride];
-    alignas(16) _Float16 p[2][scores ? 3 * 32 * pstride : 32];
+    alignas(16) _Float16 p[2][scores ? 3 * 32 * pstride : 8];
 };
 
 // A chunk's decays are mild where none is more than 2^kMild away from the middle row's: two factors in place of an exponential per pair
@@ -232,13 +234,14 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
         if (c + 1 < chunks) fetch_decays(c + 1);
         const double all = __shfl(f, 63, 64), mine = reverse ? f - g : f;
         const int at = c % L::decays;
-        lds.F[at][lane] = mine;
         lds.far[at][lane] = __builtin_amdgcn_exp2f((float)mine) * a.far_scale;
         lds.keep[at][lane] = __builtin_amdgcn_exp2f((float)(all - mine)) * a.state_scale;
         const double middle = __shfl(mine, 31, 64);
-        lds.to[at][lane] = __builtin_amdgcn_exp2f((float)(mine - middle));
-        lds.from[at][lane] = __builtin_amdgcn_exp2f((float)(middle - mine));
-        const bool mild = __all(fabs(mine - middle) <= kMild);
+        const bool   mild = __all(fabs(mine - middle) <= kMild);
+        if (mild) {
+            lds.between[at].to[lane] = __builtin_amdgcn_exp2f((float)(mine - middle));
+            lds.between[at].from[lane] = __builtin_amdgcn_exp2f((float)(middle - mine));
+        } else lds.between[at].F[lane] = mine;
         if (lane == 0) {
             lds.total[at] = all;
             lds.mild[at] = mild;
@@ -315,15 +318,15 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int s = 32 * ss + 8 * (r >> 2) + 4 * half + (r & 3);
-                    p[r] *= lds.from[now][s];
+                    p[r] *= lds.between[now].from[s];
                     if constexpr (kLow) p[r] = ldexpf(p[r], -(lds.up_k[s] + lds.up_v[s]));
                 }
             } else {
-                const double Ft = lds.F[now][32 * tt + col];
+                const double Ft = lds.between[now].F[32 * tt + col];
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int s = 32 * ss + 8 * (r >> 2) + 4 * half + (r & 3);
-                    p[r] *= __builtin_amdgcn_exp2f((float)(Ft - lds.F[now][s]));
+                    p[r] *= __builtin_amdgcn_exp2f((float)(Ft - lds.between[now].F[s]));
                     if constexpr (kLow) p[r] = ldexpf(p[r], -(lds.up_k[s] + lds.up_v[s]));
                 }
             }
@@ -451,7 +454,7 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
                 acc_t near = zero();
                 if constexpr (HALVES == 1) far = part_of_state(tt);
                 const int   t = 32 * tt + col;
-                const float of_row = ldexpf(mild ? a.pair_scale * lds.to[now][t] : a.pair_scale, kLow ? -lds.up_q[t] : 0);
+                const float of_row = ldexpf(mild ? a.pair_scale * lds.between[now].to[t] : a.pair_scale, kLow ? -lds.up_q[t] : 0);
 #pragma unroll 1
                 for (int ss = 0; ss <= tt && 32 * tt < count; ++ss) {
                     acc_t sum = zero(), p;
@@ -542,7 +545,13 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
                 if (a.x) {
                     dn += __shfl_xor(dn, 32, 64);
                     df += __shfl_xor(df, 32, 64);
-                    if (half == 0) {
+                    if (VT == 1) {
+                        if (half == 0 && there) {
+                            const size_t at = (size_t)h * a.N + (size_t)(row0 + t * dir);
+                            a.dot_near[at] = dn;
+                            a.dot_far[at] = df;
+                        }
+                    } else if (half == 0) {
                         lds.dots[2 * vt][t] = dn;
                         lds.dots[2 * vt + 1][t] = df;
                     }
@@ -550,7 +559,7 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
                 apart();
             }
             if (HALVES == 1) state_behind();
-            if (a.x) {
+            if (VT > 1 && a.x) {
                 __syncthreads();
                 if (threadIdx.x < kChunk && (int)threadIdx.x < count) {
                     float dn = 0.0f, df = 0.0f;

@@ -226,20 +226,31 @@ __global__ __launch_bounds__(kBlock) void attend_decay_sum_kernel(const double *
     if (threadIdx.x == 0) ddecay[h] = (float)(sums[0] + sums[1] + sums[2] + sums[3]);
 }
 
-// Gradients of keys or values that several heads share: the heads' parts added up in their order.  Rows of no sequence are left alone.
-template <typename T>
+// Gradients of keys or values that several heads share: the heads' parts added up in their order.  Rows of no sequence are left alone.  Bound by its
+// reads; lanes go over VEC neighbouring values of a row, 2^shift of them, and the rest of a workgroup over rows.
+template <typename T, int VEC>
 __global__ __launch_bounds__(kBlock) void attend_group_kernel(const float *__restrict__ part, T *__restrict__ out, const int32_t *offsets, const int32_t S, const int64_t N,
-                                                              const int kv, const int group, const int dim)
+                                                              const int kv, const int group, const int dim, const int shift)
 {
     const int64_t first = offsets ? span_of(offsets, 0, N, 0).begin : 0, end = offsets ? span_of(offsets, S - 1, N, 0).end : N;
-    const int64_t each = (int64_t)kv * dim, n = (end - first) * each;
-    for (int64_t i = blockIdx.x * (int64_t)kBlock + threadIdx.x; i < n; i += (int64_t)gridDim.x * kBlock) {
-        const int64_t row = first + i / each;
-        const int     c = (int)(i % each), head = c / dim, e = c % dim;
-        const float  *p = part + (row * kv + head) * (int64_t)group * dim + e;
-        float t = 0.0f;
-        for (int g = 0; g < group; ++g) t += p[(int64_t)g * dim];
-        out[row * each + c] = (T)t;
+    const int at = (int)(blockIdx.y << shift | (threadIdx.x & ((1u << shift) - 1))) * VEC, head = at / dim, e = at % dim, rows = kBlock >> shift;
+    if (at >= kv * dim) return;
+    for (int64_t row = first + (int64_t)blockIdx.x * rows + (threadIdx.x >> shift); row < end; row += (int64_t)gridDim.x * rows) {
+        const float *p = part + (row * kv + head) * (int64_t)group * dim + e;
+        float t[VEC];
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) t[i] = 0.0f;
+#pragma unroll 4
+        for (int g = 0; g < group; ++g) {
+            float x[VEC];
+            __builtin_memcpy(x, __builtin_assume_aligned(p + (int64_t)g * dim, 4 * VEC), sizeof x);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) t[i] += x[i];
+        }
+        T y[VEC];
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) y[i] = (T)t[i];
+        __builtin_memcpy(__builtin_assume_aligned(out + row * kv * (int64_t)dim + at, sizeof y), y, sizeof y);
     }
 }
 
@@ -376,6 +387,18 @@ int decay_sum(const double *parts, float *ddecay, int64_t pieces, int heads, hip
     return launch_status("attend_decay_sum_kernel");
 }
 
+template <typename T, int VEC>
+int group_sum(const float *part, void *out, const int32_t *offsets, int64_t S, int64_t N, int kv, int group, int dim, hipStream_t s) {
+    const int units = (kv * dim + VEC - 1) / VEC;
+    int shift = 0;
+    while (shift < 8 && 1 << shift < units) ++shift;
+    const int64_t rows = kBlock >> shift;
+    LaunchTimer t(s, K_ATTEND_DECAY);
+    attend_group_kernel<T, VEC><<<dim3((unsigned)std::min<int64_t>((N + rows - 1) / rows, 1 << 13), (unsigned)((units + (1 << shift) - 1) >> shift)), kBlock, 0, s>>>(
+        part, (T *)out, offsets, (int32_t)S, N, kv, group, dim, shift);
+    return launch_status("attend_group_kernel");
+}
+
 bool lent(const Space &sp, const void *ws, size_t bytes) { return !sp.bytes || (ws && ((uintptr_t)ws & 255u) == 0 && bytes >= sp.bytes); }
 
 }  // namespace
@@ -487,19 +510,15 @@ int cngp_attend_bwd(const cngp_attend_config *cfg, const void *q, const void *k,
     }
     if (int rc = call.walk(a, false)) return rc;
 
-    if (shared) {
-        LaunchTimer t(s, K_ATTEND_DECAY);
+    if (shared)
         for (int which = 0; which < 2; ++which) {
-            const int      dim = which ? V : K;
-            const float   *part = (const float *)(ws + (which ? sp.part_v : sp.part_k));
-            void          *out = which ? dv : dk;
-            const unsigned blocks = (unsigned)std::min<int64_t>((N * cfg->kv_heads * dim + kBlock - 1) / kBlock, 1 << 20);
-            if (cfg->io_dtype == CNGP_F16)
-                attend_group_kernel<_Float16><<<blocks, kBlock, 0, s>>>(part, (_Float16 *)out, offsets, (int32_t)sequences, N, cfg->kv_heads, group, dim);
-            else attend_group_kernel<float><<<blocks, kBlock, 0, s>>>(part, (float *)out, offsets, (int32_t)sequences, N, cfg->kv_heads, group, dim);
-            if (int rc = launch_status("attend_group_kernel")) return rc;
+            const int    dim = which ? V : K;
+            const float *part = (const float *)(ws + (which ? sp.part_v : sp.part_k));
+            void        *out = which ? dv : dk;
+            const bool   f16 = cfg->io_dtype == CNGP_F16, vec = dim % 4 == 0 && ((uintptr_t)out & (f16 ? 7u : 15u)) == 0;
+            const auto   sum = f16 ? vec ? group_sum<_Float16, 4> : group_sum<_Float16, 1> : vec ? group_sum<float, 4> : group_sum<float, 1>;
+            if (int rc = sum(part, out, offsets, sequences, N, cfg->kv_heads, group, dim, s)) return rc;
         }
-    }
     if (!ddecay) return CNGP_OK;
     DecayArgs d{};
     d.q_near = (const float *)(ws + sp.near_q); d.q_far = (const float *)(ws + sp.far_q);

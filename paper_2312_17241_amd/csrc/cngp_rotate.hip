@@ -34,6 +34,7 @@ struct RotateArgs {
 // begin behind the pairs are passed on as they are, 2 VEC side by side in the second form.
 template <typename T, int VEC> struct alignas(sizeof(T) * VEC) Piece { T v[VEC]; };
 
+typedef uint32_t words_t __attribute__((ext_vector_type(4)));
 template <typename T, int VEC, bool NEXT>
 struct Item {
     static constexpr int kValues = NEXT ? (VEC == 1 ? 2 : VEC) : 2 * VEC, kAngles = kValues / 2;
@@ -53,23 +54,29 @@ struct Item {
     }
     __device__ __forceinline__ bool there(const int j, const int dim) const { return (j < kAngles ? at0 + j : at1 + j - kAngles) < dim; }
     __device__ __forceinline__ int component(const int j) const { return j < kAngles ? at0 + j : at1 + j - kAngles; }
-    __device__ __forceinline__ void load(const T *p, const int dim, float (&v)[kValues]) const {
+    // what is on its way from memory: pieces of 16 bytes as they are, or values
+    struct Raw { words_t piece[VEC > 1 ? (NEXT ? 1 : 2) : 1]; float value[VEC > 1 ? 1 : kValues]; };
+    __device__ __forceinline__ void load(const T *p, const int dim, Raw &r) const {
         if constexpr (VEC > 1) {
-            if (NEXT) {
-                const Piece<T, VEC> a = *reinterpret_cast<const Piece<T, VEC> *>(p + (at0 < dim ? at0 : 0));
+            r.piece[0] = *reinterpret_cast<const words_t *>(p + (at0 < dim ? at0 : 0));
+            if constexpr (!NEXT) r.piece[1] = *reinterpret_cast<const words_t *>(p + (at1 < dim ? at1 : 0));
+        } else {
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) v[j] = at0 < dim ? (float)a.v[j] : 0.0f;
-            } else {
-                const Piece<T, VEC> a = *reinterpret_cast<const Piece<T, VEC> *>(p + (at0 < dim ? at0 : 0)), b = *reinterpret_cast<const Piece<T, VEC> *>(p + (at1 < dim ? at1 : 0));
+            for (int j = 0; j < kValues; ++j) r.value[j] = there(j, dim) ? (float)p[component(j)] : 0.0f;
+        }
+    }
+    __device__ __forceinline__ void unpack(const Raw &r, const int dim, float (&v)[kValues]) const {
+        if constexpr (VEC > 1) {
+            typedef T values_t __attribute__((ext_vector_type(VEC)));
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) {
-                    v[j] = at0 < dim ? (float)a.v[j] : 0.0f;
-                    v[VEC + j] = at1 < dim ? (float)b.v[j] : 0.0f;
-                }
+            for (int i = 0; i < (NEXT ? 1 : 2); ++i) {
+                const values_t x = __builtin_bit_cast(values_t, r.piece[i]);
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) v[i * VEC + j] = (i ? at1 : at0) < dim ? (float)x[j] : 0.0f;
             }
         } else {
 #pragma unroll
-            for (int j = 0; j < kValues; ++j) v[j] = there(j, dim) ? (float)p[component(j)] : 0.0f;
+            for (int j = 0; j < kValues; ++j) v[j] = r.value[j];
         }
     }
     __device__ __forceinline__ void store(T *p, const int dim, const float (&v)[kValues]) const {
@@ -107,6 +114,9 @@ __global__ __launch_bounds__(kBlock) void rotate_kernel(const RotateArgs a)
 {
     using I = Item<T, VEC, NEXT>;
     constexpr int V = I::kValues, A = I::kAngles, kGroups = kBlock / LANES;
+    // heads on their way, as they lie in memory (with the norm registers for more cost waves: 211, 213, 248 us for one, two, three, forward and backward of
+    // 2^15 rows, 20 heads of 128, fp16; without it three: 170, 164, 157, 2^18 rows, 5 heads of 36, fp32)
+    constexpr int AHEAD = NORM ? 1 : 3;
     const int lane = (int)threadIdx.x % LANES, group = (int)threadIdx.x / LANES, H = a.heads[0] + a.heads[1];
     float sums[2][ITEMS][V];
     if (BWD && NORM)
@@ -139,7 +149,7 @@ __global__ __launch_bounds__(kBlock) void rotate_kernel(const RotateArgs a)
                 }
             }
         }
-        // queries, then keys; a head ahead is loaded while one is worked on
+        // queries, then keys; the next heads are loaded while one is worked on
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
             const int n0 = w ? a.heads[0] : 0, first_h = (h0 > n0 ? h0 : n0) - n0, last_h = (h1 < n0 + a.heads[w] ? h1 : n0 + a.heads[w]) - n0;
@@ -153,8 +163,10 @@ __global__ __launch_bounds__(kBlock) void rotate_kernel(const RotateArgs a)
             }
             const T *from = (const T *)a.x[w] + (size_t)row * a.heads[w] * a.dim, *up = (const T *)a.dy[w] + (size_t)row * a.heads[w] * a.dim;
             T       *to = (T *)a.y[w] + (size_t)row * a.heads[w] * a.dim;
-            float x[ITEMS][V], u[ITEMS][V], xn[ITEMS][V], un[ITEMS][V];
-            auto load = [&](const int h, float (&xo)[ITEMS][V], float (&uo)[ITEMS][V]) {
+            float x[ITEMS][V], u[ITEMS][V];
+            typename I::Raw rx[AHEAD][ITEMS], ru[AHEAD][ITEMS];
+            auto load = [&](const int h, typename I::Raw (&xo)[ITEMS], typename I::Raw (&uo)[ITEMS]) {
+                if (h >= last_h) return;
 #pragma unroll
                 for (int n = 0; n < ITEMS; ++n) {
                     const I it(lane + n * LANES, a.dim, a.pairs);
@@ -162,16 +174,23 @@ __global__ __launch_bounds__(kBlock) void rotate_kernel(const RotateArgs a)
                     if (BWD) it.load(up + h * a.dim, a.dim, uo[n]);
                 }
             };
-            load(first_h, xn, un);
+#pragma unroll
+            for (int d = 0; d < AHEAD; ++d) load(first_h + d, rx[d], ru[d]);
             for (int h = first_h; h < last_h; ++h) {
 #pragma unroll
-                for (int n = 0; n < ITEMS; ++n)
+                for (int n = 0; n < ITEMS; ++n) {
+                    const I it(lane + n * LANES, a.dim, a.pairs);
+                    if (!BWD || NORM) it.unpack(rx[0][n], a.dim, x[n]);
+                    if (BWD) it.unpack(ru[0][n], a.dim, u[n]);
+                }
 #pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        if (!BWD || NORM) x[n][j] = xn[n][j];
-                        if (BWD) u[n][j] = un[n][j];
+                for (int d = 0; d + 1 < AHEAD; ++d)
+#pragma unroll
+                    for (int n = 0; n < ITEMS; ++n) {
+                        rx[d][n] = rx[d + 1][n];
+                        ru[d][n] = ru[d + 1][n];
                     }
-                if (h + 1 < last_h) load(h + 1, xn, un);
+                load(h + AHEAD, rx[AHEAD - 1], ru[AHEAD - 1]);
                 float r = 1.0f;
                 if (NORM) {
                     float t = 0.0f;
@@ -279,15 +298,19 @@ int launch(const RotateArgs &a, bool norm, bool bwd, unsigned blocks, hipStream_
 }
 template <typename T, int VEC, bool NEXT>
 int launch_lanes(const RotateArgs &a, int lanes, int items, bool norm, bool bwd, unsigned blocks, hipStream_t s) {
+    constexpr int kMost = kMostDim / Item<T, VEC, NEXT>::kValues;
     switch (lanes) {
         case 4: return launch<T, VEC, NEXT, 4, 1>(a, norm, bwd, blocks, s);
         case 8: return launch<T, VEC, NEXT, 8, 1>(a, norm, bwd, blocks, s);
         case 16: return launch<T, VEC, NEXT, 16, 1>(a, norm, bwd, blocks, s);
         case 32: return launch<T, VEC, NEXT, 32, 1>(a, norm, bwd, blocks, s);
-        default:
-            if (items <= 1) return launch<T, VEC, NEXT, 64, 1>(a, norm, bwd, blocks, s);
-            if (items <= 2) return launch<T, VEC, NEXT, 64, 2>(a, norm, bwd, blocks, s);
-            return launch<T, VEC, NEXT, 64, 4>(a, norm, bwd, blocks, s);
+        default:                         // (vectors of a head of at most 512 are fewer)
+            if constexpr (kMost > 128)
+                if (items > 2) return launch<T, VEC, NEXT, 64, 4>(a, norm, bwd, blocks, s);
+            if constexpr (kMost > 64)
+                if (items > 1) return launch<T, VEC, NEXT, 64, 2>(a, norm, bwd, blocks, s);
+            if constexpr (kMost > 32) return launch<T, VEC, NEXT, 64, 1>(a, norm, bwd, blocks, s);
+            return CNGP_ERR_INVALID;
     }
 }
 

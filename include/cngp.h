@@ -436,12 +436,13 @@ int cngp_recur_bwd(const cngp_recur_config *cfg, const void *gate, const void *x
  * Sequences, offsets and `longest` as in cngp_recur_fwd; rows of no sequence are neither used nor written.  N == sequences with offsets NULL
  * is one new token for each running sequence and has a kernel of its own.
  * States and sums in fp32, decays joined in 64 bits; products of computed values take two fp16 numbers each with fp16 storage (22 bits),
- * so that the result has its one rounding to io_dtype and little else.  |scale * v| (backward: |scale * dy|, |scale * q|) has to stay within fp16
- * where io_dtype is.  Decays above 0 work while the products of a sequence's factors stay within fp32.  A row that is not finite spoils its
+ * so that the result has its one rounding to io_dtype and little else, and fp32 arrays' rows alike.  Those numbers are brought into fp16's range by powers
+ * of two, of a row or of what is added to the state in 64 rows, by 2^60 at most there: results keep their bits while the largest of these is
+ * above 2^-50 and the state below 2^60.  Decays above 0 work while the products of a sequence's factors do.  A row that is not finite spoils its
  * sequence's later rows, and those of its 64-row piece before it (counted from the sequence's start), in the heads that read it.
  * Backward, for L = sum(y * dy) + sum(last * dlast) (either may be NULL, not both): dq, dk, dv io_dtype, written; ddecay float32 like decay, written,
  * or NULL (with one decay per head: the sum over all rows); dh0 float32 like h0, written, or NULL; it must not be dlast.  Sums are formed in
- * a fixed order: the same call gives the same bits.
+ * a fixed order: the same call gives the same bits.  With ddecay and sequences of more than 1024 rows N / 1024 + sequences stays below 2^31.
  * Workspace: cngp_attend_workspace_bytes(cfg, N, sequences, call) bytes, 256-byte aligned (may be 0), for call = the sum of
  * CNGP_ATTEND_CALL_*; undefined before and after.  Other arrays must not overlap. */
 enum { CNGP_ATTEND_ROW_DECAY = 1u };

@@ -456,6 +456,9 @@ int cngp_attend_bwd(const cngp_attend_config *cfg, const void *q, const void *k,
     Call call{cfg, decay, N, sequences, offsets, plan_of(cfg, N, sequences, ragged), {}, (char *)workspace, s};
     call.sp = space_of(cfg, call.p, N, sequences, CNGP_ATTEND_CALL_BWD | (ragged ? CNGP_ATTEND_CALL_RAGGED : 0));
     if (!lent(call.sp, workspace, workspace_bytes)) return CNGP_ERR_WORKSPACE;
+    const int64_t longest = longest_of(cfg, N, sequences, ragged);
+    const bool    stretches = longest > kAnchorChunks * kChunk;              // the decays' gradient by stretches of sequences, not sequences
+    if (ddecay && stretches && pieces(N, sequences, 1 << kAnchorShift) > 0x7fffffff) return CNGP_ERR_INVALID;
     char *ws = call.ws;
     const Space &sp = call.sp;
     const int   group = cfg->heads / cfg->kv_heads, K = cfg->key_dim, V = cfg->value_dim;
@@ -528,13 +531,12 @@ int cngp_attend_bwd(const cngp_attend_config *cfg, const void *q, const void *k,
     d.ddecay = rows ? ddecay : nullptr;
     d.parts = rows ? nullptr : (double *)(ws + sp.parts);
     d.N = N; d.S = (int32_t)sequences; d.rows_each = (int32_t)(N / sequences); d.heads = cfg->heads;
-    d.whole = longest_of(cfg, N, sequences, ragged) <= kAnchorChunks * kChunk;
+    d.whole = !stretches;
     d.pieces = d.whole ? sequences : pieces(N, sequences, 1 << kAnchorShift);
     d.kdim = V; d.vdim = K;
     d.size = K * V; d.anchor_size = (int32_t)anchor_floats(V, K);
     {
         LaunchTimer t(s, K_ATTEND_DECAY);
-        const int64_t longest = longest_of(cfg, N, sequences, ragged);
         const int     waves = (int)std::min<int64_t>(kAnchorChunks, std::max<int64_t>(1, (longest + kChunk - 1) / kChunk));
         attend_decay_kernel<<<(unsigned)std::min<int64_t>(d.pieces * d.heads, 0x3fffff), 64 * waves, 0, s>>>(d);
         if (int rc = launch_status("attend_decay_kernel")) return rc;

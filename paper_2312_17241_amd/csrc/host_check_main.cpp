@@ -150,6 +150,29 @@ int main() {
         if (cngp_probe_balance_workspace_bytes(&c) % 256) bad |= 262144;
         if (cngp_probe_balance(&c, nullptr, nullptr, 1.0f, nullptr, nullptr, nullptr, nullptr, 0, nullptr) == CNGP_OK) bad |= 262144;
     }
+    // the token mixer: the same
+    for (int it = 0; it < 2000; ++it) {
+        const int64_t  counts[] = {0, 1, 63, 4097, 100003, (int64_t)1 << 22, (int64_t)1 << 27, 0x7ffeffff, 0x7fffffff};
+        const int64_t  N = counts[below(9)], S = it % 3 ? counts[below(9)] : 1;
+        const uint32_t call = below(4);
+        const int      kv = 1 + (int)below(9), heads = it % 5 ? kv * (1 + (int)below(5)) : (int)below(5000);
+        cngp_attend_config t = {heads, kv, (int)below(140), (int)below(140), (int)below(3), (int)below(1 << 22) - 10, 0.5f, below(3)};
+        const size_t   fwd = cngp_attend_workspace_bytes(&t, N, S, call & CNGP_ATTEND_CALL_RAGGED), bwd = cngp_attend_workspace_bytes(&t, N, S, call | CNGP_ATTEND_CALL_BWD);
+        if (fwd % 256 || bwd % 256 || bwd < fwd) bad |= 524288;
+        if (N > 0 && S > 0 && cngp_attend_fwd(&t, nullptr, nullptr, nullptr, nullptr, N, nullptr, S, nullptr, nullptr, nullptr, nullptr, 0, nullptr) == CNGP_OK) bad |= 524288;
+        if (N > 0 && S > 0 && cngp_attend_bwd(&t, nullptr, nullptr, nullptr, nullptr, N, nullptr, S, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, 0, nullptr) == CNGP_OK)
+            bad |= 524288;
+        cngp_rotate_config r = {(int)below(40), (int)below(40), (int)below(520), 1 + (int)below(4), {0, 0, 0, 0}, (int)below(3), 1e-6f, below(9)};
+        for (int a = 0; a < r.axes; ++a) r.pairs[a] = (int)below(80);
+        if (cngp_rotate_workspace_bytes(&r, N) % 256) bad |= 1048576;
+        if (N > 0 && cngp_rotate_fwd(&r, nullptr, nullptr, N, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr) == CNGP_OK) bad |= 1048576;
+        if (N > 0 && cngp_rotate_bwd(&r, nullptr, nullptr, N, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, 0, nullptr) == CNGP_OK) bad |= 1048576;
+        cngp_ortho_config o = {(int)below(it % 2 ? 5 : 65540), (int)below(17000), (int)below(17000), (int)below(3), (int)below(34), 3.0f, -4.0f, 2.0f, 1e-7f, 0};
+        cngp_muon         m2 = {0.02f, 0.9f, 0.1f, 1.0f, 1};
+        if (cngp_orthogonalise_workspace_bytes(&o) % 256) bad |= 2097152;
+        if (cngp_orthogonalise(&o, nullptr, nullptr, nullptr, 0, nullptr) == CNGP_OK) bad |= 2097152;
+        if (cngp_muon_step(&o, &m2, nullptr, nullptr, nullptr, nullptr, 0, nullptr, 0, nullptr) == CNGP_OK) bad |= 2097152;
+    }
     if (bad) { std::fprintf(stderr, "host sanitizer run: inconsistent results, mask %d\n", bad); return 1; }
     std::printf("host sanitizer run: clean\n");
     return 0;

@@ -37,6 +37,7 @@ struct WalkArgs {
     int32_t      first_i, first_j, final_i, final_j;   // strides of the states' two dimensions
     float        pair_scale, far_scale, state_scale;
     int32_t      reverse, row_decay, out_f32;
+    int32_t      own;                    // the row's own part stays out of dot_near (and of the sums inside the chunk: it is added to the output)
     int32_t      whole;                  // every array's 16-byte pieces (out, x: four values) lie whole and aligned in its rows
 };
 

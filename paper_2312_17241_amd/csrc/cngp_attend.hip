@@ -475,6 +475,7 @@ int cngp_attend_bwd(const cngp_attend_config *cfg, const void *q, const void *k,
         a.first = states;
     } else a.first = h0;
     a.first_i = 1; a.first_j = V;
+    a.own = 1;
     call.output(a, dq, false);
     if (ddecay) {
         a.x = q; a.x_div = 1; a.whole = a.whole && whole_rows(q, K, cfg->io_dtype, cfg->io_dtype == CNGP_F16 ? 8 : 16);
@@ -505,6 +506,7 @@ int cngp_attend_bwd(const cngp_attend_config *cfg, const void *q, const void *k,
     a.pair_scale = a.state_scale = cfg->scale;
     a.first = cut ? states : dlast;
     a.first_i = 1; a.first_j = V;
+    a.own = 1;
     call.output(a, shared ? (void *)(ws + sp.part_k) : dk, shared);
     if (ddecay) {
         a.x = k; a.x_div = group; a.whole = a.whole && whole_rows(k, K, cfg->io_dtype, cfg->io_dtype == CNGP_F16 ? 8 : 16);

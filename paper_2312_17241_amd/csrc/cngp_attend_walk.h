@@ -127,6 +127,7 @@ struct Lds {
     double total[decays];
     int    mild[decays];
     int    lift[4];                                         // of each score tile
+    float  own[scores ? kChunk : 1];                        // a row's score with itself, where it is kept apart
     short  up_q[parts == 2 ? kChunk : 1], up_k[parts == 2 ? kChunk : 1], up_v[parts == 2 ? kChunk : 1];     // lifts of the rows
     float  dots[OUT && VT > 1 ? 2 * VT : 1][VT > 1 ? kChunk : 1];
     union {
@@ -300,8 +301,9 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
         const bool mild = OUT && __builtin_amdgcn_readfirstlane(lds.mild[now]);
         // scores of rows 32 tt .. (lanes) with rows 32 ss .. (registers), the decay between them (without the later row's part where mild), and the
         // power of two they are brought up by; what is the same for a row is left to the sums over ss
-        [[maybe_unused]] auto score = [&](const int tt, const int ss, acc_t &p) -> int {
+        [[maybe_unused]] auto score = [&](const int tt, const int ss, acc_t &p, float &own) -> int {
             p = zero();
+            own = 0.0f;
             if constexpr (!OUT) return 0;
             const int qa = (32 * tt + col) * L::kstride + 8 * half, ka = (32 * ss + col) * L::kstride + 8 * half;
 #pragma unroll
@@ -331,9 +333,12 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
                 }
             }
             if (ss == tt) {
-                const int t = anew(col - 4 * half);
+                const int t = anew(col - 4 * half), last = t - a.own;
+                if (a.own)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) p[r] = 8 * (r >> 2) + (r & 3) <= t ? p[r] : 0.0f;
+                    for (int r = 0; r < 16; ++r) own = 8 * (r >> 2) + (r & 3) == t ? p[r] : own;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) p[r] = 8 * (r >> 2) + (r & 3) <= last ? p[r] : 0.0f;
             }
 #pragma unroll
             for (int r = 0; r < 16; ++r) most = fmaxf(most, fabsf(p[r]));
@@ -342,7 +347,9 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
         if constexpr (L::scores) {
             for (int tile = wave; tile < (count > 32 ? 3 : 1); tile += WAVES) {
                 acc_t p;
-                const int   lift = score(tile > 0, tile > 1, p);
+                float own;
+                const int   lift = score(tile > 0, tile > 1, p, own);
+                if (a.own && tile != 1 && half == (col >> 2 & 1)) lds.own[tile ? 32 + col : col] = own;
                 const float f = power_of_two(lift);
                 if (lane == 0) lds.lift[tile] = lift;
                 _Float16 *to = lds.p[0] + (tile * 32 + col) * L::pstride + 4 * half;
@@ -454,13 +461,14 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
                 acc_t near = zero();
                 if constexpr (HALVES == 1) far = part_of_state(tt);
                 const int   t = 32 * tt + col;
+                [[maybe_unused]] float own = 0.0f;           // score of the row with itself
                 const float of_row = ldexpf(mild ? a.pair_scale * lds.between[now].to[t] : a.pair_scale, kLow ? -lds.up_q[t] : 0);
 #pragma unroll 1
                 for (int ss = 0; ss <= tt && 32 * tt < count; ++ss) {
                     acc_t sum = zero(), p;
                     int   lift;
                     if constexpr (L::scores) lift = __builtin_amdgcn_readfirstlane(lds.lift[tt + ss]);
-                    else lift = score(tt, ss, p);
+                    else lift = score(tt, ss, p, own);
 #pragma unroll
                     for (int s = 0; s < 2; ++s) {
                         half8_t hi, lo;
@@ -488,6 +496,11 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
                     __syncthreads();
 #pragma unroll
                     for (int r = 0; r < VR; ++r) far[r] += lds.far_half[wave < VT ? wave + VT : wave - VT][r][lane];
+                }
+                if (a.own) {
+                    if constexpr (L::scores) own = lds.own[t];
+                    else own += __shfl_xor(own, 32, 64);
+                    own *= of_row;
                 }
                 const bool there = t < count;
                 const int  base = low + (reverse ? -32 * tt : 32 * tt);
@@ -527,6 +540,12 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
                         float o[4];
 #pragma unroll
                         for (int e = 0; e < 4; ++e) o[e] = near[4 * g + e] + far[4 * g + e];
+                        if (a.own) {
+                            const _Float16 *mine_v = lds.v[0] + t * L::vstride + j0 + 8 * g;
+                            const half4_t   hi = *reinterpret_cast<const half4_t *>(mine_v), lo = *reinterpret_cast<const half4_t *>(mine_v + (kLow ? kChunk * L::vstride : 0));
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) o[e] = fmaf(own, kLow ? (float)hi[e] + (float)lo[e] : (float)hi[e], o[e]);
+                        }
                         if (WHOLE) {
                             if (8 * g < left) {
                                 if (kLow || a.out_f32) *reinterpret_cast<float4_t *>((to32 + 8 * g) + mine) = float4_t{o[0], o[1], o[2], o[3]};

@@ -146,6 +146,27 @@ def test_decays_mild_and_sharp(io, sharp):
         R.within(name, host(got), want[key], bound[key], NP[io] if name in ("dq", "dk", "dv") else np.float32)
 
 
+@pytest.mark.parametrize("D", [12, 40, 128])
+@pytest.mark.parametrize("io", [F16, F32])
+def test_gradients_of_sharp_decays(io, D):
+    """Decays of e^-12: the gradient is what the rows before give, 10^-5 of the row's own product with itself, which must not enter its sums.  Bounds as
+    in attend_bounds, with the magnitudes of q.dq and k.dk without that product."""
+    N, H = 150, 2
+    d = make(N, 1, H, H, D, D, io, True, 21)
+    d["decay"][:] = -12.0
+    f = {n: a.astype(np.float64) for n, a in d.items()}
+    want = R.attend(f["q"], f["k"], f["v"], f["decay"], [(0, N)], None, 1.0, f["dy"])
+    a = {n: np.abs(t) for n, t in f.items()}
+    m = R.attend(a["q"], a["k"], a["v"], f["decay"], [(0, N)], None, 1.0, a["dy"])
+    own = (a["q"] * a["k"]).sum(2) * (a["v"] * a["dy"]).sum(2)
+    near = (a["q"] * m["dq"]).sum(2) + (a["k"] * m["dk"]).sum(2) - 2 * own
+    bound = np.broadcast_to(R.rounds(D, D, N) * R.U * 3 * (m["dg"].max(0) + near.sum(0)), (N, H))
+    cfg = cngp.AttendConfig(H, H, D, D, io, flags=cngp.ATTEND_ROW_DECAY)
+    t = {n: dev(x) for n, x in d.items()}
+    got = cngp.attend_bwd(cfg, t["q"], t["k"], t["v"], t["decay"], dy=t["dy"])
+    R.within("ddecay", host(got[3]), want["dg"], bound)
+
+
 def test_state_updated_in_place():
     for N, S, H, D in ((6, 6, 3, 20), (640, 2, 2, 64), (2600, 1, 1, 16)):
         d = make(N, S, H, H, D, D, F32, True, 5)

@@ -2,8 +2,9 @@
 //     X = G / (|G| + eps);      each step   A = X X^T,   B = b A + c A A,   X <- a X + B X
 // The products run on the matrix cores.  One fp16 number per value would not do: the polynomial lifts small singular values by 3.4 in each
 // step and with them what a rounding put into their directions, so that 11 bits leave errors of a tenth of an entry.  Every operand is two fp16
-// numbers, the second scaled by 2^11, and a product three (high by high, and both mixed ones into sums of their own): 22 bits.
-// A and B are symmetric: tiles on and below the diagonal are computed and written twice.
+// numbers, and a product three (high by high and both mixed ones, into the same sums): 22 bits.  (Low parts scaled apart, with sums of their own, took
+// 16464 us for 4096 x 4096 and five steps, this form 5833, registers being short.)  A and B are symmetric: tiles on and below the diagonal are computed
+// and written twice.
 #include <algorithm>
 #include <cmath>
 
@@ -22,7 +23,7 @@ constexpr int kPad = 8;                                     // halves between ro
 // is left above: entries of X below 4 (so its singular values may be), of A below 16, of B below 64.
 constexpr float kScaleX = 16384.0f, kScaleA = 4096.0f, kScaleB = 1024.0f;
 constexpr int kNormParts = 1024;
-constexpr int64_t kEnoughTiles = 256;                       // of 128 x 128: a CU each
+constexpr int64_t kEnoughTiles = 256;                       // of 128 x 128: a CU each (1024 x 4096, 256 tiles: 471 us, by tiles of 64 x 64 529; 6 of 1000 x 333, 144: 254 and 237)
 constexpr int kSlots = 512, kLeastShare = 256;              // ... that run at a time; least length of a share of a contraction
 
 // High and low parts of a matrix, rows of `stride` values.
@@ -143,7 +144,7 @@ __device__ __forceinline__ float inverse_norm(const double *parts, const int cou
     return norm > 0.0 || norm != norm ? (float)(1.0 / norm) : 0.0f;
 }
 
-// X from G (transposed where `turned`), with zeros behind its edges: 64 x 64 tiles.
+// X from G (transposed where `turned`), with zeros behind its edges: 64 x 64 tiles, bound by its reads and writes (4096 x 4096 fp32: 30 us).
 template <typename T>
 __global__ __launch_bounds__(kBlock) void ortho_start_kernel(const T *__restrict__ g, const Step st, const int rows, const int cols, const bool turned, const double *__restrict__ parts,
                                                              const int count, const float eps, const float scale, const Pair X)
@@ -253,7 +254,10 @@ __device__ __forceinline__ void finish(const ProductArgs &a, const Tile &t, cons
 }
 
 // A tile of 64 U x 64 U of a product by four wavefronts of 32 U x 32 U; computed transposed (a lane has a row of C and four neighbouring columns in
-// four registers).
+// four registers).  The next piece of the contraction is fetched into registers while one is multiplied from LDS, two buffers, so one barrier a piece.
+// 4096 x 4096: 460 us the last product, 235 and 255 the triangles', 870 TFLOP/s of fp16 operations where a library product reaches 1200.  Bound by what is
+// exposed around the barriers: wavefronts wait for the matrix instructions' queue half of the time, for barriers and loads a quarter.  One buffer and three
+// workgroups to a CU took 6116 us in place of 5000 for the five steps, pieces fetched further ahead (64 x 64 tiles) 244 for 236.
 template <int WHAT, int U>
 __global__ __launch_bounds__(kBlock, 2) void ortho_product_kernel(const ProductArgs a)
 {
@@ -354,7 +358,8 @@ __global__ __launch_bounds__(kBlock, 2) void ortho_product_kernel(const ProductA
             }
 }
 
-// Shares of a contraction added up, in their order: a workgroup for 16 x 16 of a tile's 128 x 128 (a quarter of each wavefront's 32 x 32).
+// Shares of a contraction added up, in their order: a workgroup for eight columns of one of each wavefront's 32 x 32.  Bound by its reads (thirds of 144 tiles,
+// 28 MB: 13 us).
 template <int WHAT, int U>
 __global__ __launch_bounds__(kBlock) void ortho_join_kernel(const ProductArgs a)
 {
@@ -377,7 +382,8 @@ __global__ __launch_bounds__(kBlock) void ortho_join_kernel(const ProductArgs a)
 
 // How a product's tiles are shared out.  A card has room for two workgroups of 128 x 128 on each of its 256 CUs: what is left after whole turns of
 // 512 is cut along the contraction, into as many parts as there is room for (of 256 at least), and joined by a second launch.  (528 tiles of a
-// triangle of 4096: the last 16 alone took more than half of what the 512 before them did.)
+// triangle of 4096: the last 16 alone took more than half of what the 512 before them did, 5683 us in place of 5007 for the five steps.  Tiles that do not
+// fill the card go in parts of 1024 at least: 4 of 1024 x 4096, thirds of 1365, 95 + 13 us in place of 141 by 64 x 64; of 341, 26 + 23 in place of 36.)
 struct Cut {
     int U, tiles, whole, parts;
     int64_t rest() const { return (int64_t)tiles - whole; }
@@ -423,7 +429,7 @@ int product(const ProductArgs &p, int mp, int np, int batch, hipStream_t st) {
 
 // ---------------------------------------------------------------- matrices of at most 64 x 128
 // One workgroup does everything in one launch: X in registers (fp32, as the tiles of the last product come out), its two parts and those of A and
-// B in LDS.  Bound by the chain of products (four barriers a step).
+// B in LDS.  Bound by the chain of products (four barriers a step): 64 x 64, five steps 16.5 us; by the kernels above 262.
 struct SmallArgs {
     const void *g;
     void       *out;

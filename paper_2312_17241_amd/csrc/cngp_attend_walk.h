@@ -10,7 +10,7 @@
 // Precision: rounding what is computed (scores, state, decayed v) to fp16 would cost half of the result's accuracy.  It is split in two fp16
 // numbers (22 bits) after a power of two has brought its largest value to 2^13, and takes two products.  fp16 storage: q, k, v are
 // exact operands.  fp32 storage: they are split as well, each row by a power of two of its own, and products take three (the fp32 products of
-// the matrix cores have a sixteenth of the rate: 4096 rays of 64 samples, 4 heads of 16, a walk 526 us, so 110).
+// the matrix cores have a sixteenth of the rate: 4096 rays of 64 samples, 4 heads of 16, a walk 526 us, so 102).
 // Bound by the chain inside a chunk: two barriers or three, between them vector instructions (38 % of the cycles), LDS (28) and matrix instructions (17)
 // that one or two workgroups to a CU do not lay over each other.  2^15 rows, 16 heads of 128 x 128, fp16: 242 us, 1.4 TB/s.
 #pragma once
@@ -131,6 +131,8 @@ struct Lds {
     int    lift[4];                                         // of each score tile
     float  own[scores ? kChunk : 1];                        // a row's score with itself, where it is kept apart
     short  up_q[parts == 2 ? kChunk : 1], up_k[parts == 2 ? kChunk : 1], up_v[parts == 2 ? kChunk : 1];     // lifts of the rows
+    static constexpr bool folds = parts == 2 && waves == 1; // ... which go into the decays once a chunk, where no barrier is needed for that (rays: 474 against 509 us)
+    float  down[folds ? kChunk : 1];                        // 2^-(lifts of k and v)
     float  dots[OUT && VT > 1 ? 2 * VT : 1][VT > 1 ? kChunk : 1];
     union {
         struct {
@@ -293,6 +295,17 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
         rk.store(lds.k[0], lds.k[L::parts - 1], lds.up_k, k + (int64_t)low * ks, reverse, a.k ? count : 0, ks, a.kdim);
         rv.store(lds.v[0], lds.v[L::parts - 1], lds.up_v, v + (int64_t)low * vs, reverse, a.v ? count : 0, vs, a.vdim);
         __syncthreads();
+        if constexpr (L::folds) {
+            const float down = ldexpf(1.0f, -(lds.up_k[lane] + lds.up_v[lane])), down_q = OUT ? ldexpf(1.0f, -lds.up_q[lane]) : 0.0f;
+            lds.down[lane] = down;
+            lds.keep[now][lane] *= down;
+            if (OUT) lds.far[now][lane] *= down_q;
+            if (OUT && lds.mild[now]) {
+                lds.between[now].from[lane] *= down;
+                lds.between[now].to[lane] *= down_q;
+            }
+            __syncthreads();
+        }
         const double all = lds.total[now];
         whole += all;
         if (c + 1 < chunks) {
@@ -323,7 +336,7 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
                 for (int r = 0; r < 16; ++r) {
                     const int s = 32 * ss + 8 * (r >> 2) + 4 * half + (r & 3);
                     p[r] *= lds.between[now].from[s];
-                    if constexpr (kLow) p[r] = ldexpf(p[r], -(lds.up_k[s] + lds.up_v[s]));
+                    if constexpr (kLow && !L::folds) p[r] = ldexpf(p[r], -(lds.up_k[s] + lds.up_v[s]));
                 }
             } else {
                 const double Ft = lds.between[now].F[32 * tt + col];
@@ -331,7 +344,8 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
                 for (int r = 0; r < 16; ++r) {
                     const int s = 32 * ss + 8 * (r >> 2) + 4 * half + (r & 3);
                     p[r] *= __builtin_amdgcn_exp2f((float)(Ft - lds.between[now].F[s]));
-                    if constexpr (kLow) p[r] = ldexpf(p[r], -(lds.up_k[s] + lds.up_v[s]));
+                    if constexpr (L::folds) p[r] *= lds.down[s];
+                    else if constexpr (kLow) p[r] = ldexpf(p[r], -(lds.up_k[s] + lds.up_v[s]));
                 }
             }
             if (ss == tt) {
@@ -394,7 +408,7 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
                 far = mfma(lo, b, far);
                 if constexpr (kLow) far = mfma(hi, read4_4(lds.q[1] + at), far);
             }
-            const float f = ldexpf(lds.far[now][32 * tt + col], -(up + lift + (kLow ? lds.up_q[32 * tt + col] : 0)));
+            const float f = ldexpf(lds.far[now][32 * tt + col], -(up + lift + (kLow && !L::folds ? lds.up_q[32 * tt + col] : 0)));
 #pragma unroll
             for (int r = 0; r < VR; ++r) far[r] *= f;
             return far;
@@ -419,7 +433,7 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const int t = 16 * s + 8 * half + i;
-                    x[s][i] = kLow ? ((float)b[i] + (float)l[i]) * ldexpf(lds.keep[now][t], -(lds.up_k[t] + lds.up_v[t])) : (float)b[i] * lds.keep[now][t];
+                    x[s][i] = L::folds ? ((float)b[i] + (float)l[i]) * lds.keep[now][t] : kLow ? ((float)b[i] + (float)l[i]) * ldexpf(lds.keep[now][t], -(lds.up_k[t] + lds.up_v[t])) : (float)b[i] * lds.keep[now][t];
                     most = fmaxf(most, fabsf(x[s][i]));
                 }
             }
@@ -464,7 +478,7 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
                 if constexpr (HALVES == 1) far = part_of_state(tt);
                 const int   t = 32 * tt + col;
                 [[maybe_unused]] float own = 0.0f;           // score of the row with itself
-                const float of_row = ldexpf(mild ? a.pair_scale * lds.between[now].to[t] : a.pair_scale, kLow ? -lds.up_q[t] : 0);
+                const float of_row = ldexpf(mild ? a.pair_scale * lds.between[now].to[t] : a.pair_scale, kLow && !(L::folds && mild) ? -lds.up_q[t] : 0);
 #pragma unroll 1
                 for (int ss = 0; ss <= tt && 32 * tt < count; ++ss) {
                     acc_t sum = zero(), p;

@@ -21,8 +21,6 @@ struct StepArgs {
     int32_t      row_decay;
 };
 
-template <typename T> __device__ __forceinline__ float value(const T v) { return (float)v; }
-
 // One row to each sequence: a workgroup per sequence and head goes over its state once (read, decayed, the row added, written, multiplied
 // with the query), neighbouring lanes neighbouring columns of VEC values, bound by those reads and writes (512 states of 64 x 64, 17 MB: 6.2 us).
 template <typename T, int BLOCK, int VEC>

@@ -39,7 +39,7 @@ __device__ __forceinline__ half8_t read_column(const _Float16 *tile, const int s
 }
 
 // x * scale as a high and a low part; what subnormal parts lose is 2^-39 of the largest value where that has been lifted (lift_of).  (As a product and
-// sum the low part is one instruction, as a difference three: a scale of 1 has to be one that the compiler does not know, see anew.)
+// sum the low part is one instruction, as a difference three.)
 __device__ __forceinline__ void split(const float (&x)[8], const float scale, half8_t &hi, half8_t &lo) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -86,10 +86,6 @@ __device__ __forceinline__ void apart() { __builtin_amdgcn_sched_barrier(0); }
 // The same value, which the compiler takes for another one: what is computed from it in a loop is computed there, and not before it and kept in
 // registers.  (Conditions on the entries of a tile are two scalar registers each.)
 __device__ __forceinline__ int anew(int v) {
-    asm volatile("" : "+v"(v));
-    return v;
-}
-__device__ __forceinline__ float anew(float v) {
     asm volatile("" : "+v"(v));
     return v;
 }

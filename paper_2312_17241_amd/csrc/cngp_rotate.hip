@@ -210,9 +210,10 @@ __global__ __launch_bounds__(kBlock) void rotate_kernel(const RotateArgs a)
                     }
 #pragma unroll
                     for (int k = 0; k < A; ++k) {
+                        // (a sine of 0: passed on, also next to what is not finite)
                         const float p = u[n][I::first(k)], q = u[n][I::second(k)];
-                        u[n][I::first(k)] = fmaf(p, c[n][k], -(q * s[n][k]));
-                        u[n][I::second(k)] = fmaf(p, s[n][k], q * c[n][k]);
+                        u[n][I::first(k)] = s[n][k] != 0.0f ? fmaf(p, c[n][k], -(q * s[n][k])) : p * c[n][k];
+                        u[n][I::second(k)] = s[n][k] != 0.0f ? fmaf(p, s[n][k], q * c[n][k]) : q * c[n][k];
                     }
                     if (BWD && NORM) {
 #pragma unroll

@@ -474,8 +474,8 @@ int cngp_attend_bwd(const cngp_attend_config *cfg, const void *q, const void *k,
  *   gamma_q, gamma_k dev float32 [dim], or NULL
  *   q_out, k_out like q, k, written; each may be its input itself
  * Backward for L = sum(q_out * dq_out) + sum(k_out * dk_out): dq, dk like q, k, written, each may be dq_out, dk_out itself; dgamma_q, dgamma_k dev
- * float32 [dim], accumulated (+=) or written with CNGP_ZERO_GRADS (then also where N is 0), or NULL; summed in a fixed order.  q and k are
- * the forward's inputs, used with CNGP_ROTATE_NORM only.  Positions and omega are constants.
+ * float32 [dim], accumulated (+=) or written with CNGP_ZERO_GRADS (then also where N is 0, and zeros without CNGP_ROTATE_NORM), or NULL; summed in
+ * a fixed order.  q and k are the forward's inputs, used with CNGP_ROTATE_NORM only.  Positions and omega are constants.
  *   dim 1 .. 512     heads, kv_heads 0 .. 4096     axes 1 .. 4     eps >= 0     N at most 2^31 - 2^16
  *   workspace (gradients of gains only) dev, 256-byte aligned, cngp_rotate_workspace_bytes(cfg, N) bytes; undefined before and after */
 enum { CNGP_ROTATE_NORM = 2u, CNGP_ROTATE_NEXT = 4u };      /* beside CNGP_ZERO_GRADS = 1 */

@@ -379,7 +379,7 @@ int cngp_rotate_bwd(const cngp_rotate_config *cfg, const void *q, const void *k,
                     const float *gamma_k, const void *dq_out, const void *dk_out, void *dq, void *dk, float *dgamma_q, float *dgamma_k, void *workspace,
                     size_t workspace_bytes, void *stream) {
     if (int rc = check(cfg, N)) return rc;
-    const bool norm = cfg->flags & CNGP_ROTATE_NORM, gains = norm && (dgamma_q || dgamma_k);
+    const bool norm = cfg->flags & CNGP_ROTATE_NORM, gains = norm && (dgamma_q || dgamma_k);       // without norms they are zeros
     hipStream_t s = (hipStream_t)stream;
     unsigned groups = 0;
     if (N) {
@@ -393,7 +393,8 @@ int cngp_rotate_bwd(const cngp_rotate_config *cfg, const void *q, const void *k,
         a.part = gains ? (float *)workspace : nullptr;
         if (int rc = run(cfg, a, true, &groups, s)) return rc;
     }
-    if (!gains) return CNGP_OK;
+    if (!gains && !((dgamma_q || dgamma_k) && (cfg->flags & CNGP_ZERO_GRADS))) return CNGP_OK;
+    if (!norm) groups = 0;
     LaunchTimer t(s, K_ROTATE_BWD);
     rotate_gain_kernel<<<(unsigned)(2 * cfg->dim), 64, 0, s>>>((const float *)workspace, cfg->heads ? dgamma_q : nullptr, cfg->kv_heads ? dgamma_k : nullptr,
                                                                  (int)groups, cfg->dim, !(cfg->flags & CNGP_ZERO_GRADS));

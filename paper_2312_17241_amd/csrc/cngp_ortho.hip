@@ -137,11 +137,15 @@ __global__ __launch_bounds__(kBlock) void ortho_norm_kernel(const T *__restrict_
     if (threadIdx.x == 0) parts[(size_t)blockIdx.y * gridDim.x + blockIdx.x] = t;
 }
 
-__device__ __forceinline__ float inverse_norm(const double *parts, const int count, const float eps, double *room) {
+// In 64 bits, as the products with it: norms of fp32 matrices and their inverses leave fp32's range.
+__device__ __forceinline__ double inverse(const double squares, const float eps) {
+    const double norm = sqrt(squares) + (double)eps;
+    return norm > 0.0 || norm != norm ? 1.0 / norm : 0.0;
+}
+__device__ __forceinline__ double inverse_norm(const double *parts, const int count, const float eps, double *room) {
     double t = 0.0;
     for (int i = threadIdx.x; i < count; i += kBlock) t += parts[(size_t)blockIdx.z * count + i];
-    const double norm = sqrt(block_sum(t, room)) + (double)eps;
-    return norm > 0.0 || norm != norm ? (float)(1.0 / norm) : 0.0f;
+    return inverse(block_sum(t, room), eps);
 }
 
 // X from G (transposed where `turned`), with zeros behind its edges: 64 x 64 tiles, bound by its reads and writes (4096 x 4096 fp32: 30 us).
@@ -151,13 +155,13 @@ __global__ __launch_bounds__(kBlock) void ortho_start_kernel(const T *__restrict
 {
     __shared__ double room[4];
     __shared__ float  tile[64][65];
-    const float inv = inverse_norm(parts, count, eps, room) * scale;
+    const double inv = inverse_norm(parts, count, eps, room) * (double)scale;
     const size_t first = (size_t)blockIdx.z * rows * cols;
     const int m0 = (int)blockIdx.y * 64, n0 = (int)blockIdx.x * 64;     // of X
     const int c = threadIdx.x & 63;
     for (int r = threadIdx.x >> 6; r < 64; r += 4) {
         const int row = (turned ? n0 : m0) + r, col = (turned ? m0 : n0) + c;
-        const float v = row < rows && col < cols ? entry(g, st, first + (size_t)row * cols + col) * inv : 0.0f;
+        const float v = row < rows && col < cols ? (float)((double)entry(g, st, first + (size_t)row * cols + col) * inv) : 0.0f;
         if (turned) tile[c][r] = v;
         else tile[r][c] = v;
     }
@@ -173,11 +177,11 @@ template <typename T>
 __global__ __launch_bounds__(kBlock) void ortho_scale_kernel(const T *g, const Step st, T *out, const int64_t n, const double *__restrict__ parts, const int count, const float eps)
 {
     __shared__ double room[4];
-    const float inv = inverse_norm(parts, count, eps, room);
+    const double inv = inverse_norm(parts, count, eps, room);
     for (int64_t i = blockIdx.x * (int64_t)kBlock + threadIdx.x; i < n; i += (int64_t)gridDim.x * kBlock)
     {
         const size_t at = (size_t)blockIdx.z * n + i;
-        const float  v = entry(g, st, at) * inv;
+        const float  v = (float)((double)entry(g, st, at) * inv);
         if (st.m) moved(st, at, v);
         else out[at] = (T)v;
     }
@@ -455,8 +459,7 @@ __global__ __launch_bounds__(kBlock) void ortho_small_kernel(const SmallArgs a)
 #pragma unroll
         for (int u = 0; u < 8; ++u) t = fma((double)v[u], (double)v[u], t);
     }
-    const double norm = sqrt(block_sum(t, room)) + (double)a.eps;
-    const float  scale = norm > 0.0 || norm != norm ? (float)(1.0 / norm) : 0.0f;
+    const double scale = inverse(block_sum(t, room), a.eps);
     float x[kTiles][16];
     auto place = [&](const int r, const int j) -> size_t { return a.turned ? (size_t)j * a.m + r : (size_t)r * a.n + j; };
 #pragma unroll
@@ -464,7 +467,7 @@ __global__ __launch_bounds__(kBlock) void ortho_small_kernel(const SmallArgs a)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             const int j = jw + 64 * k + 8 * (r >> 2) + 4 * half + (r & 3);
-            x[k][r] = i < a.m && j < a.n ? entry(g, a.step, first + place(i, j)) * scale : 0.0f;
+            x[k][r] = i < a.m && j < a.n ? (float)((double)entry(g, a.step, first + place(i, j)) * scale) : 0.0f;
         }
     auto keep4 = [&](_Float16 *hi, _Float16 *lo, const int at, const float (&v)[4]) {
         half4_t h, l;

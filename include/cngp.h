@@ -495,9 +495,10 @@ int cngp_rotate_bwd(const cngp_rotate_config *cfg, const void *q, const void *k,
 
 /* Orthogonalised update of matrices: X with the singular vectors of G and singular values near 1, by `steps` products of a polynomial
  *     X = G / (|G|_F + eps);    each step:  A = X X^T,   X <- a X + (b A + c A A) X          (of the transposed matrix where rows > cols)
- * with the same three coefficients in every step (3.4445, -4.7750, 2.0315 bring singular values above a thousandth of the norm
- * into 0.7 .. 1.2 in five steps; 1.5, -0.5, 0 converge to 1 slowly).  The products run on the matrix cores, every operand as two fp16 numbers (22 bits), sums in fp32;
- * the norm in 64 bits.  A matrix of zeros gives zeros; one with a value that is not finite gives values that are not finite.
+ * with the same three coefficients in every step (3.4445, -4.7750, 2.0315 bring singular values from 0.0016 of the norm on into
+ * 0.68 .. 1.21 in five steps, 0.001 of it to 0.47; 1.5, -0.5, 0 converge to 1 slowly).  The products run on the matrix cores, every operand as two fp16
+ * numbers (22 bits), sums in fp32; the norm and the division by it in 64 bits.  Errors are small beside the matrix, not beside each of its entries.
+ * A matrix of zeros gives zeros; one with a value that is not finite gives values that are not finite.
  * Not part of the paper's method: an optimiser step for the matrices around the encoding, where cngp_adam_step takes arrays entry by entry.
  *   g dev io_dtype [batch, rows, cols]        out like g, written; may be g itself
  *   rows, cols 1 .. 16384      batch 1 .. 65535      steps 0 .. 32      eps >= 0      |a|, |b|, |c| <= 16, such that with s the largest singular value of

@@ -435,11 +435,14 @@ int cngp_recur_bwd(const cngp_recur_config *cfg, const void *gate, const void *x
  *   heads 1 .. 4096, a multiple of kv_heads      key_dim, value_dim 1 .. 128      N, sequences at most 2^31 - 2^16      scale finite
  * Sequences, offsets and `longest` as in cngp_recur_fwd; rows of no sequence are neither used nor written.  N == sequences with offsets NULL
  * is one new token for each running sequence and has a kernel of its own.
- * States and sums in fp32, decays joined in 64 bits; products of computed values take two fp16 numbers each with fp16 storage (22 bits),
- * so that the result has its one rounding to io_dtype and little else, and fp32 arrays' rows alike.  Those numbers are brought into fp16's range by powers
- * of two, of a row or of what is added to the state in 64 rows, by 2^60 at most there: results keep their bits while the largest of these is
- * above 2^-50 and the state below 2^60.  Decays above 0 work while the products of a sequence's factors do.  A row that is not finite spoils its
- * sequence's later rows, and those of its 64-row piece before it (counted from the sequence's start), in the heads that read it.
+ * States and sums in fp32, decays joined in 64 bits.  What is computed and enters a product (scores, the state, what is added to it) is two fp16 numbers there, 22
+ * bits, as is every value of fp32 arrays; fp16 arrays enter as they are.  A power of two brings the largest of the values that share it into fp16's range: of a row
+ * of a head (fp32 arrays), of the scores of 32 rows with 32, of the state's 32 neighbouring columns, of what 64 rows add to those (by 2^60 at most: the
+ * largest of it above 2^-50, the state below 2^60).  A value is held to 2^-38 of the largest beside it: 22 bits down to 2^-16 of that, 11 at 2^-27, none below
+ * 2^-38 (an fp32 column of v that is 10^-6 of another one comes out to 4 10^-6 of itself, one of 10^-8 to 4 10^-4; N == sequences
+ * with offsets NULL computes in fp32 alone and has no such limit).  Decays above 0 work while the products of a sequence's factors do.  A row that is not finite spoils its
+ * sequence's later rows, and those of its 64-row piece before it (counted from the sequence's start), in the heads that read it; backward, its sequence in
+ * these heads, but for dq of earlier pieces.
  * Backward, for L = sum(y * dy) + sum(last * dlast) (either may be NULL, not both): dq, dk, dv io_dtype, written; ddecay float32 like decay, written,
  * or NULL (with one decay per head: the sum over all rows); dh0 float32 like h0, written, or NULL; it must not be dlast.  Sums are formed in
  * a fixed order: the same call gives the same bits.  With ddecay and sequences of more than 1024 rows N / 1024 + sequences stays below 2^31.
@@ -468,7 +471,8 @@ int cngp_attend_bwd(const cngp_attend_config *cfg, const void *q, const void *k,
  *     pair p of u's components turned by the angle position[n][axis of p] * omega[p]; components behind the pairs pass as they are
  * Axis a turns pairs[a] pairs, axis after axis (one for texts, rows and columns of images, time besides for videos, coordinates of points).
  * Pair p holds components p and p + the number of pairs, or 2p and 2p + 1 with CNGP_ROTATE_NEXT.  Angles are formed in 64 bits
- * from the fp32 numbers, whole turns taken off there: far positions turn as exactly as near ones.  Everything else in fp32, one rounding.
+ * from the fp32 numbers, whole turns taken off there: far positions turn as exactly as near ones, up to 2^29 turns.  Everything else in fp32, the sum of a
+ * head's squares too, one rounding.
  *   q dev io_dtype [N, heads, dim]     k dev io_dtype [N, kv_heads, dim]; either number of heads may be 0, its arrays are then ignored
  *   position dev float32 [N, axes]     omega dev float32 [sum of pairs]; NULL without pairs
  *   gamma_q, gamma_k dev float32 [dim], or NULL

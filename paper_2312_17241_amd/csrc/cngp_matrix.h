@@ -38,8 +38,8 @@ __device__ __forceinline__ half8_t read_column(const _Float16 *tile, const int s
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// x * scale as a high and a low part; what subnormal parts lose is 2^-39 of the largest value where that has been lifted (lift_of).  (As a product and
-// sum the low part is one instruction, as a difference three.)
+// x * scale as a high and a low part.  Subnormal parts are kept: what is lost is half of 2^-24, 2^-38 of the largest value where that has been lifted to
+// 2^13 (lift_of).  (As a product and sum the low part is one instruction, as a difference three.)
 __device__ __forceinline__ void split(const float (&x)[8], const float scale, half8_t &hi, half8_t &lo) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {

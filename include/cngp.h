@@ -445,12 +445,13 @@ int cngp_recur_bwd(const cngp_recur_config *cfg, const void *gate, const void *x
  * these heads, but for dq of earlier pieces.
  * Backward, for L = sum(y * dy) + sum(last * dlast) (either may be NULL, not both): dq, dk, dv io_dtype, written; ddecay float32 like decay, written,
  * or NULL (with one decay per head: the sum over all rows); dh0 float32 like h0, written, or NULL; it must not be dlast.  Sums are formed in
- * a fixed order: the same call gives the same bits.  With ddecay and sequences of more than 1024 rows N / 1024 + sequences stays below 2^31.
+ * a fixed order: the same call gives the same bits.  For ddecay the states at every 64th row are kept in the workspace (N / 64 of them to a head).
  * Workspace: cngp_attend_workspace_bytes(cfg, N, sequences, call) bytes, 256-byte aligned (may be 0), for call = the sum of
  * CNGP_ATTEND_CALL_*; undefined before and after.  Other arrays must not overlap. */
 enum { CNGP_ATTEND_ROW_DECAY = 1u };
-enum { CNGP_ATTEND_CALL_BWD = 1u,     /* cngp_attend_bwd, else cngp_attend_fwd */
-       CNGP_ATTEND_CALL_RAGGED = 2u };/* offsets are given                     */
+enum { CNGP_ATTEND_CALL_BWD = 1u,       /* cngp_attend_bwd, else cngp_attend_fwd */
+       CNGP_ATTEND_CALL_RAGGED = 2u,    /* offsets are given                     */
+       CNGP_ATTEND_CALL_NO_DDECAY = 4u };/* backward, ddecay is NULL: less room   */
 typedef struct cngp_attend_config {
     int32_t  heads, kv_heads, key_dim, value_dim;
     int32_t  io_dtype;        /* cngp_dtype of q, k, v, y and their gradients */

@@ -119,23 +119,21 @@ __global__ __launch_bounds__(kBlock) void attend_carry_kernel(const CarryArgs a)
     }
 }
 
-// Gradient of the log decays.  That of row t is the part of the result that reaches over t: with near = the products inside a chunk, far = those
-// with states, D = <state, gradient of the state> at a chunk's start and T = what crosses the whole chunk,
-//     sum over s >= t of (q.dq near - k.dk near + q.dq far)  +  sum over s < t of k.dk far  +  T,     T = D - sum of q.dq far,
-// and D of the next chunk is T + sum of k.dk far.  D is formed anew from both states every kAnchorChunks chunks: sums that ran on over a long
-// sequence would bury the short memories' gradients in their rounding.  A workgroup per such stretch and head, a wavefront per chunk, a lane per row
-// (2^18 rows of 4096 sequences, 4 heads: 38 us, bound by chains of loads and permutations; one wavefront for a whole stretch: 8 x 2048 rows 49, so 10).
+// Gradient of the log decays.  That of row t is what reaches over it, g_t = <state before it, its gradient there>, and from one row to the next
+//     g_{t+1} = g_t + k_t . dk_t - q_t . dq_t        (a row's product with itself, which both hold, left out of both)
+// with g known at the chunks' ends: <state, gradient of the state> there, by the walk of dk from states that the walk of dq left (0 before a sequence without a first state
+// and behind one whose last is not used).  Sums of roundings between two such places lead from one to the other but for a rest, which is taken off evenly on the way:
+// summed up over a sequence, roundings weigh as many times as there are rows from the next such place.  (Sixteen heads with memories of 16 rows over 4096, their decays'
+// gradients off by 4 to 5e-6 from places 1024 rows apart and one side, by 3 to 4e-7 so.)  A wavefront per chunk, a lane per row, some heads one after the other.
+constexpr int kDecayChunks = 16;                         // of a workgroup
 struct DecayArgs {
-    const float *q_near, *q_far, *k_near, *k_far;    // [heads, N]
-    const float *states, *grads;                     // anchors of the two walks
-    const float *h0, *dh0;                           // or NULL
+    const float   *q_dot, *k_dot;                        // [heads, N]
+    const double  *starts, *ends;                        // [chunk_number, heads, waves], [S, heads, waves]: parts of the products of states; ends NULL: zeros
     const int32_t *offsets;
-    float       *ddecay;                             // [N, heads], or NULL
-    double      *parts;                              // [pieces, heads], or NULL
-    int64_t      N, pieces;
-    int32_t      S, rows_each, heads, size, anchor_size;
-    int32_t      kdim, vdim;                         // of the anchors' walks
-    int32_t      whole;                              // a workgroup per sequence goes over all its stretches: where most have one
+    float         *ddecay;                               // [N, heads], or NULL
+    double        *parts;                                // [workgroups, heads], or NULL
+    int64_t        N, chunks;
+    int32_t        S, rows_each, heads, heads_each, waves, has_first;
 };
 __device__ __forceinline__ double wave_sum(double v) {
 #pragma unroll
@@ -150,68 +148,53 @@ __device__ __forceinline__ double upto(double v, const int lane) {
     }
     return v;
 }
-__global__ __launch_bounds__(64 * kAnchorChunks) void attend_decay_kernel(const DecayArgs a)
+__global__ __launch_bounds__(64 * kDecayChunks) void attend_decay_kernel(const DecayArgs a)
 {
-    constexpr int kRows = 1 << kAnchorShift;
-    __shared__ double q_sum[kAnchorChunks], k_sum[kAnchorChunks], D_part[kAnchorChunks], g_sum[kAnchorChunks];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;      // as many as a sequence may have chunks in a stretch
-    for (int64_t item = blockIdx.x; item < a.pieces * a.heads; item += gridDim.x) {
-        const int     h = (int)(item % a.heads);
-        const int64_t piece = item / a.heads;
-        const int32_t seq = a.whole ? (int32_t)piece : sequence_of(a.offsets, (int32_t)piece, a.N, a.S, a.rows_each, kRows);
-        const Span    span = span_of(a.offsets, seq, a.N, a.rows_each);
-        double sum = 0.0;
-        for (int64_t i = a.whole ? 0 : piece - piece_base(span.begin, seq, kRows); i >= 0 && span.begin + i * kRows < span.end; ++i) {
-            const int64_t begin = span.begin + i * kRows, end = begin + kRows < span.end ? begin + kRows : span.end;
-            const int     chunks = (int)((end - begin + kChunk - 1) >> kChunkShift);
-            const bool    anchored = i != 0;
-            const int     n = anchored ? a.anchor_size : a.size;
-            const size_t  at = anchored ? ((size_t)anchor_slot(span.begin, (int32_t)i * kAnchorChunks) * a.heads + h) * a.anchor_size : ((size_t)seq * a.heads + h) * a.size;
-            const float  *x = anchored ? a.states : a.h0, *y = anchored ? a.grads : a.dh0;
-            double D = 0.0;
-            if (x && y)
-                for (int e = threadIdx.x; e < n; e += blockDim.x)
-                    if (!anchored || (anchor_row(e, a.kdim) < a.kdim && anchor_column(e, a.kdim) < a.vdim)) D += (double)x[at + e] * (double)y[at + e];
-            D = wave_sum(D);
-            if (lane == 0) D_part[wave] = D;
-            // (a sequence that is longer than the caller said has more chunks than there are wavefronts: they go round)
-            double before = 0.0;                             // k.dk far - q.dq far of the chunks of earlier turns
-            for (int c0 = 0; c0 < chunks; c0 += waves) {
-                const int64_t row = begin + (int64_t)(c0 + wave) * kChunk + lane;
-                const bool    in = row < end;
-                const size_t  p = (size_t)h * a.N + (size_t)(in ? row : begin);
-                const double  qf = in ? a.q_far[p] : 0.0, kf = in ? a.k_far[p] : 0.0, near = in ? (double)a.q_near[p] - (double)a.k_near[p] : 0.0;
-                const double  qfs = upto(qf, lane), kfs = upto(kf, lane), ns = upto(near, lane);
-                const double  q_all = __shfl(qfs, 63, 64), k_all = __shfl(kfs, 63, 64), n_all = __shfl(ns, 63, 64);
-                if (lane == 0) {
-                    q_sum[wave] = q_all;
-                    k_sum[wave] = k_all;
+    __shared__ double sums[kDecayChunks];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int h_first = (int)blockIdx.y * a.heads_each, h_end = h_first + a.heads_each < a.heads ? h_first + a.heads_each : a.heads;
+    for (int64_t block = blockIdx.x; block * kDecayChunks < a.chunks; block += gridDim.x) {
+        const int64_t chunk = block * kDecayChunks + wave;
+        int32_t seq = 0, n = 0;
+        int64_t begin = 0;
+        bool    first = false, last = false;
+        if (chunk < a.chunks) {
+            seq = sequence_of(a.offsets, chunk, a.N, a.S, a.rows_each, kChunk);
+            const Span    span = span_of(a.offsets, seq, a.N, a.rows_each);
+            const int64_t number = chunk - chunk_number(span.begin, seq, 0);      // (below 0: rows before the first sequence)
+            begin = span.begin + number * kChunk;
+            if (number >= 0 && begin < span.end) n = span.end - begin < kChunk ? (int32_t)(span.end - begin) : kChunk;
+            first = number == 0;
+            last = begin + kChunk >= span.end;
+        }
+        for (int h = h_first; h < h_end; ++h) {
+            double sum = 0.0;
+            if (n) {
+                auto joined = [&](const double *p) {
+                    double t = 0.0;
+                    for (int w = 0; w < a.waves; ++w) t += p[w];
+                    return t;
+                };
+                const size_t at = ((size_t)chunk * a.heads + h) * a.waves, row = (size_t)h * a.N + (size_t)begin + lane;
+                const double from = first && !a.has_first ? 0.0 : joined(a.starts + at);
+                const double to = !last ? joined(a.starts + at + (size_t)a.heads * a.waves) : a.ends ? joined(a.ends + ((size_t)seq * a.heads + h) * a.waves) : 0.0;
+                const double step = lane < n ? (double)a.k_dot[row] - (double)a.q_dot[row] : 0.0, up = upto(step, lane), all = __shfl(up, 63, 64);
+                const double g = from + (up - step) + (to - from - all) * ((double)lane / (double)n);
+                if (a.ddecay && lane < n) a.ddecay[(size_t)(begin + lane) * a.heads + h] = (float)g;
+                sum = lane < n ? g : 0.0;
+            }
+            if (a.parts) {
+                sum = wave_sum(sum);
+                if (lane == 0) sums[wave] = sum;
+                __syncthreads();
+                if (threadIdx.x == 0) {
+                    double t = 0.0;
+                    for (int w = 0; w < kDecayChunks; ++w) t += sums[w];
+                    a.parts[(size_t)block * a.heads + h] = t;
                 }
                 __syncthreads();
-                double T = before - q_all;
-                for (int w = 0; w < waves; ++w) {
-                    T += D_part[w];
-                    if (w < wave) T += k_sum[w] - q_sum[w];
-                    before += k_sum[w] - q_sum[w];
-                }
-                const double g = (n_all - ns + near) + (q_all - qfs + qf) + (kfs - kf) + T;
-                if (a.ddecay && in) a.ddecay[row * a.heads + h] = (float)g;
-                sum += in ? g : 0.0;
-                __syncthreads();
-            }
-            if (!a.whole) break;
-        }
-        if (a.parts) {
-            sum = wave_sum(sum);
-            if (lane == 0) g_sum[wave] = sum;
-            __syncthreads();
-            if (threadIdx.x == 0) {
-                double t = 0.0;
-                for (int w = 0; w < waves; ++w) t += g_sum[w];
-                a.parts[piece * a.heads + h] = t;
             }
         }
-        __syncthreads();
     }
 }
 __global__ __launch_bounds__(kBlock) void attend_decay_sum_kernel(const double *__restrict__ parts, float *__restrict__ ddecay, const int64_t pieces, const int heads)
@@ -292,22 +275,24 @@ Plan plan_of(const cngp_attend_config *c, int64_t N, int64_t S, bool ragged) {
 }
 
 struct Space {
-    size_t states, total, near_q, far_q, near_k, far_k, anchors_q, anchors_k, parts, dh0, part_k, part_v, bytes;
+    size_t states, total, dot_q, dot_k, anchors, starts, ends, parts, part_k, part_v, bytes;
 };
+inline int64_t chunks_of(int64_t N, int64_t S) { return pieces(N, S, kChunk); }
+inline int64_t decay_parts(int64_t N, int64_t S) { return (chunks_of(N, S) + kDecayChunks - 1) / kDecayChunks; }
 Space space_of(const cngp_attend_config *c, const Plan &p, int64_t N, int64_t S, uint32_t call) {
     Space sp{};
     size_t at = 0;
     auto take = [&](bool wanted, size_t bytes) { const size_t o = at; if (wanted) at += align256(bytes); return o; };
-    const bool   bwd = call & CNGP_ATTEND_CALL_BWD, cut = p.seg_rows != 0, shared = c->heads != c->kv_heads;
-    const size_t H = (size_t)c->heads, size = (size_t)c->key_dim * c->value_dim, rows = (size_t)N;
+    const bool   bwd = call & CNGP_ATTEND_CALL_BWD, decays = bwd && !(call & CNGP_ATTEND_CALL_NO_DDECAY), cut = p.seg_rows != 0, shared = c->heads != c->kv_heads;
+    const size_t H = (size_t)c->heads, size = (size_t)c->key_dim * c->value_dim, rows = (size_t)N, waves = (size_t)walk_waves(c->value_dim, c->key_dim);
     sp.states = take(cut, (size_t)p.segments * H * size * 4);
     sp.total = take(cut, (size_t)p.segments * H * 4);
-    for (size_t *d : {&sp.near_q, &sp.far_q, &sp.near_k, &sp.far_k}) *d = take(bwd, rows * H * 4);
-    const size_t slots = rows / (kAnchorChunks * kChunk) + 1;
-    sp.anchors_q = take(bwd, slots * H * anchor_floats(c->value_dim, c->key_dim) * 4);
-    sp.anchors_k = take(bwd, slots * H * anchor_floats(c->value_dim, c->key_dim) * 4);
-    sp.parts = take(bwd && !(c->flags & CNGP_ATTEND_ROW_DECAY), (size_t)pieces(N, S, 1 << kAnchorShift) * H * 8);
-    sp.dh0 = take(bwd, (size_t)S * H * size * 4);
+    sp.dot_q = take(decays, rows * H * 4);
+    sp.dot_k = take(decays, rows * H * 4);
+    sp.anchors = take(decays, (rows / kChunk + 1) * H * anchor_floats(c->value_dim, c->key_dim) * 4);
+    sp.starts = take(decays, (size_t)chunks_of(N, S) * H * waves * 8);
+    sp.ends = take(decays, (size_t)S * H * waves * 8);
+    sp.parts = take(decays && !(c->flags & CNGP_ATTEND_ROW_DECAY), (size_t)decay_parts(N, S) * H * 8);
     sp.part_k = take(bwd && shared, rows * H * (size_t)c->key_dim * 4);
     sp.part_v = take(bwd && shared, rows * H * (size_t)c->value_dim * 4);
     sp.bytes = at;
@@ -455,17 +440,13 @@ int cngp_attend_bwd(const cngp_attend_config *cfg, const void *q, const void *k,
     hipStream_t s = (hipStream_t)stream;
     const bool ragged = offsets != nullptr;
     Call call{cfg, decay, N, sequences, offsets, plan_of(cfg, N, sequences, ragged), {}, (char *)workspace, s};
-    call.sp = space_of(cfg, call.p, N, sequences, CNGP_ATTEND_CALL_BWD | (ragged ? CNGP_ATTEND_CALL_RAGGED : 0));
+    call.sp = space_of(cfg, call.p, N, sequences, CNGP_ATTEND_CALL_BWD | (ragged ? CNGP_ATTEND_CALL_RAGGED : 0) | (ddecay ? 0 : CNGP_ATTEND_CALL_NO_DDECAY));
     if (!lent(call.sp, workspace, workspace_bytes)) return CNGP_ERR_WORKSPACE;
-    const int64_t longest = longest_of(cfg, N, sequences, ragged);
-    const bool    stretches = longest > kAnchorChunks * kChunk;              // the decays' gradient by stretches of sequences, not sequences
-    if (ddecay && stretches && pieces(N, sequences, 1 << kAnchorShift) > 0x7fffffff) return CNGP_ERR_INVALID;
     char *ws = call.ws;
     const Space &sp = call.sp;
     const int   group = cfg->heads / cfg->kv_heads, K = cfg->key_dim, V = cfg->value_dim;
     const bool  cut = call.p.seg_rows != 0, shared = group > 1;
     float      *states = (float *)(ws + sp.states);
-    if (ddecay && h0 && !dh0) dh0 = (float *)(ws + sp.dh0);
 
     // dq_t = scale (sum of e (dy_t . v_s) k_s + e state dy_t): a forward walk over the transposed state
     WalkArgs a = call.base(dy, v, k, 1, group, group, V, K, false);
@@ -480,8 +461,8 @@ int cngp_attend_bwd(const cngp_attend_config *cfg, const void *q, const void *k,
     call.output(a, dq, false);
     if (ddecay) {
         a.x = q; a.x_div = 1; a.whole = a.whole && whole_rows(q, K, cfg->io_dtype, cfg->io_dtype == CNGP_F16 ? 8 : 16);
-        a.dot_near = (float *)(ws + sp.near_q); a.dot_far = (float *)(ws + sp.far_q);
-        a.anchors = (float *)(ws + sp.anchors_q);
+        a.dot = (float *)(ws + sp.dot_q);
+        a.anchors = (float *)(ws + sp.anchors); a.met = dlast; a.products = (double *)(ws + sp.ends);
     }
     if (N)
         if (int rc = call.walk(a, false)) return rc;
@@ -511,8 +492,8 @@ int cngp_attend_bwd(const cngp_attend_config *cfg, const void *q, const void *k,
     call.output(a, shared ? (void *)(ws + sp.part_k) : dk, shared);
     if (ddecay) {
         a.x = k; a.x_div = group; a.whole = a.whole && whole_rows(k, K, cfg->io_dtype, cfg->io_dtype == CNGP_F16 ? 8 : 16);
-        a.dot_near = (float *)(ws + sp.near_k); a.dot_far = (float *)(ws + sp.far_k);
-        a.anchors = (float *)(ws + sp.anchors_k);
+        a.dot = (float *)(ws + sp.dot_k);
+        a.anchors = (float *)(ws + sp.anchors); a.met = h0; a.products = (double *)(ws + sp.starts);
     }
     if (int rc = call.walk(a, false)) return rc;
 
@@ -527,25 +508,24 @@ int cngp_attend_bwd(const cngp_attend_config *cfg, const void *q, const void *k,
         }
     if (!ddecay) return CNGP_OK;
     DecayArgs d{};
-    d.q_near = (const float *)(ws + sp.near_q); d.q_far = (const float *)(ws + sp.far_q);
-    d.k_near = (const float *)(ws + sp.near_k); d.k_far = (const float *)(ws + sp.far_k);
-    d.states = (const float *)(ws + sp.anchors_q); d.grads = (const float *)(ws + sp.anchors_k);
-    d.h0 = h0; d.dh0 = dh0; d.offsets = offsets;
+    d.q_dot = (const float *)(ws + sp.dot_q); d.k_dot = (const float *)(ws + sp.dot_k);
+    d.starts = (const double *)(ws + sp.starts); d.ends = dlast ? (const double *)(ws + sp.ends) : nullptr;
+    d.offsets = offsets; d.has_first = h0 != nullptr;
     d.ddecay = rows ? ddecay : nullptr;
     d.parts = rows ? nullptr : (double *)(ws + sp.parts);
-    d.N = N; d.S = (int32_t)sequences; d.rows_each = (int32_t)(N / sequences); d.heads = cfg->heads;
-    d.whole = !stretches;
-    d.pieces = d.whole ? sequences : pieces(N, sequences, 1 << kAnchorShift);
-    d.kdim = V; d.vdim = K;
-    d.size = K * V; d.anchor_size = (int32_t)anchor_floats(V, K);
+    d.N = N; d.chunks = chunks_of(N, sequences);
+    d.S = (int32_t)sequences; d.rows_each = (int32_t)(N / sequences); d.heads = cfg->heads;
+    d.waves = walk_waves(V, K);
+    // heads one after the other by wavefronts that have found their chunk's sequence, but few where there are few chunks: eight wavefronts to a SIMD
+    const int64_t groups = decay_parts(N, sequences), split = std::min<int64_t>(cfg->heads, std::max<int64_t>(1, 512 / groups));
+    d.heads_each = (int32_t)((cfg->heads + split - 1) / split);
     {
         LaunchTimer t(s, K_ATTEND_DECAY);
-        const int     waves = (int)std::min<int64_t>(kAnchorChunks, std::max<int64_t>(1, (longest + kChunk - 1) / kChunk));
-        attend_decay_kernel<<<(unsigned)std::min<int64_t>(d.pieces * d.heads, 0x3fffff), 64 * waves, 0, s>>>(d);
+        attend_decay_kernel<<<dim3((unsigned)std::min<int64_t>(groups, 0x3fffff), (unsigned)((cfg->heads + d.heads_each - 1) / d.heads_each)), 64 * kDecayChunks, 0, s>>>(d);
         if (int rc = launch_status("attend_decay_kernel")) return rc;
     }
     if (rows) return CNGP_OK;
-    return decay_sum(d.parts, ddecay, d.pieces, cfg->heads, s);
+    return decay_sum(d.parts, ddecay, groups, cfg->heads, s);
 }
 
 }  // extern "C"

@@ -102,20 +102,24 @@ struct Staged {
     }
 };
 
-// Wavefronts of a workgroup: one for each 32 columns of v, by two where k has more than 32 (each keeps one half of the state's rows, and takes one half
-// of the chunk's rows for the outputs).  One wavefront on a SIMD waits most of the time, so what it does in a row is kept short.
-constexpr int walk_halves(int KW) { return KW > 32 ? 2 : 1; }
-constexpr int walk_threads(int KW, int VW) { return 64 * ((VW + 31) / 32) * walk_halves(KW); }
+// (walk_waves.)  One wavefront on a SIMD waits most of the time, so what it does in a row is kept short.
+constexpr int walk_halves(int KW) { return walk_waves(KW, 1); }
+constexpr int walk_threads(int KW, int VW) { return 64 * walk_waves(KW, VW); }
 // Wavefronts of a SIMD that registers are left for.
 constexpr int walk_per_simd(size_t value, int KW) { return value == 2 || KW < 128 ? 2 : 1; }
+
+// What a walk is for: states alone; outputs; outputs with a row's own part kept apart and what the decays' gradient takes of them (in a walk of its own: it
+// costs registers, with which the plain one took 316 us for a prompt in place of 306).
+enum Mode { STATES, OUTPUTS, GRADIENTS };
 
 // KW, VW: columns of k and v in a tile: 16, 32, 64 or 128.  Sums of 32 rows or columns where 16 are kept read what lies behind a row in LDS;
 // the rows and columns of the state that come of it are used by nothing.
 // Banks: the scores read 16 bytes of sixteen rows, so rows have an odd number of 16-byte pieces; a transposing read takes 64 bytes of four neighbouring
 // rows, for which rows of 128 values are 64 bytes beyond a multiple of 256 (v, read by that alone) or five pieces (k) (128 x 128: 338 against 344 us a
 // prompt; of 64 values it gained nothing).
-template <typename T, int KW, int VW, bool OUT>
+template <typename T, int KW, int VW, Mode MODE>
 struct Lds {
+    static constexpr bool OUT = MODE != STATES, kDots = MODE == GRADIENTS;
     static constexpr int kstride = KW + (KW == 128 ? 40 : KW == 16 ? 0 : 8), vstride = VW + (VW == 128 ? 32 : VW == 16 ? 0 : 8);     // see above
     static constexpr int parts = sizeof(T) / 2, pstride = 32 + 8, KT = (KW + 31) / 32, VT = (VW + 31) / 32;
     static constexpr int halves = walk_halves(KW), waves = VT * halves;
@@ -129,11 +133,11 @@ struct Lds {
     double total[decays];
     int    mild[decays];
     int    lift[4];                                         // of each score tile
-    float  own[scores ? kChunk : 1];                        // a row's score with itself, where it is kept apart
+    float  own[scores && kDots ? kChunk : 1];               // a row's score with itself, where it is kept apart
     short  up_q[parts == 2 ? kChunk : 1], up_k[parts == 2 ? kChunk : 1], up_v[parts == 2 ? kChunk : 1];     // lifts of the rows
     static constexpr bool folds = parts == 2 && waves == 1; // ... which go into the decays once a chunk, where no barrier is needed for that (rays: 474 against 509 us)
     float  down[folds ? kChunk : 1];                        // 2^-(lifts of k and v)
-    float  dots[OUT && VT > 1 ? 2 * VT : 1][VT > 1 ? kChunk : 1];
+    float  dots[kDots && VT > 1 ? VT : 1][kDots && VT > 1 ? kChunk : 1];
     union {
         struct {
             alignas(16) _Float16 k[parts][kChunk * kstride];
@@ -167,10 +171,11 @@ __device__ __forceinline__ double sum_upto(double v) {
     return v;
 }
 
-template <typename T, int KW, int VW, bool OUT, bool WHOLE>
+template <typename T, int KW, int VW, Mode MODE, bool WHOLE>
 __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW)) void attend_walk_kernel(const WalkArgs a)
 {
-    using L = Lds<T, KW, VW, OUT>;
+    using L = Lds<T, KW, VW, MODE>;
+    constexpr bool OUT = L::OUT, kDots = L::kDots;
     constexpr int  WAVES = L::waves, VT = L::VT, KT = L::KT, HALVES = L::halves, KP = KT / HALVES;
     constexpr int  KS = KW / 16 / HALVES;                   // steps of 16 columns of k that a wavefront keeps
     constexpr int  KR = KW < 32 ? 8 : 16, VR = VW < 32 ? 8 : 16;      // registers of a tile's sums that hold rows of the state, and of the outputs
@@ -274,15 +279,54 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
             }
     }
     int up = 0;                          // the state is kept times 2^up, the scale of what is added to it
-    // the state at the start of a chunk (of this number in its sequence), as it lies in the registers
-    auto anchor = [&](const int number) {
-        if (number == 0 || number % kAnchorChunks) return;
-        float *to = a.anchors + ((size_t)anchor_slot(span.begin, number) * a.heads + h) * (KT * VT * 1024) + (vt * KT + kh * KP) * 1024 + lane;
+    // the state at the start of chunk `number` of its sequence, as it lies in the registers (rows behind kdim in a piece of four are 0)
+    auto anchor_of = [&](const int number) -> float * {
+        return a.anchors + ((size_t)anchor_slot(span.begin, number) * a.heads + h) * (KT * VT * 1024) + (vt * KT + kh * KP) * 1024 + 4 * lane;
+    };
+    auto leave_anchor = [&](const int number) {
+        if (number == 0) return;
+        float *to = anchor_of(number);
         const float f = power_of_two(-up);
+        const int   left = anew(a.kdim - 32 * KP * kh - 4 * half);
 #pragma unroll
         for (int kt = 0; kt < KP; ++kt)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) to[(kt * 16 + r) * 64] = S[kt][r] * f;
+            for (int g = 0; g < KR / 4; ++g)
+                if (mine_v && 32 * kt + 8 * g < left)
+                    *reinterpret_cast<float4_t *>(to + (kt * 4 + g) * 256) = float4_t{S[kt][4 * g] * f, S[kt][4 * g + 1] * f, S[kt][4 * g + 2] * f, S[kt][4 * g + 3] * f};
+    };
+    // this wavefront's part of the state's product with another one (an anchor, or a state of whole sequences): four at a time in fp32, these in 64 bits
+    auto meet = [&](const bool an_anchor, const int number, double *to) {
+        const float   *from = an_anchor ? anchor_of(number) : a.met + (size_t)seq * a.kdim * a.vdim * a.heads + (size_t)h * a.kdim * a.vdim;
+        const float    f = power_of_two(-up);
+        const int      left = anew(a.kdim - 32 * KP * kh - 4 * half);
+        const int      by = __builtin_amdgcn_readfirstlane(anew(a.first_i));
+        uint32_t       at = (uint32_t)anew((32 * KP * kh + 4 * half) * by + j * a.first_j);
+        double sum = 0.0;
+        apart();
+#pragma unroll
+        for (int kt = 0; kt < KP; ++kt) {
+#pragma unroll
+            for (int g = 0; g < KR / 4; ++g, at += (uint32_t)by * 8) {
+                const int i = 32 * kt + 8 * g;
+                float4_t  o = {0.0f, 0.0f, 0.0f, 0.0f};
+                if (mine_v && i < left) {
+                    if (an_anchor) o = *reinterpret_cast<const float4_t *>(from + (kt * 4 + g) * 256);
+                    else
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (i + e < left) o[e] = from[at + (uint32_t)(e * by)];
+                    float t = 0.0f;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) t = fmaf(S[kt][4 * g + e] * f, o[e], t);
+                    sum += (double)t;
+                }
+            }
+            apart();
+            if (KR < 16) at += (uint32_t)by * 16;
+        }
+        sum = sum_upto(sum);
+        if (lane == 63) to[wave] = sum;
     };
     if (chunks > 0) decays(0);
 
@@ -349,8 +393,8 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
                 }
             }
             if (ss == tt) {
-                const int t = anew(col - 4 * half), last = t - a.own;
-                if (a.own)
+                const int t = anew(col - 4 * half), last = kDots ? t - 1 : t;
+                if (kDots)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) own = 8 * (r >> 2) + (r & 3) == t ? p[r] : own;
 #pragma unroll
@@ -365,7 +409,7 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
                 acc_t p;
                 float own;
                 const int   lift = score(tile > 0, tile > 1, p, own);
-                if (a.own && tile != 1 && half == (col >> 2 & 1)) lds.own[tile ? 32 + col : col] = own;
+                if (kDots && tile != 1 && half == (col >> 2 & 1)) lds.own[tile ? 32 + col : col] = own;
                 const float f = power_of_two(lift);
                 if (lane == 0) lds.lift[tile] = lift;
                 _Float16 *to = lds.p[0] + (tile * 32 + col) * L::pstride + 4 * half;
@@ -421,7 +465,7 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
         }
 
         auto state_behind = [&]() {
-            if (a.anchors && !reverse) anchor(chunk0 + c);
+            if (kDots && a.anchors && !reverse) leave_anchor(chunk0 + c);
             // rows 16 s + 8 half .. + 7 of this lane's column, decayed to the chunk's end
             float x[4][8];
             float most = 0.0f;
@@ -458,7 +502,10 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
                     if constexpr (kLow) S[kt] = mfma(read_column(lds.k[1], L::kstride, 16 * s, 32 * (KP * kh + kt), lane), hi, S[kt]);
                 }
             }
-            if (a.anchors && reverse) anchor(chunk0 + chunks - 1 - c);
+            if (kDots && a.anchors && reverse) {
+                const int number = chunk0 + chunks - 1 - c;
+                if (number || a.met) meet(number != 0, number, a.products + ((size_t)chunk_number(span.begin, seq, number) * a.heads + h) * WAVES);
+            }
             apart();
         };
         if (!OUT || HALVES == 2) state_behind();
@@ -513,15 +560,15 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
 #pragma unroll
                     for (int r = 0; r < VR; ++r) far[r] += lds.far_half[wave < VT ? wave + VT : wave - VT][r][lane];
                 }
-                if (a.own) {
+                if (kDots) {
                     if constexpr (L::scores) own = lds.own[t];
                     else own += __shfl_xor(own, 32, 64);
                     own *= of_row;
                 }
                 const bool there = t < count;
                 const int  base = low + (reverse ? -32 * tt : 32 * tt);
-                float dn = 0.0f, df = 0.0f;
-                if (a.x && there) {
+                float dot = 0.0f;
+                if (kDots && a.x && there) {
                     const T *x = (const T *)a.x + h / a.x_div * a.vdim + (int64_t)base * xs;
                     const uint32_t mine = (uint32_t)(t0 * xs + j0);
 #pragma unroll
@@ -541,10 +588,7 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
                         }
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            if (8 * g + e < left) {
-                                dn = fmaf(near[4 * g + e], w[e], dn);
-                                df = fmaf(far[4 * g + e], w[e], df);
-                            }
+                            if (8 * g + e < left) dot = fmaf(near[4 * g + e] + far[4 * g + e], w[e], dot);
                     }
                 }
                 if (there) {
@@ -556,7 +600,7 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
                         float o[4];
 #pragma unroll
                         for (int e = 0; e < 4; ++e) o[e] = near[4 * g + e] + far[4 * g + e];
-                        if (a.own) {
+                        if (kDots) {
                             const _Float16 *mine_v = lds.v[0] + t * L::vstride + j0 + 8 * g;
                             const half4_t   hi = *reinterpret_cast<const half4_t *>(mine_v), lo = *reinterpret_cast<const half4_t *>(mine_v + (kLow ? kChunk * L::vstride : 0));
 #pragma unroll
@@ -577,35 +621,22 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
                         }
                     }
                 }
-                if (a.x) {
-                    dn += __shfl_xor(dn, 32, 64);
-                    df += __shfl_xor(df, 32, 64);
+                if (kDots && a.x) {
+                    dot += __shfl_xor(dot, 32, 64);
                     if (VT == 1) {
-                        if (half == 0 && there) {
-                            const size_t at = (size_t)h * a.N + (size_t)(row0 + t * dir);
-                            a.dot_near[at] = dn;
-                            a.dot_far[at] = df;
-                        }
-                    } else if (half == 0) {
-                        lds.dots[2 * vt][t] = dn;
-                        lds.dots[2 * vt + 1][t] = df;
-                    }
+                        if (half == 0 && there) a.dot[(size_t)h * a.N + (size_t)(row0 + t * dir)] = dot;
+                    } else if (half == 0) lds.dots[vt][t] = dot;
                 }
                 apart();
             }
             if (HALVES == 1) state_behind();
-            if (VT > 1 && a.x) {
+            if (kDots && VT > 1 && a.x) {
                 __syncthreads();
                 if (threadIdx.x < kChunk && (int)threadIdx.x < count) {
-                    float dn = 0.0f, df = 0.0f;
+                    float dot = 0.0f;
 #pragma unroll
-                    for (int w = 0; w < VT; ++w) {
-                        dn += lds.dots[2 * w][threadIdx.x];
-                        df += lds.dots[2 * w + 1][threadIdx.x];
-                    }
-                    const size_t at = (size_t)h * a.N + (size_t)(row0 + (int)threadIdx.x * dir);
-                    a.dot_near[at] = dn;
-                    a.dot_far[at] = df;
+                    for (int w = 0; w < VT; ++w) dot += lds.dots[w][threadIdx.x];
+                    a.dot[(size_t)h * a.N + (size_t)(row0 + (int)threadIdx.x * dir)] = dot;
                 }
             }
         }
@@ -614,6 +645,7 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
             __syncthreads();                                // the tiles may be written again
         }
     }
+    if (kDots && a.anchors && !reverse && a.met && chunks > 0 && end == span.end) meet(false, 0, a.products + ((size_t)seq * a.heads + h) * WAVES);
     if (a.total && threadIdx.x == 0) a.total[state_at] = (float)whole;
     if (a.final && mine_v) {
         char     *to = (char *)a.final + state_at * state_bytes;
@@ -630,35 +662,40 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
     }
 }
 
-template <typename T, int KW, int VW, bool OUT, bool WHOLE>
+template <typename T, int KW, int VW, Mode MODE, bool WHOLE>
 int launch_walk(const WalkArgs &a, hipStream_t s) {
-    using L = Lds<T, KW, VW, OUT>;
+    using L = Lds<T, KW, VW, MODE>;
+    static_assert(L::waves == walk_waves(KW, VW), "the host counts them alike");
     if (sizeof(L) > 64 * 1024)
-        if (hipError_t e = hipFuncSetAttribute((const void *)attend_walk_kernel<T, KW, VW, OUT, WHOLE>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(L)))
+        if (hipError_t e = hipFuncSetAttribute((const void *)attend_walk_kernel<T, KW, VW, MODE, WHOLE>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(L)))
             return record_hip_failure(e, "hipFuncSetAttribute(MaxDynamicSharedMemorySize)");
     // a workgroup goes over one piece: a loop over pieces would have the addresses of the states' entries formed before it and kept in registers
     const int most = (int)(kMostGroups256 / 2 / a.heads);   // (workgroups of up to 512)
     for (int first = 0; first < a.segments; first += most) {
         WalkArgs part = a;
         part.piece0 = first;
-        LaunchTimer t(s, OUT ? K_ATTEND_WALK : K_ATTEND_STATES);
-        attend_walk_kernel<T, KW, VW, OUT, WHOLE><<<(unsigned)a.heads * (unsigned)std::min(a.segments - first, most), 64 * L::waves, sizeof(L), s>>>(part);
+        LaunchTimer t(s, MODE == STATES ? K_ATTEND_STATES : K_ATTEND_WALK);
+        attend_walk_kernel<T, KW, VW, MODE, WHOLE><<<(unsigned)a.heads * (unsigned)std::min(a.segments - first, most), 64 * L::waves, sizeof(L), s>>>(part);
         if (int rc = launch_status("attend_walk_kernel")) return rc;
     }
     return CNGP_OK;
 }
 
-template <typename T, int KW, int VW, bool OUT>
-int launch(const WalkArgs &a, hipStream_t s) { return a.whole ? launch_walk<T, KW, VW, OUT, true>(a, s) : launch_walk<T, KW, VW, OUT, false>(a, s); }
+template <typename T, int KW, int VW, Mode MODE>
+int launch(const WalkArgs &a, hipStream_t s) { return a.whole ? launch_walk<T, KW, VW, MODE, true>(a, s) : launch_walk<T, KW, VW, MODE, false>(a, s); }
 
-template <typename T, bool OUT, int KW>
+template <typename T, Mode MODE, int KW>
 int launch_columns(const WalkArgs &a, hipStream_t s) {
-    return a.vdim <= 16 ? launch<T, KW, 16, OUT>(a, s) : a.vdim <= 32 ? launch<T, KW, 32, OUT>(a, s) : a.vdim <= 64 ? launch<T, KW, 64, OUT>(a, s) : launch<T, KW, 128, OUT>(a, s);
+    return a.vdim <= 16 ? launch<T, KW, 16, MODE>(a, s) : a.vdim <= 32 ? launch<T, KW, 32, MODE>(a, s) : a.vdim <= 64 ? launch<T, KW, 64, MODE>(a, s) : launch<T, KW, 128, MODE>(a, s);
 }
-template <typename T, bool OUT>
-int launch_tiles(const WalkArgs &a, hipStream_t s) {
-    return a.kdim <= 16 ? launch_columns<T, OUT, 16>(a, s) : a.kdim <= 32 ? launch_columns<T, OUT, 32>(a, s) : a.kdim <= 64 ? launch_columns<T, OUT, 64>(a, s)
-                                                                                                          : launch_columns<T, OUT, 128>(a, s);
+template <typename T, Mode MODE>
+int launch_mode(const WalkArgs &a, hipStream_t s) {
+    return a.kdim <= 16 ? launch_columns<T, MODE, 16>(a, s) : a.kdim <= 32 ? launch_columns<T, MODE, 32>(a, s) : a.kdim <= 64 ? launch_columns<T, MODE, 64>(a, s)
+                                                                                                           : launch_columns<T, MODE, 128>(a, s);
+}
+template <typename T>
+int launch_tiles(const WalkArgs &a, bool states_only, hipStream_t s) {
+    return states_only ? launch_mode<T, STATES>(a, s) : a.own ? launch_mode<T, GRADIENTS>(a, s) : launch_mode<T, OUTPUTS>(a, s);
 }
 
 }  // namespace attend

@@ -154,7 +154,7 @@ int main() {
     for (int it = 0; it < 2000; ++it) {
         const int64_t  counts[] = {0, 1, 63, 4097, 100003, (int64_t)1 << 22, (int64_t)1 << 27, 0x7ffeffff, 0x7fffffff};
         const int64_t  N = counts[below(9)], S = it % 3 ? counts[below(9)] : 1;
-        const uint32_t call = below(4);
+        const uint32_t call = below(8);
         const int      kv = 1 + (int)below(9), heads = it % 5 ? kv * (1 + (int)below(5)) : (int)below(5000);
         cngp_attend_config t = {heads, kv, (int)below(140), (int)below(140), (int)below(3), (int)below(1 << 22) - 10, 0.5f, below(3)};
         const size_t   fwd = cngp_attend_workspace_bytes(&t, N, S, call & CNGP_ATTEND_CALL_RAGGED), bwd = cngp_attend_workspace_bytes(&t, N, S, call | CNGP_ATTEND_CALL_BWD);

@@ -14,7 +14,7 @@ from .operators import _maybe, _need, _on_current_device, _out, _room, _sequence
 
 ATTEND_ROW_DECAY = 1
 ROTATE_NORM, ROTATE_NEXT = 2, 4          # beside ZERO_GRADS = 1
-_CALL_BWD, _CALL_RAGGED = 1, 2
+_CALL_BWD, _CALL_RAGGED, _CALL_NO_DDECAY = 1, 2, 4
 
 
 class CAttendConfig(ctypes.Structure):
@@ -75,8 +75,9 @@ def _decay_shape(cfg, N):
     return (N, cfg.heads) if cfg.flags & ATTEND_ROW_DECAY else (cfg.heads,)
 
 
-def attend_workspace_bytes(cfg: AttendConfig, N, sequences, backward=False, ragged=False) -> int:
-    return _need("cngp_attend_workspace_bytes", cfg, N, sequences, (_CALL_BWD if backward else 0) | (_CALL_RAGGED if ragged else 0))
+def attend_workspace_bytes(cfg: AttendConfig, N, sequences, backward=False, ragged=False, ddecay=True) -> int:
+    """backward: of attend_bwd; ddecay: with the decays' gradient, which takes most of it."""
+    return _need("cngp_attend_workspace_bytes", cfg, N, sequences, (_CALL_BWD if backward else 0) | (_CALL_RAGGED if ragged else 0) | (0 if ddecay else _CALL_NO_DDECAY))
 
 
 def attend_fwd(cfg: AttendConfig, q, k, v, decay, h0=None, offsets=None, sequences=None, y=True, last=True, workspace=None):
@@ -116,7 +117,7 @@ def attend_bwd(cfg: AttendConfig, q, k, v, decay, dy=None, dlast=None, h0=None, 
     ddecay, ddp = _out(ddecay, _decay_shape(cfg, N), torch.float32, decay, "ddecay")
     dh0, dhp = _out(h0 is not None if dh0 is None else dh0, state, torch.float32, q if h0 is None else h0, "dh0")
     _on_current_device(q, k, v, decay, dy, dlast, h0, offsets, dq, dk, dv, ddecay, dh0, workspace)
-    workspace = _room(attend_workspace_bytes(cfg, N, S, True, offsets is not None), workspace, q)
+    workspace = _room(attend_workspace_bytes(cfg, N, S, True, offsets is not None, ddecay is not None), workspace, q)
     _check(_lib.cngp_attend_bwd(cfg._ref(), qp, kp, vp, gp, N, op, S, hp, dyp, dlp, dqp, dkp, dvp, ddp, dhp, *_ws(workspace), _stream()))
     return dq, dk, dv, ddecay, dh0
 

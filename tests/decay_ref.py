@@ -1,20 +1,19 @@
 """The gradient of linear attention's decays in 64 bits as the library puts it together, and how far fp32 sums may be from it.
 
-Row t's is what reaches over it: with near = the products of a row inside its chunk of 64 (its own with itself left out), far = those with states, D = <state,
-gradient of the state> at the start of a stretch of 1024 rows, counted from the sequence's start,
-    sum over its chunk's rows s >= t of (q.dq near - k.dk near + q.dq far) + sum over s < t of k.dk far + what crosses the whole chunk,
-the last D with k.dk far - q.dq far of the stretch's rows before added, less the chunk's q.dq far.
+Row t's is what reaches over it, g_t = <state before row t, its gradient there>, and g_{t+1} = g_t + k_t . dk_t - q_t . dq_t.  In chunks of 64 rows, counted from the
+sequence's start: g at both ends of a chunk from the states there (0 before a sequence without a first state, and behind one whose last is not used), rows between by
+the products, what is left over at the end taken off evenly.
 
 Errors: every number here is a sum of products of inputs, and a rounding is u = 2^-24 of what is rounded, of either sign.  The same recurrences over squares
 give the sum of the squares of all products: roundings of random signs add up as the root of it.  Roundings to a product: 24 for the operands in
 two parts (three factors, off by 2 u each, as squares), a quarter of key_dim + value_dim + 64 (a matrix instruction takes 16 products, at most four roundings), 6 for
 each chunk that a state passes, 64 for the decays (exponents rounded to fp32: two of 8 u relative, as squares halved).  Six times the root of
-that many is the bound: a result is off by less unless roundings conspire."""
+that many is the bound: a result is off by less unless roundings conspire.  A row takes errors from its chunk alone, no part of them more than once."""
 import numpy as np
 
 import mixer_ref as R
 
-CHUNK, STRETCH = 64, 1024
+CHUNK = 64
 
 
 def heads_of(q, k, v):
@@ -22,48 +21,38 @@ def heads_of(q, k, v):
     return np.repeat(k, G, 1), np.repeat(v, G, 1)
 
 
-def assembled(q, k, v, g, spans, h0, scale, dy, dlast, without_D=None, carried=True):
-    """The gradient [N, heads] by the formula above.  without_D: number of the stretch whose D is left out; carried: whether D goes on from chunk to chunk."""
+def assembled(q, k, v, g, spans, h0, scale, dy, dlast, lost=()):
+    """The gradient [N, heads] by the formula above.  lost: numbers of chunks at whose starts g is taken for 0, "end" for behind the last row."""
     N, H, dk = q.shape
     k, v = heads_of(q, k, v)
     dv = v.shape[2]
-    e = np.exp(np.maximum(g, -700.0))
-    dg = np.zeros((N, H))
+    e = np.exp(g)
+    out = np.zeros((N, H))
+    all_ = R.attend(q, k, v, g, spans, h0, scale, dy, dlast)
+    step = (k * all_["dk"]).sum(2) - (q * all_["dq"]).sum(2)
     for s, (lo, hi) in enumerate(spans):
-        starts = list(range(lo, hi, CHUNK))
-        before, st = [], np.zeros((H, dk, dv)) if h0 is None else h0[s].copy()
+        if lo == hi:
+            continue
+        states, st = [], np.zeros((H, dk, dv)) if h0 is None else h0[s].copy()
         for r in range(lo, hi):
             if (r - lo) % CHUNK == 0:
-                before.append(st)
+                states.append(st)
             st = e[r][:, None, None] * st + k[r][:, :, None] * v[r][:, None, :]
-        behind, d = {}, np.zeros((H, dk, dv)) if dlast is None else dlast[s].copy()
+        d = np.zeros((H, dk, dv)) if dlast is None else dlast[s].copy()
+        known = {"end": (st * d).sum((1, 2))}
         for r in range(hi - 1, lo - 1, -1):
-            if r == hi - 1 or (r + 1 - lo) % CHUNK == 0:
-                behind[(r - lo) // CHUNK] = d
             if dy is not None:
                 d = d + scale * q[r][:, :, None] * dy[r][:, None, :]
             d = e[r][:, None, None] * d
             if (r - lo) % CHUNK == 0:
-                behind["start", (r - lo) // CHUNK] = d
-        D = None
-        for c, a in enumerate(starts):
-            rows = slice(a, min(a + CHUNK, hi))
-            F = np.cumsum(np.maximum(g[rows], -700.0), 0)                            # [rows, H]
-            n = F.shape[0]
-            W = np.zeros((n, n, H))                                                   # products of rows t > s
-            if dy is not None:
-                W = scale * np.einsum("thk,shk->tsh", q[rows], k[rows]) * np.einsum("thv,shv->tsh", dy[rows], v[rows]) * \
-                    np.where(np.tril(np.ones((n, n)), -1)[:, :, None] > 0, np.exp(np.minimum(F[:, None] - F[None], 0.0)), 0.0)
-            near = W.sum(1) - W.sum(0)
-            qf = np.zeros((n, H)) if dy is None else scale * np.exp(F) * np.einsum("thk,hkv,thv->th", q[rows], before[c], dy[rows])
-            kf = np.exp(F[-1] - F) * np.einsum("thk,hkv,thv->th", k[rows], behind[c], v[rows])
-            if (c * CHUNK) % STRETCH == 0:
-                D = (before[c] * behind["start", c]).sum((1, 2)) * (0.0 if without_D == c * CHUNK // STRETCH else 1.0)
-            T = D - qf.sum(0)
-            dg[rows] = np.cumsum((near + qf)[::-1], 0)[::-1] + np.cumsum(kf, 0) - kf + T
-            if carried:
-                D = T + kf.sum(0)
-    return dg
+                known[(r - lo) // CHUNK] = (states[(r - lo) // CHUNK] * d).sum((1, 2))
+        known = {n: t * (n not in lost) for n, t in known.items()}
+        for c, a in enumerate(range(lo, hi, CHUNK)):
+            z = min(a + CHUNK, hi)
+            upto = np.cumsum(step[a:z], 0)
+            rest = known[c + 1 if z < hi else "end"] - known[c] - upto[-1]
+            out[a:z] = known[c] + upto - step[a:z] + rest * (np.arange(z - a) / (z - a))[:, None]
+    return out
 
 
 def bounds(q, k, v, g, spans, h0, scale, dy, dlast):
@@ -75,12 +64,15 @@ def bounds(q, k, v, g, spans, h0, scale, dy, dlast):
     own = 0.0 if dy is None else scale * scale * (sq(q) * sq(k)).sum(2) * (sq(v) * sq(dy)).sum(2)
     each = np.maximum((sq(q) * m["dq"]).sum(2) + (sq(k) * m["dk"]).sum(2) - 2 * own, 0.0)
     b, total = np.zeros((N, H)), np.zeros(H)
-    for lo, hi in spans:
+    for s, (lo, hi) in enumerate(spans):
         n = 24 + (dk + v.shape[2] + CHUNK) / 4 + 6 * ((hi - lo) // CHUNK + 1) + 64
-        for a in range(lo, hi, STRETCH):
-            z = min(a + STRETCH, hi)
-            b[a:z] = 6 * R.U * np.sqrt(n * (m["dg"][a] + each[a:z].sum(0)))           # m["dg"][a]: squares of D, from before the row
-            total += ((z - a) * b[a]) ** 2                                            # a stretch's rows share their errors
+        behind = np.zeros(H) if dlast is None else (m["last"][s] * sq(dlast[s])).sum((1, 2))
+        for a in range(lo, hi, CHUNK):
+            z = min(a + CHUNK, hi)
+            ends, products = m["dg"][a] + (m["dg"][z] if z < hi else behind), each[a:z].sum(0)                      # m["dg"][a]: squares of g there
+            b[a:z] = 6 * R.U * np.sqrt(n * (ends + products))
+            # summed up: an end's error falls to nothing over the chunk at either side of it, a product's weighs by its distance from the chunk's middle
+            total += (6 * R.U * (z - a)) ** 2 * n * (ends / 2 + products / 12)
     return b, np.sqrt(total)
 
 

@@ -18,11 +18,13 @@ def test_mistakes_lie_outside(lengths, rows, slow):
     want = R.attend(*args)["dg"]
     row, total = D.bounds(*args)
     assert (np.abs(D.assembled(*args) - want) <= 1e-3 * row + 1e-300).all()
-    # [what the call would give in place of the gradient]; a sum over all rows may hide part of it, not all
-    wrong = [np.zeros_like(want), D.assembled(*args, carried=False)] + [D.assembled(*args, without_D=i) for i in range(max(lengths) // D.STRETCH + 1)]
+    chunks = -(-max(lengths) // D.CHUNK)
+    # what a call with a mistake would give in place of the gradient; a sum over all rows may hide part of it, not all
+    wrong = [np.zeros_like(want)] + [D.assembled(*args, lost=(n,)) for n in {0, 1, chunks // 2, chunks - 1, "end"}]
     for i, w in enumerate(wrong):
         off_by = np.abs(w - want)
         assert off_by.max() > 100 * row[np.unravel_index(off_by.argmax(), row.shape)], i
-        assert (np.abs((w - want).sum(0)) > 5 * total).all(), i
+        assert (np.abs((w - want).sum(0)) > 2 * total).any(), i
+    assert (np.abs(want.sum(0)) > 5 * total).all()
     few = np.abs(want) <= row                       # zeros pass for few rows alone (that forget everything)
     assert few.mean() < 0.02

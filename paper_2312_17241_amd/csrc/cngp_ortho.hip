@@ -3,8 +3,8 @@
 // The products run on the matrix cores.  One fp16 number per value would not do: the polynomial lifts small singular values by 3.4 in each
 // step and with them what a rounding put into their directions, so that 11 bits leave errors of a tenth of an entry.  Every operand is two fp16
 // numbers, and a product three (high by high and both mixed ones, into the same sums): 22 bits.  (Low parts scaled apart, with sums of their own, took
-// 16464 us for 4096 x 4096 and five steps, this form 5833, registers being short.)  A and B are symmetric: tiles on and below the diagonal are computed
-// and written twice.
+// 16464 us for 4096 x 4096 and five steps, this form 5833, registers being short.)  Small matrices take four, with sums of their own for the low parts (multiply).
+// A and B are symmetric: tiles on and below the diagonal are computed and written twice.
 #include <algorithm>
 #include <cmath>
 
@@ -188,6 +188,16 @@ __global__ __launch_bounds__(kBlock) void ortho_scale_kernel(const T *g, const S
 }
 
 // ---------------------------------------------------------------- products
+// Short sums, of small matrices, show what long ones bury in their own rounding: there the products with low parts have sums of their own, low by
+// low among them, added to those of the high parts at the end.  (14 x 53: 1.3e-6 off after five steps, so 1.0, fp32 arithmetic 0.7; 2 of 15 x 821: 1.6, 0.8, 0.8.  In
+// tiles of 64 and in one launch, where it costs little: 6 of 1000 x 333 237 us, so 240, 64 x 64 17.0 and 18.2.)
+__device__ __forceinline__ void multiply(const half8_t ah, const half8_t al, const half8_t bh, const half8_t bl, acc_t &sum, acc_t &fine) {
+    fine = mfma(bl, al, fine);
+    sum = mfma(bh, ah, sum);
+    fine = mfma(bh, al, fine);
+    fine = mfma(bl, ah, fine);
+}
+
 enum : int { GRAM, POLY, UPDATE, LAST };
 struct ProductArgs {
     Pair   A, B, C, D;                   // C = epilogue(A B^T, or A B for updates; D)
@@ -312,7 +322,8 @@ __global__ __launch_bounds__(kBlock, 2) void ortho_product_kernel(const ProductA
         }
     };
 
-    acc_t sum[U][U];
+    constexpr bool kFine = U == 1;       // products with low parts in sums of their own, low by low among them (see multiply)
+    acc_t sum[U][U], fine = zero();
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -341,6 +352,10 @@ __global__ __launch_bounds__(kBlock, 2) void ortho_product_kernel(const ProductA
                     bl[u] = read8(q + kSizeB);
                 }
             }
+            if constexpr (kFine) {
+                multiply(ah[0], al[0], bh[0], bl[0], sum[0][0], fine);
+                continue;
+            }
 #pragma unroll
             for (int which = 0; which < 3; ++which)
 #pragma unroll
@@ -349,6 +364,7 @@ __global__ __launch_bounds__(kBlock, 2) void ortho_product_kernel(const ProductA
                     for (int w = 0; w < U; ++w) sum[u][w] = mfma(which == 2 ? bl[w] : bh[w], which == 1 ? al[u] : ah[u], sum[u][w]);
         }
     }
+    if constexpr (kFine) sum[0][0] += fine;
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -433,7 +449,7 @@ int product(const ProductArgs &p, int mp, int np, int batch, hipStream_t st) {
 
 // ---------------------------------------------------------------- matrices of at most 64 x 128
 // One workgroup does everything in one launch: X in registers (fp32, as the tiles of the last product come out), its two parts and those of A and
-// B in LDS.  Bound by the chain of products (four barriers a step): 64 x 64, five steps 16.5 us; by the kernels above 262.
+// B in LDS.  Bound by the chain of products (four barriers a step): 64 x 64, five steps 18 us; by the kernels above 262.
 struct SmallArgs {
     const void *g;
     void       *out;
@@ -490,15 +506,13 @@ __global__ __launch_bounds__(kBlock) void ortho_small_kernel(const SmallArgs a)
                 keep4(X[0], X[1], i * kRowX + jw + 64 * k + 8 * q + 4 * half, v);
             }
         __syncthreads();
-        acc_t s = zero();                // A: rows i, columns jw ..
+        acc_t s = zero(), f = zero();    // A: rows i, columns jw ..
 #pragma unroll
         for (int k = 0; k < NP / 16; ++k) {
             const int pi = i * kRowX + 16 * k + 8 * half, pj = (jw + col) * kRowX + 16 * k + 8 * half;
-            const half8_t ah = read8(X[0] + pi), al = read8(X[1] + pi), bh = read8(X[0] + pj), bl = read8(X[1] + pj);
-            s = mfma(bh, ah, s);
-            s = mfma(bh, al, s);
-            s = mfma(bl, ah, s);
+            multiply(read8(X[0] + pi), read8(X[1] + pi), read8(X[0] + pj), read8(X[1] + pj), s, f);
         }
+        s += f;
         float y[16];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
@@ -509,14 +523,13 @@ __global__ __launch_bounds__(kBlock) void ortho_small_kernel(const SmallArgs a)
         }
         __syncthreads();
         s = zero();
+        f = zero();
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const int pi = i * kRowA + 16 * k + 8 * half, pj = (jw + col) * kRowA + 16 * k + 8 * half;
-            const half8_t ah = read8(A[0] + pi), al = read8(A[1] + pi), bh = read8(A[0] + pj), bl = read8(A[1] + pj);
-            s = mfma(bh, ah, s);
-            s = mfma(bh, al, s);
-            s = mfma(bl, ah, s);
+            multiply(read8(A[0] + pi), read8(A[1] + pi), read8(A[0] + pj), read8(A[1] + pj), s, f);
         }
+        s += f;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             float v[4];
@@ -528,15 +541,13 @@ __global__ __launch_bounds__(kBlock) void ortho_small_kernel(const SmallArgs a)
 #pragma unroll
         for (int k = 0; k < kTiles; ++k) {
             s = zero();
+            f = zero();
 #pragma unroll
             for (int d = 0; d < 4; ++d) {
                 const int pi = i * kRowA + 16 * d + 8 * half;
-                const half8_t ah = read8(B[0] + pi), al = read8(B[1] + pi);
-                const half8_t bh = read_column(X[0], kRowX, 16 * d, jw + 64 * k, lane), bl = read_column(X[1], kRowX, 16 * d, jw + 64 * k, lane);
-                s = mfma(bh, ah, s);
-                s = mfma(bh, al, s);
-                s = mfma(bl, ah, s);
+                multiply(read8(B[0] + pi), read8(B[1] + pi), read_column(X[0], kRowX, 16 * d, jw + 64 * k, lane), read_column(X[1], kRowX, 16 * d, jw + 64 * k, lane), s, f);
             }
+            s += f;
 #pragma unroll
             for (int r = 0; r < 16; ++r) x[k][r] = fmaf(a.a, x[k][r], s[r] * (1.0f / (kScaleB * kScaleX)));
         }

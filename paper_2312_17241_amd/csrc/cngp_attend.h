@@ -24,7 +24,7 @@ struct WalkArgs {
     float       *final;                  // ... behind the last one, or NULL
     float       *anchors;                // states at the chunks' starts but a sequence's first, as they lie in registers: a forward walk leaves them there, a
                                          // reverse one takes products of its states with them; or NULL
-    const float *met;                    // (with anchors) states as `first` of whole sequences, for the product behind a sequence's last row of the walk; or NULL
+    const float *met;                    // (with anchors, first_i 1) states as `first` of whole sequences, for the product behind a sequence's last row of the walk; or NULL
     double      *products;               // (with anchors) <state, anchor>, a part from each wavefront: reverse [chunk_number, heads, waves], forward (met alone) [S, heads, waves]
     const void  *x;                      // rows [N, heads / x_div, vdim] to take products of the outputs with, or NULL
     float       *dot;                    // [heads, N]: x_t . out_t, the row's own part left out

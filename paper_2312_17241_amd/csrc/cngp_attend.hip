@@ -331,6 +331,13 @@ struct Call {
         a.out_f32 = f32 || c->io_dtype == CNGP_F32;
         a.whole = a.whole && a.vdim % 4 == 0 && ((uintptr_t)out & (a.out_f32 ? 15u : 7u)) == 0;
     }
+    // for the decays' gradient: states left or met with on the way, and at the end
+    void meet(WalkArgs &a, const float *met, size_t products) const {
+        a.anchors = (float *)(ws + sp.anchors);
+        a.met = met;
+        a.products = (double *)(ws + products);
+        a.whole = a.whole && ((uintptr_t)met & 15u) == 0;
+    }
     int walk(const WalkArgs &a, bool states_only) const {
         return c->io_dtype == CNGP_F16 ? attend_walk_f16(a, states_only, s) : attend_walk_f32(a, states_only, s);
     }
@@ -462,7 +469,7 @@ int cngp_attend_bwd(const cngp_attend_config *cfg, const void *q, const void *k,
     if (ddecay) {
         a.x = q; a.x_div = 1; a.whole = a.whole && whole_rows(q, K, cfg->io_dtype, cfg->io_dtype == CNGP_F16 ? 8 : 16);
         a.dot = (float *)(ws + sp.dot_q);
-        a.anchors = (float *)(ws + sp.anchors); a.met = dlast; a.products = (double *)(ws + sp.ends);
+        call.meet(a, dlast, sp.ends);
     }
     if (N)
         if (int rc = call.walk(a, false)) return rc;
@@ -493,7 +500,7 @@ int cngp_attend_bwd(const cngp_attend_config *cfg, const void *q, const void *k,
     if (ddecay) {
         a.x = k; a.x_div = group; a.whole = a.whole && whole_rows(k, K, cfg->io_dtype, cfg->io_dtype == CNGP_F16 ? 8 : 16);
         a.dot = (float *)(ws + sp.dot_k);
-        a.anchors = (float *)(ws + sp.anchors); a.met = h0; a.products = (double *)(ws + sp.starts);
+        call.meet(a, h0, sp.starts);
     }
     if (int rc = call.walk(a, false)) return rc;
 

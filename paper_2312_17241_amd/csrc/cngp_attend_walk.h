@@ -300,31 +300,33 @@ __global__ __launch_bounds__(walk_threads(KW, VW), walk_per_simd(sizeof(T), KW))
         const float   *from = an_anchor ? anchor_of(number) : a.met + (size_t)seq * a.kdim * a.vdim * a.heads + (size_t)h * a.kdim * a.vdim;
         const float    f = power_of_two(-up);
         const int      left = anew(a.kdim - 32 * KP * kh - 4 * half);
-        const int      by = __builtin_amdgcn_readfirstlane(anew(a.first_i));
-        uint32_t       at = (uint32_t)anew((32 * KP * kh + 4 * half) * by + j * a.first_j);
+        const float   *mine = an_anchor ? from : from + anew(32 * KP * kh + 4 * half + j * a.first_j);      // (such a walk's states have rows side by side)
         double sum = 0.0;
         apart();
+        float4_t o[KP][KR / 4];
 #pragma unroll
-        for (int kt = 0; kt < KP; ++kt) {
+        for (int kt = 0; kt < KP; ++kt)
 #pragma unroll
-            for (int g = 0; g < KR / 4; ++g, at += (uint32_t)by * 8) {
+            for (int g = 0; g < KR / 4; ++g) {
                 const int i = 32 * kt + 8 * g;
-                float4_t  o = {0.0f, 0.0f, 0.0f, 0.0f};
-                if (mine_v && i < left) {
-                    if (an_anchor) o = *reinterpret_cast<const float4_t *>(from + (kt * 4 + g) * 256);
-                    else
+                o[kt][g] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+                if (!mine_v || i >= left) continue;
+                if (an_anchor) o[kt][g] = *reinterpret_cast<const float4_t *>(mine + (kt * 4 + g) * 256);
+                else if (WHOLE) o[kt][g] = *reinterpret_cast<const float4_t *>(mine + i);
+                else
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (i + e < left) o[e] = from[at + (uint32_t)(e * by)];
-                    float t = 0.0f;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) t = fmaf(S[kt][4 * g + e] * f, o[e], t);
-                    sum += (double)t;
-                }
+                    for (int e = 0; e < 4; ++e)
+                        if (i + e < left) o[kt][g][e] = mine[i + e];
             }
-            apart();
-            if (KR < 16) at += (uint32_t)by * 16;
-        }
+#pragma unroll
+        for (int kt = 0; kt < KP; ++kt)
+#pragma unroll
+            for (int g = 0; g < KR / 4; ++g) {
+                float t = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) t = fmaf(S[kt][4 * g + e] * f, o[kt][g][e], t);
+                if (mine_v && 32 * kt + 8 * g < left) sum += (double)t;
+            }
         sum = sum_upto(sum);
         if (lane == 63) to[wave] = sum;
     };

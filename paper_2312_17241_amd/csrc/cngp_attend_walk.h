@@ -10,9 +10,9 @@
 // Precision: rounding what is computed (scores, state, decayed v) to fp16 would cost half of the result's accuracy.  It is split in two fp16
 // numbers (22 bits) after a power of two has brought its largest value to 2^13, and takes two products.  fp16 storage: q, k, v are
 // exact operands.  fp32 storage: they are split as well, each row by a power of two of its own, and products take three (the fp32 products of
-// the matrix cores have a sixteenth of the rate: 4096 rays of 64 samples, 4 heads of 16, a walk 526 us, so 102).
+// the matrix cores have a sixteenth of the rate: 4096 rays of 64 samples, 4 heads of 16, a walk 526 us, so 104).
 // Bound by the chain inside a chunk: two barriers or three, between them vector instructions (38 % of the cycles), LDS (28) and matrix instructions (17)
-// that one or two workgroups to a CU do not lay over each other.  2^15 rows, 16 heads of 128 x 128, fp16: 242 us, 1.4 TB/s.
+// that one or two workgroups to a CU do not lay over each other.  2^15 rows, 16 heads of 128 x 128, fp16: 250 us (233 to 264), 1.4 TB/s.
 #pragma once
 #include "cngp_attend.h"
 #include "cngp_matrix.h"

@@ -4,8 +4,8 @@
 //
 // One group of lanes takes a row and some of its heads; a lane holds the same components of every head, so the row's angles are formed
 // once for all of them: the product in 64 bits, whole turns taken off there, sine and cosine of what is left in fp32.  Bound by memory: x is
-// read and y written once, in 16-byte pieces where rows allow (2^15 rows, 20 heads of 128, fp16: 88 us forward, 3.8 TB/s, 120 backward with the gains',
-// 4.2; 2^18 rows, 5 heads of 36, fp32, no norms: 80, 4.7).
+// read and y written once, in 16-byte pieces where rows allow (2^15 rows, 20 heads of 128, fp16: 86 us forward, 3.9 TB/s, 131 backward with the gains',
+// 3.8; 2^18 rows, 5 heads of 36, fp32, no norms: 80, 4.7).
 #include <algorithm>
 #include <cmath>
 
